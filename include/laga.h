@@ -56,6 +56,7 @@ extern "C" {
 #define LAGA_ERR_DEVICE_TIMEOUT (-5)      /* only from laga_query_status: a bounded device wait ran out */
 #define LAGA_ERR_DEVICE_CHECK (-6)        /* only from laga_query_status: a device-side self-check failed
                                              (the kernel recorded where, skipped the access and returned)   */
+#define LAGA_ERR_CACHE_PLAN (-7)          /* only from laga_query_status: laga_cache_plan could not place the step */
 
 #define LAGA_FLAG_ACCUM_DW 1u             /* laga_bwd: add into dw_kv_b instead of overwriting it   */
 #define LAGA_FLAG_DETERMINISTIC 2u        /* laga_bwd: bitwise-repeatable dk_pe and dw_kv_b (see there) */
@@ -198,6 +199,95 @@ int laga_layernorm_backward(const void* dy, const void* x, const void* gamma, co
                             int D, void* dx, float* dgamma, float* dbeta, void* stream);
 
 /*
+ * Rotary positions (the path itself takes q_rope and k_pe already rotated; this is what rotates them).
+ *
+ *   y[m, i, :] = x[m, i, :] with channels [rot_begin, rot_begin + d_rot) of every head rotated:
+ *   (a, b) -> mscale * (a cos - b sin, b cos + a sin),   angle = positions[m] * freqs[j],   j = 0 .. d_rot/2 - 1
+ *   x, y bf16 [M, h, d], heads dense, rows x_pitch / y_pitch elements apart (at least h*d, multiples of 8); y may be x
+ *   itself (same pitch: only the rotated channels are touched) but not overlap it otherwise
+ *   positions int32 [M], any value, repeats allowed;   freqs fp64 [d_rot/2], radians per position
+ *   layout: which channels pair up, LAGA_ROPE_INTERLEAVED (2j, 2j+1) or LAGA_ROPE_HALF (j, j + d_rot/2)
+ *   inverse != 0: rotates back (times mscale, not divided by it): the transpose, i.e. the gradient of the forward call
+ * Angles are formed in fp64 (positions of millions stay exact); long-context scalings are choices of freqs and mscale.
+ * d: a multiple of 8, at most 1024; d_rot: a multiple of 16, at most 256; rot_begin: a multiple of 8.
+ * No status word: errors are launch errors.
+ */
+#define LAGA_ROPE_HALF 0
+#define LAGA_ROPE_INTERLEAVED 1
+int laga_rope(const void* x, long long x_pitch, const int* positions, const double* freqs, int M, int h, int d,
+              int rot_begin, int d_rot, int layout, float mscale, int inverse, void* y, long long y_pitch, void* stream);
+
+/*
+ * Between W_kv_a and the attention (Algorithm 1 step 1), one pass: LayerNorm of the latent and rotation of the shared key.
+ *   kv_a  bf16 [M, D + R], rows kv_a_pitch elements apart: what W_kv_a delivers, latent then key
+ *   latent bf16 [M, D] = LayerNorm(kv_a[:, :D]) as laga_layernorm has it;  k_pe bf16 [M, R] = kv_a[:, D:] rotated as
+ *   laga_rope has it;  mean, rstd fp32 [M] (either may be NULL; the backward needs both)
+ *   cache, slots: if not NULL, row slots[m] of the cache, bf16 [n_slots, D + R], receives latent and key side by side; a slot
+ *   outside [0, n_slots) writes nothing (padding rows of a batch).  Two rows of one call must not name the same slot.
+ * latent and k_pe may both be NULL when cache is not (serving: the token only enters the cache).  The rows of the
+ * cache that no slot names are left as they are.  Outputs must not overlap inputs or one another.
+ *
+ * laga_latent_norm_rope_backward: dkv_a bf16 [M, D + R] written; dgamma fp32 [D] and, if not NULL, dbeta fp32 [D]
+ * overwritten.  Row sums are formed per block in `workspace` (16-byte aligned, sized by the query) and added in a
+ * fixed order: the call repeats bit for bit.
+ * D: a multiple of 8, at most 1024; R: a multiple of 16, at most 256; kv_a_pitch: a multiple of 8.
+ */
+int laga_latent_norm_rope(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps,
+                          const int* positions, const double* freqs, int M, int D, int R, int layout, float mscale,
+                          void* latent, void* k_pe, float* mean, float* rstd, void* cache, const int* slots, int n_slots,
+                          void* stream);
+size_t laga_latent_norm_rope_backward_workspace_bytes(int M, int D);
+int laga_latent_norm_rope_backward(const void* dlatent, const void* dk_pe, const void* kv_a, long long kv_a_pitch,
+                                   const void* gamma, const float* mean, const float* rstd, const int* positions,
+                                   const double* freqs, int M, int D, int R, int layout, float mscale, void* dkv_a,
+                                   float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Page tables and slot maps of a paged latent cache, for one step of n_requests requests, on the GPU.
+ *   seq_lens int32 [n]   tokens each request has in the cache;  new_lens int32 [n]  tokens it adds in this step (0 allowed)
+ *   block_table int32 [n, columns]   page numbers; columns [0, ceil(seq_len / page_size)) of a row are read, the columns the
+ *                        new tokens need are written, the others left as they are
+ *   free_pages int32 [free_capacity], n_free int32 [1]   stack of free pages, top at index n_free - 1; pages come off the
+ *                        top request by request (the array itself is not written)
+ *   slots, positions int32 [max_tokens]   for every new token, requests in order: its row in the cache (page * page_size +
+ *                        offset) and its position in its request; -1 and 0 in the rows behind the last token
+ *   cu_new_lens int32 [n + 1], seq_lens_out int32 [n], n_free_out int32 [1]   prefix sums of new_lens and the new state
+ * A step that cannot be placed (a negative length, too few free pages, columns or rows) takes nothing: the tables stay, the
+ * state is handed back as it was, every slot is -1, cu_new_lens is zero, and laga_query_status(status_word) returns
+ * LAGA_ERR_CACHE_PLAN (detail 0x5000000x: 1 bad length or n_free, 2 pages, 3 columns, 4 rows).
+ * page_size: a power of two from 16 to 1024; n_requests <= 8192; columns * page_size <= 2^30.  No output may overlap an
+ * input or another output (LAGA_ERR_INVALID_ARG).  Pages in the table are not checked here; rows they would place
+ * outside 31 bits get slot -1.
+ */
+int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, int page_size, int* block_table, int columns,
+                    const int* free_pages, int free_capacity, const int* n_free, int max_tokens, int* slots, int* positions,
+                    int* cu_new_lens, int* seq_lens_out, int* n_free_out, void* status_word, void* stream);
+
+/*
+ * Attention of one new token per request over the paged latent cache (absorbed form; what laga_fwd gives for the last
+ * row of each request's sequence).
+ *   q            bf16 [B, h, d_nope+d_rope]   the new tokens' queries, rope band rotated
+ *   w_kv_b       bf16 [d_c, h*(d_nope+d_v)]   as in laga_fwd
+ *   cache        bf16 [n_pages, page_size, d_c+d_rope]   latent and rotated key of a token side by side
+ *   block_table  int32 [B, columns], seq_lens int32 [B]   on the device; seq_lens counts the tokens to attend to (the new
+ *                token included, once it has been appended); token t of request b is row t % page_size of page
+ *                block_table[b, t / page_size].  Requests may share pages.  Table entries behind a request's last page and cache
+ *                rows behind its last token are not used, whatever they hold.
+ *   out          bf16 [B, h, d_v] written; a request of length 0 gets zeros
+ *   lse          fp32 [B, h] written if not NULL (-inf for length 0)
+ * A length outside [0, columns * page_size] is clamped, and a page number outside [0, n_pages) reads as zeros; both report
+ * LAGA_ERR_DEVICE_CHECK through laga_query_status(workspace).  page_size: a power of two from 16 to 1024; n_pages * page_size
+ * and columns * page_size at most 2^30.  d_c, d_nope, d_rope, d_v: 512, 128, 64, 128.  flags must be 0.
+ * q W_uk is rounded to bf16 for the tensor cores, like the probabilities; sums, maxima and the accumulator are fp32.
+ * Nothing depends on lengths at enqueue time: the call can be captured in a graph and replayed with new lengths.
+ */
+size_t laga_paged_decode_workspace_bytes(int B, int h, int d_c, int d_nope, int d_rope, int d_v);
+int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int n_pages, int page_size,
+                      const int* block_table, int columns, const int* seq_lens, int B, int h, int d_c, int d_nope, int d_rope,
+                      int d_v, float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                      unsigned flags, void* stream);
+
+/*
  * Step entry points (the same kernels laga_fwd / laga_bwd launch, callable on their own).
  *
  * laga_up_project: Algorithm 1 step 4.   kv bf16 [S, h*(d_nope+d_v)] = c_kv . w_kv_b  (fp32 accumulate).
@@ -297,7 +387,8 @@ int laga_selftest_bounded_wait(void* status_word, unsigned budget_us, void* stre
 #define LAGA_KERNEL_V_PROJECT 10    /* absorbed form: out = W_uv o_lat (batched over heads)      */
 #define LAGA_KERNEL_ATTN_BWD_FUSED 11 /* backward attention in one pass on CTA pairs: dK, dV, dQ sums */
 #define LAGA_KERNEL_DQ_CONVERT 12   /* dQ: scale and bf16 rounding of the fp32 sums              */
-#define LAGA_KERNEL_COUNT 13
+#define LAGA_KERNEL_ATTN_DECODE 13  /* laga_paged_decode: attention over the paged latent cache       */
+#define LAGA_KERNEL_COUNT 14
 int laga_profile_kernel(int kernel_id, void* const* start_events, void* const* stop_events, int n_pairs);
 
 /*

@@ -15,9 +15,12 @@
 #include "attn_absorbed_sm100.cuh"
 #include "attn_bwd_fused_sm100.cuh"
 #include "attn_bwd_sm100.cuh"
+#include "attn_decode_sm100.cuh"
 #include "attn_fwd_sm100.cuh"
+#include "cache_plan_sm100.cuh"
 #include "gemm_sm100.cuh"
 #include "layernorm_sm100.cuh"
+#include "rope_sm100.cuh"
 
 namespace {
 
@@ -131,7 +134,11 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_bwd_dq_sm100_kernel<true>, AttnBwdDqSmem::kTotalBytes) &&
               allow_smem(attn_bwd_dq_sm100_kernel<false>, AttnBwdDqSmem::kTotalBytes) &&
               allow_smem(attn_bwd_fused_sm100_kernel<true>, AttnBwdFusedSmem::kTotalBytes) &&
-              allow_smem(attn_bwd_fused_sm100_kernel<false>, AttnBwdFusedSmem::kTotalBytes);
+              allow_smem(attn_bwd_fused_sm100_kernel<false>, AttnBwdFusedSmem::kTotalBytes) &&
+              allow_smem(attn_decode_sm100_kernel<16>, AttnDecodeSmem<16>::kTotalBytes) &&
+              allow_smem(attn_decode_sm100_kernel<32>, AttnDecodeSmem<32>::kTotalBytes) &&
+              allow_smem(attn_decode_sm100_kernel<64>, AttnDecodeSmem<64>::kTotalBytes) &&
+              allow_smem(cache_plan_kernel, 2 * (kPlanMaxRequests + 1) * static_cast<int>(sizeof(int)));
     if (ok) {
         // The fused backward assigns work to pairs statically, so its grid must not exceed the pairs the
         // device keeps resident at once (SMs that cannot form a pair inside their GPC stay idle).
@@ -684,6 +691,53 @@ int launch_attn_absorbed(const void* q, const void* q_abs, const void* c_kv, con
     return launch_status();
 }
 
+// ---- one new token per request over a paged latent cache ---------------------------------------------
+int page_shift_of(int page) {                        // log2 of a supported page size, else -1
+    for (int s = 4; s <= 10; ++s)
+        if (page == 1 << s) return s;
+    return -1;
+}
+
+struct DecodeLayout {
+    int heads, n_groups, ctas_per_group, h_pad, slots;
+    size_t q_abs, o_lat, part_o, part_ml, tile_start, total;
+};
+DecodeLayout decode_layout(int B, int h) {
+    DecodeLayout w;
+    // heads per CTA: the smallest variant that takes them all (a score tile costs the same with any of them, the
+    // value product and the queries' shared memory grow), else groups of 64
+    w.heads = h <= 16 ? 16 : h <= 32 ? 32 : 64;
+    w.n_groups = (h + w.heads - 1) / w.heads;
+    w.ctas_per_group = kDecMaxCtas / w.n_groups > 0 ? kDecMaxCtas / w.n_groups : 1;
+    w.h_pad = w.n_groups * w.heads;
+    w.slots = w.ctas_per_group + B;
+    const size_t lat_bytes = align_up(static_cast<size_t>(B) * h * kDc * 2, 1024);
+    const size_t rows = static_cast<size_t>(w.slots) * w.h_pad;
+    w.q_abs = kStatusBytes;
+    w.o_lat = w.q_abs + lat_bytes;
+    w.part_o = w.o_lat + lat_bytes;
+    w.part_ml = w.part_o + rows * kDecLat * sizeof(float);
+    w.tile_start = w.part_ml + align_up(rows * sizeof(float2), 1024);
+    w.total = w.tile_start + align_up((static_cast<size_t>(B) + 1) * sizeof(int), 1024);
+    return w;
+}
+
+template <int kHeads>
+int launch_attn_decode(const void* q, const void* q_abs, const void* cache, long long cache_rows, const AttnDecodeArgs& a,
+                       cudaStream_t stream) {
+    const uint64_t q_rows = static_cast<uint64_t>(a.B) * a.h;
+    const int box = a.page_shift < 6 ? 1 << a.page_shift : kDecKeys;
+    CUtensorMap tqa, tq, tc;
+    if (!cached_tmap_bf16(&tqa, q_abs, kDc, q_rows, kDc * 2, kHeads) ||
+        !cached_tmap_bf16(&tq, q, kDn + kDr, q_rows, (kDn + kDr) * 2, kHeads) ||
+        !cached_tmap_bf16(&tc, cache, kDecRow, static_cast<uint64_t>(cache_rows), kDecRow * 2, static_cast<uint32_t>(box)))
+        return LAGA_ERR_CUDA;
+    ScopedKernelEvents ev(LAGA_KERNEL_ATTN_DECODE, stream);
+    launch_kernel(attn_decode_sm100_kernel<kHeads>, dim3(static_cast<unsigned>(a.n_groups * a.ctas_per_group)), dim3(kDecThreads),
+                  AttnDecodeSmem<kHeads>::kTotalBytes, stream, true, tqa, tq, tc, a);
+    return launch_status();
+}
+
 // Self-test of the bounded-wait machinery every kernel here relies on: two warps wait on an mbarrier
 // that nothing will ever arrive on.  After `budget_ns` the first waiter records the site in the status
 // word and raises the abort flag, the other waiter sees the flag, and the CTA exits normally.
@@ -713,7 +767,7 @@ int zero_status_word(void* status_word, cudaStream_t stream) {
 
 extern "C" {
 
-int laga_version(void) { return 211; }
+int laga_version(void) { return 300; }
 
 const char* laga_status_string(int status) {
     switch (status) {
@@ -724,6 +778,7 @@ const char* laga_status_string(int status) {
         case LAGA_ERR_CUDA: return "LAGA_ERR_CUDA";
         case LAGA_ERR_DEVICE_TIMEOUT: return "LAGA_ERR_DEVICE_TIMEOUT";
         case LAGA_ERR_DEVICE_CHECK: return "LAGA_ERR_DEVICE_CHECK";
+        case LAGA_ERR_CACHE_PLAN: return "LAGA_ERR_CACHE_PLAN";
         default: return "LAGA_ERR_UNKNOWN";
     }
 }
@@ -1146,7 +1201,211 @@ int laga_query_status(const void* workspace, void* stream, unsigned* detail) {
     if (word == 0) return LAGA_OK;
     if ((word & 0xff000000u) == kStatusTimeout) return LAGA_ERR_DEVICE_TIMEOUT;
     if ((word & 0xff000000u) == kStatusCheck) return LAGA_ERR_DEVICE_CHECK;
+    if ((word & 0xff000000u) == kStatusCachePlan) return LAGA_ERR_CACHE_PLAN;
     return LAGA_ERR_CUDA;
+}
+
+// ---- rotary positions, latent norm + key rotation --------------------------------------------------
+static bool rotary_ok(const int* positions, const double* freqs, int d_rot, float mscale, int layout) {
+    return positions && freqs && d_rot >= 16 && d_rot <= kRopeMaxRot && d_rot % 16 == 0 && mscale == mscale &&
+           (layout == LAGA_ROPE_INTERLEAVED || layout == LAGA_ROPE_HALF) && (reinterpret_cast<uintptr_t>(positions) & 3u) == 0 &&
+           (reinterpret_cast<uintptr_t>(freqs) & 7u) == 0;
+}
+
+// [a, a + a_bytes) and [b, b + b_bytes) share a byte
+static bool overlap_bytes(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
+int laga_rope(const void* x, long long x_pitch, const int* positions, const double* freqs, int M, int h, int d, int rot_begin,
+              int d_rot, int layout, float mscale, int inverse, void* y, long long y_pitch, void* stream) {
+    if (!x || !y || M < 1 || h < 1 || d < 16 || d > kRopeMaxD || (d & 7) || rot_begin < 0 || (rot_begin & 7) ||
+        !rotary_ok(positions, freqs, d_rot, mscale, layout) || rot_begin > d - d_rot)
+        return LAGA_ERR_INVALID_ARG;
+    const long long width = static_cast<long long>(h) * d;
+    if (width > (1ll << 30) || x_pitch < width || y_pitch < width || (x_pitch & 7) || (y_pitch & 7)) return LAGA_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(y)) return LAGA_ERR_INVALID_ARG;
+    const bool in_place = x == y;
+    if (in_place ? x_pitch != y_pitch
+                 : overlap_bytes(x, ((M - 1) * static_cast<size_t>(x_pitch) + width) * 2, y, ((M - 1) * static_cast<size_t>(y_pitch) + width) * 2))
+        return LAGA_ERR_INVALID_ARG;
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    if ((rc = check_pointers({x, y, positions, freqs})) != LAGA_OK) return rc;
+    const bool interleaved = layout == LAGA_ROPE_INTERLEAVED;
+    const int units = (interleaved ? d_rot / 8 : d_rot / 16) + (in_place ? 0 : (d - d_rot) / 8);
+    // about 256 threads; in half layout two chunks a thread, and as many fewer threads (the table of the block's tokens then
+    // stays within 32 KB whatever the widths are)
+    const int chunks = (in_place ? d_rot : d) / 8;
+    const dim3 block(units, 256 / chunks);
+    const long long rows = static_cast<long long>(M) * h, per_block = static_cast<long long>(block.y) * kRopeRowsPerThread;
+    const long long blocks = (rows + per_block - 1) / per_block;
+    if (blocks > 0x7fffffffll) return LAGA_ERR_INVALID_ARG;
+    const long long tokens = h == 1 ? per_block : (per_block + h - 2) / h + 1;        // most tokens a block's rows can touch
+    const size_t smem = static_cast<size_t>(tokens < M ? tokens : M) * (d_rot / 2) * sizeof(float2);
+    const Rotary rot{positions, freqs, mscale, interleaved ? 1 : 0, inverse != 0 ? 1 : 0};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    auto xs = static_cast<const __nv_bfloat16*>(x);
+    auto ys = static_cast<__nv_bfloat16*>(y);
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (interleaved) rope_kernel<true><<<grid, block, smem, st>>>(xs, x_pitch, ys, y_pitch, M, h, d, rot_begin, d_rot, in_place, rot);
+    else rope_kernel<false><<<grid, block, smem, st>>>(xs, x_pitch, ys, y_pitch, M, h, d, rot_begin, d_rot, in_place, rot);
+    return launch_status();
+}
+
+int laga_latent_norm_rope(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps,
+                          const int* positions, const double* freqs, int M, int D, int R, int layout, float mscale, void* latent,
+                          void* k_pe, float* mean, float* rstd, void* cache, const int* slots, int n_slots, void* stream) {
+    if (!kv_a || !gamma || M < 1 || D < 8 || (D & 7) || D > kLnMaxD || !(eps >= 0.f) ||
+        !rotary_ok(positions, freqs, R, mscale, layout))
+        return LAGA_ERR_INVALID_ARG;
+    if (kv_a_pitch < D + R || (kv_a_pitch & 7) || !latent != !k_pe || !cache != !slots || (!latent && !cache) || (cache && n_slots < 1))
+        return LAGA_ERR_INVALID_ARG;
+    if (!aligned16(kv_a) || !aligned16(gamma) || !aligned16(beta) || !aligned16(latent) || !aligned16(k_pe) || !aligned16(cache) ||
+        (reinterpret_cast<uintptr_t>(slots) & 3u) || (reinterpret_cast<uintptr_t>(mean) & 3u) || (reinterpret_cast<uintptr_t>(rstd) & 3u))
+        return LAGA_ERR_INVALID_ARG;
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    if ((rc = check_pointers({kv_a, gamma, positions, freqs})) != LAGA_OK) return rc;
+    for (const void* p : {beta, static_cast<const void*>(latent), static_cast<const void*>(k_pe), static_cast<const void*>(mean),
+                          static_cast<const void*>(rstd), static_cast<const void*>(cache), static_cast<const void*>(slots)})
+        if (p && (rc = check_pointers({p})) != LAGA_OK) return rc;
+    auto bf = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
+    const LatentNormRopeArgs a{bf(kv_a), kv_a_pitch, bf(gamma), bf(beta), M, D, R, eps,
+                               Rotary{positions, freqs, mscale, layout == LAGA_ROPE_INTERLEAVED ? 1 : 0, 0},
+                               static_cast<__nv_bfloat16*>(latent), static_cast<__nv_bfloat16*>(k_pe), mean, rstd,
+                               static_cast<__nv_bfloat16*>(cache), slots, n_slots};
+    const int blocks_needed = (M + kLnWarps - 1) / kLnWarps, cap = sm_count() * 4;
+    const dim3 grid(blocks_needed < cap ? blocks_needed : cap), block(kLnWarps * 32);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (D <= 256) latent_norm_rope_fwd_kernel<1><<<grid, block, 0, st>>>(a);
+    else if (D <= 512) latent_norm_rope_fwd_kernel<2><<<grid, block, 0, st>>>(a);
+    else latent_norm_rope_fwd_kernel<4><<<grid, block, 0, st>>>(a);
+    return launch_status();
+}
+
+// blocks of the backward: one resident wave striding over the rows; each leaves one row of 2 D partial sums
+static int latent_norm_bwd_blocks(int M) {
+    const int needed = (M + kLnWarps - 1) / kLnWarps;
+    return needed < 296 ? needed : 296;
+}
+
+size_t laga_latent_norm_rope_backward_workspace_bytes(int M, int D) {
+    if (M < 1 || D < 8 || (D & 7) || D > kLnMaxD) return 0;
+    return align_up(static_cast<size_t>(latent_norm_bwd_blocks(M)) * 2 * D * sizeof(float), 1024);
+}
+
+int laga_latent_norm_rope_backward(const void* dlatent, const void* dk_pe, const void* kv_a, long long kv_a_pitch, const void* gamma,
+                                   const float* mean, const float* rstd, const int* positions, const double* freqs, int M, int D,
+                                   int R, int layout, float mscale, void* dkv_a, float* dgamma, float* dbeta, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    if (!dlatent || !dk_pe || !kv_a || !gamma || !mean || !rstd || !dkv_a || !dgamma || !workspace || M < 1 || D < 8 || (D & 7) ||
+        D > kLnMaxD || !rotary_ok(positions, freqs, R, mscale, layout) || kv_a_pitch < D + R || (kv_a_pitch & 7))
+        return LAGA_ERR_INVALID_ARG;
+    if (!aligned16(dlatent) || !aligned16(dk_pe) || !aligned16(kv_a) || !aligned16(gamma) || !aligned16(dkv_a) || !aligned16(workspace) ||
+        (reinterpret_cast<uintptr_t>(mean) & 3u) || (reinterpret_cast<uintptr_t>(rstd) & 3u) ||
+        (reinterpret_cast<uintptr_t>(dgamma) & 3u) || (reinterpret_cast<uintptr_t>(dbeta) & 3u))
+        return LAGA_ERR_INVALID_ARG;
+    if (workspace_bytes < laga_latent_norm_rope_backward_workspace_bytes(M, D)) return LAGA_ERR_WORKSPACE_TOO_SMALL;
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    if ((rc = check_pointers({dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, freqs, dkv_a, dgamma, workspace})) != LAGA_OK) return rc;
+    if (dbeta && (rc = check_pointers({dbeta})) != LAGA_OK) return rc;
+    auto bf = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
+    const LatentNormRopeBwdArgs a{bf(dlatent), bf(dk_pe), bf(kv_a), kv_a_pitch, bf(gamma), mean, rstd, M, D, R,
+                                  Rotary{positions, freqs, mscale, layout == LAGA_ROPE_INTERLEAVED ? 1 : 0, 1},
+                                  static_cast<__nv_bfloat16*>(dkv_a), static_cast<float*>(workspace)};
+    const int blocks = latent_norm_bwd_blocks(M);
+    const dim3 grid(blocks), block(kLnWarps * 32);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (D <= 256) latent_norm_rope_bwd_kernel<1><<<grid, block, 0, st>>>(a);
+    else if (D <= 512) latent_norm_rope_bwd_kernel<2><<<grid, block, 0, st>>>(a);
+    else latent_norm_rope_bwd_kernel<4><<<grid, block, 0, st>>>(a);
+    if ((rc = launch_status()) != LAGA_OK) return rc;
+    launch_kernel(latent_norm_sums_kernel, dim3((2 * D + 31) / 32), dim3(256), 0, st, true, static_cast<const float*>(workspace), blocks, D,
+                  dgamma, dbeta);
+    return launch_status();
+}
+
+// ---- the paged latent cache ------------------------------------------------------------------------
+int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, int page_size, int* block_table, int columns,
+                    const int* free_pages, int free_capacity, const int* n_free, int max_tokens, int* slots, int* positions,
+                    int* cu_new_lens, int* seq_lens_out, int* n_free_out, void* status_word, void* stream) {
+    const int shift = page_shift_of(page_size);
+    if (!seq_lens || !new_lens || !block_table || !free_pages || !n_free || !slots || !positions || !cu_new_lens || !seq_lens_out ||
+        !n_free_out || !status_word || n_requests < 1 || n_requests > kPlanMaxRequests || shift < 0 || columns < 1 || free_capacity < 1 ||
+        max_tokens < 1 || (static_cast<long long>(columns) << shift) > (1ll << 30))
+        return LAGA_ERR_INVALID_ARG;
+    // every block reads the state while block 0 writes the new one: the outputs must not be the inputs
+    const size_t n4 = static_cast<size_t>(n_requests) * 4;
+    const struct { const void* p; size_t bytes; } in[] = {{seq_lens, n4}, {new_lens, n4}, {free_pages, static_cast<size_t>(free_capacity) * 4},
+                                                          {n_free, 4}},
+        out[] = {{slots, static_cast<size_t>(max_tokens) * 4}, {positions, static_cast<size_t>(max_tokens) * 4}, {cu_new_lens, n4 + 4},
+                 {seq_lens_out, n4}, {n_free_out, 4}, {status_word, 4}, {block_table, n4 * columns}};
+    for (const auto& o : out) {
+        if (reinterpret_cast<uintptr_t>(o.p) & 3u) return LAGA_ERR_INVALID_ARG;
+        for (const auto& i : in)
+            if ((reinterpret_cast<uintptr_t>(i.p) & 3u) || overlap_bytes(i.p, i.bytes, o.p, o.bytes)) return LAGA_ERR_INVALID_ARG;
+        for (const auto& x : out)
+            if (&x != &o && overlap_bytes(x.p, x.bytes, o.p, o.bytes)) return LAGA_ERR_INVALID_ARG;
+    }
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    for (const auto& i : in) if ((rc = check_pointers({i.p})) != LAGA_OK) return rc;
+    for (const auto& o : out) if ((rc = check_pointers({o.p})) != LAGA_OK) return rc;
+    const CachePlanArgs a{seq_lens, new_lens, n_requests, shift, columns, block_table, free_pages, n_free, free_capacity, max_tokens, slots,
+                          positions, cu_new_lens, seq_lens_out, n_free_out, static_cast<unsigned*>(status_word)};
+    const int needed = (max_tokens + kPlanThreads - 1) / kPlanThreads, cap = sm_count();
+    const size_t smem = 2 * (static_cast<size_t>(n_requests) + 1) * sizeof(int);
+    cache_plan_kernel<<<needed < cap ? needed : cap, kPlanThreads, smem, static_cast<cudaStream_t>(stream)>>>(a);
+    return launch_status();
+}
+
+size_t laga_paged_decode_workspace_bytes(int B, int h, int d_c, int d_nope, int d_rope, int d_v) {
+    if (B < 1 || h < 1 || !geometry_is_v3(d_c, d_nope, d_rope, d_v)) return 0;
+    return decode_layout(B, h).total;
+}
+
+int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int n_pages, int page_size, const int* block_table,
+                      int columns, const int* seq_lens, int B, int h, int d_c, int d_nope, int d_rope, int d_v, float softmax_scale,
+                      void* out, float* lse, void* workspace, size_t workspace_bytes, unsigned flags, void* stream) {
+    const int shift = page_shift_of(page_size);
+    if (!q || !w_kv_b || !cache || !block_table || !seq_lens || !out || !workspace || B < 1 || h < 1 || n_pages < 1 || columns < 1 ||
+        shift < 0 || flags != 0 || !(softmax_scale > 0.f))
+        return LAGA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(w_kv_b) || !aligned16(cache) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) ||
+        (reinterpret_cast<uintptr_t>(block_table) & 3u) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u) ||
+        (reinterpret_cast<uintptr_t>(workspace) & 1023u))
+        return LAGA_ERR_INVALID_ARG;
+    if (!geometry_is_v3(d_c, d_nope, d_rope, d_v)) return LAGA_ERR_UNSUPPORTED;
+    // rows, keys and tiles are counted in 32 bits (byte offsets are not)
+    const long long rows = static_cast<long long>(n_pages) << shift, capacity = static_cast<long long>(columns) << shift;
+    if (rows > (1ll << 30) || capacity > (1ll << 30) || ((capacity + kDecKeys - 1) / kDecKeys) * B > 0x7fffffffll ||
+        static_cast<long long>(B) * h > (1ll << 26))
+        return LAGA_ERR_INVALID_ARG;
+    const DecodeLayout w = decode_layout(B, h);
+    if (workspace_bytes < w.total) return LAGA_ERR_WORKSPACE_TOO_SMALL;
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    if ((rc = check_pointers({q, w_kv_b, cache, block_table, seq_lens, out, workspace})) != LAGA_OK) return rc;
+    if (lse && (rc = check_pointers({lse})) != LAGA_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t* base = static_cast<uint8_t*>(workspace);
+    unsigned* status = reinterpret_cast<unsigned*>(base);
+    if ((rc = zero_status(status, st)) != LAGA_OK) return rc;
+    if ((rc = launch_q_absorb(q, w_kv_b, B, h, base + w.q_abs, status, st)) != LAGA_OK) return rc;
+    const AttnDecodeArgs a{B, h, w.n_groups, w.ctas_per_group, softmax_scale * 1.4426950408889634f, seq_lens, block_table, columns, shift,
+                           n_pages, reinterpret_cast<float*>(base + w.part_o), reinterpret_cast<float2*>(base + w.part_ml), w.h_pad,
+                           reinterpret_cast<int*>(base + w.tile_start), status};
+    if (w.heads == 16) rc = launch_attn_decode<16>(q, base + w.q_abs, cache, rows, a, st);
+    else if (w.heads == 32) rc = launch_attn_decode<32>(q, base + w.q_abs, cache, rows, a, st);
+    else rc = launch_attn_decode<64>(q, base + w.q_abs, cache, rows, a, st);
+    if (rc != LAGA_OK) return rc;
+    launch_kernel(decode_combine_kernel, dim3(static_cast<unsigned>(B) * h), dim3(128), 0, st, true, a.part_o, a.part_ml, a.tile_start, B, h,
+                  w.h_pad, w.ctas_per_group, reinterpret_cast<__nv_bfloat16*>(base + w.o_lat), lse);
+    if ((rc = launch_status()) != LAGA_OK) return rc;
+    return launch_v_project(base + w.o_lat, w_kv_b, B, h, out, status, st);
 }
 
 }  // extern "C"

@@ -7,7 +7,9 @@ there is no fallback of any kind.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -18,6 +20,7 @@ ERR_WORKSPACE_TOO_SMALL = -3
 ERR_CUDA = -4
 ERR_DEVICE_TIMEOUT = -5
 ERR_DEVICE_CHECK = -6
+ERR_CACHE_PLAN = -7
 FLAG_ACCUM_DW = 1
 FLAG_DETERMINISTIC = 2
 FLAG_KV_SAVED = 4
@@ -32,6 +35,7 @@ _lib = None
 
 # name -> (restype, argtypes); mirrors include/laga.h one to one
 _vp, _ci, _cf, _cu, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint, ctypes.c_size_t
+_ll = ctypes.c_longlong
 SIGNATURES = {
     "laga_version": (_ci, []),
     "laga_status_string": (ctypes.c_char_p, [_ci]),
@@ -49,6 +53,13 @@ SIGNATURES = {
     "laga_linear_backward": (_ci, [_vp, _vp, _vp, _ci, _ci, _ci, _vp, _vp, _cu, _vp, _vp]),
     "laga_layernorm": (_ci, [_vp, _vp, _vp, _ci, _ci, _cf, _vp, _vp, _vp, _vp]),
     "laga_layernorm_backward": (_ci, [_vp] * 5 + [_ci, _ci] + [_vp] * 4),
+    "laga_rope": (_ci, [_vp, _ll, _vp, _vp] + [_ci] * 6 + [_cf, _ci, _vp, _ll, _vp]),
+    "laga_latent_norm_rope": (_ci, [_vp, _ll, _vp, _vp, _cf, _vp, _vp] + [_ci] * 4 + [_cf] + [_vp] * 6 + [_ci, _vp]),
+    "laga_latent_norm_rope_backward_workspace_bytes": (_sz, [_ci, _ci]),
+    "laga_latent_norm_rope_backward": (_ci, [_vp, _vp, _vp, _ll] + [_vp] * 5 + [_ci] * 4 + [_cf] + [_vp] * 4 + [_sz, _vp]),
+    "laga_cache_plan": (_ci, [_vp, _vp, _ci, _ci, _vp, _ci, _vp, _ci, _vp, _ci] + [_vp] * 7),
+    "laga_paged_decode_workspace_bytes": (_sz, [_ci] * 6),
+    "laga_paged_decode": (_ci, [_vp] * 3 + [_ci, _ci, _vp, _ci, _vp] + [_ci] * 6 + [_cf, _vp, _vp, _vp, _sz, _cu, _vp]),
     "laga_up_project": (_ci, [_vp, _vp] + [_ci] * 5 + [_vp, _vp, _vp]),
     "laga_kv_backward": (_ci, [_vp] * 3 + [_ci] * 5 + [_vp, _vp, _cu, _vp, _vp]),
     "laga_query_status": (_ci, [_vp, _vp, ctypes.POINTER(_cu)]),
@@ -60,7 +71,7 @@ SIGNATURES = {
 BUILTIN_SCRATCH_MAX_TOKEN_HEADS = 32768   # S * h limit of laga_fwd_builtin_scratch (16 MiB of bf16 KV)
 KERNELS = {"up_project": 0, "attn_fwd": 1, "bwd_delta": 2, "attn_bwd_dkv": 3, "attn_bwd_dq": 4,
            "dkpe_reduce": 5, "dckv_gemm": 6, "dw_gemm": 7, "q_absorb": 8, "attn_absorbed": 9, "v_project": 10,
-           "attn_bwd_fused": 11, "dq_convert": 12}
+           "attn_bwd_fused": 11, "dq_convert": 12, "attn_decode": 13}
 
 
 class LagaError(RuntimeError):
@@ -374,6 +385,248 @@ def layernorm_backward(dy, x, gamma, mean, rstd, with_beta=True, dx=None, stream
                                            _ptr(dbeta) if dbeta is not None else None, _stream(stream, dev))
     _check(rc, "laga_layernorm_backward")
     return dx, dgamma, dbeta
+
+
+class RopePlan(NamedTuple):
+    """What the rotation needs beside the positions: freqs, fp64 [d_rot / 2] on the device (radians per position), the
+    factor on cos and sin, and which channels pair up ((2j, 2j+1) if interleaved, else (j, j + d_rot/2))."""
+    freqs: torch.Tensor
+    mscale: float = 1.0
+    interleaved: bool = True
+
+
+def rope_plan(d_rot=64, base=10000.0, scaling=None, interleaved=True, device="cuda") -> RopePlan:
+    """freqs_j = base^(-2j / d_rot), formed in float64 on the host, optionally stretched for contexts longer than the
+    ones trained on.  scaling: None or a dict with "type" and "factor" (>= 1), the stretch:
+      linear  every frequency divided by factor
+      ntk     base multiplied by factor^(d_rot / (d_rot - 2)): the slowest pair is divided by factor, the fastest kept
+      yarn    pairs that turn at most beta_slow (1) times within original_length (4096) positions are divided by factor, those
+              that turn at least beta_fast (32) times are kept, with a linear ramp between (YaRN, arXiv:2309.00071);
+              mscale = 0.1 * mscale_weight (1) * ln(factor) + 1 multiplies cos and sin."""
+    if d_rot < 4 or d_rot % 2 or not base > 1:
+        raise ValueError(f"rope_plan: d_rot must be even and at least 4 and base above 1, got {d_rot}, {base}")
+    j = torch.arange(d_rot // 2, dtype=torch.float64)
+    mscale = 1.0
+    options = dict(scaling or {"type": "none"})
+    kind, factor = options.pop("type"), float(options.pop("factor", 1.0))
+    known = {"none": (), "linear": (), "ntk": (), "yarn": ("original_length", "beta_fast", "beta_slow", "mscale_weight")}
+    if kind not in known or not factor >= 1 or any(k not in known[kind] for k in options):
+        raise ValueError(f"rope_plan: unknown or malformed scaling {scaling}")
+    if kind == "ntk":
+        base = base * factor ** (d_rot / (d_rot - 2))
+    freqs = base ** (-2 * j / d_rot)
+    if kind == "linear":
+        freqs = freqs / factor
+    elif kind == "yarn":
+        length = float(options.get("original_length", 4096))
+
+        def pair_of(turns):          # the (fractional) pair that turns so often within the original length
+            return d_rot * math.log(length / (turns * 2 * math.pi)) / (2 * math.log(base))
+
+        low = max(0, math.floor(pair_of(options.get("beta_fast", 32))))
+        high = min(d_rot - 1, math.ceil(pair_of(options.get("beta_slow", 1))))
+        stretched = ((j - low) / max(high - low, 1e-3)).clamp(0, 1)
+        freqs = freqs * (1 - stretched) + freqs / factor * stretched
+        mscale = 0.1 * float(options.get("mscale_weight", 1.0)) * math.log(factor) + 1.0
+    return RopePlan(freqs.to(device), mscale, bool(interleaved))
+
+
+def _rows(t, name, dims, dtype=torch.bfloat16):
+    """A CUDA tensor whose rows (first axis) are dense and may be any pitch apart; returns the pitch in elements."""
+    expect = 1
+    ok = t.is_cuda and t.dtype == dtype and t.dim() == dims
+    if ok:
+        for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+            ok = ok and (stride == expect or size == 1)
+            expect *= size
+        pitch = t.stride(0) if t.shape[0] > 1 else expect
+    if not ok or pitch < expect:
+        raise ValueError(f"{name}: expected a {dims}-d CUDA {dtype} tensor with dense rows, got {t.dtype} {tuple(t.shape)} "
+                         f"strides {t.stride()} on {t.device}")
+    return pitch
+
+
+def _rope_args(rope, positions, M, d_rot=None):
+    n = rope.freqs.shape[0]
+    _dev(rope.freqs, torch.float64, (n,), "freqs")
+    _dev(positions, torch.int32, (M,), "positions")
+    if d_rot is not None and 2 * n != d_rot:
+        raise ValueError(f"the plan rotates {2 * n} channels, the tensor has {d_rot}")
+    return 2 * n
+
+
+def rope(x, positions, rope, rot_begin=None, inverse=False, y=None, stream=None):
+    """laga_rope: x bf16 [M, h, d] (rows may be strided) with channels [rot_begin, rot_begin + d_rot) of every head
+    rotated (default: the last ones).  positions int32 [M].  inverse: the transpose (gradient).  y: a new tensor, or x itself
+    for the rotation in place.  Returns y."""
+    M, h, d = x.shape
+    x_pitch = _rows(x, "x", 3)
+    d_rot = _rope_args(rope, positions, M)
+    y = torch.empty(M, h, d, dtype=torch.bfloat16, device=x.device) if y is None else y
+    y_pitch = _rows(y, "y", 3)
+    if tuple(y.shape) != (M, h, d):
+        raise ValueError(f"y: expected shape {(M, h, d)}, got {tuple(y.shape)}")
+    dev = same_device(x, positions, rope.freqs, y)
+    if M == 0:
+        return y
+    with _on(dev):
+        rc = lib().laga_rope(_ptr(x), x_pitch, _ptr(positions), _ptr(rope.freqs), M, h, d, d - d_rot if rot_begin is None else rot_begin,
+                             d_rot, int(rope.interleaved), float(rope.mscale), int(bool(inverse)), _ptr(y), y_pitch,
+                             _stream(stream, dev))
+    _check(rc, "laga_rope")
+    return y
+
+
+def _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, latent, k_pe, mean, rstd, cache, slots, stream):
+    M, D = kv_a.shape[0], gamma.shape[0]
+    R = kv_a.shape[1] - D
+    pitch = _rows(kv_a, "kv_a", 2)
+    _dev(gamma, torch.bfloat16, (D,), "gamma")
+    if beta is not None:
+        _dev(beta, torch.bfloat16, (D,), "beta")
+    _rope_args(rope, positions, M, R)
+    n_slots = 0
+    if cache is not None:
+        if cache.dim() < 2:
+            raise ValueError(f"cache: expected [..., {D + R}], got {tuple(cache.shape)}")
+        _dev(cache, torch.bfloat16, tuple(cache.shape[:-1]) + (D + R,), "cache")
+        _dev(slots, torch.int32, (M,), "slots")
+        n_slots = cache.numel() // (D + R)
+    dev = same_device(kv_a, gamma, beta, positions, rope.freqs, latent, k_pe, cache, slots)
+    if M == 0:
+        return
+    with _on(dev):
+        rc = lib().laga_latent_norm_rope(_ptr(kv_a), pitch, _ptr(gamma), _ptr(beta), float(eps), _ptr(positions), _ptr(rope.freqs), M, D,
+                                         R, int(rope.interleaved), float(rope.mscale), _ptr(latent), _ptr(k_pe), _ptr(mean),
+                                         _ptr(rstd), _ptr(cache), _ptr(slots), n_slots, _stream(stream, dev))
+    _check(rc, "laga_latent_norm_rope")
+
+
+def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps=1e-5, latent=None, k_pe=None, cache=None, slots=None, stream=None):
+    """laga_latent_norm_rope: kv_a bf16 [M, D + R] (rows may be strided) -> (latent bf16 [M, D], k_pe bf16 [M, R], mean, rstd
+    fp32 [M]).  With cache (bf16 [..., D + R]) and slots (int32 [M]) the rows also enter the cache."""
+    M, D = kv_a.shape[0], gamma.shape[0]
+    R = kv_a.shape[1] - D
+    if (cache is None) != (slots is None):
+        raise ValueError("cache and slots go together")
+    new = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device=kv_a.device)  # noqa: E731
+    latent = new(M, D) if latent is None else _dev(latent, torch.bfloat16, (M, D), "latent")
+    k_pe = new(M, R) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
+    mean, rstd = torch.empty(2, M, dtype=torch.float32, device=kv_a.device).unbind(0)
+    _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, latent, k_pe, mean, rstd, cache, slots, stream)
+    return latent, k_pe, mean, rstd
+
+
+def cache_append(kv_a, gamma, beta, positions, rope, slots, cache, eps=1e-5, stream=None):
+    """laga_latent_norm_rope into the cache alone: row slots[m] of cache (bf16 [..., D + R]) receives the normalised latent and
+    the rotated key of kv_a's row m; a slot outside the cache (-1) writes nothing.  Returns cache."""
+    _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, None, None, None, None, cache, slots, stream)
+    return cache
+
+
+def latent_norm_rope_backward(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope, with_beta=True, dkv_a=None, workspace=None,
+                              stream=None):
+    """laga_latent_norm_rope_backward: returns (dkv_a bf16 [M, D + R], dgamma fp32 [D], dbeta fp32 [D] or None)."""
+    M, D = dlatent.shape
+    R = dk_pe.shape[1]
+    _dev(dlatent, torch.bfloat16, (M, D), "dlatent")
+    _dev(dk_pe, torch.bfloat16, (M, R), "dk_pe")
+    pitch = _rows(kv_a, "kv_a", 2)
+    if tuple(kv_a.shape) != (M, D + R):
+        raise ValueError(f"kv_a: expected shape {(M, D + R)}, got {tuple(kv_a.shape)}")
+    _dev(gamma, torch.bfloat16, (D,), "gamma")
+    _dev(mean, torch.float32, (M,), "mean")
+    _dev(rstd, torch.float32, (M,), "rstd")
+    _rope_args(rope, positions, M, R)
+    dev = same_device(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope.freqs, dkv_a, workspace)
+    dkv_a = (torch.empty(M, D + R, dtype=torch.bfloat16, device=dev) if dkv_a is None else
+             _dev(dkv_a, torch.bfloat16, (M, D + R), "dkv_a"))
+    if M == 0:
+        sums = torch.zeros(2, D, dtype=torch.float32, device=dev)
+        return dkv_a, sums[0], sums[1] if with_beta else None
+    need = int(lib().laga_latent_norm_rope_backward_workspace_bytes(M, D))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    dgamma, dbeta = torch.empty(2, D, dtype=torch.float32, device=dev).unbind(0)
+    with _on(dev):
+        rc = lib().laga_latent_norm_rope_backward(
+            _ptr(dlatent), _ptr(dk_pe), _ptr(kv_a), pitch, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(positions), _ptr(rope.freqs), M, D,
+            R, int(rope.interleaved), float(rope.mscale), _ptr(dkv_a), _ptr(dgamma), _ptr(dbeta) if with_beta else None,
+            _ptr(workspace), workspace.numel(), _stream(stream, dev))
+    _check(rc, "laga_latent_norm_rope_backward")
+    return dkv_a, dgamma, dbeta if with_beta else None
+
+
+class CachePlan(NamedTuple):
+    """One step's tables: see laga_cache_plan in include/laga.h.  status: pass to query_status / check_status."""
+    slots: torch.Tensor          # int32 [max_tokens]
+    positions: torch.Tensor      # int32 [max_tokens]
+    cu_new_lens: torch.Tensor    # int32 [n + 1]
+    seq_lens: torch.Tensor       # int32 [n], the new lengths
+    n_free: torch.Tensor         # int32 [1], the new stack height
+    status: torch.Tensor         # int32 [1]
+
+
+def cache_plan(seq_lens, new_lens, block_table, free_pages, n_free, page_size, max_tokens, out=None, stream=None) -> CachePlan:
+    """laga_cache_plan: pages, slots and positions for a step that adds new_lens[b] tokens to request b.  block_table
+    (int32 [n, columns]) is written in place where the new tokens need pages; everything else comes back new (or in `out`,
+    a CachePlan of an earlier call with the same sizes)."""
+    n, columns = block_table.shape
+    _dev(seq_lens, torch.int32, (n,), "seq_lens")
+    _dev(new_lens, torch.int32, (n,), "new_lens")
+    _dev(block_table, torch.int32, (n, columns), "block_table")
+    _dev(free_pages, torch.int32, (free_pages.numel(),), "free_pages")
+    _dev(n_free, torch.int32, (1,), "n_free")
+    dev = same_device(seq_lens, new_lens, block_table, free_pages, n_free, *(out or ()))
+    if out is None:
+        whole = torch.empty(2 * max_tokens + 2 * n + 3, dtype=torch.int32, device=dev)
+        out = CachePlan(*whole.split([max_tokens, max_tokens, n + 1, n, 1, 1]))
+    else:
+        for name, size in zip(CachePlan._fields, (max_tokens, max_tokens, n + 1, n, 1, 1)):
+            _dev(getattr(out, name), torch.int32, (size,), name)
+    with _on(dev):
+        rc = lib().laga_cache_plan(_ptr(seq_lens), _ptr(new_lens), n, int(page_size), _ptr(block_table), columns, _ptr(free_pages),
+                                   free_pages.numel(), _ptr(n_free), int(max_tokens), _ptr(out.slots), _ptr(out.positions),
+                                   _ptr(out.cu_new_lens), _ptr(out.seq_lens), _ptr(out.n_free), _ptr(out.status), _stream(stream, dev))
+    _check(rc, "laga_cache_plan")
+    return out
+
+
+def paged_decode_workspace_bytes(B, h, d_c=512, d_nope=128, d_rope=64, d_v=128) -> int:
+    return int(lib().laga_paged_decode_workspace_bytes(B, h, d_c, d_nope, d_rope, d_v))
+
+
+def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, out=None, lse=None, workspace=None, stream=None):
+    """laga_paged_decode: attention of one new token per request (q bf16 [B, h, 192], rope band rotated) over a paged cache
+    (bf16 [n_pages, page_size, 576]; block_table int32 [B, columns], seq_lens int32 [B], both on the device).  lse: fp32 [B, h] to
+    have it written.  Returns (out bf16 [B, h, 128], lse or None, workspace)."""
+    B, h, d_qk = q.shape
+    _dev(q, torch.bfloat16, (B, h, d_qk), "q")
+    n_pages, page_size, row = cache.shape
+    _dev(cache, torch.bfloat16, (n_pages, page_size, row), "cache")
+    d_c = w_kv_b.shape[0]
+    d_rope = row - d_c
+    d_nope, d_v = d_qk - d_rope, w_kv_b.shape[1] // h - (d_qk - d_rope)
+    _dev(w_kv_b, torch.bfloat16, (d_c, h * (d_nope + d_v)), "w_kv_b")
+    _dev(block_table, torch.int32, (B, block_table.shape[1]), "block_table")
+    _dev(seq_lens, torch.int32, (B,), "seq_lens")
+    dev = same_device(q, w_kv_b, cache, block_table, seq_lens, out, lse, workspace)
+    if softmax_scale is None:
+        softmax_scale = d_qk ** -0.5
+    out = torch.empty(B, h, d_v, dtype=torch.bfloat16, device=dev) if out is None else _dev(out, torch.bfloat16, (B, h, d_v), "out")
+    if lse is not None:
+        _dev(lse, torch.float32, (B, h), "lse")
+    need = paged_decode_workspace_bytes(B, h, d_c, d_nope, d_rope, d_v)
+    if need == 0:
+        raise LagaError(ERR_UNSUPPORTED, "laga_paged_decode_workspace_bytes")
+    if workspace is None:
+        workspace = alloc_workspace(need, dev)
+    with _on(dev):
+        rc = lib().laga_paged_decode(_ptr(q), _ptr(w_kv_b), _ptr(cache), n_pages, page_size, _ptr(block_table), block_table.shape[1],
+                                     _ptr(seq_lens), B, h, d_c, d_nope, d_rope, d_v, float(softmax_scale), _ptr(out), _ptr(lse),
+                                     _ptr(workspace), workspace.numel(), 0, _stream(stream, dev))
+    _check(rc, "laga_paged_decode")
+    return out, lse, workspace
 
 
 def up_project(c_kv, w_kv_b, h, d_nope=128, d_v=128, kv=None, status_word=None, stream=None):
