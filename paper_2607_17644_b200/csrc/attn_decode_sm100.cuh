@@ -13,18 +13,21 @@
 // slot -- and decode_combine_kernel joins a request's pieces.
 //
 // Tiles.  kHeads (16, 32 or 64) heads per CTA; more heads are more CTAs over the same keys (L2 serves the second read).
-//   scores   S[heads x 64 keys] = Q (A, rows = heads, of 128 MMA rows only the first kHeads mean anything; the others read
-//            whatever shared memory follows and are ignored) . K^T (B, K-major key tile): a head's row sits in one TMEM lane, so
-//            the softmax needs no exchange between threads
+//   scores   S[heads x 64 keys] = Q (A, rows = heads; of the 64 MMA rows only the first kHeads mean anything, the others read
+//            whatever shared memory follows and are ignored) . K^T (B, K-major key tile).  Rows 16w .. 16w+15 of an M = 64
+//            product lie in lanes 32w .. 32w+15 of TMEM: sixteen heads per softmax warp, read so that all 32 threads
+//            have 32 scores each (tmem_ld_16x64)
 //   output   O^T[512 latents x heads] (+)= V^T (A, MN-major: the very same key tile) . P^T (B: the softmax's bf16 P in shared memory):
 //            the long side is the MMA's M, so few heads waste nothing and O takes 4 * kHeads TMEM columns
-// The tile is loaded once, in nine 64-channel slabs: the rope slab (only the scores read it) and four units of two slabs (128
-// latents).  Rope slabs and units go around two rings with a barrier per entry, so the next tiles' loads are always in
-// flight while this tile is scored, exponentiated and multiplied.
+// The tile is loaded once, in nine 64-channel slabs: the rope slab, which only the scores read, and two halves of four slabs (256
+// latents), which go around a ring with a barrier per entry, so that the next tiles' loads are in flight while this
+// tile is scored, exponentiated and multiplied.
 //
-//   warps 0..3  softmax (thread = head row), rescaling of O^T when a running maximum moved by more than 2^8, drain
-//   warp 4      TMA producer (page table entries are fetched 32 at a time, one batch ahead)
-//   warp 5      MMA issuer: takes whatever is ready, P.V first (it frees units), else the next unit's score MMAs
+//   warps 0..3  softmax (16 heads per warp), rescaling of O^T when a running maximum moved by more than 2^8, drain
+//   warp 7      TMA producer (page table entries are fetched ahead of their use)
+//   warps 6, 5  issuers of the score and of the value MMAs: apart, because a lane that has issued MMAs sees no barrier until the tensor
+//               pipe has taken them, and neither product's start should wait for the other's
+//   (warp 4 does nothing: it keeps the others off the scheduler of softmax warp 0)
 //
 // Rows behind a request's last token may hold anything, NaN included: their scores are replaced by -inf, and their
 // rows of the tile are zeroed in shared memory before P.V (0 * NaN is NaN).
@@ -34,33 +37,30 @@
 
 namespace laga {
 
-constexpr int kDecThreads = 192;
+constexpr int kDecThreads = 256;            // (warp 4 idles: see the roles)
+constexpr int kDecProducerWarp = 7, kDecScoreWarp = 6, kDecValueWarp = 5;
 constexpr int kDecKeys = 64;
 constexpr int kDecMaxCtas = 148;             // CTAs over all head groups (the workspace is sized by it)
 constexpr int kDecRow = 576;                 // channels of a cached token
 constexpr int kDecLat = 512;
 
-// Shared memory for kHeads heads per CTA.  Shared memory is what limits the loads in flight: 64 heads' queries take 72 KB
-// of it, so that variant keeps one P buffer.
+// Shared memory for kHeads heads per CTA: what the queries and P leave holds the tiles, 3, 2.5 or 2 of them.
 template <int kHeads>
 struct AttnDecodeSmem {
-    static constexpr int kQBufs = kHeads == 16 ? 2 : 1;
-    static constexpr int kPBufs = kHeads == 64 ? 1 : 2;
-    static constexpr int kRopes = kHeads == 64 ? 2 : kHeads == 32 ? 3 : 4;
-    static constexpr int kUnits = kHeads == 64 ? 8 : 9;
+    static constexpr int kHalves = kHeads == 16 ? 6 : kHeads == 32 ? 5 : 4;      // half tiles in the ring
     static constexpr int kQSlab = kHeads * 128;               // kHeads rows x 64 channels
     static constexpr int kPTile = kHeads * 128;               // kHeads rows x 64 keys
     static constexpr int kSlab = kDecKeys * 128;              // 64 keys x 64 channels
-    static constexpr int kUnit = 2 * kSlab;
+    static constexpr int kHalf = 4 * kSlab;                   // 64 keys x 256 latents
     static constexpr int kQ = 0;
-    static constexpr int kP = kQ + kQBufs * 9 * kQSlab;
-    static constexpr int kRope = kP + kPBufs * kPTile;
-    static constexpr int kUnit0 = kRope + kRopes * kSlab;
-    static constexpr int kAlpha = kUnit0 + kUnits * kUnit;    // two buffers of kHeads factors, then of a word per warp
+    static constexpr int kP = kQ + 9 * kQSlab;                // two buffers
+    static constexpr int kRope = kP + 2 * kPTile;             // one slab: it is free again as soon as it has been scored
+    static constexpr int kHalf0 = kRope + kSlab;
+    static constexpr int kAlpha = kHalf0 + kHalves * kHalf;   // two buffers of kHeads factors, then of a word per warp
     static constexpr int kBar = kAlpha + 2 * kHeads * 4 + 32;
-    static constexpr int kTotalBytes = kBar + 64 * 8;
-    // the MMA's rows kHeads..127 of the last query slab read up to here
-    static_assert(kQ + (kQBufs * 9 - 1) * kQSlab + 128 * 128 <= kAlpha, "score MMAs read past the operand area");
+    static constexpr int kTotalBytes = kBar + 48 * 8;
+    // the MMA's rows kHeads..63 of the last query slab read up to here
+    static_assert(kQ + 8 * kQSlab + 64 * 128 <= kAlpha, "score MMAs read past the operand area");
 };
 static_assert(AttnDecodeSmem<16>::kTotalBytes <= 232448 && AttnDecodeSmem<32>::kTotalBytes <= 232448 &&
               AttnDecodeSmem<64>::kTotalBytes <= 232448, "decode kernel exceeds the 227 KB of shared memory per CTA");
@@ -117,57 +117,62 @@ struct DecodeCursor {
 template <int kHeads>
 __global__ void __launch_bounds__(kDecThreads, 1)
 attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __grid_constant__ CUtensorMap tmap_q,
-                         const __grid_constant__ CUtensorMap tmap_cache, const AttnDecodeArgs args) {
+                         const __grid_constant__ CUtensorMap tmap_rope, const __grid_constant__ CUtensorMap tmap_lat,
+                         const AttnDecodeArgs args) {
     using L = AttnDecodeSmem<kHeads>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBar);
-    uint64_t* u_full = bars;                          // [kUnits]
-    uint64_t* u_empty = u_full + L::kUnits;
-    uint64_t* r_full = u_empty + L::kUnits;           // [kRopes]
-    uint64_t* r_empty = r_full + L::kRopes;
-    uint64_t* q_full = r_empty + L::kRopes;           // [kQBufs]
-    uint64_t* q_empty = q_full + L::kQBufs;
-    uint64_t* s_full = q_empty + L::kQBufs;           // [2] scores of tile T are in TMEM buffer T & 1
+    uint64_t* h_full = bars;                          // [kHalves] half tile has landed
+    uint64_t* h_empty = h_full + L::kHalves;          // ... has been scored and multiplied
+    uint64_t* r_full = h_empty + L::kHalves;          // rope slab
+    uint64_t* r_empty = r_full + 1;
+    uint64_t* q_full = r_empty + 1;                   // the piece's queries
+    uint64_t* q_empty = q_full + 1;
+    uint64_t* s_full = q_empty + 1;                    // [2] scores of tile T are in TMEM buffer T & 1
     uint64_t* p_full = s_full + 2;                    // [2] P of tile T is in shared memory, O^T is rescaled
     uint64_t* pv_done = p_full + 2;                   // [2] O^T += V^T P^T of tile T has completed
     uint64_t* a_full = pv_done + 2;                   // [2] rescaling factors of tile T are in shared memory
     uint64_t* o_full = a_full + 2;                    // a piece's accumulator is complete
     uint64_t* o_free = o_full + 1;                    // ... and has been drained
-    uint64_t* quiesce_bar = o_free + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 48);
+    uint64_t* quiesce_bar = o_free + 1;               // [2] abort path only: the issuers' last commits
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 36);
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
     int* start_b = reinterpret_cast<int*>(tmem_slot + 2);
     int* start_t = start_b + 1;
     int* scan = start_b + 2;                          // [6] per-warp sums of the tile counts
-    static_assert(2 * L::kUnits + 2 * L::kRopes + 2 * L::kQBufs + 11 <= 48, "barriers overlap the scalars");
+    static_assert(2 * L::kHalves + 4 + 12 <= 36, "barriers overlap the scalars");
     float* alpha_s = reinterpret_cast<float*>(smem + L::kAlpha);
     volatile int* moved_s = reinterpret_cast<volatile int*>(alpha_s + 2 * kHeads);     // [2 buffers][4 warps]
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // (warp-uniform for the compiler)
     const int group = static_cast<int>(blockIdx.x) % args.n_groups;
     const int cta = static_cast<int>(blockIdx.x) / args.n_groups;
     const int head0 = group * kHeads;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < L::kUnits; ++i) { mbar_init(&u_full[i], 1); mbar_init(&u_empty[i], 1); }
-        for (int i = 0; i < L::kRopes; ++i) { mbar_init(&r_full[i], 1); mbar_init(&r_empty[i], 1); }
-        for (int i = 0; i < L::kQBufs; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 128); mbar_init(&pv_done[i], 1); mbar_init(&a_full[i], kHeads < 32 ? 32 : kHeads); }
-        mbar_init(o_full, 1); mbar_init(o_free, 128); mbar_init(quiesce_bar, 1);
+        for (int i = 0; i < L::kHalves; ++i) { mbar_init(&h_full[i], 1); mbar_init(&h_empty[i], 1); }
+        mbar_init(r_full, 1); mbar_init(r_empty, 1); mbar_init(q_full, 1); mbar_init(q_empty, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); mbar_init(&pv_done[i], 1); mbar_init(&a_full[i], kHeads / 16); }
+        mbar_init(o_full, 1); mbar_init(o_free, 4); mbar_init(quiesce_bar, 1); mbar_init(quiesce_bar + 1, 1);
         abort_flag->value = (smem_u32(smem) & 1023u) != 0u ? 1u : 0u;
         *start_b = 0; *start_t = 0;
         mbar_fence_init();
-        tma_prefetch_desc(&tmap_qabs); tma_prefetch_desc(&tmap_q); tma_prefetch_desc(&tmap_cache);
+        tma_prefetch_desc(&tmap_qabs); tma_prefetch_desc(&tmap_q); tma_prefetch_desc(&tmap_rope); tma_prefetch_desc(&tmap_lat);
     }
-    if (warp == 5) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
+    if (warp == kDecScoreWarp) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     grid_launch_dependents();
-    grid_dependency_wait();          // global memory from here on
-    const uint32_t tmem_base = *tmem_slot;
-    const uint32_t tmem_s = tmem_base + 256;
-    if (threadIdx.x == 0 && abort_flag->value != 0u) atomicCAS(args.status, kStatusOk, kStatusCheck | 0xD4u);
+    // Launched to overlap decode_absorb_kernel, the only kernel of the call before this one, which itself starts after everything
+    // earlier on the stream.  Only the absorbed queries (and the status word, which it clears) are its work: lengths, page
+    // table and cache are read at once, and the producer alone waits, before it fetches its first queries.
+    // All 512 columns are this CTA's, so they start at column 0: an immediate in every MMA (checked, not trusted).
+    constexpr uint32_t tmem_base = 0, tmem_s = 256;
+    if (threadIdx.x == 0 && (abort_flag->value != 0u || *tmem_slot != tmem_base)) {
+        abort_flag->value = 1u;
+        atomicCAS(args.status, kStatusOk, kStatusCheck | 0xD4u);
+    }
 
     // ---- the line of tiles, and where this CTA's stretch begins --------------------------------------------
     int my_tiles = 0;
@@ -207,195 +212,224 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
 
     if (abort_flag->value != 0u || my_tiles <= 0) {
         // nothing to do (or nothing may be done): fall through to the common exit
-    } else if (warp == 4) {
+    } else if (warp == kDecProducerWarp) {
         // ---- producer ------------------------------------------------------------------------------------
-        ArmedBarriers armed(bars);
-        uint32_t nu = 0, nr = 0, nq = 0;
-        const int sub_shift = args.page_shift < 6 ? args.page_shift : 6;       // a box is one page or a whole tile, if smaller
-        const int n_sub = kDecKeys >> sub_shift, sub_rows = 1 << sub_shift;
         const int n_rows = args.n_pages << args.page_shift;
-        bool ok = true;
-        DecodeCursor cur(args, my_tiles, first_b, first_t);
-        bool new_piece = true;
-        int batch0 = 0, row_cur = 0, row_next = 0;       // first row of sub-box (batch0 + lane), and of the batch after it
-        // first cache row of sub-box s of the request (s counts boxes of sub_rows keys)
-        auto sub_row = [&](int b, int len, int s) -> int {
-            const int key = s << sub_shift;
-            if (key >= len || key < 0) return n_rows;                          // beyond the request: never issued
-            const int page = __ldg(args.block_table + static_cast<size_t>(b) * args.columns + (key >> args.page_shift));
+        // first cache row of the keys from `key` on, within one page
+        auto row_of = [&](const DecodeCursor& c, int key) -> int {
+            if (key >= c.len) return n_rows;                                   // beyond the request: never issued
+            const int page = __ldg(args.block_table + static_cast<size_t>(c.b) * args.columns + (key >> args.page_shift));
             if (page < 0 || page >= args.n_pages) {                            // a bad entry: zeros, and a status
                 atomicCAS(args.status, kStatusOk, kStatusCheck | 0xF1u);
                 return n_rows;                                                 // out of the map's range: TMA fills zeros
             }
             return (page << args.page_shift) + (key & ((1 << args.page_shift) - 1));
         };
-        while (!cur.done()) {
-            if (new_piece) {
-                const uint32_t qb = nq % L::kQBufs;
-                ok = mbar_wait(&q_empty[qb], ((nq / L::kQBufs) & 1u) ^ 1u, abort_flag, args.status, 0xB0);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                if (lane == 0) {
-                    mbar_arrive_expect_tx(&q_full[qb], 9 * L::kQSlab);
-                    armed.arm(&q_full[qb], nq / L::kQBufs);
-                    uint8_t* dst = smem + L::kQ + qb * 9 * L::kQSlab;
-                    tma_load_2d_chk(args.status, dst, &tmap_q, &q_full[qb], 128, cur.b * args.h + head0);          // rope band first
-                    for (int c = 0; c < 8; ++c)
-                        tma_load_2d_chk(args.status, dst + (1 + c) * L::kQSlab, &tmap_qabs, &q_full[qb], c * 64, cur.b * args.h + head0);
-                }
-                ++nq;
-                batch0 = cur.t * n_sub;
-                row_cur = sub_row(cur.b, cur.len, batch0 + lane);
-                row_next = sub_row(cur.b, cur.len, batch0 + 32 + lane);
-                new_piece = false;
-            }
-            const int s0 = cur.t * n_sub;
-            if (s0 - batch0 >= 32) {
-                batch0 += 32;
-                row_cur = row_next;
-                row_next = sub_row(cur.b, cur.len, batch0 + 32 + lane);
-            }
-            const int valid = cur.valid();
-            const int boxes = (valid + sub_rows - 1) >> sub_shift;              // sub-boxes of this tile that hold a key
-            const int row = __shfl_sync(0xffffffffu, row_cur, (s0 - batch0 + lane) & 31);   // lane s: sub-box s of this tile
-            const uint32_t box_bytes = static_cast<uint32_t>(boxes) * sub_rows * 128;
+        auto load_queries = [&](const DecodeCursor& c, uint32_t piece, ArmedBarriers& armed) -> bool {
+            if (!mbar_wait(q_empty, (piece & 1u) ^ 1u, abort_flag, args.status, 0xB0)) return false;
+            mbar_arrive_expect_tx(q_full, 9 * L::kQSlab);
+            armed.arm(q_full, piece);
+            uint8_t* dst = smem + L::kQ;
+            tma_load_2d_chk(args.status, dst, &tmap_q, q_full, 128, c.b * args.h + head0);          // rope band first
+            for (int k = 0; k < 8; ++k)
+                tma_load_2d_chk(args.status, dst + (1 + k) * L::kQSlab, &tmap_qabs, q_full, k * 64, c.b * args.h + head0);
+            return true;
+        };
+        grid_dependency_wait();
+        uint32_t slot = 0, par = 0, r_par = 0, pieces = 0;
+        bool new_piece = true, ok = true;
+        if (args.page_shift >= 6) {
+            // A tile lies in one page: three copies, by one lane.  A 3-d view of the cache (64 channels, rows, nine channel groups)
+            // lets one copy fill four slabs; what limits this warp is its instruction count, as it does the MMA lanes'.
+            if (elect_one()) {
+                ArmedBarriers armed(bars);
+                DecodeCursor cur(args, my_tiles, first_b, first_t);
+                int row = row_of(cur, cur.t * kDecKeys);
+                while (!cur.done()) {
+                    if (new_piece && !load_queries(cur, pieces++, armed)) break;
+                    new_piece = cur.ends_piece();
+                    DecodeCursor next = cur;
+                    next.next(args);
+                    const int next_row = next.done() ? 0 : row_of(next, next.t * kDecKeys);         // a tile ahead
+                    if (!mbar_wait(r_empty, r_par ^ 1u, abort_flag, args.status, 0xB1)) break;
+                    mbar_arrive_expect_tx(r_full, L::kSlab);
+                    armed.arm(r_full, r_par);
+                    tma_load_3d(smem + L::kRope, &tmap_rope, r_full, 0, row, 8);
+                    r_par ^= 1u;
 #pragma unroll 1
-            for (int e = 0; e < 5; ++e) {                                       // the rope slab, then the four units
-                uint64_t *full, *empty;
-                uint8_t* dst;
-                uint32_t phase, slot;
-                if (e == 0) {
-                    slot = nr % L::kRopes; phase = nr / L::kRopes; ++nr;
-                    full = &r_full[slot]; empty = &r_empty[slot]; dst = smem + L::kRope + slot * L::kSlab;
-                } else {
-                    slot = nu % L::kUnits; phase = nu / L::kUnits; ++nu;
-                    full = &u_full[slot]; empty = &u_empty[slot]; dst = smem + L::kUnit0 + slot * L::kUnit;
+                    for (int half = 0; half < 2; ++half) {
+                        ok = mbar_wait(&h_empty[slot], par ^ 1u, abort_flag, args.status, 0xB8);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx(&h_full[slot], L::kHalf);
+                        armed.arm(&h_full[slot], par);
+                        tma_load_3d(smem + L::kHalf0 + slot * L::kHalf, &tmap_lat, &h_full[slot], 0, row, half * 4);
+                        if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
+                    }
+                    if (!ok) break;
+                    cur = next;
+                    row = next_row;
                 }
-                ok = mbar_wait(empty, (phase & 1u) ^ 1u, abort_flag, args.status, 0xB1);
+                if (abort_flag->value != 0u) armed.quiesce();
+            }
+        } else {
+            // Pages of 16 or 32 rows: four or two boxes a slab, a box per lane.  Lane l also keeps the page of box l of the next 32.
+            ArmedBarriers armed(bars);
+            const int n_sub = kDecKeys >> args.page_shift, page = 1 << args.page_shift;
+            DecodeCursor cur(args, my_tiles, first_b, first_t);
+            int batch = 0, row_cur = 0, row_next = 0;       // first box of the batch; rows of box batch + lane and batch + 32 + lane
+            while (!cur.done()) {
+                if (new_piece) {
+                    if (lane == 0) ok = load_queries(cur, pieces, armed);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    ++pieces;
+                    batch = cur.t * n_sub;
+                    row_cur = row_of(cur, (batch + lane) << args.page_shift);
+                    row_next = row_of(cur, (batch + 32 + lane) << args.page_shift);
+                }
+                new_piece = cur.ends_piece();
+                if (cur.t * n_sub - batch >= 32) {
+                    batch += 32;
+                    row_cur = row_next;
+                    row_next = row_of(cur, (batch + 32 + lane) << args.page_shift);
+                }
+                const int boxes = (cur.valid() + page - 1) >> args.page_shift;              // boxes of this tile that hold a key
+                const int sub = lane & (n_sub - 1);
+                const int row = __shfl_sync(0xffffffffu, row_cur, cur.t * n_sub - batch + sub);
+                const uint32_t bytes = static_cast<uint32_t>(boxes) * page * 128;
+                if (lane == 0) {
+                    ok = mbar_wait(r_empty, r_par ^ 1u, abort_flag, args.status, 0xB1);
+                    if (ok) {
+                        mbar_arrive_expect_tx(r_full, bytes);
+                        armed.arm(r_full, r_par);
+                    }
+                }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (lane == 0) {
-                    mbar_arrive_expect_tx(full, e == 0 ? box_bytes : 2 * box_bytes);
-                    armed.arm(full, phase);
-                }
-                __syncwarp();
-                if (lane < boxes) {
-                    uint8_t* at = dst + lane * sub_rows * 128;
-                    if (e == 0) {
-                        tma_load_2d(at, &tmap_cache, full, kDecLat, row);
-                    } else {
-                        tma_load_2d(at, &tmap_cache, full, (e - 1) * 128, row);
-                        tma_load_2d(at + L::kSlab, &tmap_cache, full, (e - 1) * 128 + 64, row);
+                if (lane < boxes) tma_load_3d(smem + L::kRope + lane * page * 128, &tmap_rope, r_full, 0, row, 8);
+                r_par ^= 1u;
+                for (int half = 0; half < 2; ++half) {
+                    if (lane == 0) {
+                        ok = mbar_wait(&h_empty[slot], par ^ 1u, abort_flag, args.status, 0xB8);
+                        if (ok) {
+                            mbar_arrive_expect_tx(&h_full[slot], 4 * bytes);
+                            armed.arm(&h_full[slot], par);
+                        }
                     }
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    const int slab = lane / n_sub;                                          // lanes 0 .. 4 n_sub - 1: box `sub` of slab `slab`
+                    if (slab < 4 && sub < boxes)
+                        tma_load_3d(smem + L::kHalf0 + slot * L::kHalf + slab * L::kSlab + sub * page * 128, &tmap_rope, &h_full[slot], 0, row,
+                                    half * 4 + slab);
+                    if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                 }
+                if (!ok) break;
+                cur.next(args);
             }
-            if (!ok) break;
-            new_piece = cur.ends_piece();
-            cur.next(args);
+            __syncwarp();
+            if (lane == 0 && abort_flag->value != 0u) armed.quiesce();
         }
-        __syncwarp();
-        if (lane == 0 && abort_flag->value != 0u) armed.quiesce();
-    } else if (warp == 5) {
-        // ---- MMA issuer ----------------------------------------------------------------------------------
+    } else if (warp == kDecScoreWarp) {
+        // ---- issuer of the score MMAs ----------------------------------------------------------------------
         if (elect_one()) {
-            constexpr uint32_t idesc_qk = make_idesc_bf16(128, kDecKeys, 0, 0);
-            constexpr uint32_t idesc_pv = make_idesc_bf16(128, kHeads, 1, 0);
-            DecodeCursor qk(args, my_tiles, first_b, first_t), pv = qk;
-            uint32_t Tq = 0, Tp = 0;                 // tiles scored / multiplied so far
-            uint32_t nu = 0, nr = 0, nq = 0;         // ring entries the score MMAs have taken
-            uint32_t pv_unit = 0, pieces = 0;
-            int part = 0;                            // of the tile being scored: 0 = rope slab next, 1..4 = unit next
-            bool qk_new = true, pv_new = true, ok = true;
-            unsigned long long t0 = global_timer_ns();
-            uint32_t polls = 0;
-            while (!pv.done()) {
-                bool progress = false;
-                if (Tp < Tq && mbar_try_wait(&p_full[Tp & 1u], (Tp >> 1) & 1u)) {
-                    // the first tile of a piece overwrites O^T: the piece before it must have been drained
-                    if (pv_new && pieces > 0) {
-                        ok = mbar_wait(o_free, (pieces - 1) & 1u, abort_flag, args.status, 0xB3);
-                        if (!ok) break;
-                    }
+            constexpr uint32_t idesc = make_idesc_bf16(64, kDecKeys, 0, 0);
+            const uint32_t q_lo = desc_lo(desc_k_major(smem_u32(smem + L::kQ))), r_lo = desc_lo(desc_k_major(smem_u32(smem + L::kRope))),
+                           k_lo = desc_lo(desc_k_major(smem_u32(smem + L::kHalf0))), hi = desc_hi(desc_k_major(0));
+            uint32_t slot = 0, h_par = 0, pieces = 0;
+            bool ok = true, new_piece = true, early = false;
+            DecodeCursor cur(args, my_tiles, first_b, first_t);
+            for (uint32_t T = 0; !cur.done(); ++T) {
+                const uint32_t buf = T & 1u, par = (T >> 1) & 1u, d = tmem_s + buf * kDecKeys;
+                // A barrier probe queues behind the lane's MMAs until the tensor pipe has taken them, so each is made before the
+                // MMAs that precede its use: `early` holds this tile's, made before the last MMAs of the tile before.
+                if (!early) {
+                    if (T >= 2) ok = mbar_wait(&p_full[buf], par ^ 1u, abort_flag, args.status, 0xB2);     // the scores of tile T - 2 have been read
+                    if (ok) ok = mbar_wait(r_full, T & 1u, abort_flag, args.status, 0xB4);
+                }
+                if (ok && new_piece) ok = mbar_wait(q_full, pieces & 1u, abort_flag, args.status, 0xB3);
+                if (!ok) break;
+                bool here = mbar_test_wait(&h_full[slot], h_par);
+                tc_fence_after_sync();
+                uint32_t a_lo = q_lo;
+                mma_ss_chain4_first(d, a_lo, hi, r_lo, hi, idesc);
+                mma_commit(r_empty);
+                a_lo += L::kQSlab / 16;
+                new_piece = cur.ends_piece();
+                cur.next(args);
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    if (!here) ok = mbar_wait(&h_full[slot], h_par, abort_flag, args.status, 0xB5);
+                    if (!ok) break;
+                    const uint32_t b_lo = k_lo + slot * (L::kHalf / 16);
+                    if (++slot == L::kHalves) { slot = 0; h_par ^= 1u; }
+                    if (half == 0) here = mbar_test_wait(&h_full[slot], h_par);
                     tc_fence_after_sync();
-                    const int k_steps = (pv.valid() + 15) >> 4;
-                    const uint32_t sp = smem_u32(smem + L::kP + (Tp % L::kPBufs) * L::kPTile);
-                    for (int u = 0; u < 4; ++u) {
-                        const uint32_t slot = pv_unit % L::kUnits;
-                        ++pv_unit;
-                        const uint32_t sv = smem_u32(smem + L::kUnit0 + slot * L::kUnit);
-                        for (int kk = 0; kk < k_steps; ++kk)
-                            mma_ss(tmem_base + u * kHeads, desc_mn_major(sv + kk * 2048, L::kSlab), desc_k_major(sp + kk * 32), idesc_pv,
-                                   (!pv_new || kk > 0) ? 1u : 0u);
-                        mma_commit(&u_empty[slot]);
+                    mma_ss_chain8_two_slabs<L::kQSlab / 16, L::kSlab / 16>(d, a_lo, hi, b_lo, hi, idesc);
+                    if (half == 1) {
+                        const bool taken = T < 1 || mbar_test_wait(&p_full[buf ^ 1u], ((T + 1) >> 1 & 1u) ^ 1u), landed = mbar_test_wait(r_full, (T + 1) & 1u);
+                        early = taken && landed;
                     }
-                    mma_commit(&pv_done[Tp & 1u]);
-                    pv_new = pv.ends_piece();
-                    if (pv_new) { mma_commit(o_full); ++pieces; }
-                    pv.next(args);
-                    ++Tp;
-                    progress = true;
-                } else if (!qk.done() && Tq <= Tp + 1) {     // at most two score tiles: the older one's P has been taken
-                    const uint32_t qb = nq % L::kQBufs;
-                    if (part == 0) {
-                        const uint32_t slot = nr % L::kRopes;
-                        if (mbar_try_wait(&r_full[slot], (nr / L::kRopes) & 1u) &&
-                            (!qk_new || mbar_try_wait(&q_full[qb], (nq / L::kQBufs) & 1u))) {
-                            qk_new = false;
-                            tc_fence_after_sync();
-                            const uint32_t sq = smem_u32(smem + L::kQ + qb * 9 * L::kQSlab);
-                            const uint32_t sk = smem_u32(smem + L::kRope + slot * L::kSlab);
-#pragma unroll
-                            for (int kk = 0; kk < 4; ++kk)
-                                mma_ss(tmem_s + (Tq & 1u) * kDecKeys, desc_k_major(sq + kk * 32), desc_k_major(sk + kk * 32), idesc_qk, kk > 0 ? 1u : 0u);
-                            mma_commit(&r_empty[slot]);
-                            ++nr;
-                            part = 1;
-                            progress = true;
-                        }
-                    } else {
-                        const uint32_t slot = nu % L::kUnits;
-                        if (mbar_try_wait(&u_full[slot], (nu / L::kUnits) & 1u)) {
-                            tc_fence_after_sync();
-                            const uint32_t sq = smem_u32(smem + L::kQ + qb * 9 * L::kQSlab) + (2 * part - 1) * L::kQSlab;
-                            const uint32_t sk = smem_u32(smem + L::kUnit0 + slot * L::kUnit);
-#pragma unroll
-                            for (int kk = 0; kk < 8; ++kk)
-                                mma_ss(tmem_s + (Tq & 1u) * kDecKeys, desc_k_major(sq + (kk >> 2) * L::kQSlab + (kk & 3) * 32),
-                                       desc_k_major(sk + (kk >> 2) * L::kSlab + (kk & 3) * 32), idesc_qk, 1u);
-                            ++nu;
-                            progress = true;
-                            if (++part == 5) {
-                                part = 0;
-                                mma_commit(&s_full[Tq & 1u]);
-                                qk_new = qk.ends_piece();
-                                if (qk_new) { mma_commit(&q_empty[qb]); ++nq; }
-                                qk.next(args);
-                                ++Tq;
-                            }
-                        }
-                    }
+                    mma_ss_chain8_two_slabs<L::kQSlab / 16, L::kSlab / 16>(d, a_lo + 2 * L::kQSlab / 16, hi, b_lo + 2 * L::kSlab / 16, hi, idesc);
+                    a_lo += 4 * L::kQSlab / 16;
                 }
-                if (progress) {
-                    polls = 0;
-                } else if ((++polls & 0xffu) == 0u) {        // bounded, like every wait
-                    if (polls == 256u) t0 = global_timer_ns();
-                    if (abort_flag->value != 0u) break;
-                    if (global_timer_ns() - t0 > kWaitBudgetNs) {
-                        abort_flag->value = 1u;
-                        atomicCAS(args.status, kStatusOk, kStatusTimeout | 0xB4u);
-                        break;
-                    }
-                }
+                if (!ok) break;
+                mma_commit(&s_full[buf]);
+                if (new_piece) { mma_commit(q_empty); ++pieces; }
             }
             if (abort_flag->value != 0u) { mma_commit(quiesce_bar); mbar_wait_quiesce(quiesce_bar, 0); }
         }
-    } else {
+    } else if (warp == kDecValueWarp) {
+        // ---- issuer of the value MMAs ----------------------------------------------------------------------
+        if (elect_one()) {
+            constexpr uint32_t idesc = make_idesc_bf16(128, kHeads, 1, 0);
+            const uint32_t v_lo = desc_lo(desc_mn_major(smem_u32(smem + L::kHalf0), L::kSlab)), v_hi = desc_hi(desc_mn_major(0, L::kSlab)),
+                           p_lo = desc_lo(desc_k_major(smem_u32(smem + L::kP))), p_hi = desc_hi(desc_k_major(0));
+            uint32_t slot = 0, pieces = 0;
+            bool ok = true, new_piece = true;
+            DecodeCursor cur(args, my_tiles, first_b, first_t);
+            for (uint32_t T = 0; !cur.done(); ++T) {
+                const uint32_t buf = T & 1u;
+                const int k_steps = (cur.valid() + 15) >> 4;
+                ok = mbar_wait(&p_full[buf], (T >> 1) & 1u, abort_flag, args.status, 0xB6);
+                // the first tile of a piece overwrites O^T: the piece before it must have been drained
+                if (ok && new_piece && pieces > 0) ok = mbar_wait(o_free, (pieces - 1) & 1u, abort_flag, args.status, 0xB7);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t b_lo = p_lo + buf * (L::kPTile / 16);
+#pragma unroll 1
+                for (uint32_t half = 0; half < 2; ++half) {
+                    const uint32_t a_lo = v_lo + slot * (L::kHalf / 16), d = tmem_base + half * (2 * kHeads);
+                    if (k_steps == 4) {
+                        mma_ss_chain4_mn_k(d, a_lo, v_hi, b_lo, p_hi, idesc, new_piece ? 0u : 1u);
+                        mma_ss_chain4_mn_k(d + kHeads, a_lo + 2 * L::kSlab / 16, v_hi, b_lo, p_hi, idesc, new_piece ? 0u : 1u);
+                    } else {
+#pragma unroll 1
+                        for (int kk = 0; kk < 2 * k_steps; ++kk) {
+                            const int u = kk >= k_steps, k = kk - u * k_steps;
+                            mma_ss(d + u * kHeads, desc_of(a_lo + u * (2 * L::kSlab / 16) + k * 128, v_hi), desc_of(b_lo + k * 2, p_hi), idesc,
+                                   (!new_piece || k > 0) ? 1u : 0u);
+                        }
+                    }
+                    mma_commit(&h_empty[slot]);
+                    if (++slot == L::kHalves) slot = 0;
+                }
+                mma_commit(&pv_done[buf]);
+                new_piece = cur.ends_piece();
+                if (new_piece) { mma_commit(o_full); ++pieces; }
+                cur.next(args);
+            }
+            if (abort_flag->value != 0u) { mma_commit(quiesce_bar + 1); mbar_wait_quiesce(quiesce_bar + 1, 0); }
+        }
+    } else if (warp < 4) {
         // ---- softmax, rescaling, drain -------------------------------------------------------------------
-        const int row = warp * 32 + lane;                     // head within the group == TMEM lane
-        const bool softmax_warp = warp * 32 < kHeads;
-        const bool live = row < kHeads && head0 + row < args.h;
+        // Warp w owns heads 16w .. 16w+15 of the group (its sixteen lanes of the M = 64 score tile); thread l holds sixteen
+        // scores of head 16w + l/4 and sixteen of head 16w + l/4 + 8, so that a head's row is four neighbouring threads'.
+        const bool softmax_warp = warp * 16 < kHeads;
+        const int r0 = warp * 16 + (lane >> 2), r1 = r0 + 8;   // heads within the group
+        const bool live0 = head0 + r0 < args.h, live1 = head0 + r1 < args.h;
         const uint32_t lane_addr = static_cast<uint32_t>(warp * 32) << 16;
-        float m_run = -INFINITY, l_run = 0.f;
+        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;      // running maxima (log2 domain); this thread's part of the sums
         uint32_t T = 0, pieces = 0;
         bool ok = true, first = true;
         DecodeCursor cur(args, my_tiles, first_b, first_t);
@@ -406,57 +440,71 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
             tc_fence_after_sync();
             const int valid = cur.valid();
             if (softmax_warp) {
-                uint32_t sv[kDecKeys];
-                tmem_ld_x32(tmem_s + buf * kDecKeys + lane_addr, sv);
-                tmem_ld_x32(tmem_s + buf * kDecKeys + lane_addr + 32, sv + 32);
+                uint32_t sv[32];
+                tmem_ld_16x64(tmem_s + buf * kDecKeys + lane_addr, sv);
                 tmem_ld_wait();
                 if (valid < kDecKeys) {
 #pragma unroll
-                    for (int c = 0; c < kDecKeys; ++c)
-                        if (c >= valid) sv[c] = __float_as_uint(-INFINITY);
+                    for (int i = 0; i < 32; ++i)
+                        if ((i >> 2) * 8 + (lane & 3) * 2 + (i & 1) >= valid) sv[i] = __float_as_uint(-INFINITY);
                 }
-                float mx = __uint_as_float(sv[0]);
+                float x0[4], x1[4];
 #pragma unroll
-                for (int c = 1; c < kDecKeys - 1; c += 2) mx = fmax3(mx, __uint_as_float(sv[c]), __uint_as_float(sv[c + 1]));
-                mx = fmaxf(mx, __uint_as_float(sv[kDecKeys - 1]));
-                const float m_cand = fmaxf(m_run, mx * args.scale_log2);
-                const bool move = live && (m_cand - m_run) > 8.0f;        // lazy rescale: only when it fell behind by 2^8
-                const float m_new = (move || first) ? m_cand : m_run;
-                const float alpha = move && !first ? fast_exp2(m_run - m_new) : 1.0f;
-                m_run = m_new;
-                float sums[4] = {0.f, 0.f, 0.f, 0.f};
-                uint32_t pk[kDecKeys / 2];
-#pragma unroll
-                for (int c = 0; c < kDecKeys / 2; ++c) {
-                    const float p0 = fast_exp2(fmaf(__uint_as_float(sv[2 * c]), args.scale_log2, -m_new));
-                    const float p1 = fast_exp2(fmaf(__uint_as_float(sv[2 * c + 1]), args.scale_log2, -m_new));
-                    sums[c & 3] += p0 + p1;
-                    pk[c] = pack_bf16x2(p0, p1);
+                for (int e = 0; e < 4; ++e) {
+                    x0[e] = fmaxf(__uint_as_float(sv[8 * e]), __uint_as_float(sv[8 * e + 1]));
+                    x1[e] = fmaxf(__uint_as_float(sv[8 * e + 2]), __uint_as_float(sv[8 * e + 3]));
+                    x0[e] = fmax3(x0[e], __uint_as_float(sv[8 * e + 4]), __uint_as_float(sv[8 * e + 5]));
+                    x1[e] = fmax3(x1[e], __uint_as_float(sv[8 * e + 6]), __uint_as_float(sv[8 * e + 7]));
                 }
-                l_run = l_run * alpha + ((sums[0] + sums[1]) + (sums[2] + sums[3]));
-                if (row < kHeads) alpha_s[buf * kHeads + row] = alpha;
-                const bool any = __any_sync(0xffffffffu, move && !first);
+                float mx0 = fmaxf(fmax3(x0[0], x0[1], x0[2]), x0[3]), mx1 = fmaxf(fmax3(x1[0], x1[1], x1[2]), x1[3]);
+#pragma unroll
+                for (int d = 1; d < 4; d <<= 1) {
+                    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
+                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
+                }
+                const float c0 = fmaxf(m0, mx0 * args.scale_log2), c1 = fmaxf(m1, mx1 * args.scale_log2);
+                const bool move0 = live0 && (c0 - m0) > 8.0f, move1 = live1 && (c1 - m1) > 8.0f;   // lazy: only when it fell behind by 2^8
+                const float n0 = (move0 || first) ? c0 : m0, n1 = (move1 || first) ? c1 : m1;
+                const float f0 = move0 && !first ? fast_exp2(m0 - n0) : 1.0f, f1 = move1 && !first ? fast_exp2(m1 - n1) : 1.0f;
+                m0 = n0; m1 = n1;
+                const bool any = __any_sync(0xffffffffu, (move0 || move1) && !first);
+                if ((lane & 3) == 0) { alpha_s[buf * kHeads + r0] = f0; alpha_s[buf * kHeads + r1] = f1; }
                 if (lane == 0) moved_s[buf * 4 + warp] = any ? 1 : 0;
                 __syncwarp();
-                mbar_arrive(&a_full[buf]);
+                if (lane == 0) mbar_arrive(&a_full[buf]);
+                float s0[2] = {0.f, 0.f}, s1[2] = {0.f, 0.f};
+                uint32_t pk[16];                        // pk[2j], pk[2j+1]: columns 8j + 2(l%4), +1 of heads r0 and r1
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float a0 = fast_exp2(fmaf(__uint_as_float(sv[4 * j]), args.scale_log2, -n0));
+                    const float a1 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 1]), args.scale_log2, -n0));
+                    const float b0 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 2]), args.scale_log2, -n1));
+                    const float b1 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 3]), args.scale_log2, -n1));
+                    s0[j & 1] += a0 + a1;
+                    s1[j & 1] += b0 + b1;
+                    pk[2 * j] = pack_bf16x2(a0, a1);
+                    pk[2 * j + 1] = pack_bf16x2(b0, b1);
+                }
+                l0 = l0 * f0 + (s0[0] + s0[1]);
+                l1 = l1 * f1 + (s1[0] + s1[1]);
                 // P of the tile that used this buffer before has been multiplied
-                if (T >= L::kPBufs) {
-                    const uint32_t prev = T - L::kPBufs;
-                    ok = mbar_wait_warp(&pv_done[prev & 1u], (prev >> 1) & 1u, abort_flag, args.status, 0xC1);
+                if (T >= 2) {
+                    ok = mbar_wait_warp(&pv_done[buf], par ^ 1u, abort_flag, args.status, 0xC1);
                     if (!ok) break;
                 }
-                if (row < kHeads) {       // row of 128 bytes, 16-byte chunks swizzled like every operand tile
-                    uint8_t* dst = smem + L::kP + (T % L::kPBufs) * L::kPTile + row * 128;
+                // rows of 128 bytes (64 keys of a head), 16-byte chunks swizzled like every operand tile; blocks: heads 0..7 and 8..15 of the
+                // warp, key groups 2j and 2j + 1
+                const int prow = warp * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
+                const uint32_t pbase = smem_u32(smem + L::kP + buf * L::kPTile) + prow * 128;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        *reinterpret_cast<uint4*>(dst + ((c ^ (row & 7)) << 4)) = make_uint4(pk[4 * c], pk[4 * c + 1], pk[4 * c + 2], pk[4 * c + 3]);
-                }
+                for (int j = 0; j < 4; ++j)
+                    stmatrix_x4(pbase + (((2 * j + (lane >> 4)) ^ (lane & 7)) << 4), pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
             }
             ok = mbar_wait_warp(&a_full[buf], par, abort_flag, args.status, 0xC4);    // factors and flags are written
             if (!ok) break;
             bool moved = false;
 #pragma unroll
-            for (int w = 0; w * 32 < kHeads; ++w) moved |= moved_s[buf * 4 + w] != 0;
+            for (int w = 0; w * 16 < kHeads; ++w) moved |= moved_s[buf * 4 + w] != 0;
             if (moved) {
                 // O^T is at rest once P.V of the previous tile has completed; this tile's waits for p_full below
                 const uint32_t prev = T - 1;
@@ -478,14 +526,15 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 const int n_zero = 16 - (valid & 15);
                 for (int i = threadIdx.x; i < 8 * 8 * n_zero; i += 128) {       // 8 slabs x rows x eight 16-byte chunks
                     const int slab = i / (8 * n_zero), r = valid + (i >> 3) % n_zero;
-                    const uint32_t slot = (4 * T + (slab >> 1)) % L::kUnits;
-                    *reinterpret_cast<uint4*>(smem + L::kUnit0 + slot * L::kUnit + (slab & 1) * L::kSlab + r * 128 + (i & 7) * 16) =
+                    const uint32_t slot = (2 * T + (slab >> 2)) % L::kHalves;
+                    *reinterpret_cast<uint4*>(smem + L::kHalf0 + slot * L::kHalf + (slab & 3) * L::kSlab + r * 128 + (i & 7) * 16) =
                         make_uint4(0u, 0u, 0u, 0u);
                 }
             }
             fence_async_shared();
             tc_fence_before_sync();
-            mbar_arrive(&p_full[buf]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[buf]);
             first = false;
             const bool ends = cur.ends_piece();
             if (ends) {
@@ -493,10 +542,10 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 if (!ok) break;
                 tc_fence_after_sync();
                 const size_t slot = static_cast<size_t>(cta) + cur.b;
-                float* dst = args.part_o + (slot * args.h_pad + head0) * kDecLat + row;
+                float* dst = args.part_o + (slot * args.h_pad + head0) * kDecLat + warp * 32 + lane;
                 const int n_heads = min(kHeads, args.h - head0);
 #pragma unroll 1
-                for (int c = 0; c < 4 * kHeads; c += 16) {    // latents (c / kHeads) * 128 + row of heads c % kHeads ..
+                for (int c = 0; c < 4 * kHeads; c += 16) {    // latents (c / kHeads) * 128 + TMEM lane of heads c % kHeads ..
                     uint32_t o[16];
                     tmem_ld_x16(tmem_base + lane_addr + c, o);
                     tmem_ld_wait();
@@ -504,55 +553,286 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     for (int v = 0; v < 16; ++v)
                         if ((c % kHeads) + v < n_heads) dst[static_cast<size_t>((c % kHeads) + v) * kDecLat + (c / kHeads) * 128] = __uint_as_float(o[v]);
                 }
-                if (live) args.part_ml[slot * args.h_pad + head0 + row] = make_float2(m_run, l_run);
+                if (softmax_warp) {
+#pragma unroll
+                    for (int d = 1; d < 4; d <<= 1) {
+                        l0 += __shfl_xor_sync(0xffffffffu, l0, d);
+                        l1 += __shfl_xor_sync(0xffffffffu, l1, d);
+                    }
+                    float2* ml = args.part_ml + slot * args.h_pad + head0;
+                    if ((lane & 3) == 0 && live0) ml[r0] = make_float2(m0, l0);
+                    if ((lane & 3) == 0 && live1) ml[r1] = make_float2(m1, l1);
+                }
                 tc_fence_before_sync();
-                mbar_arrive(o_free);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(o_free);
                 ++pieces;
-                m_run = -INFINITY; l_run = 0.f;
+                m0 = m1 = -INFINITY; l0 = l1 = 0.f;
                 first = true;
             }
             cur.next(args);
             ++T;
         }
     }
+    grid_dependency_wait();          // a CTA without work too: this kernel's completion stands for the one before it
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 5) { tc_fence_after_sync(); tmem_dealloc(tmem_base, 512); }
+    if (warp == kDecScoreWarp) { tc_fence_after_sync(); tmem_dealloc(*tmem_slot, 512); }
 }
 
-// Joins the pieces of one (request, head): o_lat = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c, rounded once to bf16
-// for the value projection's tensor-core product.  A request without tokens has no piece: zeros, LSE -inf.
-__global__ void __launch_bounds__(128)
-decode_combine_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const int* __restrict__ tile_start,
-                      int B, int h, int h_pad, int ctas_per_group, __nv_bfloat16* __restrict__ o_lat, float* __restrict__ lse) {
+// q_abs[b, i, :] = W_uk[i] q_nope[b, i, :] for a tile of kRequests requests: D[128 latents x requests] = W_uk (A: rows = latents,
+// K-major as it lies) . q^T (B: rows = requests), eight MMAs.  The weights are the M side, so a small batch pads
+// nothing but the result's columns, and 4 * h CTAs share the read of W_uk.  First kernel of the call: clears the status slot.
+constexpr int kAbsorbThreads = 128;
+template <int kRequests>
+struct DecodeAbsorbSmem {
+    static constexpr int kW = 0;                                 // two slabs of 128 rows x 64 channels
+    static constexpr int kQ = kW + 2 * 128 * 128;                // two slabs of kRequests rows
+    static constexpr int kBar = kQ + 2 * kRequests * 128;
+    static constexpr int kTotalBytes = kBar + 32;
+};
+template <int kRequests>
+__global__ void __launch_bounds__(kAbsorbThreads)
+decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, int B, int h,
+                     __nv_bfloat16* __restrict__ q_abs, unsigned* status, int status_words) {
+    using L = DecodeAbsorbSmem<kRequests>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
+    uint64_t* done = full + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 2);
+    AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int c0 = blockIdx.x * 128, head = blockIdx.y, b0 = blockIdx.z * kRequests;
+    constexpr uint32_t kCols = kRequests < 32 ? 32 : kRequests;
+    // the status slot, before any kernel of the call can write to it: the attention kernel starts once every CTA has come by the
+    // launch signal below, and no wait of this kernel gives up within two seconds
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < status_words) {
+        status[threadIdx.x] = 0u;
+        __threadfence();
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(full, 1); mbar_init(done, 1);
+        abort_flag->value = 0;
+        mbar_fence_init();
+    }
+    if (warp == 0) { tmem_alloc(tmem_slot, kCols); tmem_relinquish(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    grid_launch_dependents();
+    const uint32_t tmem = *tmem_slot;
+    if (warp == 0) {
+        if (elect_one()) {
+            mbar_arrive_expect_tx(full, 2 * 128 * 128 + 2 * kRequests * 128);
+            for (int k = 0; k < 2; ++k) {
+                tma_load_2d_chk(status, smem + L::kW + k * 128 * 128, &tmap_w, full, head * 256 + k * 64, c0);
+                tma_load_2d_chk(status, smem + L::kQ + k * kRequests * 128, &tmap_q, full, head * 192 + k * 64, b0);
+            }
+            if (mbar_wait(full, 0, abort_flag, status, 0xB9)) {
+                tc_fence_after_sync();
+                constexpr uint32_t idesc = make_idesc_bf16(128, kRequests, 0, 0);
+                const uint64_t da = desc_k_major(smem_u32(smem + L::kW)), db = desc_k_major(smem_u32(smem + L::kQ));
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                    mma_ss(tmem, da + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, db + (kk >> 2) * (kRequests * 128 / 16) + (kk & 3) * 2, idesc,
+                           kk > 0 ? 1u : 0u);
+                mma_commit(done);
+            } else {
+                mbar_wait_quiesce(full, 0);
+            }
+        }
+        __syncwarp();
+    }
+    if (mbar_wait_warp(done, 0, abort_flag, status, 0xBA)) {
+        tc_fence_after_sync();
+        const uint32_t lane_addr = static_cast<uint32_t>(warp * 32) << 16;
+#pragma unroll 1
+        for (int c = 0; c < kRequests && b0 + c < B; c += 16) {
+            uint32_t v[16];
+            tmem_ld_x16(tmem + lane_addr + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (b0 + c + r < B)
+                    q_abs[(static_cast<size_t>(b0 + c + r) * h + head) * kDecLat + c0 + warp * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[r]));
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) { tc_fence_after_sync(); tmem_dealloc(tmem, kCols); }
+}
+
+// Joins the pieces of each (request, head) and carries the result to the value dimension:
+//     o[c] = sum_p 2^(m_p - M) o_p[c] / sum_p 2^(m_p - M) l_p,      out[v] = sum_c W_uv[c, v] o[c]
+// One CTA per head and up to 16 requests: D[128 values x 32] = W_uv^T (A, MN-major, 512 rows of the weights as they lie) . o^T (B).  o is
+// fp32; rounded to bf16 it would cost as much accuracy as the result's own rounding, so B holds it in two parts, hi = bf16(o)
+// in rows 0..15 and lo = bf16(o - hi) in rows 16..31 -- columns that the MMA computes in the time of sixteen -- and the two
+// halves of D are added.  The weights' tile is requested before this kernel waits for the attention kernel (nothing in the
+// call writes them); the pieces are read by groups of 128 threads, one request each, or all four groups on one request
+// where a long context left more than kCombineSplit pieces of it.
+// A request without tokens has no piece: zeros, LSE -inf.
+constexpr int kProjectThreads = 512;
+constexpr int kCombineSplit = 8;
+struct DecodeProjectSmem {
+    static constexpr int kW = 0;                                 // two slabs of 512 rows x 64 values
+    static constexpr int kWSlab = 512 * 128;
+    static constexpr int kO = kW + 2 * kWSlab;                   // eight slabs of 32 rows x 64 latents
+    static constexpr int kOSlab = 32 * 128;
+    static constexpr int kRed = kO + 8 * kOSlab;                 // [4][512] floats
+    static constexpr int kBar = kRed + 4 * 512 * 4;
+    static constexpr int kTotalBytes = kBar + 32;
+};
+__global__ void __launch_bounds__(kProjectThreads, 1)
+decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
+                      const int* __restrict__ tile_start, int B, int h, int h_pad, int ctas_per_group, int requests_per_cta,
+                      __nv_bfloat16* __restrict__ out, float* __restrict__ lse, unsigned* status) {
+    using L = DecodeProjectSmem;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
+    uint64_t* done = full + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 2);
+    AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
+    float* red = reinterpret_cast<float*>(smem + L::kRed);
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int head = blockIdx.x, b0 = blockIdx.y * requests_per_cta, n_req = min(requests_per_cta, B - b0);
+    if (threadIdx.x == 0) {
+        mbar_init(full, 1); mbar_init(done, 1);
+        abort_flag->value = 0;
+        mbar_fence_init();
+        mbar_arrive_expect_tx(full, 2 * L::kWSlab);
+        for (int k = 0; k < 4; ++k)                              // slab k / 2, rows 256 (k % 2) ..
+            tma_load_2d_chk(status, smem + L::kW + k * (L::kWSlab / 2), &tmap_wv, full, head * 256 + (k >> 1) * 64, (k & 1) * 256);
+    }
+    if (warp == 0) { __syncwarp(); tmem_alloc(tmem_slot, 32); tmem_relinquish(); }
+    // rows of B that no request fills: zero (their columns of D are never read, but nothing uninitialised should be multiplied)
+    for (int i = threadIdx.x; i < 8 * 32 * 8; i += kProjectThreads)
+        *reinterpret_cast<uint4*>(smem + L::kO + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
     grid_launch_dependents();
     grid_dependency_wait();
-    const int b = blockIdx.x / h, head = blockIdx.x - b * h;
-    const int total = tile_start[B], begin = tile_start[b], end = tile_start[b + 1];
+
+    const int group = warp >> 2, cg = threadIdx.x & 127;         // thread's four channels: 4 cg ..
+    const int total = tile_start[B];
     const int per = max(1, (total + ctas_per_group - 1) / ctas_per_group);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float M = -INFINITY, l = 0.f;
-    if (end > begin) {
-        const int c0 = begin / per, c1 = (end - 1) / per;
-        for (int c = c0; c <= c1; ++c) {
+    // weighted sum over pieces first + skip, first + skip + step, ... of request b; M and the full l on every thread
+    auto gather = [&](int b, int first, int last, int skip, int step, float& M, float& l) -> float4 {
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        M = -INFINITY; l = 0.f;
+        for (int c = first + lane; c <= last; c += 32) {
             const float m = part_ml[static_cast<size_t>(c + b) * h_pad + head].x;
-            M = c == c0 ? m : fmaxf(M, m);
+            M = fmaxf(M, m);
         }
-        for (int c = c0; c <= c1; ++c) {
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        for (int c = first + lane; c <= last; c += 32) {
+            const float2 ml = part_ml[static_cast<size_t>(c + b) * h_pad + head];
+            l = fmaf(ml.y, fast_exp2(ml.x - M), l);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+#pragma unroll 4
+        for (int c = first + skip; c <= last; c += step) {
             const size_t at = static_cast<size_t>(c + b) * h_pad + head;
-            const float2 ml = part_ml[at];
-            const float w = fast_exp2(ml.x - M);
-            const float4 o = reinterpret_cast<const float4*>(part_o + at * kDecLat)[threadIdx.x];
-            l = fmaf(ml.y, w, l);
+            const float w = fast_exp2(part_ml[at].x - M);
+            const float4 o = reinterpret_cast<const float4*>(part_o + at * kDecLat)[cg];
             acc.x = fmaf(o.x, w, acc.x); acc.y = fmaf(o.y, w, acc.y);
             acc.z = fmaf(o.z, w, acc.z); acc.w = fmaf(o.w, w, acc.w);
         }
-        const float inv = 1.0f / l;
-        acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+        return acc;
+    };
+    auto store = [&](int r, float4 o, float inv) {               // both parts of request r's row, swizzled
+        const float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+        float rest[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rest[e] = x[e] - __bfloat162float(__float2bfloat16_rn(x[e]));
+        uint8_t* slab = smem + L::kO + (cg >> 4) * L::kOSlab;    // 16 threads of four channels per slab
+        const int chunk = (cg & 15) >> 1, in_chunk = (cg & 1) * 8;
+        *reinterpret_cast<uint2*>(slab + r * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+        *reinterpret_cast<uint2*>(slab + (16 + r) * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) =
+            make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
+    };
+    for (int r0 = 0; r0 < n_req; r0 += 4) {
+        int first[4], last[4], most = 0;                         // pieces of the four requests (last < first: none)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int b = b0 + r0 + g;
+            const int begin = r0 + g < n_req ? tile_start[b] : 0, end = r0 + g < n_req ? tile_start[b + 1] : 0;
+            first[g] = begin / per;
+            last[g] = end > begin ? (end - 1) / per : first[g] - 1;
+            most = max(most, last[g] - first[g] + 1);
+        }
+        if (most <= kCombineSplit) {
+            int f = first[0], e = last[0];
+#pragma unroll
+            for (int g = 1; g < 4; ++g)
+                if (group == g) { f = first[g]; e = last[g]; }
+            const int r = r0 + group;
+            if (r < n_req) {
+                float M = -INFINITY, l = 0.f;
+                const float4 o = gather(b0 + r, f, e, 0, 1, M, l);
+                const bool any = e >= f;
+                store(r, o, any ? 1.0f / l : 0.f);
+                if (lse != nullptr && cg == 0) lse[static_cast<size_t>(b0 + r) * h + head] = any ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            }
+        } else {
+#pragma unroll 1
+            for (int g = 0; g < 4 && r0 + g < n_req; ++g) {
+                float M, l;
+                const float4 mine = gather(b0 + r0 + g, first[g], last[g], group, 4, M, l);
+                __syncthreads();                                 // the sums of the request before have been read
+                reinterpret_cast<float4*>(red)[group * 128 + cg] = mine;
+                __syncthreads();
+                if (group == g) {
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 x = reinterpret_cast<const float4*>(red)[k * 128 + cg];
+                        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+                    }
+                    const bool any = last[g] >= first[g];
+                    store(r0 + g, o, any ? 1.0f / l : 0.f);
+                    if (lse != nullptr && cg == 0)
+                        lse[static_cast<size_t>(b0 + r0 + g) * h + head] = any ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                }
+            }
+        }
     }
-    reinterpret_cast<uint2*>(o_lat + static_cast<size_t>(blockIdx.x) * kDecLat)[threadIdx.x] =
-        make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-    if (lse != nullptr && threadIdx.x == 0) lse[blockIdx.x] = end > begin ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    fence_async_shared();
+    __syncthreads();
+    if (warp == 0) {
+        if (elect_one()) {
+            if (mbar_wait(full, 0, abort_flag, status, 0xBB)) {
+                tc_fence_after_sync();
+                constexpr uint32_t idesc = make_idesc_bf16(128, 32, 1, 0);
+                const uint32_t a_lo = desc_lo(desc_mn_major(smem_u32(smem + L::kW), L::kWSlab)), a_hi = desc_hi(desc_mn_major(0, L::kWSlab)),
+                               b_lo = desc_lo(desc_k_major(smem_u32(smem + L::kO))), b_hi = desc_hi(desc_k_major(0));
+#pragma unroll 1
+                for (uint32_t s = 0; s < 8; ++s)                 // 64 latents: four steps of 16 rows of W_uv
+                    mma_ss_chain4_mn_k(tmem, a_lo + s * (64 * 128 / 16), a_hi, b_lo + s * (L::kOSlab / 16), b_hi, idesc, s > 0 ? 1u : 0u);
+                mma_commit(done);
+            } else {
+                mbar_wait_quiesce(full, 0);
+            }
+        }
+        __syncwarp();
+    }
+    if (warp < 4 && mbar_wait_warp(done, 0, abort_flag, status, 0xBC)) {
+        tc_fence_after_sync();
+        uint32_t v[32];
+        tmem_ld_x32(tmem + (static_cast<uint32_t>(warp * 32) << 16), v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (r < n_req)
+                out[(static_cast<size_t>(b0 + r) * h + head) * 128 + warp * 32 + lane] =
+                    __float2bfloat16_rn(__uint_as_float(v[r]) + __uint_as_float(v[16 + r]));
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) { tc_fence_after_sync(); tmem_dealloc(tmem, 32); }
 }
 
 }  // namespace laga

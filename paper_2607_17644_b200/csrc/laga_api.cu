@@ -75,6 +75,20 @@ bool make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t inner_elems, ui
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The latent cache as (64 channels) x rows x (nine groups of 64 channels): a box of box_groups groups of box_rows rows lands in
+// shared memory as that many slabs, 128-byte swizzled like every operand tile.
+bool make_tmap_cache(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows, uint32_t box_groups) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {64u, rows, kDecRow / 64};
+    cuuint64_t strides[2] = {kDecRow * 2, 128u};
+    cuuint32_t box[3] = {64u, box_rows, box_groups};
+    cuuint32_t estr[3] = {1u, 1u, 1u};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // ---- launch status slot ---------------------------------------------------------------------------
 // The first kStatusBytes of every workspace: word 0 is the device status word; the work counters of the
 // persistent attention kernels and their clock probes follow.  The first kStatusClearBytes (all of
@@ -138,6 +152,8 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_decode_sm100_kernel<16>, AttnDecodeSmem<16>::kTotalBytes) &&
               allow_smem(attn_decode_sm100_kernel<32>, AttnDecodeSmem<32>::kTotalBytes) &&
               allow_smem(attn_decode_sm100_kernel<64>, AttnDecodeSmem<64>::kTotalBytes) &&
+              allow_smem(decode_absorb_kernel<64>, DecodeAbsorbSmem<64>::kTotalBytes) &&
+              allow_smem(decode_project_kernel, DecodeProjectSmem::kTotalBytes) &&
               allow_smem(cache_plan_kernel, 2 * (kPlanMaxRequests + 1) * static_cast<int>(sizeof(int)));
     if (ok) {
         // The fused backward assigns work to pairs statically, so its grid must not exceed the pairs the
@@ -225,8 +241,10 @@ struct TmapKey {
     const void* base;
     uint64_t inner, rows, stride;
     uint32_t box_rows;
+    uint32_t cache_groups;      // 0: a 2-d map; else a cache map with this many channel groups in its box
     bool operator==(const TmapKey& o) const {
-        return base == o.base && inner == o.inner && rows == o.rows && stride == o.stride && box_rows == o.box_rows;
+        return base == o.base && inner == o.inner && rows == o.rows && stride == o.stride && box_rows == o.box_rows &&
+               cache_groups == o.cache_groups;
     }
 };
 struct TmapCache {
@@ -240,12 +258,14 @@ struct TmapCache {
 TmapCache g_tmaps;
 
 bool cached_tmap_bf16(CUtensorMap* map, const void* base, uint64_t inner_elems, uint64_t rows, uint64_t row_stride_bytes,
-                      uint32_t box_rows) {
-    const TmapKey key{base, inner_elems, rows, row_stride_bytes, box_rows};
+                      uint32_t box_rows, uint32_t cache_groups = 0) {
+    const TmapKey key{base, inner_elems, rows, row_stride_bytes, box_rows, cache_groups};
     std::lock_guard<std::mutex> lock(g_tmaps.mutex);
     for (int i = 0; i < TmapCache::kEntries; ++i)
         if (g_tmaps.used[i] && g_tmaps.keys[i] == key) { *map = g_tmaps.maps[i]; return true; }
-    if (!make_tmap_bf16(map, base, inner_elems, rows, row_stride_bytes, box_rows)) return false;
+    if (!(cache_groups ? make_tmap_cache(map, base, rows, box_rows, cache_groups)
+                       : make_tmap_bf16(map, base, inner_elems, rows, row_stride_bytes, box_rows)))
+        return false;
     const int slot = g_tmaps.next;
     g_tmaps.next = (slot + 1) % TmapCache::kEntries;
     g_tmaps.keys[slot] = key;
@@ -700,7 +720,7 @@ int page_shift_of(int page) {                        // log2 of a supported page
 
 struct DecodeLayout {
     int heads, n_groups, ctas_per_group, h_pad, slots;
-    size_t q_abs, o_lat, part_o, part_ml, tile_start, total;
+    size_t q_abs, part_o, part_ml, tile_start, total;
 };
 DecodeLayout decode_layout(int B, int h) {
     DecodeLayout w;
@@ -714,12 +734,23 @@ DecodeLayout decode_layout(int B, int h) {
     const size_t lat_bytes = align_up(static_cast<size_t>(B) * h * kDc * 2, 1024);
     const size_t rows = static_cast<size_t>(w.slots) * w.h_pad;
     w.q_abs = kStatusBytes;
-    w.o_lat = w.q_abs + lat_bytes;
-    w.part_o = w.o_lat + lat_bytes;
+    w.part_o = w.q_abs + lat_bytes;
     w.part_ml = w.part_o + rows * kDecLat * sizeof(float);
     w.tile_start = w.part_ml + align_up(rows * sizeof(float2), 1024);
     w.total = w.tile_start + align_up((static_cast<size_t>(B) + 1) * sizeof(int), 1024);
     return w;
+}
+
+template <int kRequests>
+int launch_decode_absorb(const void* q, const void* w, int B, int h, void* q_abs, unsigned* status, cudaStream_t stream) {
+    const uint64_t q_row = static_cast<uint64_t>(h) * (kDn + kDr), w_row = static_cast<uint64_t>(h) * (kDn + kDv);
+    CUtensorMap tw, tq;
+    if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, kRequests))
+        return LAGA_ERR_CUDA;
+    launch_kernel(decode_absorb_kernel<kRequests>, dim3(kDc / 128, h, (B + kRequests - 1) / kRequests), dim3(kAbsorbThreads),
+                  DecodeAbsorbSmem<kRequests>::kTotalBytes, stream, false, tw, tq, B, h, static_cast<__nv_bfloat16*>(q_abs), status,
+                  static_cast<int>(kStatusClearBytes / sizeof(unsigned)));
+    return launch_status();
 }
 
 template <int kHeads>
@@ -727,14 +758,29 @@ int launch_attn_decode(const void* q, const void* q_abs, const void* cache, long
                        cudaStream_t stream) {
     const uint64_t q_rows = static_cast<uint64_t>(a.B) * a.h;
     const int box = a.page_shift < 6 ? 1 << a.page_shift : kDecKeys;
-    CUtensorMap tqa, tq, tc;
+    CUtensorMap tqa, tq, tr, tl;
     if (!cached_tmap_bf16(&tqa, q_abs, kDc, q_rows, kDc * 2, kHeads) ||
         !cached_tmap_bf16(&tq, q, kDn + kDr, q_rows, (kDn + kDr) * 2, kHeads) ||
-        !cached_tmap_bf16(&tc, cache, kDecRow, static_cast<uint64_t>(cache_rows), kDecRow * 2, static_cast<uint32_t>(box)))
+        !cached_tmap_bf16(&tr, cache, kDecRow, static_cast<uint64_t>(cache_rows), kDecRow * 2, static_cast<uint32_t>(box), 1) ||
+        !cached_tmap_bf16(&tl, cache, kDecRow, static_cast<uint64_t>(cache_rows), kDecRow * 2, static_cast<uint32_t>(box), 4))
         return LAGA_ERR_CUDA;
     ScopedKernelEvents ev(LAGA_KERNEL_ATTN_DECODE, stream);
     launch_kernel(attn_decode_sm100_kernel<kHeads>, dim3(static_cast<unsigned>(a.n_groups * a.ctas_per_group)), dim3(kDecThreads),
-                  AttnDecodeSmem<kHeads>::kTotalBytes, stream, true, tqa, tq, tc, a);
+                  AttnDecodeSmem<kHeads>::kTotalBytes, stream, true, tqa, tq, tr, tl, a);
+    return launch_status();
+}
+
+int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, float* lse, cudaStream_t stream) {
+    const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv);
+    CUtensorMap tw;      // starts at W's column d_nope: column 0 of the map is V channel 0 of head 0
+    if (!cached_tmap_bf16(&tw, static_cast<const uint8_t*>(w) + kDn * 2, w_row - kDn, kDc, w_row * 2, 256)) return LAGA_ERR_CUDA;
+    // Requests per CTA: the fewest of 4, 8 and 16 that still fit one wave.  Each CTA reads its head's 128 KB of W_uv, but joining
+    // pieces is what takes time, and four requests at a time is what a CTA's threads do at once.
+    int per_cta = 4;
+    while (per_cta < 16 && static_cast<long long>(a.h) * ((a.B + per_cta - 1) / per_cta) > sm_count()) per_cta *= 2;
+    launch_kernel(decode_project_kernel, dim3(a.h, (a.B + per_cta - 1) / per_cta), dim3(kProjectThreads), DecodeProjectSmem::kTotalBytes, stream,
+                  true, tw, static_cast<const float*>(a.part_o), static_cast<const float2*>(a.part_ml), static_cast<const int*>(a.tile_start),
+                  a.B, a.h, a.h_pad, a.ctas_per_group, per_cta, static_cast<__nv_bfloat16*>(out), lse, a.status);
     return launch_status();
 }
 
@@ -1382,7 +1428,7 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
     // rows, keys and tiles are counted in 32 bits (byte offsets are not)
     const long long rows = static_cast<long long>(n_pages) << shift, capacity = static_cast<long long>(columns) << shift;
     if (rows > (1ll << 30) || capacity > (1ll << 30) || ((capacity + kDecKeys - 1) / kDecKeys) * B > 0x7fffffffll ||
-        static_cast<long long>(B) * h > (1ll << 26))
+        static_cast<long long>(B) * h > (1ll << 26) || h > 65535 || B > 65535 * 4)
         return LAGA_ERR_INVALID_ARG;
     const DecodeLayout w = decode_layout(B, h);
     if (workspace_bytes < w.total) return LAGA_ERR_WORKSPACE_TOO_SMALL;
@@ -1393,8 +1439,10 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t* base = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(base);
-    if ((rc = zero_status(status, st)) != LAGA_OK) return rc;
-    if ((rc = launch_q_absorb(q, w_kv_b, B, h, base + w.q_abs, status, st)) != LAGA_OK) return rc;
+    // tiles of 16 requests for the smallest batches, of 64 otherwise (a CTA reads its 32 KB of W_uk once per tile)
+    rc = B <= 16 ? launch_decode_absorb<16>(q, w_kv_b, B, h, base + w.q_abs, status, st)
+                 : launch_decode_absorb<64>(q, w_kv_b, B, h, base + w.q_abs, status, st);
+    if (rc != LAGA_OK) return rc;
     const AttnDecodeArgs a{B, h, w.n_groups, w.ctas_per_group, softmax_scale * 1.4426950408889634f, seq_lens, block_table, columns, shift,
                            n_pages, reinterpret_cast<float*>(base + w.part_o), reinterpret_cast<float2*>(base + w.part_ml), w.h_pad,
                            reinterpret_cast<int*>(base + w.tile_start), status};
@@ -1402,10 +1450,7 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
     else if (w.heads == 32) rc = launch_attn_decode<32>(q, base + w.q_abs, cache, rows, a, st);
     else rc = launch_attn_decode<64>(q, base + w.q_abs, cache, rows, a, st);
     if (rc != LAGA_OK) return rc;
-    launch_kernel(decode_combine_kernel, dim3(static_cast<unsigned>(B) * h), dim3(128), 0, st, true, a.part_o, a.part_ml, a.tile_start, B, h,
-                  w.h_pad, w.ctas_per_group, reinterpret_cast<__nv_bfloat16*>(base + w.o_lat), lse);
-    if ((rc = launch_status()) != LAGA_OK) return rc;
-    return launch_v_project(base + w.o_lat, w_kv_b, B, h, out, status, st);
+    return launch_decode_project(w_kv_b, a, out, lse, st);
 }
 
 }  // extern "C"

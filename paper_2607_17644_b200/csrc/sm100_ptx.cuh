@@ -69,6 +69,20 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
     return done != 0;
 }
 
+// The same question without waiting for the answer to become yes: try_wait may suspend the thread for a while first, which is what a
+// waiting thread wants and a thread that has other work to look at does not.
+__device__ __forceinline__ bool mbar_test_wait(uint64_t* bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+
 // Shared by every role of a CTA: once set, all later waits return at once so the CTA can unwind.
 struct AbortFlag {
     volatile uint32_t value;
@@ -177,6 +191,14 @@ __device__ __forceinline__ void tma_load_2d(void* smem_dst, const CUtensorMap* m
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
         ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y)
+        : "memory");
+}
+
+// x, y, z: coordinates in a 3-d map, innermost first.
+__device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
         : "memory");
 }
 
@@ -429,8 +451,50 @@ __device__ __forceinline__ void mma_ts_chain8_k128(uint32_t d_tmem, uint32_t a_t
         ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(bar0), "r"(bar1)
         : "memory");
 }
+// The chains of the decode kernel: both operands in shared memory, offsets of A and B apart.
+#define LAGA_MMA_SS_STEP2(AOFF, BOFF, P)                                                                              \
+    "add.u32 lo, %1, " AOFF ";\n\tmov.b64 da, {lo, %2};\n\tadd.u32 lo, %3, " BOFF ";\n\tmov.b64 db, {lo, %4};\n\t"  \
+    "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, " P ";\n\t"
+// S = Q K^T over one 64-channel slab, both K-major (four steps of 32 bytes = 2 descriptor units): overwrites D.
+__device__ __forceinline__ void mma_ss_chain4_first(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                                    uint32_t idesc) {
+    asm volatile(
+        "{\n\t.reg .pred p0, p1;\n\t.reg .b32 lo;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t"
+        LAGA_MMA_SS_STEP2("0", "0", "p0") LAGA_MMA_SS_STEP2("2", "2", "p1") LAGA_MMA_SS_STEP2("4", "4", "p1") LAGA_MMA_SS_STEP2("6", "6", "p1")
+        "}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc)
+        : "memory");
+}
+// S += Q K^T over two slabs, kASlab and kBSlab descriptor units apart (eight steps).
+template <int kASlab, int kBSlab>
+__device__ __forceinline__ void mma_ss_chain8_two_slabs(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                                        uint32_t idesc) {
+    asm volatile(
+        "{\n\t.reg .pred p1;\n\t.reg .b32 lo;\n\t.reg .b64 da, db;\n\t"
+        "setp.eq.b32 p1, 0, 0;\n\t"
+        LAGA_MMA_SS_STEP2("0", "0", "p1") LAGA_MMA_SS_STEP2("2", "2", "p1") LAGA_MMA_SS_STEP2("4", "4", "p1") LAGA_MMA_SS_STEP2("6", "6", "p1")
+        LAGA_MMA_SS_STEP2("%6", "%7", "p1") LAGA_MMA_SS_STEP2("%6 + 2", "%7 + 2", "p1")
+        LAGA_MMA_SS_STEP2("%6 + 4", "%7 + 4", "p1") LAGA_MMA_SS_STEP2("%6 + 6", "%7 + 6", "p1")
+        "}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "n"(kASlab), "n"(kBSlab)
+        : "memory");
+}
+// D (+)= A B: A MN-major (16 rows of K = 2048 bytes = 128 units per step), B K-major (2 units per step), four steps;
+// accumulate_first == 0 overwrites D.
+__device__ __forceinline__ void mma_ss_chain4_mn_k(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                                   uint32_t idesc, uint32_t accumulate_first) {
+    asm volatile(
+        "{\n\t.reg .pred p0, p1;\n\t.reg .b32 lo;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p0, %6, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t"
+        LAGA_MMA_SS_STEP2("0", "0", "p0") LAGA_MMA_SS_STEP2("128", "2", "p1") LAGA_MMA_SS_STEP2("256", "4", "p1") LAGA_MMA_SS_STEP2("384", "6", "p1")
+        "}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate_first)
+        : "memory");
+}
 __device__ __forceinline__ uint32_t desc_lo(uint64_t desc) { return static_cast<uint32_t>(desc); }
 __device__ __forceinline__ uint32_t desc_hi(uint64_t desc) { return static_cast<uint32_t>(desc >> 32); }
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo, uint32_t hi) { return (static_cast<uint64_t>(hi) << 32) | lo; }
 
 // Arrive (count 1) on `bar` once every MMA this thread issued so far has completed.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
@@ -471,6 +535,27 @@ __device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t* r) {
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr)
         : "memory");
+}
+// Sixteen TMEM lanes x 64 columns over all 32 threads of the warp: thread l holds, for each group j of eight columns,
+// r[4j], r[4j+1] = columns 8j + 2(l % 4), + 1 of lane l / 4, and r[4j+2], r[4j+3] = the same of lane l / 4 + 8.
+__device__ __forceinline__ void tmem_ld_16x64(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+          "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+          "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
+          "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+// Four 8 x 8 blocks of 16-bit values to shared memory: thread l holds in v[i] the pair of columns 2(l % 4), + 1 of row l / 4 of
+// block i; threads 8i .. 8i+7 give the addresses of block i's rows (16 bytes each).
+__device__ __forceinline__ void stmatrix_x4(uint32_t addr, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v0), "r"(v1), "r"(v2), "r"(v3)
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
     asm volatile(
