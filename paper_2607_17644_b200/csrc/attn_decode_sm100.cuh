@@ -142,7 +142,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
     int* scan = start_b + 2;                          // [6] per-warp sums of the tile counts
     static_assert(2 * L::kHalves + 4 + 12 <= 36, "barriers overlap the scalars");
     float* alpha_s = reinterpret_cast<float*>(smem + L::kAlpha);
-    volatile int* moved_s = reinterpret_cast<volatile int*>(alpha_s + 2 * kHeads);     // [2 buffers][4 warps]
+    int* moved_s = reinterpret_cast<int*>(alpha_s + 2 * kHeads);     // [2 buffers][4 warps]: the tile (+ 1) that wrote it last
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;   // (warp-uniform for the compiler)
     const int group = static_cast<int>(blockIdx.x) % args.n_groups;
@@ -156,6 +156,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
         mbar_init(o_full, 1); mbar_init(o_free, 4); mbar_init(quiesce_bar, 1); mbar_init(quiesce_bar + 1, 1);
         abort_flag->value = (smem_u32(smem) & 1023u) != 0u ? 1u : 0u;
         *start_b = 0; *start_t = 0;
+        for (int i = 0; i < 8; ++i) moved_s[i] = 0;
         mbar_fence_init();
         tma_prefetch_desc(&tmap_qabs); tma_prefetch_desc(&tmap_q); tma_prefetch_desc(&tmap_rope); tma_prefetch_desc(&tmap_lat);
     }
@@ -435,11 +436,13 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
         DecodeCursor cur(args, my_tiles, first_b, first_t);
         while (!cur.done()) {
             const uint32_t buf = T & 1u, par = (T >> 1) & 1u;
-            ok = mbar_wait_warp(&s_full[buf], par, abort_flag, args.status, 0xC0);
-            if (!ok) break;
-            tc_fence_after_sync();
             const int valid = cur.valid();
+            const int tag = static_cast<int>(T) + 1;
+            int4 flags;                                       // per softmax warp: tag if one of its maxima moved in this tile
             if (softmax_warp) {
+                ok = mbar_wait_warp(&s_full[buf], par, abort_flag, args.status, 0xC0);
+                if (!ok) break;
+                tc_fence_after_sync();
                 uint32_t sv[32];
                 tmem_ld_16x64(tmem_s + buf * kDecKeys + lane_addr, sv);
                 tmem_ld_wait();
@@ -465,17 +468,18 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 const float c0 = fmaxf(m0, mx0 * args.scale_log2), c1 = fmaxf(m1, mx1 * args.scale_log2);
                 const bool move0 = live0 && (c0 - m0) > 8.0f, move1 = live1 && (c1 - m1) > 8.0f;   // lazy: only when it fell behind by 2^8
                 const float n0 = (move0 || first) ? c0 : m0, n1 = (move1 || first) ? c1 : m1;
-                const float f0 = move0 && !first ? fast_exp2(m0 - n0) : 1.0f, f1 = move1 && !first ? fast_exp2(m1 - n1) : 1.0f;
+                if (__any_sync(0xffffffffu, (move0 || move1) && !first)) {
+                    const float f0 = move0 ? fast_exp2(m0 - n0) : 1.0f, f1 = move1 ? fast_exp2(m1 - n1) : 1.0f;
+                    l0 *= f0; l1 *= f1;
+                    if ((lane & 3) == 0) { alpha_s[buf * kHeads + r0] = f0; alpha_s[buf * kHeads + r1] = f1; }
+                    if (lane == 0) moved_s[buf * 4 + warp] = tag;
+                    __syncwarp();
+                }
                 m0 = n0; m1 = n1;
-                const bool any = __any_sync(0xffffffffu, (move0 || move1) && !first);
-                if ((lane & 3) == 0) { alpha_s[buf * kHeads + r0] = f0; alpha_s[buf * kHeads + r1] = f1; }
-                if (lane == 0) moved_s[buf * 4 + warp] = any ? 1 : 0;
-                __syncwarp();
                 if (lane == 0) mbar_arrive(&a_full[buf]);
                 float s0[2] = {0.f, 0.f}, s1[2] = {0.f, 0.f};
                 uint32_t pk[16];                        // pk[2j], pk[2j+1]: columns 8j + 2(l%4), +1 of heads r0 and r1
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                auto exps = [&](int j) {
                     const float a0 = fast_exp2(fmaf(__uint_as_float(sv[4 * j]), args.scale_log2, -n0));
                     const float a1 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 1]), args.scale_log2, -n0));
                     const float b0 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 2]), args.scale_log2, -n1));
@@ -484,11 +488,17 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     s1[j & 1] += b0 + b1;
                     pk[2 * j] = pack_bf16x2(a0, a1);
                     pk[2 * j + 1] = pack_bf16x2(b0, b1);
-                }
-                l0 = l0 * f0 + (s0[0] + s0[1]);
-                l1 = l1 * f1 + (s1[0] + s1[1]);
-                // P of the tile that used this buffer before has been multiplied
-                if (T >= 2) {
+                };
+#pragma unroll
+                for (int j = 0; j < 5; ++j) exps(j);
+                // the two barriers this tile still needs, asked while there are exponentials to do: P of the tile that used the buffer
+                // before has been multiplied; every softmax warp has said whether its maxima moved
+                const bool p_free = T < 2 || mbar_test_wait(&pv_done[buf], par ^ 1u), told = mbar_test_wait(&a_full[buf], par);
+#pragma unroll
+                for (int j = 5; j < 8; ++j) exps(j);
+                l0 += s0[0] + s0[1];
+                l1 += s1[0] + s1[1];
+                if (!__all_sync(0xffffffffu, p_free)) {
                     ok = mbar_wait_warp(&pv_done[buf], par ^ 1u, abort_flag, args.status, 0xC1);
                     if (!ok) break;
                 }
@@ -499,13 +509,17 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     stmatrix_x4(pbase + (((2 * j + (lane >> 4)) ^ (lane & 7)) << 4), pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+                if (!__all_sync(0xffffffffu, told)) {
+                    ok = mbar_wait_warp(&a_full[buf], par, abort_flag, args.status, 0xC4);
+                    if (!ok) break;
+                }
+            } else {
+                ok = mbar_wait_warp(&a_full[buf], par, abort_flag, args.status, 0xC4);
+                if (!ok) break;
+                tc_fence_after_sync();
             }
-            ok = mbar_wait_warp(&a_full[buf], par, abort_flag, args.status, 0xC4);    // factors and flags are written
-            if (!ok) break;
-            bool moved = false;
-#pragma unroll
-            for (int w = 0; w * 16 < kHeads; ++w) moved |= moved_s[buf * 4 + w] != 0;
-            if (moved) {
+            flags = reinterpret_cast<const int4*>(moved_s)[buf];
+            if (flags.x == tag || flags.y == tag || flags.z == tag || flags.w == tag) {
                 // O^T is at rest once P.V of the previous tile has completed; this tile's waits for p_full below
                 const uint32_t prev = T - 1;
                 ok = mbar_wait_warp(&pv_done[prev & 1u], (prev >> 1) & 1u, abort_flag, args.status, 0xC2);
@@ -513,11 +527,13 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 tc_fence_after_sync();
 #pragma unroll 1
                 for (int c = 0; c < 4 * kHeads; c += 16) {
+                    const int w = (c % kHeads) >> 4;          // sixteen columns: the heads of softmax warp w
+                    if ((w == 0 ? flags.x : w == 1 ? flags.y : w == 2 ? flags.z : flags.w) != tag) continue;
                     uint32_t o[16];
                     tmem_ld_x16(tmem_base + lane_addr + c, o);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) o[v] = __float_as_uint(__uint_as_float(o[v]) * alpha_s[buf * kHeads + (c + v) % kHeads]);
+                    for (int v = 0; v < 16; ++v) o[v] = __float_as_uint(__uint_as_float(o[v]) * alpha_s[buf * kHeads + c % kHeads + v]);
                     tmem_st_x16(tmem_base + lane_addr + c, o);
                 }
                 tmem_st_wait();
@@ -668,18 +684,18 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 // fp32; rounded to bf16 it would cost as much accuracy as the result's own rounding, so B holds it in two parts, hi = bf16(o)
 // in rows 0..15 and lo = bf16(o - hi) in rows 16..31 -- columns that the MMA computes in the time of sixteen -- and the two
 // halves of D are added.  The weights' tile is requested before this kernel waits for the attention kernel (nothing in the
-// call writes them); the pieces are read by groups of 128 threads, one request each, or all four groups on one request
-// where a long context left more than kCombineSplit pieces of it.
+// call writes them).  A warp per request turns the maxima and sums into weights first, so that the loads of the pieces
+// themselves (2 KB each) depend on nothing and run eight deep.
 // A request without tokens has no piece: zeros, LSE -inf.
 constexpr int kProjectThreads = 512;
-constexpr int kCombineSplit = 8;
 struct DecodeProjectSmem {
     static constexpr int kW = 0;                                 // two slabs of 512 rows x 64 values
     static constexpr int kWSlab = 512 * 128;
     static constexpr int kO = kW + 2 * kWSlab;                   // eight slabs of 32 rows x 64 latents
     static constexpr int kOSlab = 32 * 128;
     static constexpr int kRed = kO + 8 * kOSlab;                 // [4][512] floats
-    static constexpr int kBar = kRed + 4 * 512 * 4;
+    static constexpr int kWeights = kRed + 4 * 512 * 4;          // a float per piece: at most one per CTA and one more per request
+    static constexpr int kBar = kWeights + (kDecMaxCtas + 20) * 4;
     static constexpr int kTotalBytes = kBar + 32;
 };
 __global__ void __launch_bounds__(kProjectThreads, 1)
@@ -693,6 +709,7 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 2);
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
     float* red = reinterpret_cast<float*>(smem + L::kRed);
+    float* weights = reinterpret_cast<float*>(smem + L::kWeights);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int head = blockIdx.x, b0 = blockIdx.y * requests_per_cta, n_req = min(requests_per_cta, B - b0);
     if (threadIdx.x == 0) {
@@ -714,90 +731,88 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
     grid_launch_dependents();
     grid_dependency_wait();
 
-    const int group = warp >> 2, cg = threadIdx.x & 127;         // thread's four channels: 4 cg ..
     const int total = tile_start[B];
     const int per = max(1, (total + ctas_per_group - 1) / ctas_per_group);
-    // weighted sum over pieces first + skip, first + skip + step, ... of request b; M and the full l on every thread
-    auto gather = [&](int b, int first, int last, int skip, int step, float& M, float& l) -> float4 {
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        M = -INFINITY; l = 0.f;
-        for (int c = first + lane; c <= last; c += 32) {
-            const float m = part_ml[static_cast<size_t>(c + b) * h_pad + head].x;
-            M = fmaxf(M, m);
+    // Weights: warp r takes request r.  Lane l of every warp knows the pieces of request l.
+    int first = 0, count = 0;
+    if (lane < n_req) {
+        const int begin = tile_start[b0 + lane], end = tile_start[b0 + lane + 1];
+        first = begin / per;
+        count = end > begin ? (end - 1) / per - first + 1 : 0;
+    }
+    int base = count;                                            // where the request's weights begin in shared memory
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, base, d);
+        if (lane >= d) base += v;
+    }
+    base -= count;
+    if (warp < n_req) {
+        const int f = __shfl_sync(0xffffffffu, first, warp), n = __shfl_sync(0xffffffffu, count, warp), at = __shfl_sync(0xffffffffu, base, warp);
+        const float2* ml = part_ml + static_cast<size_t>(f + b0 + warp) * h_pad + head;
+        float2 mine[(kDecMaxCtas + 31) / 32];                    // a request has at most one piece per CTA
+        float M = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < (kDecMaxCtas + 31) / 32; ++k) {
+            const int c = k * 32 + lane;
+            mine[k] = c < n ? ml[static_cast<size_t>(c) * h_pad] : make_float2(-INFINITY, 0.f);
+            M = fmaxf(M, mine[k].x);
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        for (int c = first + lane; c <= last; c += 32) {
-            const float2 ml = part_ml[static_cast<size_t>(c + b) * h_pad + head];
-            l = fmaf(ml.y, fast_exp2(ml.x - M), l);
-        }
+#pragma unroll
+        for (int k = 0; k < (kDecMaxCtas + 31) / 32; ++k)
+            if (k * 32 + lane < n) {
+                mine[k].x = fast_exp2(mine[k].x - M);
+                l = fmaf(mine[k].x, mine[k].y, l);
+            }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-#pragma unroll 4
-        for (int c = first + skip; c <= last; c += step) {
-            const size_t at = static_cast<size_t>(c + b) * h_pad + head;
-            const float w = fast_exp2(part_ml[at].x - M);
-            const float4 o = reinterpret_cast<const float4*>(part_o + at * kDecLat)[cg];
-            acc.x = fmaf(o.x, w, acc.x); acc.y = fmaf(o.y, w, acc.y);
-            acc.z = fmaf(o.z, w, acc.z); acc.w = fmaf(o.w, w, acc.w);
+        const float inv = 1.0f / l;
+#pragma unroll
+        for (int k = 0; k < (kDecMaxCtas + 31) / 32; ++k)
+            if (k * 32 + lane < n) weights[at + k * 32 + lane] = mine[k].x * inv;
+        if (lse != nullptr && lane == 0)
+            lse[static_cast<size_t>(b0 + warp) * h + head] = n > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
+    __syncthreads();
+    // Sums: four groups of 128 threads, four channels a thread.  A group takes every fourth request; with one or two requests in
+    // the CTA four or two groups share one (every fourth or second piece).
+    const int group = warp >> 2, cg = threadIdx.x & 127;
+    const int split = n_req == 1 ? 4 : n_req == 2 ? 2 : 1;
+    for (int r0 = 0; r0 < n_req; r0 += 4 / split) {
+        const int r = r0 + group / split, src = r < n_req ? r : 0;
+        const int f = __shfl_sync(0xffffffffu, first, src), n = r < n_req ? __shfl_sync(0xffffffffu, count, src) : 0,
+                  at = __shfl_sync(0xffffffffu, base, src);
+        const float4* o = reinterpret_cast<const float4*>(part_o + (static_cast<size_t>(f + b0 + src) * h_pad + head) * kDecLat) + cg;
+        const size_t step = static_cast<size_t>(h_pad) * (kDecLat / 4);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int c = group % split; c < n; c += split) {
+            const float w = weights[at + c];
+            const float4 x = o[c * step];
+            acc.x = fmaf(x.x, w, acc.x); acc.y = fmaf(x.y, w, acc.y);
+            acc.z = fmaf(x.z, w, acc.z); acc.w = fmaf(x.w, w, acc.w);
         }
-        return acc;
-    };
-    auto store = [&](int r, float4 o, float inv) {               // both parts of request r's row, swizzled
-        const float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
-        float rest[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) rest[e] = x[e] - __bfloat162float(__float2bfloat16_rn(x[e]));
-        uint8_t* slab = smem + L::kO + (cg >> 4) * L::kOSlab;    // 16 threads of four channels per slab
-        const int chunk = (cg & 15) >> 1, in_chunk = (cg & 1) * 8;
-        *reinterpret_cast<uint2*>(slab + r * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-        *reinterpret_cast<uint2*>(slab + (16 + r) * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) =
-            make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
-    };
-    for (int r0 = 0; r0 < n_req; r0 += 4) {
-        int first[4], last[4], most = 0;                         // pieces of the four requests (last < first: none)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int b = b0 + r0 + g;
-            const int begin = r0 + g < n_req ? tile_start[b] : 0, end = r0 + g < n_req ? tile_start[b + 1] : 0;
-            first[g] = begin / per;
-            last[g] = end > begin ? (end - 1) / per : first[g] - 1;
-            most = max(most, last[g] - first[g] + 1);
+        if (split > 1) {
+            reinterpret_cast<float4*>(red)[group * 128 + cg] = acc;
+            __syncthreads();
+            acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < split; ++k) {
+                const float4 x = reinterpret_cast<const float4*>(red)[(group / split * split + k) * 128 + cg];
+                acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+            }
         }
-        if (most <= kCombineSplit) {
-            int f = first[0], e = last[0];
+        if (r < n_req && group % split == 0) {                   // both parts of request r's row, swizzled
+            const float x[4] = {acc.x, acc.y, acc.z, acc.w};
+            float rest[4];
 #pragma unroll
-            for (int g = 1; g < 4; ++g)
-                if (group == g) { f = first[g]; e = last[g]; }
-            const int r = r0 + group;
-            if (r < n_req) {
-                float M = -INFINITY, l = 0.f;
-                const float4 o = gather(b0 + r, f, e, 0, 1, M, l);
-                const bool any = e >= f;
-                store(r, o, any ? 1.0f / l : 0.f);
-                if (lse != nullptr && cg == 0) lse[static_cast<size_t>(b0 + r) * h + head] = any ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
-            }
-        } else {
-#pragma unroll 1
-            for (int g = 0; g < 4 && r0 + g < n_req; ++g) {
-                float M, l;
-                const float4 mine = gather(b0 + r0 + g, first[g], last[g], group, 4, M, l);
-                __syncthreads();                                 // the sums of the request before have been read
-                reinterpret_cast<float4*>(red)[group * 128 + cg] = mine;
-                __syncthreads();
-                if (group == g) {
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float4 x = reinterpret_cast<const float4*>(red)[k * 128 + cg];
-                        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
-                    }
-                    const bool any = last[g] >= first[g];
-                    store(r0 + g, o, any ? 1.0f / l : 0.f);
-                    if (lse != nullptr && cg == 0)
-                        lse[static_cast<size_t>(b0 + r0 + g) * h + head] = any ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
-                }
-            }
+            for (int e = 0; e < 4; ++e) rest[e] = x[e] - __bfloat162float(__float2bfloat16_rn(x[e]));
+            uint8_t* slab = smem + L::kO + (cg >> 4) * L::kOSlab;    // 16 threads of four channels per slab
+            const int chunk = (cg & 15) >> 1, in_chunk = (cg & 1) * 8;
+            *reinterpret_cast<uint2*>(slab + r * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+            *reinterpret_cast<uint2*>(slab + (16 + r) * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) =
+                make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
         }
     }
     fence_async_shared();
