@@ -203,12 +203,12 @@ int laga_layernorm_backward(const void* dy, const void* x, const void* gamma, co
  *
  *   y[m, i, :] = x[m, i, :] with channels [rot_begin, rot_begin + d_rot) of every head rotated:
  *   (a, b) -> mscale * (a cos - b sin, b cos + a sin),   angle = positions[m] * freqs[j],   j = 0 .. d_rot/2 - 1
- *   x, y bf16 [M, h, d], heads dense, rows x_pitch / y_pitch elements apart (at least h*d, multiples of 8); y may be x
+ *   x, y bf16 [M, h, d], heads dense, rows x_pitch / y_pitch elements apart (at least h*d, at most 2^30, multiples of 8); y may be x
  *   itself (same pitch: only the rotated channels are touched) but not overlap it otherwise
  *   positions int32 [M], any value, repeats allowed;   freqs fp64 [d_rot/2], radians per position
  *   layout: which channels pair up, LAGA_ROPE_INTERLEAVED (2j, 2j+1) or LAGA_ROPE_HALF (j, j + d_rot/2)
  *   inverse != 0: rotates back (times mscale, not divided by it): the transpose, i.e. the gradient of the forward call
- * Angles are formed in fp64 (positions of millions stay exact); long-context scalings are choices of freqs and mscale.
+ * Angles are formed in 64 bits (positions of millions stay exact); long-context scalings are choices of freqs and mscale.
  * d: a multiple of 8, at most 1024; d_rot: a multiple of 16, at most 256; rot_begin: a multiple of 8.
  * No status word: errors are launch errors.
  */

@@ -210,6 +210,7 @@ int check_pointers(std::initializer_list<const void*> ptrs) {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return LAGA_ERR_CUDA;
     for (const void* p : ptrs) {
+        if (p == nullptr) continue;                  // an optional tensor left out (required ones have been checked for NULL)
         cudaPointerAttributes attr;
         if (cudaPointerGetAttributes(&attr, p) != cudaSuccess) {
             (void)cudaGetLastError();
@@ -1270,7 +1271,7 @@ int laga_rope(const void* x, long long x_pitch, const int* positions, const doub
         !rotary_ok(positions, freqs, d_rot, mscale, layout) || rot_begin > d - d_rot)
         return LAGA_ERR_INVALID_ARG;
     const long long width = static_cast<long long>(h) * d;
-    if (width > (1ll << 30) || x_pitch < width || y_pitch < width || (x_pitch & 7) || (y_pitch & 7)) return LAGA_ERR_INVALID_ARG;
+    if (width > (1ll << 30) || x_pitch > (1ll << 30) || y_pitch > (1ll << 30) || x_pitch < width || y_pitch < width || (x_pitch & 7) || (y_pitch & 7)) return LAGA_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(y)) return LAGA_ERR_INVALID_ARG;
     const bool in_place = x == y;
     if (in_place ? x_pitch != y_pitch
@@ -1280,23 +1281,23 @@ int laga_rope(const void* x, long long x_pitch, const int* positions, const doub
     if (rc != LAGA_OK) return rc;
     if ((rc = check_pointers({x, y, positions, freqs})) != LAGA_OK) return rc;
     const bool interleaved = layout == LAGA_ROPE_INTERLEAVED;
-    const int units = (interleaved ? d_rot / 8 : d_rot / 16) + (in_place ? 0 : (d - d_rot) / 8);
-    // about 256 threads; in half layout two chunks a thread, and as many fewer threads (the table of the block's tokens then
-    // stays within 32 KB whatever the widths are)
-    const int chunks = (in_place ? d_rot : d) / 8;
-    const dim3 block(units, 256 / chunks);
+    // about 256 threads, a row of units of eight channels for each of blockDim.y heads (the table of the block's tokens then stays
+    // within 32 KB whatever the widths are)
+    const int units = (in_place ? d_rot : d) / 8;
+    const dim3 block(units, 256 / units);
     const long long rows = static_cast<long long>(M) * h, per_block = static_cast<long long>(block.y) * kRopeRowsPerThread;
     const long long blocks = (rows + per_block - 1) / per_block;
     if (blocks > 0x7fffffffll) return LAGA_ERR_INVALID_ARG;
     const long long tokens = h == 1 ? per_block : (per_block + h - 2) / h + 1;        // most tokens a block's rows can touch
     const size_t smem = static_cast<size_t>(tokens < M ? tokens : M) * (d_rot / 2) * sizeof(float2);
-    const Rotary rot{positions, freqs, mscale, interleaved ? 1 : 0, inverse != 0 ? 1 : 0};
+    const RopeArgs a{static_cast<const __nv_bfloat16*>(x), static_cast<__nv_bfloat16*>(y), static_cast<unsigned>(x_pitch * 2),
+                     static_cast<unsigned>(y_pitch * 2), M, h, d, rot_begin, d_rot, in_place ? 1 : 0,
+                     static_cast<unsigned>(((1ull << 32) + h - 1) / h),
+                     Rotary{positions, freqs, mscale, interleaved ? 1 : 0, inverse != 0 ? 1 : 0}};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto xs = static_cast<const __nv_bfloat16*>(x);
-    auto ys = static_cast<__nv_bfloat16*>(y);
     const dim3 grid(static_cast<unsigned>(blocks));
-    if (interleaved) rope_kernel<true><<<grid, block, smem, st>>>(xs, x_pitch, ys, y_pitch, M, h, d, rot_begin, d_rot, in_place, rot);
-    else rope_kernel<false><<<grid, block, smem, st>>>(xs, x_pitch, ys, y_pitch, M, h, d, rot_begin, d_rot, in_place, rot);
+    if (interleaved) rope_kernel<true><<<grid, block, smem, st>>>(a);
+    else rope_kernel<false><<<grid, block, smem, st>>>(a);
     return launch_status();
 }
 
@@ -1313,21 +1314,19 @@ int laga_latent_norm_rope(const void* kv_a, long long kv_a_pitch, const void* ga
         return LAGA_ERR_INVALID_ARG;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
-    if ((rc = check_pointers({kv_a, gamma, positions, freqs})) != LAGA_OK) return rc;
-    for (const void* p : {beta, static_cast<const void*>(latent), static_cast<const void*>(k_pe), static_cast<const void*>(mean),
-                          static_cast<const void*>(rstd), static_cast<const void*>(cache), static_cast<const void*>(slots)})
-        if (p && (rc = check_pointers({p})) != LAGA_OK) return rc;
+    if ((rc = check_pointers({kv_a, gamma, beta, positions, freqs, latent, k_pe, mean, rstd, cache, slots})) != LAGA_OK) return rc;
     auto bf = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
     const LatentNormRopeArgs a{bf(kv_a), kv_a_pitch, bf(gamma), bf(beta), M, D, R, eps,
                                Rotary{positions, freqs, mscale, layout == LAGA_ROPE_INTERLEAVED ? 1 : 0, 0},
                                static_cast<__nv_bfloat16*>(latent), static_cast<__nv_bfloat16*>(k_pe), mean, rstd,
                                static_cast<__nv_bfloat16*>(cache), slots, n_slots};
-    const int blocks_needed = (M + kLnWarps - 1) / kLnWarps, cap = sm_count() * 4;
+    const int blocks_needed = (M + kLnWarps - 1) / kLnWarps, cap = sm_count() * 3;      // one resident wave at D <= 512
     const dim3 grid(blocks_needed < cap ? blocks_needed : cap), block(kLnWarps * 32);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (D <= 256) latent_norm_rope_fwd_kernel<1><<<grid, block, 0, st>>>(a);
-    else if (D <= 512) latent_norm_rope_fwd_kernel<2><<<grid, block, 0, st>>>(a);
-    else latent_norm_rope_fwd_kernel<4><<<grid, block, 0, st>>>(a);
+    if (D == 512) latent_norm_rope_fwd_kernel<2, true><<<grid, block, 0, st>>>(a);
+    else if (D <= 256) latent_norm_rope_fwd_kernel<1, false><<<grid, block, 0, st>>>(a);
+    else if (D < 512) latent_norm_rope_fwd_kernel<2, false><<<grid, block, 0, st>>>(a);
+    else latent_norm_rope_fwd_kernel<4, false><<<grid, block, 0, st>>>(a);
     return launch_status();
 }
 
@@ -1356,8 +1355,8 @@ int laga_latent_norm_rope_backward(const void* dlatent, const void* dk_pe, const
     if (workspace_bytes < laga_latent_norm_rope_backward_workspace_bytes(M, D)) return LAGA_ERR_WORKSPACE_TOO_SMALL;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
-    if ((rc = check_pointers({dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, freqs, dkv_a, dgamma, workspace})) != LAGA_OK) return rc;
-    if (dbeta && (rc = check_pointers({dbeta})) != LAGA_OK) return rc;
+    if ((rc = check_pointers({dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, freqs, dkv_a, dgamma, dbeta, workspace})) != LAGA_OK)
+        return rc;
     auto bf = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
     const LatentNormRopeBwdArgs a{bf(dlatent), bf(dk_pe), bf(kv_a), kv_a_pitch, bf(gamma), mean, rstd, M, D, R,
                                   Rotary{positions, freqs, mscale, layout == LAGA_ROPE_INTERLEAVED ? 1 : 0, 1},
@@ -1365,11 +1364,12 @@ int laga_latent_norm_rope_backward(const void* dlatent, const void* dk_pe, const
     const int blocks = latent_norm_bwd_blocks(M);
     const dim3 grid(blocks), block(kLnWarps * 32);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (D <= 256) latent_norm_rope_bwd_kernel<1><<<grid, block, 0, st>>>(a);
-    else if (D <= 512) latent_norm_rope_bwd_kernel<2><<<grid, block, 0, st>>>(a);
-    else latent_norm_rope_bwd_kernel<4><<<grid, block, 0, st>>>(a);
+    if (D == 512) latent_norm_rope_bwd_kernel<2, true><<<grid, block, 0, st>>>(a);
+    else if (D <= 256) latent_norm_rope_bwd_kernel<1, false><<<grid, block, 0, st>>>(a);
+    else if (D < 512) latent_norm_rope_bwd_kernel<2, false><<<grid, block, 0, st>>>(a);
+    else latent_norm_rope_bwd_kernel<4, false><<<grid, block, 0, st>>>(a);
     if ((rc = launch_status()) != LAGA_OK) return rc;
-    launch_kernel(latent_norm_sums_kernel, dim3((2 * D + 31) / 32), dim3(256), 0, st, true, static_cast<const float*>(workspace), blocks, D,
+    launch_kernel(latent_norm_sums_kernel, dim3((2 * D + 31) / 32), dim3(1024), 0, st, true, static_cast<const float*>(workspace), blocks, D,
                   dgamma, dbeta);
     return launch_status();
 }
@@ -1398,8 +1398,9 @@ int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, in
     }
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
-    for (const auto& i : in) if ((rc = check_pointers({i.p})) != LAGA_OK) return rc;
-    for (const auto& o : out) if ((rc = check_pointers({o.p})) != LAGA_OK) return rc;
+    if ((rc = check_pointers({seq_lens, new_lens, free_pages, n_free, slots, positions, cu_new_lens, seq_lens_out, n_free_out, status_word,
+                              block_table})) != LAGA_OK)
+        return rc;
     const CachePlanArgs a{seq_lens, new_lens, n_requests, shift, columns, block_table, free_pages, n_free, free_capacity, max_tokens, slots,
                           positions, cu_new_lens, seq_lens_out, n_free_out, static_cast<unsigned*>(status_word)};
     const int needed = (max_tokens + kPlanThreads - 1) / kPlanThreads, cap = sm_count();
@@ -1434,8 +1435,7 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
     if (workspace_bytes < w.total) return LAGA_ERR_WORKSPACE_TOO_SMALL;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
-    if ((rc = check_pointers({q, w_kv_b, cache, block_table, seq_lens, out, workspace})) != LAGA_OK) return rc;
-    if (lse && (rc = check_pointers({lse})) != LAGA_OK) return rc;
+    if ((rc = check_pointers({q, w_kv_b, cache, block_table, seq_lens, out, lse, workspace})) != LAGA_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t* base = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(base);

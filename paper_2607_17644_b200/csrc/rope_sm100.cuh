@@ -7,12 +7,14 @@
 //                                                            the gradient (mscale included)
 // for the pairs (2j, 2j+1) of the rotated channels (interleaved) or (j, j + d_rot/2) (half).
 //
-// The angle is formed in fp64: at position 4e6 an fp32 product is off by a quarter of a radian.  It is reduced to a
-// fraction of a turn there (one multiplication, one rounding, one subtraction; B200 has fp64 at half the fp32 rate),
-// and sine and cosine of the reduced angle in [-pi, pi] come from the special-function unit, whose absolute error
+// The angle needs more than fp32: at position 4e6 an fp32 product is off by a quarter of a radian.  It is formed in fixed point: freq /
+// (2 pi), reduced to its fraction in fp64, becomes a 64-bit fraction of a turn, and position times that, modulo 2^64, is the
+// fraction of a turn to 2^-34 at any 32-bit position -- two integer multiplications, where fp64 arithmetic cost three times the
+// instructions.  Sine and cosine of the reduced angle in [-pi, pi] come from the special-function unit, whose absolute error
 // below 2^-21 is far under the half step (2^-9) of the bf16 result.
 //
-// Everything here is bound by HBM: one read and one write of every element.
+// Everything here reads and writes every element once; the kernels come close enough to HBM speed that instructions count
+// (a warp moves 512 bytes per load, and an SM gets 4 instructions per clock for about 23 bytes per clock).
 #pragma once
 #include "layernorm_sm100.cuh"
 #include "sm100_ptx.cuh"
@@ -30,11 +32,15 @@ struct Rotary {
     int interleaved, inverse;
 };
 
-// (cos, sin) * mscale of one pair at one position; `inverse` turns the other way.
-__device__ __forceinline__ float2 rotary_turn(const Rotary& r, int position, int pair) {
-    constexpr double kInvTwoPi = 0.15915494309189533577;
-    const double turns = static_cast<double>(position) * (__ldg(r.freqs + pair) * kInvTwoPi);
-    const float phi = static_cast<float>(turns - rint(turns)) * 6.2831853071795865f;
+// freq (radians per position) as a 64-bit fraction of a turn per position
+__device__ __forceinline__ unsigned long long rotary_step(double freq) {
+    const double turns = freq * 0.15915494309189533577;
+    return static_cast<unsigned long long>((turns - floor(turns)) * 18446744073709551616.0);
+}
+// (cos, sin) * mscale of a pair at one position; `inverse` turns the other way.
+__device__ __forceinline__ float2 rotary_turn(const Rotary& r, int position, unsigned long long step) {
+    const unsigned long long turn = static_cast<unsigned long long>(static_cast<long long>(position)) * step;
+    const float phi = static_cast<float>(static_cast<int>(turn >> 32)) * 1.4629180792671596e-9f;      // 2 pi / 2^32
     float s, c;
     __sincosf(phi, &s, &c);
     if (r.inverse) s = -s;
@@ -48,79 +54,95 @@ __device__ __forceinline__ float2 rotary_apply(float2 turn, float a, float b) {
 // pitches in elements.  A block takes rows_per_block = blockDim.y * 4 rows (m, i) of the flattened [M, h]: the loads
 // go out first, then the block's threads fill the table of (cos, sin) of the tokens those rows touch (once per token,
 // not once per head: with 16 heads that is 1/16 of the fp64 and special-function work), then each thread rotates or
-// copies its 16-byte chunks.  threadIdx.x is the chunk within the head, so no index needs a division but the token's.
-// Half layout: the thread of a chunk in the first half of the rotated channels also owns the partner chunk, and the
-// partner's own thread does not exist (units_per_head counts it out), so x and y may be the same buffer.
+// copies its 16 bytes.  threadIdx.x is the unit within the head, so no index needs a division but the token's.
+// A unit is eight channels: a 16-byte chunk, or in half layout, among the rotated channels, four of the first half and
+// their four partners, so that in both layouts a unit is whole pairs and x and y may be the same buffer.
 // in_place: only the rotated units run.
-template <bool kInterleaved>
-__global__ void __launch_bounds__(256)
-rope_kernel(const __nv_bfloat16* x, long long x_pitch, __nv_bfloat16* y, long long y_pitch, int M, int h, int d,
-            int rot_begin, int d_rot, int in_place, Rotary rot) {
-    extern __shared__ float2 turns[];                       // [tokens of this block][d_rot / 2]
-    const int n_pairs = d_rot >> 1;
-    const int rot_units = kInterleaved ? d_rot >> 3 : d_rot >> 4;
-    const int before = in_place ? 0 : rot_begin >> 3;       // units copied in front of the rotated ones
-    const int u = threadIdx.x;
-    const bool rotates = u >= before && u < before + rot_units;
-    // first channel of this thread's unit
-    const int c0 = u < before ? u * 8 : rotates ? rot_begin + (u - before) * 8 : rot_begin + d_rot + (u - before - rot_units) * 8;
-    const long long rows = static_cast<long long>(M) * h;
-    const long long row0 = static_cast<long long>(blockIdx.x) * (blockDim.y * kRopeRowsPerThread);
-    const long long row_end = min(rows, row0 + blockDim.y * kRopeRowsPerThread);
-    const int first_token = static_cast<int>(row0 / h);
-    const int n_tokens = static_cast<int>((row_end - 1) / h) - first_token + 1;
+struct RopeArgs {
+    const __nv_bfloat16* x;
+    __nv_bfloat16* y;
+    unsigned x_pitch, y_pitch;             // bytes
+    int M, h, d, rot_begin, d_rot, in_place;
+    unsigned h_magic;                      // ceil(2^32 / h) for h <= kRopeMagicHeads
+    Rotary rot;
+};
+constexpr int kRopeMagicHeads = 1024;
 
-    uint4 v[kRopeRowsPerThread], w[kRopeRowsPerThread];
-    int token[kRopeRowsPerThread], head[kRopeRowsPerThread];
+template <bool kInterleaved>
+__global__ void __launch_bounds__(256, 5)
+rope_kernel(const RopeArgs a) {
+    extern __shared__ float2 turns[];                       // [tokens of this block][d_rot / 2]
+    const int n_pairs = a.d_rot >> 1;
+    const int before = a.in_place ? 0 : a.rot_begin >> 3;   // units copied in front of the rotated ones
+    const int u = static_cast<int>(threadIdx.x) - before;   // rotated unit, if it is one
+    const bool rotates = u >= 0 && u < (a.d_rot >> 3);
+    const bool split = !kInterleaved && rotates;            // two runs of four channels, n_pairs apart
+    const int c0 = split ? a.rot_begin + u * 4 : rotates ? a.rot_begin + u * 8 : static_cast<int>(threadIdx.x) * 8;
+    const long long row0 = static_cast<long long>(blockIdx.x) * (blockDim.y * kRopeRowsPerThread);
+    const int n_rows = static_cast<int>(min(static_cast<long long>(blockDim.y * kRopeRowsPerThread), static_cast<long long>(a.M) * a.h - row0));
+    const int first_token = static_cast<int>(row0 / a.h), first_head = static_cast<int>(row0 - static_cast<long long>(first_token) * a.h);
+    // (token, head) of the block's row i: i + first_head is below h + 1024
+    auto token_of = [&](int i) -> int {
+        const unsigned r = static_cast<unsigned>(i + first_head);
+        return a.h <= kRopeMagicHeads ? static_cast<int>(__umulhi(r, a.h_magic)) : static_cast<int>(r >= static_cast<unsigned>(a.h));
+    };
+    const uint8_t* x0 = reinterpret_cast<const uint8_t*>(a.x) + static_cast<long long>(first_token) * a.x_pitch + c0 * 2;
+    uint8_t* y0 = reinterpret_cast<uint8_t*>(a.y) + static_cast<long long>(first_token) * a.y_pitch + c0 * 2;
+    const int gap = split ? n_pairs * 2 : 8;                // bytes between the unit's halves
+
+    uint4 v[kRopeRowsPerThread];
+    int token[kRopeRowsPerThread], head_at[kRopeRowsPerThread];
 #pragma unroll
     for (int k = 0; k < kRopeRowsPerThread; ++k) {
-        const long long row = row0 + threadIdx.y + k * blockDim.y;
-        token[k] = -1;
-        if (row < row_end) {
-            // row - first_token * h is below 2^31 and small: 32-bit division
-            const unsigned r = static_cast<unsigned>(row - static_cast<long long>(first_token) * h);
-            token[k] = static_cast<int>(r / static_cast<unsigned>(h));
-            head[k] = static_cast<int>(r) - token[k] * h;
-            const __nv_bfloat16* src = x + (first_token + token[k]) * x_pitch + head[k] * d + c0;
-            v[k] = *reinterpret_cast<const uint4*>(src);
-            if (!kInterleaved && rotates) w[k] = *reinterpret_cast<const uint4*>(src + n_pairs);
+        const int i = threadIdx.y + k * blockDim.y;
+        token[k] = a.h == 1 ? i : token_of(i);
+        head_at[k] = (i + first_head - token[k] * a.h) * a.d * 2;
+        if (i < n_rows) {
+            const uint8_t* src = x0 + static_cast<unsigned long long>(static_cast<unsigned>(token[k])) * a.x_pitch + head_at[k];
+            if (split) {
+                const uint2 lo = *reinterpret_cast<const uint2*>(src), hi = *reinterpret_cast<const uint2*>(src + gap);
+                v[k] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            } else {
+                v[k] = *reinterpret_cast<const uint4*>(src);
+            }
         }
     }
+    const int n_tokens = (a.h == 1 ? n_rows - 1 : token_of(n_rows - 1)) + 1;
     for (int t = threadIdx.y * blockDim.x + threadIdx.x; t < n_tokens * n_pairs; t += blockDim.x * blockDim.y) {
         const int tok = t / n_pairs;
-        turns[t] = rotary_turn(rot, __ldg(rot.positions + first_token + tok), t - tok * n_pairs);
+        turns[t] = rotary_turn(a.rot, __ldg(a.rot.positions + first_token + tok), rotary_step(__ldg(a.rot.freqs + t - tok * n_pairs)));
     }
     __syncthreads();
+    if (rotates) {
+#pragma unroll
+        for (int k = 0; k < kRopeRowsPerThread; ++k) {
+            if (static_cast<int>(threadIdx.y + k * blockDim.y) >= n_rows) break;
+            const float4* turn = reinterpret_cast<const float4*>(turns + token[k] * n_pairs + u * 4);
+            const float4 t01 = turn[0], t23 = turn[1];
+            const float2 t[4] = {make_float2(t01.x, t01.y), make_float2(t01.z, t01.w), make_float2(t23.x, t23.y), make_float2(t23.z, t23.w)};
+            float f[8];
+            ln_unpack(v[k], f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float& p = kInterleaved ? f[2 * e] : f[e];
+                float& q = kInterleaved ? f[2 * e + 1] : f[4 + e];
+                const float2 r = rotary_apply(t[e], p, q);
+                p = r.x;
+                q = r.y;
+            }
+            v[k] = ln_pack(f);
+        }
+    }
 #pragma unroll
     for (int k = 0; k < kRopeRowsPerThread; ++k) {
-        if (token[k] < 0) continue;
-        __nv_bfloat16* dst = y + (first_token + token[k]) * y_pitch + head[k] * d + c0;
-        if (rotates) {
-            const float2* turn = turns + token[k] * n_pairs;
-            float a[8], b[8];
-            ln_unpack(v[k], a);
-            if (kInterleaved) {
-                turn += (u - before) * 4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 r = rotary_apply(turn[e], a[2 * e], a[2 * e + 1]);
-                    a[2 * e] = r.x;
-                    a[2 * e + 1] = r.y;
-                }
-            } else {
-                turn += (u - before) * 8;
-                ln_unpack(w[k], b);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 r = rotary_apply(turn[e], a[e], b[e]);
-                    a[e] = r.x;
-                    b[e] = r.y;
-                }
-                *reinterpret_cast<uint4*>(dst + n_pairs) = ln_pack(b);
-            }
-            v[k] = ln_pack(a);
+        if (static_cast<int>(threadIdx.y + k * blockDim.y) >= n_rows) break;
+        uint8_t* dst = y0 + static_cast<unsigned long long>(static_cast<unsigned>(token[k])) * a.y_pitch + head_at[k];
+        if (split) {
+            *reinterpret_cast<uint2*>(dst) = make_uint2(v[k].x, v[k].y);
+            *reinterpret_cast<uint2*>(dst + gap) = make_uint2(v[k].z, v[k].w);
+        } else {
+            *reinterpret_cast<uint4*>(dst) = v[k];
         }
-        *reinterpret_cast<uint4*>(dst) = v[k];
     }
 }
 
@@ -144,11 +166,6 @@ struct LatentNormRopeArgs {
     int n_slots;
 };
 
-// The two channels of pair j among the rotated ones.
-__device__ __forceinline__ float2 rotary_load_pair(const __nv_bfloat16* src, int j, int n_pairs, bool interleaved) {
-    if (interleaved) return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(src + 2 * j));
-    return make_float2(__bfloat162float(src[j]), __bfloat162float(src[j + n_pairs]));
-}
 __device__ __forceinline__ void rotary_store_pair(__nv_bfloat16* dst, int j, int n_pairs, bool interleaved, float2 v) {
     if (interleaved) {
         *reinterpret_cast<__nv_bfloat162*>(dst + 2 * j) = __floats2bfloat162_rn(v.x, v.y);
@@ -158,64 +175,143 @@ __device__ __forceinline__ void rotary_store_pair(__nv_bfloat16* dst, int j, int
     }
 }
 
+// A pair as it lies in memory, so that a row can be fetched ahead in few registers.
+__device__ __forceinline__ uint32_t rotary_fetch_pair(const __nv_bfloat16* src, int j, int n_pairs, bool interleaved) {
+    if (interleaved) return *reinterpret_cast<const uint32_t*>(src + 2 * j);
+    const unsigned short* u = reinterpret_cast<const unsigned short*>(src);
+    return u[j] | (static_cast<uint32_t>(u[j + n_pairs]) << 16);
+}
+__device__ __forceinline__ float2 rotary_pair_of(uint32_t raw) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw)); }
+
+// What a warp fetches of a row: its 16-byte chunks, the pair its lane rotates (the first 32 pairs), position and slot.
 template <int kLnChunks>
-__global__ void __launch_bounds__(kLnWarps * 32)
+struct LatentRow {
+    uint4 v[kLnChunks];
+    uint32_t pair;
+    int position, slot;
+};
+template <int kLnChunks, bool kFull>
+__device__ __forceinline__ void latent_fetch(const LatentNormRopeArgs& a, int m, int lane, LatentRow<kLnChunks>& r) {
+    const __nv_bfloat16* row = a.kv_a + m * a.kv_a_pitch;
+#pragma unroll
+    for (int i = 0; i < kLnChunks; ++i) {
+        const int c = i * 256 + lane * 8;
+        r.v[i] = kFull || c < a.D ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    r.pair = lane < (a.R >> 1) ? rotary_fetch_pair(row + a.D, lane, a.R >> 1, a.rot.interleaved) : 0u;
+    r.position = __ldg(a.rot.positions + m);
+    r.slot = a.cache != nullptr ? __ldg(a.slots + m) : -1;
+}
+
+// Two fp32 values in one register pair: one instruction for two additions, products or fused multiply-adds.
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 f2_parts(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ void f2_unpack(const uint4& v, F2* f) {     // eight bf16
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = f2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
+}
+__device__ __forceinline__ uint4 f2_pack(const F2* f) {
+    uint4 v;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 t = f2_parts(f[k]);
+        w[k] = pack_bf16x2(t.x, t.y);
+    }
+    return v;
+}
+
+// A row's work is a chain (load, mean, variance, store) whose latency one warp cannot hide, so each warp has the row after
+// this one in flight while it computes; gamma and beta stay in registers, unpacked, and the arithmetic runs two values at
+// a time.  kFull: D is kLnChunks * 256, no lane idles.
+template <int kLnChunks, bool kFull>
+__global__ void __launch_bounds__(kLnWarps * 32, kLnChunks <= 2 ? 3 : 1)
 latent_norm_rope_fwd_kernel(const LatentNormRopeArgs a) {
     const int lane = threadIdx.x & 31;
     const int n_warps = gridDim.x * kLnWarps;
     const float inv_d = 1.0f / static_cast<float>(a.D);
     const int n_pairs = a.R >> 1;
-    for (int m = blockIdx.x * kLnWarps + (threadIdx.x >> 5); m < a.M; m += n_warps) {
-        const __nv_bfloat16* row = a.kv_a + m * a.kv_a_pitch;
+    F2 gamma[kLnChunks][4], beta[kLnChunks][4];
+#pragma unroll
+    for (int i = 0; i < kLnChunks; ++i) {
+        const int c = i * 256 + lane * 8;
+        const bool in = kFull || c < a.D;
+        f2_unpack(in ? __ldg(reinterpret_cast<const uint4*>(a.gamma + c)) : make_uint4(0u, 0u, 0u, 0u), gamma[i]);
+        f2_unpack(in && a.beta != nullptr ? __ldg(reinterpret_cast<const uint4*>(a.beta + c)) : make_uint4(0u, 0u, 0u, 0u), beta[i]);
+    }
+    const unsigned long long step = lane < n_pairs ? rotary_step(__ldg(a.rot.freqs + lane)) : 0ull;
+    int m = blockIdx.x * kLnWarps + (threadIdx.x >> 5);
+    LatentRow<kLnChunks> next;
+    if (m < a.M) latent_fetch<kLnChunks, kFull>(a, m, lane, next);
+    for (; m < a.M; m += n_warps) {
+        const LatentRow<kLnChunks> row = next;
+        if (m + n_warps < a.M) latent_fetch<kLnChunks, kFull>(a, m + n_warps, lane, next);
         __nv_bfloat16* cache_row = nullptr;
-        if (a.cache != nullptr) {
-            const int slot = __ldg(a.slots + m);
-            if (slot >= 0 && slot < a.n_slots) cache_row = a.cache + static_cast<size_t>(slot) * (a.D + a.R);
-            else if (a.latent == nullptr) continue;                     // nothing of this row goes anywhere
-        }
-        const int position = __ldg(a.rot.positions + m);
-        float v[kLnChunks][8];
-        float sum = 0.f;
+        if (row.slot >= 0 && row.slot < a.n_slots) cache_row = a.cache + static_cast<size_t>(row.slot) * (a.D + a.R);
+        else if (a.latent == nullptr) continue;                         // nothing of this row goes anywhere
+        F2 v[kLnChunks][4], sum = f2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < kLnChunks; ++i) {
-            const int c = i * 256 + lane * 8;
-            if (c < a.D) {
-                ln_unpack(*reinterpret_cast<const uint4*>(row + c), v[i]);
+            f2_unpack(row.v[i], v[i]);                                  // (zeros beyond D)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sum += v[i][k];
-            }
+            for (int k = 0; k < 4; ++k) sum = f2_add(sum, v[i][k]);
         }
-        // the key, under the latent's loads
-        for (int j = lane; j < n_pairs; j += 32) {
-            const float2 in = rotary_load_pair(row + a.D, j, n_pairs, a.rot.interleaved);
-            const float2 out = rotary_apply(rotary_turn(a.rot, position, j), in.x, in.y);
-            if (a.k_pe != nullptr) rotary_store_pair(a.k_pe + static_cast<size_t>(m) * a.R, j, n_pairs, a.rot.interleaved, out);
-            if (cache_row != nullptr) rotary_store_pair(cache_row + a.D, j, n_pairs, a.rot.interleaved, out);
-        }
-        const float mean = ln_warp_sum(sum) * inv_d;
-        float sq = 0.f;
+        const float2 sums = f2_parts(sum);
+        const float mean = ln_warp_sum(sums.x + sums.y) * inv_d;
+        const F2 minus = f2(-mean, -mean);
+        F2 sq = f2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < kLnChunks; ++i)
-            if (i * 256 + lane * 8 < a.D)
+            if (kFull || i * 256 + lane * 8 < a.D)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float t = v[i][k] - mean;
-                    sq = fmaf(t, t, sq);
+                for (int k = 0; k < 4; ++k) {
+                    v[i][k] = f2_add(v[i][k], minus);
+                    sq = f2_fma(v[i][k], v[i][k], sq);
                 }
-        const float rstd = rsqrtf(ln_warp_sum(sq) * inv_d + a.eps);
+        // the key, under the second sum
+        if (lane < n_pairs) {
+            const float2 in = rotary_pair_of(row.pair), out = rotary_apply(rotary_turn(a.rot, row.position, step), in.x, in.y);
+            if (a.k_pe != nullptr) rotary_store_pair(a.k_pe + static_cast<size_t>(m) * a.R, lane, n_pairs, a.rot.interleaved, out);
+            if (cache_row != nullptr) rotary_store_pair(cache_row + a.D, lane, n_pairs, a.rot.interleaved, out);
+        }
+        const float2 sqs = f2_parts(sq);
+        const float rstd = rsqrtf(ln_warp_sum(sqs.x + sqs.y) * inv_d + a.eps);
+        const F2 scale = f2(rstd, rstd);
 #pragma unroll
         for (int i = 0; i < kLnChunks; ++i) {
             const int c = i * 256 + lane * 8;
-            if (c < a.D) {
-                float gm[8], bt[8], o[8];
-                ln_unpack(__ldg(reinterpret_cast<const uint4*>(a.gamma + c)), gm);
-                if (a.beta != nullptr) ln_unpack(__ldg(reinterpret_cast<const uint4*>(a.beta + c)), bt);
+            if (kFull || c < a.D) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] = fmaf((v[i][k] - mean) * rstd, gm[k], a.beta != nullptr ? bt[k] : 0.f);
-                const uint4 packed = ln_pack(o);
+                for (int k = 0; k < 4; ++k) v[i][k] = f2_fma(f2_mul(v[i][k], scale), gamma[i][k], beta[i][k]);
+                const uint4 packed = f2_pack(v[i]);
                 if (a.latent != nullptr) *reinterpret_cast<uint4*>(a.latent + static_cast<size_t>(m) * a.D + c) = packed;
                 if (cache_row != nullptr) *reinterpret_cast<uint4*>(cache_row + c) = packed;
             }
+        }
+        for (int j = lane + 32; j < n_pairs; j += 32) {                 // keys wider than 64 channels
+            const float2 in = rotary_pair_of(rotary_fetch_pair(a.kv_a + m * a.kv_a_pitch + a.D, j, n_pairs, a.rot.interleaved));
+            const float2 out = rotary_apply(rotary_turn(a.rot, row.position, rotary_step(__ldg(a.rot.freqs + j))), in.x, in.y);
+            if (a.k_pe != nullptr) rotary_store_pair(a.k_pe + static_cast<size_t>(m) * a.R, j, n_pairs, a.rot.interleaved, out);
+            if (cache_row != nullptr) rotary_store_pair(cache_row + a.D, j, n_pairs, a.rot.interleaved, out);
         }
         if (lane == 0) {
             if (a.mean != nullptr) a.mean[m] = mean;
@@ -239,59 +335,98 @@ struct LatentNormRopeBwdArgs {
 };
 
 template <int kLnChunks>
-__global__ void __launch_bounds__(kLnWarps * 32)
+struct LatentBwdRow {
+    uint4 x[kLnChunks], dy[kLnChunks];
+    uint32_t pair;
+    int position;
+    float mean, rstd;
+};
+template <int kLnChunks, bool kFull>
+__device__ __forceinline__ void latent_bwd_fetch(const LatentNormRopeBwdArgs& a, int m, int lane, LatentBwdRow<kLnChunks>& r) {
+    const __nv_bfloat16* x = a.kv_a + m * a.kv_a_pitch;
+    const __nv_bfloat16* dy = a.dlatent + static_cast<size_t>(m) * a.D;
+#pragma unroll
+    for (int i = 0; i < kLnChunks; ++i) {
+        const int c = i * 256 + lane * 8;
+        r.x[i] = kFull || c < a.D ? *reinterpret_cast<const uint4*>(x + c) : make_uint4(0u, 0u, 0u, 0u);
+        r.dy[i] = kFull || c < a.D ? *reinterpret_cast<const uint4*>(dy + c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    r.pair = lane < (a.R >> 1) ? rotary_fetch_pair(a.dk_pe + static_cast<size_t>(m) * a.R, lane, a.R >> 1, a.rot.interleaved) : 0u;
+    r.position = __ldg(a.rot.positions + m);
+    r.mean = __ldg(a.mean + m);
+    r.rstd = __ldg(a.rstd + m);
+}
+
+template <int kLnChunks, bool kFull>
+__global__ void __launch_bounds__(kLnWarps * 32, kLnChunks <= 2 ? 2 : 1)
 latent_norm_rope_bwd_kernel(const LatentNormRopeBwdArgs a) {
     __shared__ float part[kLnWarps][kLnChunks * 256];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n_warps = gridDim.x * kLnWarps;
     const float inv_d = 1.0f / static_cast<float>(a.D);
     const int n_pairs = a.R >> 1;
-    float acc_g[kLnChunks][8], acc_b[kLnChunks][8];
+    F2 acc_g[kLnChunks][4], acc_b[kLnChunks][4];
+    uint4 gamma[kLnChunks];
 #pragma unroll
-    for (int i = 0; i < kLnChunks; ++i)
+    for (int i = 0; i < kLnChunks; ++i) {
+        const int c = i * 256 + lane * 8;
+        gamma[i] = kFull || c < a.D ? __ldg(reinterpret_cast<const uint4*>(a.gamma + c)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) acc_g[i][k] = acc_b[i][k] = 0.f;
-    for (int m = blockIdx.x * kLnWarps + warp; m < a.M; m += n_warps) {
-        const float mean = __ldg(a.mean + m), rstd = __ldg(a.rstd + m);
-        const int position = __ldg(a.rot.positions + m);
-        const __nv_bfloat16* xr = a.kv_a + m * a.kv_a_pitch;
-        const __nv_bfloat16* gr = a.dlatent + static_cast<size_t>(m) * a.D;
+        for (int k = 0; k < 4; ++k) acc_g[i][k] = acc_b[i][k] = f2(0.f, 0.f);
+    }
+    const unsigned long long step = lane < n_pairs ? rotary_step(__ldg(a.rot.freqs + lane)) : 0ull;
+    int m = blockIdx.x * kLnWarps + warp;
+    LatentBwdRow<kLnChunks> next;
+    if (m < a.M) latent_bwd_fetch<kLnChunks, kFull>(a, m, lane, next);
+    for (; m < a.M; m += n_warps) {
+        const LatentBwdRow<kLnChunks> row = next;
+        if (m + n_warps < a.M) latent_bwd_fetch<kLnChunks, kFull>(a, m + n_warps, lane, next);
         __nv_bfloat16* out = a.dkv_a + static_cast<size_t>(m) * (a.D + a.R);
-        float xh[kLnChunks][8], g[kLnChunks][8];
-        float s1 = 0.f, s2 = 0.f;
+        const F2 rstd = f2(row.rstd, row.rstd), shift = f2(-row.mean * row.rstd, -row.mean * row.rstd);
+        F2 xh[kLnChunks][4], g[kLnChunks][4], t1 = f2(0.f, 0.f), t2 = f2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < kLnChunks; ++i) {
-            const int c = i * 256 + lane * 8;
-            if (c < a.D) {
-                float xv[8], dv[8], gm[8];
-                ln_unpack(*reinterpret_cast<const uint4*>(xr + c), xv);
-                ln_unpack(*reinterpret_cast<const uint4*>(gr + c), dv);
-                ln_unpack(__ldg(reinterpret_cast<const uint4*>(a.gamma + c)), gm);
+            F2 dv[4];
+            f2_unpack(row.x[i], xh[i]);
+            f2_unpack(row.dy[i], dv);
+            f2_unpack(gamma[i], g[i]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    xh[i][k] = (xv[k] - mean) * rstd;
-                    g[i][k] = dv[k] * gm[k];
-                    s1 += g[i][k];
-                    s2 = fmaf(g[i][k], xh[i][k], s2);
-                    acc_g[i][k] = fmaf(dv[k], xh[i][k], acc_g[i][k]);
-                    acc_b[i][k] += dv[k];
-                }
+            for (int k = 0; k < 4; ++k) {
+                xh[i][k] = f2_fma(xh[i][k], rstd, shift);
+                g[i][k] = f2_mul(dv[k], g[i][k]);                       // (zeros beyond D: dy is)
+                t1 = f2_add(t1, g[i][k]);
+                t2 = f2_fma(g[i][k], xh[i][k], t2);
+                acc_g[i][k] = f2_fma(dv[k], xh[i][k], acc_g[i][k]);
+                acc_b[i][k] = f2_add(acc_b[i][k], dv[k]);
             }
         }
-        for (int j = lane; j < n_pairs; j += 32) {
-            const float2 in = rotary_load_pair(a.dk_pe + static_cast<size_t>(m) * a.R, j, n_pairs, a.rot.interleaved);
-            rotary_store_pair(out + a.D, j, n_pairs, a.rot.interleaved, rotary_apply(rotary_turn(a.rot, position, j), in.x, in.y));
+        if (lane < n_pairs) {
+            const float2 in = rotary_pair_of(row.pair);
+            rotary_store_pair(out + a.D, lane, n_pairs, a.rot.interleaved, rotary_apply(rotary_turn(a.rot, row.position, step), in.x, in.y));
         }
-        s1 = ln_warp_sum(s1) * inv_d;
-        s2 = ln_warp_sum(s2) * inv_d;
+        for (int j = lane + 32; j < n_pairs; j += 32) {                 // keys wider than 64 channels
+            const float2 in = rotary_pair_of(rotary_fetch_pair(a.dk_pe + static_cast<size_t>(m) * a.R, j, n_pairs, a.rot.interleaved));
+            rotary_store_pair(out + a.D, j, n_pairs, a.rot.interleaved,
+                              rotary_apply(rotary_turn(a.rot, row.position, rotary_step(__ldg(a.rot.freqs + j))), in.x, in.y));
+        }
+        const float2 u1 = f2_parts(t1), u2 = f2_parts(t2);
+        float s1 = u1.x + u1.y, s2 = u2.x + u2.y;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            s1 += __shfl_xor_sync(0xffffffffu, s1, d);
+            s2 += __shfl_xor_sync(0xffffffffu, s2, d);
+        }
+        // rstd * (g - s1 - xhat * s2)
+        s1 *= -inv_d * row.rstd;
+        s2 *= -inv_d * row.rstd;
+        const F2 p1 = f2(s1, s1), p2 = f2(s2, s2);
 #pragma unroll
         for (int i = 0; i < kLnChunks; ++i) {
             const int c = i * 256 + lane * 8;
-            if (c < a.D) {
-                float o[8];
+            if (kFull || c < a.D) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] = rstd * (g[i][k] - s1 - xh[i][k] * s2);
-                *reinterpret_cast<uint4*>(out + c) = ln_pack(o);
+                for (int k = 0; k < 4; ++k) g[i][k] = f2_fma(xh[i][k], p2, f2_fma(g[i][k], rstd, p1));
+                *reinterpret_cast<uint4*>(out + c) = f2_pack(g[i]);
             }
         }
     }
@@ -304,7 +439,8 @@ latent_norm_rope_bwd_kernel(const LatentNormRopeBwdArgs a) {
             const int c = i * 256 + lane * 8;
             if (c < a.D)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) part[warp][c + k] = pass == 0 ? acc_g[i][k] : acc_b[i][k];
+                for (int k = 0; k < 4; ++k)
+                    *reinterpret_cast<float2*>(&part[warp][c + 2 * k]) = f2_parts(pass == 0 ? acc_g[i][k] : acc_b[i][k]);
         }
         __syncthreads();
         for (int c = threadIdx.x; c < a.D; c += kLnWarps * 32) {
@@ -316,23 +452,26 @@ latent_norm_rope_bwd_kernel(const LatentNormRopeBwdArgs a) {
     }
 }
 
-// dgamma and dbeta from the per-block sums: 32 columns a block, eight warps on interleaved blocks' rows, added in a
-// fixed order.  Columns [0, D) are dgamma, [D, 2D) dbeta (dropped when dbeta is null).
-__global__ void __launch_bounds__(256)
+// dgamma and dbeta from the per-block sums: 32 columns a block, 32 warps on interleaved blocks' rows (ten loads each, all in
+// flight at once: the kernel is one round trip to L2), added in a fixed order.  Columns [0, D) are dgamma, [D, 2D) dbeta
+// (dropped when dbeta is null).
+__global__ void __launch_bounds__(1024)
 latent_norm_sums_kernel(const float* __restrict__ partial, int n_blocks, int D, float* dgamma, float* dbeta) {
-    __shared__ float part[8][33];
+    __shared__ float part[32][33];
     grid_dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     float s = 0.f;
-    if (c < 2 * D)
-        for (int b = warp; b < n_blocks; b += 8) s += partial[static_cast<size_t>(b) * 2 * D + c];
+    if (c < 2 * D) {
+#pragma unroll 10
+        for (int b = warp; b < n_blocks; b += 32) s += partial[static_cast<size_t>(b) * 2 * D + c];
+    }
     part[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && c < 2 * D) {
         s = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) s += part[w][lane];
+        for (int w = 0; w < 32; ++w) s += part[w][lane];
         if (c < D) dgamma[c] = s;
         else if (dbeta != nullptr) dbeta[c - D] = s;
     }

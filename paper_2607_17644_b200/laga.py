@@ -6,6 +6,7 @@ there is no fallback of any kind.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -107,17 +108,19 @@ def _check(code: int, where: str):
         raise LagaError(code, where)
 
 
+# The calls are enqueued from Python, and a decode step makes a handful of them for a few microseconds of device work each: the
+# helpers below are on that path, so they avoid temporaries (plain integers for pointers, no context manager where the tensors'
+# device is already current, no Stream object for the current stream).
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream, device):
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
 def _dev(t: torch.Tensor, dtype, shape, name):
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.shape == shape):
         raise ValueError(f"{name}: expected contiguous CUDA {dtype} tensor of shape {tuple(shape)}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
@@ -135,9 +138,12 @@ def same_device(*tensors) -> torch.device:
     return dev
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(device):
     """Context that makes `device` current for the duration of a library call."""
-    return torch.cuda.device(device)
+    return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
 
 def _geometry(q, c_kv, k_pe, w_kv_b, d_v):
@@ -433,6 +439,8 @@ def rope_plan(d_rot=64, base=10000.0, scaling=None, interleaved=True, device="cu
 
 def _rows(t, name, dims, dtype=torch.bfloat16):
     """A CUDA tensor whose rows (first axis) are dense and may be any pitch apart; returns the pitch in elements."""
+    if t.is_cuda and t.dtype == dtype and t.dim() == dims and t.is_contiguous():
+        return math.prod(t.shape[1:])
     expect = 1
     ok = t.is_cuda and t.dtype == dtype and t.dim() == dims
     if ok:
@@ -509,10 +517,12 @@ def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps=1e-5, latent=None, 
     R = kv_a.shape[1] - D
     if (cache is None) != (slots is None):
         raise ValueError("cache and slots go together")
-    new = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device=kv_a.device)  # noqa: E731
-    latent = new(M, D) if latent is None else _dev(latent, torch.bfloat16, (M, D), "latent")
-    k_pe = new(M, R) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
-    mean, rstd = torch.empty(2, M, dtype=torch.float32, device=kv_a.device).unbind(0)
+    dev = kv_a.device
+    latent = (torch.empty((M, D), dtype=torch.bfloat16, device=dev) if latent is None else
+              _dev(latent, torch.bfloat16, (M, D), "latent"))
+    k_pe = torch.empty((M, R), dtype=torch.bfloat16, device=dev) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
+    mean = torch.empty(M, dtype=torch.float32, device=dev)
+    rstd = torch.empty(M, dtype=torch.float32, device=dev)
     _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, latent, k_pe, mean, rstd, cache, slots, stream)
     return latent, k_pe, mean, rstd
 
@@ -547,14 +557,15 @@ def latent_norm_rope_backward(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions
     need = int(lib().laga_latent_norm_rope_backward_workspace_bytes(M, D))
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    dgamma, dbeta = torch.empty(2, D, dtype=torch.float32, device=dev).unbind(0)
+    dgamma = torch.empty(D, dtype=torch.float32, device=dev)
+    dbeta = torch.empty(D, dtype=torch.float32, device=dev) if with_beta else None
     with _on(dev):
         rc = lib().laga_latent_norm_rope_backward(
             _ptr(dlatent), _ptr(dk_pe), _ptr(kv_a), pitch, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(positions), _ptr(rope.freqs), M, D,
-            R, int(rope.interleaved), float(rope.mscale), _ptr(dkv_a), _ptr(dgamma), _ptr(dbeta) if with_beta else None,
+            R, int(rope.interleaved), float(rope.mscale), _ptr(dkv_a), _ptr(dgamma), _ptr(dbeta),
             _ptr(workspace), workspace.numel(), _stream(stream, dev))
     _check(rc, "laga_latent_norm_rope_backward")
-    return dkv_a, dgamma, dbeta if with_beta else None
+    return dkv_a, dgamma, dbeta
 
 
 class CachePlan(NamedTuple):
@@ -616,10 +627,10 @@ def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, ou
     out = torch.empty(B, h, d_v, dtype=torch.bfloat16, device=dev) if out is None else _dev(out, torch.bfloat16, (B, h, d_v), "out")
     if lse is not None:
         _dev(lse, torch.float32, (B, h), "lse")
-    need = paged_decode_workspace_bytes(B, h, d_c, d_nope, d_rope, d_v)
-    if need == 0:
-        raise LagaError(ERR_UNSUPPORTED, "laga_paged_decode_workspace_bytes")
     if workspace is None:
+        need = paged_decode_workspace_bytes(B, h, d_c, d_nope, d_rope, d_v)
+        if need == 0:
+            raise LagaError(ERR_UNSUPPORTED, "laga_paged_decode_workspace_bytes")
         workspace = alloc_workspace(need, dev)
     with _on(dev):
         rc = lib().laga_paged_decode(_ptr(q), _ptr(w_kv_b), _ptr(cache), n_pages, page_size, _ptr(block_table), block_table.shape[1],
