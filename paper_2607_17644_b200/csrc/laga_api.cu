@@ -1323,10 +1323,11 @@ int laga_latent_norm_rope(const void* kv_a, long long kv_a_pitch, const void* ga
     const int blocks_needed = (M + kLnWarps - 1) / kLnWarps, cap = sm_count() * 3;      // one resident wave at D <= 512
     const dim3 grid(blocks_needed < cap ? blocks_needed : cap), block(kLnWarps * 32);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (D == 512) latent_norm_rope_fwd_kernel<2, true><<<grid, block, 0, st>>>(a);
-    else if (D <= 256) latent_norm_rope_fwd_kernel<1, false><<<grid, block, 0, st>>>(a);
-    else if (D < 512) latent_norm_rope_fwd_kernel<2, false><<<grid, block, 0, st>>>(a);
-    else latent_norm_rope_fwd_kernel<4, false><<<grid, block, 0, st>>>(a);
+    const size_t smem = static_cast<size_t>(kLnWarps) * (D <= 512 ? latent_depth<2>() : latent_depth<4>()) * (D + R) * 2;      // at most 48 KB
+    if (D == 512) latent_norm_rope_fwd_kernel<2, true><<<grid, block, smem, st>>>(a);
+    else if (D <= 256) latent_norm_rope_fwd_kernel<1, false><<<grid, block, smem, st>>>(a);
+    else if (D < 512) latent_norm_rope_fwd_kernel<2, false><<<grid, block, smem, st>>>(a);
+    else latent_norm_rope_fwd_kernel<4, false><<<grid, block, smem, st>>>(a);
     return launch_status();
 }
 

@@ -470,9 +470,9 @@ def rope(x, positions, rope, rot_begin=None, inverse=False, y=None, stream=None)
     M, h, d = x.shape
     x_pitch = _rows(x, "x", 3)
     d_rot = _rope_args(rope, positions, M)
-    y = torch.empty(M, h, d, dtype=torch.bfloat16, device=x.device) if y is None else y
+    y = x.new_empty((M, h, d)) if y is None else y
     y_pitch = _rows(y, "y", 3)
-    if tuple(y.shape) != (M, h, d):
+    if y.shape != (M, h, d):
         raise ValueError(f"y: expected shape {(M, h, d)}, got {tuple(y.shape)}")
     dev = same_device(x, positions, rope.freqs, y)
     if M == 0:
@@ -517,12 +517,11 @@ def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps=1e-5, latent=None, 
     R = kv_a.shape[1] - D
     if (cache is None) != (slots is None):
         raise ValueError("cache and slots go together")
-    dev = kv_a.device
-    latent = (torch.empty((M, D), dtype=torch.bfloat16, device=dev) if latent is None else
-              _dev(latent, torch.bfloat16, (M, D), "latent"))
-    k_pe = torch.empty((M, R), dtype=torch.bfloat16, device=dev) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
-    mean = torch.empty(M, dtype=torch.float32, device=dev)
-    rstd = torch.empty(M, dtype=torch.float32, device=dev)
+    _dev(gamma, torch.bfloat16, (D,), "gamma")
+    latent = gamma.new_empty((M, D)) if latent is None else _dev(latent, torch.bfloat16, (M, D), "latent")
+    k_pe = gamma.new_empty((M, R)) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
+    mean = gamma.new_empty(M, dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, latent, k_pe, mean, rstd, cache, slots, stream)
     return latent, k_pe, mean, rstd
 
@@ -549,21 +548,20 @@ def latent_norm_rope_backward(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions
     _dev(rstd, torch.float32, (M,), "rstd")
     _rope_args(rope, positions, M, R)
     dev = same_device(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope.freqs, dkv_a, workspace)
-    dkv_a = (torch.empty(M, D + R, dtype=torch.bfloat16, device=dev) if dkv_a is None else
-             _dev(dkv_a, torch.bfloat16, (M, D + R), "dkv_a"))
+    dkv_a = dlatent.new_empty((M, D + R)) if dkv_a is None else _dev(dkv_a, torch.bfloat16, (M, D + R), "dkv_a")
     if M == 0:
         sums = torch.zeros(2, D, dtype=torch.float32, device=dev)
         return dkv_a, sums[0], sums[1] if with_beta else None
     need = int(lib().laga_latent_norm_rope_backward_workspace_bytes(M, D))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    dgamma = torch.empty(D, dtype=torch.float32, device=dev)
-    dbeta = torch.empty(D, dtype=torch.float32, device=dev) if with_beta else None
+        workspace = mean.new_empty(need // 4)
+    dgamma = mean.new_empty(D)
+    dbeta = torch.empty_like(dgamma) if with_beta else None
     with _on(dev):
         rc = lib().laga_latent_norm_rope_backward(
             _ptr(dlatent), _ptr(dk_pe), _ptr(kv_a), pitch, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(positions), _ptr(rope.freqs), M, D,
             R, int(rope.interleaved), float(rope.mscale), _ptr(dkv_a), _ptr(dgamma), _ptr(dbeta),
-            _ptr(workspace), workspace.numel(), _stream(stream, dev))
+            _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, dev))
     _check(rc, "laga_latent_norm_rope_backward")
     return dkv_a, dgamma, dbeta
 
@@ -590,8 +588,8 @@ def cache_plan(seq_lens, new_lens, block_table, free_pages, n_free, page_size, m
     _dev(n_free, torch.int32, (1,), "n_free")
     dev = same_device(seq_lens, new_lens, block_table, free_pages, n_free, *(out or ()))
     if out is None:
-        whole = torch.empty(2 * max_tokens + 2 * n + 3, dtype=torch.int32, device=dev)
-        out = CachePlan(*whole.split([max_tokens, max_tokens, n + 1, n, 1, 1]))
+        whole = seq_lens.new_empty(2 * max_tokens + 2 * n + 3)
+        out = CachePlan(*torch.split_with_sizes(whole, [max_tokens, max_tokens, n + 1, n, 1, 1]))
     else:
         for name, size in zip(CachePlan._fields, (max_tokens, max_tokens, n + 1, n, 1, 1)):
             _dev(getattr(out, name), torch.int32, (size,), name)
@@ -624,7 +622,7 @@ def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, ou
     dev = same_device(q, w_kv_b, cache, block_table, seq_lens, out, lse, workspace)
     if softmax_scale is None:
         softmax_scale = d_qk ** -0.5
-    out = torch.empty(B, h, d_v, dtype=torch.bfloat16, device=dev) if out is None else _dev(out, torch.bfloat16, (B, h, d_v), "out")
+    out = q.new_empty((B, h, d_v)) if out is None else _dev(out, torch.bfloat16, (B, h, d_v), "out")
     if lse is not None:
         _dev(lse, torch.float32, (B, h), "lse")
     if workspace is None:
