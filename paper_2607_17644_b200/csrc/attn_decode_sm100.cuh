@@ -74,17 +74,14 @@ struct AttnDecodeArgs {
     float* part_o;                     // [slots][h_pad][512], unnormalised
     float2* part_ml;                   // [slots][h_pad]: running maximum (log2 domain), sum
     int h_pad;
-    int* tile_start;                   // [B + 1] first tile of each request on the line; written by CTA 0 for the combine
     unsigned* status;
 };
 
+// Length of a request, held within the table's row whatever the caller's array says (2^30 tokens at most).
+__device__ __forceinline__ int decode_clamp(int len, int columns, int page_shift) { return max(0, min(len, columns << page_shift)); }
 __device__ __forceinline__ int decode_len(const AttnDecodeArgs& a, int b) {
-    const int len = __ldg(a.seq_lens + b);
-    const long long most = static_cast<long long>(a.columns) << a.page_shift;
-    if (len < 0 || len > most) {       // never read past the table's row
-        atomicCAS(a.status, kStatusOk, kStatusCheck | 0xF0u);
-        return len < 0 ? 0 : static_cast<int>(most);
-    }
+    const int given = __ldg(a.seq_lens + b), len = decode_clamp(given, a.columns, a.page_shift);
+    if (len != given) atomicCAS(a.status, kStatusOk, kStatusCheck | 0xF0u);
     return len;
 }
 
@@ -199,14 +196,11 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
         const int per = (total + args.ctas_per_group - 1) / args.ctas_per_group;
         const int g0 = cta * per;
         my_tiles = min(per, total - g0);               // may be negative: nothing to do
-        const bool publish = blockIdx.x == 0;
         for (int b = b0; b < b1; ++b) {
             const int n = (decode_len(args, b) + kDecKeys - 1) / kDecKeys;
-            if (publish) args.tile_start[b] = before;
             if (g0 >= before && g0 < before + n) { *start_b = b; *start_t = g0 - before; }
             before += n;
         }
-        if (publish && threadIdx.x == 0) args.tile_start[args.B] = total;
         __syncthreads();
     }
     const int first_b = *start_b, first_t = *start_t;
@@ -687,20 +681,21 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 // call writes them).  A warp per request turns the maxima and sums into weights first, so that the loads of the pieces
 // themselves (2 KB each) depend on nothing and run eight deep.
 // A request without tokens has no piece: zeros, LSE -inf.
-constexpr int kProjectThreads = 512;
+constexpr int kProjectThreads = 1024, kProjectGroups = kProjectThreads / 128;
 struct DecodeProjectSmem {
     static constexpr int kW = 0;                                 // two slabs of 512 rows x 64 values
     static constexpr int kWSlab = 512 * 128;
     static constexpr int kO = kW + 2 * kWSlab;                   // eight slabs of 32 rows x 64 latents
     static constexpr int kOSlab = 32 * 128;
-    static constexpr int kRed = kO + 8 * kOSlab;                 // [4][512] floats
-    static constexpr int kWeights = kRed + 4 * 512 * 4;          // a float per piece: at most one per CTA and one more per request
+    static constexpr int kRed = kO + 8 * kOSlab;                 // [groups][512] floats
+    static constexpr int kWeights = kRed + kProjectGroups * 512 * 4;          // a float per piece: at most one per CTA and one more per request
     static constexpr int kBar = kWeights + (kDecMaxCtas + 20) * 4;
     static constexpr int kTotalBytes = kBar + 32;
 };
 __global__ void __launch_bounds__(kProjectThreads, 1)
 decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
-                      const int* __restrict__ tile_start, int B, int h, int h_pad, int ctas_per_group, int requests_per_cta,
+                      const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad, int ctas_per_group,
+                      int requests_per_cta,
                       __nv_bfloat16* __restrict__ out, float* __restrict__ lse, unsigned* status) {
     using L = DecodeProjectSmem;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -710,6 +705,7 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
     float* red = reinterpret_cast<float*>(smem + L::kRed);
     float* weights = reinterpret_cast<float*>(smem + L::kWeights);
+    int* sums = reinterpret_cast<int*>(red);                     // 64 words, before `red` is needed
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int head = blockIdx.x, b0 = blockIdx.y * requests_per_cta, n_req = min(requests_per_cta, B - b0);
     if (threadIdx.x == 0) {
@@ -729,17 +725,46 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
     grid_launch_dependents();
-    grid_dependency_wait();
-
-    const int total = tile_start[B];
-    const int per = max(1, (total + ctas_per_group - 1) / ctas_per_group);
-    // Weights: warp r takes request r.  Lane l of every warp knows the pieces of request l.
+    // Where the requests' tiles lie on the line, from the lengths again (an input of the call: nothing to wait for).  Lane l of
+    // every warp then knows the pieces of request b0 + l.
     int first = 0, count = 0;
-    if (lane < n_req) {
-        const int begin = tile_start[b0 + lane], end = tile_start[b0 + lane + 1];
+    {
+        const int run = (B + kProjectThreads - 1) / kProjectThreads;
+        const int s0 = min(B, static_cast<int>(threadIdx.x) * run), s1 = min(B, s0 + run);
+        int sum = 0, before = 0;                                 // tiles of this thread's requests, and of those of them before b0
+        for (int b = s0; b < s1; ++b) {
+            const int n = (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kDecKeys - 1) / kDecKeys;
+            sum += n;
+            before += b < b0 ? n : 0;
+        }
+        const int mine = lane < n_req ? (decode_clamp(__ldg(seq_lens + b0 + lane), columns, page_shift) + kDecKeys - 1) / kDecKeys : 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            before += __shfl_xor_sync(0xffffffffu, before, d);
+        }
+        if (lane == 0) { sums[warp] = sum; sums[32 + warp] = before; }
+        __syncthreads();
+        sum = sums[lane];
+        before = sums[32 + lane];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            before += __shfl_xor_sync(0xffffffffu, before, d);
+        }
+        const int per = max(1, (sum + ctas_per_group - 1) / ctas_per_group);
+        int incl = mine;
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += v;
+        }
+        const int begin = before + incl - mine;
         first = begin / per;
-        count = end > begin ? (end - 1) / per - first + 1 : 0;
+        count = mine > 0 ? (begin + mine - 1) / per - first + 1 : 0;
     }
+    grid_dependency_wait();
+    // Weights: warp r takes request r.
     int base = count;                                            // where the request's weights begin in shared memory
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) {
@@ -776,11 +801,11 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
             lse[static_cast<size_t>(b0 + warp) * h + head] = n > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
     }
     __syncthreads();
-    // Sums: four groups of 128 threads, four channels a thread.  A group takes every fourth request; with one or two requests in
-    // the CTA four or two groups share one (every fourth or second piece).
+    // Sums: groups of 128 threads, four channels a thread, a request each; with fewer requests than groups, the groups that share one
+    // take every second, fourth or eighth piece.
     const int group = warp >> 2, cg = threadIdx.x & 127;
-    const int split = n_req == 1 ? 4 : n_req == 2 ? 2 : 1;
-    for (int r0 = 0; r0 < n_req; r0 += 4 / split) {
+    const int split = n_req == 1 ? kProjectGroups : n_req == 2 ? kProjectGroups / 2 : n_req <= 4 ? kProjectGroups / 4 : 1;
+    for (int r0 = 0; r0 < n_req; r0 += kProjectGroups / split) {
         const int r = r0 + group / split, src = r < n_req ? r : 0;
         const int f = __shfl_sync(0xffffffffu, first, src), n = r < n_req ? __shfl_sync(0xffffffffu, count, src) : 0,
                   at = __shfl_sync(0xffffffffu, base, src);

@@ -118,7 +118,7 @@ def test_paged_decode_refusals_and_sizes(laga):
         heads = 16 if h <= 16 else 32 if h <= 32 else 64
         groups = -(-h // heads)
         slots = max(1, 148 // groups) + B
-        assert size(B, h) >= slots * groups * heads * (512 * 4 + 8) + B * h * 512 * 2 + 4 * (B + 1) + 1024
+        assert size(B, h) >= slots * groups * heads * (512 * 4 + 8) + B * h * 512 * 2 + 1024
 
 
 def test_binding_refuses_cpu_tensors_and_wrong_types(laga):
