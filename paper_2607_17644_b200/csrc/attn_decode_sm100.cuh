@@ -210,6 +210,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
     } else if (warp == kDecProducerWarp) {
         // ---- producer ------------------------------------------------------------------------------------
         const int n_rows = args.n_pages << args.page_shift;
+        const uint64_t once = l2_evict_first();              // (the head groups that share a tile read it at nearly the same time)
         // first cache row of the keys from `key` on, within one page
         auto row_of = [&](const DecodeCursor& c, int key) -> int {
             if (key >= c.len) return n_rows;                                   // beyond the request: never issued
@@ -249,7 +250,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     if (!mbar_wait(r_empty, r_par ^ 1u, abort_flag, args.status, 0xB1)) break;
                     mbar_arrive_expect_tx(r_full, L::kSlab);
                     armed.arm(r_full, r_par);
-                    tma_load_3d(smem + L::kRope, &tmap_rope, r_full, 0, row, 8);
+                    tma_load_3d(smem + L::kRope, &tmap_rope, r_full, 0, row, 8, once);
                     r_par ^= 1u;
 #pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
@@ -257,7 +258,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                         if (!ok) break;
                         mbar_arrive_expect_tx(&h_full[slot], L::kHalf);
                         armed.arm(&h_full[slot], par);
-                        tma_load_3d(smem + L::kHalf0 + slot * L::kHalf, &tmap_lat, &h_full[slot], 0, row, half * 4);
+                        tma_load_3d(smem + L::kHalf0 + slot * L::kHalf, &tmap_lat, &h_full[slot], 0, row, half * 4, once);
                         if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                     }
                     if (!ok) break;
@@ -301,7 +302,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (lane < boxes) tma_load_3d(smem + L::kRope + lane * page * 128, &tmap_rope, r_full, 0, row, 8);
+                if (lane < boxes) tma_load_3d(smem + L::kRope + lane * page * 128, &tmap_rope, r_full, 0, row, 8, once);
                 r_par ^= 1u;
                 for (int half = 0; half < 2; ++half) {
                     if (lane == 0) {
@@ -316,7 +317,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     const int slab = lane / n_sub;                                          // lanes 0 .. 4 n_sub - 1: box `sub` of slab `slab`
                     if (slab < 4 && sub < boxes)
                         tma_load_3d(smem + L::kHalf0 + slot * L::kHalf + slab * L::kSlab + sub * page * 128, &tmap_rope, &h_full[slot], 0, row,
-                                    half * 4 + slab);
+                                    half * 4 + slab, once);
                     if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                 }
                 if (!ok) break;
@@ -604,7 +605,7 @@ struct DecodeAbsorbSmem {
 template <int kRequests>
 __global__ void __launch_bounds__(kAbsorbThreads)
 decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, int B, int h,
-                     __nv_bfloat16* __restrict__ q_abs, unsigned* status, int status_words) {
+                     const __nv_bfloat16* __restrict__ w, __nv_bfloat16* __restrict__ q_abs, unsigned* status, int status_words) {
     using L = DecodeAbsorbSmem<kRequests>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
@@ -631,6 +632,11 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
     tc_fence_after_sync();
     grid_launch_dependents();
     const uint32_t tmem = *tmem_slot;
+    if (b0 == 0) {      // W_uv of the same rows, for decode_project_kernel: 256 bytes a row, pages apart, slow to come from memory when needed
+        const __nv_bfloat16* row = w + (static_cast<size_t>(c0 + threadIdx.x) * h + head) * 256 + 128;
+        l2_prefetch(row);
+        l2_prefetch(row + 64);
+    }
     if (warp == 0) {
         if (elect_one()) {
             mbar_arrive_expect_tx(full, 2 * 128 * 128 + 2 * kRequests * 128);

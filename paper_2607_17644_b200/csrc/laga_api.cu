@@ -748,7 +748,7 @@ int launch_decode_absorb(const void* q, const void* w, int B, int h, void* q_abs
     if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, kRequests))
         return LAGA_ERR_CUDA;
     launch_kernel(decode_absorb_kernel<kRequests>, dim3(kDc / 128, h, (B + kRequests - 1) / kRequests), dim3(kAbsorbThreads),
-                  DecodeAbsorbSmem<kRequests>::kTotalBytes, stream, false, tw, tq, B, h, static_cast<__nv_bfloat16*>(q_abs), status,
+                  DecodeAbsorbSmem<kRequests>::kTotalBytes, stream, false, tw, tq, B, h, static_cast<const __nv_bfloat16*>(w), static_cast<__nv_bfloat16*>(q_abs), status,
                   static_cast<int>(kStatusClearBytes / sizeof(unsigned)));
     return launch_status();
 }
