@@ -10,7 +10,7 @@ absence is an error: there is no CPU or eager fallback.
 """
 from .inputs import CONFIGS, CONFIG_SEEDS, LagaShape, make_inputs  # noqa: F401
 
-__all__ = ["CONFIGS", "CONFIG_SEEDS", "LagaShape", "make_inputs", "laga", "laga_attention", "LagaBlock"]
+__all__ = ["CONFIGS", "CONFIG_SEEDS", "LagaShape", "make_inputs", "laga", "laga_attention", "LagaBlock", "LatentCache"]
 
 
 def __getattr__(name):
@@ -21,4 +21,6 @@ def __getattr__(name):
         return importlib.import_module(".autograd", __name__).laga_attention
     if name == "LagaBlock":               # Algorithm 1 with one rank, every step on the library's kernels
         return importlib.import_module(".block", __name__).LagaBlock
+    if name == "LatentCache":             # paged latent cache of a service: page pool, tables, lengths
+        return importlib.import_module(".serving", __name__).LatentCache
     raise AttributeError(name)

@@ -6,9 +6,15 @@ step executed by the library's kernels:
   step 7   W_o(reshape(out))                                                        laga_linear
 
 Steps 2, 3 and 6 are the sequence-parallel exchanges (``sp.py``); with one rank they are the identity.
-This module is torch.autograd plumbing only: three ``autograd.Function``s that hand tensors to the C ABI
+This module is torch.autograd plumbing only: ``autograd.Function``s that hand tensors to the C ABI
 entry points and a module that owns the block's weights.  As in Algorithm 1, q_rope and k_pe are taken as
-the projections deliver them (the paper's algorithm has no rotary step of its own).
+the projections deliver them (the paper's algorithm has no rotary step of its own) unless the block is given a
+rotation (``rope``, from ``laga.rope_plan``): then step 1 ends with laga_rope on the queries, and laga_latent_norm_rope
+takes the latent's norm and the key's rotation in one pass over what W_kv_a delivers.
+
+In service the block keeps, per token, the normalised latent and the rotated key in a paged cache (``serving.LatentCache``):
+``prefill`` runs prompts through the path above and fills the cache, ``decode`` adds one token per request and attends
+to the cache through laga_paged_decode.
 
 Weights are stored as [in_features, out_features] (y = x W), the layout ``W_kv_b`` already has.  Weight
 gradients leave the kernels in fp32 and are handed to autograd in the weight's dtype.
@@ -50,6 +56,46 @@ class _LayerNorm(torch.autograd.Function):
         return dx, dgamma.to(gamma.dtype), (dbeta.to(gamma.dtype) if ctx.has_beta else None), None
 
 
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, positions, rope):
+        ctx.save_for_backward(positions, rope.freqs)
+        ctx.mscale, ctx.interleaved = rope.mscale, rope.interleaved
+        return laga.rope(x, positions, rope)
+
+    @staticmethod
+    def backward(ctx, dy):
+        positions, freqs = ctx.saved_tensors
+        return laga.rope(dy.contiguous(), positions, laga.RopePlan(freqs, ctx.mscale, ctx.interleaved), inverse=True), None, None
+
+
+class _LatentNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, kv_a, gamma, beta, positions, rope, eps):
+        latent, k_pe, mean, rstd = laga.latent_norm_rope(kv_a, gamma, beta, positions, rope, eps)
+        ctx.save_for_backward(kv_a, gamma, mean, rstd, positions, rope.freqs)
+        ctx.mscale, ctx.interleaved, ctx.has_beta = rope.mscale, rope.interleaved, beta is not None
+        return latent, k_pe
+
+    @staticmethod
+    def backward(ctx, dlatent, dk_pe):
+        kv_a, gamma, mean, rstd, positions, freqs = ctx.saved_tensors
+        dkv_a, dgamma, dbeta = laga.latent_norm_rope_backward(dlatent.contiguous(), dk_pe.contiguous(), kv_a, gamma, mean, rstd, positions,
+                                                              laga.RopePlan(freqs, ctx.mscale, ctx.interleaved),
+                                                              with_beta=ctx.has_beta)
+        return dkv_a, dgamma.to(gamma.dtype), (dbeta.to(gamma.dtype) if ctx.has_beta else None), None, None, None
+
+
+def rotary(x: torch.Tensor, positions: torch.Tensor, rope) -> torch.Tensor:
+    """The last channels of every head of x [S, h, d] rotated, through laga_rope (differentiable in x)."""
+    return _Rotary.apply(x, positions, rope)
+
+
+def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps: float = 1e-5):
+    """(latent, k_pe) from the output of W_kv_a, through laga_latent_norm_rope / laga_latent_norm_rope_backward."""
+    return _LatentNormRope.apply(kv_a, gamma, beta, positions, rope, eps)
+
+
 def linear(x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
     """y[M, N] = x[M, K] . w[K, N] through laga_linear / laga_linear_backward (bf16 CUDA tensors)."""
     return _Linear.apply(x, w)
@@ -63,12 +109,14 @@ def layernorm(x: torch.Tensor, gamma: torch.Tensor, beta=None, eps: float = 1e-5
 class LagaBlock(torch.nn.Module):
     """hidden [S, d_model] -> [S, d_model]: Algorithm 1 with P = 1 for ``n_heads`` heads of the DeepSeek-V3
     geometry (d_nope 128, d_rope 64, d_v 128, d_c 512).  ``forward(hidden, cu_seqlens=None)``: with
-    ``cu_seqlens`` the rows are packed sequences and attention stays inside each."""
+    ``cu_seqlens`` the rows are packed sequences and attention stays inside each.  ``rope``: the rotation of the rope bands
+    (``laga.rope_plan``); None takes them as the projections deliver them, and the block then has no prefill / decode."""
 
     D_NOPE, D_ROPE, D_V, D_C = 128, 64, 128, 512
 
-    def __init__(self, d_model: int, n_heads: int, eps: float = 1e-5, device="cuda", seed: int = 0):
+    def __init__(self, d_model: int, n_heads: int, eps: float = 1e-5, device="cuda", seed: int = 0, rope=None):
         super().__init__()
+        self.rope = rope
         g = torch.Generator().manual_seed(seed)
 
         def weight(k, n):     # variance-preserving draw, rounded once to bf16
@@ -83,11 +131,64 @@ class LagaBlock(torch.nn.Module):
         self.ln_gamma = torch.nn.Parameter(torch.ones(self.D_C, dtype=torch.bfloat16, device=device))
         self.ln_beta = torch.nn.Parameter(torch.zeros(self.D_C, dtype=torch.bfloat16, device=device))
 
-    def forward(self, hidden: torch.Tensor, cu_seqlens=None, causal: bool = True) -> torch.Tensor:
+    @staticmethod
+    def positions(n_tokens: int, cu_seqlens=None, device="cuda") -> torch.Tensor:
+        """int32 [n_tokens]: each token's place in its sequence (the rows are one sequence without cu_seqlens)."""
+        pos = torch.arange(n_tokens, dtype=torch.int32)
+        for begin, end in zip(cu_seqlens[:-1], cu_seqlens[1:]) if cu_seqlens is not None else ():
+            pos[int(begin):int(end)] -= int(begin)
+        return pos.to(device, non_blocking=True)
+
+    def _project(self, hidden, positions):
+        """Step 1: queries, latent and shared key."""
         S = hidden.shape[0]
-        q = linear(hidden, self.w_q).view(S, self.n_heads, self.D_NOPE + self.D_ROPE)            # step 1
+        q = linear(hidden, self.w_q).view(S, self.n_heads, self.D_NOPE + self.D_ROPE)
         kv_a = linear(hidden, self.w_kv_a)
-        latent = layernorm(kv_a[:, :self.D_C].contiguous(), self.ln_gamma, self.ln_beta, self.eps)
-        k_pe = kv_a[:, self.D_C:].contiguous()
+        if self.rope is None:
+            latent = layernorm(kv_a[:, :self.D_C].contiguous(), self.ln_gamma, self.ln_beta, self.eps)
+            return q, latent, kv_a[:, self.D_C:].contiguous()
+        return (rotary(q, positions, self.rope),
+                *latent_norm_rope(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, self.eps))
+
+    def forward(self, hidden: torch.Tensor, cu_seqlens=None, causal: bool = True, positions=None) -> torch.Tensor:
+        """positions (int32 [S], only with ``rope``): by default each token's place in its sequence."""
+        S = hidden.shape[0]
+        if self.rope is not None and positions is None:
+            positions = self.positions(S, cu_seqlens, hidden.device)
+        q, latent, k_pe = self._project(hidden, positions)                                        # step 1
         out = laga_attention(q, latent, k_pe, self.w_kv_b, causal=causal, cu_seqlens=cu_seqlens)   # steps 4-5
         return linear(out.reshape(S, self.n_heads * self.D_V), self.w_o)                          # step 7
+
+    def _service(self):
+        if self.rope is None:
+            raise ValueError("prefill and decode need the block's rotation: LagaBlock(..., rope=laga.rope_plan(64))")
+
+    @torch.no_grad()
+    def prefill(self, hidden: torch.Tensor, pages: torch.Tensor, step, cu_seqlens) -> torch.Tensor:
+        """Prompts of requests that have nothing in the cache yet, packed: hidden [T, d_model], cu_seqlens their host
+        boundaries (the same lengths that ``step``, a plan of ``LatentCache.plan``, was made for), pages one layer's
+        cache [n_pages, page_size, 576].  Returns the block's output [T, d_model]; the cache holds the prompts afterwards."""
+        self._service()
+        T = hidden.shape[0]
+        q = laga.linear(hidden, self.w_q)[0].view(T, self.n_heads, self.D_NOPE + self.D_ROPE)
+        kv_a = laga.linear(hidden, self.w_kv_a)[0]
+        positions, slots = step.positions[:T], step.slots[:T]
+        laga.rope(q, positions, self.rope, y=q)
+        latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
+        out = laga.fwd(q, latent, k_pe, self.w_kv_b, cu_seqlens=cu_seqlens)[0]
+        return laga.linear(out.view(T, self.n_heads * self.D_V), self.w_o)[0]
+
+    @torch.no_grad()
+    def decode(self, hidden: torch.Tensor, pages: torch.Tensor, step, block_table: torch.Tensor, workspace=None) -> torch.Tensor:
+        """One new token for each of B requests: hidden [B, d_model], ``step`` a plan that gives every request one token,
+        block_table the plan's table [B, columns].  Appends the tokens' latents and keys to ``pages`` and attends to each request's
+        whole cache, the new token included.  Every call reads lengths and tables on the device, so a step can be captured in a
+        graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``) and replayed."""
+        self._service()
+        B = hidden.shape[0]
+        q = laga.linear(hidden, self.w_q)[0].view(B, self.n_heads, self.D_NOPE + self.D_ROPE)
+        kv_a = laga.linear(hidden, self.w_kv_a)[0]
+        laga.rope(q, step.positions, self.rope, y=q)
+        laga.cache_append(kv_a, self.ln_gamma, self.ln_beta, step.positions, self.rope, step.slots, pages, eps=self.eps)
+        out = laga.paged_decode(q, self.w_kv_b, pages, block_table, step.seq_lens, workspace=workspace)[0]
+        return laga.linear(out.view(B, self.n_heads * self.D_V), self.w_o)[0]

@@ -11,7 +11,7 @@
 // (2 pi), reduced to its fraction in fp64, becomes a 64-bit fraction of a turn, and position times that, modulo 2^64, is the
 // fraction of a turn to 2^-34 at any 32-bit position -- two integer multiplications, where fp64 arithmetic cost three times the
 // instructions.  Sine and cosine of the reduced angle in [-pi, pi] come from the special-function unit, whose absolute error
-// below 2^-21 is far under the half step (2^-9) of the bf16 result.
+// below 2^-21 is far under the half step (2^-8) of the bf16 result.
 //
 // Everything here reads and writes every element once; the kernels come close enough to HBM speed that instructions count
 // (a warp moves 512 bytes per load, and an SM gets 4 instructions per clock for about 23 bytes per clock).

@@ -1,0 +1,50 @@
+"""State of a service around ``LagaBlock``: a pool of cache pages shared by a fixed number of request rows.
+
+One token's entry is its normalised latent and its rotated shared key, 576 bf16 channels for all heads together.  The
+tables are the same for every layer, so one ``LatentCache`` serves a stack of layers: ``pages[layer]`` is what a layer's
+calls read and write.  Everything lives on the device and is updated there (laga_cache_plan); nothing here waits for the GPU.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import laga
+
+
+class LatentCache:
+    """n_pages pages of page_size tokens (a power of two from 16 to 1024) in each of n_layers layers; n_requests rows of at
+    most max_tokens tokens."""
+
+    ROW = 576
+
+    def __init__(self, n_pages: int, n_requests: int, max_tokens: int, page_size: int = 64, n_layers: int = 1, device="cuda"):
+        if min(n_pages, n_requests, max_tokens, n_layers) < 1:
+            raise ValueError("LatentCache: sizes must be at least 1")
+        if page_size not in (16, 32, 64, 128, 256, 512, 1024):
+            raise ValueError(f"LatentCache: page_size must be a power of two from 16 to 1024, got {page_size}")
+        i32 = dict(dtype=torch.int32, device=device)
+        self.page_size, self.columns = page_size, -(-max_tokens // page_size)
+        self.pages = [torch.zeros(n_pages, page_size, self.ROW, dtype=torch.bfloat16, device=device) for _ in range(n_layers)]
+        self.block_table = torch.zeros(n_requests, self.columns, **i32)
+        self.seq_lens = torch.zeros(n_requests, **i32)
+        self.free_pages = torch.zeros(n_pages + 1, **i32)          # a stack; the last entry only absorbs what `release` drops
+        self.free_pages[:n_pages] = torch.arange(n_pages - 1, -1, -1, **i32)
+        self.n_free = torch.full((1,), n_pages, **i32)
+
+    def plan(self, new_lens: torch.Tensor, max_tokens: int) -> laga.CachePlan:
+        """Places new_lens[b] (int32 [n_requests], on the device) tokens for each request and makes the result the cache's
+        state.  A step that does not fit takes nothing and gives every row slot -1: ``laga.check_status(plan.status)`` tells."""
+        step = laga.cache_plan(self.seq_lens, new_lens, self.block_table, self.free_pages, self.n_free, self.page_size, max_tokens)
+        self.seq_lens.copy_(step.seq_lens)
+        self.n_free.copy_(step.n_free)
+        return step
+
+    def release(self, request: int) -> None:
+        """Gives a request's pages back and empties its row."""
+        column = torch.arange(self.columns, device=self.seq_lens.device)
+        held = (self.seq_lens[request] + self.page_size - 1) // self.page_size
+        # behind the top of the stack; columns the request does not hold go to the spare last entry
+        at = torch.where(column < held, self.n_free + column, self.free_pages.numel() - 1)
+        self.free_pages.scatter_(0, at, self.block_table[request])
+        self.n_free += held
+        self.seq_lens[request] = 0

@@ -1,0 +1,170 @@
+"""The rotary block in training and in service: gradients through the whole block against the float64 pieces, prompts and
+decode steps through the paged cache against the same tokens in one pass, captured decode steps, and release of pages."""
+import pytest
+import torch
+
+import serving_reference as ref
+from parity import rel_l2
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2607_17644_b200 as _pkg
+    _pkg.laga.lib()
+    return _pkg
+
+
+def bf(t):
+    return t.to(torch.float32).to(BF16)
+
+
+def make_block(pkg, d_model=512, heads=4, interleaved=True, seed=3):
+    blk = pkg.LagaBlock(d_model, heads, seed=seed, rope=pkg.laga.rope_plan(64, interleaved=interleaved))
+    with torch.no_grad():
+        g = torch.Generator().manual_seed(seed)
+        blk.ln_gamma.copy_((1 + 0.2 * torch.randn(512, generator=g)).to(BF16))
+        blk.ln_beta.copy_((0.1 * torch.randn(512, generator=g)).to(BF16))
+    return blk
+
+
+@pytest.mark.parametrize("interleaved,cu", [(True, None), (False, [0, 130, 131, 400])])
+def test_block_with_rotation_forward_and_backward(pkg, oracle, interleaved, cu):
+    """As the block's test without rotation, with the float64 rotation in between; bf16 exactly where the block hands a bf16
+    tensor on.  Tolerances are that test's: the rotation adds one rounding to q and k_pe, which that chain had none of, of
+    at most 2^-8 relative against the chain's 1e-2."""
+    blk = make_block(pkg, interleaved=interleaved)
+    S, H = 400, blk.n_heads
+    g = torch.Generator().manual_seed(11)
+    hidden, d_out = (torch.randn(S, 512, generator=g).to(BF16) for _ in range(2))
+    h_dev = hidden.cuda().requires_grad_(True)
+    y = blk(h_dev, cu_seqlens=cu)
+    y.backward(d_out.cuda())
+    w_q, w_kv_a, w_kv_b, w_o = (p.detach().cpu() for p in (blk.w_q, blk.w_kv_a, blk.w_kv_b, blk.w_o))
+    gamma, beta, freqs = blk.ln_gamma.detach().cpu(), blk.ln_beta.detach().cpu(), blk.rope.freqs.cpu()
+    bounds = cu or [0, S]
+    pos = blk.positions(S, cu, "cpu")
+    assert pos.tolist() == [i for a, b in zip(bounds[:-1], bounds[1:]) for i in range(b - a)]
+    turn = lambda t, inv=False: ref.rotate(t.double(), pos, freqs, 1.0, interleaved, inv)[0]  # noqa: E731
+    q = bf(turn(bf(oracle.linear(hidden, w_q)).view(S, H, 192)))
+    kv_a = bf(oracle.linear(hidden, w_kv_a))
+    pre = kv_a[:, :512].contiguous()
+    latent, k_pe = bf(oracle.layernorm(pre, gamma, beta, blk.eps)[0]), bf(turn(kv_a[:, 512:]))
+    out = torch.zeros(S, H, 128, dtype=torch.float64)
+    for a, b in zip(bounds[:-1], bounds[1:]):
+        out[a:b] = oracle.fwd(q[a:b], latent[a:b], k_pe[a:b], w_kv_b, 128, 192 ** -0.5, causal=True, kv_round_bf16=True)[0]
+    out_b = bf(out).reshape(S, H * 128)
+    assert rel_l2(y.detach(), oracle.linear(out_b, w_o)) <= 1e-2
+    d2, dw_o = oracle.linear_bwd(d_out, out_b, w_o)
+    d3 = bf(d2).view(S, H, 128)
+    dq, dlat, dkpe = torch.zeros(S, H, 192).double(), torch.zeros(S, 512).double(), torch.zeros(S, 64).double()
+    dw_kv_b = torch.zeros_like(w_kv_b, dtype=torch.float64)
+    for a, b in zip(bounds[:-1], bounds[1:]):
+        r = oracle.bwd(q[a:b], latent[a:b], k_pe[a:b], w_kv_b, d3[a:b], 128, 192 ** -0.5, causal=True, kv_round_bf16=True)
+        dq[a:b], dlat[a:b], dkpe[a:b] = r["dq"], r["dc_kv"], r["dk_pe"]
+        dw_kv_b += r["dw"]
+    dpre, dgamma, dbeta = oracle.layernorm_bwd(bf(dlat), pre, gamma, blk.eps)
+    d_kv_a = torch.cat([bf(dpre), bf(turn(bf(dkpe), True))], 1)
+    dh1, dw_q = oracle.linear_bwd(bf(turn(bf(dq), True)).reshape(S, H * 192), hidden, w_q)
+    dh2, dw_kv_a = oracle.linear_bwd(d_kv_a, hidden, w_kv_a)
+    assert rel_l2(h_dev.grad, bf(dh1).double() + bf(dh2).double()) <= 1.5e-2
+    for name, want in (("w_q", dw_q), ("w_kv_a", dw_kv_a), ("w_kv_b", dw_kv_b), ("w_o", dw_o), ("ln_gamma", dgamma), ("ln_beta", dbeta)):
+        assert rel_l2(getattr(blk, name).grad, want) <= 2e-2, name
+
+
+def test_prompts_and_decode_steps_against_one_pass(pkg):
+    """Three requests, prompts of 70, 1 and 129 tokens, then 20 decode steps (crossing pages): every output row against the
+    block's forward over the whole sequences.  The decode's absorbed form and the forward's explicit form round differently
+    (q W_uk and the latent output against K and V), each by a few bf16 half steps (each at most 2^-8 relative) on a chain of
+    equal roundings: 2e-2 on the output rows, which the block's own comparison bounds at 1e-2 a side."""
+    laga = pkg.laga
+    blk = make_block(pkg, heads=16)
+    prompts, steps, page = [70, 1, 129], 20, 16
+    g = torch.Generator().manual_seed(5)
+    seqs = [torch.randn(n + steps, 512, generator=g).to(BF16).cuda() for n in prompts]
+    cache = pkg.LatentCache(n_pages=24, n_requests=3, max_tokens=160, page_size=page)
+    pages = cache.pages[0]
+    cu = [0, 70, 71, 200]
+    step = cache.plan(torch.tensor(prompts, dtype=torch.int32, device="cuda"), 200)
+    laga.check_status(step.status)
+    outs = [blk.prefill(torch.cat([s[:n] for s, n in zip(seqs, prompts)]), pages, step, cu)]
+    one = torch.ones(3, dtype=torch.int32, device="cuda")
+    decoded = []
+    for i in range(steps):
+        step = cache.plan(one, 3)
+        decoded.append(blk.decode(torch.stack([s[n + i] for s, n in zip(seqs, prompts)]), pages, step, cache.block_table))
+        laga.check_status(step.status)
+    assert cache.seq_lens.tolist() == [n + steps for n in prompts]
+    assert cache.n_free.item() == 24 - sum(-(-(n + steps) // page) for n in prompts)
+    held = [cache.block_table[b, : -(-(n + steps) // page)].tolist() for b, n in enumerate(prompts)]
+    assert len(set(sum(held, []))) == len(sum(held, []))                # no page twice
+    for b, n in enumerate(prompts):
+        whole = blk(seqs[b])
+        assert rel_l2(outs[0][cu[b]:cu[b + 1]], whole[:n]) <= 1e-6      # the same kernels on the same rows
+        assert rel_l2(torch.stack([d[b] for d in decoded]), whole[n:]) <= 2e-2
+
+
+def test_captured_decode_steps_equal_eager_ones(pkg):
+    """plan + decode captured once and replayed: lengths, tables and pages advance on the device."""
+    laga = pkg.laga
+    blk = make_block(pkg, heads=16)
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn(6, 4, 512, generator=g).to(BF16).cuda()
+
+    def service():
+        cache = pkg.LatentCache(n_pages=16, n_requests=4, max_tokens=64, page_size=16)
+        first = torch.tensor([14, 0, 30, 5], dtype=torch.int32, device="cuda")
+        prompt = torch.randn(49, 512, generator=torch.Generator().manual_seed(7)).to(BF16).cuda()
+        blk.prefill(prompt, cache.pages[0], cache.plan(first, 49), [0, 14, 14, 44, 49])
+        return cache
+
+    one = torch.ones(4, dtype=torch.int32, device="cuda")
+    eager_cache, cache = service(), service()
+    ws = laga.alloc_workspace(laga.paged_decode_workspace_bytes(4, 16))
+    eager = []
+    for i in range(6):
+        step = eager_cache.plan(one, 4)
+        eager.append(blk.decode(x[i], eager_cache.pages[0], step, eager_cache.block_table))
+    static = torch.empty_like(x[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step = cache.plan(one, 4)
+        y = blk.decode(static, cache.pages[0], step, cache.block_table, workspace=ws)
+    for i in range(6):
+        static.copy_(x[i])
+        graph.replay()
+        assert torch.equal(y, eager[i]), i
+    assert torch.equal(cache.seq_lens, eager_cache.seq_lens) and torch.equal(cache.block_table, eager_cache.block_table)
+
+
+def test_full_cache_takes_nothing_and_release_gives_back(pkg):
+    laga = pkg.laga
+    cache = pkg.LatentCache(n_pages=4, n_requests=2, max_tokens=64, page_size=16)
+    cache.plan(torch.tensor([33, 16], dtype=torch.int32, device="cuda"), 64)
+    assert cache.n_free.item() == 0
+    before = cache.block_table.clone()
+    full = cache.plan(torch.tensor([0, 1], dtype=torch.int32, device="cuda"), 64)
+    with pytest.raises(laga.LagaError) as err:
+        laga.check_status(full.status)
+    assert err.value.code == laga.ERR_CACHE_PLAN
+    assert cache.seq_lens.tolist() == [33, 16] and torch.equal(cache.block_table, before) and bool((full.slots == -1).all())
+    pages = sorted(before[0, :3].tolist())
+    cache.release(0)
+    assert cache.seq_lens.tolist() == [0, 16] and cache.n_free.item() == 3 and sorted(cache.free_pages[:3].tolist()) == pages
+    again = cache.plan(torch.tensor([16, 17], dtype=torch.int32, device="cuda"), 64)
+    laga.check_status(again.status)
+    assert cache.n_free.item() == 0 and cache.seq_lens.tolist() == [16, 33]
+    assert sorted(cache.block_table[0, :1].tolist() + cache.block_table[1, :3].tolist()) == [0, 1, 2, 3]
+
+
+def test_service_needs_a_rotation(pkg):
+    blk = pkg.LagaBlock(256, 2)
+    with pytest.raises(ValueError):
+        blk.decode(None, None, None, None)
+    with pytest.raises(ValueError):
+        pkg.LatentCache(4, 2, 64, page_size=24)
