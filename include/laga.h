@@ -255,7 +255,7 @@ int laga_latent_norm_rope_backward(const void* dlatent, const void* dk_pe, const
  * A step that cannot be placed (a negative length, too few free pages, columns or rows) takes nothing: the tables stay, the
  * state is handed back as it was, every slot is -1, cu_new_lens is zero, and laga_query_status(status_word) returns
  * LAGA_ERR_CACHE_PLAN (detail 0x5000000x: 1 bad length or n_free, 2 pages, 3 columns, 4 rows).
- * page_size: a power of two from 16 to 1024; n_requests <= 8192; columns * page_size <= 2^30.  No output may overlap an
+ * page_size: a power of two from 16 to 1024; n_requests <= 8192; max_tokens and columns * page_size <= 2^30.  No output may overlap an
  * input or another output (LAGA_ERR_INVALID_ARG).  Pages in the table are not checked here; rows they would place
  * outside 31 bits get slot -1.
  */
@@ -277,7 +277,7 @@ int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, in
  *   lse          fp32 [B, h] written if not NULL (-inf for length 0)
  * A length outside [0, columns * page_size] is clamped, and a page number outside [0, n_pages) reads as zeros; both report
  * LAGA_ERR_DEVICE_CHECK through laga_query_status(workspace).  page_size: a power of two from 16 to 1024; n_pages * page_size
- * and columns * page_size at most 2^30.  d_c, d_nope, d_rope, d_v: 512, 128, 64, 128.  flags must be 0.
+ * and columns * page_size at most 2^30, B * columns * page_size at most 2^36, B * h at most 2^26.  d_c, d_nope, d_rope, d_v: 512, 128, 64, 128.  flags must be 0.
  * q W_uk is rounded to bf16 for the tensor cores, like the probabilities; sums, maxima and the accumulator are fp32.
  * Nothing depends on lengths at enqueue time: the call can be captured in a graph and replayed with new lengths.
  */

@@ -151,7 +151,8 @@ class LagaBlock(torch.nn.Module):
                 *latent_norm_rope(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, self.eps))
 
     def forward(self, hidden: torch.Tensor, cu_seqlens=None, causal: bool = True, positions=None) -> torch.Tensor:
-        """positions (int32 [S], only with ``rope``): by default each token's place in its sequence."""
+        """positions (int32 [S] on the device, only with ``rope``): by default each token's place in its sequence, which
+        the call then copies from the host (give them to capture a step in a graph)."""
         S = hidden.shape[0]
         if self.rope is not None and positions is None:
             positions = self.positions(S, cu_seqlens, hidden.device)

@@ -250,7 +250,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     if (!mbar_wait(r_empty, r_par ^ 1u, abort_flag, args.status, 0xB1)) break;
                     mbar_arrive_expect_tx(r_full, L::kSlab);
                     armed.arm(r_full, r_par);
-                    tma_load_3d(smem + L::kRope, &tmap_rope, r_full, 0, row, 8, once);
+                    tma_load_3d_chk(args.status, smem + L::kRope, &tmap_rope, r_full, 0, row, 8, once);
                     r_par ^= 1u;
 #pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
@@ -258,7 +258,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                         if (!ok) break;
                         mbar_arrive_expect_tx(&h_full[slot], L::kHalf);
                         armed.arm(&h_full[slot], par);
-                        tma_load_3d(smem + L::kHalf0 + slot * L::kHalf, &tmap_lat, &h_full[slot], 0, row, half * 4, once);
+                        tma_load_3d_chk(args.status, smem + L::kHalf0 + slot * L::kHalf, &tmap_lat, &h_full[slot], 0, row, half * 4, once);
                         if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                     }
                     if (!ok) break;
@@ -302,7 +302,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (lane < boxes) tma_load_3d(smem + L::kRope + lane * page * 128, &tmap_rope, r_full, 0, row, 8, once);
+                if (lane < boxes) tma_load_3d_chk(args.status, smem + L::kRope + lane * page * 128, &tmap_rope, r_full, 0, row, 8, once);
                 r_par ^= 1u;
                 for (int half = 0; half < 2; ++half) {
                     if (lane == 0) {
@@ -316,7 +316,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     if (!ok) break;
                     const int slab = lane / n_sub;                                          // lanes 0 .. 4 n_sub - 1: box `sub` of slab `slab`
                     if (slab < 4 && sub < boxes)
-                        tma_load_3d(smem + L::kHalf0 + slot * L::kHalf + slab * L::kSlab + sub * page * 128, &tmap_rope, &h_full[slot], 0, row,
+                        tma_load_3d_chk(args.status, smem + L::kHalf0 + slot * L::kHalf + slab * L::kSlab + sub * page * 128, &tmap_rope, &h_full[slot], 0, row,
                                     half * 4 + slab, once);
                     if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                 }
@@ -554,7 +554,8 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 tc_fence_after_sync();
                 const size_t slot = static_cast<size_t>(cta) + cur.b;
                 float* dst = args.part_o + (slot * args.h_pad + head0) * kDecLat + warp * 32 + lane;
-                const int n_heads = min(kHeads, args.h - head0);
+                // (a slot past the workspace would mean that the roles disagree about the pieces)
+                const int n_heads = device_check(slot < static_cast<size_t>(args.ctas_per_group) + args.B, args.status, 0xEA0000u | cta) ? min(kHeads, args.h - head0) : 0;
 #pragma unroll 1
                 for (int c = 0; c < 4 * kHeads; c += 16) {    // latents (c / kHeads) * 128 + TMEM lane of heads c % kHeads ..
                     uint32_t o[16];
@@ -564,7 +565,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     for (int v = 0; v < 16; ++v)
                         if ((c % kHeads) + v < n_heads) dst[static_cast<size_t>((c % kHeads) + v) * kDecLat + (c / kHeads) * 128] = __uint_as_float(o[v]);
                 }
-                if (softmax_warp) {
+                if (softmax_warp && n_heads > 0) {
 #pragma unroll
                     for (int d = 1; d < 4; d <<= 1) {
                         l0 += __shfl_xor_sync(0xffffffffu, l0, d);

@@ -1380,7 +1380,7 @@ int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, in
     const int shift = page_shift_of(page_size);
     if (!seq_lens || !new_lens || !block_table || !free_pages || !n_free || !slots || !positions || !cu_new_lens || !seq_lens_out ||
         !n_free_out || !status_word || n_requests < 1 || n_requests > kPlanMaxRequests || shift < 0 || columns < 1 || free_capacity < 1 ||
-        max_tokens < 1 || (static_cast<long long>(columns) << shift) > (1ll << 30))
+        max_tokens < 1 || max_tokens > (1 << 30) || (static_cast<long long>(columns) << shift) > (1ll << 30))
         return LAGA_ERR_INVALID_ARG;
     // every block reads the state while block 0 writes the new one: the outputs must not be the inputs
     const size_t n4 = static_cast<size_t>(n_requests) * 4;
@@ -1427,7 +1427,7 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
     if (!geometry_is_v3(d_c, d_nope, d_rope, d_v)) return LAGA_ERR_UNSUPPORTED;
     // rows, keys and tiles are counted in 32 bits (byte offsets are not)
     const long long rows = static_cast<long long>(n_pages) << shift, capacity = static_cast<long long>(columns) << shift;
-    if (rows > (1ll << 30) || capacity > (1ll << 30) || ((capacity + kDecKeys - 1) / kDecKeys) * B > 0x7fffffffll ||
+    if (rows > (1ll << 30) || capacity > (1ll << 30) || ((capacity + kDecKeys - 1) / kDecKeys) * B > (1ll << 30) ||
         static_cast<long long>(B) * h > (1ll << 26) || h > 65535 || B > 65535 * 8)
         return LAGA_ERR_INVALID_ARG;
     const DecodeLayout w = decode_layout(B, h);

@@ -234,6 +234,15 @@ __device__ __forceinline__ void tma_load_2d_chk(unsigned int* status, void* smem
 }
 
 // ------------------------------------------------------------------------------------------------
+// 3-d loads of the decode kernel: rows not negative (past the end is legal: zeros), channel group inside the row.
+// ------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tma_load_3d_chk(unsigned int* status, void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int y,
+                                                int z, uint64_t policy) {
+    if (device_check((x & 7) == 0 && x >= 0 && y >= 0 && z >= 0 && z < 9 && (smem_u32(smem_dst) & 1023u) == 0u, status, 0xE80000u | (y & 0xffff)))
+        tma_load_3d(smem_dst, map, bar, x, y, z, policy);
+}
+
+// ------------------------------------------------------------------------------------------------
 // TMEM allocation (one warp executes these, all 32 lanes converged)
 // ------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tmem_alloc(uint32_t* smem_result, uint32_t n_cols) {

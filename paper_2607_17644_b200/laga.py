@@ -183,6 +183,9 @@ def _cu_seqlens(cu_seqlens):
 
 def alloc_workspace(n_bytes: int, device="cuda") -> torch.Tensor:
     """A 1024-byte aligned byte buffer (torch's caching allocator aligns to at least 512; over-allocate)."""
+    buf = torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    if buf.data_ptr() % 1024 == 0:
+        return buf
     buf = torch.empty(n_bytes + 1024, dtype=torch.uint8, device=device)
     off = (-buf.data_ptr()) % 1024
     return buf[off:off + n_bytes]
@@ -470,10 +473,12 @@ def rope(x, positions, rope, rot_begin=None, inverse=False, y=None, stream=None)
     M, h, d = x.shape
     x_pitch = _rows(x, "x", 3)
     d_rot = _rope_args(rope, positions, M)
-    y = x.new_empty((M, h, d)) if y is None else y
-    y_pitch = _rows(y, "y", 3)
-    if y.shape != (M, h, d):
-        raise ValueError(f"y: expected shape {(M, h, d)}, got {tuple(y.shape)}")
+    if y is None:
+        y, y_pitch = x.new_empty((M, h, d)), h * d
+    else:
+        y_pitch = _rows(y, "y", 3)
+        if y.shape != (M, h, d):
+            raise ValueError(f"y: expected shape {(M, h, d)}, got {tuple(y.shape)}")
     dev = same_device(x, positions, rope.freqs, y)
     if M == 0:
         return y

@@ -18,8 +18,8 @@ class LatentCache:
     ROW = 576
 
     def __init__(self, n_pages: int, n_requests: int, max_tokens: int, page_size: int = 64, n_layers: int = 1, device="cuda"):
-        if min(n_pages, n_requests, max_tokens, n_layers) < 1:
-            raise ValueError("LatentCache: sizes must be at least 1")
+        if min(n_pages, n_requests, max_tokens, n_layers) < 1 or n_requests > 8192:
+            raise ValueError("LatentCache: sizes must be at least 1, and n_requests at most 8192")
         if page_size not in (16, 32, 64, 128, 256, 512, 1024):
             raise ValueError(f"LatentCache: page_size must be a power of two from 16 to 1024, got {page_size}")
         i32 = dict(dtype=torch.int32, device=device)

@@ -86,7 +86,7 @@ def test_cache_plan_refusals(laga):
     assert call(n=0) == bad and call(n=8193) == bad and call(columns=0) == bad and call(cap=0) == bad and call(rows=0) == bad
     for page in (0, 1, 8, 48, 100, 2048, -64):
         assert call(page=page) == bad
-    assert call(page=1024, columns=(1 << 20) + 1) == bad
+    assert call(page=1024, columns=(1 << 20) + 1) == bad and call(rows=(1 << 30) + 1) == bad
     assert call(seq_out=at(0)) == bad                             # outputs apart from inputs ...
     assert call(free_out=at(4)) == bad
     assert call(slots=P((4 << 32) + 4)) == bad                    # (inside the free stack)
@@ -109,7 +109,7 @@ def test_paged_decode_refusals_and_sizes(laga):
     assert call(scale=0.0) == bad and call(scale=float("nan")) == bad and call(flags=1) == bad
     assert call(ws=P((7 << 32) + 16)) == bad and call(q=P(24)) == bad and call(lens=P(6)) == bad
     assert call(pages=(1 << 24) + 1) == bad and call(columns=(1 << 24) + 1) == bad
-    assert call(columns=1 << 24, B=128) == bad                     # tiles counted in 32 bits
+    assert call(columns=1 << 24, B=65) == bad                     # tiles counted in 32 bits
     assert call(dc=256) == laga.ERR_UNSUPPORTED and call(dv=64) == laga.ERR_UNSUPPORTED
     assert call(ws_bytes=4096) == laga.ERR_WORKSPACE_TOO_SMALL
     size = laga.paged_decode_workspace_bytes
