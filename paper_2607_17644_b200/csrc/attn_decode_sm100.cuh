@@ -136,7 +136,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
     int* start_b = reinterpret_cast<int*>(tmem_slot + 2);
     int* start_t = start_b + 1;
-    int* scan = start_b + 2;                          // [6] per-warp sums of the tile counts
+    int* scan = start_b + 2;                          // [8] per-warp sums of the tile counts
     static_assert(2 * L::kHalves + 4 + 12 <= 36, "barriers overlap the scalars");
     float* alpha_s = reinterpret_cast<float*>(smem + L::kAlpha);
     int* moved_s = reinterpret_cast<int*>(alpha_s + 2 * kHeads);     // [2 buffers][4 warps]: the tile (+ 1) that wrote it last
@@ -223,6 +223,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
         };
         auto load_queries = [&](const DecodeCursor& c, uint32_t piece, ArmedBarriers& armed) -> bool {
             if (!mbar_wait(q_empty, (piece & 1u) ^ 1u, abort_flag, args.status, 0xB0)) return false;
+            grid_dependency_wait();                  // (returns at once after the first time)
             mbar_arrive_expect_tx(q_full, 9 * L::kQSlab);
             armed.arm(q_full, piece);
             uint8_t* dst = smem + L::kQ;
@@ -231,7 +232,6 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 tma_load_2d_chk(args.status, dst + (1 + k) * L::kQSlab, &tmap_qabs, q_full, k * 64, c.b * args.h + head0);
             return true;
         };
-        grid_dependency_wait();
         uint32_t slot = 0, par = 0, r_par = 0, pieces = 0;
         bool new_piece = true, ok = true;
         if (args.page_shift >= 6) {
@@ -242,8 +242,6 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 DecodeCursor cur(args, my_tiles, first_b, first_t);
                 int row = row_of(cur, cur.t * kDecKeys);
                 while (!cur.done()) {
-                    if (new_piece && !load_queries(cur, pieces++, armed)) break;
-                    new_piece = cur.ends_piece();
                     DecodeCursor next = cur;
                     next.next(args);
                     const int next_row = next.done() ? 0 : row_of(next, next.t * kDecKeys);         // a tile ahead
@@ -261,7 +259,10 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                         tma_load_3d_chk(args.status, smem + L::kHalf0 + slot * L::kHalf, &tmap_lat, &h_full[slot], 0, row, half * 4, once);
                         if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                     }
+                    // a piece's queries after its first tile: they wait for the last scores of the piece before (and, once, for the absorption)
+                    if (ok && new_piece) ok = load_queries(cur, pieces++, armed);
                     if (!ok) break;
+                    new_piece = cur.ends_piece();
                     cur = next;
                     row = next_row;
                 }
@@ -275,15 +276,10 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
             int batch = 0, row_cur = 0, row_next = 0;       // first box of the batch; rows of box batch + lane and batch + 32 + lane
             while (!cur.done()) {
                 if (new_piece) {
-                    if (lane == 0) ok = load_queries(cur, pieces, armed);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    ++pieces;
                     batch = cur.t * n_sub;
                     row_cur = row_of(cur, (batch + lane) << args.page_shift);
                     row_next = row_of(cur, (batch + 32 + lane) << args.page_shift);
                 }
-                new_piece = cur.ends_piece();
                 if (cur.t * n_sub - batch >= 32) {
                     batch += 32;
                     row_cur = row_next;
@@ -320,7 +316,10 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                                     half * 4 + slab, once);
                     if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                 }
+                if (ok && new_piece && lane == 0) ok = load_queries(cur, pieces++, armed);
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
+                new_piece = cur.ends_piece();
                 cur.next(args);
             }
             __syncwarp();
