@@ -555,14 +555,20 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 float* dst = args.part_o + (slot * args.h_pad + head0) * kDecLat + warp * 32 + lane;
                 // (a slot past the workspace would mean that the roles disagree about the pieces)
                 const int n_heads = device_check(slot < static_cast<size_t>(args.ctas_per_group) + args.B, args.status, 0xEA0000u | cta) ? min(kHeads, args.h - head0) : 0;
-#pragma unroll 1
-                for (int c = 0; c < 4 * kHeads; c += 16) {    // latents (c / kHeads) * 128 + TMEM lane of heads c % kHeads ..
-                    uint32_t o[16];
-                    tmem_ld_x16(tmem_base + lane_addr + c, o);
-                    tmem_ld_wait();
+                // Columns c .. c+31 of TMEM are latents (c / kHeads) * 128 + lane of heads c % kHeads ..: a store of a warp is 128 bytes of one
+                // head's row.  The accumulator is up to 256 columns and nothing else of the CTA moves meanwhile, so the loop is
+                // unrolled (constant offsets) and the next columns are on their way while these are stored.
+                uint32_t o[2][32];
+                tmem_ld_x32(tmem_base + lane_addr, o[0]);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        if ((c % kHeads) + v < n_heads) dst[static_cast<size_t>((c % kHeads) + v) * kDecLat + (c / kHeads) * 128] = __uint_as_float(o[v]);
+                for (int c = 0; c < 4 * kHeads; c += 32) {
+                    tmem_ld_wait();
+                    if (c + 32 < 4 * kHeads) tmem_ld_x32(tmem_base + lane_addr + c + 32, o[(c / 32 + 1) & 1]);
+#pragma unroll
+                    for (int v = 0; v < 32; ++v) {
+                        const int head = (c + v) % kHeads, latent = (c + v) / kHeads * 128;
+                        if (head < n_heads) dst[head * kDecLat + latent] = __uint_as_float(o[(c / 32) & 1][v]);
+                    }
                 }
                 if (softmax_warp && n_heads > 0) {
 #pragma unroll
