@@ -154,6 +154,10 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_decode_sm100_kernel<64>, AttnDecodeSmem<64>::kTotalBytes) &&
               allow_smem(decode_absorb_kernel<64>, DecodeAbsorbSmem<64>::kTotalBytes) &&
               allow_smem(decode_project_kernel, DecodeProjectSmem::kTotalBytes) &&
+              allow_smem(latent_norm_rope_fwd_kernel<2, false>, latent_fwd_smem(256, kRopeMaxRot)) &&
+              allow_smem(latent_norm_rope_fwd_kernel<4, false>, latent_fwd_smem(512, kRopeMaxRot)) &&
+              allow_smem(latent_norm_rope_fwd_kernel<4, true>, latent_fwd_smem(512, kRopeMaxRot)) &&
+              allow_smem(latent_norm_rope_fwd_kernel<8, false>, latent_fwd_smem(kLnMaxD, kRopeMaxRot)) &&
               allow_smem(cache_plan_kernel, 2 * (kPlanMaxRequests + 1) * static_cast<int>(sizeof(int)));
     if (ok) {
         // The fused backward assigns work to pairs statically, so its grid must not exceed the pairs the
@@ -1318,14 +1322,15 @@ int laga_latent_norm_rope(const void* kv_a, long long kv_a_pitch, const void* ga
                                Rotary{positions, freqs, mscale, layout == LAGA_ROPE_INTERLEAVED ? 1 : 0, 0},
                                static_cast<__nv_bfloat16*>(latent), static_cast<__nv_bfloat16*>(k_pe), mean, rstd,
                                static_cast<__nv_bfloat16*>(cache), slots, n_slots};
-    const int blocks_needed = (M + kLnWarps - 1) / kLnWarps, cap = sm_count() * 3;      // one resident wave at D <= 512
+    const int rows_per_block = kLnWarps * 2, blocks_needed = M / rows_per_block + (M % rows_per_block != 0);
+    const int cap = sm_count() * 2;              // one resident wave at D <= 512
     const dim3 grid(blocks_needed < cap ? blocks_needed : cap), block(kLnWarps * 32);
+    const size_t smem = latent_fwd_smem(D, R);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const size_t smem = static_cast<size_t>(kLnWarps) * (D <= 512 ? latent_depth<2>() : latent_depth<4>()) * (D + R) * 2;      // at most 48 KB
-    if (D == 512) latent_norm_rope_fwd_kernel<2, true><<<grid, block, smem, st>>>(a);
-    else if (D <= 256) latent_norm_rope_fwd_kernel<1, false><<<grid, block, smem, st>>>(a);
-    else if (D < 512) latent_norm_rope_fwd_kernel<2, false><<<grid, block, smem, st>>>(a);
-    else latent_norm_rope_fwd_kernel<4, false><<<grid, block, smem, st>>>(a);
+    if (D == 512) latent_norm_rope_fwd_kernel<4, true><<<grid, block, smem, st>>>(a);
+    else if (D <= 256) latent_norm_rope_fwd_kernel<2, false><<<grid, block, smem, st>>>(a);
+    else if (D < 512) latent_norm_rope_fwd_kernel<4, false><<<grid, block, smem, st>>>(a);
+    else latent_norm_rope_fwd_kernel<8, false><<<grid, block, smem, st>>>(a);
     return launch_status();
 }
 

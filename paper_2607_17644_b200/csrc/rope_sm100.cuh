@@ -147,9 +147,9 @@ rope_kernel(const RopeArgs a) {
 }
 
 // ---- latent norm + key rotation ----------------------------------------------------------------------------
-// kv_a rows are D latent channels followed by R key channels (what W_kv_a delivers).  One warp per row: the latent is
-// normalised exactly as layernorm_fwd_kernel does it, and the key is rotated with one pair per lane (a row's 32 pairs are
-// 32 lanes' sine and cosine: no table, no exchange).  Destinations, each optional: dense latent [M, D] and k_pe [M, R],
+// kv_a rows are D latent channels followed by R key channels (what W_kv_a delivers).  The latent is normalised exactly as
+// layernorm_fwd_kernel does it (mean first, then the squares of the differences), and a lane rotates its pairs of the key with a
+// sine and cosine of its own: no table, no exchange.  Destinations, each optional: dense latent [M, D] and k_pe [M, R],
 // and the row slots[m] of a cache whose rows are the D + R channels side by side (a slot outside [0, n_slots) writes
 // nothing: padding).
 struct LatentNormRopeArgs {
@@ -189,11 +189,6 @@ __device__ __forceinline__ void row_copy16(void* smem_dst, const void* src) {
 __device__ __forceinline__ void row_copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kPending>
 __device__ __forceinline__ void row_copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
-// `channels` bf16 (a multiple of 8) by the whole warp
-__device__ __forceinline__ void row_copy(uint8_t* dst, const __nv_bfloat16* src, int channels, int lane) {
-    for (int c = lane * 8; c < channels; c += 256) row_copy16(dst + c * 2, src + c);
-}
-
 // Two fp32 values in one register pair: one instruction for two additions, products or fused multiply-adds.
 struct F2 {
     unsigned long long v;
@@ -231,68 +226,86 @@ __device__ __forceinline__ uint4 f2_pack(const F2* f) {
     return v;
 }
 
-// One warp per row, kDepth rows of it in shared memory; gamma and beta stay in registers, unpacked, and the arithmetic
-// runs two values at a time.  kFull: D is kLnChunks * 256, no lane idles.
-template <int kLnChunks>
-constexpr int latent_depth() { return kLnChunks <= 2 ? 4 : 2; }
-template <int kLnChunks, bool kFull>
-__global__ void __launch_bounds__(kLnWarps * 32, kLnChunks <= 2 ? 3 : 1)
+// Half a warp per row: what a row costs beside its elements (addresses, position, slot, reductions, loop) is issued once for two rows;
+// with a warp per row those instructions were more than half of the kernel (330 a row, now 247).  Measured at 65536 rows of 512 + 64
+// channels into the cache: 28.2 us, 5.4 TB/s (a warp per row, ring of four: 30.7; one row ahead in registers: 36.4).
+// kLatentDepth rows per half warp are in shared memory or on their way; gamma and beta stay in registers as bf16, and the
+// arithmetic runs two values at a time.  kChunks = ceil(D / 128) chunks of eight channels a lane; kFull: D is kChunks * 128.
+constexpr int kLatentDepth = 2;
+__host__ __device__ constexpr int latent_fwd_smem(int D, int R) { return kLnWarps * 2 * kLatentDepth * (D + R) * 2; }
+__device__ __forceinline__ float half_warp_sum(float v) {
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+template <int kChunks, bool kFull>
+__global__ void __launch_bounds__(kLnWarps * 32, kChunks <= 4 ? 2 : 1)
 latent_norm_rope_fwd_kernel(const LatentNormRopeArgs a) {
-    constexpr int kDepth = latent_depth<kLnChunks>();
-    extern __shared__ __align__(16) uint8_t ring[];          // [warps][kDepth][D + R] bf16
-    const int lane = threadIdx.x & 31;
-    const int n_warps = gridDim.x * kLnWarps;
+    extern __shared__ __align__(16) uint8_t ring[];          // [warps][2][kLatentDepth][D + R] bf16
+    const int lane = threadIdx.x & 31, q = lane & 15;
+    const int stride = gridDim.x * kLnWarps * 2;
     const float inv_d = 1.0f / static_cast<float>(a.D);
     const int n_pairs = a.R >> 1, row_bytes = (a.D + a.R) * 2;
-    uint8_t* rows = ring + (threadIdx.x >> 5) * kDepth * row_bytes;
-    const int m0 = blockIdx.x * kLnWarps + (threadIdx.x >> 5);
-    auto fetch = [&](int m, int stage) {
-        if (m < a.M) row_copy(rows + stage * row_bytes, a.kv_a + m * a.kv_a_pitch, a.D + a.R, lane);
+    uint8_t* rows = ring + (threadIdx.x >> 4) * kLatentDepth * row_bytes;
+    int m = (blockIdx.x * kLnWarps + (threadIdx.x >> 5)) * 2;              // the warp's first row; this half's is m + (lane >> 4)
+    const int sub = lane >> 4;
+    auto fetch = [&](int r, int stage) {
+        if (r < a.M) {
+            const __nv_bfloat16* src = a.kv_a + r * a.kv_a_pitch;
+            uint8_t* dst = rows + stage * row_bytes;
+            for (int c = q * 8; c < a.D + a.R; c += 128) row_copy16(dst + c * 2, src + c);
+        }
         row_copy_commit();                                   // (an empty group keeps the count)
     };
 #pragma unroll
-    for (int k = 0; k < kDepth - 1; ++k) fetch(m0 + k * n_warps, k);
-    int position = m0 < a.M ? __ldg(a.rot.positions + m0) : 0, slot = m0 < a.M && a.cache != nullptr ? __ldg(a.slots + m0) : -1;
-    F2 gamma[kLnChunks][4], beta[kLnChunks][4];
-#pragma unroll
-    for (int i = 0; i < kLnChunks; ++i) {
-        const int c = i * 256 + lane * 8;
-        const bool in = kFull || c < a.D;
-        f2_unpack(in ? __ldg(reinterpret_cast<const uint4*>(a.gamma + c)) : make_uint4(0u, 0u, 0u, 0u), gamma[i]);
-        f2_unpack(in && a.beta != nullptr ? __ldg(reinterpret_cast<const uint4*>(a.beta + c)) : make_uint4(0u, 0u, 0u, 0u), beta[i]);
+    for (int k = 0; k < kLatentDepth - 1; ++k) fetch(m + sub + k * stride, k);
+    int position = 0, slot = -1;
+    if (m + sub < a.M) {
+        position = __ldg(a.rot.positions + m + sub);
+        if (a.cache != nullptr) slot = __ldg(a.slots + m + sub);
     }
-    const unsigned long long step = lane < n_pairs ? rotary_step(__ldg(a.rot.freqs + lane)) : 0ull;
+    uint4 gamma[kChunks], beta[kChunks];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int c = i * 128 + q * 8;
+        const bool in = kFull || c < a.D;
+        gamma[i] = in ? __ldg(reinterpret_cast<const uint4*>(a.gamma + c)) : make_uint4(0u, 0u, 0u, 0u);
+        beta[i] = in && a.beta != nullptr ? __ldg(reinterpret_cast<const uint4*>(a.beta + c)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    const unsigned long long step0 = q < n_pairs ? rotary_step(__ldg(a.rot.freqs + q)) : 0ull,
+                             step1 = q + 16 < n_pairs ? rotary_step(__ldg(a.rot.freqs + q + 16)) : 0ull;
     int stage = 0;
-    for (int m = m0; m < a.M; m += n_warps) {
+    for (; m < a.M; m += stride) {
+        const int mine = m + sub;
         __syncwarp();                                        // the row this fetch replaces has been read by every lane
-        fetch(m + (kDepth - 1) * n_warps, stage == 0 ? kDepth - 1 : stage - 1);
+        fetch(mine + (kLatentDepth - 1) * stride, stage == 0 ? kLatentDepth - 1 : stage - 1);
         const int here = position, to = slot;
-        if (m + n_warps < a.M) {
-            position = __ldg(a.rot.positions + m + n_warps);
-            if (a.cache != nullptr) slot = __ldg(a.slots + m + n_warps);
+        if (mine + stride < a.M) {
+            position = __ldg(a.rot.positions + mine + stride);
+            if (a.cache != nullptr) slot = __ldg(a.slots + mine + stride);
         }
-        row_copy_wait<kDepth - 1>();
+        row_copy_wait<kLatentDepth - 1>();
         __syncwarp();
         const uint8_t* row = rows + stage * row_bytes;
-        if (++stage == kDepth) stage = 0;
-        __nv_bfloat16* cache_row = nullptr;
-        if (to >= 0 && to < a.n_slots) cache_row = a.cache + static_cast<size_t>(to) * (a.D + a.R);
-        else if (a.latent == nullptr) continue;                         // nothing of this row goes anywhere
-        F2 v[kLnChunks][4], sum = f2(0.f, 0.f);
+        if (++stage == kLatentDepth) stage = 0;
+        const bool live = mine < a.M;                        // (the second half of the last warp may have no row)
+        const bool dense = live && a.latent != nullptr, cached = live && to >= 0 && to < a.n_slots;
+        __nv_bfloat16* cache_row = a.cache + static_cast<size_t>(cached ? to : 0) * (a.D + a.R);
+        F2 v[kChunks][4], sum = f2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < kLnChunks; ++i) {
-            const int c = i * 256 + lane * 8;
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = i * 128 + q * 8;
             f2_unpack(kFull || c < a.D ? *reinterpret_cast<const uint4*>(row + c * 2) : make_uint4(0u, 0u, 0u, 0u), v[i]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) sum = f2_add(sum, v[i][k]);
         }
         const float2 sums = f2_parts(sum);
-        const float mean = ln_warp_sum(sums.x + sums.y) * inv_d;
+        const float mean = half_warp_sum(sums.x + sums.y) * inv_d;
         const F2 minus = f2(-mean, -mean);
         F2 sq = f2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < kLnChunks; ++i)
-            if (kFull || i * 256 + lane * 8 < a.D)
+        for (int i = 0; i < kChunks; ++i)
+            if (kFull || i * 128 + q * 8 < a.D)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     v[i][k] = f2_add(v[i][k], minus);
@@ -300,29 +313,35 @@ latent_norm_rope_fwd_kernel(const LatentNormRopeArgs a) {
                 }
         // the key, under the second sum
         const __nv_bfloat16* key = reinterpret_cast<const __nv_bfloat16*>(row) + a.D;
-        for (int j = lane; j < n_pairs; j += 32) {
+        auto turn_pair = [&](int j, unsigned long long step) {
             const float2 in = rotary_load_pair(key, j, n_pairs, a.rot.interleaved);
-            const float2 out = rotary_apply(rotary_turn(a.rot, here, j == lane ? step : rotary_step(__ldg(a.rot.freqs + j))), in.x, in.y);
-            if (a.k_pe != nullptr) rotary_store_pair(a.k_pe + static_cast<size_t>(m) * a.R, j, n_pairs, a.rot.interleaved, out);
-            if (cache_row != nullptr) rotary_store_pair(cache_row + a.D, j, n_pairs, a.rot.interleaved, out);
-        }
+            const float2 out = rotary_apply(rotary_turn(a.rot, here, step), in.x, in.y);
+            if (dense) rotary_store_pair(a.k_pe + static_cast<size_t>(mine) * a.R, j, n_pairs, a.rot.interleaved, out);
+            if (cached) rotary_store_pair(cache_row + a.D, j, n_pairs, a.rot.interleaved, out);
+        };
+        if (q < n_pairs) turn_pair(q, step0);
+        if (q + 16 < n_pairs) turn_pair(q + 16, step1);
+        for (int j = q + 32; j < n_pairs; j += 16) turn_pair(j, rotary_step(__ldg(a.rot.freqs + j)));
         const float2 sqs = f2_parts(sq);
-        const float rstd = rsqrtf(ln_warp_sum(sqs.x + sqs.y) * inv_d + a.eps);
+        const float rstd = rsqrtf(half_warp_sum(sqs.x + sqs.y) * inv_d + a.eps);
         const F2 scale = f2(rstd, rstd);
 #pragma unroll
-        for (int i = 0; i < kLnChunks; ++i) {
-            const int c = i * 256 + lane * 8;
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = i * 128 + q * 8;
             if (kFull || c < a.D) {
+                F2 gm[4], bt[4];
+                f2_unpack(gamma[i], gm);
+                f2_unpack(beta[i], bt);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[i][k] = f2_fma(f2_mul(v[i][k], scale), gamma[i][k], beta[i][k]);
+                for (int k = 0; k < 4; ++k) v[i][k] = f2_fma(f2_mul(v[i][k], scale), gm[k], bt[k]);
                 const uint4 packed = f2_pack(v[i]);
-                if (a.latent != nullptr) *reinterpret_cast<uint4*>(a.latent + static_cast<size_t>(m) * a.D + c) = packed;
-                if (cache_row != nullptr) *reinterpret_cast<uint4*>(cache_row + c) = packed;
+                if (dense) *reinterpret_cast<uint4*>(a.latent + static_cast<size_t>(mine) * a.D + c) = packed;
+                if (cached) *reinterpret_cast<uint4*>(cache_row + c) = packed;
             }
         }
-        if (lane == 0) {
-            if (a.mean != nullptr) a.mean[m] = mean;
-            if (a.rstd != nullptr) a.rstd[m] = rstd;
+        if (q == 0 && live) {
+            if (a.mean != nullptr) a.mean[mine] = mean;
+            if (a.rstd != nullptr) a.rstd[mine] = rstd;
         }
     }
 }

@@ -130,10 +130,13 @@ def same_device(*tensors) -> torch.device:
     """All tensors of a call must live on ONE device: the library launches on the current device, so the
     call runs under that device (see ``_on``) and a tensor from anywhere else is refused here, before the
     C side would refuse its pointer."""
-    present = [t for t in tensors if t is not None]
-    dev = present[0].device
-    for t in present[1:]:
-        if t.device != dev:
+    dev = index = None
+    for t in tensors:
+        if t is None:
+            continue
+        if dev is None:
+            dev, index = t.device, t.get_device()
+        elif t.get_device() != index or (index < 0 and t.device != dev):      # (the index alone tells CUDA devices apart)
             raise ValueError(f"tensors of one call are on different devices: {dev} and {t.device}")
     return dev
 
@@ -522,7 +525,6 @@ def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps=1e-5, latent=None, 
     R = kv_a.shape[1] - D
     if (cache is None) != (slots is None):
         raise ValueError("cache and slots go together")
-    _dev(gamma, torch.bfloat16, (D,), "gamma")
     latent = gamma.new_empty((M, D)) if latent is None else _dev(latent, torch.bfloat16, (M, D), "latent")
     k_pe = gamma.new_empty((M, R)) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
     mean = gamma.new_empty(M, dtype=torch.float32)
