@@ -611,7 +611,7 @@ struct DecodeAbsorbSmem {
 template <int kRequests>
 __global__ void __launch_bounds__(kAbsorbThreads)
 decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, int B, int h,
-                     const __nv_bfloat16* __restrict__ w, __nv_bfloat16* __restrict__ q_abs, unsigned* status, int status_words) {
+                     __nv_bfloat16* __restrict__ q_abs, unsigned* status, int status_words) {
     using L = DecodeAbsorbSmem<kRequests>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
@@ -638,11 +638,6 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
     tc_fence_after_sync();
     grid_launch_dependents();
     const uint32_t tmem = *tmem_slot;
-    if (b0 == 0) {      // W_uv of the same rows, for decode_project_kernel: 256 bytes a row, pages apart, slow to come from memory when needed
-        const __nv_bfloat16* row = w + (static_cast<size_t>(c0 + threadIdx.x) * h + head) * 256 + 128;
-        l2_prefetch(row);
-        l2_prefetch(row + 64);
-    }
     if (warp == 0) {
         if (elect_one()) {
             mbar_arrive_expect_tx(full, 2 * 128 * 128 + 2 * kRequests * 128);
@@ -686,70 +681,78 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 
 // Joins the pieces of each (request, head) and carries the result to the value dimension:
 //     o[c] = sum_p 2^(m_p - M) o_p[c] / sum_p 2^(m_p - M) l_p,      out[v] = sum_c W_uv[c, v] o[c]
-// One CTA per head and up to 16 requests: D[128 values x 32] = W_uv^T (A, MN-major, 512 rows of the weights as they lie) . o^T (B).  o is
-// fp32; rounded to bf16 it would cost as much accuracy as the result's own rounding, so B holds it in two parts, hi = bf16(o)
-// in rows 0..15 and lo = bf16(o - hi) in rows 16..31 -- columns that the MMA computes in the time of sixteen -- and the two
-// halves of D are added.  The weights' tile is requested before this kernel waits for the attention kernel (nothing in the
-// call writes them).  A warp per request turns the maxima and sums into weights first, so that the loads of the pieces
-// themselves (2 KB each) depend on nothing and run eight deep.
+// A CTA keeps one head's W_uv (128 KB) in shared memory and takes tiles of up to 16 requests: D[128 values x 32] = W_uv^T (A, MN-major, 512
+// rows of the weights as they lie) . o^T (B).  o is fp32; rounded to bf16 it would cost as much accuracy as the result's own
+// rounding, so B holds it in two parts, hi = bf16(o) in rows 0..15 and lo = bf16(o - hi) in rows 16..31 -- columns that the MMA
+// computes in the time of sixteen -- and the two halves of D are added.
+// The weights' tile is requested before this kernel waits for the attention kernel (nothing in the call writes them).  A warp per
+// request turns the maxima and sums into weights, so that the loads of the pieces themselves (2 KB each) depend on nothing.
+// With few requests a CTA has one tile and all of this is latency; with many it is a pipeline: the next tile's maxima are on
+// their way while this tile's pieces are summed, and its MMAs and stores run under the next tile's sums (250 short requests of
+// 64 heads: 54 -> 20 us against a CTA per tile; 2048 of 16 heads: 112 -> 46).
 // A request without tokens has no piece: zeros, LSE -inf.
 constexpr int kProjectThreads = 1024, kProjectGroups = kProjectThreads / 128;
 struct DecodeProjectSmem {
     static constexpr int kW = 0;                                 // two slabs of 512 rows x 64 values
     static constexpr int kWSlab = 512 * 128;
-    static constexpr int kO = kW + 2 * kWSlab;                   // eight slabs of 32 rows x 64 latents
+    static constexpr int kO = kW + 2 * kWSlab;                   // two buffers of eight slabs of 32 rows x 64 latents
     static constexpr int kOSlab = 32 * 128;
-    static constexpr int kRed = kO + 8 * kOSlab;                 // [groups][512] floats
-    static constexpr int kWeights = kRed + kProjectGroups * 512 * 4;          // a float per piece: at most one per CTA and one more per request
-    static constexpr int kBar = kWeights + (kDecMaxCtas + 20) * 4;
-    static constexpr int kTotalBytes = kBar + 32;
+    static constexpr int kRed = kO + 2 * 8 * kOSlab;             // [groups][512] floats
+    static constexpr int kWeights = kRed + kProjectGroups * 512 * 4;     // two buffers: a float per piece, at most one per CTA and one more per request
+    static constexpr int kMaxPieces = kDecMaxCtas + 20;
+    static constexpr int kBar = kWeights + 2 * kMaxPieces * 4;
+    static constexpr int kTotalBytes = kBar + 48;
 };
+static_assert(DecodeProjectSmem::kTotalBytes <= 232448 && DecodeProjectSmem::kBar % 8 == 0, "projection kernel's shared memory");
 __global__ void __launch_bounds__(kProjectThreads, 1)
 decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
                       const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad, int ctas_per_group,
-                      int requests_per_cta,
-                      __nv_bfloat16* __restrict__ out, float* __restrict__ lse, unsigned* status) {
+                      int tile_requests, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, unsigned* status) {
     using L = DecodeProjectSmem;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
-    uint64_t* done = full + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 2);
+    uint64_t* done = full + 1;                                   // [2] the MMAs of the tile in buffer i have completed
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 3);
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
     float* red = reinterpret_cast<float*>(smem + L::kRed);
-    float* weights = reinterpret_cast<float*>(smem + L::kWeights);
     int* sums = reinterpret_cast<int*>(red);                     // 64 words, before `red` is needed
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int head = blockIdx.x, b0 = blockIdx.y * requests_per_cta, n_req = min(requests_per_cta, B - b0);
+    const int head = blockIdx.x;
+    const int n_tiles = (B + tile_requests - 1) / tile_requests, tiles_each = (n_tiles + gridDim.y - 1) / gridDim.y;
+    const int tile0 = blockIdx.y * tiles_each, my_tiles = min(tiles_each, n_tiles - tile0);      // (may be none)
     if (threadIdx.x == 0) {
-        mbar_init(full, 1); mbar_init(done, 1);
+        mbar_init(full, 1); mbar_init(done, 1); mbar_init(done + 1, 1);
         abort_flag->value = 0;
         mbar_fence_init();
-        mbar_arrive_expect_tx(full, 2 * L::kWSlab);
-        for (int k = 0; k < 4; ++k)                              // slab k / 2, rows 256 (k % 2) ..
-            tma_load_2d_chk(status, smem + L::kW + k * (L::kWSlab / 2), &tmap_wv, full, head * 256 + (k >> 1) * 64, (k & 1) * 256);
+        if (my_tiles > 0) {
+            mbar_arrive_expect_tx(full, 2 * L::kWSlab);
+            for (int k = 0; k < 4; ++k)                          // slab k / 2, rows 256 (k % 2) ..
+                tma_load_2d_chk(status, smem + L::kW + k * (L::kWSlab / 2), &tmap_wv, full, head * 256 + (k >> 1) * 64, (k & 1) * 256);
+        }
     }
-    if (warp == 0) { __syncwarp(); tmem_alloc(tmem_slot, 32); tmem_relinquish(); }
+    if (warp == 0) { __syncwarp(); tmem_alloc(tmem_slot, 64); tmem_relinquish(); }
     // rows of B that no request fills: zero (their columns of D are never read, but nothing uninitialised should be multiplied)
-    for (int i = threadIdx.x; i < 8 * 32 * 8; i += kProjectThreads)
+    for (int i = threadIdx.x; i < 2 * 8 * 32 * 8; i += kProjectThreads)
         *reinterpret_cast<uint4*>(smem + L::kO + i * 16) = make_uint4(0u, 0u, 0u, 0u);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
     grid_launch_dependents();
-    // Where the requests' tiles lie on the line, from the lengths again (an input of the call: nothing to wait for).  Lane l of
-    // every warp then knows the pieces of request b0 + l.
-    int first = 0, count = 0;
+
+    // Where the requests' tiles lie on the line, from the lengths again (an input of the call: nothing to wait for).
+    auto tiles_of = [&](int b) { return (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kDecKeys - 1) / kDecKeys; };
+    int per, position;                                           // tiles of a stretch; position of this CTA's first request
     {
+        const int b_first = tile0 * tile_requests;
         const int run = (B + kProjectThreads - 1) / kProjectThreads;
         const int s0 = min(B, static_cast<int>(threadIdx.x) * run), s1 = min(B, s0 + run);
-        int sum = 0, before = 0;                                 // tiles of this thread's requests, and of those of them before b0
+        int sum = 0, before = 0;                                 // tiles of this thread's requests, and of those of them before b_first
         for (int b = s0; b < s1; ++b) {
-            const int n = (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kDecKeys - 1) / kDecKeys;
+            const int n = tiles_of(b);
             sum += n;
-            before += b < b0 ? n : 0;
+            before += b < b_first ? n : 0;
         }
-        const int mine = lane < n_req ? (decode_clamp(__ldg(seq_lens + b0 + lane), columns, page_shift) + kDecKeys - 1) / kDecKeys : 0;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
             sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -764,127 +767,185 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
             sum += __shfl_xor_sync(0xffffffffu, sum, d);
             before += __shfl_xor_sync(0xffffffffu, before, d);
         }
-        const int per = max(1, (sum + ctas_per_group - 1) / ctas_per_group);
+        per = max(1, (sum + ctas_per_group - 1) / ctas_per_group);
+        position = before;
+    }
+    // Lane l of every warp knows the pieces of the tile's request l: first stretch, how many, where their weights begin.
+    struct Tile { int b0, n_req, first, count, base; };
+    auto locate = [&](int tile) {
+        Tile t;
+        t.b0 = tile * tile_requests;
+        t.n_req = min(tile_requests, B - t.b0);
+        const int mine = lane < t.n_req ? tiles_of(t.b0 + lane) : 0;
         int incl = mine;
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, d);
             if (lane >= d) incl += v;
         }
-        const int begin = before + incl - mine;
-        first = begin / per;
-        count = mine > 0 ? (begin + mine - 1) / per - first + 1 : 0;
-    }
-    grid_dependency_wait();
-    // Weights: warp r takes request r.
-    int base = count;                                            // where the request's weights begin in shared memory
+        const int begin = position + incl - mine;
+        t.first = begin / per;
+        t.count = mine > 0 ? (begin + mine - 1) / per - t.first + 1 : 0;
+        position += __shfl_sync(0xffffffffu, incl, 15);
+        t.base = t.count;
 #pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, base, d);
-        if (lane >= d) base += v;
-    }
-    base -= count;
-    if (warp < n_req) {
-        const int f = __shfl_sync(0xffffffffu, first, warp), n = __shfl_sync(0xffffffffu, count, warp), at = __shfl_sync(0xffffffffu, base, warp);
-        const float2* ml = part_ml + static_cast<size_t>(f + b0 + warp) * h_pad + head;
-        float2 mine[(kDecMaxCtas + 31) / 32];                    // a request has at most one piece per CTA
+        for (int d = 1; d < 16; d <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, t.base, d);
+            if (lane >= d) t.base += v;
+        }
+        t.base -= t.count;
+        return t;
+    };
+    // Weights: warp r takes request r; the loads and what is made of them apart, so that other work can lie between.
+    constexpr int kMlChunks = (kDecMaxCtas + 31) / 32;           // a request has at most one piece per CTA
+    float2 ml[kMlChunks];
+    auto fetch_ml = [&](const Tile& t) {
+        if (warp >= t.n_req) return;
+        const int f = __shfl_sync(0xffffffffu, t.first, warp), n = __shfl_sync(0xffffffffu, t.count, warp);
+        const float2* src = part_ml + static_cast<size_t>(f + t.b0 + warp) * h_pad + head;
+#pragma unroll
+        for (int k = 0; k < kMlChunks; ++k) {
+            const int c = k * 32 + lane;
+            ml[k] = c < n ? src[static_cast<size_t>(c) * h_pad] : make_float2(-INFINITY, 0.f);
+        }
+    };
+    auto make_weights = [&](const Tile& t, int buf) {
+        if (warp >= t.n_req) return;
+        const int n = __shfl_sync(0xffffffffu, t.count, warp);
+        float* weights = reinterpret_cast<float*>(smem + L::kWeights) + buf * L::kMaxPieces + __shfl_sync(0xffffffffu, t.base, warp);
         float M = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int k = 0; k < (kDecMaxCtas + 31) / 32; ++k) {
-            const int c = k * 32 + lane;
-            mine[k] = c < n ? ml[static_cast<size_t>(c) * h_pad] : make_float2(-INFINITY, 0.f);
-            M = fmaxf(M, mine[k].x);
-        }
+        for (int k = 0; k < kMlChunks; ++k) M = fmaxf(M, ml[k].x);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
 #pragma unroll
-        for (int k = 0; k < (kDecMaxCtas + 31) / 32; ++k)
+        for (int k = 0; k < kMlChunks; ++k)
             if (k * 32 + lane < n) {
-                mine[k].x = fast_exp2(mine[k].x - M);
-                l = fmaf(mine[k].x, mine[k].y, l);
+                ml[k].x = fast_exp2(ml[k].x - M);
+                l = fmaf(ml[k].x, ml[k].y, l);
             }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
         const float inv = 1.0f / l;
 #pragma unroll
-        for (int k = 0; k < (kDecMaxCtas + 31) / 32; ++k)
-            if (k * 32 + lane < n) weights[at + k * 32 + lane] = mine[k].x * inv;
+        for (int k = 0; k < kMlChunks; ++k)
+            if (k * 32 + lane < n) weights[k * 32 + lane] = ml[k].x * inv;
         if (lse != nullptr && lane == 0)
-            lse[static_cast<size_t>(b0 + warp) * h + head] = n > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
-    }
-    __syncthreads();
-    // Sums: groups of 128 threads, four channels a thread, a request each; with fewer requests than groups, the groups that share one
-    // take every second, fourth or eighth piece.
+            lse[static_cast<size_t>(t.b0 + warp) * h + head] = n > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    };
+    // Sums: groups of 128 threads, four channels a thread.  A group takes two requests of the tile at once; with fewer requests than groups,
+    // the groups that share one take every second, fourth or eighth piece.
     const int group = warp >> 2, cg = threadIdx.x & 127;
-    const int split = n_req == 1 ? kProjectGroups : n_req == 2 ? kProjectGroups / 2 : n_req <= 4 ? kProjectGroups / 4 : 1;
-    for (int r0 = 0; r0 < n_req; r0 += kProjectGroups / split) {
-        const int r = r0 + group / split, src = r < n_req ? r : 0;
-        const int f = __shfl_sync(0xffffffffu, first, src), n = r < n_req ? __shfl_sync(0xffffffffu, count, src) : 0,
-                  at = __shfl_sync(0xffffffffu, base, src);
-        const float4* o = reinterpret_cast<const float4*>(part_o + (static_cast<size_t>(f + b0 + src) * h_pad + head) * kDecLat) + cg;
-        const size_t step = static_cast<size_t>(h_pad) * (kDecLat / 4);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int c = group % split; c < n; c += split) {
-            const float w = weights[at + c];
-            const float4 x = o[c * step];
-            acc.x = fmaf(x.x, w, acc.x); acc.y = fmaf(x.y, w, acc.y);
-            acc.z = fmaf(x.z, w, acc.z); acc.w = fmaf(x.w, w, acc.w);
+    auto store_row = [&](int buf, int r, float4 o) {             // both parts of request r's row, swizzled
+        const float x[4] = {o.x, o.y, o.z, o.w};
+        float rest[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rest[e] = x[e] - __bfloat162float(__float2bfloat16_rn(x[e]));
+        uint8_t* slab = smem + L::kO + (buf * 8 + (cg >> 4)) * L::kOSlab;      // 16 threads of four channels per slab
+        const int chunk = (cg & 15) >> 1, in_chunk = (cg & 1) * 8;
+        *reinterpret_cast<uint2*>(slab + r * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+        *reinterpret_cast<uint2*>(slab + (16 + r) * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) =
+            make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
+    };
+    const size_t step = static_cast<size_t>(h_pad) * (kDecLat / 4);
+    auto sum_pieces = [&](const Tile& t, int buf) {
+        const float* weights = reinterpret_cast<const float*>(smem + L::kWeights) + buf * L::kMaxPieces;
+        auto row_of = [&](int r) {
+            return reinterpret_cast<const float4*>(part_o + (static_cast<size_t>(__shfl_sync(0xffffffffu, t.first, r) + t.b0 + r) * h_pad + head) * kDecLat) + cg;
+        };
+        const int split = t.n_req == 1 ? kProjectGroups : t.n_req == 2 ? kProjectGroups / 2 : t.n_req <= 4 ? kProjectGroups / 4 : 1;
+        const int r0 = group / split, r1 = r0 + kProjectGroups;  // (r1 only where split is 1)
+        const float4 *o0 = row_of(r0 & 15), *o1 = row_of(r1 & 15);
+        const int n0 = r0 < t.n_req ? __shfl_sync(0xffffffffu, t.count, r0 & 15) : 0, n1 = r1 < t.n_req && split == 1 ? __shfl_sync(0xffffffffu, t.count, r1 & 15) : 0;
+        const float *w0 = weights + __shfl_sync(0xffffffffu, t.base, r0 & 15), *w1 = weights + __shfl_sync(0xffffffffu, t.base, r1 & 15);
+        float4 a0 = make_float4(0.f, 0.f, 0.f, 0.f), a1 = a0;
+        const int both = split == 1 ? min(n0, n1) : 0;
+        auto add = [&](float4& a, float w, const float4& x) {
+            a.x = fmaf(x.x, w, a.x); a.y = fmaf(x.y, w, a.y); a.z = fmaf(x.z, w, a.z); a.w = fmaf(x.w, w, a.w);
+        };
+#pragma unroll 2
+        for (int c = 0; c < both; ++c) {
+            const float4 x = o0[c * step], y = o1[c * step];
+            add(a0, w0[c], x);
+            add(a1, w1[c], y);
         }
+#pragma unroll 4
+        for (int c = both + group % split; c < n0; c += split) add(a0, w0[c], o0[c * step]);
+#pragma unroll 4
+        for (int c = both; c < n1; ++c) add(a1, w1[c], o1[c * step]);
         if (split > 1) {
-            reinterpret_cast<float4*>(red)[group * 128 + cg] = acc;
+            reinterpret_cast<float4*>(red)[group * 128 + cg] = a0;
             __syncthreads();
-            acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            a0 = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < split; ++k) {
                 const float4 x = reinterpret_cast<const float4*>(red)[(group / split * split + k) * 128 + cg];
-                acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+                a0.x += x.x; a0.y += x.y; a0.z += x.z; a0.w += x.w;
             }
         }
-        if (r < n_req && group % split == 0) {                   // both parts of request r's row, swizzled
-            const float x[4] = {acc.x, acc.y, acc.z, acc.w};
-            float rest[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) rest[e] = x[e] - __bfloat162float(__float2bfloat16_rn(x[e]));
-            uint8_t* slab = smem + L::kO + (cg >> 4) * L::kOSlab;    // 16 threads of four channels per slab
-            const int chunk = (cg & 15) >> 1, in_chunk = (cg & 1) * 8;
-            *reinterpret_cast<uint2*>(slab + r * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-            *reinterpret_cast<uint2*>(slab + (16 + r) * 128 + ((chunk ^ (r & 7)) << 4) + in_chunk) =
-                make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
-        }
-    }
-    fence_async_shared();
-    __syncthreads();
-    if (warp == 0) {
-        if (elect_one()) {
-            if (mbar_wait(full, 0, abort_flag, status, 0xBB)) {
-                tc_fence_after_sync();
-                constexpr uint32_t idesc = make_idesc_bf16(128, 32, 1, 0);
-                const uint32_t a_lo = desc_lo(desc_mn_major(smem_u32(smem + L::kW), L::kWSlab)), a_hi = desc_hi(desc_mn_major(0, L::kWSlab)),
-                               b_lo = desc_lo(desc_k_major(smem_u32(smem + L::kO))), b_hi = desc_hi(desc_k_major(0));
-#pragma unroll 1
-                for (uint32_t s = 0; s < 8; ++s)                 // 64 latents: four steps of 16 rows of W_uv
-                    mma_ss_chain4_mn_k(tmem, a_lo + s * (64 * 128 / 16), a_hi, b_lo + s * (L::kOSlab / 16), b_hi, idesc, s > 0 ? 1u : 0u);
-                mma_commit(done);
-            } else {
-                mbar_wait_quiesce(full, 0);
-            }
-        }
-        __syncwarp();
-    }
-    if (warp < 4 && mbar_wait_warp(done, 0, abort_flag, status, 0xBC)) {
+        if (r0 < t.n_req && group % split == 0) store_row(buf, r0, a0);
+        if (r1 < t.n_req && split == 1) store_row(buf, r1, a1);
+    };
+    auto write_out = [&](int b0, int n_req, int buf) {           // warps 0..3: D of a tile whose MMAs have completed
         tc_fence_after_sync();
         uint32_t v[32];
-        tmem_ld_x32(tmem + (static_cast<uint32_t>(warp * 32) << 16), v);
+        tmem_ld_x32(tmem + buf * 32 + (static_cast<uint32_t>(warp * 32) << 16), v);
         tmem_ld_wait();
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             if (r < n_req)
                 out[(static_cast<size_t>(b0 + r) * h + head) * 128 + warp * 32 + lane] =
                     __float2bfloat16_rn(__uint_as_float(v[r]) + __uint_as_float(v[16 + r]));
+        tc_fence_before_sync();
+    };
+
+    // (No role leaves this loop early: a wait that gave up skips its work and the rest of the launch runs through.)
+    Tile t{0, 0, 0, 0, 0};
+    if (my_tiles > 0) t = locate(tile0);
+    grid_dependency_wait();
+    if (my_tiles > 0) {
+        fetch_ml(t);
+        make_weights(t, 0);
+        __syncthreads();
+        for (int i = 0; i < my_tiles; ++i) {
+            const int buf = i & 1;
+            Tile next = t;
+            if (i + 1 < my_tiles) {
+                next = locate(tile0 + i + 1);
+                fetch_ml(next);
+            }
+            // the MMAs that read this buffer two tiles ago have completed
+            const bool free = i < 2 || mbar_wait_warp(&done[buf], ((i >> 1) & 1u) ^ 1u, abort_flag, status, 0xBB);
+            if (free || t.n_req <= 4) sum_pieces(t, buf);        // (the sums of a tile of four or fewer synchronise: all threads or none)
+            if (i + 1 < my_tiles) make_weights(next, buf ^ 1);
+            fence_async_shared();
+            __syncthreads();
+            if (warp == 0) {
+                if (elect_one()) {
+                    if (i > 0 || mbar_wait(full, 0, abort_flag, status, 0xBC)) {
+                        tc_fence_after_sync();
+                        constexpr uint32_t idesc = make_idesc_bf16(128, 32, 1, 0);
+                        const uint32_t a_lo = desc_lo(desc_mn_major(smem_u32(smem + L::kW), L::kWSlab)), a_hi = desc_hi(desc_mn_major(0, L::kWSlab)),
+                                       b_lo = desc_lo(desc_k_major(smem_u32(smem + L::kO + buf * 8 * L::kOSlab))), b_hi = desc_hi(desc_k_major(0));
+#pragma unroll 1
+                        for (uint32_t s = 0; s < 8; ++s)         // 64 latents: four steps of 16 rows of W_uv
+                            mma_ss_chain4_mn_k(tmem + buf * 32, a_lo + s * (64 * 128 / 16), a_hi, b_lo + s * (L::kOSlab / 16), b_hi, idesc, s > 0 ? 1u : 0u);
+                        mma_commit(&done[buf]);
+                    } else {
+                        mbar_wait_quiesce(full, 0);
+                    }
+                }
+                __syncwarp();
+            }
+            if (i > 0 && warp < 4 && mbar_wait_warp(&done[buf ^ 1], ((i - 1) >> 1) & 1u, abort_flag, status, 0xBD))
+                write_out(t.b0 - tile_requests, tile_requests, buf ^ 1);
+            if (i + 1 == my_tiles && warp < 4 && mbar_wait_warp(&done[buf], (i >> 1) & 1u, abort_flag, status, 0xBE))
+                write_out(t.b0, t.n_req, buf);
+            t = next;
+        }
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 0) { tc_fence_after_sync(); tmem_dealloc(tmem, 32); }
+    if (warp == 0) { tc_fence_after_sync(); tmem_dealloc(tmem, 64); }
 }
 
 }  // namespace laga

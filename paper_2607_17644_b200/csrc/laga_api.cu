@@ -752,7 +752,7 @@ int launch_decode_absorb(const void* q, const void* w, int B, int h, void* q_abs
     if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, kRequests))
         return LAGA_ERR_CUDA;
     launch_kernel(decode_absorb_kernel<kRequests>, dim3(kDc / 128, h, (B + kRequests - 1) / kRequests), dim3(kAbsorbThreads),
-                  DecodeAbsorbSmem<kRequests>::kTotalBytes, stream, false, tw, tq, B, h, static_cast<const __nv_bfloat16*>(w), static_cast<__nv_bfloat16*>(q_abs), status,
+                  DecodeAbsorbSmem<kRequests>::kTotalBytes, stream, false, tw, tq, B, h, static_cast<__nv_bfloat16*>(q_abs), status,
                   static_cast<int>(kStatusClearBytes / sizeof(unsigned)));
     return launch_status();
 }
@@ -778,12 +778,14 @@ int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, flo
     const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv);
     CUtensorMap tw;      // starts at W's column d_nope: column 0 of the map is V channel 0 of head 0
     if (!cached_tmap_bf16(&tw, static_cast<const uint8_t*>(w) + kDn * 2, w_row - kDn, kDc, w_row * 2, 256)) return LAGA_ERR_CUDA;
-    // Requests per CTA: 8, which a CTA's threads join at once, or 16 where that saves a wave (each CTA reads its head's 128 KB of W_uv).
-    int per_cta = 8;
-    while (per_cta < 16 && static_cast<long long>(a.h) * ((a.B + per_cta - 1) / per_cta) > sm_count()) per_cta *= 2;
-    launch_kernel(decode_project_kernel, dim3(a.h, (a.B + per_cta - 1) / per_cta), dim3(kProjectThreads), DecodeProjectSmem::kTotalBytes, stream,
+    // Tiles of 8 requests, which a CTA's threads join at once, where every tile can have a CTA of its own; otherwise of 16, and as
+    // many CTAs per head as fit the GPU, each with a run of tiles (it reads its head's 128 KB of W_uv once).
+    const int sms = sm_count();
+    const int tile = static_cast<long long>(a.h) * ((a.B + 7) / 8) <= sms ? 8 : 16;
+    const int n_tiles = (a.B + tile - 1) / tile, most = sms / a.h > 0 ? sms / a.h : 1;
+    launch_kernel(decode_project_kernel, dim3(a.h, n_tiles < most ? n_tiles : most), dim3(kProjectThreads), DecodeProjectSmem::kTotalBytes, stream,
                   true, tw, static_cast<const float*>(a.part_o), static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift,
-                  a.B, a.h, a.h_pad, a.ctas_per_group, per_cta, static_cast<__nv_bfloat16*>(out), lse, a.status);
+                  a.B, a.h, a.h_pad, a.ctas_per_group, tile, static_cast<__nv_bfloat16*>(out), lse, a.status);
     return launch_status();
 }
 

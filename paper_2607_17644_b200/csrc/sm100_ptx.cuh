@@ -207,7 +207,6 @@ __device__ __forceinline__ uint64_t l2_evict_first() {
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     return policy;
 }
-__device__ __forceinline__ void l2_prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // TMA store of one box from shared memory (bulk async-group completion).  The shared-memory source must have
 // been written, fenced into the async proxy (fence_async_shared) and the writers synchronised before the issue.
