@@ -32,6 +32,8 @@
 // Rows behind a request's last token may hold anything, NaN included: their scores are replaced by -inf, and their
 // rows of the tile are zeroed in shared memory before P.V (0 * NaN is NaN).
 #pragma once
+#include <type_traits>
+
 #include "attn_fwd_sm100.cuh"
 #include "sm100_ptx.cuh"
 
@@ -687,20 +689,21 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 // computes in the time of sixteen -- and the two halves of D are added.
 // The weights' tile is requested before this kernel waits for the attention kernel (nothing in the call writes them).  A warp per
 // request turns the maxima and sums into weights, so that the loads of the pieces themselves (2 KB each) depend on nothing.
-// With few requests a CTA has one tile and all of this is latency; with many it is a pipeline: the next tile's maxima are on
-// their way while this tile's pieces are summed, and its MMAs and stores run under the next tile's sums (250 short requests of
-// 64 heads: 54 -> 20 us against a CTA per tile; 2048 of 16 heads: 112 -> 46).
+// With few requests a CTA has one tile, all of this is latency, and all warps sum pieces.  With many it is a pipeline: warps 0..15 sum
+// this tile's pieces (four requests a thread at once) while warps 16..23 make the next tile's weights, 24..27 write the tile before and
+// warp 31 issues MMAs; one barrier per tile.
 // A request without tokens has no piece: zeros, LSE -inf.
-constexpr int kProjectThreads = 1024, kProjectGroups = kProjectThreads / 128;
+constexpr int kProjectThreads = 1024;
 struct DecodeProjectSmem {
     static constexpr int kW = 0;                                 // two slabs of 512 rows x 64 values
     static constexpr int kWSlab = 512 * 128;
     static constexpr int kO = kW + 2 * kWSlab;                   // two buffers of eight slabs of 32 rows x 64 latents
     static constexpr int kOSlab = 32 * 128;
-    static constexpr int kRed = kO + 2 * 8 * kOSlab;             // [groups][512] floats
-    static constexpr int kWeights = kRed + kProjectGroups * 512 * 4;     // two buffers: a float per piece, at most one per CTA and one more per request
+    static constexpr int kRed = kO + 2 * 8 * kOSlab;             // [8 groups][512] floats
+    static constexpr int kWeights = kRed + 8 * 512 * 4;     // two buffers: (weight, sum) per piece, at most one piece per CTA and one more per request
     static constexpr int kMaxPieces = kDecMaxCtas + 20;
-    static constexpr int kBar = kWeights + 2 * kMaxPieces * 4;
+    static constexpr int kTable = kWeights + 2 * kMaxPieces * 8;  // three tiles' pieces: 16 int4 each
+    static constexpr int kBar = kTable + 3 * 16 * 16;
     static constexpr int kTotalBytes = kBar + 48;
 };
 static_assert(DecodeProjectSmem::kTotalBytes <= 232448 && DecodeProjectSmem::kBar % 8 == 0, "projection kernel's shared memory");
@@ -742,7 +745,7 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
 
     // Where the requests' tiles lie on the line, from the lengths again (an input of the call: nothing to wait for).
     auto tiles_of = [&](int b) { return (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kDecKeys - 1) / kDecKeys; };
-    int per, position;                                           // tiles of a stretch; position of this CTA's first request
+    int per, position;                                           // tiles of a stretch; position on the line of the next tile's first request
     {
         const int b_first = tile0 * tile_requests;
         const int run = (B + kProjectThreads - 1) / kProjectThreads;
@@ -770,71 +773,66 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
         per = max(1, (sum + ctas_per_group - 1) / ctas_per_group);
         position = before;
     }
-    // Lane l of every warp knows the pieces of the tile's request l: first stretch, how many, where their weights begin.
-    struct Tile { int b0, n_req, first, count, base; };
-    auto locate = [&](int tile) {
-        Tile t;
-        t.b0 = tile * tile_requests;
-        t.n_req = min(tile_requests, B - t.b0);
-        const int mine = lane < t.n_req ? tiles_of(t.b0 + lane) : 0;
+    // The pieces of the tile's request l -- first stretch, how many, where their weights begin -- go to the table of the tile (three, by
+    // tile number), one warp's work: warp 28's, two tiles ahead, in the order of the tiles.
+    int4* table = reinterpret_cast<int4*>(smem + L::kTable);
+    auto locate = [&](int i) {
+        const int b = (tile0 + i) * tile_requests + lane;
+        const int mine = lane < tile_requests && b < B && i < my_tiles ? tiles_of(b) : 0;
         int incl = mine;
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, d);
             if (lane >= d) incl += v;
         }
-        const int begin = position + incl - mine;
-        t.first = begin / per;
-        t.count = mine > 0 ? (begin + mine - 1) / per - t.first + 1 : 0;
+        const int begin = position + incl - mine, first = begin / per;
+        const int count = mine > 0 ? (begin + mine - 1) / per - first + 1 : 0;
         position += __shfl_sync(0xffffffffu, incl, 15);
-        t.base = t.count;
+        int base = count;
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, t.base, d);
-            if (lane >= d) t.base += v;
+            const int v = __shfl_up_sync(0xffffffffu, base, d);
+            if (lane >= d) base += v;
         }
-        t.base -= t.count;
-        return t;
+        if (lane < 16) table[i % 3 * 16 + lane] = make_int4(first, count, base - count, 0);
     };
-    // Weights: warp r takes request r; the loads and what is made of them apart, so that other work can lie between.
-    constexpr int kMlChunks = (kDecMaxCtas + 31) / 32;           // a request has at most one piece per CTA
-    float2 ml[kMlChunks];
-    auto fetch_ml = [&](const Tile& t) {
-        if (warp >= t.n_req) return;
-        const int f = __shfl_sync(0xffffffffu, t.first, warp), n = __shfl_sync(0xffffffffu, t.count, warp);
-        const float2* src = part_ml + static_cast<size_t>(f + t.b0 + warp) * h_pad + head;
-#pragma unroll
-        for (int k = 0; k < kMlChunks; ++k) {
-            const int c = k * 32 + lane;
-            ml[k] = c < n ? src[static_cast<size_t>(c) * h_pad] : make_float2(-INFINITY, 0.f);
-        }
+    struct Tile { int b0, n_req; const int4* pieces; };
+    auto tile_at = [&](int i) {
+        const int b = (tile0 + i) * tile_requests;
+        return Tile{b, min(tile_requests, B - b), table + i % 3 * 16};
     };
+    // Weights: half a warp per request, warps 16..23.
     auto make_weights = [&](const Tile& t, int buf) {
-        if (warp >= t.n_req) return;
-        const int n = __shfl_sync(0xffffffffu, t.count, warp);
-        float* weights = reinterpret_cast<float*>(smem + L::kWeights) + buf * L::kMaxPieces + __shfl_sync(0xffffffffu, t.base, warp);
+        if (warp < 16 || warp >= 24) return;
+        const int r = (warp - 16) * 2 + (lane >> 4), q = lane & 15;
+        const int4 p = t.pieces[r];                              // (first, count, base)
+        const int n = r < t.n_req ? p.y : 0;
+        float2* weights = reinterpret_cast<float2*>(smem + L::kWeights) + buf * L::kMaxPieces + p.z;
+        const float2* src = part_ml + static_cast<size_t>(p.x + t.b0 + r) * h_pad + head;
         float M = -INFINITY, l = 0.f;
+#pragma unroll 4
+        for (int c = q; c < n; c += 16) {
+            const float2 ml = src[static_cast<size_t>(c) * h_pad];
+            weights[c] = ml;
+            M = fmaxf(M, ml.x);
+        }
 #pragma unroll
-        for (int k = 0; k < kMlChunks; ++k) M = fmaxf(M, ml[k].x);
+        for (int d = 8; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        for (int c = q; c < n; c += 16) {                        // (a lane reads what it wrote)
+            const float2 ml = weights[c];
+            const float w = fast_exp2(ml.x - M);
+            l = fmaf(w, ml.y, l);
+            weights[c].x = w;
+        }
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-#pragma unroll
-        for (int k = 0; k < kMlChunks; ++k)
-            if (k * 32 + lane < n) {
-                ml[k].x = fast_exp2(ml[k].x - M);
-                l = fmaf(ml[k].x, ml[k].y, l);
-            }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+        for (int d = 8; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
         const float inv = 1.0f / l;
-#pragma unroll
-        for (int k = 0; k < kMlChunks; ++k)
-            if (k * 32 + lane < n) weights[k * 32 + lane] = ml[k].x * inv;
-        if (lse != nullptr && lane == 0)
-            lse[static_cast<size_t>(t.b0 + warp) * h + head] = n > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        for (int c = q; c < n; c += 16) weights[c].x *= inv;
+        if (lse != nullptr && q == 0 && r < t.n_req)
+            lse[static_cast<size_t>(t.b0 + r) * h + head] = n > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
     };
-    // Sums: groups of 128 threads, four channels a thread.  A group takes two requests of the tile at once; with fewer requests than groups,
-    // the groups that share one take every second, fourth or eighth piece.
+    // Sums: groups of 128 threads, four channels a thread, kEach requests a group at once; with fewer requests than groups, the groups
+    // that share one take every second, fourth or eighth piece.
     const int group = warp >> 2, cg = threadIdx.x & 127;
     auto store_row = [&](int buf, int r, float4 o) {             // both parts of request r's row, swizzled
         const float x[4] = {o.x, o.y, o.z, o.w};
@@ -848,78 +846,103 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
             make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
     };
     const size_t step = static_cast<size_t>(h_pad) * (kDecLat / 4);
-    auto sum_pieces = [&](const Tile& t, int buf) {
-        const float* weights = reinterpret_cast<const float*>(smem + L::kWeights) + buf * L::kMaxPieces;
-        auto row_of = [&](int r) {
-            return reinterpret_cast<const float4*>(part_o + (static_cast<size_t>(__shfl_sync(0xffffffffu, t.first, r) + t.b0 + r) * h_pad + head) * kDecLat) + cg;
-        };
-        const int split = t.n_req == 1 ? kProjectGroups : t.n_req == 2 ? kProjectGroups / 2 : t.n_req <= 4 ? kProjectGroups / 4 : 1;
-        const int r0 = group / split, r1 = r0 + kProjectGroups;  // (r1 only where split is 1)
-        const float4 *o0 = row_of(r0 & 15), *o1 = row_of(r1 & 15);
-        const int n0 = r0 < t.n_req ? __shfl_sync(0xffffffffu, t.count, r0 & 15) : 0, n1 = r1 < t.n_req && split == 1 ? __shfl_sync(0xffffffffu, t.count, r1 & 15) : 0;
-        const float *w0 = weights + __shfl_sync(0xffffffffu, t.base, r0 & 15), *w1 = weights + __shfl_sync(0xffffffffu, t.base, r1 & 15);
-        float4 a0 = make_float4(0.f, 0.f, 0.f, 0.f), a1 = a0;
-        const int both = split == 1 ? min(n0, n1) : 0;
-        auto add = [&](float4& a, float w, const float4& x) {
-            a.x = fmaf(x.x, w, a.x); a.y = fmaf(x.y, w, a.y); a.z = fmaf(x.z, w, a.z); a.w = fmaf(x.w, w, a.w);
-        };
-#pragma unroll 2
-        for (int c = 0; c < both; ++c) {
-            const float4 x = o0[c * step], y = o1[c * step];
-            add(a0, w0[c], x);
-            add(a1, w1[c], y);
+    auto sum_pieces = [&](auto each, const Tile& t, int buf) {
+        constexpr int kEach = decltype(each)::value, kGroups = 16 / kEach;
+        const float2* weights = reinterpret_cast<const float2*>(smem + L::kWeights) + buf * L::kMaxPieces;
+        const int split = t.n_req == 1 ? kGroups : t.n_req == 2 ? kGroups / 2 : t.n_req <= kGroups / 2 ? kGroups / 4 : 1;
+        const float4* o[kEach];
+        const float2* w[kEach];
+        int n[kEach], most = 0;
+        float4 acc[kEach];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int r = group / split + k * kGroups, at = r & 15;            // (k > 0 only where split is 1)
+            const bool in = r < t.n_req && (k == 0 || split == 1);
+            const int4 p = t.pieces[at];
+            o[k] = reinterpret_cast<const float4*>(part_o + (static_cast<size_t>(p.x + t.b0 + at) * h_pad + head) * kDecLat) + cg;
+            w[k] = weights + p.z;
+            n[k] = in ? p.y : 0;
+            most = max(most, n[k]);
+            acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-#pragma unroll 4
-        for (int c = both + group % split; c < n0; c += split) add(a0, w0[c], o0[c * step]);
-#pragma unroll 4
-        for (int c = both; c < n1; ++c) add(a1, w1[c], o1[c * step]);
-        if (split > 1) {
-            reinterpret_cast<float4*>(red)[group * 128 + cg] = a0;
-            __syncthreads();
-            a0 = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (split == 1) {
+#pragma unroll 2
+            for (int c = 0; c < most; ++c)
+#pragma unroll
+                for (int k = 0; k < kEach; ++k)
+                    if (c < n[k]) {
+                        const float4 x = o[k][c * step];
+                        const float wc = w[k][c].x;
+                        acc[k].x = fmaf(x.x, wc, acc[k].x); acc[k].y = fmaf(x.y, wc, acc[k].y);
+                        acc[k].z = fmaf(x.z, wc, acc[k].z); acc[k].w = fmaf(x.w, wc, acc[k].w);
+                    }
+        } else {
+#pragma unroll 8
+            for (int c = group % split; c < n[0]; c += split) {
+                const float4 x = o[0][c * step];
+                const float wc = w[0][c].x;
+                acc[0].x = fmaf(x.x, wc, acc[0].x); acc[0].y = fmaf(x.y, wc, acc[0].y);
+                acc[0].z = fmaf(x.z, wc, acc[0].z); acc[0].w = fmaf(x.w, wc, acc[0].w);
+            }
+            reinterpret_cast<float4*>(red)[group * 128 + cg] = acc[0];
+            asm volatile("bar.sync 1, %0;" ::"n"(kGroups * 128) : "memory");   // the summing warps; none of them ever leaves early
+            acc[0] = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < split; ++k) {
                 const float4 x = reinterpret_cast<const float4*>(red)[(group / split * split + k) * 128 + cg];
-                a0.x += x.x; a0.y += x.y; a0.z += x.z; a0.w += x.w;
+                acc[0].x += x.x; acc[0].y += x.y; acc[0].z += x.z; acc[0].w += x.w;
             }
         }
-        if (r0 < t.n_req && group % split == 0) store_row(buf, r0, a0);
-        if (r1 < t.n_req && split == 1) store_row(buf, r1, a1);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int r = group / split + k * kGroups;
+            if (r < t.n_req && group % split == 0 && (k == 0 || split == 1)) store_row(buf, r, acc[k]);
+        }
     };
-    auto write_out = [&](int b0, int n_req, int buf) {           // warps 0..3: D of a tile whose MMAs have completed
+    auto write_out = [&](int b0, int n_req, int buf) {           // warps 24..27: D of a tile whose MMAs have completed
         tc_fence_after_sync();
         uint32_t v[32];
-        tmem_ld_x32(tmem + buf * 32 + (static_cast<uint32_t>(warp * 32) << 16), v);
+        tmem_ld_x32(tmem + buf * 32 + (static_cast<uint32_t>((warp & 3) * 32) << 16), v);
         tmem_ld_wait();
+        __nv_bfloat16* dst = out + (static_cast<size_t>(b0) * h + head) * 128 + (warp & 3) * 32 + lane;
+        const size_t pitch = static_cast<size_t>(h) * 128;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            if (r < n_req)
-                out[(static_cast<size_t>(b0 + r) * h + head) * 128 + warp * 32 + lane] =
-                    __float2bfloat16_rn(__uint_as_float(v[r]) + __uint_as_float(v[16 + r]));
+        for (int r = 0; r < 16; ++r, dst += pitch)
+            if (r < n_req) *dst = __float2bfloat16_rn(__uint_as_float(v[r]) + __uint_as_float(v[16 + r]));
         tc_fence_before_sync();
     };
 
     // (No role leaves this loop early: a wait that gave up skips its work and the rest of the launch runs through.)
-    Tile t{0, 0, 0, 0, 0};
-    if (my_tiles > 0) t = locate(tile0);
+    const bool pipelined = my_tiles > 1, writer = warp >= 24 && warp < 28;
+    if (warp == 28) {
+        locate(0);
+        locate(1);
+    }
+    __syncthreads();
     grid_dependency_wait();
     if (my_tiles > 0) {
-        fetch_ml(t);
-        make_weights(t, 0);
+        make_weights(tile_at(0), 0);
         __syncthreads();
         for (int i = 0; i < my_tiles; ++i) {
             const int buf = i & 1;
-            Tile next = t;
-            if (i + 1 < my_tiles) {
-                next = locate(tile0 + i + 1);
-                fetch_ml(next);
+            const Tile t = tile_at(i);
+            if (!pipelined) {
+                sum_pieces(std::integral_constant<int, 2>{}, t, buf);
+            } else {
+                if (warp < 16) {
+                    // the MMAs that read this buffer two tiles ago have completed
+                    const bool free = i < 2 || mbar_wait_warp(&done[buf], ((i >> 1) & 1u) ^ 1u, abort_flag, status, 0xBB);
+                    if (free || t.n_req <= 4) sum_pieces(std::integral_constant<int, 4>{}, t, buf);    // (few requests: its barrier wants every summing warp)
+                } else {
+                    if (i > 0 && writer && mbar_wait_warp(&done[buf ^ 1], ((i - 1) >> 1) & 1u, abort_flag, status, 0xBD))
+                        write_out(t.b0 - tile_requests, tile_requests, buf ^ 1);
+                    if (i + 1 < my_tiles) make_weights(tile_at(i + 1), buf ^ 1);
+                    if (warp == 28) locate(i + 2);
+                }
             }
-            // the MMAs that read this buffer two tiles ago have completed
-            const bool free = i < 2 || mbar_wait_warp(&done[buf], ((i >> 1) & 1u) ^ 1u, abort_flag, status, 0xBB);
-            if (free || t.n_req <= 4) sum_pieces(t, buf);        // (the sums of a tile of four or fewer synchronise: all threads or none)
-            if (i + 1 < my_tiles) make_weights(next, buf ^ 1);
             fence_async_shared();
+            tc_fence_before_sync();
             __syncthreads();
-            if (warp == 0) {
+            if (warp == 31) {
                 if (elect_one()) {
                     if (i > 0 || mbar_wait(full, 0, abort_flag, status, 0xBC)) {
                         tc_fence_after_sync();
@@ -936,11 +959,7 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
                 }
                 __syncwarp();
             }
-            if (i > 0 && warp < 4 && mbar_wait_warp(&done[buf ^ 1], ((i - 1) >> 1) & 1u, abort_flag, status, 0xBD))
-                write_out(t.b0 - tile_requests, tile_requests, buf ^ 1);
-            if (i + 1 == my_tiles && warp < 4 && mbar_wait_warp(&done[buf], (i >> 1) & 1u, abort_flag, status, 0xBE))
-                write_out(t.b0, t.n_req, buf);
-            t = next;
+            if (i + 1 == my_tiles && writer && mbar_wait_warp(&done[buf], (i >> 1) & 1u, abort_flag, status, 0xBE)) write_out(t.b0, t.n_req, buf);
         }
     }
     tc_fence_before_sync();
