@@ -612,8 +612,8 @@ struct DecodeAbsorbSmem {
 };
 template <int kRequests>
 __global__ void __launch_bounds__(kAbsorbThreads)
-decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, int B, int h,
-                     __nv_bfloat16* __restrict__ q_abs, unsigned* status, int status_words) {
+decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q,
+                     const __grid_constant__ CUtensorMap tmap_out, unsigned* status, int status_words) {
     using L = DecodeAbsorbSmem<kRequests>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
@@ -662,19 +662,29 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
         }
         __syncwarp();
     }
-    if (mbar_wait_warp(done, 0, abort_flag, status, 0xBA)) {
+    const bool ok = mbar_wait_warp(done, 0, abort_flag, status, 0xBA);
+    if (ok) {
+        // D is latents x requests, the output requests x latents: transposed on its way through shared memory (over the weights, which
+        // the MMAs have read), in the boxes of 64 latents that TMA stores; requests past B are clipped by the map.
         tc_fence_after_sync();
-        const uint32_t lane_addr = static_cast<uint32_t>(warp * 32) << 16;
-#pragma unroll 1
-        for (int c = 0; c < kRequests && b0 + c < B; c += 16) {
+        const int c = warp * 32 + lane;
+        uint8_t* box = smem + L::kW + (c >> 6) * (kRequests * 128) + (c & 7) * 2;
+        const int chunk = (c & 63) >> 3;
+#pragma unroll
+        for (int r0 = 0; r0 < kRequests; r0 += 16) {
             uint32_t v[16];
-            tmem_ld_x16(tmem + lane_addr + c, v);
+            tmem_ld_x16(tmem + (static_cast<uint32_t>(warp * 32) << 16) + r0, v);
             tmem_ld_wait();
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                if (b0 + c + r < B)
-                    q_abs[(static_cast<size_t>(b0 + c + r) * h + head) * kDecLat + c0 + warp * 32 + lane] = __float2bfloat16_rn(__uint_as_float(v[r]));
+                *reinterpret_cast<__nv_bfloat16*>(box + (r0 + r) * 128 + ((chunk ^ (r & 7)) << 4)) = __float2bfloat16_rn(__uint_as_float(v[r]));
         }
+        fence_async_shared();
+    }
+    if (__syncthreads_and(ok) && threadIdx.x == 0) {
+        for (int k = 0; k < 2; ++k) tma_store_2d(&tmap_out, smem + L::kW + k * kRequests * 128, head * kDecLat + c0 + k * 64, b0);
+        tma_store_commit();
+        tma_store_wait_all();
     }
     tc_fence_before_sync();
     __syncthreads();

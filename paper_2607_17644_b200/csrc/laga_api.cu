@@ -748,12 +748,13 @@ DecodeLayout decode_layout(int B, int h) {
 template <int kRequests>
 int launch_decode_absorb(const void* q, const void* w, int B, int h, void* q_abs, unsigned* status, cudaStream_t stream) {
     const uint64_t q_row = static_cast<uint64_t>(h) * (kDn + kDr), w_row = static_cast<uint64_t>(h) * (kDn + kDv);
-    CUtensorMap tw, tq;
-    if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, kRequests))
+    CUtensorMap tw, tq, to;
+    const uint64_t o_row = static_cast<uint64_t>(h) * kDecLat;
+    if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, kRequests) ||
+        !cached_tmap_bf16(&to, q_abs, o_row, B, o_row * 2, kRequests))
         return LAGA_ERR_CUDA;
     launch_kernel(decode_absorb_kernel<kRequests>, dim3(kDc / 128, h, (B + kRequests - 1) / kRequests), dim3(kAbsorbThreads),
-                  DecodeAbsorbSmem<kRequests>::kTotalBytes, stream, false, tw, tq, B, h, static_cast<__nv_bfloat16*>(q_abs), status,
-                  static_cast<int>(kStatusClearBytes / sizeof(unsigned)));
+                  DecodeAbsorbSmem<kRequests>::kTotalBytes, stream, false, tw, tq, to, status, static_cast<int>(kStatusClearBytes / sizeof(unsigned)));
     return launch_status();
 }
 
@@ -1445,9 +1446,9 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t* base = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(base);
-    // Tiles of 16 requests (64 requests, 16 heads: 256 CTAs share the work instead of 64, 6.2 -> 3.9 us) until the 32 KB of W_uk that
-    // each CTA reads add up: beyond 128 requests tiles of 64
-    rc = B <= 128 ? launch_decode_absorb<16>(q, w_kv_b, B, h, base + w.q_abs, status, st)
+    // Tiles of 16 requests where one holds them all, of 64 otherwise: each CTA reads its 32 KB of W_uk once per tile (2048 requests: 20 us
+    // less than with 16; at 64 requests, where 16 gives four times the CTAs, the two are even)
+    rc = B <= 16 ? launch_decode_absorb<16>(q, w_kv_b, B, h, base + w.q_abs, status, st)
                  : launch_decode_absorb<64>(q, w_kv_b, B, h, base + w.q_abs, status, st);
     if (rc != LAGA_OK) return rc;
     const AttnDecodeArgs a{B, h, w.n_groups, w.ctas_per_group, softmax_scale * 1.4426950408889634f, seq_lens, block_table, columns, shift,
