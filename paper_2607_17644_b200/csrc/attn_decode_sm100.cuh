@@ -10,7 +10,7 @@
 // ceil(total / CTAs) tiles, whatever requests it crosses, so ragged batches and one long request alike fill the GPU
 // (one CTA per SM, no counter).  Each (CTA, request) piece leaves its unnormalised accumulator, running maximum and sum
 // in the workspace at slot c + b -- both only grow along the line and one of them does at every step, so no two pieces share a
-// slot -- and decode_combine_kernel joins a request's pieces.
+// slot -- and decode_project_kernel joins a request's pieces.
 //
 // Tiles.  kHeads (16, 32 or 64) heads per CTA; more heads are more CTAs over the same keys (L2 serves the second read).
 //   scores   S[heads x 64 keys] = Q (A, rows = heads; of the 64 MMA rows only the first kHeads mean anything, the others read
@@ -45,6 +45,7 @@ constexpr int kDecKeys = 64;
 constexpr int kDecMaxCtas = 148;             // CTAs over all head groups (the workspace is sized by it)
 constexpr int kDecRow = 576;                 // channels of a cached token
 constexpr int kDecLat = 512;
+constexpr float kDecLowest = -3.0e38f;
 
 // Shared memory for kHeads heads per CTA: what the queries and P leave holds the tiles, 3, 2.5 or 2 of them.
 template <int kHeads>
@@ -426,7 +427,9 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
         const int r0 = warp * 16 + (lane >> 2), r1 = r0 + 8;   // heads within the group
         const bool live0 = head0 + r0 < args.h, live1 = head0 + r1 < args.h;
         const uint32_t lane_addr = static_cast<uint32_t>(warp * 32) << 16;
-        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;      // running maxima (log2 domain); this thread's part of the sums
+        // running maxima (log2 domain) and this thread's part of the sums; a maximum starts just above the lowest number, not at -inf, so
+        // that keys whose score is -inf weigh exp2(-inf) = 0 even where there is nothing else yet (-inf - -inf is NaN)
+        float m0 = kDecLowest, m1 = kDecLowest, l0 = 0.f, l1 = 0.f;
         uint32_t T = 0, pieces = 0;
         bool ok = true, first = true;
         DecodeCursor cur(args, my_tiles, first_b, first_t);
@@ -586,7 +589,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 __syncwarp();
                 if (lane == 0) mbar_arrive(o_free);
                 ++pieces;
-                m0 = m1 = -INFINITY; l0 = l1 = 0.f;
+                m0 = m1 = kDecLowest; l0 = l1 = 0.f;
                 first = true;
             }
             cur.next(args);
@@ -697,8 +700,8 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 // rows of the weights as they lie) . o^T (B).  o is fp32; rounded to bf16 it would cost as much accuracy as the result's own
 // rounding, so B holds it in two parts, hi = bf16(o) in rows 0..15 and lo = bf16(o - hi) in rows 16..31 -- columns that the MMA
 // computes in the time of sixteen -- and the two halves of D are added.
-// The weights' tile is requested before this kernel waits for the attention kernel (nothing in the call writes them).  A warp per
-// request turns the maxima and sums into weights, so that the loads of the pieces themselves (2 KB each) depend on nothing.
+// The weights' tile is requested before this kernel waits for the attention kernel (nothing in the call writes them).  Half
+// a warp per request turns the maxima and sums into weights, so that the loads of the pieces themselves (2 KB each) depend on nothing.
 // With few requests a CTA has one tile, all of this is latency, and all warps sum pieces.  With many it is a pipeline: warps 0..15 sum
 // this tile's pieces (four requests a thread at once) while warps 16..23 make the next tile's weights, 24..27 write the tile before and
 // warp 31 issues MMAs; one barrier per tile.

@@ -82,6 +82,16 @@ def test_batches_and_heads(laga, B, h):
     check(tensors, *run(laga, tensors))
 
 
+@pytest.mark.parametrize("B,h", [(17, 128), (34, 128), (45, 64), (129, 33), (300, 16)])
+def test_several_request_tiles_per_head(laga, B, h):
+    """More tiles of 16 requests than CTAs for a head: the joining kernel's pipeline, with last tiles of 1, 2, 12 and 13 requests."""
+    g = torch.Generator().manual_seed(B + h)
+    lens = torch.randint(0, 70, (B,), generator=g).tolist()
+    lens[-1] = 1500                                     # one request in many pieces, in the last tile
+    tensors = case(lens, h, 32, seed=10)
+    check(tensors, *run(laga, tensors))
+
+
 @pytest.mark.parametrize("lens,h,page", [([511], 16, 32), ([9001], 16, 64), ([20011, 3], 4, 16), ([12345, 1, 0, 6000], 64, 64), ([15000, 777], 128, 256)])
 def test_long_contexts(laga, lens, h, page):
     tensors = case(lens, h, page, seed=2)
@@ -126,6 +136,25 @@ def test_values_that_are_not_finite(laga):
     assert bool(torch.isnan(out[1].float()).all()) and bool(torch.isnan(lse[1]).all())
     assert not bool(torch.isfinite(out[0].float()).all())
     assert torch.equal(out[2], clean[2])
+
+
+def test_keys_of_minus_infinity(laga):
+    """Tokens taken out by a key of minus infinity weigh nothing, also where they fill a tile, or all that one CTA has of the
+    request: the result is that of the other tokens alone."""
+    lens = [20000, 100]
+    q, w, cache, table, lens = case(lens, 4, 16, seed=9, fill=0.0)
+    q[..., 128 + 3] = q[..., 128 + 3].abs().clamp_min(0.125)
+    rows = cache[table[0].long()].reshape(-1, 576)[:20000]
+    at = torch.arange(20000)
+    out_of = (at < 2048) | ((at // 64) % 2 == 0) | (at % 64 == 11) | (at >= 19000)
+    rows[out_of, 512 + 3] = -math.inf
+    cache[table[0].long()] = rows.view(-1, 16, 576)
+    kept = cache.clone()
+    left = rows[~out_of]
+    n = -(-len(left) // 16)
+    kept[table[0, :n].long()] = torch.nn.functional.pad(left, (0, 0, 0, 16 * n - len(left))).view(-1, 16, 576)
+    out, lse = run(laga, (q, w, cache, table, lens))
+    check((q, w, kept, table, torch.tensor([len(left), 100], dtype=torch.int32)), out, lse)
 
 
 def test_shared_pages_and_repeated_requests(laga):
