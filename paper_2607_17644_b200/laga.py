@@ -149,6 +149,15 @@ def _on(device):
     return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
 
+def _new(like, shape, stream, dtype=None):
+    """What a call on `stream` writes, from that stream's pool: the current stream's pool may hand out memory that its own queued
+    work still uses, and give it away again before `stream` is done with it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def _geometry(q, c_kv, k_pe, w_kv_b, d_v):
     S, h, d_qk = q.shape
     d_c, d_rope = c_kv.shape[1], k_pe.shape[1]
@@ -477,7 +486,7 @@ def rope(x, positions, rope, rot_begin=None, inverse=False, y=None, stream=None)
     x_pitch = _rows(x, "x", 3)
     d_rot = _rope_args(rope, positions, M)
     if y is None:
-        y, y_pitch = x.new_empty((M, h, d)), h * d
+        y, y_pitch = _new(x, (M, h, d), stream), h * d
     else:
         y_pitch = _rows(y, "y", 3)
         if y.shape != (M, h, d):
@@ -525,10 +534,10 @@ def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps=1e-5, latent=None, 
     R = kv_a.shape[1] - D
     if (cache is None) != (slots is None):
         raise ValueError("cache and slots go together")
-    latent = gamma.new_empty((M, D)) if latent is None else _dev(latent, torch.bfloat16, (M, D), "latent")
-    k_pe = gamma.new_empty((M, R)) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
-    mean = gamma.new_empty(M, dtype=torch.float32)
-    rstd = torch.empty_like(mean)
+    latent = _new(gamma, (M, D), stream) if latent is None else _dev(latent, torch.bfloat16, (M, D), "latent")
+    k_pe = _new(gamma, (M, R), stream) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
+    mean = _new(gamma, M, stream, torch.float32)
+    rstd = _new(gamma, M, stream, torch.float32)
     _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, latent, k_pe, mean, rstd, cache, slots, stream)
     return latent, k_pe, mean, rstd
 
@@ -555,15 +564,15 @@ def latent_norm_rope_backward(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions
     _dev(rstd, torch.float32, (M,), "rstd")
     _rope_args(rope, positions, M, R)
     dev = same_device(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope.freqs, dkv_a, workspace)
-    dkv_a = dlatent.new_empty((M, D + R)) if dkv_a is None else _dev(dkv_a, torch.bfloat16, (M, D + R), "dkv_a")
+    dkv_a = _new(dlatent, (M, D + R), stream) if dkv_a is None else _dev(dkv_a, torch.bfloat16, (M, D + R), "dkv_a")
     if M == 0:
         sums = torch.zeros(2, D, dtype=torch.float32, device=dev)
         return dkv_a, sums[0], sums[1] if with_beta else None
     need = int(lib().laga_latent_norm_rope_backward_workspace_bytes(M, D))
     if workspace is None:
-        workspace = mean.new_empty(need // 4)
-    dgamma = mean.new_empty(D)
-    dbeta = torch.empty_like(dgamma) if with_beta else None
+        workspace = _new(mean, need // 4, stream)
+    dgamma = _new(mean, D, stream)
+    dbeta = _new(mean, D, stream) if with_beta else None
     with _on(dev):
         rc = lib().laga_latent_norm_rope_backward(
             _ptr(dlatent), _ptr(dk_pe), _ptr(kv_a), pitch, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(positions), _ptr(rope.freqs), M, D,
@@ -595,7 +604,7 @@ def cache_plan(seq_lens, new_lens, block_table, free_pages, n_free, page_size, m
     _dev(n_free, torch.int32, (1,), "n_free")
     dev = same_device(seq_lens, new_lens, block_table, free_pages, n_free, *(out or ()))
     if out is None:
-        whole = seq_lens.new_empty(2 * max_tokens + 2 * n + 3)
+        whole = _new(seq_lens, 2 * max_tokens + 2 * n + 3, stream)
         out = CachePlan(*torch.split_with_sizes(whole, [max_tokens, max_tokens, n + 1, n, 1, 1]))
     else:
         for name, size in zip(CachePlan._fields, (max_tokens, max_tokens, n + 1, n, 1, 1)):
@@ -629,14 +638,15 @@ def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, ou
     dev = same_device(q, w_kv_b, cache, block_table, seq_lens, out, lse, workspace)
     if softmax_scale is None:
         softmax_scale = d_qk ** -0.5
-    out = q.new_empty((B, h, d_v)) if out is None else _dev(out, torch.bfloat16, (B, h, d_v), "out")
+    out = _new(q, (B, h, d_v), stream) if out is None else _dev(out, torch.bfloat16, (B, h, d_v), "out")
     if lse is not None:
         _dev(lse, torch.float32, (B, h), "lse")
     if workspace is None:
         need = paged_decode_workspace_bytes(B, h, d_c, d_nope, d_rope, d_v)
         if need == 0:
             raise LagaError(ERR_UNSUPPORTED, "laga_paged_decode_workspace_bytes")
-        workspace = alloc_workspace(need, dev)
+        with _HERE if stream is None else torch.cuda.stream(stream):       # (the pool: see _new)
+            workspace = alloc_workspace(need, dev)
     with _on(dev):
         rc = lib().laga_paged_decode(_ptr(q), _ptr(w_kv_b), _ptr(cache), n_pages, page_size, _ptr(block_table), block_table.shape[1],
                                      _ptr(seq_lens), B, h, d_c, d_nope, d_rope, d_v, float(softmax_scale), _ptr(out), _ptr(lse),

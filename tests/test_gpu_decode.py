@@ -201,6 +201,20 @@ def test_results_repeat_and_do_not_depend_on_the_workspace(laga):
     assert torch.equal(a, b) and torch.equal(a, c)
 
 
+def test_what_a_side_stream_writes_comes_from_its_pool(laga):
+    """The current stream must not get the output or the workspace back while the side stream may still be at work."""
+    q, w, cache, table, lens = (t.cuda() for t in case([300, 20], 16, 64, seed=11))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out, _, ws = laga.paged_decode(q, w, cache, table, lens, stream=side)
+    mine = {out.untyped_storage().data_ptr(), ws.untyped_storage().data_ptr()}
+    n_out, n_ws = out.numel(), ws.numel()
+    del out, ws
+    again = [torch.empty(n_out, dtype=BF16, device="cuda"), laga.alloc_workspace(n_ws)]
+    assert not mine & {t.untyped_storage().data_ptr() for t in again}
+    torch.cuda.synchronize()
+
+
 def test_captured_and_replayed_with_other_lengths(laga):
     """One captured call serves every step: lengths, table and queries are read when it is replayed."""
     q, w, cache, table, lens = (t.cuda() for t in case([500, 300, 64], 16, 64, seed=8, fill=0.0))
