@@ -225,12 +225,12 @@ int laga_rope(const void* x, long long x_pitch, const int* positions, const doub
  *   cache, slots: if not NULL, row slots[m] of the cache, bf16 [n_slots, D + R], receives latent and key side by side; a slot
  *   outside [0, n_slots) writes nothing (padding rows of a batch).  Two rows of one call must not name the same slot.
  * latent and k_pe may both be NULL when cache is not (serving: the token only enters the cache).  The rows of the
- * cache that no slot names are left as they are.  Outputs must not overlap inputs or one another.
+ * cache that no slot names are left as they are.  Outputs must not overlap inputs or one another (LAGA_ERR_INVALID_ARG).
  *
  * laga_latent_norm_rope_backward: dkv_a bf16 [M, D + R] written; dgamma fp32 [D] and, if not NULL, dbeta fp32 [D]
  * overwritten.  Row sums are formed per block in `workspace` (16-byte aligned, sized by the query) and added in a
- * fixed order: the call repeats bit for bit.
- * D: a multiple of 8, at most 1024; R: a multiple of 16, at most 256; kv_a_pitch: a multiple of 8.
+ * fixed order: the call repeats bit for bit.  Its outputs and the workspace must not overlap its inputs or one another either.
+ * D: a multiple of 8, at most 1024; R: a multiple of 16, at most 256; kv_a_pitch: a multiple of 8, at most 2^30; M at most 2^30.
  */
 int laga_latent_norm_rope(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps,
                           const int* positions, const double* freqs, int M, int D, int R, int layout, float mscale,
@@ -275,6 +275,7 @@ int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, in
  *                rows behind its last token are not used, whatever they hold.
  *   out          bf16 [B, h, d_v] written; a request of length 0 gets zeros
  *   lse          fp32 [B, h] written if not NULL (-inf for length 0)
+ * Outputs and the workspace must not overlap inputs or one another (LAGA_ERR_INVALID_ARG).
  * A length outside [0, columns * page_size] is clamped, and a page number outside [0, n_pages) reads as zeros; both report
  * LAGA_ERR_DEVICE_CHECK through laga_query_status(workspace).  page_size: a power of two from 16 to 1024; n_pages * page_size
  * and columns * page_size at most 2^30, B * columns * page_size at most 2^36, B * h at most 2^26.  d_c, d_nope, d_rope, d_v: 512, 128, 64, 128.  flags must be 0.

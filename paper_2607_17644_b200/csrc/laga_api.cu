@@ -1270,6 +1270,19 @@ static bool overlap_bytes(const void* a, size_t a_bytes, const void* b, size_t b
     return x < y + b_bytes && y < x + a_bytes;
 }
 
+struct Span { const void* p; size_t bytes; };                // p may be NULL: an argument that is not there
+// An output that shares memory with an input or with another output.
+static bool outputs_clash(std::initializer_list<Span> in, std::initializer_list<Span> out) {
+    for (const Span* o = out.begin(); o != out.end(); ++o) {
+        if (o->p == nullptr) continue;
+        for (const Span& i : in)
+            if (i.p != nullptr && overlap_bytes(i.p, i.bytes, o->p, o->bytes)) return true;
+        for (const Span* x = out.begin(); x != o; ++x)
+            if (x->p != nullptr && overlap_bytes(x->p, x->bytes, o->p, o->bytes)) return true;
+    }
+    return false;
+}
+
 int laga_rope(const void* x, long long x_pitch, const int* positions, const double* freqs, int M, int h, int d, int rot_begin,
               int d_rot, int layout, float mscale, int inverse, void* y, long long y_pitch, void* stream) {
     if (!x || !y || M < 1 || h < 1 || d < 16 || d > kRopeMaxD || (d & 7) || rot_begin < 0 || (rot_begin & 7) ||
@@ -1281,6 +1294,9 @@ int laga_rope(const void* x, long long x_pitch, const int* positions, const doub
     const bool in_place = x == y;
     if (in_place ? x_pitch != y_pitch
                  : overlap_bytes(x, ((M - 1) * static_cast<size_t>(x_pitch) + width) * 2, y, ((M - 1) * static_cast<size_t>(y_pitch) + width) * 2))
+        return LAGA_ERR_INVALID_ARG;
+    if (outputs_clash({{positions, static_cast<size_t>(M) * 4}, {freqs, static_cast<size_t>(d_rot) * 4}},
+                      {{y, ((M - 1) * static_cast<size_t>(y_pitch) + width) * 2}}))
         return LAGA_ERR_INVALID_ARG;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
@@ -1309,13 +1325,18 @@ int laga_rope(const void* x, long long x_pitch, const int* positions, const doub
 int laga_latent_norm_rope(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps,
                           const int* positions, const double* freqs, int M, int D, int R, int layout, float mscale, void* latent,
                           void* k_pe, float* mean, float* rstd, void* cache, const int* slots, int n_slots, void* stream) {
-    if (!kv_a || !gamma || M < 1 || D < 8 || (D & 7) || D > kLnMaxD || !(eps >= 0.f) ||
+    if (!kv_a || !gamma || M < 1 || M > kLatentMaxRows || D < 8 || (D & 7) || D > kLnMaxD || !(eps >= 0.f) ||
         !rotary_ok(positions, freqs, R, mscale, layout))
         return LAGA_ERR_INVALID_ARG;
     if (kv_a_pitch < D + R || (kv_a_pitch & 7) || !latent != !k_pe || !cache != !slots || (!latent && !cache) || (cache && n_slots < 1))
         return LAGA_ERR_INVALID_ARG;
     if (!aligned16(kv_a) || !aligned16(gamma) || !aligned16(beta) || !aligned16(latent) || !aligned16(k_pe) || !aligned16(cache) ||
         (reinterpret_cast<uintptr_t>(slots) & 3u) || (reinterpret_cast<uintptr_t>(mean) & 3u) || (reinterpret_cast<uintptr_t>(rstd) & 3u))
+        return LAGA_ERR_INVALID_ARG;
+    const size_t m = static_cast<size_t>(M);
+    if (kv_a_pitch > (1ll << 30) ||
+        outputs_clash({{kv_a, ((m - 1) * kv_a_pitch + D + R) * 2}, {gamma, D * 2ull}, {beta, D * 2ull}, {positions, m * 4}, {freqs, R * 4ull}, {slots, m * 4}},
+                      {{latent, m * D * 2}, {k_pe, m * R * 2}, {mean, m * 4}, {rstd, m * 4}, {cache, static_cast<size_t>(n_slots) * (D + R) * 2}}))
         return LAGA_ERR_INVALID_ARG;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
@@ -1352,14 +1373,19 @@ int laga_latent_norm_rope_backward(const void* dlatent, const void* dk_pe, const
                                    const float* mean, const float* rstd, const int* positions, const double* freqs, int M, int D,
                                    int R, int layout, float mscale, void* dkv_a, float* dgamma, float* dbeta, void* workspace,
                                    size_t workspace_bytes, void* stream) {
-    if (!dlatent || !dk_pe || !kv_a || !gamma || !mean || !rstd || !dkv_a || !dgamma || !workspace || M < 1 || D < 8 || (D & 7) ||
-        D > kLnMaxD || !rotary_ok(positions, freqs, R, mscale, layout) || kv_a_pitch < D + R || (kv_a_pitch & 7))
+    if (!dlatent || !dk_pe || !kv_a || !gamma || !mean || !rstd || !dkv_a || !dgamma || !workspace || M < 1 || M > kLatentMaxRows || D < 8 || (D & 7) ||
+        D > kLnMaxD || !rotary_ok(positions, freqs, R, mscale, layout) || kv_a_pitch < D + R || (kv_a_pitch & 7) || kv_a_pitch > (1ll << 30))
         return LAGA_ERR_INVALID_ARG;
     if (!aligned16(dlatent) || !aligned16(dk_pe) || !aligned16(kv_a) || !aligned16(gamma) || !aligned16(dkv_a) || !aligned16(workspace) ||
         (reinterpret_cast<uintptr_t>(mean) & 3u) || (reinterpret_cast<uintptr_t>(rstd) & 3u) ||
         (reinterpret_cast<uintptr_t>(dgamma) & 3u) || (reinterpret_cast<uintptr_t>(dbeta) & 3u))
         return LAGA_ERR_INVALID_ARG;
-    if (workspace_bytes < laga_latent_norm_rope_backward_workspace_bytes(M, D)) return LAGA_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = laga_latent_norm_rope_backward_workspace_bytes(M, D), m = static_cast<size_t>(M);
+    if (workspace_bytes < need) return LAGA_ERR_WORKSPACE_TOO_SMALL;
+    if (outputs_clash({{dlatent, m * D * 2}, {dk_pe, m * R * 2}, {kv_a, ((m - 1) * kv_a_pitch + D + R) * 2}, {gamma, D * 2ull}, {mean, m * 4},
+                       {rstd, m * 4}, {positions, m * 4}, {freqs, R * 4ull}},
+                      {{dkv_a, m * (D + R) * 2}, {dgamma, D * 4ull}, {dbeta, D * 4ull}, {workspace, need}}))
+        return LAGA_ERR_INVALID_ARG;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
     if ((rc = check_pointers({dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, freqs, dkv_a, dgamma, dbeta, workspace})) != LAGA_OK)
@@ -1391,18 +1417,16 @@ int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, in
         max_tokens < 1 || max_tokens > (1 << 30) || (static_cast<long long>(columns) << shift) > (1ll << 30))
         return LAGA_ERR_INVALID_ARG;
     // every block reads the state while block 0 writes the new one: the outputs must not be the inputs
-    const size_t n4 = static_cast<size_t>(n_requests) * 4;
-    const struct { const void* p; size_t bytes; } in[] = {{seq_lens, n4}, {new_lens, n4}, {free_pages, static_cast<size_t>(free_capacity) * 4},
-                                                          {n_free, 4}},
-        out[] = {{slots, static_cast<size_t>(max_tokens) * 4}, {positions, static_cast<size_t>(max_tokens) * 4}, {cu_new_lens, n4 + 4},
-                 {seq_lens_out, n4}, {n_free_out, 4}, {status_word, 4}, {block_table, n4 * columns}};
-    for (const auto& o : out) {
-        if (reinterpret_cast<uintptr_t>(o.p) & 3u) return LAGA_ERR_INVALID_ARG;
-        for (const auto& i : in)
-            if ((reinterpret_cast<uintptr_t>(i.p) & 3u) || overlap_bytes(i.p, i.bytes, o.p, o.bytes)) return LAGA_ERR_INVALID_ARG;
-        for (const auto& x : out)
-            if (&x != &o && overlap_bytes(x.p, x.bytes, o.p, o.bytes)) return LAGA_ERR_INVALID_ARG;
-    }
+    const size_t n4 = static_cast<size_t>(n_requests) * 4, rows4 = static_cast<size_t>(max_tokens) * 4;
+    for (const void* p : {static_cast<const void*>(seq_lens), static_cast<const void*>(new_lens), static_cast<const void*>(free_pages),
+                          static_cast<const void*>(n_free), static_cast<const void*>(slots), static_cast<const void*>(positions),
+                          static_cast<const void*>(cu_new_lens), static_cast<const void*>(seq_lens_out), static_cast<const void*>(n_free_out),
+                          static_cast<const void*>(status_word), static_cast<const void*>(block_table)})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return LAGA_ERR_INVALID_ARG;
+    if (outputs_clash({{seq_lens, n4}, {new_lens, n4}, {free_pages, static_cast<size_t>(free_capacity) * 4}, {n_free, 4}},
+                      {{slots, rows4}, {positions, rows4}, {cu_new_lens, n4 + 4}, {seq_lens_out, n4}, {n_free_out, 4}, {status_word, 4},
+                       {block_table, n4 * columns}}))
+        return LAGA_ERR_INVALID_ARG;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
     if ((rc = check_pointers({seq_lens, new_lens, free_pages, n_free, slots, positions, cu_new_lens, seq_lens_out, n_free_out, status_word,
@@ -1440,6 +1464,11 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
         return LAGA_ERR_INVALID_ARG;
     const DecodeLayout w = decode_layout(B, h);
     if (workspace_bytes < w.total) return LAGA_ERR_WORKSPACE_TOO_SMALL;
+    const size_t b = static_cast<size_t>(B), bh = b * h;
+    if (outputs_clash({{q, bh * 192 * 2}, {w_kv_b, static_cast<size_t>(h) * 512 * 256 * 2}, {cache, static_cast<size_t>(rows) * kDecRow * 2},
+                       {block_table, b * columns * 4}, {seq_lens, b * 4}},
+                      {{out, bh * 128 * 2}, {lse, bh * 4}, {workspace, w.total}}))
+        return LAGA_ERR_INVALID_ARG;
     int rc = check_device();
     if (rc != LAGA_OK) return rc;
     if ((rc = check_pointers({q, w_kv_b, cache, block_table, seq_lens, out, lse, workspace})) != LAGA_OK) return rc;

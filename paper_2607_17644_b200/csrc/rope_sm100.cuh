@@ -232,6 +232,7 @@ __device__ __forceinline__ uint4 f2_pack(const F2* f) {
 // kLatentDepth rows per half warp are in shared memory or on their way; gamma and beta stay in registers as bf16, and the
 // arithmetic runs two values at a time.  kChunks = ceil(D / 128) chunks of eight channels a lane; kFull: D is kChunks * 128.
 constexpr int kLatentDepth = 2;
+constexpr int kLatentMaxRows = 1 << 30;      // row numbers one or two strides ahead stay within 31 bits
 __host__ __device__ constexpr int latent_fwd_smem(int D, int R) { return kLnWarps * 2 * kLatentDepth * (D + R) * 2; }
 __device__ __forceinline__ float half_warp_sum(float v) {
 #pragma unroll

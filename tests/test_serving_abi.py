@@ -42,6 +42,7 @@ def test_rope_refusals(laga):
     assert call(ms=float("nan")) == bad
     assert call(y=at(0), yp=4 * 192) == bad                      # in place needs one pitch
     assert call(y=P((1 << 32) + 384)) == bad                     # overlaps x without being x
+    assert call(y=at(1)) == bad and call(y=at(2)) == bad
 
 
 def test_latent_norm_rope_refusals(laga):
@@ -62,12 +63,21 @@ def test_latent_norm_rope_refusals(laga):
     assert fwd(cache=at(8)) == bad and fwd(slots=at(8)) == bad
     assert fwd(cache=at(8), slots=at(9), n_slots=0) == bad
     assert fwd(beta=P(8)) == bad
+    assert fwd(M=(1 << 30) + 1) == bad and fwd(pitch=(1 << 30) + 8) == bad
+    for name in ("lat", "kpe", "mean", "rstd"):                   # outputs apart from inputs ...
+        for i in (0, 1, 2, 3):
+            assert fwd(**{name: at(i)}) == bad, (name, i)
+    assert fwd(cache=at(0), slots=at(9), n_slots=4) == bad and fwd(cache=at(8), slots=at(8), n_slots=4) == bad
+    assert fwd(rstd=at(6)) == bad and fwd(kpe=P((5 << 32) + 4 * 512 * 2 - 16)) == bad      # ... and from one another
+    assert fwd(cache=at(4), slots=at(9), n_slots=4) == bad
 
     def bwd(dl=at(0), ws=at(9), ws_bytes=1 << 30, M=4, D=512, R=64, pitch=576):
         return lib.laga_latent_norm_rope_backward(dl, at(1), at(2), pitch, at(3), at(4), at(5), at(6), at(7), M, D, R, 0, 1.0, at(8), at(10),
                                                   None, ws, ws_bytes, None)
 
     assert bwd(dl=None) == bad and bwd(ws=None) == bad and bwd(M=0) == bad and bwd(D=20) == bad and bwd(R=20) == bad and bwd(pitch=512) == bad
+    assert bwd(M=(1 << 30) + 1) == bad and bwd(pitch=(1 << 30) + 8) == bad
+    assert bwd(dl=at(8)) == bad and bwd(ws=at(2)) == bad and bwd(ws=at(10)) == bad and bwd(dl=P((10 << 32) + 1024)) == bad
     assert bwd(ws_bytes=16) == laga.ERR_WORKSPACE_TOO_SMALL
     size = lib.laga_latent_norm_rope_backward_workspace_bytes
     assert size(1, 512) == 4096 and size(1 << 20, 512) == 296 * 4096 and size(0, 512) == 0 and size(5, 2048) == 0
@@ -110,6 +120,9 @@ def test_paged_decode_refusals_and_sizes(laga):
     assert call(ws=P((7 << 32) + 16)) == bad and call(q=P(24)) == bad and call(lens=P(6)) == bad
     assert call(pages=(1 << 24) + 1) == bad and call(columns=(1 << 24) + 1) == bad
     assert call(columns=1 << 24, B=65) == bad                     # tiles counted in 32 bits
+    for i in (0, 1, 2, 3, 4):                                     # outputs and workspace apart from inputs and from one another
+        assert call(out=at(i)) == bad and call(lse=at(i)) == bad and call(ws=at(i)) == bad, i
+    assert call(lse=at(5)) == bad and call(ws=at(5)) == bad and call(lse=P((7 << 32) + 64)) == bad
     assert call(dc=256) == laga.ERR_UNSUPPORTED and call(dv=64) == laga.ERR_UNSUPPORTED
     assert call(ws_bytes=4096) == laga.ERR_WORKSPACE_TOO_SMALL
     size = laga.paged_decode_workspace_bytes
