@@ -180,16 +180,21 @@ class LagaBlock(torch.nn.Module):
         return laga.linear(out.view(T, self.n_heads * self.D_V), self.w_o)[0]
 
     @torch.no_grad()
-    def decode(self, hidden: torch.Tensor, pages: torch.Tensor, step, block_table: torch.Tensor, workspace=None) -> torch.Tensor:
+    def decode(self, hidden: torch.Tensor, pages: torch.Tensor, step, block_table: torch.Tensor, workspace=None, requests=None) -> torch.Tensor:
         """One new token for each of B requests: hidden [B, d_model], ``step`` a plan that gives every request one token,
-        block_table the plan's table [B, columns].  Appends the tokens' latents and keys to ``pages`` and attends to each request's
+        block_table the plan's table [B, columns].  Where the plan gave only some requests a token, ``requests`` (int64 [B], on the
+        device, ascending) names them; rows of ``hidden`` behind the plan's tokens are padding (any request's number, results to be
+        ignored).  Appends the tokens' latents and keys to ``pages`` and attends to each request's
         whole cache, the new token included.  Every call reads lengths and tables on the device, so a step can be captured in a
         graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``) and replayed."""
         self._service()
         B = hidden.shape[0]
         q = laga.linear(hidden, self.w_q)[0].view(B, self.n_heads, self.D_NOPE + self.D_ROPE)
         kv_a = laga.linear(hidden, self.w_kv_a)[0]
-        laga.rope(q, step.positions, self.rope, y=q)
-        laga.cache_append(kv_a, self.ln_gamma, self.ln_beta, step.positions, self.rope, step.slots, pages, eps=self.eps)
-        out = laga.paged_decode(q, self.w_kv_b, pages, block_table, step.seq_lens, workspace=workspace)[0]
+        positions, slots, lens = step.positions[:B], step.slots[:B], step.seq_lens
+        if requests is not None:
+            block_table, lens = block_table.index_select(0, requests), lens.index_select(0, requests)
+        laga.rope(q, positions, self.rope, y=q)
+        laga.cache_append(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, slots, pages, eps=self.eps)
+        out = laga.paged_decode(q, self.w_kv_b, pages, block_table, lens, workspace=workspace)[0]
         return laga.linear(out.view(B, self.n_heads * self.D_V), self.w_o)[0]

@@ -108,6 +108,31 @@ def test_prompts_and_decode_steps_against_one_pass(pkg):
         assert rel_l2(torch.stack([d[b] for d in decoded]), whole[n:]) <= 2e-2
 
 
+def test_decode_step_for_some_of_the_requests(pkg):
+    """Requests 0 and 2 of three take a token, in a batch padded to four rows: each as it does in a service of its own, and the
+    padding and request 1 leave the cache as it was.  (Not bit for bit: another batch splits the contexts elsewhere.  2e-2: see
+    the test against one pass.)"""
+    laga = pkg.laga
+    blk = make_block(pkg, heads=16)
+    g = torch.Generator().manual_seed(12)
+    lens = [40, 25, 33]
+    prompts = [torch.randn(n, 512, generator=g).to(BF16).cuda() for n in lens]
+    token = torch.randn(4, 512, generator=g).to(BF16).cuda()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    cache = pkg.LatentCache(n_pages=12, n_requests=3, max_tokens=64, page_size=16)
+    blk.prefill(torch.cat(prompts), cache.pages[0], cache.plan(torch.tensor(lens, **i32), 98), [0, 40, 65, 98])
+    before = cache.pages[0].clone()
+    step = cache.plan(torch.tensor([1, 0, 1], **i32), 4)
+    laga.check_status(step.status)
+    requests = torch.tensor([0, 2, 2, 2], device="cuda")
+    y = blk.decode(token, cache.pages[0], step, cache.block_table, requests=requests)
+    changed = (cache.pages[0] != before).any(-1).view(-1).nonzero().view(-1).tolist()
+    assert sorted(changed) == sorted(step.slots[:2].tolist()) and step.slots[2:].tolist() == [-1, -1]
+    for row, b in enumerate((0, 2)):
+        whole = blk(torch.cat([prompts[b], token[row:row + 1]]))
+        assert rel_l2(y[row], whole[-1]) <= 2e-2
+
+
 def test_captured_decode_steps_equal_eager_ones(pkg):
     """plan + decode captured once and replayed: lengths, tables and pages advance on the device."""
     laga = pkg.laga
