@@ -1,4 +1,5 @@
-"""In-tree build of the CUDA library (``liblaga.so``) with nvcc for sm_100a.
+"""In-tree build of the CUDA library (``liblaga.so``) with nvcc for sm_100a, and of the compiled part of its Python binding
+(``_binding.so``) with g++.
 
 Run as ``python -m paper_2607_17644_b200.build`` or call :func:`build`.  nvcc cross-compiles
 without a GPU present.  The library is rebuilt only when a source is newer than it.
@@ -9,11 +10,13 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 ROOT = os.path.dirname(PKG_DIR)
 LIB_PATH = os.path.join(PKG_DIR, "liblaga.so")
+BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "liblaga_debug.so")   # the checked build (-DLAGA_DEBUG), see sm100_ptx.cuh
 
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -25,9 +28,31 @@ def sources():
             sorted(glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))))
 
 
+def build_binding(force: bool = False, verbose: bool = False) -> str:
+    """Build _binding.so (csrc/binding.cpp) against the headers of the installed torch.  With the system's g++ and not $CXX: torch's
+    exceptions pass through it, so it must share torch's C++ runtime, which a compiler set up to link its own would not."""
+    source, header = os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "laga.h")
+    if not force and os.path.exists(BINDING_PATH) and os.path.getmtime(BINDING_PATH) >= max(os.path.getmtime(source), os.path.getmtime(header)):
+        return BINDING_PATH
+    import torch
+    base = os.path.dirname(torch.__file__)
+    tmp = BINDING_PATH + f".tmp{os.getpid()}"
+    cmd = ["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           *(f"-I{d}" for d in (os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
+                                sysconfig.get_paths()["include"], "/usr/local/cuda/include")),
+           source, "-o", tmp, f"-L{os.path.join(base, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
+    if verbose:
+        print(" ".join(cmd), file=sys.stderr)
+    subprocess.run(cmd, check=True)
+    os.replace(tmp, BINDING_PATH)
+    return BINDING_PATH
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=(), debug: bool = False) -> str:
-    """Build the library (debug=True: the checked build, whose kernels verify their own index arithmetic
+    """Build the library and, beside it, the binding (debug=True: the checked build, whose kernels verify their own index arithmetic
     and report LAGA_ERR_DEVICE_CHECK instead of making a bad access; selected at run time by LAGA_DEBUG=1)."""
+    build_binding(force, verbose)
     cus, deps = sources()
     target = DEBUG_LIB_PATH if debug else LIB_PATH
     newest = max(os.path.getmtime(p) for p in cus + deps)

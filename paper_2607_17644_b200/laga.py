@@ -33,6 +33,7 @@ FLAG_FUSED_KV_REBUILD = 16
 DEBUG = os.environ.get("LAGA_DEBUG", "0") not in ("", "0")
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblaga_debug.so" if DEBUG else "liblaga.so")
 _lib = None
+_binding = None
 
 # name -> (restype, argtypes); mirrors include/laga.h one to one
 _vp, _ci, _cf, _cu, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint, ctypes.c_size_t
@@ -95,6 +96,32 @@ def lib():
     return _lib
 
 
+def _load_binding():
+    """The compiled side of the rotary, cache and decode calls (csrc/binding.cpp), bound to the library that `lib` loads."""
+    global _binding
+    try:
+        from . import _binding as module
+    except ImportError as missing:
+        raise ImportError("the compiled binding is missing: build it with `python -m paper_2607_17644_b200.build`") from missing
+    names = ("laga_rope", "laga_latent_norm_rope", "laga_latent_norm_rope_backward_workspace_bytes", "laga_latent_norm_rope_backward",
+             "laga_cache_plan", "laga_paged_decode_workspace_bytes", "laga_paged_decode")
+    module.bind(_check, *(ctypes.cast(getattr(lib(), name), _vp).value for name in names))
+    _binding = module
+    return module
+
+
+def _run(entry, stream, first, *rest):
+    """Calls the binding's `entry`, whose outputs and workspace come from the pool of the stream that it runs on: another stream's
+    pool may hand out memory that that stream's queued work still uses, and give it away again too early."""
+    call = getattr(_binding or _load_binding(), entry)
+    if stream is None:
+        return call(first, *rest)
+    if stream.device != first.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {first.device}")
+    with torch.cuda.stream(stream):
+        return call(first, *rest)
+
+
 def version() -> int:
     return int(lib().laga_version())
 
@@ -147,15 +174,6 @@ _HERE = contextlib.nullcontext()
 def _on(device):
     """Context that makes `device` current for the duration of a library call."""
     return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
-
-
-def _new(like, shape, stream, dtype=None):
-    """What a call on `stream` writes, from that stream's pool: the current stream's pool may hand out memory that its own queued
-    work still uses, and give it away again before `stream` is done with it."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
 
 
 def _geometry(q, c_kv, k_pe, w_kv_b, d_v):
@@ -452,134 +470,30 @@ def rope_plan(d_rot=64, base=10000.0, scaling=None, interleaved=True, device="cu
     return RopePlan(freqs.to(device), mscale, bool(interleaved))
 
 
-def _rows(t, name, dims, dtype=torch.bfloat16):
-    """A CUDA tensor whose rows (first axis) are dense and may be any pitch apart; returns the pitch in elements."""
-    if t.is_cuda and t.dtype == dtype and t.dim() == dims and t.is_contiguous():
-        return math.prod(t.shape[1:])
-    expect = 1
-    ok = t.is_cuda and t.dtype == dtype and t.dim() == dims
-    if ok:
-        for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-            ok = ok and (stride == expect or size == 1)
-            expect *= size
-        pitch = t.stride(0) if t.shape[0] > 1 else expect
-    if not ok or pitch < expect:
-        raise ValueError(f"{name}: expected a {dims}-d CUDA {dtype} tensor with dense rows, got {t.dtype} {tuple(t.shape)} "
-                         f"strides {t.stride()} on {t.device}")
-    return pitch
-
-
-def _rope_args(rope, positions, M, d_rot=None):
-    n = rope.freqs.shape[0]
-    _dev(rope.freqs, torch.float64, (n,), "freqs")
-    _dev(positions, torch.int32, (M,), "positions")
-    if d_rot is not None and 2 * n != d_rot:
-        raise ValueError(f"the plan rotates {2 * n} channels, the tensor has {d_rot}")
-    return 2 * n
-
-
 def rope(x, positions, rope, rot_begin=None, inverse=False, y=None, stream=None):
     """laga_rope: x bf16 [M, h, d] (rows may be strided) with channels [rot_begin, rot_begin + d_rot) of every head
     rotated (default: the last ones).  positions int32 [M].  inverse: the transpose (gradient).  y: a new tensor, or x itself
     for the rotation in place.  Returns y."""
-    M, h, d = x.shape
-    x_pitch = _rows(x, "x", 3)
-    d_rot = _rope_args(rope, positions, M)
-    if y is None:
-        y, y_pitch = _new(x, (M, h, d), stream), h * d
-    else:
-        y_pitch = _rows(y, "y", 3)
-        if y.shape != (M, h, d):
-            raise ValueError(f"y: expected shape {(M, h, d)}, got {tuple(y.shape)}")
-    dev = same_device(x, positions, rope.freqs, y)
-    if M == 0:
-        return y
-    with _on(dev):
-        rc = lib().laga_rope(_ptr(x), x_pitch, _ptr(positions), _ptr(rope.freqs), M, h, d, d - d_rot if rot_begin is None else rot_begin,
-                             d_rot, int(rope.interleaved), float(rope.mscale), int(bool(inverse)), _ptr(y), y_pitch,
-                             _stream(stream, dev))
-    _check(rc, "laga_rope")
-    return y
-
-
-def _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, latent, k_pe, mean, rstd, cache, slots, stream):
-    M, D = kv_a.shape[0], gamma.shape[0]
-    R = kv_a.shape[1] - D
-    pitch = _rows(kv_a, "kv_a", 2)
-    _dev(gamma, torch.bfloat16, (D,), "gamma")
-    if beta is not None:
-        _dev(beta, torch.bfloat16, (D,), "beta")
-    _rope_args(rope, positions, M, R)
-    n_slots = 0
-    if cache is not None:
-        if cache.dim() < 2:
-            raise ValueError(f"cache: expected [..., {D + R}], got {tuple(cache.shape)}")
-        _dev(cache, torch.bfloat16, tuple(cache.shape[:-1]) + (D + R,), "cache")
-        _dev(slots, torch.int32, (M,), "slots")
-        n_slots = cache.numel() // (D + R)
-    dev = same_device(kv_a, gamma, beta, positions, rope.freqs, latent, k_pe, cache, slots)
-    if M == 0:
-        return
-    with _on(dev):
-        rc = lib().laga_latent_norm_rope(_ptr(kv_a), pitch, _ptr(gamma), _ptr(beta), float(eps), _ptr(positions), _ptr(rope.freqs), M, D,
-                                         R, int(rope.interleaved), float(rope.mscale), _ptr(latent), _ptr(k_pe), _ptr(mean),
-                                         _ptr(rstd), _ptr(cache), _ptr(slots), n_slots, _stream(stream, dev))
-    _check(rc, "laga_latent_norm_rope")
+    return _run("rope", stream, x, positions, rope, rot_begin, inverse, y)
 
 
 def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps=1e-5, latent=None, k_pe=None, cache=None, slots=None, stream=None):
     """laga_latent_norm_rope: kv_a bf16 [M, D + R] (rows may be strided) -> (latent bf16 [M, D], k_pe bf16 [M, R], mean, rstd
     fp32 [M]).  With cache (bf16 [..., D + R]) and slots (int32 [M]) the rows also enter the cache."""
-    M, D = kv_a.shape[0], gamma.shape[0]
-    R = kv_a.shape[1] - D
-    if (cache is None) != (slots is None):
-        raise ValueError("cache and slots go together")
-    latent = _new(gamma, (M, D), stream) if latent is None else _dev(latent, torch.bfloat16, (M, D), "latent")
-    k_pe = _new(gamma, (M, R), stream) if k_pe is None else _dev(k_pe, torch.bfloat16, (M, R), "k_pe")
-    mean = _new(gamma, M, stream, torch.float32)
-    rstd = _new(gamma, M, stream, torch.float32)
-    _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, latent, k_pe, mean, rstd, cache, slots, stream)
-    return latent, k_pe, mean, rstd
+    return _run("latent_norm_rope", stream, kv_a, gamma, beta, positions, rope, eps, True, latent, k_pe, cache, slots)
 
 
 def cache_append(kv_a, gamma, beta, positions, rope, slots, cache, eps=1e-5, stream=None):
     """laga_latent_norm_rope into the cache alone: row slots[m] of cache (bf16 [..., D + R]) receives the normalised latent and
     the rotated key of kv_a's row m; a slot outside the cache (-1) writes nothing.  Returns cache."""
-    _latent_norm_rope(kv_a, gamma, beta, positions, rope, eps, None, None, None, None, cache, slots, stream)
+    _run("latent_norm_rope", stream, kv_a, gamma, beta, positions, rope, eps, False, None, None, cache, slots)
     return cache
 
 
 def latent_norm_rope_backward(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope, with_beta=True, dkv_a=None, workspace=None,
                               stream=None):
     """laga_latent_norm_rope_backward: returns (dkv_a bf16 [M, D + R], dgamma fp32 [D], dbeta fp32 [D] or None)."""
-    M, D = dlatent.shape
-    R = dk_pe.shape[1]
-    _dev(dlatent, torch.bfloat16, (M, D), "dlatent")
-    _dev(dk_pe, torch.bfloat16, (M, R), "dk_pe")
-    pitch = _rows(kv_a, "kv_a", 2)
-    if tuple(kv_a.shape) != (M, D + R):
-        raise ValueError(f"kv_a: expected shape {(M, D + R)}, got {tuple(kv_a.shape)}")
-    _dev(gamma, torch.bfloat16, (D,), "gamma")
-    _dev(mean, torch.float32, (M,), "mean")
-    _dev(rstd, torch.float32, (M,), "rstd")
-    _rope_args(rope, positions, M, R)
-    dev = same_device(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope.freqs, dkv_a, workspace)
-    dkv_a = _new(dlatent, (M, D + R), stream) if dkv_a is None else _dev(dkv_a, torch.bfloat16, (M, D + R), "dkv_a")
-    if M == 0:
-        sums = torch.zeros(2, D, dtype=torch.float32, device=dev)
-        return dkv_a, sums[0], sums[1] if with_beta else None
-    need = int(lib().laga_latent_norm_rope_backward_workspace_bytes(M, D))
-    if workspace is None:
-        workspace = _new(mean, need // 4, stream)
-    dgamma = _new(mean, D, stream)
-    dbeta = _new(mean, D, stream) if with_beta else None
-    with _on(dev):
-        rc = lib().laga_latent_norm_rope_backward(
-            _ptr(dlatent), _ptr(dk_pe), _ptr(kv_a), pitch, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(positions), _ptr(rope.freqs), M, D,
-            R, int(rope.interleaved), float(rope.mscale), _ptr(dkv_a), _ptr(dgamma), _ptr(dbeta),
-            _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, dev))
-    _check(rc, "laga_latent_norm_rope_backward")
-    return dkv_a, dgamma, dbeta
+    return _run("latent_norm_rope_backward", stream, dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope, with_beta, dkv_a, workspace)
 
 
 class CachePlan(NamedTuple):
@@ -596,25 +510,8 @@ def cache_plan(seq_lens, new_lens, block_table, free_pages, n_free, page_size, m
     """laga_cache_plan: pages, slots and positions for a step that adds new_lens[b] tokens to request b.  block_table
     (int32 [n, columns]) is written in place where the new tokens need pages; everything else comes back new (or in `out`,
     a CachePlan of an earlier call with the same sizes)."""
-    n, columns = block_table.shape
-    _dev(seq_lens, torch.int32, (n,), "seq_lens")
-    _dev(new_lens, torch.int32, (n,), "new_lens")
-    _dev(block_table, torch.int32, (n, columns), "block_table")
-    _dev(free_pages, torch.int32, (free_pages.numel(),), "free_pages")
-    _dev(n_free, torch.int32, (1,), "n_free")
-    dev = same_device(seq_lens, new_lens, block_table, free_pages, n_free, *(out or ()))
-    if out is None:
-        whole = _new(seq_lens, 2 * max_tokens + 2 * n + 3, stream)
-        out = CachePlan(*torch.split_with_sizes(whole, [max_tokens, max_tokens, n + 1, n, 1, 1]))
-    else:
-        for name, size in zip(CachePlan._fields, (max_tokens, max_tokens, n + 1, n, 1, 1)):
-            _dev(getattr(out, name), torch.int32, (size,), name)
-    with _on(dev):
-        rc = lib().laga_cache_plan(_ptr(seq_lens), _ptr(new_lens), n, int(page_size), _ptr(block_table), columns, _ptr(free_pages),
-                                   free_pages.numel(), _ptr(n_free), int(max_tokens), _ptr(out.slots), _ptr(out.positions),
-                                   _ptr(out.cu_new_lens), _ptr(out.seq_lens), _ptr(out.n_free), _ptr(out.status), _stream(stream, dev))
-    _check(rc, "laga_cache_plan")
-    return out
+    plan = _run("cache_plan", stream, seq_lens, new_lens, block_table, free_pages, n_free, page_size, max_tokens, out)
+    return CachePlan._make(plan) if out is None else plan
 
 
 def paged_decode_workspace_bytes(B, h, d_c=512, d_nope=128, d_rope=64, d_v=128) -> int:
@@ -625,34 +522,7 @@ def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, ou
     """laga_paged_decode: attention of one new token per request (q bf16 [B, h, 192], rope band rotated) over a paged cache
     (bf16 [n_pages, page_size, 576]; block_table int32 [B, columns], seq_lens int32 [B], both on the device).  lse: fp32 [B, h] to
     have it written.  Returns (out bf16 [B, h, 128], lse or None, workspace)."""
-    B, h, d_qk = q.shape
-    _dev(q, torch.bfloat16, (B, h, d_qk), "q")
-    n_pages, page_size, row = cache.shape
-    _dev(cache, torch.bfloat16, (n_pages, page_size, row), "cache")
-    d_c = w_kv_b.shape[0]
-    d_rope = row - d_c
-    d_nope, d_v = d_qk - d_rope, w_kv_b.shape[1] // h - (d_qk - d_rope)
-    _dev(w_kv_b, torch.bfloat16, (d_c, h * (d_nope + d_v)), "w_kv_b")
-    _dev(block_table, torch.int32, (B, block_table.shape[1]), "block_table")
-    _dev(seq_lens, torch.int32, (B,), "seq_lens")
-    dev = same_device(q, w_kv_b, cache, block_table, seq_lens, out, lse, workspace)
-    if softmax_scale is None:
-        softmax_scale = d_qk ** -0.5
-    out = _new(q, (B, h, d_v), stream) if out is None else _dev(out, torch.bfloat16, (B, h, d_v), "out")
-    if lse is not None:
-        _dev(lse, torch.float32, (B, h), "lse")
-    if workspace is None:
-        need = paged_decode_workspace_bytes(B, h, d_c, d_nope, d_rope, d_v)
-        if need == 0:
-            raise LagaError(ERR_UNSUPPORTED, "laga_paged_decode_workspace_bytes")
-        with _HERE if stream is None else torch.cuda.stream(stream):       # (the pool: see _new)
-            workspace = alloc_workspace(need, dev)
-    with _on(dev):
-        rc = lib().laga_paged_decode(_ptr(q), _ptr(w_kv_b), _ptr(cache), n_pages, page_size, _ptr(block_table), block_table.shape[1],
-                                     _ptr(seq_lens), B, h, d_c, d_nope, d_rope, d_v, float(softmax_scale), _ptr(out), _ptr(lse),
-                                     _ptr(workspace), workspace.numel(), 0, _stream(stream, dev))
-    _check(rc, "laga_paged_decode")
-    return out, lse, workspace
+    return _run("paged_decode", stream, q, w_kv_b, cache, block_table, seq_lens, softmax_scale, out, lse, workspace)
 
 
 def up_project(c_kv, w_kv_b, h, d_nope=128, d_v=128, kv=None, status_word=None, stream=None):
