@@ -398,6 +398,7 @@ template <int kLnChunks, bool kFull>
 __global__ void __launch_bounds__(kLnWarps * 32, kLnChunks <= 2 ? 2 : 1)
 latent_norm_rope_bwd_kernel(const LatentNormRopeBwdArgs a) {
     __shared__ float part[kLnWarps][kLnChunks * 256];
+    grid_launch_dependents();                                // the sums' blocks may take their places as these leave theirs
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n_warps = gridDim.x * kLnWarps;
     const float inv_d = 1.0f / static_cast<float>(a.D);
