@@ -3,7 +3,7 @@
 // A decode step makes a handful of these calls for 2 to 15 us of device work each, so what a call costs on the host is what a
 // service that does not capture its steps pays.  Checks, allocations and the call are compiled here.  Measured per call, calls in a row, a
 // B200's host, against ctypes with the same checks and allocations from Python: rotation 10.6 -> 5.0 us, latent norm 19.3 -> 9.1, its
-// backward 23.2 -> 10.8, into the cache 12 -> 4.6, plan 16.2 -> 9.6, one token's attention 20.9 -> 12 (its three kernels then take 14.5).
+// backward 23.2 -> 10.8, into the cache 12 -> 4.6, plan 16.2 -> 7.4, one token's attention 20.9 -> 12 (its three kernels then take 14.5).
 // The kernels' library is not linked: `bind` takes the addresses of its functions from the one that the package has loaded (the
 // ordinary or the checked build).
 #define PY_SSIZE_T_CLEAN
@@ -12,7 +12,6 @@
 #include <climits>
 #include <cmath>
 #include <cstring>
-#include <vector>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
@@ -118,6 +117,14 @@ struct Plan {
 
 // ---- results -----------------------------------------------------------------------------------------
 Tensor fresh(const Tensor& like, at::IntArrayRef shape, ScalarType dtype) { return at::empty(shape, like.options().dtype(dtype)); }
+// Elements offset .. offset + n of `whole`: a tensor on the same storage, made directly (of six results, six allocations or six
+// dispatched views would cost more than the call itself).
+Tensor part(const Tensor& whole, int64_t offset, int64_t n) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+    impl->set_storage_offset(offset);
+    impl->set_sizes_contiguous({n});
+    return Tensor(std::move(impl));
+}
 // 1024-byte aligned (the allocator aligns to 512 at least)
 Tensor workspace_of(const Tensor& like, size_t bytes) {
     const int64_t n = static_cast<int64_t>(bytes);
@@ -228,8 +235,9 @@ PyObject* py_latent_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (dense) {
         if (!latent.defined()) latent = fresh(kv_a, {M, D}, ScalarType::BFloat16);
         if (!k_pe.defined()) k_pe = fresh(kv_a, {M, R}, ScalarType::BFloat16);
-        mean = fresh(kv_a, {M}, ScalarType::Float);
-        rstd = fresh(kv_a, {M}, ScalarType::Float);
+        const Tensor statistics = fresh(kv_a, {2 * M}, ScalarType::Float);
+        mean = part(statistics, 0, M);
+        rstd = part(statistics, M, M);
     }
     if (M > 0)
         enqueue(device, "laga_latent_norm_rope", [&](void* stream) {
@@ -311,9 +319,10 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
     }
     const c10::Device device = one_device({&seq_lens, &new_lens, &table, &free_pages, &n_free, &out[0], &out[1], &out[2], &out[3], &out[4], &out[5]});
-    if (a[7] == Py_None) {                                    // one allocation: views cost less than five more
-        const std::vector<Tensor> parts = fresh(seq_lens, {2ll * max_tokens + 2 * requests + 3}, ScalarType::Int).split_with_sizes(sizes);
-        for (int i = 0; i < 6; ++i) out[i] = parts[i];
+    if (a[7] == Py_None) {
+        const Tensor whole = fresh(seq_lens, {2ll * max_tokens + 2 * requests + 3}, ScalarType::Int);
+        int64_t offset = 0;
+        for (int i = 0; i < 6; offset += sizes[i++]) out[i] = part(whole, offset, sizes[i]);
     }
     enqueue(device, "laga_cache_plan", [&](void* stream) {
         return library.cache_plan(data<int>(seq_lens), data<int>(new_lens), size32(requests, "block_table"), page_size, data<int>(table),
