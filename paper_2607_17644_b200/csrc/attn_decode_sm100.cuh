@@ -18,7 +18,11 @@
 //            product lie in lanes 32w .. 32w+15 of TMEM: sixteen heads per softmax warp, read so that all 32 threads
 //            have 32 scores each (tmem_ld_16x64)
 //   output   O^T[512 latents x heads] (+)= V^T (A, MN-major: the very same key tile) . P^T (B: the softmax's bf16 P in shared memory):
-//            the long side is the MMA's M, so few heads waste nothing and O takes 4 * kHeads TMEM columns
+//            the long side is the MMA's M, so few heads waste nothing and O takes 4 * kHeads TMEM columns.  Up to 32 heads a CTA P
+//            comes in two parts, bf16(p) and bf16(p - bf16(p)), as further columns that the drain adds up: an MMA of 128 x 32 costs
+//            its issue, as one of 128 x 16 does, and of the path's three roundings to bf16 (q W_uk, P, the result) one goes (error against
+//            float64 with 16 heads 2.5e-3 -> 2.1e-3; the result's rounding alone is 1.7e-3).  With 64 heads the columns would
+//            neither be free (the MMAs bound that case) nor fit TMEM beside the scores.
 // The tile is loaded once, in nine 64-channel slabs: the rope slab, which only the scores read, and two halves of four slabs (256
 // latents), which go around a ring with a barrier per entry, so that the next tiles' loads are in flight while this
 // tile is scored, exponentiated and multiplied.
@@ -52,7 +56,9 @@ template <int kHeads>
 struct AttnDecodeSmem {
     static constexpr int kHalves = kHeads == 16 ? 6 : kHeads == 32 ? 5 : 4;      // half tiles in the ring
     static constexpr int kQSlab = kHeads * 128;               // kHeads rows x 64 channels
-    static constexpr int kPTile = kHeads * 128;               // kHeads rows x 64 keys
+    static constexpr int kParts = kHeads <= 32 ? 2 : 1;       // P as bf16(p) and bf16(p - bf16(p)), or as bf16(p) alone
+    static constexpr int kCols = kParts * kHeads;             // rows of the P tile, and TMEM columns of 128 latents of O^T
+    static constexpr int kPTile = kCols * 128;                // kCols rows x 64 keys
     static constexpr int kSlab = kDecKeys * 128;              // 64 keys x 64 channels
     static constexpr int kHalf = 4 * kSlab;                   // 64 keys x 256 latents
     static constexpr int kQ = 0;
@@ -380,7 +386,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
     } else if (warp == kDecValueWarp) {
         // ---- issuer of the value MMAs ----------------------------------------------------------------------
         if (elect_one()) {
-            constexpr uint32_t idesc = make_idesc_bf16(128, kHeads, 1, 0);
+            constexpr uint32_t idesc = make_idesc_bf16(128, L::kCols, 1, 0);
             const uint32_t v_lo = desc_lo(desc_mn_major(smem_u32(smem + L::kHalf0), L::kSlab)), v_hi = desc_hi(desc_mn_major(0, L::kSlab)),
                            p_lo = desc_lo(desc_k_major(smem_u32(smem + L::kP))), p_hi = desc_hi(desc_k_major(0));
             uint32_t slot = 0, pieces = 0;
@@ -397,15 +403,15 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 const uint32_t b_lo = p_lo + buf * (L::kPTile / 16);
 #pragma unroll 1
                 for (uint32_t half = 0; half < 2; ++half) {
-                    const uint32_t a_lo = v_lo + slot * (L::kHalf / 16), d = tmem_base + half * (2 * kHeads);
+                    const uint32_t a_lo = v_lo + slot * (L::kHalf / 16), d = tmem_base + half * (2 * L::kCols);
                     if (k_steps == 4) {
                         mma_ss_chain4_mn_k(d, a_lo, v_hi, b_lo, p_hi, idesc, new_piece ? 0u : 1u);
-                        mma_ss_chain4_mn_k(d + kHeads, a_lo + 2 * L::kSlab / 16, v_hi, b_lo, p_hi, idesc, new_piece ? 0u : 1u);
+                        mma_ss_chain4_mn_k(d + L::kCols, a_lo + 2 * L::kSlab / 16, v_hi, b_lo, p_hi, idesc, new_piece ? 0u : 1u);
                     } else {
 #pragma unroll 1
                         for (int kk = 0; kk < 2 * k_steps; ++kk) {
                             const int u = kk >= k_steps, k = kk - u * k_steps;
-                            mma_ss(d + u * kHeads, desc_of(a_lo + u * (2 * L::kSlab / 16) + k * 128, v_hi), desc_of(b_lo + k * 2, p_hi), idesc,
+                            mma_ss(d + u * L::kCols, desc_of(a_lo + u * (2 * L::kSlab / 16) + k * 128, v_hi), desc_of(b_lo + k * 2, p_hi), idesc,
                                    (!new_piece || k > 0) ? 1u : 0u);
                         }
                     }
@@ -477,7 +483,11 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 m0 = n0; m1 = n1;
                 if (lane == 0) mbar_arrive(&a_full[buf]);
                 float s0[2] = {0.f, 0.f}, s1[2] = {0.f, 0.f};
-                uint32_t pk[16];                        // pk[2j], pk[2j+1]: columns 8j + 2(l%4), +1 of heads r0 and r1
+                // pk[2j], pk[2j+1]: columns 8j + 2(l%4), +1 of heads r0 and r1; pr: what their rounding left
+                uint32_t pk[16], pr[L::kParts == 2 ? 16 : 1];
+                auto rest = [](float a, float b, uint32_t both) {
+                    return pack_bf16x2(a - __uint_as_float(both << 16), b - __uint_as_float(both & 0xffff0000u));
+                };
                 auto exps = [&](int j) {
                     const float a0 = fast_exp2(fmaf(__uint_as_float(sv[4 * j]), args.scale_log2, -n0));
                     const float a1 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 1]), args.scale_log2, -n0));
@@ -487,6 +497,10 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                     s1[j & 1] += b0 + b1;
                     pk[2 * j] = pack_bf16x2(a0, a1);
                     pk[2 * j + 1] = pack_bf16x2(b0, b1);
+                    if constexpr (L::kParts == 2) {
+                        pr[2 * j] = rest(a0, a1, pk[2 * j]);
+                        pr[2 * j + 1] = rest(b0, b1, pk[2 * j + 1]);
+                    }
                 };
 #pragma unroll
                 for (int j = 0; j < 5; ++j) exps(j);
@@ -508,6 +522,12 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     stmatrix_x4(pbase + (((2 * j + (lane >> 4)) ^ (lane & 7)) << 4), pk[4 * j], pk[4 * j + 1], pk[4 * j + 2], pk[4 * j + 3]);
+                if constexpr (L::kParts == 2) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        stmatrix_x4(pbase + kHeads * 128 + (((2 * j + (lane >> 4)) ^ (lane & 7)) << 4), pr[4 * j], pr[4 * j + 1], pr[4 * j + 2],
+                                    pr[4 * j + 3]);
+                }
                 if (!__all_sync(0xffffffffu, told)) {
                     ok = mbar_wait_warp(&a_full[buf], par, abort_flag, args.status, 0xC4);
                     if (!ok) break;
@@ -525,7 +545,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 if (!ok) break;
                 tc_fence_after_sync();
 #pragma unroll 1
-                for (int c = 0; c < 4 * kHeads; c += 16) {
+                for (int c = 0; c < 4 * L::kCols; c += 16) {
                     const int w = (c % kHeads) >> 4;          // sixteen columns: the heads of softmax warp w
                     if ((w == 0 ? flags.x : w == 1 ? flags.y : w == 2 ? flags.z : flags.w) != tag) continue;
                     uint32_t o[16];
@@ -560,19 +580,28 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 float* dst = args.part_o + (slot * args.h_pad + head0) * kDecLat + warp * 32 + lane;
                 // (a slot past the workspace would mean that the roles disagree about the pieces)
                 const int n_heads = device_check(slot < static_cast<size_t>(args.ctas_per_group) + args.B, args.status, 0xEA0000u | cta) ? min(kHeads, args.h - head0) : 0;
-                // Columns c .. c+31 of TMEM are latents (c / kHeads) * 128 + lane of heads c % kHeads ..: a store of a warp is 128 bytes of one
+                // Columns c .. c+31 of TMEM are latents (c / kCols) * 128 + lane of heads c % kHeads ..: a store of a warp is 128 bytes of one
                 // head's row.  The accumulator is up to 256 columns and nothing else of the CTA moves meanwhile, so the loop is
-                // unrolled (constant offsets) and the next columns are on their way while these are stored.
-                uint32_t o[2][32];
-                tmem_ld_x32(tmem_base + lane_addr, o[0]);
+                // unrolled (constant offsets) and the next columns are on their way while these are stored.  A step holds all parts
+                // of its values: 32 columns, or with 32 heads twice that.
+                constexpr int kStep = kHeads == 32 ? 64 : 32;
+                uint32_t o[2][kStep];
+                auto load = [&](int c, uint32_t* r) {
 #pragma unroll
-                for (int c = 0; c < 4 * kHeads; c += 32) {
+                    for (int k = 0; k < kStep; k += 32) tmem_ld_x32(tmem_base + lane_addr + c + k, r + k);
+                };
+                load(0, o[0]);
+#pragma unroll
+                for (int c = 0; c < 4 * L::kCols; c += kStep) {
                     tmem_ld_wait();
-                    if (c + 32 < 4 * kHeads) tmem_ld_x32(tmem_base + lane_addr + c + 32, o[(c / 32 + 1) & 1]);
+                    if (c + kStep < 4 * L::kCols) load(c + kStep, o[(c / kStep + 1) & 1]);
+                    const uint32_t* r = o[(c / kStep) & 1];
 #pragma unroll
-                    for (int v = 0; v < 32; ++v) {
-                        const int head = (c + v) % kHeads, latent = (c + v) / kHeads * 128;
-                        if (head < n_heads) dst[head * kDecLat + latent] = __uint_as_float(o[(c / 32) & 1][v]);
+                    for (int v = 0; v < kStep / L::kParts; ++v) {
+                        const int head = (c + v) % kHeads, latent = (c + v) / L::kCols * 128;
+                        float x = __uint_as_float(r[v]);
+                        if constexpr (L::kParts == 2) x += __uint_as_float(r[v + kHeads]);
+                        if (head < n_heads) dst[head * kDecLat + latent] = x;
                     }
                 }
                 if (softmax_warp && n_heads > 0) {
