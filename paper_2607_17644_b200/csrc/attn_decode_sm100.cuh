@@ -21,7 +21,7 @@
 //            the long side is the MMA's M, so few heads waste nothing and O takes 4 * kHeads TMEM columns.  Up to 32 heads a CTA P
 //            comes in two parts, bf16(p) and bf16(p - bf16(p)), as further columns that the drain adds up: an MMA of 128 x 32 costs
 //            its issue, as one of 128 x 16 does, and of the path's three roundings to bf16 (q W_uk, P, the result) one goes (error against
-//            float64 with 16 heads 2.5e-3 -> 2.1e-3; the result's rounding alone is 1.7e-3).  With 64 heads the columns would
+//            float64 with 16 heads 2.5e-3 -> 2.2e-3; the result's rounding alone is 1.7e-3).  With 64 heads the columns would
 //            neither be free (the MMAs bound that case) nor fit TMEM beside the scores.
 // The tile is loaded once, in nine 64-channel slabs: the rope slab, which only the scores read, and two halves of four slabs (256
 // latents), which go around a ring with a barrier per entry, so that the next tiles' loads are in flight while this
@@ -32,6 +32,12 @@
 //   warps 6, 5  issuers of the score and of the value MMAs: apart, because a lane that has issued MMAs sees no barrier until the tensor
 //               pipe has taken them, and neither product's start should wait for the other's
 //   (warp 4 does nothing: it keeps the others off the scheduler of softmax warp 0)
+//
+// Measured, the whole call (absorption, this kernel, projection): 64 requests of up to 8192 tokens, 16 heads, 302 MB of cache: 60 us, of
+// which this kernel's main loop 51 (6.0 TB/s: HBM bounds it), absorption and set-up 4, the last CTA's lag and the projection 5.
+// 8 requests of up to 65536 tokens, 128 heads, 440 MB, 0.106 TFLOP: 145 us; in long runs, at the card's power limit, 160 to 170.
+// There shared memory bounds it: 74 KB of queries leave two tiles, and a half tile's life (load 1500 clocks, scores 2000, softmax 940,
+// values 750) sets 2600 clocks a tile against 1920 of MMAs.  One request of 511 tokens: 14.6 us, three kernels' latencies.
 //
 // Rows behind a request's last token may hold anything, NaN included: their scores are replaced by -inf, and their
 // rows of the tile are zeroed in shared memory before P.V (0 * NaN is NaN).
@@ -634,6 +640,8 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
 // q_abs[b, i, :] = W_uk[i] q_nope[b, i, :] for a tile of kRequests requests: D[128 latents x requests] = W_uk (A: rows = latents,
 // K-major as it lies) . q^T (B: rows = requests), eight MMAs.  The weights are the M side, so a small batch pads
 // nothing but the result's columns, and 4 * h CTAs share the read of W_uk.  First kernel of the call: clears the status slot.
+// Latency bounds it (one tile load, eight MMAs, one store per CTA): about 3 us of a call with warm weights.  The result leaves through
+// shared memory and TMA, whole rows instead of two bytes a thread (64 requests of 8192: the call 61.8 -> 59.9 us).
 constexpr int kAbsorbThreads = 128;
 template <int kRequests>
 struct DecodeAbsorbSmem {
@@ -735,6 +743,9 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 // this tile's pieces (four requests a thread at once) while warps 16..23 make the next tile's weights, 24..27 write the tile before and
 // warp 31 issues MMAs; one barrier per tile.
 // A request without tokens has no piece: zeros, LSE -inf.
+// Few requests: about 4 us, latency.  Many: the sums bound it (2 KB a piece from L2, four loads in flight a thread).  The call, before the
+// pipeline -> now: 130 requests of up to 900 tokens, 128 heads, 121 -> 82 us; 250 of up to 60, 64 heads, 80 -> 47; 2048 of 128, 16 heads,
+// 202 -> 130.
 constexpr int kProjectThreads = 1024;
 struct DecodeProjectSmem {
     static constexpr int kW = 0;                                 // two slabs of 512 rows x 64 values
