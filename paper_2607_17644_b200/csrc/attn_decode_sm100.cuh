@@ -29,9 +29,10 @@
 //
 //   warps 0..3  softmax (16 heads per warp), rescaling of O^T when a running maximum moved by more than 2^8, drain
 //   warp 7      TMA producer (page table entries are fetched ahead of their use)
+//   warp 4      fetches the first queries, beside the producer's way to the first tile (lengths, page table); then it is done, and keeps
+//               the others off the scheduler of softmax warp 0
 //   warps 6, 5  issuers of the score and of the value MMAs: apart, because a lane that has issued MMAs sees no barrier until the tensor
 //               pipe has taken them, and neither product's start should wait for the other's
-//   (warp 4 does nothing: it keeps the others off the scheduler of softmax warp 0)
 //
 // Measured, the whole call (absorption, this kernel, projection): 64 requests of up to 8192 tokens, 16 heads, 302 MB of cache: 60 us, of
 // which this kernel's main loop 51 (6.0 TB/s: HBM bounds it), absorption and set-up 4, the last CTA's lag and the projection 5.
@@ -49,8 +50,8 @@
 
 namespace laga {
 
-constexpr int kDecThreads = 256;            // (warp 4 idles: see the roles)
-constexpr int kDecProducerWarp = 7, kDecScoreWarp = 6, kDecValueWarp = 5;
+constexpr int kDecThreads = 256;
+constexpr int kDecProducerWarp = 7, kDecScoreWarp = 6, kDecValueWarp = 5, kDecQueryWarp = 4;
 constexpr int kDecKeys = 64;
 constexpr int kDecMaxCtas = 148;             // CTAs over all head groups (the workspace is sized by it)
 constexpr int kDecRow = 576;                 // channels of a cached token
@@ -179,7 +180,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
     grid_launch_dependents();
     // Launched to overlap decode_absorb_kernel, the only kernel of the call before this one, which itself starts after everything
     // earlier on the stream.  Only the absorbed queries (and the status word, which it clears) are its work: lengths, page
-    // table and cache are read at once, and the producer alone waits, before it fetches its first queries.
+    // table and cache are read at once, and only who fetches queries waits for it first.
     // All 512 columns are this CTA's, so they start at column 0: an immediate in every MMA (checked, not trusted).
     constexpr uint32_t tmem_base = 0, tmem_s = 256;
     if (threadIdx.x == 0 && (abort_flag->value != 0u || *tmem_slot != tmem_base)) {
@@ -220,6 +221,15 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
     }
     const int first_b = *start_b, first_t = *start_t;
 
+    auto fetch_queries = [&](int b) {
+        grid_dependency_wait();                              // (returns at once after the first time)
+        mbar_arrive_expect_tx(q_full, 9 * L::kQSlab);
+        uint8_t* dst = smem + L::kQ;
+        tma_load_2d_chk(args.status, dst, &tmap_q, q_full, 128, b * args.h + head0);          // rope band first
+        for (int k = 0; k < 8; ++k)
+            tma_load_2d_chk(args.status, dst + (1 + k) * L::kQSlab, &tmap_qabs, q_full, k * 64, b * args.h + head0);
+    };
+
     if (abort_flag->value != 0u || my_tiles <= 0) {
         // nothing to do (or nothing may be done): fall through to the common exit
     } else if (warp == kDecProducerWarp) {
@@ -237,14 +247,9 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
             return (page << args.page_shift) + (key & ((1 << args.page_shift) - 1));
         };
         auto load_queries = [&](const DecodeCursor& c, uint32_t piece, ArmedBarriers& armed) -> bool {
-            if (!mbar_wait(q_empty, (piece & 1u) ^ 1u, abort_flag, args.status, 0xB0)) return false;
-            grid_dependency_wait();                  // (returns at once after the first time)
-            mbar_arrive_expect_tx(q_full, 9 * L::kQSlab);
+            if (piece > 0 && !mbar_wait(q_empty, (piece & 1u) ^ 1u, abort_flag, args.status, 0xB0)) return false;
             armed.arm(q_full, piece);
-            uint8_t* dst = smem + L::kQ;
-            tma_load_2d_chk(args.status, dst, &tmap_q, q_full, 128, c.b * args.h + head0);          // rope band first
-            for (int k = 0; k < 8; ++k)
-                tma_load_2d_chk(args.status, dst + (1 + k) * L::kQSlab, &tmap_qabs, q_full, k * 64, c.b * args.h + head0);
+            if (piece > 0) fetch_queries(c.b);               // (the first are the query warp's)
             return true;
         };
         uint32_t slot = 0, par = 0, r_par = 0, pieces = 0;
@@ -274,7 +279,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                         tma_load_3d_chk(args.status, smem + L::kHalf0 + slot * L::kHalf, &tmap_lat, &h_full[slot], 0, row, half * 4, once);
                         if (++slot == L::kHalves) { slot = 0; par ^= 1u; }
                     }
-                    // a piece's queries after its first tile: they wait for the last scores of the piece before (and, once, for the absorption)
+                    // a piece's queries after its first tile: they wait for the last scores of the piece before
                     if (ok && new_piece) ok = load_queries(cur, pieces++, armed);
                     if (!ok) break;
                     new_piece = cur.ends_piece();
@@ -340,6 +345,8 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
             __syncwarp();
             if (lane == 0 && abort_flag->value != 0u) armed.quiesce();
         }
+    } else if (warp == kDecQueryWarp) {
+        if (elect_one()) fetch_queries(first_b);             // (the first request with tokens at or behind first_b is first_b: a tile of it is here)
     } else if (warp == kDecScoreWarp) {
         // ---- issuer of the score MMAs ----------------------------------------------------------------------
         if (elect_one()) {
@@ -900,16 +907,18 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
     };
     const size_t step = static_cast<size_t>(h_pad) * (kDecLat / 4);
     auto sum_pieces = [&](auto each, const Tile& t, int buf) {
-        constexpr int kEach = decltype(each)::value, kGroups = 16 / kEach;
+        constexpr int kEach = decltype(each)::value, kGroups = 16 / kEach, kLogGroups = kEach == 4 ? 2 : 3;
+        constexpr bool kFew = kEach == 2;                    // a CTA's only tile: the weights are made here, under the first pieces' loads
         const float2* weights = reinterpret_cast<const float2*>(smem + L::kWeights) + buf * L::kMaxPieces;
-        const int split = t.n_req == 1 ? kGroups : t.n_req == 2 ? kGroups / 2 : t.n_req <= kGroups / 2 ? kGroups / 4 : 1;
+        const int log_split = t.n_req == 1 ? kLogGroups : t.n_req == 2 ? kLogGroups - 1 : t.n_req <= kGroups / 2 ? kLogGroups - 2 : 0;
+        const int split = 1 << log_split, share = group & (split - 1);
         const float4* o[kEach];
         const float2* w[kEach];
         int n[kEach], most = 0;
         float4 acc[kEach];
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const int r = group / split + k * kGroups, at = r & 15;            // (k > 0 only where split is 1)
+            const int r = (group >> log_split) + k * kGroups, at = r & 15;     // (k > 0 only where split is 1)
             const bool in = r < t.n_req && (k == 0 || split == 1);
             const int4 p = t.pieces[at];
             o[k] = reinterpret_cast<const float4*>(part_o + (static_cast<size_t>(p.x + t.b0 + at) * h_pad + head) * kDecLat) + cg;
@@ -918,9 +927,27 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
             most = max(most, n[k]);
             acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
+        // two pieces: the first of each request where split is 1, this group's first two of its request otherwise
+        float4 ahead[kFew ? kEach : 1];
+        if constexpr (kFew) {
+            const bool whole = split == 1;
+            const int at0 = whole ? 0 : share, at1 = whole ? 0 : share + split;
+            const bool has0 = at0 < n[0], has1 = at1 < (whole ? n[1] : n[0]);
+            if (has0) ahead[0] = o[0][at0 * step];
+            if (has1) ahead[1] = (whole ? o[1] : o[0])[at1 * step];
+            make_weights(t, buf);
+            __syncthreads();
+            const float w0 = has0 ? w[0][at0].x : 0.f, w1 = has1 ? (whole ? w[1] : w[0])[at1].x : 0.f;
+            if (has0) acc[0] = make_float4(ahead[0].x * w0, ahead[0].y * w0, ahead[0].z * w0, ahead[0].w * w0);
+            if (has1) {
+                const float4 x = make_float4(ahead[1].x * w1, ahead[1].y * w1, ahead[1].z * w1, ahead[1].w * w1);
+                if (whole) acc[1] = x;
+                else acc[0] = make_float4(acc[0].x + x.x, acc[0].y + x.y, acc[0].z + x.z, acc[0].w + x.w);
+            }
+        }
         if (split == 1) {
 #pragma unroll 2
-            for (int c = 0; c < most; ++c)
+            for (int c = kFew ? 1 : 0; c < most; ++c)
 #pragma unroll
                 for (int k = 0; k < kEach; ++k)
                     if (c < n[k]) {
@@ -931,7 +958,7 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
                     }
         } else {
 #pragma unroll 8
-            for (int c = group % split; c < n[0]; c += split) {
+            for (int c = share + (kFew ? kEach * split : 0); c < n[0]; c += split) {
                 const float4 x = o[0][c * step];
                 const float wc = w[0][c].x;
                 acc[0].x = fmaf(x.x, wc, acc[0].x); acc[0].y = fmaf(x.y, wc, acc[0].y);
@@ -941,14 +968,14 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
             asm volatile("bar.sync 1, %0;" ::"n"(kGroups * 128) : "memory");   // the summing warps; none of them ever leaves early
             acc[0] = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < split; ++k) {
-                const float4 x = reinterpret_cast<const float4*>(red)[(group / split * split + k) * 128 + cg];
+                const float4 x = reinterpret_cast<const float4*>(red)[(group - share + k) * 128 + cg];
                 acc[0].x += x.x; acc[0].y += x.y; acc[0].z += x.z; acc[0].w += x.w;
             }
         }
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const int r = group / split + k * kGroups;
-            if (r < t.n_req && group % split == 0 && (k == 0 || split == 1)) store_row(buf, r, acc[k]);
+            const int r = (group >> log_split) + k * kGroups;
+            if (r < t.n_req && share == 0 && (k == 0 || split == 1)) store_row(buf, r, acc[k]);
         }
     };
     auto write_out = [&](int b0, int n_req, int buf) {           // warps 24..27: D of a tile whose MMAs have completed
@@ -973,8 +1000,10 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
     __syncthreads();
     grid_dependency_wait();
     if (my_tiles > 0) {
-        make_weights(tile_at(0), 0);
-        __syncthreads();
+        if (pipelined) {
+            make_weights(tile_at(0), 0);
+            __syncthreads();
+        }
         for (int i = 0; i < my_tiles; ++i) {
             const int buf = i & 1;
             const Tile t = tile_at(i);
