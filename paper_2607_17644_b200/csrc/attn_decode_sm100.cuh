@@ -29,8 +29,8 @@
 //
 //   warps 0..3  softmax (16 heads per warp), rescaling of O^T when a running maximum moved by more than 2^8, drain
 //   warp 7      TMA producer (page table entries are fetched ahead of their use)
-//   warp 4      fetches the first queries, beside the producer's way to the first tile (lengths, page table); then it is done, and keeps
-//               the others off the scheduler of softmax warp 0
+//   warp 4      fetches the first queries, beside the producer's way to the first tile (lengths, page table; one request of 511 tokens:
+//               the call 14.6 -> 13.7 us); then it is done, and keeps the others off the scheduler of softmax warp 0
 //   warps 6, 5  issuers of the score and of the value MMAs: apart, because a lane that has issued MMAs sees no barrier until the tensor
 //               pipe has taken them, and neither product's start should wait for the other's
 //
@@ -38,7 +38,7 @@
 // which this kernel's main loop 51 (6.0 TB/s: HBM bounds it), absorption and set-up 4, the last CTA's lag and the projection 5.
 // 8 requests of up to 65536 tokens, 128 heads, 440 MB, 0.106 TFLOP: 145 us; in long runs, at the card's power limit, 160 to 170.
 // There shared memory bounds it: 74 KB of queries leave two tiles, and a half tile's life (load 1500 clocks, scores 2000, softmax 940,
-// values 750) sets 2600 clocks a tile against 1920 of MMAs.  One request of 511 tokens: 14.6 us, three kernels' latencies.
+// values 750) sets 2600 clocks a tile against 1920 of MMAs.  One request of 511 tokens: 13.4 us, three kernels' latencies.
 //
 // Rows behind a request's last token may hold anything, NaN included: their scores are replaced by -inf, and their
 // rows of the tile are zeroed in shared memory before P.V (0 * NaN is NaN).
@@ -750,8 +750,9 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 // this tile's pieces (four requests a thread at once) while warps 16..23 make the next tile's weights, 24..27 write the tile before and
 // warp 31 issues MMAs; one barrier per tile.
 // A request without tokens has no piece: zeros, LSE -inf.
-// Few requests: about 4 us, latency.  Many: the sums bound it (2 KB a piece from L2, four loads in flight a thread).  The call, before the
-// pipeline -> now: 130 requests of up to 900 tokens, 128 heads, 121 -> 82 us; 250 of up to 60, 64 heads, 80 -> 47; 2048 of 128, 16 heads,
+// Few requests: about 4 us, latency; the first pieces are read while their weights are made (one request of 511 tokens: the call 13.7 ->
+// 13.4 us).  Many: the sums bound it (2 KB a piece from L2, four loads in flight a thread).  The call, before the
+// pipeline -> now: 130 requests of up to 900 tokens, 128 heads, 121 -> 82 us; 250 of up to 60, 64 heads, 80 -> 45; 2048 of 128, 16 heads,
 // 202 -> 130.
 constexpr int kProjectThreads = 1024;
 struct DecodeProjectSmem {
