@@ -201,3 +201,32 @@ def test_empty_batches(laga):
     assert latent.shape == (0, 512) and k_pe.shape == (0, 64)
     dkv, dgamma, dbeta = laga.latent_norm_rope_backward(latent, k_pe, kv, gamma, mean, rstd, none, rope)
     assert dkv.shape == (0, 576) and not dgamma.any() and not dbeta.any()
+
+
+def test_given_buffers_come_back_and_plans_are_checked(laga):
+    plan = laga.rope_plan(64)
+    x, pos = torch.randn(5, 2, 192, device="cuda").to(BF16), torch.arange(5, dtype=torch.int32, device="cuda")
+    y = torch.empty_like(x)
+    assert laga.rope(x, pos, plan, y=y) is y and torch.equal(laga.rope(x, pos, plan), y)
+    assert laga.rope(x, pos, plan, y=x) is x and torch.equal(x, y)
+    for wrong in ((plan.freqs, 1.0), plan.freqs, None):
+        with pytest.raises(TypeError):
+            laga.rope(x, pos, wrong)
+    for freqs in (plan.freqs.float(), plan.freqs.cpu(), plan.freqs.repeat(2)[::2]):
+        with pytest.raises(ValueError):
+            laga.rope(x, pos, laga.RopePlan(freqs))
+    for positions in (pos.long(), pos[:4], pos.cpu()):
+        with pytest.raises(ValueError):
+            laga.rope(x, positions, plan)
+    with pytest.raises(ValueError):
+        laga.rope(x, pos, plan, y=y[:4])
+    with pytest.raises(laga.LagaError):
+        laga.rope(x, pos, plan, rot_begin=136)
+    kv, gamma = torch.randn(5, 576, device="cuda").to(BF16), torch.ones(512, dtype=BF16, device="cuda")
+    latent, k_pe = torch.empty(5, 512, dtype=BF16, device="cuda"), torch.empty(5, 64, dtype=BF16, device="cuda")
+    out = laga.latent_norm_rope(kv, gamma, None, pos, plan, latent=latent, k_pe=k_pe)
+    assert out[0] is latent and out[1] is k_pe and out[2].shape == out[3].shape == (5,)
+    with pytest.raises(laga.LagaError):                              # an output over another
+        laga.latent_norm_rope(kv, gamma, None, pos, plan, latent=latent, k_pe=latent.view(-1)[:320].view(5, 64))
+    with pytest.raises(ValueError):
+        laga.latent_norm_rope(kv, gamma[:504], None, pos, plan)

@@ -152,6 +152,20 @@ def test_binding_refuses_cpu_tensors_and_wrong_types(laga):
         laga.paged_decode(x, torch.zeros(512, 512, dtype=torch.bfloat16), torch.zeros(2, 64, 576, dtype=torch.bfloat16), i.view(4, 1), i)
 
 
+def test_binding_refuses_what_is_no_tensor_or_no_plan(laga):
+    rope = laga.rope_plan(64, device="cpu")
+    x, i = torch.zeros(4, 2, 192, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: laga.rope(None, i, rope), lambda: laga.rope(x.tolist(), i, rope), lambda: laga.latent_norm_rope(x, x, 3, i, rope),
+                 lambda: laga.cache_append(x, None, None, i, rope, i, x), lambda: laga.paged_decode(x, x, x, None, i),
+                 lambda: laga.cache_plan(i, i, None, i, i, 64, 4)):
+        with pytest.raises(TypeError):
+            call()
+    from paper_2607_17644_b200 import _binding
+    for entry in ("rope", "latent_norm_rope", "latent_norm_rope_backward", "cache_plan", "paged_decode", "bind"):
+        with pytest.raises(TypeError):
+            getattr(_binding, entry)(x)
+
+
 def test_rope_plan_frequencies(laga):
     j = torch.arange(32, dtype=torch.float64)
     plain = laga.rope_plan(64, device="cpu")
