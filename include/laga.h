@@ -273,8 +273,8 @@ int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, in
  *                token included, once it has been appended); token t of request b is row t % page_size of page
  *                block_table[b, t / page_size].  Requests may share pages.  Table entries behind a request's last page and cache
  *                rows behind its last token are not used, whatever they hold.
- *   out          bf16 [B, h, d_v] written; a request of length 0 gets zeros
- *   lse          fp32 [B, h] written if not NULL (-inf for length 0)
+ *   out          bf16 [B, h, d_v] written; a request of length 0, or whose every score is -inf, gets zeros
+ *   lse          fp32 [B, h] written if not NULL (-inf for those)
  * Outputs and the workspace must not overlap inputs or one another (LAGA_ERR_INVALID_ARG).
  * A length outside [0, columns * page_size] is clamped, and a page number outside [0, n_pages) reads as zeros; both report
  * LAGA_ERR_DEVICE_CHECK through laga_query_status(workspace).  page_size: a power of two from 16 to 1024; n_pages * page_size

@@ -749,7 +749,7 @@ decode_absorb_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_co
 // With few requests a CTA has one tile, all of this is latency, and all warps sum pieces.  With many it is a pipeline: warps 0..15 sum
 // this tile's pieces (four requests a thread at once) while warps 16..23 make the next tile's weights, 24..27 write the tile before and
 // warp 31 issues MMAs; one barrier per tile.
-// A request without tokens has no piece: zeros, LSE -inf.
+// A request without tokens has no piece, and one whose every score is -inf has sums of 0: zeros, LSE -inf.
 // Few requests: about 4 us, latency; the first pieces are read while their weights are made (one request of 511 tokens: the call 13.7 ->
 // 13.4 us).  Many: the sums bound it (2 KB a piece from L2, four loads in flight a thread).  The call, before the
 // pipeline -> now: 130 requests of up to 900 tokens, 128 heads, 121 -> 82 us; 250 of up to 60, 64 heads, 80 -> 45; 2048 of 128, 16 heads,
@@ -887,7 +887,7 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
         }
 #pragma unroll
         for (int d = 8; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-        const float inv = 1.0f / l;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;             // (nothing left: every score was -inf; a NaN stays one)
         for (int c = q; c < n; c += 16) weights[c].x *= inv;
         if (lse != nullptr && q == 0 && r < t.n_req)
             lse[static_cast<size_t>(t.b0 + r) * h + head] = n > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
