@@ -56,7 +56,7 @@ constexpr int kDecKeys = 64;
 constexpr int kDecMaxCtas = 148;             // CTAs over all head groups (the workspace is sized by it)
 constexpr int kDecRow = 576;                 // channels of a cached token
 constexpr int kDecLat = 512;
-constexpr float kDecLowest = -3.0e38f;
+constexpr float kDecLowest = -3.402823466e38f;      // the lowest fp32 number
 
 // Shared memory for kHeads heads per CTA: what the queries and P leave holds the tiles, 3, 2.5 or 2 of them.
 template <int kHeads>
@@ -446,7 +446,7 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
         const int r0 = warp * 16 + (lane >> 2), r1 = r0 + 8;   // heads within the group
         const bool live0 = head0 + r0 < args.h, live1 = head0 + r1 < args.h;
         const uint32_t lane_addr = static_cast<uint32_t>(warp * 32) << 16;
-        // running maxima (log2 domain) and this thread's part of the sums; a maximum starts just above the lowest number, not at -inf, so
+        // running maxima (log2 domain) and this thread's part of the sums; a maximum starts at the lowest number, not at -inf, so
         // that keys whose score is -inf weigh exp2(-inf) = 0 even where there is nothing else yet (-inf - -inf is NaN)
         float m0 = kDecLowest, m1 = kDecLowest, l0 = 0.f, l1 = 0.f;
         uint32_t T = 0, pieces = 0;
@@ -501,11 +501,13 @@ attn_decode_sm100_kernel(const __grid_constant__ CUtensorMap tmap_qabs, const __
                 auto rest = [](float a, float b, uint32_t both) {
                     return pack_bf16x2(a - __uint_as_float(both << 16), b - __uint_as_float(both & 0xffff0000u));
                 };
+                // The product is rounded as the maximum's was, not fused with the subtraction: the largest score's exponent is then 0 whatever its
+                // size (fused, it is the maximum's rounding: 1e30 where every score is near the lowest number).
                 auto exps = [&](int j) {
-                    const float a0 = fast_exp2(fmaf(__uint_as_float(sv[4 * j]), args.scale_log2, -n0));
-                    const float a1 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 1]), args.scale_log2, -n0));
-                    const float b0 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 2]), args.scale_log2, -n1));
-                    const float b1 = fast_exp2(fmaf(__uint_as_float(sv[4 * j + 3]), args.scale_log2, -n1));
+                    const float a0 = fast_exp2(__fmul_rn(__uint_as_float(sv[4 * j]), args.scale_log2) - n0);
+                    const float a1 = fast_exp2(__fmul_rn(__uint_as_float(sv[4 * j + 1]), args.scale_log2) - n0);
+                    const float b0 = fast_exp2(__fmul_rn(__uint_as_float(sv[4 * j + 2]), args.scale_log2) - n1);
+                    const float b1 = fast_exp2(__fmul_rn(__uint_as_float(sv[4 * j + 3]), args.scale_log2) - n1);
                     s0[j & 1] += a0 + a1;
                     s1[j & 1] += b0 + b1;
                     pk[2 * j] = pack_bf16x2(a0, a1);
