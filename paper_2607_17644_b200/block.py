@@ -110,13 +110,16 @@ class LagaBlock(torch.nn.Module):
     """hidden [S, d_model] -> [S, d_model]: Algorithm 1 with P = 1 for ``n_heads`` heads of the DeepSeek-V3
     geometry (d_nope 128, d_rope 64, d_v 128, d_c 512).  ``forward(hidden, cu_seqlens=None)``: with
     ``cu_seqlens`` the rows are packed sequences and attention stays inside each.  ``rope``: the rotation of the rope bands
-    (``laga.rope_plan``); None takes them as the projections deliver them, and the block then has no prefill / decode."""
+    (``laga.rope_plan``); None takes them as the projections deliver them, and the block then has no prefill / decode.
+    ``softmax_scale``: the factor on the scores in training and service (default 192^-0.5).  YaRN's factor is one on whole scores, and a
+    plan's mscale reaches the 64 rotated channels of the 192 alone: with it give the plan mscale_weight 0 and the block
+    192^-0.5 * (0.1 ln(factor) + 1)^2."""
 
     D_NOPE, D_ROPE, D_V, D_C = 128, 64, 128, 512
 
-    def __init__(self, d_model: int, n_heads: int, eps: float = 1e-5, device="cuda", seed: int = 0, rope=None):
+    def __init__(self, d_model: int, n_heads: int, eps: float = 1e-5, device="cuda", seed: int = 0, rope=None, softmax_scale=None):
         super().__init__()
-        self.rope = rope
+        self.rope, self.softmax_scale = rope, softmax_scale
         g = torch.Generator().manual_seed(seed)
 
         def weight(k, n):     # variance-preserving draw, rounded once to bf16
@@ -157,7 +160,8 @@ class LagaBlock(torch.nn.Module):
         if self.rope is not None and positions is None:
             positions = self.positions(S, cu_seqlens, hidden.device)
         q, latent, k_pe = self._project(hidden, positions)                                        # step 1
-        out = laga_attention(q, latent, k_pe, self.w_kv_b, causal=causal, cu_seqlens=cu_seqlens)   # steps 4-5
+        out = laga_attention(q, latent, k_pe, self.w_kv_b, causal=causal, softmax_scale=self.softmax_scale,
+                             cu_seqlens=cu_seqlens)                                               # steps 4-5
         return linear(out.reshape(S, self.n_heads * self.D_V), self.w_o)                          # step 7
 
     def _service(self):
@@ -176,7 +180,7 @@ class LagaBlock(torch.nn.Module):
         positions, slots = step.positions[:T], step.slots[:T]
         laga.rope(q, positions, self.rope, y=q)
         latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
-        out = laga.fwd(q, latent, k_pe, self.w_kv_b, cu_seqlens=cu_seqlens)[0]
+        out = laga.fwd(q, latent, k_pe, self.w_kv_b, softmax_scale=self.softmax_scale, cu_seqlens=cu_seqlens)[0]
         return laga.linear(out.view(T, self.n_heads * self.D_V), self.w_o)[0]
 
     @torch.no_grad()
@@ -196,5 +200,5 @@ class LagaBlock(torch.nn.Module):
             block_table, lens = block_table.index_select(0, requests), lens.index_select(0, requests)
         laga.rope(q, positions, self.rope, y=q)
         laga.cache_append(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, slots, pages, eps=self.eps)
-        out = laga.paged_decode(q, self.w_kv_b, pages, block_table, lens, workspace=workspace)[0]
+        out = laga.paged_decode(q, self.w_kv_b, pages, block_table, lens, softmax_scale=self.softmax_scale, workspace=workspace)[0]
         return laga.linear(out.view(B, self.n_heads * self.D_V), self.w_o)[0]

@@ -441,7 +441,8 @@ def rope_plan(d_rot=64, base=10000.0, scaling=None, interleaved=True, device="cu
       ntk     base multiplied by factor^(d_rot / (d_rot - 2)): the slowest pair is divided by factor, the fastest kept
       yarn    pairs that turn at most beta_slow (1) times within original_length (4096) positions are divided by factor, those
               that turn at least beta_fast (32) times are kept, with a linear ramp between (YaRN, arXiv:2309.00071);
-              mscale = 0.1 * mscale_weight (1) * ln(factor) + 1 multiplies cos and sin."""
+              mscale = 0.1 * mscale_weight (1) * ln(factor) + 1 multiplies cos and sin.  Where only part of a head is rotated that reaches
+              only that part of a score: mscale_weight 0 here and (0.1 ln(factor) + 1)^2 on the softmax scale reach all of it."""
     if d_rot < 4 or d_rot % 2 or not base > 1:
         raise ValueError(f"rope_plan: d_rot must be even and at least 4 and base above 1, got {d_rot}, {base}")
     j = torch.arange(d_rot // 2, dtype=torch.float64)
