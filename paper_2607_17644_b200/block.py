@@ -169,10 +169,11 @@ class LagaBlock(torch.nn.Module):
             raise ValueError("prefill and decode need the block's rotation: LagaBlock(..., rope=laga.rope_plan(64))")
 
     @torch.no_grad()
-    def prefill(self, hidden: torch.Tensor, pages: torch.Tensor, step, cu_seqlens) -> torch.Tensor:
+    def prefill(self, hidden: torch.Tensor, pages: torch.Tensor, step, cu_seqlens, workspace=None) -> torch.Tensor:
         """Prompts of requests that have nothing in the cache yet, packed: hidden [T, d_model], cu_seqlens their host
         boundaries (the same lengths that ``step``, a plan of ``LatentCache.plan``, was made for), pages one layer's
-        cache [n_pages, page_size, 576].  Returns the block's output [T, d_model]; the cache holds the prompts afterwards."""
+        cache [n_pages, page_size, 576].  Returns the block's output [T, d_model]; the cache holds the prompts afterwards.
+        workspace (``laga.fwd_varlen_workspace_bytes``): give one to have the attention's status, as for ``decode``."""
         self._service()
         T = hidden.shape[0]
         q = laga.linear(hidden, self.w_q)[0].view(T, self.n_heads, self.D_NOPE + self.D_ROPE)
@@ -180,7 +181,7 @@ class LagaBlock(torch.nn.Module):
         positions, slots = step.positions[:T], step.slots[:T]
         laga.rope(q, positions, self.rope, y=q)
         latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
-        out = laga.fwd(q, latent, k_pe, self.w_kv_b, softmax_scale=self.softmax_scale, cu_seqlens=cu_seqlens)[0]
+        out = laga.fwd(q, latent, k_pe, self.w_kv_b, softmax_scale=self.softmax_scale, workspace=workspace, cu_seqlens=cu_seqlens)[0]
         return laga.linear(out.view(T, self.n_heads * self.D_V), self.w_o)[0]
 
     @torch.no_grad()
@@ -190,7 +191,9 @@ class LagaBlock(torch.nn.Module):
         device, ascending) names them; rows of ``hidden`` behind the plan's tokens are padding (any request's number, results to be
         ignored).  Appends the tokens' latents and keys to ``pages`` and attends to each request's
         whole cache, the new token included.  Every call reads lengths and tables on the device, so a step can be captured in a
-        graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``) and replayed."""
+        graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``) and replayed.  A page number outside the cache or a
+        length outside the table shows only in the workspace's status: give one, and ``laga.check_status(workspace)`` raises
+        (with no workspace given, nothing of it is left to ask)."""
         self._service()
         B = hidden.shape[0]
         q = laga.linear(hidden, self.w_q)[0].view(B, self.n_heads, self.D_NOPE + self.D_ROPE)
