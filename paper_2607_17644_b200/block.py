@@ -168,19 +168,36 @@ class LagaBlock(torch.nn.Module):
         if self.rope is None:
             raise ValueError("prefill and decode need the block's rotation: LagaBlock(..., rope=laga.rope_plan(64))")
 
+    @staticmethod
+    def _not_these_prompts(step, positions, cu_seqlens) -> torch.Tensor:
+        """A truth value on the device: the plan is not one of prompts with these boundaries from position 0 on (rows behind its last
+        token are padding).  Where it is not, the plan's status says so (detail 0x50000005)."""
+        row = wanted = torch.arange(positions.numel(), dtype=torch.int32, device=positions.device)
+        n_tokens = step.cu_new_lens[-1]
+        if cu_seqlens is not None:
+            cu = torch.as_tensor(cu_seqlens, dtype=torch.int32).to(positions.device, non_blocking=True)
+            wanted = row - cu[torch.searchsorted(cu, row, right=True) - 1]
+        refused = ((positions != wanted) & (row < n_tokens)).any() | (n_tokens > positions.numel()) | (step.status[0] != 0)
+        step.status.masked_fill_(refused & (step.status == 0), 0x50000005)
+        return refused
+
     @torch.no_grad()
     def prefill(self, hidden: torch.Tensor, pages: torch.Tensor, step, cu_seqlens, workspace=None) -> torch.Tensor:
         """Prompts of requests that have nothing in the cache yet, packed: hidden [T, d_model], cu_seqlens their host
         boundaries (the same lengths that ``step``, a plan of ``LatentCache.plan``, was made for), pages one layer's
         cache [n_pages, page_size, 576].  Returns the block's output [T, d_model]; the cache holds the prompts afterwards.
-        workspace (``laga.fwd_varlen_workspace_bytes``): give one to have the attention's status, as for ``decode``."""
+        workspace (``laga.fwd_varlen_workspace_bytes``): give one to have the attention's status, as for ``decode``.
+        A step that is not that -- a request held tokens already, other lengths, a plan that could not be placed -- is refused on the
+        device: nothing enters the cache, the output is NaN, and ``laga.check_status(step.status)`` raises LAGA_ERR_CACHE_PLAN."""
         self._service()
         T = hidden.shape[0]
         q = laga.linear(hidden, self.w_q)[0].view(T, self.n_heads, self.D_NOPE + self.D_ROPE)
         kv_a = laga.linear(hidden, self.w_kv_a)[0]
-        positions, slots = step.positions[:T], step.slots[:T]
+        positions = step.positions[:T]
+        refused = self._not_these_prompts(step, positions, cu_seqlens)
+        slots, gamma = torch.where(refused, -1, step.slots[:T]), torch.where(refused, float("nan"), self.ln_gamma)
         laga.rope(q, positions, self.rope, y=q)
-        latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
+        latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
         out = laga.fwd(q, latent, k_pe, self.w_kv_b, softmax_scale=self.softmax_scale, workspace=workspace, cu_seqlens=cu_seqlens)[0]
         return laga.linear(out.view(T, self.n_heads * self.D_V), self.w_o)[0]
 

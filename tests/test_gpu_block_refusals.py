@@ -1,0 +1,60 @@
+"""Steps that are not what the block's prefill is for are refused on the device, not answered wrongly."""
+import pytest
+import torch
+
+from parity import rel_l2
+from test_gpu_serving import BF16, make_block, pkg  # noqa: F401  (pkg: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def i32(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def rows(n, seed):
+    return torch.randn(n, 512, generator=torch.Generator().manual_seed(seed)).to(BF16).cuda()
+
+
+@pytest.fixture(scope="module")
+def blk(pkg):  # noqa: F811
+    return make_block(pkg, heads=16)
+
+
+def service(pkg, blk, lens=(40, 25, 33)):  # noqa: F811
+    cache = pkg.LatentCache(n_pages=12, n_requests=len(lens), max_tokens=64, page_size=16)
+    x = rows(sum(lens), 1)
+    cu = [sum(lens[:b]) for b in range(len(lens) + 1)]
+    step = cache.plan(i32(*lens), sum(lens))
+    blk.prefill(x, cache.pages[0], step, cu)
+    pkg.laga.check_status(step.status)
+    return cache, [x[a:b] for a, b in zip(cu[:-1], cu[1:])]
+
+
+@pytest.mark.parametrize("new,n,cu", [((10, 0, 0), 10, [0, 10]),              # request 0 holds tokens
+                                      ((0, 3, 10), 13, [0, 3, 13]),           # one of two does not (it was released)
+                                      ((0, 10, 0), 8, [0, 8]),                # fewer rows than the plan's tokens
+                                      ((0, 10, 0), 10, [0, 4, 10]),           # other lengths than the plan's
+                                      ((0, 200, 0), 10, [0, 10])])            # a plan that could not be placed
+def test_prefill_of_another_step_is_refused(pkg, blk, new, n, cu):  # noqa: F811
+    laga = pkg.laga
+    cache, _ = service(pkg, blk)
+    cache.release(1)
+    before = cache.pages[0].clone()
+    step = cache.plan(i32(*new), max(n, 10))
+    y = blk.prefill(rows(n, 2), cache.pages[0], step, cu)
+    code, detail = laga.query_status(step.status)
+    assert code == laga.ERR_CACHE_PLAN and detail == (0x50000003 if max(new) == 200 else 0x50000005)
+    assert torch.equal(cache.pages[0], before) and bool(y.isnan().all())
+
+
+@pytest.mark.parametrize("cu,pad", [([0, 10], 0), (None, 0), ([0, 10, 16], 6), ([0, 16], 6), ([0, 0, 10, 10], 0)])
+def test_prefill_of_its_own_step_is_not(pkg, blk, cu, pad):  # noqa: F811
+    """A released row again, padded or not, with boundaries given or one sequence."""
+    cache, _ = service(pkg, blk)
+    cache.release(1)
+    step = cache.plan(i32(0, 10, 0), 10 + pad)
+    x = rows(10 + pad, 3)
+    y = blk.prefill(x, cache.pages[0], step, cu)
+    pkg.laga.check_status(step.status)
+    assert rel_l2(y[:10], blk(x[:10]).detach()) <= 1e-6
