@@ -25,6 +25,7 @@ import torch
 
 from . import laga
 from .autograd import laga_attention
+from .serving import rows_are_requests
 
 
 class _Linear(torch.autograd.Function):
@@ -204,10 +205,11 @@ class LagaBlock(torch.nn.Module):
     @torch.no_grad()
     def decode(self, hidden: torch.Tensor, pages: torch.Tensor, step, block_table: torch.Tensor, workspace=None, requests=None) -> torch.Tensor:
         """One new token for each of B requests: hidden [B, d_model], ``step`` a plan that gives every request one token,
-        block_table the plan's table [B, columns].  Where the plan gave only some requests a token, ``requests`` (int64 [B], on the
-        device, ascending) names them; rows of ``hidden`` behind the plan's tokens are padding (any request's number, results to be
-        ignored).  Appends the tokens' latents and keys to ``pages`` and attends to each request's
-        whole cache, the new token included.  Every call reads lengths and tables on the device, so a step can be captured in a
+        block_table the plan's table [B, columns].  After a plan that does not, rows that are not their request's one token are refused
+        on the device: nothing of them enters the cache, their attention is zeros, the workspace's status LAGA_ERR_DEVICE_CHECK.
+        Where the plan gave only some requests a token, ``requests`` (int64 [B], on the device, ascending) names them; rows of
+        ``hidden`` behind the plan's tokens are padding (any request's number, results to be ignored).
+        Appends the tokens' latents and keys to ``pages`` and attends to each request's whole cache, the new token included.  Every call reads lengths and tables on the device, so a step can be captured in a
         graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``) and replayed.  A page number outside the cache or a
         length outside the table shows only in the workspace's status: give one, and ``laga.check_status(workspace)`` raises
         (with no workspace given, nothing of it is left to ask)."""
@@ -215,9 +217,13 @@ class LagaBlock(torch.nn.Module):
         B = hidden.shape[0]
         q = laga.linear(hidden, self.w_q)[0].view(B, self.n_heads, self.D_NOPE + self.D_ROPE)
         kv_a = laga.linear(hidden, self.w_kv_a)[0]
-        positions, slots, lens = step.positions[:B], step.slots[:B], step.seq_lens
+        positions = step.positions[:B]
         if requests is not None:
-            block_table, lens = block_table.index_select(0, requests), lens.index_select(0, requests)
+            slots, block_table, lens = step.slots[:B], block_table.index_select(0, requests), step.seq_lens.index_select(0, requests)
+        elif getattr(step, "row_lens", None) is not None:
+            slots, lens = step.row_slots, step.row_lens
+        else:                                    # a plan of laga.cache_plan itself
+            slots, lens = rows_are_requests(step, torch.arange(B + 1, dtype=torch.int32, device=hidden.device))
         laga.rope(q, positions, self.rope, y=q)
         laga.cache_append(kv_a, self.ln_gamma, self.ln_beta, positions, self.rope, slots, pages, eps=self.eps)
         out = laga.paged_decode(q, self.w_kv_b, pages, block_table, lens, softmax_scale=self.softmax_scale, workspace=workspace)[0]

@@ -11,6 +11,22 @@ import torch
 from . import laga
 
 
+class CacheStep(laga.CachePlan):
+    """A plan of a LatentCache.  Beside the plan's tensors, for the calls in which row b is request b's one new token: row_slots and
+    row_lens (int32 [n_requests]), the plan's slots and lengths, -1 in rows that are not (see `rows_are_requests`)."""
+
+    row_slots = row_lens = None
+
+
+def rows_are_requests(step: laga.CachePlan, ranks: torch.Tensor):
+    """(row_slots, row_lens) of a plan; ranks: int32 0 .. n_requests.  Token b of the step is request b's only one where b tokens come
+    before the request's and b + 1 before the next: a request with none or with several moves those behind it to other rows."""
+    n = ranks.numel() - 1
+    same = step.cu_new_lens == ranks
+    yes = same[1:] & same[:-1]
+    return torch.where(yes, step.slots[:n], -1), torch.where(yes, step.seq_lens, -1)
+
+
 class LatentCache:
     """n_pages pages of page_size tokens (a power of two from 16 to 1024) in each of n_layers layers; n_requests rows of at
     most max_tokens tokens."""
@@ -30,13 +46,17 @@ class LatentCache:
         self.free_pages = torch.zeros(n_pages + 1, **i32)          # a stack; the last entry only absorbs what `release` drops
         self.free_pages[:n_pages] = torch.arange(n_pages - 1, -1, -1, **i32)
         self.n_free = torch.full((1,), n_pages, **i32)
+        self._ranks = torch.arange(n_requests + 1, **i32)
 
-    def plan(self, new_lens: torch.Tensor, max_tokens: int) -> laga.CachePlan:
+    def plan(self, new_lens: torch.Tensor, max_tokens: int) -> CacheStep:
         """Places new_lens[b] (int32 [n_requests], on the device) tokens for each request and makes the result the cache's
         state.  A step that does not fit takes nothing and gives every row slot -1: ``laga.check_status(plan.status)`` tells."""
-        step = laga.cache_plan(self.seq_lens, new_lens, self.block_table, self.free_pages, self.n_free, self.page_size, max_tokens)
+        step = CacheStep._make(laga.cache_plan(self.seq_lens, new_lens, self.block_table, self.free_pages, self.n_free, self.page_size,
+                                               max_tokens))
         self.seq_lens.copy_(step.seq_lens)
         self.n_free.copy_(step.n_free)
+        if max_tokens >= self.seq_lens.numel():                     # (once a step here, not once a layer in `LagaBlock.decode`)
+            step.row_slots, step.row_lens = rows_are_requests(step, self._ranks)
         return step
 
     def release(self, request: int) -> None:

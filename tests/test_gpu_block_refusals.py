@@ -1,4 +1,4 @@
-"""Steps that are not what the block's prefill is for are refused on the device, not answered wrongly."""
+"""Steps that are not what the block's prefill and decode are for are refused on the device, not answered wrongly."""
 import pytest
 import torch
 
@@ -58,3 +58,38 @@ def test_prefill_of_its_own_step_is_not(pkg, blk, cu, pad):  # noqa: F811
     y = blk.prefill(x, cache.pages[0], step, cu)
     pkg.laga.check_status(step.status)
     assert rel_l2(y[:10], blk(x[:10]).detach()) <= 1e-6
+
+
+@pytest.mark.parametrize("plain", [False, True])
+@pytest.mark.parametrize("new,right", [((1, 0, 1), [0]), ((0, 1, 1), []), ((2, 0, 1), [2]), ((1, 2, 0), [0]), ((1, 1, 1), [0, 1, 2])])
+def test_decode_of_rows_that_are_not_their_requests(pkg, blk, new, right, plain):  # noqa: F811
+    laga = pkg.laga
+    cache, prompts = service(pkg, blk)
+    before = cache.pages[0].clone()
+    step = cache.plan(i32(*new), 3)
+    laga.check_status(step.status)
+    if plain:
+        step = laga.CachePlan._make(step)
+    token = rows(3, 4)
+    ws = laga.alloc_workspace(laga.paged_decode_workspace_bytes(3, 16))
+    y = blk.decode(token, cache.pages[0], step, cache.block_table, workspace=ws)
+    changed = (cache.pages[0] != before).any(-1).view(-1).nonzero().view(-1).tolist()
+    assert sorted(changed) == sorted(step.slots[b].item() for b in right)
+    assert laga.query_status(ws)[0] == (laga.OK if len(right) == 3 else laga.ERR_DEVICE_CHECK)
+    for b in range(3):
+        if b in right:             # 2e-2: as in the service's test against one pass
+            assert rel_l2(y[b], blk(torch.cat([prompts[b], token[b:b + 1]]))[-1].detach()) <= 2e-2
+        else:
+            assert not y[b].any()
+
+
+def test_decode_after_a_plan_that_was_not_placed(pkg, blk):  # noqa: F811
+    laga = pkg.laga
+    cache, _ = service(pkg, blk)
+    cache.n_free.zero_()
+    before = cache.pages[0].clone()
+    step = cache.plan(i32(30, 1, 1), 3)
+    assert laga.query_status(step.status)[0] == laga.ERR_CACHE_PLAN
+    ws = laga.alloc_workspace(laga.paged_decode_workspace_bytes(3, 16))
+    y = blk.decode(rows(3, 5), cache.pages[0], step, cache.block_table, workspace=ws)
+    assert laga.query_status(ws)[0] == laga.ERR_DEVICE_CHECK and not y.any() and torch.equal(cache.pages[0], before)
