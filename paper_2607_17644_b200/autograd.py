@@ -10,9 +10,34 @@ without a bf16 round trip) and autograd gets no gradient for the weight.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import laga
+
+
+class _Gradient(torch.autograd.Function):
+    """A gradient computed under ``create_graph``: like the gradient itself, and an error where it is differentiated."""
+
+    @staticmethod
+    def forward(ctx, backward, function_ctx, n_grads, *tensors):
+        return backward(function_ctx, *tensors[:n_grads])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("second derivatives are not available: the library's backward passes are not differentiable")
+
+
+def first_order(backward):
+    """Marks a Function's backward as not differentiable, through the incoming gradients or through what the forward saved.  (Unmarked, its
+    result would be a constant under ``create_graph``, and second derivatives silently incomplete.)"""
+    @functools.wraps(backward)
+    def call(ctx, *grads):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads)
+        return _Gradient.apply(backward, ctx, len(grads), *grads, *ctx.saved_tensors)
+    return call
 
 
 class _LagaAttention(torch.autograd.Function):
@@ -26,6 +51,7 @@ class _LagaAttention(torch.autograd.Function):
         return out, lse
 
     @staticmethod
+    @first_order
     def backward(ctx, dout, _dlse):
         q, c_kv, k_pe, w_kv_b, out, lse = ctx.saved_tensors
         acc = ctx.dw_fp32_out

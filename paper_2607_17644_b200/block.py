@@ -24,7 +24,7 @@ from __future__ import annotations
 import torch
 
 from . import laga
-from .autograd import laga_attention
+from .autograd import first_order, laga_attention
 from .serving import rows_are_requests
 
 
@@ -36,6 +36,7 @@ class _Linear(torch.autograd.Function):
         return y
 
     @staticmethod
+    @first_order
     def backward(ctx, dy):
         x, w = ctx.saved_tensors
         dx, dw, _ = laga.linear_backward(dy.contiguous(), x, w)
@@ -51,6 +52,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @first_order
     def backward(ctx, dy):
         x, gamma, mean, rstd = ctx.saved_tensors
         dx, dgamma, dbeta = laga.layernorm_backward(dy.contiguous(), x, gamma, mean, rstd, with_beta=ctx.has_beta)
@@ -65,6 +67,7 @@ class _Rotary(torch.autograd.Function):
         return laga.rope(x, positions, rope)
 
     @staticmethod
+    @first_order
     def backward(ctx, dy):
         positions, freqs = ctx.saved_tensors
         return laga.rope(dy.contiguous(), positions, laga.RopePlan(freqs, ctx.mscale, ctx.interleaved), inverse=True), None, None
@@ -79,6 +82,7 @@ class _LatentNormRope(torch.autograd.Function):
         return latent, k_pe
 
     @staticmethod
+    @first_order
     def backward(ctx, dlatent, dk_pe):
         kv_a, gamma, mean, rstd, positions, freqs = ctx.saved_tensors
         dkv_a, dgamma, dbeta = laga.latent_norm_rope_backward(dlatent.contiguous(), dk_pe.contiguous(), kv_a, gamma, mean, rstd, positions,
