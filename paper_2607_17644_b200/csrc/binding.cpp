@@ -9,6 +9,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -324,7 +325,12 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int64_t offset = 0;
         for (int i = 0; i < 6; offset += sizes[i++]) out[i] = part(whole, offset, sizes[i]);
     }
-    enqueue(device, "laga_cache_plan", [&](void* stream) {
+    if (requests == 0) {                                     // a step of nothing: the entry point takes at least one request
+        if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1)) != 0) raise_for(LAGA_ERR_INVALID_ARG, "laga_cache_plan");
+        out[0].fill_(-1);
+        for (int i : {1, 2, 5}) out[i].zero_();
+        out[4].copy_(n_free);
+    } else enqueue(device, "laga_cache_plan", [&](void* stream) {
         return library.cache_plan(data<int>(seq_lens), data<int>(new_lens), size32(requests, "block_table"), page_size, data<int>(table),
                                   size32(columns, "block_table"), data<int>(free_pages), size32(free_pages.numel(), "free_pages"),
                                   data<int>(n_free), max_tokens, data<int>(out[0]), data<int>(out[1]), data<int>(out[2]), data<int>(out[3]),
@@ -360,8 +366,14 @@ PyObject* py_paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     TORCH_CHECK_VALUE(!workspace.defined() || workspace.is_contiguous(), "workspace: expected a contiguous tensor");
     const c10::Device device = one_device({&q, &w, &cache, &table, &seq_lens, &out, &lse, &workspace});
     const int b = size32(B, "q"), heads = size32(h, "q"), dims[4] = {size32(d_c, "w_kv_b"), size32(d_nope, "q"), size32(d_rope, "cache"), size32(d_v, "w_kv_b")};
-    const size_t need = library.decode_workspace_bytes(b, heads, dims[0], dims[1], dims[2], dims[3]);
+    const size_t need = library.decode_workspace_bytes(b > 0 ? b : 1, heads, dims[0], dims[1], dims[2], dims[3]);
     if (need == 0) raise_for(LAGA_ERR_UNSUPPORTED, "laga_paged_decode_workspace_bytes");
+    if (B == 0) {                                            // nothing to do: a status word that says so
+        if (!out.defined()) out = fresh(q, {0, h, d_v}, ScalarType::BFloat16);
+        if (workspace.defined()) workspace.flatten().narrow(0, 0, std::min<int64_t>(workspace.numel(), 4)).zero_();
+        else workspace = at::zeros({1024}, q.options().dtype(ScalarType::Byte));
+        return wrap_all(out, lse, workspace);
+    }
     if (!workspace.defined()) workspace = workspace_of(q, need);
     if (!out.defined()) out = fresh(q, {B, h, d_v}, ScalarType::BFloat16);
     enqueue(device, "laga_paged_decode", [&](void* stream) {

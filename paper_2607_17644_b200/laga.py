@@ -510,7 +510,7 @@ class CachePlan(NamedTuple):
 def cache_plan(seq_lens, new_lens, block_table, free_pages, n_free, page_size, max_tokens, out=None, stream=None) -> CachePlan:
     """laga_cache_plan: pages, slots and positions for a step that adds new_lens[b] tokens to request b.  block_table
     (int32 [n, columns]) is written in place where the new tokens need pages; everything else comes back new (or in `out`,
-    a CachePlan of an earlier call with the same sizes)."""
+    a CachePlan of an earlier call with the same sizes).  No requests at all: a step of nothing."""
     plan = _run("cache_plan", stream, seq_lens, new_lens, block_table, free_pages, n_free, page_size, max_tokens, out)
     return CachePlan._make(plan) if out is None else plan
 
@@ -522,7 +522,7 @@ def paged_decode_workspace_bytes(B, h, d_c=512, d_nope=128, d_rope=64, d_v=128) 
 def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, out=None, lse=None, workspace=None, stream=None):
     """laga_paged_decode: attention of one new token per request (q bf16 [B, h, 192], rope band rotated) over a paged cache
     (bf16 [n_pages, page_size, 576]; block_table int32 [B, columns], seq_lens int32 [B], both on the device).  lse: fp32 [B, h] to
-    have it written.  Returns (out bf16 [B, h, 128], lse or None, workspace)."""
+    have it written.  Returns (out bf16 [B, h, 128], lse or None, workspace); with B = 0 there is nothing to do."""
     return _run("paged_decode", stream, q, w_kv_b, cache, block_table, seq_lens, softmax_scale, out, lse, workspace)
 
 
