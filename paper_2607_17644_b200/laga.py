@@ -448,9 +448,11 @@ def rope_plan(d_rot=64, base=10000.0, scaling=None, interleaved=True, device="cu
     j = torch.arange(d_rot // 2, dtype=torch.float64)
     mscale = 1.0
     options = dict(scaling or {"type": "none"})
-    kind, factor = options.pop("type"), float(options.pop("factor", 1.0))
+    kind = options.pop("type", None)
+    factor = float(options.pop("factor", 1.0 if kind == "none" else math.nan))
     known = {"none": (), "linear": (), "ntk": (), "yarn": ("original_length", "beta_fast", "beta_slow", "mscale_weight")}
-    if kind not in known or not factor >= 1 or any(k not in known[kind] for k in options):
+    if (kind not in known or not 1 <= factor < math.inf or (kind == "none" and factor != 1) or any(k not in known[kind] for k in options)
+            or not all(float(options.get(k, 1)) > 0 for k in ("original_length", "beta_fast", "beta_slow"))):
         raise ValueError(f"rope_plan: unknown or malformed scaling {scaling}")
     if kind == "ntk":
         base = base * factor ** (d_rot / (d_rot - 2))
