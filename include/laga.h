@@ -208,7 +208,7 @@ int laga_layernorm_backward(const void* dy, const void* x, const void* gamma, co
  *   positions int32 [M], any value, repeats allowed;   freqs fp64 [d_rot/2], radians per position
  *   layout: which channels pair up, LAGA_ROPE_INTERLEAVED (2j, 2j+1) or LAGA_ROPE_HALF (j, j + d_rot/2)
  *   inverse != 0: rotates back (times mscale, not divided by it): the transpose, i.e. the gradient of the forward call
- * Angles are formed in 64 bits (positions of millions stay exact); long-context scalings are choices of freqs and mscale.
+ * Angles are formed in 64 bits: off by at most |position * freq| 2^-52 + 2^-20 radians.  Long-context scalings are choices of freqs and mscale.
  * d: a multiple of 8, at most 1024; d_rot: a multiple of 16, at most 256; rot_begin: a multiple of 8.
  * No status word: errors are launch errors.
  */
