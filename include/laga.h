@@ -280,7 +280,7 @@ int laga_cache_plan(const int* seq_lens, const int* new_lens, int n_requests, in
  * LAGA_ERR_DEVICE_CHECK through laga_query_status(workspace).  page_size: a power of two from 16 to 1024; n_pages * page_size
  * and columns * page_size at most 2^30, B * columns * page_size at most 2^36, B * h at most 2^26.  d_c, d_nope, d_rope, d_v: 512, 128, 64, 128.  flags must be 0.
  * q W_uk is rounded to bf16 for the tensor cores, like the probabilities (which up to 32 heads are carried in two bf16 parts); sums,
- * maxima and the accumulator are fp32.
+ * maxima and the accumulator are fp32 (scores as powers of two, times log2(e): below -2.3e38 one counts as -inf).
  * Nothing depends on lengths at enqueue time: the call can be captured in a graph and replayed with new lengths.
  */
 size_t laga_paged_decode_workspace_bytes(int B, int h, int d_c, int d_nope, int d_rope, int d_v);
