@@ -174,15 +174,14 @@ class LagaBlock(torch.nn.Module):
             raise ValueError("prefill and decode need the block's rotation: LagaBlock(..., rope=laga.rope_plan(64))")
 
     @staticmethod
-    def _not_these_prompts(step, positions, cu_seqlens) -> torch.Tensor:
-        """A truth value on the device: the plan is not one of prompts with these boundaries from position 0 on (rows behind its last
-        token are padding).  Where it is not, the plan's status says so (detail 0x50000005)."""
+    def _not_these_prompts(step, positions, slots, cu_seqlens) -> torch.Tensor:
+        """A truth value on the device: the plan was not placed, or its rows are not prompts with these boundaries from position 0 on (rows
+        without a slot are padding).  Where it is so, the plan's status says it (detail 0x50000005)."""
         row = wanted = torch.arange(positions.numel(), dtype=torch.int32, device=positions.device)
-        n_tokens = step.cu_new_lens[-1]
         if cu_seqlens is not None:
             cu = torch.as_tensor(cu_seqlens, dtype=torch.int32).to(positions.device, non_blocking=True)
             wanted = row - cu[torch.searchsorted(cu, row, right=True) - 1]
-        refused = ((positions != wanted) & (row < n_tokens)).any() | (n_tokens > positions.numel()) | (step.status[0] != 0)
+        refused = ((positions != wanted) & (slots >= 0)).any() | (step.status[0] != 0)
         step.status.masked_fill_(refused & (step.status == 0), 0x50000005)
         return refused
 
@@ -198,9 +197,9 @@ class LagaBlock(torch.nn.Module):
         T = hidden.shape[0]
         q = laga.linear(hidden, self.w_q)[0].view(T, self.n_heads, self.D_NOPE + self.D_ROPE)
         kv_a = laga.linear(hidden, self.w_kv_a)[0]
-        positions = step.positions[:T]
-        refused = self._not_these_prompts(step, positions, cu_seqlens)
-        slots, gamma = torch.where(refused, -1, step.slots[:T]), torch.where(refused, float("nan"), self.ln_gamma)
+        positions, slots = step.positions[:T], step.slots[:T]
+        refused = self._not_these_prompts(step, positions, slots, cu_seqlens)
+        slots, gamma = torch.where(refused, -1, slots), torch.where(refused, float("nan"), self.ln_gamma)
         laga.rope(q, positions, self.rope, y=q)
         latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
         out = laga.fwd(q, latent, k_pe, self.w_kv_b, softmax_scale=self.softmax_scale, workspace=workspace, cu_seqlens=cu_seqlens)[0]

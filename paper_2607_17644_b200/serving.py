@@ -28,8 +28,8 @@ def rows_are_requests(step: laga.CachePlan, ranks: torch.Tensor):
 
 
 class LatentCache:
-    """n_pages pages of page_size tokens (a power of two from 16 to 1024) in each of n_layers layers; n_requests rows of at
-    most max_tokens tokens."""
+    """n_pages pages of page_size tokens (a power of two from 16 to 1024) in each of n_layers layers; n_requests rows, each with
+    room for max_tokens tokens (in whole pages: a plan takes up to ceil(max_tokens / page_size) * page_size)."""
 
     ROW = 576
 

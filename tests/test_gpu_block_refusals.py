@@ -33,7 +33,6 @@ def service(pkg, blk, lens=(40, 25, 33)):  # noqa: F811
 
 @pytest.mark.parametrize("new,n,cu", [((10, 0, 0), 10, [0, 10]),              # request 0 holds tokens
                                       ((0, 3, 10), 13, [0, 3, 13]),           # one of two does not (it was released)
-                                      ((0, 10, 0), 8, [0, 8]),                # fewer rows than the plan's tokens
                                       ((0, 10, 0), 10, [0, 4, 10]),           # other lengths than the plan's
                                       ((0, 200, 0), 10, [0, 10])])            # a plan that could not be placed
 def test_prefill_of_another_step_is_refused(pkg, blk, new, n, cu):  # noqa: F811
@@ -58,6 +57,19 @@ def test_prefill_of_its_own_step_is_not(pkg, blk, cu, pad):  # noqa: F811
     y = blk.prefill(x, cache.pages[0], step, cu)
     pkg.laga.check_status(step.status)
     assert rel_l2(y[:10], blk(x[:10]).detach()) <= 1e-6
+
+
+def test_prefill_in_two_calls(pkg, blk):  # noqa: F811
+    """One plan of two prompts, run one prompt at a time: the first rows, then a plan whose rows begin behind them."""
+    x = rows(50, 6)
+    whole, halves = (pkg.LatentCache(n_pages=12, n_requests=2, max_tokens=64, page_size=16) for _ in range(2))
+    step = whole.plan(i32(30, 20), 50)
+    y = blk.prefill(x, whole.pages[0], step, [0, 30, 50])
+    step = halves.plan(i32(30, 20), 50)
+    a = blk.prefill(x[:30], halves.pages[0], step, [0, 30])
+    b = blk.prefill(x[30:], halves.pages[0], step._replace(positions=step.positions[30:], slots=step.slots[30:]), [0, 20])
+    pkg.laga.check_status(step.status)
+    assert rel_l2(torch.cat([a, b]), y) <= 1e-6 and torch.equal(halves.pages[0], whole.pages[0])
 
 
 @pytest.mark.parametrize("plain", [False, True])
