@@ -290,6 +290,36 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
                       unsigned flags, void* stream);
 
 /*
+ * The paged latent cache in 8 bits: 644 bytes a token instead of 1152.
+ *
+ * Format.  A page of n tokens is n * 644 bytes: n rows of 640 e4m3 codes (512 of the normalised latent, 64 of the rotated key, 64 of what
+ * the key's first codes left), then the n rows' scales in fp32.  latent = scale * code, key = scale * (code + second code).  The scale is
+ * the smallest power of two, 2^-32 at least, with which no channel exceeds 448 scale, and each code the nearest (ties to even): a latent
+ * channel is off by at most 2^-4 of itself, a key channel by 2^-8, and by 2^-10 of the scale where they are smaller than 2^-6 of it.
+ * A token with a channel that is not finite is NaN in all of them.  Pages, slots, tables and lengths are those of the bf16 cache
+ * (laga_cache_plan makes them); the cache is 16-byte aligned, page_size a power of two from 16 to 1024, n_pages * page_size at most 2^30.
+ *
+ * laga_cache8_append: laga_latent_norm_rope into such a cache, with D = 512 and R = 64 (kv_a, gamma, beta, positions, freqs, layout, mscale
+ *   and slots as there): row slots[m] receives token m, rounded once, from fp32; a slot outside the cache writes nothing.
+ * laga_cache8_read: latent bf16 [M, 512] (exact) and k_pe bf16 [M, 64] (rounded once) of the rows slots[m], what laga_fwd takes as c_kv and
+ *   k_pe; zeros where a slot is outside the cache.  Slots may repeat.
+ * laga_paged_decode8: laga_paged_decode over such a cache, with its arguments, limits, errors and results, and a workspace of its own size.  The
+ *   scale must be a power of two, or zero for a row of zeros.  q W_uk and the rotated queries are carried in two e4m3 parts each, over a power
+ *   of two for each request and head (together 2^-8 of a channel, half a step of bf16); so are the probabilities (2^-8; over 32 heads 2^-7, half
+ *   a step more), each tile of 128 keys at a reference of its own: weights below 2^-16 of a tile's largest may be dropped.  Sums,
+ *   references and the accumulator are fp32.
+ */
+int laga_cache8_append(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps, const int* positions,
+                       const double* freqs, int M, int layout, float mscale, void* cache, int n_pages, int page_size, const int* slots,
+                       void* stream);
+int laga_cache8_read(const void* cache, int n_pages, int page_size, const int* slots, int M, void* latent, void* k_pe, void* stream);
+size_t laga_paged_decode8_workspace_bytes(int B, int h, int d_c, int d_nope, int d_rope, int d_v);
+int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int n_pages, int page_size,
+                       const int* block_table, int columns, const int* seq_lens, int B, int h, int d_c, int d_nope, int d_rope,
+                       int d_v, float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                       unsigned flags, void* stream);
+
+/*
  * Step entry points (the same kernels laga_fwd / laga_bwd launch, callable on their own).
  *
  * laga_up_project: Algorithm 1 step 4.   kv bf16 [S, h*(d_nope+d_v)] = c_kv . w_kv_b  (fp32 accumulate).

@@ -37,6 +37,10 @@ struct Library {
     decltype(&laga_cache_plan) cache_plan;
     decltype(&laga_paged_decode_workspace_bytes) decode_workspace_bytes;
     decltype(&laga_paged_decode) paged_decode;
+    decltype(&laga_cache8_append) cache8_append;
+    decltype(&laga_cache8_read) cache8_read;
+    decltype(&laga_paged_decode8_workspace_bytes) decode8_workspace_bytes;
+    decltype(&laga_paged_decode8) paged_decode8;
 } library;
 PyObject* fail = nullptr;                                     // fail(code, where) raises the package's error
 
@@ -96,6 +100,21 @@ c10::Device one_device(std::initializer_list<const Tensor*> tensors) {
     }
     return first->device();
 }
+
+// A cache in 8 bits: pages of page_size tokens, 644 bytes each.
+struct Pages8 {
+    static constexpr int64_t kToken = 644;
+    int n_pages, page_size;
+    explicit Pages8(const Tensor& cache) {
+        const bool ok = cache.is_cuda() && cache.scalar_type() == ScalarType::Byte && cache.is_contiguous() && cache.dim() == 2 &&
+                        cache.size(1) > 0 && cache.size(1) % kToken == 0;
+        TORCH_CHECK_VALUE(ok, "cache: expected contiguous CUDA Byte [pages, page_size * ", kToken, "], got ", cache.scalar_type(), " ", cache.sizes(),
+                          " strides ", cache.strides(), " on ", cache.device());
+        n_pages = size32(cache.size(0), "cache");
+        page_size = size32(cache.size(1) / kToken, "cache");
+    }
+};
+bool is_8bit(const Tensor& cache) { return cache.defined() && cache.scalar_type() == ScalarType::Byte; }
 
 struct Plan {
     Tensor freqs;
@@ -220,6 +239,20 @@ PyObject* py_latent_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (beta.defined()) expect(beta, ScalarType::BFloat16, {D}, "beta");
     TORCH_CHECK_VALUE(cache.defined() == slots.defined(), "cache and slots go together");
     TORCH_CHECK_VALUE(dense || cache.defined(), "cache: expected a tensor");
+    if (is_8bit(cache)) {                                    // cache_append into a cache of codes
+        TORCH_CHECK_VALUE(!dense, "cache: dense results go with a cache of bf16 rows; cache_append writes one in 8 bits, cache_read reads it back");
+        TORCH_CHECK_VALUE(D == 512 && R == 64, "cache: in 8 bits a token is 512 + 64 channels, kv_a has ", D, " + ", R);
+        const Pages8 pages(cache);
+        expect(slots, ScalarType::Int, {M}, "slots");
+        const c10::Device device = one_device({&kv_a, &gamma, &beta, &positions, &plan.freqs, &cache, &slots});
+        if (M > 0)
+            enqueue(device, "laga_cache8_append", [&](void* stream) {
+                return library.cache8_append(data(kv_a), pitch, data(gamma), data(beta), eps, data<int>(positions), data<double>(plan.freqs),
+                                             size32(M, "kv_a"), plan.interleaved, plan.mscale, data(cache), pages.n_pages, pages.page_size,
+                                             data<int>(slots), stream);
+            });
+        Py_RETURN_NONE;
+    }
     int64_t n_slots = 0;
     if (cache.defined()) {
         TORCH_CHECK_VALUE(cache.is_cuda() && cache.scalar_type() == ScalarType::BFloat16 && cache.is_contiguous() && cache.dim() >= 2 &&
@@ -341,6 +374,28 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// cache_read(cache, slots, latent | None, k_pe | None) -> (latent, k_pe)
+PyObject* py_cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    arguments(n, 4);
+    const Tensor &cache = tensor(a[0], "cache"), &slots = tensor(a[1], "slots");
+    const Pages8 pages(cache);
+    const int64_t M = slots.numel();
+    expect(slots, ScalarType::Int, {M}, "slots");
+    Tensor latent = maybe(a[2], "latent"), k_pe = maybe(a[3], "k_pe");
+    if (latent.defined()) expect(latent, ScalarType::BFloat16, {M, 512}, "latent");
+    if (k_pe.defined()) expect(k_pe, ScalarType::BFloat16, {M, 64}, "k_pe");
+    const c10::Device device = one_device({&cache, &slots, &latent, &k_pe});
+    if (!latent.defined()) latent = fresh(cache, {M, 512}, ScalarType::BFloat16);
+    if (!k_pe.defined()) k_pe = fresh(cache, {M, 64}, ScalarType::BFloat16);
+    if (M > 0)
+        enqueue(device, "laga_cache8_read", [&](void* stream) {
+            return library.cache8_read(data(cache), pages.n_pages, pages.page_size, data<int>(slots), size32(M, "slots"), data(latent), data(k_pe), stream);
+        });
+    return wrap_all(latent, k_pe);
+    END_HANDLE_TH_ERRORS
+}
+
 // paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale | None, out | None, lse | None, workspace | None)
 // -> (out, lse | None, workspace)
 PyObject* py_paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -348,14 +403,19 @@ PyObject* py_paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     arguments(n, 9);
     const Tensor &q = tensor(a[0], "q"), &w = tensor(a[1], "w_kv_b"), &cache = tensor(a[2], "cache"), &table = tensor(a[3], "block_table"),
                  &seq_lens = tensor(a[4], "seq_lens");
-    TORCH_CHECK_VALUE(q.dim() == 3 && w.dim() == 2 && cache.dim() == 3 && table.dim() == 2, "paged_decode: expected q [B, h, d], w_kv_b [d_c, n], ",
+    const bool codes = is_8bit(cache);                       // a cache in 8 bits
+    TORCH_CHECK_VALUE(q.dim() == 3 && w.dim() == 2 && (codes || cache.dim() == 3) && table.dim() == 2, "paged_decode: expected q [B, h, d], w_kv_b [d_c, n], ",
                       "cache [pages, page_size, row] and block_table [B, columns], got ", q.sizes(), ", ", w.sizes(), ", ", cache.sizes(), ", ",
                       table.sizes());
-    const int64_t B = q.size(0), h = q.size(1), d_qk = q.size(2), d_c = w.size(0), d_rope = cache.size(2) - d_c, d_nope = d_qk - d_rope,
+    const int64_t B = q.size(0), h = q.size(1), d_qk = q.size(2), d_c = w.size(0), d_rope = codes ? 64 : cache.size(2) - d_c, d_nope = d_qk - d_rope,
                   d_v = h > 0 ? w.size(1) / h - d_nope : 0;
     TORCH_CHECK_VALUE(h > 0, "q: no heads");
     expect(q, ScalarType::BFloat16, {B, h, d_qk}, "q");
-    expect(cache, ScalarType::BFloat16, cache.sizes(), "cache");
+    if (!codes) expect(cache, ScalarType::BFloat16, cache.sizes(), "cache");
+    const int n_pages = codes ? Pages8(cache).n_pages : size32(cache.size(0), "cache"), page_size = codes ? Pages8(cache).page_size : size32(cache.size(1), "cache");
+    const auto workspace_bytes = codes ? library.decode8_workspace_bytes : library.decode_workspace_bytes;
+    const auto paged_decode = codes ? library.paged_decode8 : library.paged_decode;
+    const char* const name = codes ? "laga_paged_decode8" : "laga_paged_decode";
     expect(w, ScalarType::BFloat16, {d_c, h * (d_nope + d_v)}, "w_kv_b");
     expect(table, ScalarType::Int, {B, table.size(1)}, "block_table");
     expect(seq_lens, ScalarType::Int, {B}, "seq_lens");
@@ -366,7 +426,7 @@ PyObject* py_paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     TORCH_CHECK_VALUE(!workspace.defined() || workspace.is_contiguous(), "workspace: expected a contiguous tensor");
     const c10::Device device = one_device({&q, &w, &cache, &table, &seq_lens, &out, &lse, &workspace});
     const int b = size32(B, "q"), heads = size32(h, "q"), dims[4] = {size32(d_c, "w_kv_b"), size32(d_nope, "q"), size32(d_rope, "cache"), size32(d_v, "w_kv_b")};
-    const size_t need = library.decode_workspace_bytes(b > 0 ? b : 1, heads, dims[0], dims[1], dims[2], dims[3]);
+    const size_t need = workspace_bytes(b > 0 ? b : 1, heads, dims[0], dims[1], dims[2], dims[3]);
     if (need == 0) raise_for(LAGA_ERR_UNSUPPORTED, "laga_paged_decode_workspace_bytes");
     if (B == 0) {                                            // nothing to do: a status word that says so
         if (!out.defined()) out = fresh(q, {0, h, d_v}, ScalarType::BFloat16);
@@ -376,10 +436,10 @@ PyObject* py_paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (!workspace.defined()) workspace = workspace_of(q, need);
     if (!out.defined()) out = fresh(q, {B, h, d_v}, ScalarType::BFloat16);
-    enqueue(device, "laga_paged_decode", [&](void* stream) {
-        return library.paged_decode(data(q), data(w), data(cache), size32(cache.size(0), "cache"), size32(cache.size(1), "cache"), data<int>(table),
-                                    size32(table.size(1), "block_table"), data<int>(seq_lens), b, heads, dims[0], dims[1], dims[2], dims[3],
-                                    static_cast<float>(scale), data(out), data<float>(lse), data(workspace), workspace.nbytes(), 0, stream);
+    enqueue(device, name, [&](void* stream) {
+        return paged_decode(data(q), data(w), data(cache), n_pages, page_size, data<int>(table),
+                            size32(table.size(1), "block_table"), data<int>(seq_lens), b, heads, dims[0], dims[1], dims[2], dims[3],
+                            static_cast<float>(scale), data(out), data<float>(lse), data(workspace), workspace.nbytes(), 0, stream);
     });
     return wrap_all(out, lse, workspace);
     END_HANDLE_TH_ERRORS
@@ -412,6 +472,7 @@ PyMethodDef methods[] = {method<py_bind>("bind"),
                          method<py_latent_norm_rope>("latent_norm_rope"),
                          method<py_latent_norm_rope_backward>("latent_norm_rope_backward"),
                          method<py_cache_plan>("cache_plan"),
+                         method<py_cache_read>("cache_read"),
                          method<py_paged_decode>("paged_decode"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

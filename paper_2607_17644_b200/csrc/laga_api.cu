@@ -15,8 +15,10 @@
 #include "attn_absorbed_sm100.cuh"
 #include "attn_bwd_fused_sm100.cuh"
 #include "attn_bwd_sm100.cuh"
+#include "attn_decode8_sm100.cuh"
 #include "attn_decode_sm100.cuh"
 #include "attn_fwd_sm100.cuh"
+#include "cache8_sm100.cuh"
 #include "cache_plan_sm100.cuh"
 #include "gemm_sm100.cuh"
 #include "layernorm_sm100.cuh"
@@ -90,6 +92,24 @@ bool make_tmap_cache(CUtensorMap* map, const void* base, uint64_t rows, uint32_t
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Maps over 8-bit codes (boxes of 128 of them, out of range reads as zero):
+//   kMapPages    the cache: 640 codes x rows of a page x pages (`rows` pages, `stride` bytes apart, of `inner` rows each), 128-byte swizzle
+//   kMapQueries  2-d, 128-byte swizzle: the queries' rows as the attention reads them
+//   kMapStore    2-d, no swizzle: the same rows as decode_absorb8_kernel writes them
+enum : uint32_t { kMapPages = 16, kMapQueries = 17, kMapStore = 18 };
+bool make_tmap_codes(CUtensorMap* map, uint32_t kind, const void* base, uint64_t inner, uint64_t rows, uint64_t stride, uint32_t box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const bool pages = kind == kMapPages;
+    cuuint64_t dims[3] = {pages ? kC8Row : inner, pages ? inner : rows, rows};
+    cuuint64_t strides[2] = {pages ? kC8Row : stride, stride};
+    cuuint32_t box[3] = {128u, box_rows, 1u};
+    cuuint32_t estr[3] = {1u, 1u, 1u};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, pages ? 3 : 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              kind == kMapStore ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // ---- launch status slot ---------------------------------------------------------------------------
 // The first kStatusBytes of every workspace: word 0 is the device status word; the work counters of the
 // persistent attention kernels and their clock probes follow.  The first kStatusClearBytes (all of
@@ -154,6 +174,10 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_decode_sm100_kernel<32>, AttnDecodeSmem<32>::kTotalBytes) &&
               allow_smem(attn_decode_sm100_kernel<64>, AttnDecodeSmem<64>::kTotalBytes) &&
               allow_smem(decode_absorb_kernel<64>, DecodeAbsorbSmem<64>::kTotalBytes) &&
+              allow_smem(attn_decode8_sm100_kernel<16>, AttnDecode8Smem<16>::kTotalBytes) &&
+              allow_smem(attn_decode8_sm100_kernel<32>, AttnDecode8Smem<32>::kTotalBytes) &&
+              allow_smem(attn_decode8_sm100_kernel<64>, AttnDecode8Smem<64>::kTotalBytes) &&
+              allow_smem(decode_absorb8_kernel<64>, DecodeAbsorb8Smem<64>::kTotalBytes) &&
               allow_smem(decode_project_kernel, DecodeProjectSmem::kTotalBytes) &&
               allow_smem(latent_norm_rope_fwd_kernel<2, false>, latent_fwd_smem(256, kRopeMaxRot)) &&
               allow_smem(latent_norm_rope_fwd_kernel<4, false>, latent_fwd_smem(512, kRopeMaxRot)) &&
@@ -248,7 +272,7 @@ struct TmapKey {
     const void* base;
     uint64_t inner, rows, stride;
     uint32_t box_rows;
-    uint32_t cache_groups;      // 0: a 2-d map; else a cache map with this many channel groups in its box
+    uint32_t cache_groups;      // 0: a 2-d map; up to 9: a cache map with this many channel groups in its box; from kMapPages on: a map of codes
     bool operator==(const TmapKey& o) const {
         return base == o.base && inner == o.inner && rows == o.rows && stride == o.stride && box_rows == o.box_rows &&
                cache_groups == o.cache_groups;
@@ -268,6 +292,10 @@ bool cached_tmap_bf16(CUtensorMap* map, const void* base, uint64_t inner_elems, 
     return g_tmaps.get(TmapKey{base, inner_elems, rows, row_stride_bytes, box_rows, cache_groups}, map, [&](CUtensorMap* m) {
         return cache_groups ? make_tmap_cache(m, base, rows, box_rows, cache_groups) : make_tmap_bf16(m, base, inner_elems, rows, row_stride_bytes, box_rows);
     });
+}
+bool cached_tmap_codes(CUtensorMap* map, uint32_t kind, const void* base, uint64_t inner, uint64_t rows, uint64_t stride, uint32_t box_rows) {
+    return g_tmaps.get(TmapKey{base, inner, rows, stride, box_rows, kind}, map,
+                       [&](CUtensorMap* m) { return make_tmap_codes(m, kind, base, inner, rows, stride, box_rows); });
 }
 
 // ---- launches ----------------------------------------------------------------------------------------
@@ -780,6 +808,48 @@ int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, flo
     launch_kernel(decode_project_kernel, dim3(a.h, n_tiles < most ? n_tiles : most), dim3(kProjectThreads), DecodeProjectSmem::kTotalBytes, stream,
                   true, tw, static_cast<const float*>(a.part_o), static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift,
                   a.B, a.h, a.h_pad, a.ctas_per_group, tile, static_cast<__nv_bfloat16*>(out), lse, a.status);
+    return launch_status();
+}
+
+// ---- the same over a cache in 8 bits ---------------------------------------------------------------------
+struct Decode8Layout {
+    DecodeLayout d;
+    size_t q_rows, q_scale;                           // in the place of d's q_abs
+};
+Decode8Layout decode8_layout(int B, int h) {
+    Decode8Layout w;
+    w.d = decode_layout(B, h);
+    const size_t heads = static_cast<size_t>(B) * w.d.h_pad, parts = static_cast<size_t>(w.d.slots) * w.d.h_pad;
+    w.q_rows = kStatusBytes;
+    w.q_scale = w.q_rows + align_up(heads * 2 * kC8Row, 1024);
+    w.d.part_o = w.q_scale + align_up(heads * sizeof(float), 1024);
+    w.d.part_ml = w.d.part_o + parts * kDecLat * sizeof(float);
+    w.d.total = w.d.part_ml + align_up(parts * sizeof(float2), 1024);
+    return w;
+}
+
+template <int kRequests>
+int launch_decode_absorb8(const void* q, const void* w, int B, int h, int h_pad, uint8_t* rows, float* q_scale, unsigned* status, cudaStream_t stream) {
+    const uint64_t q_row = static_cast<uint64_t>(h) * (kDn + kDr), w_row = static_cast<uint64_t>(h) * (kDn + kDv), request = 2ull * h_pad * kC8Row;
+    CUtensorMap tw, tq, to;
+    if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, kRequests) ||
+        !cached_tmap_codes(&to, kMapStore, rows, request, B, request, kRequests))
+        return LAGA_ERR_CUDA;
+    launch_kernel(decode_absorb8_kernel<kRequests>, dim3(kDc / 128, h, (B + kRequests - 1) / kRequests), dim3(kAbsorbThreads),
+                  DecodeAbsorb8Smem<kRequests>::kTotalBytes, stream, false, tw, tq, to, static_cast<const __nv_bfloat16*>(q), B, h, h_pad, rows, q_scale,
+                  status, static_cast<int>(kStatusClearBytes / sizeof(unsigned)));
+    return launch_status();
+}
+
+template <int kHeads>
+int launch_attn_decode8(const uint8_t* q_rows, const AttnDecode8Args& a, cudaStream_t stream) {
+    CUtensorMap tq, tc;
+    if (!cached_tmap_codes(&tq, kMapQueries, q_rows, kC8Row, 2ull * a.d.B * a.d.h_pad, kC8Row, 2 * kHeads) ||
+        !cached_tmap_codes(&tc, kMapPages, a.cache.base, 1ull << a.d.page_shift, a.d.n_pages, a.cache.page_bytes(), a.d.page_shift < 6 ? 1u << a.d.page_shift : 64u))
+        return LAGA_ERR_CUDA;
+    ScopedKernelEvents ev(LAGA_KERNEL_ATTN_DECODE, stream);
+    launch_kernel(attn_decode8_sm100_kernel<kHeads>, dim3(static_cast<unsigned>(a.d.n_groups * a.d.ctas_per_group)), dim3(AttnDecode8Smem<kHeads>::kThreads),
+                  AttnDecode8Smem<kHeads>::kTotalBytes, stream, true, tq, tc, a);
     return launch_status();
 }
 
@@ -1481,6 +1551,105 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
     else rc = launch_attn_decode<64>(q, base + w.q_abs, cache, rows, a, st);
     if (rc != LAGA_OK) return rc;
     return launch_decode_project(w_kv_b, a, out, lse, st);
+}
+
+// ---- the paged latent cache in 8 bits --------------------------------------------------------------
+int laga_cache8_append(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps, const int* positions,
+                       const double* freqs, int M, int layout, float mscale, void* cache, int n_pages, int page_size, const int* slots,
+                       void* stream) {
+    const int shift = page_shift_of(page_size);
+    if (!kv_a || !gamma || !cache || !slots || M < 1 || M > kLatentMaxRows || !(eps >= 0.f) || n_pages < 1 || shift < 0 ||
+        !rotary_ok(positions, freqs, kDr, mscale, layout) || kv_a_pitch < kDc + kDr || (kv_a_pitch & 7) || kv_a_pitch > (1ll << 30))
+        return LAGA_ERR_INVALID_ARG;
+    if (!aligned16(kv_a) || !aligned16(gamma) || !aligned16(beta) || !aligned16(cache) || (reinterpret_cast<uintptr_t>(slots) & 3u))
+        return LAGA_ERR_INVALID_ARG;
+    const long long rows = static_cast<long long>(n_pages) << shift;
+    const size_t m = static_cast<size_t>(M);
+    if (rows > (1ll << 30) ||
+        outputs_clash({{kv_a, ((m - 1) * kv_a_pitch + kDc + kDr) * 2}, {gamma, kDc * 2ull}, {beta, kDc * 2ull}, {positions, m * 4}, {freqs, kDr * 4ull}, {slots, m * 4}},
+                      {{cache, static_cast<size_t>(rows) * kC8Token}}))
+        return LAGA_ERR_INVALID_ARG;
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    if ((rc = check_pointers({kv_a, gamma, beta, positions, freqs, cache, slots})) != LAGA_OK) return rc;
+    auto bf = [](const void* p) { return static_cast<const __nv_bfloat16*>(p); };
+    const Cache8AppendArgs a{bf(kv_a), kv_a_pitch, bf(gamma), bf(beta), M, eps, Rotary{positions, freqs, mscale, layout == LAGA_ROPE_INTERLEAVED ? 1 : 0, 0},
+                             Cache8{static_cast<uint8_t*>(cache), shift, static_cast<int>(rows)}, slots};
+    const int rows_per_block = kLnWarps * 2, needed = M / rows_per_block + (M % rows_per_block != 0), cap = sm_count() * 2;       // one resident wave
+    const dim3 grid(needed < cap ? needed : cap), block(kLnWarps * 32);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (layout == LAGA_ROPE_INTERLEAVED) cache8_append_kernel<true><<<grid, block, 0, st>>>(a);
+    else cache8_append_kernel<false><<<grid, block, 0, st>>>(a);
+    return launch_status();
+}
+
+int laga_cache8_read(const void* cache, int n_pages, int page_size, const int* slots, int M, void* latent, void* k_pe, void* stream) {
+    const int shift = page_shift_of(page_size);
+    if (!cache || !slots || !latent || !k_pe || M < 1 || M > kLatentMaxRows || n_pages < 1 || shift < 0) return LAGA_ERR_INVALID_ARG;
+    if (!aligned16(cache) || !aligned16(latent) || !aligned16(k_pe) || (reinterpret_cast<uintptr_t>(slots) & 3u)) return LAGA_ERR_INVALID_ARG;
+    const long long rows = static_cast<long long>(n_pages) << shift;
+    const size_t m = static_cast<size_t>(M);
+    if (rows > (1ll << 30) || outputs_clash({{cache, static_cast<size_t>(rows) * kC8Token}, {slots, m * 4}}, {{latent, m * kDc * 2}, {k_pe, m * kDr * 2}}))
+        return LAGA_ERR_INVALID_ARG;
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    if ((rc = check_pointers({cache, slots, latent, k_pe})) != LAGA_OK) return rc;
+    const Cache8ReadArgs a{Cache8{static_cast<uint8_t*>(const_cast<void*>(cache)), shift, static_cast<int>(rows)}, slots, M, static_cast<__nv_bfloat16*>(latent),
+                           static_cast<__nv_bfloat16*>(k_pe)};
+    const int per_block = kC8ReadY * kC8ReadRows;
+    cache8_read_kernel<<<M / per_block + (M % per_block != 0), dim3(kC8ReadUnits, kC8ReadY), 0, static_cast<cudaStream_t>(stream)>>>(a);
+    return launch_status();
+}
+
+size_t laga_paged_decode8_workspace_bytes(int B, int h, int d_c, int d_nope, int d_rope, int d_v) {
+    if (B < 1 || h < 1 || !geometry_is_v3(d_c, d_nope, d_rope, d_v)) return 0;
+    return decode8_layout(B, h).d.total;
+}
+
+int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int n_pages, int page_size, const int* block_table,
+                       int columns, const int* seq_lens, int B, int h, int d_c, int d_nope, int d_rope, int d_v, float softmax_scale,
+                       void* out, float* lse, void* workspace, size_t workspace_bytes, unsigned flags, void* stream) {
+    const int shift = page_shift_of(page_size);
+    if (!q || !w_kv_b || !cache || !block_table || !seq_lens || !out || !workspace || B < 1 || h < 1 || n_pages < 1 || columns < 1 ||
+        shift < 0 || flags != 0 || !(softmax_scale > 0.f))
+        return LAGA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(w_kv_b) || !aligned16(cache) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) ||
+        (reinterpret_cast<uintptr_t>(block_table) & 3u) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u) ||
+        (reinterpret_cast<uintptr_t>(workspace) & 1023u))
+        return LAGA_ERR_INVALID_ARG;
+    if (!geometry_is_v3(d_c, d_nope, d_rope, d_v)) return LAGA_ERR_UNSUPPORTED;
+    // rows, keys and units are counted in 32 bits (byte offsets are not), rows of queries too: two for each padded head
+    const long long rows = static_cast<long long>(n_pages) << shift, capacity = static_cast<long long>(columns) << shift;
+    if (rows > (1ll << 30) || capacity > (1ll << 30) || ((capacity + kDecKeys - 1) / kDecKeys) * B > (1ll << 30) ||
+        static_cast<long long>(B) * h > (1ll << 26) || h > 65535 || B > 65535 * 8)
+        return LAGA_ERR_INVALID_ARG;
+    const Decode8Layout w = decode8_layout(B, h);
+    if (workspace_bytes < w.d.total) return LAGA_ERR_WORKSPACE_TOO_SMALL;
+    const size_t b = static_cast<size_t>(B), bh = b * h;
+    if (outputs_clash({{q, bh * 192 * 2}, {w_kv_b, static_cast<size_t>(h) * 512 * 256 * 2}, {cache, static_cast<size_t>(rows) * kC8Token},
+                       {block_table, b * columns * 4}, {seq_lens, b * 4}},
+                      {{out, bh * 128 * 2}, {lse, bh * 4}, {workspace, w.d.total}}))
+        return LAGA_ERR_INVALID_ARG;
+    int rc = check_device();
+    if (rc != LAGA_OK) return rc;
+    if ((rc = check_pointers({q, w_kv_b, cache, block_table, seq_lens, out, lse, workspace})) != LAGA_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint8_t* base = static_cast<uint8_t*>(workspace);
+    unsigned* status = reinterpret_cast<unsigned*>(base);
+    float* q_scale = reinterpret_cast<float*>(base + w.q_scale);
+    // (the tiles of requests as in laga_paged_decode)
+    rc = B <= 16 ? launch_decode_absorb8<16>(q, w_kv_b, B, h, w.d.h_pad, base + w.q_rows, q_scale, status, st)
+                 : launch_decode_absorb8<64>(q, w_kv_b, B, h, w.d.h_pad, base + w.q_rows, q_scale, status, st);
+    if (rc != LAGA_OK) return rc;
+    const AttnDecode8Args a{AttnDecodeArgs{B, h, w.d.n_groups, w.d.ctas_per_group, softmax_scale * 1.4426950408889634f, seq_lens, block_table, columns, shift,
+                                           n_pages, reinterpret_cast<float*>(base + w.d.part_o), reinterpret_cast<float2*>(base + w.d.part_ml), w.d.h_pad,
+                                           status},
+                            Cache8{static_cast<uint8_t*>(const_cast<void*>(cache)), shift, static_cast<int>(rows)}, q_scale};
+    if (w.d.heads == 16) rc = launch_attn_decode8<16>(base + w.q_rows, a, st);
+    else if (w.d.heads == 32) rc = launch_attn_decode8<32>(base + w.q_rows, a, st);
+    else rc = launch_attn_decode8<64>(base + w.q_rows, a, st);
+    if (rc != LAGA_OK) return rc;
+    return launch_decode_project(w_kv_b, a.d, out, lse, st);
 }
 
 }  // extern "C"

@@ -4,6 +4,7 @@
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -711,6 +712,93 @@ __device__ __forceinline__ void mma_commit_pair(uint64_t* bar, uint16_t cta_mask
                  ::"r"(smem_u32(bar)), "h"(cta_mask)
                  : "memory");
 }
+
+// ------------------------------------------------------------------------------------------------
+// 8-bit operands
+// ------------------------------------------------------------------------------------------------
+// The operand tiles above with one byte an element: a row of 128 bytes is 128 elements, an MMA consumes K = 32 of them, and both
+// operands' types are fields of the instruction descriptor.  K-major tiles advance by 32 bytes a step as bf16 ones do; MN-major tiles
+// (rows = K index) by 32 rows.  MN-major rows shorter than 128 bytes have the swizzle of their length: 16-byte chunk c of row k at
+// c ^ ((k >> 1) & 3) in rows of 64 bytes, at c ^ ((k >> 2) & 1) in rows of 32; the next group of eight rows is the stride offset away.
+enum { kE4m3 = 0, kE5m2 = 1 };
+__host__ __device__ constexpr uint32_t make_idesc_f8(int a_type, int b_type, int m, int n, int a_mn_major, int b_mn_major) {
+    return (1u << 4)                                   // D format  : fp32
+           | (static_cast<uint32_t>(a_type) << 7) | (static_cast<uint32_t>(b_type) << 10)
+           | (static_cast<uint32_t>(a_mn_major) << 15) | (static_cast<uint32_t>(b_mn_major) << 16)
+           | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+// MN-major operand whose rows of kRowBytes (32, 64 or 128) are one atom wide.
+template <int kRowBytes>
+__device__ __forceinline__ uint64_t desc_mn_major_narrow(uint32_t smem_addr) {
+    static_assert(kRowBytes == 32 || kRowBytes == 64 || kRowBytes == 128, "row of a swizzled operand");
+    constexpr uint64_t swizzle = kRowBytes == 128 ? 2ull : kRowBytes == 64 ? 4ull : 6ull;
+    return static_cast<uint64_t>((smem_addr & 0x3ffffu) >> 4) | (1ull << 16) | (static_cast<uint64_t>(kRowBytes * 8 >> 4) << 32) | kDescVersionSm100 |
+           (swizzle << 61);
+}
+__device__ __forceinline__ void mma8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// D (+)= A B over 128 elements of K: four steps, the operands advancing by kAStep and kBStep descriptor units; accumulate_first == 0
+// overwrites D.
+#define LAGA_MMA8_STEP(I, P)                                                                                                  \
+    "add.u32 lo, %1, %7 * " #I ";\n\tmov.b64 da, {lo, %2};\n\tadd.u32 lo, %3, %8 * " #I ";\n\tmov.b64 db, {lo, %4};\n\t"       \
+    "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %5, " #P ";\n\t"
+template <int kAStep, int kBStep>
+__device__ __forceinline__ void mma8_ss_chain4(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                               uint32_t accumulate_first) {
+    asm volatile(
+        "{\n\t.reg .pred p0, p1;\n\t.reg .b32 lo;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p0, %6, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t"
+        LAGA_MMA8_STEP(0, p0) LAGA_MMA8_STEP(1, p1) LAGA_MMA8_STEP(2, p1) LAGA_MMA8_STEP(3, p1)
+        "}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate_first), "n"(kAStep), "n"(kBStep)
+        : "memory");
+}
+// Untiled copy: addresses and size multiples of 16 bytes.
+__device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem_dst)),
+                 "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+// A box of codes of the 8-bit cache: channel, row of a page, page (past the last: zeros).
+__device__ __forceinline__ void tma_load_codes_chk(unsigned int* status, void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z,
+                                                   uint64_t policy) {
+    if (device_check((x & 15) == 0 && x >= 0 && x < 640 && y >= 0 && y < 1024 && z >= 0 && (smem_u32(smem_dst) & 1023u) == 0u, status, 0xE90000u | (z & 0xffff)))
+        tma_load_3d(smem_dst, map, bar, x, y, z, policy);
+}
+// Two values to two codes, `lo` in the low byte; past the largest number they become it, NaN stays NaN.
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2_of_half2(uint32_t h) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+    return r;
+}
+__device__ __forceinline__ uint32_t e5m2x2_of_half2(uint32_t h) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+    return r;
+}
+// ... and back (exact).
+__device__ __forceinline__ uint32_t half2_of_e4m3x2(uint32_t codes) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(codes)));
+    return r;
+}
+__device__ __forceinline__ uint32_t half2_of_e5m2x2(uint32_t codes) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(codes)));
+    return r;
+}
+__device__ __forceinline__ float2 float2_of_half2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 
 // ------------------------------------------------------------------------------------------------
 // Small helpers

@@ -62,6 +62,10 @@ SIGNATURES = {
     "laga_cache_plan": (_ci, [_vp, _vp, _ci, _ci, _vp, _ci, _vp, _ci, _vp, _ci] + [_vp] * 7),
     "laga_paged_decode_workspace_bytes": (_sz, [_ci] * 6),
     "laga_paged_decode": (_ci, [_vp] * 3 + [_ci, _ci, _vp, _ci, _vp] + [_ci] * 6 + [_cf, _vp, _vp, _vp, _sz, _cu, _vp]),
+    "laga_cache8_append": (_ci, [_vp, _ll, _vp, _vp, _cf, _vp, _vp, _ci, _ci, _cf, _vp, _ci, _ci, _vp, _vp]),
+    "laga_cache8_read": (_ci, [_vp, _ci, _ci, _vp, _ci, _vp, _vp, _vp]),
+    "laga_paged_decode8_workspace_bytes": (_sz, [_ci] * 6),
+    "laga_paged_decode8": (_ci, [_vp] * 3 + [_ci, _ci, _vp, _ci, _vp] + [_ci] * 6 + [_cf, _vp, _vp, _vp, _sz, _cu, _vp]),
     "laga_up_project": (_ci, [_vp, _vp] + [_ci] * 5 + [_vp, _vp, _vp]),
     "laga_kv_backward": (_ci, [_vp] * 3 + [_ci] * 5 + [_vp, _vp, _cu, _vp, _vp]),
     "laga_query_status": (_ci, [_vp, _vp, ctypes.POINTER(_cu)]),
@@ -104,7 +108,8 @@ def _load_binding():
     except ImportError as missing:
         raise ImportError("the compiled binding is missing: build it with `python -m paper_2607_17644_b200.build`") from missing
     names = ("laga_rope", "laga_latent_norm_rope", "laga_latent_norm_rope_backward_workspace_bytes", "laga_latent_norm_rope_backward",
-             "laga_cache_plan", "laga_paged_decode_workspace_bytes", "laga_paged_decode")
+             "laga_cache_plan", "laga_paged_decode_workspace_bytes", "laga_paged_decode", "laga_cache8_append", "laga_cache8_read",
+             "laga_paged_decode8_workspace_bytes", "laga_paged_decode8")
     module.bind(_check, *(ctypes.cast(getattr(lib(), name), _vp).value for name in names))
     _binding = module
     return module
@@ -488,9 +493,20 @@ def latent_norm_rope(kv_a, gamma, beta, positions, rope, eps=1e-5, latent=None, 
 
 def cache_append(kv_a, gamma, beta, positions, rope, slots, cache, eps=1e-5, stream=None):
     """laga_latent_norm_rope into the cache alone: row slots[m] of cache (bf16 [..., D + R]) receives the normalised latent and
-    the rotated key of kv_a's row m; a slot outside the cache (-1) writes nothing.  Returns cache."""
+    the rotated key of kv_a's row m; a slot outside the cache (-1) writes nothing.  Returns cache.
+    A cache in 8 bits (uint8 [n_pages, page_size * CACHE8_TOKEN], the format in include/laga.h; D = 512, R = 64) receives them as e4m3 codes
+    and a scale: laga_cache8_append."""
     _run("latent_norm_rope", stream, kv_a, gamma, beta, positions, rope, eps, False, None, None, cache, slots)
     return cache
+
+
+CACHE8_TOKEN = 644           # bytes of a token in a cache in 8 bits
+
+
+def cache_read(cache, slots, latent=None, k_pe=None, stream=None):
+    """laga_cache8_read: rows slots[m] (int32 [M]) of a cache in 8 bits (uint8 [n_pages, page_size * CACHE8_TOKEN]) as (latent bf16
+    [M, 512], k_pe bf16 [M, 64]), what ``fwd`` takes as c_kv and k_pe; zeros where a slot is outside the cache (-1)."""
+    return _run("cache_read", stream, cache, slots, latent, k_pe)
 
 
 def latent_norm_rope_backward(dlatent, dk_pe, kv_a, gamma, mean, rstd, positions, rope, with_beta=True, dkv_a=None, workspace=None,
@@ -517,14 +533,16 @@ def cache_plan(seq_lens, new_lens, block_table, free_pages, n_free, page_size, m
     return CachePlan._make(plan) if out is None else plan
 
 
-def paged_decode_workspace_bytes(B, h, d_c=512, d_nope=128, d_rope=64, d_v=128) -> int:
-    return int(lib().laga_paged_decode_workspace_bytes(B, h, d_c, d_nope, d_rope, d_v))
+def paged_decode_workspace_bytes(B, h, d_c=512, d_nope=128, d_rope=64, d_v=128, cache8=False) -> int:
+    """cache8: for a cache in 8 bits."""
+    size = lib().laga_paged_decode8_workspace_bytes if cache8 else lib().laga_paged_decode_workspace_bytes
+    return int(size(B, h, d_c, d_nope, d_rope, d_v))
 
 
 def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, out=None, lse=None, workspace=None, stream=None):
     """laga_paged_decode: attention of one new token per request (q bf16 [B, h, 192], rope band rotated) over a paged cache
-    (bf16 [n_pages, page_size, 576]; block_table int32 [B, columns], seq_lens int32 [B], both on the device).  lse: fp32 [B, h] to
-    have it written.  Returns (out bf16 [B, h, 128], lse or None, workspace); with B = 0 there is nothing to do."""
+    (bf16 [n_pages, page_size, 576]; block_table int32 [B, columns], seq_lens int32 [B], both on the device), or, as
+    laga_paged_decode8, over one in 8 bits (uint8 [n_pages, page_size * CACHE8_TOKEN]).  lse: fp32 [B, h] to have it written.  Returns (out bf16 [B, h, 128], lse or None, workspace); with B = 0 there is nothing to do."""
     return _run("paged_decode", stream, q, w_kv_b, cache, block_table, seq_lens, softmax_scale, out, lse, workspace)
 
 
