@@ -306,7 +306,7 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
  * laga_paged_decode8: laga_paged_decode over such a cache, with its arguments, limits, errors and results, and a workspace of its own size.  The
  *   scale must be a power of two, or zero for a row of zeros.  q W_uk and the rotated queries are carried in two e4m3 parts each, over a power
  *   of two for each request and head (together 2^-8 of a channel, half a step of bf16); so are the probabilities (2^-8; over 32 heads 2^-7, half
- *   a step more), each tile of 128 keys at a reference of its own: weights below 2^-16 of a tile's largest may be dropped.  Sums,
+ *   a step more), each tile of 128 keys at a reference of its own: weights below 2^-12 of a tile's largest may be dropped.  Sums,
  *   references and the accumulator are fp32.
  */
 int laga_cache8_append(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps, const int* positions,

@@ -11,9 +11,10 @@
 // The token's scale belongs to both products: scores are s_t r f (hi + lo) . row_t, and as 2^m p_t c_t = s_t p_t code_t the scale goes
 // into the probability, whose exponent it adds to (it is a power of two):
 //     y_t = score_t log2(e) + log2 s_t,   P_t = 2^(y_t - m),   O = sum P_t code_t,   l = sum P_t / s_t,   out = O / l
-// What e4m3 can hold of P is 2^17, so the reference m is kept near the tile's maximum of y, both ways: where a tile's lies outside (m + 1, m + 8]
-// it becomes that maximum less 5 (never more than 2^40 below its highest: what came before is then all that counts, and the
-// accumulator must not overflow), and O and l are rescaled.  Weights of 2^-16 of a tile's largest are kept with 32 heads.
+// What e4m3 can hold of P is 2^17, so the reference m is kept near the tile's maximum of y, both ways: where a tile's lies outside [m, m + 11]
+// it becomes that maximum less 7 (never more than 2^40 below its highest: what came before is then all that counts, and the
+// accumulator must not overflow), and O and l are rescaled.  Weights of 2^-12 of a tile's largest are kept, and typically
+// of 2^-19.
 //
 // Scores are computed the other way round from the bf16 kernel, S^T[128 keys x (hi, lo columns of the heads)] = K (A) . Q^T (B): the long
 // operand is read from shared memory once for both parts, a thread has all 16 heads' scores of one key, so no reduction is on
@@ -22,8 +23,8 @@
 //
 // Work split: the line of 64-key units of all requests in equal stretches, as there; a tile is two units, or one where a piece ends in an
 // odd one.  A tile is five slabs of 128 keys x 128 codes around a ring with a barrier per slab: the key's first (only scores read it).
-//   warps 0 .. 4g-1  softmax: group w / 4 has heads 16 (w / 4) .., its thread l of warp w % 4 key 32 (w % 4) + l; and the drain
-//   then four warps: first queries; value MMAs; score MMAs; TMA producer
+//   warps 0 .. 4g-1  softmax: group w / 4 has 8 heads (16 where the CTA has 64), its thread l of warp w % 4 key 32 (w % 4) + l; and the drain
+//   then four warps: TMA producer of the latent's last two slabs; value MMAs; score MMAs (and the first queries); TMA producer of the rest
 #pragma once
 #include "attn_decode_sm100.cuh"
 #include "cache8_sm100.cuh"
@@ -32,17 +33,19 @@ namespace laga {
 
 constexpr int kD8Keys = 128;                 // keys of a tile
 constexpr int kD8Unit = kDecKeys;            // keys of a unit of the line
-constexpr float kD8Lift = 5.0f;              // a tile's maximum starts at 2^5
-constexpr float kD8Low = 1.0f, kD8High = 8.0f;
+constexpr float kD8Lift = 7.0f;              // where a tile's maximum is put ...
+constexpr float kD8High = 11.0f;             // ... and the most it may become; the least is 0
 constexpr float kD8Fall = 40.0f;
 constexpr float kD8LoScale = 32.0f;
 
 template <int kHeads>
 struct AttnDecode8Smem {
-    static constexpr int kGroups = kHeads / 16;
+    static constexpr int kPer = kHeads == 64 ? 16 : 8;         // heads of a softmax group
+    static constexpr int kGroups = kHeads / kPer;
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 32 * (kSoftWarps + 4);
     static constexpr bool kSplit = kHeads <= 32;               // both parts of P as columns
+    static constexpr float kDrop = kSplit ? 3.0f : 0.0f;       // P = 2^(d - kDrop): at most 2^8 in e4m3 (hi and 32 times the rest), 2^11 in e5m2 and its rest
     static constexpr int kCols = kSplit ? 2 * kHeads : kHeads; // TMEM columns of 128 latents of O^T
     static constexpr int kPRow = kSplit ? 2 * kHeads : kHeads; // bytes of a key's row of P
     static constexpr int kPTile = kD8Keys * kPRow;
@@ -54,7 +57,7 @@ struct AttnDecode8Smem {
     static constexpr int kP = kQ + 5 * kQSlab;                 // two buffers, or the two parts
     static constexpr int kSlab0 = kP + 2 * kPTile;
     static constexpr int kScale = kSlab0 + kSlabs * kSlab;
-    static constexpr int kRef = kScale + kScales * kD8Keys * 4;    // per head: m, query factor, rescaling factor, highest m, tile maximum
+    static constexpr int kRef = kScale + kScales * kD8Keys * 4;    // per head: m; query factor, step of m and its power, tile maximum (the last four: a piece's sums, a row a warp)
     static constexpr int kVote = kRef + 5 * kHeads * 4;            // [2][groups][4 warps]
     static constexpr int kBar = kVote + 2 * kGroups * 16;
     static constexpr int kBars = 2 * kSlabs + 12 + kScales + kGroups;
@@ -96,13 +99,36 @@ struct Decode8Cursor {
     }
 };
 
-// Floats as integers of the same order (NaN above or below everything), and back.
+// kN values a lane, each reduced over the warp: the halves of the values change sides until a lane has one, value lane / (32 / kN).  (kN plus a
+// few shuffles; the warp-wide reduction instruction is one for each value, but takes some 18 clocks of a unit that the SM's warps share.)
+template <int kN, class Op>
+__device__ __forceinline__ float warp_reduce_each(float (&v)[kN], int lane, Op op) {
+    int dist = 16;
+#pragma unroll
+    for (int n = kN / 2; n > 0; n >>= 1, dist >>= 1) {
+        const bool upper = (lane & dist) != 0;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float out = upper ? v[i] : v[i + n], keep = upper ? v[i + n] : v[i];
+            v[i] = op(keep, __shfl_xor_sync(0xffffffffu, out, dist));
+        }
+    }
+#pragma unroll
+    for (int e = 16 / kN; e > 0; e >>= 1) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], e));
+    return v[0];
+}
+// Floats as integers of the same order, and back.
 __device__ __forceinline__ int ordered(float x) {
     const int i = __float_as_int(x);
     return i ^ ((i >> 31) & 0x7fffffff);
 }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 constexpr int kOrderedLowest = static_cast<int>(0x80000000u);
+template <int kPer>
+__device__ __forceinline__ void tmem_ld_heads(uint32_t taddr, uint32_t* r) {
+    if constexpr (kPer == 16) tmem_ld_x16(taddr, r);
+    else tmem_ld_x8(taddr, r);
+}
 
 template <int kHeads>
 __global__ void __launch_bounds__(AttnDecode8Smem<kHeads>::kThreads, 1)
@@ -131,14 +157,14 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
     int* start_t = start_b + 1;
     int* scan = start_b + 2;                          // per-warp sums of the unit counts
     float* ref_s = reinterpret_cast<float*>(smem + L::kRef);
-    float *factor_s = ref_s + kHeads, *alpha_s = factor_s + kHeads, *peak_s = alpha_s + kHeads;
-    int* top_s = reinterpret_cast<int*>(peak_s + kHeads);
+    float *factor_s = ref_s + kHeads, *step_s = factor_s + kHeads, *alpha_s = step_s + kHeads;
+    int* top_s = reinterpret_cast<int*>(alpha_s + kHeads);
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int group = static_cast<int>(blockIdx.x) % args.n_groups;
     const int cta = static_cast<int>(blockIdx.x) / args.n_groups;
     const int head0 = group * kHeads;
-    constexpr int kQueryWarp = L::kSoftWarps, kValueWarp = kQueryWarp + 1, kScoreWarp = kQueryWarp + 2, kProducerWarp = kQueryWarp + 3;
+    constexpr int kProducerWarp2 = L::kSoftWarps, kValueWarp = kProducerWarp2 + 1, kScoreWarp = kProducerWarp2 + 2, kProducerWarp = kProducerWarp2 + 3;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < L::kSlabs; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
@@ -152,7 +178,6 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         mbar_fence_init();
         tma_prefetch_desc(&tmap_q); tma_prefetch_desc(&tmap_codes);
     }
-    if (threadIdx.x < kHeads) top_s[threadIdx.x] = kOrderedLowest;
     if (warp == kScoreWarp) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
@@ -206,91 +231,116 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             tma_load_2d_chk(args.status, smem + L::kQ + k * L::kQSlab, &tmap_q, q_full, k * 128, 2 * (b * args.h_pad + head0));
     };
 
+    // ---- producers: boxes of min(page, 64) keys, kSubs of them a slab ----------------------------------------
+    // Two lanes share a tile's slabs.  What limits them is their instruction count -- a lane beside busy softmax warps runs at four to six
+    // clocks an instruction, a copy's operands go through uniform registers -- so addresses are plain words, and what is in flight is worked
+    // out only where a wait has given up.  kFirst: the lane with the key's slab, the latent's first two, the scales and the queries.
+    auto produce = [&](auto subs, auto first_half) {
+        constexpr int kSubs = decltype(subs)::value, kBox = kD8Keys / kSubs;
+        constexpr bool kFirst = decltype(first_half)::value;
+        constexpr uint32_t kBegin = kFirst ? 0 : 3, kCount = kFirst ? 3 : 2;
+        const uint64_t once = args.n_groups == 1 ? l2_evict_first() : l2_evict_normal();      // (head groups read a tile one after another)
+        const int shift = args.page_shift, in_page = (1 << shift) - 1, n_pages = args.n_pages;
+        const uint32_t full_a = smem_u32(full), empty_a = smem_u32(empty), slab_a = smem_u32(smem + L::kSlab0);
+        int pages[kSubs], pages_next[kSubs];                 // of the tile's boxes; a tile ahead
+        auto fetch_pages = [&](const Decode8Cursor& c, int* p) {
+            if (c.done()) return;
+            const int* row = args.block_table + static_cast<size_t>(c.b) * args.columns;
+            const int k0 = c.t * kD8Unit;
+#pragma unroll
+            for (int i = 0; i < kSubs; ++i) p[i] = k0 + i * kBox < c.len ? __ldg(row + ((k0 + i * kBox) >> shift)) : 0;
+        };
+        Decode8Cursor cur(args, my_units, first_b, first_t);
+        fetch_pages(cur, pages);
+        uint32_t slot = kBegin, par = 0, pieces = 0, T = 0;
+        bool new_piece = true, ok = true;
+        while (!cur.done()) {
+            Decode8Cursor next = cur;
+            next.next(args);
+            fetch_pages(next, pages_next);
+            const int boxes = (cur.valid() + kBox - 1) / kBox, row0 = (cur.t * kD8Unit) & in_page;       // boxes of this tile that hold a key
+            float* scales = reinterpret_cast<float*>(smem + L::kScale) + (T % L::kScales) * kD8Keys;
+            bool all_there = true;
+#pragma unroll
+            for (int i = 0; i < kSubs; ++i) all_there = all_there && static_cast<uint32_t>(pages[i]) < static_cast<uint32_t>(n_pages);
+            uint32_t there = static_cast<uint32_t>(boxes);   // boxes whose page is one
+            if (!all_there) {
+#pragma unroll
+                for (int i = 0; i < kSubs; ++i) {
+                    if (i >= boxes || static_cast<uint32_t>(pages[i]) < static_cast<uint32_t>(n_pages)) continue;
+                    pages[i] = n_pages;                      // out of the map's range: TMA fills zeros
+                    --there;
+                    atomicCAS(args.status, kStatusOk, kStatusCheck | 0xF2u);
+                    if (kFirst) {
+                        for (int k = 0; k < kBox; ++k) scales[i * kBox + k] = 1.0f;
+                        fence_async_shared();
+                    }
+                }
+            }
+            if constexpr (!kFirst && L::kSlabs < 10) {       // less than two tiles: the last slab waits for the values of the tile before
+#pragma unroll
+                for (int i = 0; i < kSubs; ++i)
+                    if (i < boxes) tma_prefetch_codes(&tmap_codes, 3 * 128, (row0 + i * kBox) & in_page, pages[i]);
+            }
+#pragma unroll
+            for (uint32_t s = 0; s < kCount; ++s) {          // the key's slab, then the latent's four
+                const uint32_t bar = full_a + slot * 8;
+                if (!mbar_test_wait_u32(empty_a + slot * 8, par ^ 1u)) ok = mbar_wait(&empty[slot], par ^ 1u, abort_flag, args.status, 0x80);
+                if (!ok) break;
+                mbar_arrive_expect_tx_u32(bar, boxes * (kBox * 128));
+                const uint32_t dst = slab_a + slot * L::kSlab;
+                const int channel = kBegin + s == 0 ? kC8Lat : static_cast<int>(kBegin + s - 1) * 128;
+#pragma unroll
+                for (int i = 0; i < kSubs; ++i)
+                    if (i < boxes) tma_load_codes_chk(args.status, dst + i * (kBox * 128), &tmap_codes, bar, channel, (row0 + i * kBox) & in_page, pages[i], once);
+                if (kFirst && s == 0) {
+                    uint64_t* c_bar = &c_full[T % L::kScales];
+                    mbar_arrive_expect_tx(c_bar, there * (kBox * 4));
+#pragma unroll
+                    for (int i = 0; i < kSubs; ++i)
+                        if (i < boxes && pages[i] < n_pages)
+                            bulk_load(scales + i * kBox, all.cache.base + pages[i] * all.cache.page_bytes() + (static_cast<size_t>(kC8Row) << shift) +
+                                      ((row0 + i * kBox) & in_page) * 4, kBox * 4, c_bar);
+                }
+                slot += s + 1 < kCount ? 1u : 6u - kCount;
+                if (slot >= L::kSlabs) { slot -= L::kSlabs; par ^= 1u; }
+            }
+            if (!ok) break;
+            // a piece's queries after its first tile: they wait for the last scores of the piece before (the first are the score warp's)
+            if (kFirst && new_piece) {
+                if (pieces > 0) ok = mbar_wait(q_empty, (pieces & 1u) ^ 1u, abort_flag, args.status, 0x81);
+                if (!ok) break;
+                if (pieces > 0) fetch_queries(cur.b);
+                ++pieces;
+            }
+            new_piece = cur.ends_piece();
+            cur = next;
+#pragma unroll
+            for (int i = 0; i < kSubs; ++i) pages[i] = pages_next[i];
+            ++T;
+        }
+        // What a lane has armed is complete when every barrier has left the phase that it was armed for last: slots behind `slot` are a round
+        // behind.  (A barrier that was never armed, or is the other lane's, costs the limit at most.)
+        if (abort_flag->value != 0u) {
+            for (uint32_t i = 0; i < L::kSlabs; ++i) mbar_wait_quiesce(&full[i], i < slot ? par : par ^ 1u);
+            if (kFirst) {
+                for (uint32_t k = 1; k <= L::kScales && k <= T; ++k) mbar_wait_quiesce(&c_full[(T - k) % L::kScales], ((T - k) / L::kScales) & 1u);
+                if (pieces > 0) mbar_wait_quiesce(q_full, (pieces - 1) & 1u);
+            }
+        }
+    };
+    auto produce_half = [&](auto first_half) {
+        if (args.page_shift >= 6) produce(std::integral_constant<int, 2>{}, first_half);
+        else if (args.page_shift == 5) produce(std::integral_constant<int, 4>{}, first_half);
+        else produce(std::integral_constant<int, 8>{}, first_half);
+    };
+
     if (abort_flag->value != 0u || my_units <= 0) {
         // nothing to do (or nothing may be done): fall through to the common exit
     } else if (warp == kProducerWarp) {
-        // ---- producer: a lane per box of min(page, 64) keys -------------------------------------------------
-        // Lane l also keeps the page of box l of the next 32.
-        const uint64_t once = l2_evict_first();
-        const int shift = args.page_shift, box_shift = min(shift, 6), box = 1 << box_shift, n_sub = kD8Keys >> box_shift;
-        auto page_of = [&](const Decode8Cursor& c, int i) -> int {
-            const long long key = static_cast<long long>(i) << box_shift;
-            if (key >= c.len) return args.n_pages;                             // beyond the request: never issued
-            const int page = __ldg(args.block_table + static_cast<size_t>(c.b) * args.columns + (key >> shift));
-            if (page >= 0 && page < args.n_pages) return page;
-            atomicCAS(args.status, kStatusOk, kStatusCheck | 0xF2u);           // a bad entry: zeros, and a status
-            return args.n_pages;                                               // out of the map's range: TMA fills zeros
-        };
-        ArmedBarriers armed(bars);
-        Decode8Cursor cur(args, my_units, first_b, first_t);
-        uint32_t slot = 0, par = 0, pieces = 0, T = 0;
-        bool new_piece = true, ok = true;
-        int batch = 0, page_cur = 0, page_next = 0;          // first box of the batch; pages of box batch + lane and batch + 32 + lane
-        while (!cur.done()) {
-            const int first = cur.t << (6 - box_shift);
-            if (new_piece) {
-                batch = first;
-                page_cur = page_of(cur, batch + lane);
-                page_next = page_of(cur, batch + 32 + lane);
-            }
-            if (first - batch >= 32) {
-                batch += 32;
-                page_cur = page_next;
-                page_next = page_of(cur, batch + 32 + lane);
-            }
-            const int boxes = (cur.valid() + box - 1) >> box_shift;                 // boxes of this tile that hold a key
-            const int page = __shfl_sync(0xffffffffu, page_cur, first - batch + (lane & (n_sub - 1)));
-            const int row = ((first + lane) << box_shift) & ((1 << shift) - 1);
-            const bool there = page < args.n_pages;
-            const uint32_t bytes = static_cast<uint32_t>(boxes) << (box_shift + 7);
-            const uint32_t scale_bytes = __popc(__ballot_sync(0xffffffffu, lane < boxes && there)) << (box_shift + 2);
-            uint64_t* c_bar = &c_full[T % L::kScales];
-            float* scales = reinterpret_cast<float*>(smem + L::kScale) + (T % L::kScales) * kD8Keys + (lane << box_shift);
-#pragma unroll 1
-            for (int s = 0; s < 5; ++s) {                    // the key's slab, then the latent's four
-                ok = mbar_wait_warp(&empty[slot], par ^ 1u, abort_flag, args.status, 0x80);
-                if (!ok) break;
-                if (s == 0 && lane < boxes && !there) {
-                    for (int i = 0; i < box; ++i) scales[i] = 1.0f;
-                    fence_async_shared();
-                }
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive_expect_tx(&full[slot], bytes);
-                    armed.arm(&full[slot], par);
-                    if (s == 0) {
-                        mbar_arrive_expect_tx(c_bar, scale_bytes);
-                        armed.arm(c_bar, T / L::kScales);
-                    }
-                }
-                __syncwarp();
-                if (lane < boxes) {
-                    tma_load_codes_chk(args.status, smem + L::kSlab0 + slot * L::kSlab + (lane << (box_shift + 7)), &tmap_codes, &full[slot],
-                                       s == 0 ? kC8Lat : (s - 1) * 128, row, page, once);
-                    if (s == 0 && there)
-                        bulk_load(scales, all.cache.base + page * all.cache.page_bytes() + (static_cast<size_t>(kC8Row) << shift) + row * 4, box * 4, c_bar);
-                }
-                if (++slot == L::kSlabs) { slot = 0; par ^= 1u; }
-            }
-            // a piece's queries after its first tile: they wait for the last scores of the piece before (the first are the query warp's)
-            if (ok && new_piece) {
-                if (lane == 0 && pieces > 0) {
-                    ok = mbar_wait(q_empty, (pieces & 1u) ^ 1u, abort_flag, args.status, 0x81);
-                    if (ok) fetch_queries(cur.b);
-                }
-                if (lane == 0 && ok) armed.arm(q_full, pieces);
-                ++pieces;
-            }
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            new_piece = cur.ends_piece();
-            cur.next(args);
-            ++T;
-        }
-        __syncwarp();
-        if (lane == 0 && abort_flag->value != 0u) armed.quiesce();
-    } else if (warp == kQueryWarp) {
-        if (elect_one()) fetch_queries(first_b);             // (a unit of first_b is here, so it is the first request with tokens)
+        if (elect_one()) produce_half(std::true_type{});
+    } else if (warp == kProducerWarp2) {
+        if (elect_one()) produce_half(std::false_type{});
     } else if (warp == kScoreWarp) {
         // ---- issuer of the score MMAs ------------------------------------------------------------------------
         if (elect_one()) {
@@ -299,6 +349,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                            hi = desc_hi(desc_k_major(0));
             uint32_t slot = 0, par = 0, pieces = 0;
             bool ok = true, new_piece = true;
+            fetch_queries(first_b);                          // (a unit of first_b is here, so it is the first request with tokens)
             Decode8Cursor cur(args, my_units, first_b, first_t);
             for (uint32_t T = 0; !cur.done(); ++T) {
                 const uint32_t buf = T & 1u, d = tmem_s + buf * (2 * kHeads);
@@ -307,14 +358,18 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 if (!ok) break;
                 new_piece = cur.ends_piece();
                 cur.next(args);
+                // A barrier probe queues behind the lane's MMAs until the tensor pipe has taken them, so the next slab's is made before this one's.
+                bool here = mbar_test_wait(&full[slot], par);
 #pragma unroll 1
                 for (int s = 0; s < 5; ++s) {
-                    ok = mbar_wait(&full[slot], par, abort_flag, args.status, 0x84);
+                    if (!here) ok = mbar_wait(&full[slot], par, abort_flag, args.status, 0x84);
                     if (!ok) break;
-                    tc_fence_after_sync();
-                    mma8_ss_chain4<2, 2>(d, k_lo + slot * (L::kSlab / 16), hi, q_lo + (s == 0 ? 4 : s - 1) * (L::kQSlab / 16), hi, idesc, s > 0 ? 1u : 0u);
-                    if (s == 0) mma_commit(&empty[slot]);
+                    const uint32_t at = slot;
                     if (++slot == L::kSlabs) { slot = 0; par ^= 1u; }
+                    if (s < 4) here = mbar_test_wait(&full[slot], par);
+                    tc_fence_after_sync();
+                    mma8_ss_chain4<2, 2>(d, k_lo + at * (L::kSlab / 16), hi, q_lo + (s == 0 ? 4 : s - 1) * (L::kQSlab / 16), hi, idesc, s > 0 ? 1u : 0u);
+                    if (s == 0) mma_commit(&empty[at]);
                 }
                 if (!ok) break;
                 mma_commit(&s_full[buf]);
@@ -368,179 +423,224 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         }
     } else if (warp < L::kSoftWarps) {
         // ---- softmax, rescaling, drain -----------------------------------------------------------------------
+        constexpr int kPer = L::kPer, kPairs = kPer / 2, kShare = 32 / kPer;
         const int g = warp >> 2, quarter = warp & 3, key = quarter * 32 + lane, tid = key;      // (thread of the group)
-        const int h0 = g * 16;                                 // the group's heads within the CTA's
-        const int n_live = max(0, min(16, args.h - head0 - h0));
-        const uint32_t live = (1u << n_live) - 1u;
+        const int h0 = g * kPer;                               // the group's heads within the CTA's
+        const int n_live = max(0, min(kPer, args.h - head0 - h0));
+        const uint32_t live = (1u << n_live) - 1u;             // bit i: the group's head i is one
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t col_o = tmem_base + lane_addr + (L::kSplit ? g * 32 : g * 16);
+        // sixteen heads' scores are 32 columns, first the products with hi, then those with lo; so are their columns of O^T where P has two parts
+        const uint32_t sixteen = static_cast<uint32_t>(h0 >> 4), within = static_cast<uint32_t>(h0 & 15);
+        const uint32_t col_s = tmem_s + lane_addr + sixteen * 32 + within, col_o = tmem_base + lane_addr + (L::kSplit ? sixteen * 32 + within : h0);
         int* vote_s = reinterpret_cast<int*>(smem + L::kVote) + g * 4;
-        F2 l2[8];                                              // this key's part of the sums
+        float* lsum_s = factor_s;                              // [4 warps][kHeads], where a piece's per-head words are no longer needed
+        F2 l2[kPairs];                                         // this key's part of the sums
         uint32_t T = 0, pieces = 0, pos = 0, meetings = 0;     // pos: the tile's first slab
-        bool ok = true, first = true;
-        auto meet = [&]() -> bool {                            // the group's four warps, and what they wrote to shared memory
+        bool ok = true, first = true, seen = false;            // seen, peak: of the group's head `tid`, whether some key had a weight, and its highest m
+        float peak = kDecLowest;
+        auto arrive = [&]() {                                  // the group's four warps meet: what they wrote to shared memory is there
             __syncwarp();
             if (lane == 0) mbar_arrive(&group_bar[g]);
-            return mbar_wait_warp(&group_bar[g], meetings++ & 1u, abort_flag, args.status, 0x87);
         };
+        auto wait_for_group = [&]() -> bool { return mbar_wait_warp(&group_bar[g], meetings++ & 1u, abort_flag, args.status, 0x87); };
         Decode8Cursor cur(args, my_units, first_b, first_t);
+        auto query_scale = [&](const Decode8Cursor& c) -> float {
+            return tid < n_live && !c.done() ? __ldg(all.q_scale + static_cast<size_t>(c.b) * args.h_pad + head0 + h0 + tid) * args.scale_log2 : 0.f;
+        };
         grid_dependency_wait();
+        float factor = query_scale(cur);
         while (!cur.done()) {
             const uint32_t buf = T & 1u, par = (T >> 1) & 1u;
             const int valid = cur.valid();
             if (first) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) l2[i] = f2(0.f, 0.f);
-                if (tid < 16) {
-                    ref_s[h0 + tid] = peak_s[h0 + tid] = kDecLowest;
-                    factor_s[h0 + tid] = __ldg(all.q_scale + static_cast<size_t>(cur.b) * args.h_pad + head0 + h0 + tid) * args.scale_log2;
+                for (int i = 0; i < kPairs; ++i) l2[i] = f2(0.f, 0.f);
+                if (tid < kPer) {
+                    factor_s[h0 + tid] = factor;
+                    ref_s[h0 + tid] = tid < n_live ? 0.f : 1e30f;        // (a head that is none: every weight zero, and no rescaling for it)
+                    top_s[h0 + tid] = kOrderedLowest;
                 }
-                if (!meet()) break;
+                seen = false;
+                peak = kDecLowest;
+                arrive();
+                if (!wait_for_group()) break;
             }
-            ok = mbar_wait_warp(&c_full[T % L::kScales], (T / L::kScales) & 1u, abort_flag, args.status, 0x88);
-            if (ok) ok = mbar_wait_warp(&s_full[buf], par, abort_flag, args.status, 0x89);
-            if (!ok) break;
+            {
+                // (asked together: an answer takes some 90 clocks even where it is yes)
+                const bool scales = mbar_test_wait(&c_full[T % L::kScales], (T / L::kScales) & 1u), scores = mbar_test_wait(&s_full[buf], par);
+                if (!__all_sync(0xffffffffu, scales && scores)) {
+                    ok = mbar_wait_warp(&c_full[T % L::kScales], (T / L::kScales) & 1u, abort_flag, args.status, 0x88);
+                    if (ok) ok = mbar_wait_warp(&s_full[buf], par, abort_flag, args.status, 0x89);
+                    if (!ok) break;
+                }
+            }
             tc_fence_after_sync();
-            F2 y[8];
+            // d = y - m
+            F2 d[kPairs];
             float s = reinterpret_cast<const float*>(smem + L::kScale)[(T % L::kScales) * kD8Keys + key];
             {
-                uint32_t raw[32];
-                tmem_ld_x32(tmem_s + buf * (2 * kHeads) + g * 32 + lane_addr, raw);
+                uint32_t hi[kPer], lo[kPer];
+                tmem_ld_heads<kPer>(col_s + buf * (2 * kHeads), hi);
+                tmem_ld_heads<kPer>(col_s + buf * (2 * kHeads) + 16, lo);
                 if (key >= valid) s = 1.0f;
-                const uint32_t e = __float_as_uint(s) >> 23 & 0xffu;
-                const float ef = static_cast<float>(static_cast<int>(e) - 127);
+                const float ef = static_cast<float>(static_cast<int>(__float_as_uint(s) >> 23 & 0xffu) - 127);
+                const F2 s2 = f2(s, s), e2 = f2(ef, ef), minus1 = f2(-1.0f, -1.0f);
+                const ulonglong2 *f = reinterpret_cast<const ulonglong2*>(factor_s + h0), *m = reinterpret_cast<const ulonglong2*>(ref_s + h0);
                 tmem_ld_wait();
-                const F2 s2 = f2(s, s), e2 = f2(ef, ef);
-                const ulonglong2* f = reinterpret_cast<const ulonglong2*>(factor_s + h0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const ulonglong2 f4 = f[i];
+                for (int i = 0; i < kPairs; i += 2) {
+                    const ulonglong2 f4 = f[i >> 1], m4 = m[i >> 1];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const int c = 4 * i + 2 * j;
-                        const F2 both = f2_add(f2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), f2(__uint_as_float(raw[16 + c]), __uint_as_float(raw[17 + c])));
-                        y[2 * i + j] = f2_fma(f2_mul(both, s2), F2{j == 0 ? f4.x : f4.y}, e2);
+                        const int c = 2 * (i + j);
+                        const F2 both = f2_add(f2(__uint_as_float(hi[c]), __uint_as_float(hi[c + 1])), f2(__uint_as_float(lo[c]), __uint_as_float(lo[c + 1])));
+                        // (y rounded before m is taken off: the largest score of a tile is then at its place whatever its size)
+                        const F2 y = f2_fma(f2_mul(both, s2), F2{j == 0 ? f4.x : f4.y}, e2);
+                        d[i + j] = f2_fma(F2{j == 0 ? m4.x : m4.y}, minus1, y);
                     }
                 }
             }
             if (key >= valid) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = f2(-INFINITY, -INFINITY);
+                for (int i = 0; i < kPairs; ++i) d[i] = f2(-INFINITY, -INFINITY);
             }
-            // Does the reference hold?  For every head some key must lie above m + 1, and none above m + 8.
-            {
-                const ulonglong2* m = reinterpret_cast<const ulonglong2*>(ref_s + h0);
-                uint32_t above = 0u;
+            // Does the reference hold?  For every head some key must have d >= 0, and none more than kD8High: a bit a head, and the last.  (A piece's
+            // first tile has no reference yet.)
+            if (!first) {
+                uint32_t held = 0u;
                 float most = -INFINITY;
-                const F2 minus1 = f2(-1.0f, -1.0f);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const ulonglong2 m4 = m[i];
+                for (int i = 0; i < kPairs; ++i) {
+                    const float2 v = f2_parts(d[i]);
+                    held |= __any_sync(0xffffffffu, v.x >= 0.f) ? 1u << (2 * i) : 0u;
+                    held |= __any_sync(0xffffffffu, v.y >= 0.f) ? 2u << (2 * i) : 0u;
+                    most = fmax3(most, v.x, v.y);
+                }
+                held |= __any_sync(0xffffffffu, most > kD8High) ? 1u << 16 : 0u;
+                if (lane == 0) vote_s[buf * (4 * L::kGroups) + quarter] = static_cast<int>(held);
+                arrive();
+            }
+            // Probabilities and their parts, while the group's other warps vote
+            F2 p[kPairs];
+            uint32_t hi[kPer / 4], lo[kPer / 4];
+            auto weigh = [&]() {
+#pragma unroll
+                for (int i = 0; i < kPer / 4; ++i) {
+                    uint32_t a[2], b[2];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float2 d = f2_parts(f2_fma(F2{j == 0 ? m4.x : m4.y}, minus1, y[2 * i + j]));
-                        above |= (d.x > kD8Low ? 1u : 0u) << (4 * i + 2 * j);
-                        above |= (d.y > kD8Low ? 1u : 0u) << (4 * i + 2 * j + 1);
-                        if (4 * i + 2 * j < n_live) most = fmaxf(most, d.x);
-                        if (4 * i + 2 * j + 1 < n_live) most = fmaxf(most, d.y);
+                        const float2 v = f2_parts(L::kSplit ? f2_add(d[2 * i + j], f2(-L::kDrop, -L::kDrop)) : d[2 * i + j]);
+                        const float2 w = make_float2(fast_exp2(v.x), fast_exp2(v.y));
+                        p[2 * i + j] = f2(w.x, w.y);
+                        const __half2 ph = __floats2half2_rn(w.x, w.y);
+                        const uint32_t p16 = *reinterpret_cast<const uint32_t*>(&ph);
+                        a[j] = L::kSplit ? e4m3x2_of_half2(p16) : e5m2x2_of_half2(p16);
+                        const uint32_t held = L::kSplit ? half2_of_e4m3x2(a[j]) : half2_of_e5m2x2(a[j]);
+                        __half2 rest = __hsub2(ph, *reinterpret_cast<const __half2*>(&held));
+                        if constexpr (L::kSplit) rest = __hmul2(rest, __float2half2_rn(kD8LoScale));
+                        b[j] = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&rest));
+                    }
+                    hi[i] = __byte_perm(a[0], a[1], 0x5410);
+                    lo[i] = __byte_perm(b[0], b[1], 0x5410);
+                }
+            };
+            if (!first) weigh();
+            // (asked now: P's buffer, whose last use must have been multiplied)
+            const uint32_t prev = T - (L::kSplit ? 2 : 1);
+            const bool has_prev = T >= (L::kSplit ? 2 : 1), p_free = !has_prev || mbar_test_wait(&pv_done[prev & 1u], (prev >> 1) & 1u);
+            bool holds = false;
+            if (!first) {
+                if (!wait_for_group()) break;
+                const int4 votes = *reinterpret_cast<const int4*>(vote_s + buf * (4 * L::kGroups));
+                const uint32_t held = static_cast<uint32_t>(votes.x | votes.y | votes.z | votes.w);
+                holds = (held >> 16) == 0u && (held & live) == live;
+            }
+            if (!holds) {
+                // The heads' maxima over the tile, then the references they ask for.
+                float tops[kPer];
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    const float2 v = f2_parts(d[i]);
+                    tops[2 * i] = v.x;
+                    tops[2 * i + 1] = v.y;
+                }
+                const float most = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
+                if ((lane & (kShare - 1)) == 0) atomicMax(&top_s[h0 + lane / kShare], ordered(most));
+                arrive();
+                if (!wait_for_group()) break;
+                if (tid < kPer) {
+                    const float top = unordered(top_s[h0 + tid]), m = ref_s[h0 + tid];
+                    top_s[h0 + tid] = kOrderedLowest;
+                    if (seen) peak = fmaxf(peak, m);
+                    float to = m;
+                    if (tid < n_live && top > -INFINITY && !(top >= 0.f && top <= kD8High)) to = fmaxf(m + (top - kD8Lift), peak - kD8Fall);
+                    ref_s[h0 + tid] = to;
+                    step_s[h0 + tid] = to - m;                 // (the step that was taken, with the sum's rounding)
+                    alpha_s[h0 + tid] = fast_exp2(m - to);
+                    seen = seen || top > -INFINITY;
+                }
+                arrive();
+                if (!wait_for_group()) break;
+                const ulonglong2 *step = reinterpret_cast<const ulonglong2*>(step_s + h0), *alpha = reinterpret_cast<const ulonglong2*>(alpha_s + h0);
+                const F2 minus1 = f2(-1.0f, -1.0f);
+#pragma unroll
+                for (int i = 0; i < kPairs; i += 2) {
+                    const ulonglong2 t4 = step[i >> 1], a4 = alpha[i >> 1];
+                    d[i] = f2_fma(F2{t4.x}, minus1, d[i]);
+                    d[i + 1] = f2_fma(F2{t4.y}, minus1, d[i + 1]);
+                    if (!first) {
+                        l2[i] = f2_mul(l2[i], F2{a4.x});
+                        l2[i + 1] = f2_mul(l2[i + 1], F2{a4.y});
                     }
                 }
-                above |= (most > kD8High ? 1u : 0u) << 16;
-                above = __reduce_or_sync(0xffffffffu, above);
-                if (lane == 0) vote_s[buf * (4 * L::kGroups) + quarter] = static_cast<int>(above);
-            }
-            if (!meet()) break;
-            const int4 votes = *reinterpret_cast<const int4*>(vote_s + buf * (4 * L::kGroups));
-            const uint32_t vote = static_cast<uint32_t>(votes.x | votes.y | votes.z | votes.w);
-            if ((vote & 0x10000u) != 0u || (vote & live) != live) {
-                // The heads' maxima over the tile, then the references they ask for.
-                int mine = kOrderedLowest;
-#pragma unroll
-                for (int h = 0; h < 16; ++h) {
-                    const float2 v = f2_parts(y[h >> 1]);
-                    const int most = __reduce_max_sync(0xffffffffu, ordered((h & 1) ? v.y : v.x));
-                    if (lane == h) mine = most;
-                }
-                if (lane < 16) atomicMax(&top_s[h0 + lane], mine);
-                if (!meet()) break;
-                if (tid < 16) {
-                    const float top = unordered(top_s[h0 + tid]), m = ref_s[h0 + tid], peak = peak_s[h0 + tid];
-                    top_s[h0 + tid] = kOrderedLowest;
-                    float to = m;
-                    if (top > -INFINITY && !(top - m > kD8Low && top - m <= kD8High)) to = fmaxf(top - kD8Lift, peak - kD8Fall);
-                    alpha_s[h0 + tid] = to == m ? 1.0f : fast_exp2(m - to);
-                    ref_s[h0 + tid] = to;
-                    peak_s[h0 + tid] = fmaxf(peak, to);
-                }
-                if (!meet()) break;
-                const float* alpha = alpha_s + h0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) l2[i] = f2_mul(l2[i], f2(alpha[2 * i], alpha[2 * i + 1]));
+                weigh();
                 if (!first) {
                     // O^T is at rest once the values of the tile before have been multiplied; this tile's wait for p_full below
                     ok = mbar_wait_warp(&pv_done[(T - 1) & 1u], ((T - 1) >> 1) & 1u, abort_flag, args.status, 0x8A);
                     if (!ok) break;
                     tc_fence_after_sync();
 #pragma unroll 1
-                    for (int c = 0; c < 4 * L::kCols; c += L::kCols) {
-#pragma unroll 1
-                        for (int part = 0; part < (L::kSplit ? 2 : 1); ++part) {
-                            uint32_t o[16];
-                            tmem_ld_x16(col_o + c + part * 16, o);
-                            tmem_ld_wait();
+                    for (int h = 0; h < kPer; ++h) {           // (mostly one head's reference has moved: its columns alone)
+                        if (step_s[h0 + h] == 0.f) continue;   // (the same for the whole group)
+                        const float by = alpha_s[h0 + h];
+                        uint32_t o[4], rest[4];
 #pragma unroll
-                            for (int v = 0; v < 16; ++v) o[v] = __float_as_uint(__uint_as_float(o[v]) * alpha[v]);
-                            tmem_st_x16(col_o + c + part * 16, o);
+                        for (int c = 0; c < 4; ++c) {
+                            tmem_ld_x1(col_o + c * L::kCols + h, &o[c]);
+                            if constexpr (L::kSplit) tmem_ld_x1(col_o + c * L::kCols + 16 + h, &rest[c]);
+                        }
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            tmem_st_x1(col_o + c * L::kCols + h, __float_as_uint(__uint_as_float(o[c]) * by));
+                            if constexpr (L::kSplit) tmem_st_x1(col_o + c * L::kCols + 16 + h, __float_as_uint(__uint_as_float(rest[c]) * by));
                         }
                     }
                     tmem_st_wait();
                 }
+            } else {
+                seen = true;
             }
-            // Probabilities and their parts
-            uint32_t hi[4], lo[4];
             {
                 const float inv = __uint_as_float((254u - min(254u, __float_as_uint(s) >> 23 & 0xffu)) << 23);      // 1 / s
-                const F2 inv2 = f2(inv, inv), minus1 = f2(-1.0f, -1.0f);
-                const ulonglong2* m = reinterpret_cast<const ulonglong2*>(ref_s + h0);
+                const F2 inv2 = f2(inv, inv);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const ulonglong2 m4 = m[i];
-                    uint32_t a[2], b[2];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float2 d = f2_parts(f2_fma(F2{j == 0 ? m4.x : m4.y}, minus1, y[2 * i + j]));
-                        const float2 p = make_float2(fast_exp2(d.x), fast_exp2(d.y));
-                        l2[2 * i + j] = f2_fma(f2(p.x, p.y), inv2, l2[2 * i + j]);
-                        const __half2 ph = __floats2half2_rn(p.x, p.y);
-                        const uint32_t p16 = *reinterpret_cast<const uint32_t*>(&ph);
-                        if constexpr (L::kSplit) {
-                            a[j] = e4m3x2_of_half2(p16);
-                            const uint32_t h16 = half2_of_e4m3x2(a[j]);
-                            const __half2 rest = __hmul2(__hsub2(ph, *reinterpret_cast<const __half2*>(&h16)), __float2half2_rn(kD8LoScale));
-                            b[j] = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&rest));
-                        } else {
-                            a[j] = e5m2x2_of_half2(p16);
-                            const uint32_t h16 = half2_of_e5m2x2(a[j]);
-                            const __half2 rest = __hsub2(ph, *reinterpret_cast<const __half2*>(&h16));
-                            b[j] = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&rest));
-                        }
-                    }
-                    hi[i] = a[0] | (a[1] << 16);
-                    lo[i] = b[0] | (b[1] << 16);
-                }
+                for (int i = 0; i < kPairs; ++i) l2[i] = f2_fma(p[i], inv2, l2[i]);
             }
-            // the buffer's last use has been multiplied
-            if (L::kSplit ? T >= 2 : T >= 1) {
-                const uint32_t prev = T - (L::kSplit ? 2 : 1);
+            if (!__all_sync(0xffffffffu, p_free)) {
                 ok = mbar_wait_warp(&pv_done[prev & 1u], (prev >> 1) & 1u, abort_flag, args.status, 0x8B);
                 if (!ok) break;
             }
             {
                 uint8_t* row = smem + L::kP + (L::kSplit ? buf * L::kPTile : 0) + key * L::kPRow;
                 const int turn = L::kPRow == 32 ? (key >> 2) & 1 : (key >> 1) & 3;
-                const int c_hi = L::kSplit ? 2 * g : g, c_lo = L::kSplit ? 2 * g + 1 : g;
-                *reinterpret_cast<uint4*>(row + ((c_hi ^ turn) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                *reinterpret_cast<uint4*>(row + (L::kSplit ? 0 : L::kPTile) + ((c_lo ^ turn) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                if constexpr (L::kSplit) {                     // sixteen heads: a chunk of hi, a chunk of lo; this group's are half of each
+                    *reinterpret_cast<uint2*>(row + (((2 * sixteen) ^ turn) << 4) + within) = make_uint2(hi[0], hi[1]);
+                    *reinterpret_cast<uint2*>(row + (((2 * sixteen + 1) ^ turn) << 4) + within) = make_uint2(lo[0], lo[1]);
+                } else {
+                    *reinterpret_cast<uint4*>(row + ((g ^ turn) << 4)) = make_uint4(hi[0], hi[1], hi[kPer / 4 - 2], hi[kPer / 4 - 1]);
+                    *reinterpret_cast<uint4*>(row + L::kPTile + ((g ^ turn) << 4)) = make_uint4(lo[0], lo[1], lo[kPer / 4 - 2], lo[kPer / 4 - 1]);
+                }
             }
             if (g == 0 && (valid & 31)) {     // rows of the last 32-key step that no token owns: zero, whatever the page holds (0 * NaN is NaN)
                 const int n_zero = 32 - (valid & 31);
@@ -556,52 +656,64 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             __syncwarp();
             if (lane == 0) mbar_arrive(&p_full[buf]);
             first = false;
-            if (cur.ends_piece()) {
+            const bool ends = cur.ends_piece();
+            const int b = cur.b;
+            cur.next(args);
+            if (ends) {
+                factor = query_scale(cur);                     // the next piece's, on its way meanwhile
+                // the sums over the 128 keys, within the warp
+                float sums[kPer];
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    const float2 v = f2_parts(l2[i]);
+                    sums[2 * i] = v.x;
+                    sums[2 * i + 1] = v.y;
+                }
+                const float sum = warp_reduce_each(sums, lane, [](float x, float y) { return x + y; });
                 ok = mbar_wait_warp(o_full, pieces & 1u, abort_flag, args.status, 0x8C);
                 if (!ok) break;
                 tc_fence_after_sync();
-                const size_t slot = static_cast<size_t>(cta) + cur.b;
+                // (O is complete: every warp of the group has handed over its P, so the per-head words but m have been read)
+                if ((lane & (kShare - 1)) == 0) lsum_s[quarter * kHeads + h0 + lane / kShare] = sum;
+                arrive();
+                const size_t slot = static_cast<size_t>(cta) + b;
                 // (a slot past the workspace would mean that the roles disagree about the pieces)
                 const bool store = device_check(slot < static_cast<size_t>(args.ctas_per_group) + args.B, args.status, 0xEB0000u | cta);
-                float* dst = args.part_o + (slot * args.h_pad + head0 + h0) * kDecLat + key;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t o[L::kSplit ? 32 : 16];
-                    if constexpr (L::kSplit) tmem_ld_x32(col_o + c * L::kCols, o);
-                    else tmem_ld_x16(col_o + c * L::kCols, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        float x = __uint_as_float(o[v]);
-                        if constexpr (L::kSplit) x = fmaf(__uint_as_float(o[(16 + v) % (L::kSplit ? 32 : 16)]), 1.0f / kD8LoScale, x);
-                        if (store && v < n_live) dst[v * kDecLat + c * 128] = x;
-                    }
-                }
-                // the sums over the 128 keys: within the warp, then the warps one after another (a fixed order)
-                float sums = 0.f;
-#pragma unroll
-                for (int h = 0; h < 16; ++h) {
-                    const float2 v = f2_parts(l2[h >> 1]);
-                    float x = (h & 1) ? v.y : v.x;
-#pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-                    if (lane == h) sums = x;
-                }
+                // A head's 512 latents in the order that a thread has them in, latent 128 c + l at 4 l + c: 16 bytes a store, 512 of a warp side by side.
+                float4* dst = reinterpret_cast<float4*>(args.part_o + (slot * args.h_pad + head0 + h0) * kDecLat) + key;
 #pragma unroll 1
-                for (int w = 0; w < 4; ++w) {
-                    if (quarter == w && lane < 16) alpha_s[h0 + lane] = (w == 0 ? 0.f : alpha_s[h0 + lane]) + sums;
-                    if (ok) ok = meet();
+                for (int v0 = 0; v0 < kPer; v0 += 8) {
+                    float x[8][4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t o[8], rest[8];
+                        tmem_ld_x8(col_o + c * L::kCols + v0, o);
+                        if constexpr (L::kSplit) tmem_ld_x8(col_o + c * L::kCols + 16, rest);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int v = 0; v < 8; ++v) {
+                            x[v][c] = __uint_as_float(o[v]);
+                            if constexpr (L::kSplit) x[v][c] = fmaf(__uint_as_float(rest[v]), 1.0f / kD8LoScale, x[v][c]);
+                        }
+                    }
+                    if (v0 + 8 == kPer) {                      // the next piece's values may be multiplied while these are stored
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(o_free);
+                    }
+#pragma unroll
+                    for (int v = 0; v < 8; ++v)
+                        if (store && v0 + v < n_live) dst[(v0 + v) * (kDecLat / 4)] = make_float4(x[v][0], x[v][1], x[v][2], x[v][3]);
                 }
-                if (!ok) break;
-                if (store && tid < n_live) args.part_ml[slot * args.h_pad + head0 + h0 + tid] = make_float2(ref_s[h0 + tid], alpha_s[h0 + tid]);
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(o_free);
+                if (!wait_for_group()) break;
+                if (store && tid < n_live) {
+                    const float l = ((lsum_s[h0 + tid] + lsum_s[kHeads + h0 + tid]) + lsum_s[2 * kHeads + h0 + tid]) + lsum_s[3 * kHeads + h0 + tid];
+                    // (no weight at all: nothing that another piece's reference should be compared with)
+                    args.part_ml[slot * args.h_pad + head0 + h0 + tid] = make_float2(l == 0.f ? kDecLowest : ref_s[h0 + tid] + L::kDrop, l);
+                }
                 ++pieces;
                 first = true;
-                if (!meet()) break;          // the references have been read
             }
-            cur.next(args);
             ++T;
             pos += 5;
             if (pos >= L::kSlabs) pos -= L::kSlabs;
@@ -617,178 +729,247 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
 // beside it, over the smallest power of two that brings the 576 channels within 448, in two e4m3 parts:
 //     rows ((b * h_pad / 16 + i / 16) * 2 + part) * 16 + i % 16 of 640 codes: 512 absorbed, the rotated part twice (for the key's codes and
 //     for their rests);   q_scale[b][i] the power of two
-// A CTA has 128 latents of a head; the four of a head are a cluster and tell one another their largest magnitudes.
-template <int kRequests>
+// A CTA has all 512 latents of a head, 128 KB of W_uk: their largest magnitude is one CTA's (four CTAs of 128 latents as a cluster that told one
+// another: 10.5 us for 8 requests of 128 heads).  Four groups of four warps have 128 latents each.
+//   kRows false  D[128 latents x 16 requests] = W_uk (A) . q^T (B) for each group: a lane has a latent.  Few requests: nothing is padded but columns.
+//   kRows true   D[128 requests x 128 latents] = q (A) . W_uk^T (B): a thread has a request's row, whose magnitude needs no other lane and whose
+//                codes are whole chunks; a head's weights are read once for 128 requests.
+constexpr int kAbsorb8Threads = 512;
+template <bool kRows>
 struct DecodeAbsorb8Smem {
-    static constexpr int kW = 0;                                 // two slabs of 128 rows x 64 channels; later the two parts' boxes
-    static constexpr int kQ = kW + 2 * 128 * 128;                // two slabs of kRequests rows
-    static constexpr int kMax = kQ + 2 * kRequests * 128;        // [4 warps][kRequests], [kRequests] of the rotated part, [4 CTAs][kRequests]
-    static constexpr int kInv = kMax + 9 * kRequests * 4;        // [kRequests] 1 / scale
-    static constexpr int kBar = kInv + kRequests * 4;
-    static constexpr int kTotalBytes = kBar + 32;
+    static constexpr int kTile = kRows ? 128 : 16;               // requests
+    static constexpr int kW = 0;                                 // four blocks of 128 latents, two slabs of 64 channels each; later the parts' boxes
+    static constexpr int kWBlock = 2 * 128 * 128;
+    static constexpr int kQ = kW + 4 * kWBlock;                  // two slabs of kTile rows
+    static constexpr int kMax = kQ + 2 * kTile * 128;            // largest magnitudes: [4 groups][128], or [17][16] (16 warps, rotated part) and 1 / scale
+    static constexpr int kMaxWords = kRows ? 4 * 128 : 18 * 16;
+    static constexpr int kBar = kMax + kMaxWords * 4;
+    static constexpr int kTotalBytes = kBar + 8 * 8 + 16;
+    static_assert(kTotalBytes <= 232448, "shared memory of the absorption");
 };
-template <int kRequests>
-__global__ void __cluster_dims__(4, 1, 1) __launch_bounds__(kAbsorbThreads)
+template <bool kRows>
+__global__ void __launch_bounds__(kAbsorb8Threads, 1)
 decode_absorb8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_out,
                       const __nv_bfloat16* __restrict__ q, int B, int h, int h_pad, uint8_t* __restrict__ rows, float* __restrict__ q_scale,
                       unsigned* status, int status_words) {
-    using L = DecodeAbsorb8Smem<kRequests>;
+    using L = DecodeAbsorb8Smem<kRows>;
+    constexpr int kTile = L::kTile, kN = kRows ? 128 : 16;       // kN: TMEM columns of a block
     extern __shared__ __align__(1024) uint8_t smem[];
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
-    uint64_t* done = full + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 2);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);      // [4] a block's weights (the first: and the queries)
+    uint64_t* done = full + 4;                                         // [4] its product
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 8);
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
-    uint32_t *warp_max = reinterpret_cast<uint32_t*>(smem + L::kMax), *rope_max = warp_max + 4 * kRequests, *cta_max = rope_max + kRequests;
-    float* inv_s = reinterpret_cast<float*>(smem + L::kInv);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int rank = static_cast<int>(cluster_cta_rank()), head = blockIdx.y, b0 = blockIdx.z * kRequests, c0 = rank * 128;
-    constexpr uint32_t kCols = kRequests < 32 ? 32 : kRequests;
+    const int block = warp >> 2, head = blockIdx.x, b0 = blockIdx.y * kTile;
     // the status slot, before any kernel of the call can write to it (as in decode_absorb_kernel)
-    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < status_words) {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < status_words) {
         status[threadIdx.x] = 0u;
         __threadfence();
     }
     if (threadIdx.x == 0) {
-        mbar_init(full, 1); mbar_init(done, 1);
+        for (int i = 0; i < 8; ++i) mbar_init(&full[i], 1);
         abort_flag->value = 0;
         mbar_fence_init();
+        for (int j = 0; j < 4; ++j) {
+            mbar_arrive_expect_tx(&full[j], L::kWBlock + (j == 0 ? 2 * kTile * 128 : 0));
+            for (int k = 0; k < 2; ++k) {
+                if (j == 0) tma_load_2d_chk(status, smem + L::kQ + k * kTile * 128, &tmap_q, full, head * 192 + k * 64, b0);
+                tma_load_2d_chk(status, smem + L::kW + j * L::kWBlock + k * 128 * 128, &tmap_w, &full[j], head * 256 + k * 64, j * 128);
+            }
+        }
     }
-    if (warp == 0) { tmem_alloc(tmem_slot, kCols); tmem_relinquish(); }
+    if (warp == 1) { tmem_alloc(tmem_slot, 4 * kN); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (the peers run: waited for before the first word to them)
     grid_launch_dependents();
     const uint32_t tmem = *tmem_slot;
     if (warp == 0) {
         if (elect_one()) {
-            mbar_arrive_expect_tx(full, 2 * 128 * 128 + 2 * kRequests * 128);
-            for (int k = 0; k < 2; ++k) {
-                tma_load_2d_chk(status, smem + L::kW + k * 128 * 128, &tmap_w, full, head * 256 + k * 64, c0);
-                tma_load_2d_chk(status, smem + L::kQ + k * kRequests * 128, &tmap_q, full, head * 192 + k * 64, b0);
-            }
-            if (mbar_wait(full, 0, abort_flag, status, 0x90)) {
+            constexpr uint32_t idesc = kRows ? make_idesc_bf16(128, 128, 0, 0) : make_idesc_bf16(128, 16, 0, 0);
+            const uint64_t dq = desc_k_major(smem_u32(smem + L::kQ));
+            bool ok = true;
+            for (int j = 0; j < 4 && ok; ++j) {
+                ok = mbar_wait(&full[j], 0, abort_flag, status, 0x90);
+                if (!ok) break;
                 tc_fence_after_sync();
-                constexpr uint32_t idesc = make_idesc_bf16(128, kRequests, 0, 0);
-                const uint64_t da = desc_k_major(smem_u32(smem + L::kW)), db = desc_k_major(smem_u32(smem + L::kQ));
+                const uint64_t dw = desc_k_major(smem_u32(smem + L::kW + j * L::kWBlock));
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    mma_ss(tmem, da + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, db + (kk >> 2) * (kRequests * 128 / 16) + (kk & 3) * 2, idesc,
-                           kk > 0 ? 1u : 0u);
-                mma_commit(done);
-            } else {
-                mbar_wait_quiesce(full, 0);
+                for (int kk = 0; kk < 8; ++kk) {
+                    const uint64_t w = dw + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, x = dq + (kk >> 2) * (kTile * 128 / 16) + (kk & 3) * 2;
+                    mma_ss(tmem + j * kN, kRows ? x : w, kRows ? w : x, idesc, kk > 0 ? 1u : 0u);
+                }
+                mma_commit(&done[j]);
             }
+            if (!ok)
+                for (int j = 0; j < 4; ++j) mbar_wait_quiesce(&full[j], 0);
         }
         __syncwarp();
     }
-    // The rotated part, eight threads a request, eight channels a thread: sixteen requests at a time.
-    const int j = threadIdx.x & 7;
-    auto rotated = [&](int r) {
-        return r < B - b0 ? *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + r) * h + head) * 192 + 128 + j * 8) : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t column = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + block * kN;
+    const size_t row0 = (head >> 4) * 32 + (head & 15);          // of the request's 2 h_pad rows: the head's first part; the second 16 on
+    // A pair of values as codes and the codes of what is left (taken of the value rounded to fp16: 2^-12 of it, where the parts together hold 2^-8).
+    auto parts = [](F2 x, F2 inv, uint32_t& hi, uint32_t& lo) {
+        const float2 w = f2_parts(f2_mul(x, inv));
+        const __half2 w16 = __floats2half2_rn(w.x, w.y);
+        hi = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&w16));
+        const uint32_t held = half2_of_e4m3x2(hi);
+        const __half2 rest = __hsub2(w16, *reinterpret_cast<const __half2*>(&held));
+        lo = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&rest));
     };
+    auto rotated = [&](int r, int c) {                           // eight channels of a request's rotated part
+        return r < B - b0 ? *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + r) * h + head) * 192 + 128 + c) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    auto store_rotated = [&](uint4 v, int r, int c, float inv) {
+        float t[8];
+        ln_unpack(v, t);
+        uint32_t a[4], b[4];
 #pragma unroll
-    for (int r0 = 0; r0 < kRequests; r0 += 16) {
-        const int r = r0 + static_cast<int>(threadIdx.x >> 3);
-        const uint4 v = rotated(r);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        uint32_t most = 0u;
+        for (int m = 0; m < 4; ++m) parts(f2(t[2 * m], t[2 * m + 1]), f2(inv, inv), a[m], b[m]);
+        const uint2 hi = make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)),
+                    lo = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
+        uint8_t* dst = rows + (static_cast<size_t>(b0 + r) * 2 * h_pad + row0) * kC8Row + kC8Lat + c;
+        *reinterpret_cast<uint2*>(dst) = hi;
+        *reinterpret_cast<uint2*>(dst + kC8Key) = hi;
+        *reinterpret_cast<uint2*>(dst + 16 * kC8Row) = lo;
+        *reinterpret_cast<uint2*>(dst + 16 * kC8Row + kC8Key) = lo;
+    };
+    auto exponent_of = [](float most) { return max(scale_exponent(__float_as_uint(most)), -100); };
+    if constexpr (kRows) {
+        const int r = (warp & 3) * 32 + lane;                    // this thread's request; its group's block of latents and 16 rotated channels
+        const bool live = b0 + r < B;
+        const uint4 t0 = rotated(r, block * 16), t1 = rotated(r, block * 16 + 8);
+        float* group_max = reinterpret_cast<float*>(smem + L::kMax);
+        float most = 0.f;                                        // (a NaN loses: its code says so by itself)
+        {
+            float t[16];
+            ln_unpack(t0, t);
+            ln_unpack(t1, t + 8);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) most = max(most, max((w[k] << 16) & 0x7fffffffu, w[k] & 0x7fff0000u));
-#pragma unroll
-        for (int d = 1; d < 8; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
-        if (j == 0) rope_max[r] = most;
-    }
-    const bool ok = mbar_wait_warp(done, 0, abort_flag, status, 0x91);
-    tc_fence_after_sync();
-    const uint32_t column = tmem + (static_cast<uint32_t>(warp * 32) << 16);
-#pragma unroll 1
-    for (int r0 = 0; r0 < kRequests; r0 += 16) {
-        uint32_t v[16], mine = 0u;
-        tmem_ld_x16(column + r0, v);
-        tmem_ld_wait();
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const uint32_t most = __reduce_max_sync(0xffffffffu, v[r] & 0x7fffffffu);
-            if (lane == r) mine = most;
+            for (int i = 0; i < 16; i += 2) most = fmax3(most, fabsf(t[i]), fabsf(t[i + 1]));
         }
-        if (lane < 16) warp_max[warp * kRequests + r0 + lane] = mine;
-    }
-    __syncthreads();
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (threadIdx.x < kRequests) {
-        const int r = threadIdx.x;
-        uint32_t most = rope_max[r];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) most = max(most, warp_max[w * kRequests + r]);
-#pragma unroll
-        for (uint32_t peer = 0; peer < 4; ++peer)
-            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(cluster_map(cta_max + rank * kRequests + r, peer)), "r"(most) : "memory");
-    }
-    cluster_sync();
-    if (threadIdx.x < kRequests) {
-        const int r = threadIdx.x;
-        const uint32_t most = max(max(cta_max[r], cta_max[kRequests + r]), max(cta_max[2 * kRequests + r], cta_max[3 * kRequests + r]));
-        const int e = max(scale_exponent(most), -100);
-        inv_s[r] = e == 128 ? 0.f : exact_exp2(-e);
-        if (rank == 0 && b0 + r < B) q_scale[static_cast<size_t>(b0 + r) * h_pad + head] = exact_exp2(e);
-    }
-    __syncthreads();
-    // D is latents x requests, a part's box requests x 128 latents: transposed on the way through shared memory (over the weights, which the
-    // MMAs have read); requests past B are clipped by the map.
-    uint8_t* box = smem + L::kW + warp * 32 + lane;
+        const bool ok = mbar_wait_warp(&done[block], 0, abort_flag, status, 0x91);
+        tc_fence_after_sync();
+        // (Rolled loops: a CTA goes through this once, and unrolled, 64 pairs, the instructions' way into the SM took 7 us.)
+        uint32_t v[32];
 #pragma unroll 1
-    for (int r0 = 0; r0 < kRequests; r0 += 16) {
+        for (int c = 0; c < 128; c += 32) {
+            tmem_ld_x32(column + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) most = fmax3(most, fabsf(__uint_as_float(v[i])), fabsf(__uint_as_float(v[i + 1])));
+        }
+        group_max[block * 128 + r] = most;
+        __syncthreads();
+        const int e = exponent_of(fmaxf(fmaxf(group_max[r], group_max[128 + r]), fmaxf(group_max[256 + r], group_max[384 + r])));
+        const float inv = e == 128 ? 0.f : exact_exp2(-e);
+        if (ok && live && block == 0) q_scale[static_cast<size_t>(b0 + r) * h_pad + head] = exact_exp2(e);
+        // Ten boxes of 128 requests x 128 codes -- four blocks of latents and the rotated part, two parts each -- over the weights and queries,
+        // which the MMAs have read (every group has seen its own complete before the barrier above), and from there whole rows by TMA: a
+        // lane that stored its own row would touch 32 lines an instruction.
+        uint8_t* line = smem + L::kW + r * 128;                  // + box * 16 KB; 16-byte chunk c at c ^ (r & 7)
+        auto put = [&](int box, int chunk, uint4 x) { *reinterpret_cast<uint4*>(line + box * (128 * 128) + ((chunk ^ (r & 7)) << 4)) = x; };
+#pragma unroll 1
+        for (int k = 0; k < 9; ++k) {                            // sixteen values a turn: the block's, then the rotated
+            float t[16];
+            if (k < 8) {
+                tmem_ld_x16(column + 16 * k, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) t[i] = __uint_as_float(v[i]);
+            } else {
+                ln_unpack(t0, t);
+                ln_unpack(t1, t + 8);
+            }
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t a[2], b[2];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) parts(f2(t[4 * i + 2 * m], t[4 * i + 2 * m + 1]), f2(inv, inv), a[m], b[m]);
+                hi[i] = __byte_perm(a[0], a[1], 0x5410);
+                lo[i] = __byte_perm(b[0], b[1], 0x5410);
+            }
+            const uint4 h4 = make_uint4(hi[0], hi[1], hi[2], hi[3]), l4 = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            const int pair = k < 8 ? 2 * block : 8, chunk = k < 8 ? k : block;
+            put(pair, chunk, h4);
+            put(pair + 1, chunk, l4);
+            if (k == 8) {                                        // (for the key's rests)
+                put(8, 4 + block, h4);
+                put(9, 4 + block, l4);
+            }
+        }
+        fence_async_shared();
+        if (__syncthreads_and(ok) && threadIdx.x == 0) {
+            for (int j = 0; j < 5; ++j)
+                for (int part = 0; part < 2; ++part)
+                    tma_store_2d(&tmap_out, smem + L::kW + (2 * j + part) * (128 * 128), (static_cast<int>(row0) + part * 16) * kC8Row + j * 128, b0);
+            tma_store_commit();
+            tma_store_wait_all();
+        }
+    } else {
+        uint32_t* warp_max = reinterpret_cast<uint32_t*>(smem + L::kMax);      // magnitudes as the bits of absolute values
+        float* inv_s = reinterpret_cast<float*>(warp_max + 17 * 16);
+        // the rotated part: eight threads a request, eight channels a thread
+        const int r8 = threadIdx.x >> 3, c8 = (threadIdx.x & 7) * 8;
+        uint4 turned = make_uint4(0u, 0u, 0u, 0u);
+        if (warp < 4) {
+            turned = rotated(r8, c8);
+            const uint32_t w[4] = {turned.x, turned.y, turned.z, turned.w};
+            uint32_t most = 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) most = max(most, max((w[k] << 16) & 0x7fffffffu, w[k] & 0x7fff0000u));
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+            if ((threadIdx.x & 7) == 0) warp_max[16 * 16 + r8] = most;
+        }
+        const bool ok = mbar_wait_warp(&done[block], 0, abort_flag, status, 0x92);
+        tc_fence_after_sync();
         uint32_t v[16];
-        tmem_ld_x16(column + r0, v);
+        tmem_ld_x16(column, v);
         tmem_ld_wait();
+        float mags[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mags[r] = fabsf(__uint_as_float(v[r]));
+        const float mine = warp_reduce_each(mags, lane, [](float x, float y) { return fmaxf(x, y); });
+        if ((lane & 1) == 0) warp_max[warp * 16 + (lane >> 1)] = __float_as_uint(mine);
+        __syncthreads();
+        if (threadIdx.x < 16) {
+            const int r = threadIdx.x;
+            uint32_t most = 0u;
+#pragma unroll
+            for (int w = 0; w < 17; ++w) most = max(most, warp_max[w * 16 + r]);
+            const int e = exponent_of(__uint_as_float(most));
+            inv_s[r] = e == 128 ? 0.f : exact_exp2(-e);
+            if (b0 + r < B) q_scale[static_cast<size_t>(b0 + r) * h_pad + head] = exact_exp2(e);
+        }
+        __syncthreads();
+        // D is latents x requests, a part's box requests x 128 latents: transposed on the way through shared memory (over the weights, which the
+        // MMAs have read); requests past B are clipped by the map.
+        uint8_t* box = smem + L::kW + block * 2 * (16 * 128) + (warp & 3) * 32 + lane;
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-            const float x = __uint_as_float(v[r]) * inv_s[r0 + r], y = __uint_as_float(v[r + 1]) * inv_s[r0 + r + 1];
-            const uint32_t hi = e4m3x2(x, y);
-            const float2 held = float2_of_half2(half2_of_e4m3x2(hi));
-            const uint32_t lo = e4m3x2(x - held.x, y - held.y);
-            uint8_t* at = box + (r0 + r) * 128;
+            uint32_t hi, lo;
+            parts(f2(__uint_as_float(v[r]), __uint_as_float(v[r + 1])), f2(inv_s[r], inv_s[r + 1]), hi, lo);
+            uint8_t* at = box + r * 128;
             at[0] = static_cast<uint8_t>(hi);
             at[128] = static_cast<uint8_t>(hi >> 8);
-            at[kRequests * 128] = static_cast<uint8_t>(lo);
-            at[kRequests * 128 + 128] = static_cast<uint8_t>(lo >> 8);
+            at[16 * 128] = static_cast<uint8_t>(lo);
+            at[16 * 128 + 128] = static_cast<uint8_t>(lo >> 8);
         }
-    }
-    fence_async_shared();
-    const int row0 = (head >> 4) * 32 + (head & 15);             // of the request's 2 h_pad rows: the head's first part; the second 16 on
-    // the rotated part: each CTA of the cluster takes its share of the requests
-#pragma unroll
-    for (int r0 = 0; r0 < kRequests; r0 += 16) {
-        const int r = r0 + static_cast<int>(threadIdx.x >> 3);
-        if ((r0 >> 4) % 4 != rank || r >= B - b0) continue;
-        const uint4 v = rotated(r);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        const float inv = inv_s[r];
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float x = __uint_as_float(w[k] << 16) * inv, y = __uint_as_float(w[k] & 0xffff0000u) * inv;
-            hi[k] = e4m3x2(x, y);
-            const float2 held = float2_of_half2(half2_of_e4m3x2(hi[k]));
-            lo[k] = e4m3x2(x - held.x, y - held.y);
+        fence_async_shared();
+        if (warp < 4 && r8 < B - b0) store_rotated(turned, r8, c8, inv_s[r8]);
+        if (__syncthreads_and(ok) && threadIdx.x == 0) {
+            for (int j = 0; j < 4; ++j)
+                for (int part = 0; part < 2; ++part)
+                    tma_store_2d(&tmap_out, smem + L::kW + (2 * j + part) * (16 * 128), (static_cast<int>(row0) + part * 16) * kC8Row + j * 128, b0);
+            tma_store_commit();
+            tma_store_wait_all();
         }
-        uint8_t* dst = rows + (static_cast<size_t>(b0 + r) * 2 * h_pad + row0) * kC8Row + kC8Lat + j * 8;
-        const uint2 h2 = make_uint2(hi[0] | (hi[1] << 16), hi[2] | (hi[3] << 16)), l2 = make_uint2(lo[0] | (lo[1] << 16), lo[2] | (lo[3] << 16));
-        *reinterpret_cast<uint2*>(dst) = h2;
-        *reinterpret_cast<uint2*>(dst + kC8Key) = h2;
-        *reinterpret_cast<uint2*>(dst + 16 * kC8Row) = l2;
-        *reinterpret_cast<uint2*>(dst + 16 * kC8Row + kC8Key) = l2;
-    }
-    if (__syncthreads_and(ok) && threadIdx.x == 0) {
-        for (int part = 0; part < 2; ++part)
-            tma_store_2d(&tmap_out, smem + L::kW + part * kRequests * 128, (row0 + part * 16) * kC8Row + c0, b0);
-        tma_store_commit();
-        tma_store_wait_all();
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 0) { tc_fence_after_sync(); tmem_dealloc(tmem, kCols); }
+    if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 4 * kN); }
 }
 
 }  // namespace laga

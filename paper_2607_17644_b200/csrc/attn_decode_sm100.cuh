@@ -770,6 +770,8 @@ struct DecodeProjectSmem {
     static constexpr int kTotalBytes = kBar + 48;
 };
 static_assert(DecodeProjectSmem::kTotalBytes <= 232448 && DecodeProjectSmem::kBar % 8 == 0, "projection kernel's shared memory");
+// kTurned: the pieces hold latent 128 c + l at 4 l + c.  The order of a product's terms is free: the weights' rows are loaded in it.
+template <bool kTurned>
 __global__ void __launch_bounds__(kProjectThreads, 1)
 decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
                       const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad, int ctas_per_group,
@@ -792,8 +794,11 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
         mbar_fence_init();
         if (my_tiles > 0) {
             mbar_arrive_expect_tx(full, 2 * L::kWSlab);
-            for (int k = 0; k < 4; ++k)                          // slab k / 2, rows 256 (k % 2) ..
-                tma_load_2d_chk(status, smem + L::kW + k * (L::kWSlab / 2), &tmap_wv, full, head * 256 + (k >> 1) * 64, (k & 1) * 256);
+            for (int k = 0; k < 4; ++k) {                        // slab k / 2, rows 256 (k % 2) ..
+                uint8_t* dst = smem + L::kW + k * (L::kWSlab / 2);
+                if constexpr (kTurned) tma_load_turned_chk(status, dst, &tmap_wv, full, head * 256 + (k >> 1) * 64, (k & 1) * 64);
+                else tma_load_2d_chk(status, dst, &tmap_wv, full, head * 256 + (k >> 1) * 64, (k & 1) * 256);
+            }
         }
     }
     if (warp == 0) { __syncwarp(); tmem_alloc(tmem_slot, 64); tmem_relinquish(); }

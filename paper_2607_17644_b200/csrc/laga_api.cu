@@ -94,12 +94,20 @@ bool make_tmap_cache(CUtensorMap* map, const void* base, uint64_t rows, uint32_t
 
 // Maps over 8-bit codes (boxes of 128 of them, out of range reads as zero):
 //   kMapPages    the cache: 640 codes x rows of a page x pages (`rows` pages, `stride` bytes apart, of `inner` rows each), 128-byte swizzle
-//   kMapQueries  2-d, 128-byte swizzle: the queries' rows as the attention reads them
-//   kMapStore    2-d, no swizzle: the same rows as decode_absorb8_kernel writes them
-enum : uint32_t { kMapPages = 16, kMapQueries = 17, kMapStore = 18 };
+//   kMapQueries  2-d, 128-byte swizzle: the queries' rows, as the attention reads them and decode_absorb8_kernel<true> writes them
+//   kMapStore    2-d, no swizzle: as decode_absorb8_kernel<false> writes them
+// and one over bf16 weights, kMapTurned: W's rows r as (r % 128, r / 128), boxes of 64 channels x 4 x 64, 128-byte swizzle (`rows`: 512)
+enum : uint32_t { kMapPages = 16, kMapQueries = 17, kMapStore = 18, kMapTurned = 19 };
 bool make_tmap_codes(CUtensorMap* map, uint32_t kind, const void* base, uint64_t inner, uint64_t rows, uint64_t stride, uint32_t box_rows) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
+    if (kind == kMapTurned) {
+        cuuint64_t dims[3] = {inner, 4u, rows / 4};
+        cuuint64_t strides[2] = {stride * (rows / 4), stride};
+        cuuint32_t box[3] = {64u, 4u, 64u}, estr[3] = {1u, 1u, 1u};
+        return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
     const bool pages = kind == kMapPages;
     cuuint64_t dims[3] = {pages ? kC8Row : inner, pages ? inner : rows, rows};
     cuuint64_t strides[2] = {pages ? kC8Row : stride, stride};
@@ -177,8 +185,10 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_decode8_sm100_kernel<16>, AttnDecode8Smem<16>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<32>, AttnDecode8Smem<32>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<64>, AttnDecode8Smem<64>::kTotalBytes) &&
-              allow_smem(decode_absorb8_kernel<64>, DecodeAbsorb8Smem<64>::kTotalBytes) &&
-              allow_smem(decode_project_kernel, DecodeProjectSmem::kTotalBytes) &&
+              allow_smem(decode_absorb8_kernel<false>, DecodeAbsorb8Smem<false>::kTotalBytes) &&
+              allow_smem(decode_absorb8_kernel<true>, DecodeAbsorb8Smem<true>::kTotalBytes) &&
+              allow_smem(decode_project_kernel<false>, DecodeProjectSmem::kTotalBytes) &&
+              allow_smem(decode_project_kernel<true>, DecodeProjectSmem::kTotalBytes) &&
               allow_smem(latent_norm_rope_fwd_kernel<2, false>, latent_fwd_smem(256, kRopeMaxRot)) &&
               allow_smem(latent_norm_rope_fwd_kernel<4, false>, latent_fwd_smem(512, kRopeMaxRot)) &&
               allow_smem(latent_norm_rope_fwd_kernel<4, true>, latent_fwd_smem(512, kRopeMaxRot)) &&
@@ -796,16 +806,18 @@ int launch_attn_decode(const void* q, const void* q_abs, const void* cache, long
     return launch_status();
 }
 
-int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, float* lse, cudaStream_t stream) {
+int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, float* lse, cudaStream_t stream, bool turned = false) {
     const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv);
+    const void* wv = static_cast<const uint8_t*>(w) + kDn * 2;
     CUtensorMap tw;      // starts at W's column d_nope: column 0 of the map is V channel 0 of head 0
-    if (!cached_tmap_bf16(&tw, static_cast<const uint8_t*>(w) + kDn * 2, w_row - kDn, kDc, w_row * 2, 256)) return LAGA_ERR_CUDA;
+    if (turned ? !cached_tmap_codes(&tw, kMapTurned, wv, w_row - kDn, kDc, w_row * 2, 64) : !cached_tmap_bf16(&tw, wv, w_row - kDn, kDc, w_row * 2, 256))
+        return LAGA_ERR_CUDA;
     // Tiles of 8 requests, which a CTA's threads join at once, where every tile can have a CTA of its own; otherwise of 16, and as
     // many CTAs per head as fit the GPU, each with a run of tiles (it reads its head's 128 KB of W_uv once).
     const int sms = sm_count();
     const int tile = static_cast<long long>(a.h) * ((a.B + 7) / 8) <= sms ? 8 : 16;
     const int n_tiles = (a.B + tile - 1) / tile, most = sms / a.h > 0 ? sms / a.h : 1;
-    launch_kernel(decode_project_kernel, dim3(a.h, n_tiles < most ? n_tiles : most), dim3(kProjectThreads), DecodeProjectSmem::kTotalBytes, stream,
+    launch_kernel(turned ? decode_project_kernel<true> : decode_project_kernel<false>, dim3(a.h, n_tiles < most ? n_tiles : most), dim3(kProjectThreads), DecodeProjectSmem::kTotalBytes, stream,
                   true, tw, static_cast<const float*>(a.part_o), static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift,
                   a.B, a.h, a.h_pad, a.ctas_per_group, tile, static_cast<__nv_bfloat16*>(out), lse, a.status);
     return launch_status();
@@ -828,16 +840,18 @@ Decode8Layout decode8_layout(int B, int h) {
     return w;
 }
 
-template <int kRequests>
 int launch_decode_absorb8(const void* q, const void* w, int B, int h, int h_pad, uint8_t* rows, float* q_scale, unsigned* status, cudaStream_t stream) {
     const uint64_t q_row = static_cast<uint64_t>(h) * (kDn + kDr), w_row = static_cast<uint64_t>(h) * (kDn + kDv), request = 2ull * h_pad * kC8Row;
+    // Tiles of 16 requests where each can have an SM of its own; otherwise of 128, which read a head's weights once.
+    const bool few = static_cast<long long>(h) * ((B + 15) / 16) <= sm_count();
+    const int tile = few ? 16 : 128, words = static_cast<int>(kStatusClearBytes / sizeof(unsigned));
     CUtensorMap tw, tq, to;
-    if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, kRequests) ||
-        !cached_tmap_codes(&to, kMapStore, rows, request, B, request, kRequests))
+    if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, tile) ||
+        !cached_tmap_codes(&to, few ? kMapStore : kMapQueries, rows, request, B, request, tile))
         return LAGA_ERR_CUDA;
-    launch_kernel(decode_absorb8_kernel<kRequests>, dim3(kDc / 128, h, (B + kRequests - 1) / kRequests), dim3(kAbsorbThreads),
-                  DecodeAbsorb8Smem<kRequests>::kTotalBytes, stream, false, tw, tq, to, static_cast<const __nv_bfloat16*>(q), B, h, h_pad, rows, q_scale,
-                  status, static_cast<int>(kStatusClearBytes / sizeof(unsigned)));
+    launch_kernel(few ? decode_absorb8_kernel<false> : decode_absorb8_kernel<true>, dim3(h, (B + tile - 1) / tile), dim3(kAbsorb8Threads),
+                  few ? DecodeAbsorb8Smem<false>::kTotalBytes : DecodeAbsorb8Smem<true>::kTotalBytes, stream, false, tw, tq, to,
+                  static_cast<const __nv_bfloat16*>(q), B, h, h_pad, rows, q_scale, status, words);
     return launch_status();
 }
 
@@ -1637,10 +1651,7 @@ int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int
     uint8_t* base = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(base);
     float* q_scale = reinterpret_cast<float*>(base + w.q_scale);
-    // (the tiles of requests as in laga_paged_decode)
-    rc = B <= 16 ? launch_decode_absorb8<16>(q, w_kv_b, B, h, w.d.h_pad, base + w.q_rows, q_scale, status, st)
-                 : launch_decode_absorb8<64>(q, w_kv_b, B, h, w.d.h_pad, base + w.q_rows, q_scale, status, st);
-    if (rc != LAGA_OK) return rc;
+    if ((rc = launch_decode_absorb8(q, w_kv_b, B, h, w.d.h_pad, base + w.q_rows, q_scale, status, st)) != LAGA_OK) return rc;
     const AttnDecode8Args a{AttnDecodeArgs{B, h, w.d.n_groups, w.d.ctas_per_group, softmax_scale * 1.4426950408889634f, seq_lens, block_table, columns, shift,
                                            n_pages, reinterpret_cast<float*>(base + w.d.part_o), reinterpret_cast<float2*>(base + w.d.part_ml), w.d.h_pad,
                                            status},
@@ -1649,7 +1660,7 @@ int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int
     else if (w.d.heads == 32) rc = launch_attn_decode8<32>(base + w.q_rows, a, st);
     else rc = launch_attn_decode8<64>(base + w.q_rows, a, st);
     if (rc != LAGA_OK) return rc;
-    return launch_decode_project(w_kv_b, a.d, out, lse, st);
+    return launch_decode_project(w_kv_b, a.d, out, lse, st, true);
 }
 
 }  // extern "C"

@@ -209,6 +209,12 @@ __device__ __forceinline__ uint64_t l2_evict_first() {
     return policy;
 }
 
+__device__ __forceinline__ uint64_t l2_evict_normal() {
+    uint64_t policy;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
+}
+
 // TMA store of one box from shared memory (bulk async-group completion).  The shared-memory source must have
 // been written, fenced into the async proxy (fence_async_shared) and the writers synchronised before the issue.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* smem_src, int x, int y) {
@@ -592,6 +598,20 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r) {
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+__device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+        : "r"(taddr)
+        : "memory");
+}
+// One column.
+__device__ __forceinline__ void tmem_ld_x1(uint32_t taddr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r[0]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_x1(uint32_t taddr, uint32_t r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(r) : "memory");
+}
 __device__ __forceinline__ void tmem_ld_wait() {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
@@ -765,11 +785,42 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
                  "l"(src), "r"(bytes), "r"(smem_u32(bar))
                  : "memory");
 }
+// The same with shared-memory addresses as words.
+__device__ __forceinline__ void mbar_arrive_expect_tx_u32(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_test_wait_u32(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
 // A box of codes of the 8-bit cache: channel, row of a page, page (past the last: zeros).
-__device__ __forceinline__ void tma_load_codes_chk(unsigned int* status, void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z,
+__device__ __forceinline__ void tma_load_codes_chk(unsigned int* status, uint32_t smem_dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z,
                                                    uint64_t policy) {
-    if (device_check((x & 15) == 0 && x >= 0 && x < 640 && y >= 0 && y < 1024 && z >= 0 && (smem_u32(smem_dst) & 1023u) == 0u, status, 0xE90000u | (z & 0xffff)))
-        tma_load_3d(smem_dst, map, bar, x, y, z, policy);
+    if (device_check((x & 15) == 0 && x >= 0 && x < 640 && y >= 0 && y < 1024 && z >= 0 && (smem_dst & 1023u) == 0u, status, 0xE90000u | (z & 0xffff)))
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;"
+            ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z), "l"(policy)
+            : "memory");
+}
+// A box of the weights' map by (channel, row % 128, row / 128): 64 channels x all four of the last x 64 of the middle one.
+__device__ __forceinline__ void tma_load_turned_chk(unsigned int* status, void* smem_dst, const CUtensorMap* map, uint64_t* bar, int x, int row) {
+    if (device_check((x & 7) == 0 && x >= 0 && row >= 0 && row < 128 && (smem_u32(smem_dst) & 1023u) == 0u, status, 0xE60000u | (x & 0xffff)))
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+            ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(0), "r"(row)
+            : "memory");
+}
+// A box of codes to L2 only.
+__device__ __forceinline__ void tma_prefetch_codes(const CUtensorMap* map, int x, int y, int z) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z)
+                 : "memory");
 }
 // Two values to two codes, `lo` in the low byte; past the largest number they become it, NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
