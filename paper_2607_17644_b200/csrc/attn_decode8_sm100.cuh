@@ -729,36 +729,69 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
 // beside it, over the smallest power of two that brings the 576 channels within 448, in two e4m3 parts:
 //     rows ((b * h_pad / 16 + i / 16) * 2 + part) * 16 + i % 16 of 640 codes: 512 absorbed, the rotated part twice (for the key's codes and
 //     for their rests);   q_scale[b][i] the power of two
-// A CTA has all 512 latents of a head, 128 KB of W_uk: their largest magnitude is one CTA's (four CTAs of 128 latents as a cluster that told one
-// another: 10.5 us for 8 requests of 128 heads).  Four groups of four warps have 128 latents each.
-//   kRows false  D[128 latents x 16 requests] = W_uk (A) . q^T (B) for each group: a lane has a latent.  Few requests: nothing is padded but columns.
-//   kRows true   D[128 requests x 128 latents] = q (A) . W_uk^T (B): a thread has a request's row, whose magnitude needs no other lane and whose
-//                codes are whole chunks; a head's weights are read once for 128 requests.
+//
+// Few requests, decode_absorb8_kernel: a CTA has all 512 latents of a head, 128 KB of W_uk, for 16 requests; four groups of four warps have
+// 128 latents each, D[128 latents x 16 requests] = W_uk (A) . q^T (B).  A lane has a latent, nothing is padded but columns.
+// Many, decode_absorb8_rows_kernel: a CTA has 128 latents of a head for 128 requests, D[128 requests x 128 latents] = q (A) . W_uk^T (B).  A thread
+// has a request's row, whose magnitude needs no other lane; the four CTAs of a head are a cluster and tell one another theirs.
+// The loops over a row are rolled: a CTA goes through them once, and instructions that are taken in for one use are slow ones.
 constexpr int kAbsorb8Threads = 512;
-template <bool kRows>
 struct DecodeAbsorb8Smem {
-    static constexpr int kTile = kRows ? 128 : 16;               // requests
+    static constexpr int kTile = 16;                             // requests
     static constexpr int kW = 0;                                 // four blocks of 128 latents, two slabs of 64 channels each; later the parts' boxes
     static constexpr int kWBlock = 2 * 128 * 128;
     static constexpr int kQ = kW + 4 * kWBlock;                  // two slabs of kTile rows
-    static constexpr int kMax = kQ + 2 * kTile * 128;            // largest magnitudes: [4 groups][128], or [17][16] (16 warps, rotated part) and 1 / scale
-    static constexpr int kMaxWords = kRows ? 4 * 128 : 18 * 16;
-    static constexpr int kBar = kMax + kMaxWords * 4;
+    static constexpr int kMax = kQ + 2 * kTile * 128;            // [17][16]: largest magnitudes of 16 warps and of the rotated part; then 1 / scale
+    static constexpr int kBar = kMax + 18 * 16 * 4;
     static constexpr int kTotalBytes = kBar + 8 * 8 + 16;
-    static_assert(kTotalBytes <= 232448, "shared memory of the absorption");
 };
-template <bool kRows>
+static_assert(DecodeAbsorb8Smem::kTotalBytes <= 232448, "shared memory of the absorption");
+
+// A pair of values as codes and the codes of what is left (taken of the value rounded to fp16: 2^-12 of it, where the parts together hold 2^-8).
+__device__ __forceinline__ void absorb8_parts(F2 x, float inv, uint32_t& hi, uint32_t& lo) {
+    const float2 w = f2_parts(f2_mul(x, f2(inv, inv)));
+    const __half2 w16 = __floats2half2_rn(w.x, w.y);
+    hi = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&w16));
+    const uint32_t held = half2_of_e4m3x2(hi);
+    const __half2 rest = __hsub2(w16, *reinterpret_cast<const __half2*>(&held));
+    lo = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&rest));
+}
+__device__ __forceinline__ int absorb8_exponent(float most) { return max(scale_exponent(__float_as_uint(most)), -100); }
+// Eight rotated channels c .. of a request (row: its head's first part of the queries' rows), twice: for the key's codes and for their rests.
+__device__ __forceinline__ void absorb8_store_rotated(uint4 v, uint8_t* row, int c, float inv) {
+    float t[8];
+    ln_unpack(v, t);
+    uint32_t a[4], b[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) absorb8_parts(f2(t[2 * m], t[2 * m + 1]), inv, a[m], b[m]);
+    const uint2 hi = make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)),
+                lo = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
+    uint8_t* dst = row + kC8Lat + c;
+    *reinterpret_cast<uint2*>(dst) = hi;
+    *reinterpret_cast<uint2*>(dst + kC8Key) = hi;
+    *reinterpret_cast<uint2*>(dst + 16 * kC8Row) = lo;
+    *reinterpret_cast<uint2*>(dst + 16 * kC8Row + kC8Key) = lo;
+}
+__device__ __forceinline__ float absorb8_magnitude(uint4 v) {
+    float t[8], most = 0.f;
+    ln_unpack(v, t);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) most = fmax3(most, fabsf(t[i]), fabsf(t[i + 1]));      // (a NaN loses: its code says so by itself)
+    return most;
+}
+
 __global__ void __launch_bounds__(kAbsorb8Threads, 1)
 decode_absorb8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_out,
                       const __nv_bfloat16* __restrict__ q, int B, int h, int h_pad, uint8_t* __restrict__ rows, float* __restrict__ q_scale,
                       unsigned* status, int status_words) {
-    using L = DecodeAbsorb8Smem<kRows>;
-    constexpr int kTile = L::kTile, kN = kRows ? 128 : 16;       // kN: TMEM columns of a block
+    using L = DecodeAbsorb8Smem;
+    constexpr int kTile = L::kTile;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);      // [4] a block's weights (the first: and the queries)
     uint64_t* done = full + 4;                                         // [4] its product
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 8);
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
+    float *warp_max = reinterpret_cast<float*>(smem + L::kMax), *inv_s = warp_max + 17 * 16;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int block = warp >> 2, head = blockIdx.x, b0 = blockIdx.y * kTile;
     // the status slot, before any kernel of the call can write to it (as in decode_absorb_kernel)
@@ -778,7 +811,7 @@ decode_absorb8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
             }
         }
     }
-    if (warp == 1) { tmem_alloc(tmem_slot, 4 * kN); tmem_relinquish(); }
+    if (warp == 1) { tmem_alloc(tmem_slot, 64); tmem_relinquish(); }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -786,7 +819,7 @@ decode_absorb8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
     const uint32_t tmem = *tmem_slot;
     if (warp == 0) {
         if (elect_one()) {
-            constexpr uint32_t idesc = kRows ? make_idesc_bf16(128, 128, 0, 0) : make_idesc_bf16(128, 16, 0, 0);
+            constexpr uint32_t idesc = make_idesc_bf16(128, kTile, 0, 0);
             const uint64_t dq = desc_k_major(smem_u32(smem + L::kQ));
             bool ok = true;
             for (int j = 0; j < 4 && ok; ++j) {
@@ -795,10 +828,9 @@ decode_absorb8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
                 tc_fence_after_sync();
                 const uint64_t dw = desc_k_major(smem_u32(smem + L::kW + j * L::kWBlock));
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    const uint64_t w = dw + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, x = dq + (kk >> 2) * (kTile * 128 / 16) + (kk & 3) * 2;
-                    mma_ss(tmem + j * kN, kRows ? x : w, kRows ? w : x, idesc, kk > 0 ? 1u : 0u);
-                }
+                for (int kk = 0; kk < 8; ++kk)
+                    mma_ss(tmem + j * kTile, dw + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, dq + (kk >> 2) * (kTile * 128 / 16) + (kk & 3) * 2, idesc,
+                           kk > 0 ? 1u : 0u);
                 mma_commit(&done[j]);
             }
             if (!ok)
@@ -806,170 +838,200 @@ decode_absorb8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
         }
         __syncwarp();
     }
-    const uint32_t column = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + block * kN;
     const size_t row0 = (head >> 4) * 32 + (head & 15);          // of the request's 2 h_pad rows: the head's first part; the second 16 on
-    // A pair of values as codes and the codes of what is left (taken of the value rounded to fp16: 2^-12 of it, where the parts together hold 2^-8).
-    auto parts = [](F2 x, F2 inv, uint32_t& hi, uint32_t& lo) {
-        const float2 w = f2_parts(f2_mul(x, inv));
-        const __half2 w16 = __floats2half2_rn(w.x, w.y);
-        hi = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&w16));
-        const uint32_t held = half2_of_e4m3x2(hi);
-        const __half2 rest = __hsub2(w16, *reinterpret_cast<const __half2*>(&held));
-        lo = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&rest));
-    };
-    auto rotated = [&](int r, int c) {                           // eight channels of a request's rotated part
-        return r < B - b0 ? *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + r) * h + head) * 192 + 128 + c) : make_uint4(0u, 0u, 0u, 0u);
-    };
-    auto store_rotated = [&](uint4 v, int r, int c, float inv) {
-        float t[8];
-        ln_unpack(v, t);
-        uint32_t a[4], b[4];
+    // the rotated part: eight threads a request, eight channels a thread
+    const int r8 = threadIdx.x >> 3, c8 = (threadIdx.x & 7) * 8;
+    uint4 turned = make_uint4(0u, 0u, 0u, 0u);
+    if (warp < 4) {
+        if (r8 < B - b0) turned = *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + r8) * h + head) * 192 + 128 + c8);
+        float most = absorb8_magnitude(turned);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) parts(f2(t[2 * m], t[2 * m + 1]), f2(inv, inv), a[m], b[m]);
-        const uint2 hi = make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)),
-                    lo = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
-        uint8_t* dst = rows + (static_cast<size_t>(b0 + r) * 2 * h_pad + row0) * kC8Row + kC8Lat + c;
-        *reinterpret_cast<uint2*>(dst) = hi;
-        *reinterpret_cast<uint2*>(dst + kC8Key) = hi;
-        *reinterpret_cast<uint2*>(dst + 16 * kC8Row) = lo;
-        *reinterpret_cast<uint2*>(dst + 16 * kC8Row + kC8Key) = lo;
-    };
-    auto exponent_of = [](float most) { return max(scale_exponent(__float_as_uint(most)), -100); };
-    if constexpr (kRows) {
-        const int r = (warp & 3) * 32 + lane;                    // this thread's request; its group's block of latents and 16 rotated channels
-        const bool live = b0 + r < B;
-        const uint4 t0 = rotated(r, block * 16), t1 = rotated(r, block * 16 + 8);
-        float* group_max = reinterpret_cast<float*>(smem + L::kMax);
-        float most = 0.f;                                        // (a NaN loses: its code says so by itself)
-        {
-            float t[16];
-            ln_unpack(t0, t);
-            ln_unpack(t1, t + 8);
+        for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        if ((threadIdx.x & 7) == 0) warp_max[16 * 16 + r8] = most;
+    }
+    const bool ok = mbar_wait_warp(&done[block], 0, abort_flag, status, 0x91);
+    tc_fence_after_sync();
+    uint32_t v[16];
+    tmem_ld_x16(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + block * kTile, v);
+    tmem_ld_wait();
+    float mags[16];
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) most = fmax3(most, fabsf(t[i]), fabsf(t[i + 1]));
-        }
-        const bool ok = mbar_wait_warp(&done[block], 0, abort_flag, status, 0x91);
-        tc_fence_after_sync();
-        // (Rolled loops: a CTA goes through this once, and unrolled, 64 pairs, the instructions' way into the SM took 7 us.)
-        uint32_t v[32];
-#pragma unroll 1
-        for (int c = 0; c < 128; c += 32) {
-            tmem_ld_x32(column + c, v);
-            tmem_ld_wait();
+    for (int r = 0; r < 16; ++r) mags[r] = fabsf(__uint_as_float(v[r]));
+    const float mine = warp_reduce_each(mags, lane, [](float x, float y) { return fmaxf(x, y); });
+    if ((lane & 1) == 0) warp_max[warp * 16 + (lane >> 1)] = mine;
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        const int r = threadIdx.x;
+        float most = 0.f;
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) most = fmax3(most, fabsf(__uint_as_float(v[i])), fabsf(__uint_as_float(v[i + 1])));
-        }
-        group_max[block * 128 + r] = most;
-        __syncthreads();
-        const int e = exponent_of(fmaxf(fmaxf(group_max[r], group_max[128 + r]), fmaxf(group_max[256 + r], group_max[384 + r])));
-        const float inv = e == 128 ? 0.f : exact_exp2(-e);
-        if (ok && live && block == 0) q_scale[static_cast<size_t>(b0 + r) * h_pad + head] = exact_exp2(e);
-        // Ten boxes of 128 requests x 128 codes -- four blocks of latents and the rotated part, two parts each -- over the weights and queries,
-        // which the MMAs have read (every group has seen its own complete before the barrier above), and from there whole rows by TMA: a
-        // lane that stored its own row would touch 32 lines an instruction.
-        uint8_t* line = smem + L::kW + r * 128;                  // + box * 16 KB; 16-byte chunk c at c ^ (r & 7)
-        auto put = [&](int box, int chunk, uint4 x) { *reinterpret_cast<uint4*>(line + box * (128 * 128) + ((chunk ^ (r & 7)) << 4)) = x; };
-#pragma unroll 1
-        for (int k = 0; k < 9; ++k) {                            // sixteen values a turn: the block's, then the rotated
-            float t[16];
-            if (k < 8) {
-                tmem_ld_x16(column + 16 * k, v);
-                tmem_ld_wait();
+        for (int w = 0; w < 17; ++w) most = fmaxf(most, warp_max[w * 16 + r]);
+        const int e = absorb8_exponent(most);
+        inv_s[r] = e == 128 ? 0.f : exact_exp2(-e);
+        if (b0 + r < B) q_scale[static_cast<size_t>(b0 + r) * h_pad + head] = exact_exp2(e);
+    }
+    __syncthreads();
+    // D is latents x requests, a part's box requests x 128 latents: transposed on the way through shared memory (over the weights, which the
+    // MMAs have read); requests past B are clipped by the map.
+    uint8_t* box = smem + L::kW + block * 2 * (16 * 128) + (warp & 3) * 32 + lane;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) t[i] = __uint_as_float(v[i]);
-            } else {
-                ln_unpack(t0, t);
-                ln_unpack(t1, t + 8);
-            }
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t a[2], b[2];
-#pragma unroll
-                for (int m = 0; m < 2; ++m) parts(f2(t[4 * i + 2 * m], t[4 * i + 2 * m + 1]), f2(inv, inv), a[m], b[m]);
-                hi[i] = __byte_perm(a[0], a[1], 0x5410);
-                lo[i] = __byte_perm(b[0], b[1], 0x5410);
-            }
-            const uint4 h4 = make_uint4(hi[0], hi[1], hi[2], hi[3]), l4 = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            const int pair = k < 8 ? 2 * block : 8, chunk = k < 8 ? k : block;
-            put(pair, chunk, h4);
-            put(pair + 1, chunk, l4);
-            if (k == 8) {                                        // (for the key's rests)
-                put(8, 4 + block, h4);
-                put(9, 4 + block, l4);
-            }
-        }
-        fence_async_shared();
-        if (__syncthreads_and(ok) && threadIdx.x == 0) {
-            for (int j = 0; j < 5; ++j)
-                for (int part = 0; part < 2; ++part)
-                    tma_store_2d(&tmap_out, smem + L::kW + (2 * j + part) * (128 * 128), (static_cast<int>(row0) + part * 16) * kC8Row + j * 128, b0);
-            tma_store_commit();
-            tma_store_wait_all();
-        }
-    } else {
-        uint32_t* warp_max = reinterpret_cast<uint32_t*>(smem + L::kMax);      // magnitudes as the bits of absolute values
-        float* inv_s = reinterpret_cast<float*>(warp_max + 17 * 16);
-        // the rotated part: eight threads a request, eight channels a thread
-        const int r8 = threadIdx.x >> 3, c8 = (threadIdx.x & 7) * 8;
-        uint4 turned = make_uint4(0u, 0u, 0u, 0u);
-        if (warp < 4) {
-            turned = rotated(r8, c8);
-            const uint32_t w[4] = {turned.x, turned.y, turned.z, turned.w};
-            uint32_t most = 0u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) most = max(most, max((w[k] << 16) & 0x7fffffffu, w[k] & 0x7fff0000u));
-#pragma unroll
-            for (int d = 1; d < 8; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
-            if ((threadIdx.x & 7) == 0) warp_max[16 * 16 + r8] = most;
-        }
-        const bool ok = mbar_wait_warp(&done[block], 0, abort_flag, status, 0x92);
-        tc_fence_after_sync();
-        uint32_t v[16];
-        tmem_ld_x16(column, v);
-        tmem_ld_wait();
-        float mags[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mags[r] = fabsf(__uint_as_float(v[r]));
-        const float mine = warp_reduce_each(mags, lane, [](float x, float y) { return fmaxf(x, y); });
-        if ((lane & 1) == 0) warp_max[warp * 16 + (lane >> 1)] = __float_as_uint(mine);
-        __syncthreads();
-        if (threadIdx.x < 16) {
-            const int r = threadIdx.x;
-            uint32_t most = 0u;
-#pragma unroll
-            for (int w = 0; w < 17; ++w) most = max(most, warp_max[w * 16 + r]);
-            const int e = exponent_of(__uint_as_float(most));
-            inv_s[r] = e == 128 ? 0.f : exact_exp2(-e);
-            if (b0 + r < B) q_scale[static_cast<size_t>(b0 + r) * h_pad + head] = exact_exp2(e);
-        }
-        __syncthreads();
-        // D is latents x requests, a part's box requests x 128 latents: transposed on the way through shared memory (over the weights, which the
-        // MMAs have read); requests past B are clipped by the map.
-        uint8_t* box = smem + L::kW + block * 2 * (16 * 128) + (warp & 3) * 32 + lane;
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-            uint32_t hi, lo;
-            parts(f2(__uint_as_float(v[r]), __uint_as_float(v[r + 1])), f2(inv_s[r], inv_s[r + 1]), hi, lo);
-            uint8_t* at = box + r * 128;
-            at[0] = static_cast<uint8_t>(hi);
-            at[128] = static_cast<uint8_t>(hi >> 8);
-            at[16 * 128] = static_cast<uint8_t>(lo);
-            at[16 * 128 + 128] = static_cast<uint8_t>(lo >> 8);
-        }
-        fence_async_shared();
-        if (warp < 4 && r8 < B - b0) store_rotated(turned, r8, c8, inv_s[r8]);
-        if (__syncthreads_and(ok) && threadIdx.x == 0) {
-            for (int j = 0; j < 4; ++j)
-                for (int part = 0; part < 2; ++part)
-                    tma_store_2d(&tmap_out, smem + L::kW + (2 * j + part) * (16 * 128), (static_cast<int>(row0) + part * 16) * kC8Row + j * 128, b0);
-            tma_store_commit();
-            tma_store_wait_all();
-        }
+    for (int r = 0; r < 16; r += 2) {
+        const float2 x = make_float2(__uint_as_float(v[r]) * inv_s[r], __uint_as_float(v[r + 1]) * inv_s[r + 1]);
+        uint32_t hi, lo;
+        absorb8_parts(f2(x.x, x.y), 1.0f, hi, lo);
+        uint8_t* at = box + r * 128;
+        at[0] = static_cast<uint8_t>(hi);
+        at[128] = static_cast<uint8_t>(hi >> 8);
+        at[16 * 128] = static_cast<uint8_t>(lo);
+        at[16 * 128 + 128] = static_cast<uint8_t>(lo >> 8);
+    }
+    fence_async_shared();
+    if (warp < 4 && r8 < B - b0) absorb8_store_rotated(turned, rows + (static_cast<size_t>(b0 + r8) * 2 * h_pad + row0) * kC8Row, c8, inv_s[r8]);
+    if (__syncthreads_and(ok) && threadIdx.x == 0) {
+        for (int j = 0; j < 4; ++j)
+            for (int part = 0; part < 2; ++part)
+                tma_store_2d(&tmap_out, smem + L::kW + (2 * j + part) * (16 * 128), (static_cast<int>(row0) + part * 16) * kC8Row + j * 128, b0);
+        tma_store_commit();
+        tma_store_wait_all();
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 4 * kN); }
+    if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 64); }
+}
+
+constexpr int kAbsorbRows = 128, kAbsorbRowsThreads = 256;
+struct DecodeAbsorb8RowsSmem {
+    static constexpr int kW = 0;                                 // two slabs of 128 rows x 64 channels; later the parts' boxes
+    static constexpr int kQ = kW + 2 * 128 * 128;
+    static constexpr int kMax = kQ + 2 * 128 * 128;              // [2 groups][128], [4 CTAs][128], [128] of the rotated part
+    static constexpr int kBar = kMax + 7 * 128 * 4;
+    static constexpr int kTotalBytes = kBar + 32;
+};
+__global__ void __cluster_dims__(4, 1, 1) __launch_bounds__(kAbsorbRowsThreads)
+decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_out,
+                           const __nv_bfloat16* __restrict__ q, int B, int h, int h_pad, uint8_t* __restrict__ rows, float* __restrict__ q_scale,
+                           unsigned* status, int status_words) {
+    using L = DecodeAbsorb8RowsSmem;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
+    uint64_t* done = full + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 2);
+    AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
+    float *group_max = reinterpret_cast<float*>(smem + L::kMax), *cta_max = group_max + 2 * kAbsorbRows, *turned_max = cta_max + 4 * kAbsorbRows;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int rank = static_cast<int>(cluster_cta_rank()), head = blockIdx.y, b0 = blockIdx.z * kAbsorbRows, c0 = rank * 128;
+    const int half = warp >> 2, r = (warp & 3) * 32 + lane;      // this thread's request; its half of the latents
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < status_words) {       // (as in decode_absorb_kernel)
+        status[threadIdx.x] = 0u;
+        __threadfence();
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(full, 1); mbar_init(done, 1);
+        abort_flag->value = 0;
+        mbar_fence_init();
+        mbar_arrive_expect_tx(full, 4 * 128 * 128);
+        for (int k = 0; k < 2; ++k) {
+            tma_load_2d_chk(status, smem + L::kW + k * 128 * 128, &tmap_w, full, head * 256 + k * 64, c0);
+            tma_load_2d_chk(status, smem + L::kQ + k * 128 * 128, &tmap_q, full, head * 192 + k * 64, b0);
+        }
+    }
+    if (warp == 1) { tmem_alloc(tmem_slot, 128); tmem_relinquish(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (the peers run: waited for before the first word to them)
+    grid_launch_dependents();
+    const uint32_t tmem = *tmem_slot;
+    if (warp == 0) {
+        if (elect_one()) {
+            if (mbar_wait(full, 0, abort_flag, status, 0x92)) {
+                tc_fence_after_sync();
+                constexpr uint32_t idesc = make_idesc_bf16(128, 128, 0, 0);
+                const uint64_t da = desc_k_major(smem_u32(smem + L::kQ)), db = desc_k_major(smem_u32(smem + L::kW));
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                    mma_ss(tmem, da + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, db + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, idesc, kk > 0 ? 1u : 0u);
+                mma_commit(done);
+            } else {
+                mbar_wait_quiesce(full, 0);
+            }
+        }
+        __syncwarp();
+    }
+    // The rotated part of a quarter of the requests, eight threads a request: this CTA's.
+    const int r8 = rank * 32 + static_cast<int>(threadIdx.x >> 3), c8 = (threadIdx.x & 7) * 8;
+    const bool live8 = b0 + r8 < B;
+    uint4 turned = make_uint4(0u, 0u, 0u, 0u);
+    if (live8) turned = *reinterpret_cast<const uint4*>(q + (static_cast<size_t>(b0 + r8) * h + head) * 192 + 128 + c8);
+    {
+        float most = absorb8_magnitude(turned);
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        if ((threadIdx.x & 7) == 0) turned_max[r8] = most;
+    }
+    const bool ok = mbar_wait_warp(done, 0, abort_flag, status, 0x93);
+    tc_fence_after_sync();
+    const uint32_t column = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64;
+    float most = 0.f;
+    uint32_t v[32];
+#pragma unroll 1
+    for (int c = 0; c < 64; c += 32) {
+        tmem_ld_x32(column + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) most = fmax3(most, fabsf(__uint_as_float(v[i])), fabsf(__uint_as_float(v[i + 1])));
+    }
+    group_max[half * kAbsorbRows + r] = most;
+    __syncthreads();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (half == 0) {
+        most = fmaxf(most, group_max[kAbsorbRows + r]);
+        if (r >> 5 == rank) most = fmaxf(most, turned_max[r]);
+#pragma unroll
+        for (uint32_t peer = 0; peer < 4; ++peer)
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_map(cta_max + rank * kAbsorbRows + r, peer)), "f"(most) : "memory");
+    }
+    cluster_sync();
+    auto exponent = [&](int i) {
+        return absorb8_exponent(fmaxf(fmaxf(cta_max[i], cta_max[kAbsorbRows + i]), fmaxf(cta_max[2 * kAbsorbRows + i], cta_max[3 * kAbsorbRows + i])));
+    };
+    const int e = exponent(r);
+    const float inv = e == 128 ? 0.f : exact_exp2(-e);
+    if (rank == 0 && half == 0 && b0 + r < B) q_scale[static_cast<size_t>(b0 + r) * h_pad + head] = exact_exp2(e);
+    // The two parts' boxes of 128 requests x 128 codes over the weights, which the MMAs have read (each thread has seen that above), and from there
+    // whole rows by TMA: a lane that stored its own row would touch 32 lines an instruction.  Requests past B are clipped by the map.
+    uint8_t* line = smem + L::kW + r * 128;                      // + part * 16 KB; 16-byte chunk c at c ^ (r & 7)
+#pragma unroll 1
+    for (int k = 0; k < 4; ++k) {
+        tmem_ld_x16(column + 16 * k, v);
+        tmem_ld_wait();
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t a[2], b[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) absorb8_parts(f2(__uint_as_float(v[4 * i + 2 * m]), __uint_as_float(v[4 * i + 2 * m + 1])), inv, a[m], b[m]);
+            hi[i] = __byte_perm(a[0], a[1], 0x5410);
+            lo[i] = __byte_perm(b[0], b[1], 0x5410);
+        }
+        const int chunk = ((half * 4 + k) ^ (r & 7)) << 4;
+        *reinterpret_cast<uint4*>(line + chunk) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(line + 128 * 128 + chunk) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    fence_async_shared();
+    const size_t row0 = (head >> 4) * 32 + (head & 15);          // of the request's 2 h_pad rows: the head's first part; the second 16 on
+    if (live8) {
+        const int e8 = exponent(r8);
+        absorb8_store_rotated(turned, rows + (static_cast<size_t>(b0 + r8) * 2 * h_pad + row0) * kC8Row, c8, e8 == 128 ? 0.f : exact_exp2(-e8));
+    }
+    if (__syncthreads_and(ok) && threadIdx.x == 0) {
+        for (int part = 0; part < 2; ++part)
+            tma_store_2d(&tmap_out, smem + L::kW + part * (128 * 128), (static_cast<int>(row0) + part * 16) * kC8Row + c0, b0);
+        tma_store_commit();
+        tma_store_wait_all();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 128); }
 }
 
 }  // namespace laga

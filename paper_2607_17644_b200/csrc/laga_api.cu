@@ -94,8 +94,8 @@ bool make_tmap_cache(CUtensorMap* map, const void* base, uint64_t rows, uint32_t
 
 // Maps over 8-bit codes (boxes of 128 of them, out of range reads as zero):
 //   kMapPages    the cache: 640 codes x rows of a page x pages (`rows` pages, `stride` bytes apart, of `inner` rows each), 128-byte swizzle
-//   kMapQueries  2-d, 128-byte swizzle: the queries' rows, as the attention reads them and decode_absorb8_kernel<true> writes them
-//   kMapStore    2-d, no swizzle: as decode_absorb8_kernel<false> writes them
+//   kMapQueries  2-d, 128-byte swizzle: the queries' rows, as the attention reads them and decode_absorb8_rows_kernel writes them
+//   kMapStore    2-d, no swizzle: as decode_absorb8_kernel writes them
 // and one over bf16 weights, kMapTurned: W's rows r as (r % 128, r / 128), boxes of 64 channels x 4 x 64, 128-byte swizzle (`rows`: 512)
 enum : uint32_t { kMapPages = 16, kMapQueries = 17, kMapStore = 18, kMapTurned = 19 };
 bool make_tmap_codes(CUtensorMap* map, uint32_t kind, const void* base, uint64_t inner, uint64_t rows, uint64_t stride, uint32_t box_rows) {
@@ -185,8 +185,8 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_decode8_sm100_kernel<16>, AttnDecode8Smem<16>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<32>, AttnDecode8Smem<32>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<64>, AttnDecode8Smem<64>::kTotalBytes) &&
-              allow_smem(decode_absorb8_kernel<false>, DecodeAbsorb8Smem<false>::kTotalBytes) &&
-              allow_smem(decode_absorb8_kernel<true>, DecodeAbsorb8Smem<true>::kTotalBytes) &&
+              allow_smem(decode_absorb8_kernel, DecodeAbsorb8Smem::kTotalBytes) &&
+              allow_smem(decode_absorb8_rows_kernel, DecodeAbsorb8RowsSmem::kTotalBytes) &&
               allow_smem(decode_project_kernel<false>, DecodeProjectSmem::kTotalBytes) &&
               allow_smem(decode_project_kernel<true>, DecodeProjectSmem::kTotalBytes) &&
               allow_smem(latent_norm_rope_fwd_kernel<2, false>, latent_fwd_smem(256, kRopeMaxRot)) &&
@@ -842,15 +842,16 @@ Decode8Layout decode8_layout(int B, int h) {
 
 int launch_decode_absorb8(const void* q, const void* w, int B, int h, int h_pad, uint8_t* rows, float* q_scale, unsigned* status, cudaStream_t stream) {
     const uint64_t q_row = static_cast<uint64_t>(h) * (kDn + kDr), w_row = static_cast<uint64_t>(h) * (kDn + kDv), request = 2ull * h_pad * kC8Row;
-    // Tiles of 16 requests where each can have an SM of its own; otherwise of 128, which read a head's weights once.
+    // Tiles of 16 requests where each can have an SM of its own; otherwise of 128, for which a head's weights are read once.
     const bool few = static_cast<long long>(h) * ((B + 15) / 16) <= sm_count();
-    const int tile = few ? 16 : 128, words = static_cast<int>(kStatusClearBytes / sizeof(unsigned));
+    const int tile = few ? DecodeAbsorb8Smem::kTile : kAbsorbRows, words = static_cast<int>(kStatusClearBytes / sizeof(unsigned));
     CUtensorMap tw, tq, to;
     if (!cached_tmap_bf16(&tw, w, w_row, kDc, w_row * 2, 128) || !cached_tmap_bf16(&tq, q, q_row, B, q_row * 2, tile) ||
         !cached_tmap_codes(&to, few ? kMapStore : kMapQueries, rows, request, B, request, tile))
         return LAGA_ERR_CUDA;
-    launch_kernel(few ? decode_absorb8_kernel<false> : decode_absorb8_kernel<true>, dim3(h, (B + tile - 1) / tile), dim3(kAbsorb8Threads),
-                  few ? DecodeAbsorb8Smem<false>::kTotalBytes : DecodeAbsorb8Smem<true>::kTotalBytes, stream, false, tw, tq, to,
+    const dim3 grid = few ? dim3(h, (B + tile - 1) / tile) : dim3(4, h, (B + tile - 1) / tile);
+    launch_kernel(few ? decode_absorb8_kernel : decode_absorb8_rows_kernel, grid, dim3(few ? kAbsorb8Threads : kAbsorbRowsThreads),
+                  few ? DecodeAbsorb8Smem::kTotalBytes : DecodeAbsorb8RowsSmem::kTotalBytes, stream, false, tw, tq, to,
                   static_cast<const __nv_bfloat16*>(q), B, h, h_pad, rows, q_scale, status, words);
     return launch_status();
 }
