@@ -303,8 +303,8 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
  *   and slots as there): row slots[m] receives token m, rounded once, from fp32; a slot outside the cache writes nothing.
  * laga_cache8_read: latent bf16 [M, 512] (exact) and k_pe bf16 [M, 64] (rounded once) of the rows slots[m], what laga_fwd takes as c_kv and
  *   k_pe; zeros where a slot is outside the cache.  Slots may repeat.
- * laga_paged_decode8: laga_paged_decode over such a cache, with its arguments, limits, errors and results, and a workspace of its own size.  The
- *   scale must be a power of two, or zero for a row of zeros.  q W_uk and the rotated queries are carried in two e4m3 parts each, over a power
+ * laga_paged_decode8: laga_paged_decode over such a cache, with its arguments, limits, errors and results, and a workspace of its own size.  A
+ *   scale must be a power of two from 2^-32 on, or zero in a row whose codes are zeros (a page that was cleared: a row of zeros).  q W_uk and the rotated queries are carried in two e4m3 parts each, over a power
  *   of two for each request and head (together 2^-8 of a channel, half a step of bf16); so are the probabilities (2^-8; over 32 heads 2^-7, half
  *   a step more), each tile of 128 keys at a reference of its own: weights below 2^-12 of a tile's largest may be dropped.  Sums,
  *   references and the accumulator are fp32.

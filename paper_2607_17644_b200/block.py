@@ -12,9 +12,9 @@ the projections deliver them (the paper's algorithm has no rotary step of its ow
 rotation (``rope``, from ``laga.rope_plan``): then step 1 ends with laga_rope on the queries, and laga_latent_norm_rope
 takes the latent's norm and the key's rotation in one pass over what W_kv_a delivers.
 
-In service the block keeps, per token, the normalised latent and the rotated key in a paged cache (``serving.LatentCache``):
-``prefill`` runs prompts through the path above and fills the cache, ``decode`` adds one token per request and attends
-to the cache through laga_paged_decode.
+In service the block keeps, per token, the normalised latent and the rotated key in a paged cache (``serving.LatentCache``), in bf16 or
+in 8 bits: ``prefill`` runs prompts through the path above and fills the cache, ``decode`` adds one token per request and attends
+to the cache through laga_paged_decode or laga_paged_decode8.
 
 Weights are stored as [in_features, out_features] (y = x W), the layout ``W_kv_b`` already has.  Weight
 gradients leave the kernels in fp32 and are handed to autograd in the weight's dtype.
@@ -190,6 +190,7 @@ class LagaBlock(torch.nn.Module):
         """Prompts of requests that have nothing in the cache yet, packed: hidden [T, d_model], cu_seqlens their host
         boundaries (the same lengths that ``step``, a plan of ``LatentCache.plan``, was made for), pages one layer's
         cache [n_pages, page_size, 576].  Returns the block's output [T, d_model]; the cache holds the prompts afterwards.
+        With a cache in 8 bits the prompts attend to what it holds of them (laga_cache8_read), as every later token will.
         workspace (``laga.fwd_varlen_workspace_bytes``): give one to have the attention's status, as for ``decode``.
         A step that is not that -- a request held tokens already, other lengths, a plan that could not be placed -- is refused on the
         device: nothing enters the cache, the output is NaN, and ``laga.check_status(step.status)`` raises LAGA_ERR_CACHE_PLAN."""
@@ -201,7 +202,12 @@ class LagaBlock(torch.nn.Module):
         refused = self._not_these_prompts(step, positions, slots, cu_seqlens)
         slots, gamma = torch.where(refused, -1, slots), torch.where(refused, float("nan"), self.ln_gamma)
         laga.rope(q, positions, self.rope, y=q)
-        latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
+        if pages.dtype == torch.uint8:
+            laga.cache_append(kv_a, gamma, self.ln_beta, positions, self.rope, slots, pages, eps=self.eps)
+            latent, k_pe = laga.cache_read(pages, slots)
+            k_pe.masked_fill_(refused, float("nan"))         # (nothing was written, so nothing is read)
+        else:
+            latent, k_pe, _, _ = laga.latent_norm_rope(kv_a, gamma, self.ln_beta, positions, self.rope, self.eps, cache=pages, slots=slots)
         out = laga.fwd(q, latent, k_pe, self.w_kv_b, softmax_scale=self.softmax_scale, workspace=workspace, cu_seqlens=cu_seqlens)[0]
         return laga.linear(out.view(T, self.n_heads * self.D_V), self.w_o)[0]
 
@@ -213,7 +219,7 @@ class LagaBlock(torch.nn.Module):
         Where the plan gave only some requests a token, ``requests`` (int64 [B], on the device, ascending) names them; rows of
         ``hidden`` behind the plan's tokens are padding (any request's number, results to be ignored).
         Appends the tokens' latents and keys to ``pages`` and attends to each request's whole cache, the new token included.  Every call reads lengths and tables on the device, so a step can be captured in a
-        graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``) and replayed.  A page number outside the cache or a
+        graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``, with cache8 for a cache in 8 bits) and replayed.  A page number outside the cache or a
         length outside the table shows only in the workspace's status: give one, and ``laga.check_status(workspace)`` raises
         (with no workspace given, nothing of it is left to ask)."""
         self._service()

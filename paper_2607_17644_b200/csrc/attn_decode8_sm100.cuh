@@ -482,7 +482,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 uint32_t hi[kPer], lo[kPer];
                 tmem_ld_heads<kPer>(col_s + buf * (2 * kHeads), hi);
                 tmem_ld_heads<kPer>(col_s + buf * (2 * kHeads) + 16, lo);
-                if (key >= valid) s = 1.0f;
+                if (key >= valid || s == 0.f) s = 1.0f;        // (a page as it was made, of zeros: a row of zeros)
                 const float ef = static_cast<float>(static_cast<int>(__float_as_uint(s) >> 23 & 0xffu) - 127);
                 const F2 s2 = f2(s, s), e2 = f2(ef, ef), minus1 = f2(-1.0f, -1.0f);
                 const ulonglong2 *f = reinterpret_cast<const ulonglong2*>(factor_s + h0), *m = reinterpret_cast<const ulonglong2*>(ref_s + h0);
@@ -495,7 +495,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                         const int c = 2 * (i + j);
                         const F2 both = f2_add(f2(__uint_as_float(hi[c]), __uint_as_float(hi[c + 1])), f2(__uint_as_float(lo[c]), __uint_as_float(lo[c + 1])));
                         // (y rounded before m is taken off: the largest score of a tile is then at its place whatever its size)
-                        const F2 y = f2_fma(f2_mul(both, s2), F2{j == 0 ? f4.x : f4.y}, e2);
+                        const F2 y = f2_fma(both, f2_mul(F2{j == 0 ? f4.x : f4.y}, s2), e2);
                         d[i + j] = f2_fma(F2{j == 0 ? m4.x : m4.y}, minus1, y);
                     }
                 }
