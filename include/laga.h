@@ -304,10 +304,11 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
  * laga_cache8_read: latent bf16 [M, 512] (exact) and k_pe bf16 [M, 64] (rounded once) of the rows slots[m], what laga_fwd takes as c_kv and
  *   k_pe; zeros where a slot is outside the cache.  Slots may repeat.
  * laga_paged_decode8: laga_paged_decode over such a cache, with its arguments, limits, errors and results, and a workspace of its own size.  A
- *   scale must be a power of two from 2^-32 on, or zero in a row whose codes are zeros (a page that was cleared: a row of zeros).  q W_uk and the rotated queries are carried in two e4m3 parts each, over a power
- *   of two for each request and head (together 2^-8 of a channel, half a step of bf16); so are the probabilities (2^-8; over 32 heads 2^-7, half
- *   a step more), each tile of 128 keys at a reference of its own: weights below 2^-12 of a tile's largest may be dropped.  Sums,
- *   references and the accumulator are fp32.
+ *   scale must be a power of two from 2^-32 on, or zero in a row whose codes are zeros (a page that was cleared: a row of zeros).  q W_uk and
+ *   the rotated queries are carried in two e4m3 parts each, over a power of two for each request and head (together 2^-8 of a channel, half a
+ *   step of bf16).  So are the weights, each the probability times the token's scale (2^-8, over 32 heads 2^-7 of it), at a reference that each
+ *   tile of 128 keys is held to: besides, a weight may be off by 2^-12 of its tile's largest (over 32 heads 2^-10), so that smaller ones may be
+ *   lost.  Sums, references and the accumulator are fp32.
  */
 int laga_cache8_append(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps, const int* positions,
                        const double* freqs, int M, int layout, float mscale, void* cache, int n_pages, int page_size, const int* slots,

@@ -32,11 +32,33 @@
 namespace laga {
 
 constexpr int kD8Keys = 128;                 // keys of a tile
-constexpr int kD8Unit = kDecKeys;            // keys of a unit of the line
+constexpr int kD8Unit = kDecKeys;            // keys of a unit of the line: a tile is one or two
 constexpr float kD8Lift = 7.0f;              // where a tile's maximum is put ...
 constexpr float kD8High = 11.0f;             // ... and the most it may become; the least is 0
 constexpr float kD8Fall = 40.0f;
 constexpr float kD8LoScale = 32.0f;
+
+// Two pairs of fp16 numbers as four codes and the codes of what is left: e4m3, and 32 times the rest; or e5m2, and the rest in e4m3.  (One block of
+// instructions: halves of registers that the compiler sees one by one are moved about.)
+__device__ __forceinline__ void parts_e4m3_scaled(uint32_t x, uint32_t y, uint32_t& hi, uint32_t& lo) {
+    asm("{\n\t.reg .b16 a, b;\n\t.reg .b32 u, v, s;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f16x2 a, %2;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %3;\n\t"
+        "mov.b32 %0, {a, b};\n\tcvt.rn.f16x2.e4m3x2 u, a;\n\tcvt.rn.f16x2.e4m3x2 v, b;\n\t"
+        "mov.b32 s, 0x50005000;\n\t"                        // 32 twice
+        "sub.rn.f16x2 u, %2, u;\n\tsub.rn.f16x2 v, %3, v;\n\tmul.rn.f16x2 u, u, s;\n\tmul.rn.f16x2 v, v, s;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f16x2 a, u;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, v;\n\tmov.b32 %1, {a, b};\n\t}"
+        : "=&r"(hi), "=&r"(lo)
+        : "r"(x), "r"(y));
+}
+__device__ __forceinline__ void parts_e5m2_e4m3(uint32_t x, uint32_t y, uint32_t& hi, uint32_t& lo) {
+    asm("{\n\t.reg .b16 a, b;\n\t.reg .b32 u, v;\n\t"
+        "cvt.rn.satfinite.e5m2x2.f16x2 a, %2;\n\tcvt.rn.satfinite.e5m2x2.f16x2 b, %3;\n\t"
+        "mov.b32 %0, {a, b};\n\tcvt.rn.f16x2.e5m2x2 u, a;\n\tcvt.rn.f16x2.e5m2x2 v, b;\n\t"
+        "sub.rn.f16x2 u, %2, u;\n\tsub.rn.f16x2 v, %3, v;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f16x2 a, u;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, v;\n\tmov.b32 %1, {a, b};\n\t}"
+        : "=&r"(hi), "=&r"(lo)
+        : "r"(x), "r"(y));
+}
 
 template <int kHeads>
 struct AttnDecode8Smem {
@@ -91,8 +113,11 @@ struct Decode8Cursor {
     __device__ __forceinline__ int units() const { return min(min(2, n - t), left); }
     __device__ __forceinline__ bool ends_piece() const { return t + 2 >= n || left <= 2; }
     __device__ __forceinline__ int valid() const { return min(units() * kD8Unit, len - t * kD8Unit); }
-    __device__ __forceinline__ void next(const AttnDecodeArgs& a) {
-        const int u = units();
+    __device__ __forceinline__ void next(const AttnDecodeArgs& a) { advance(a, units()); }
+    // The same by pieces: the keys of this one from here on, tiles of kD8Keys and what is left; and the next one.
+    __device__ __forceinline__ int piece_keys() const { return min(min(n - t, left) * kD8Unit, len - t * kD8Unit); }
+    __device__ __forceinline__ void next_piece(const AttnDecodeArgs& a) { advance(a, min(n - t, left)); }
+    __device__ __forceinline__ void advance(const AttnDecodeArgs& a, int u) {
         left -= u;
         t += u;
         if (t >= n && left > 0) { t = 0; ++b; open(a); }
@@ -124,12 +149,6 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 constexpr int kOrderedLowest = static_cast<int>(0x80000000u);
-template <int kPer>
-__device__ __forceinline__ void tmem_ld_heads(uint32_t taddr, uint32_t* r) {
-    if constexpr (kPer == 16) tmem_ld_x16(taddr, r);
-    else tmem_ld_x8(taddr, r);
-}
-
 template <int kHeads>
 __global__ void __launch_bounds__(AttnDecode8Smem<kHeads>::kThreads, 1)
 attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_codes, const AttnDecode8Args all) {
@@ -277,11 +296,6 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     }
                 }
             }
-            if constexpr (!kFirst && L::kSlabs < 10) {       // less than two tiles: the last slab waits for the values of the tile before
-#pragma unroll
-                for (int i = 0; i < kSubs; ++i)
-                    if (i < boxes) tma_prefetch_codes(&tmap_codes, 3 * 128, (row0 + i * kBox) & in_page, pages[i]);
-            }
 #pragma unroll
             for (uint32_t s = 0; s < kCount; ++s) {          // the key's slab, then the latent's four
                 const uint32_t bar = full_a + slot * 8;
@@ -427,7 +441,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         const int g = warp >> 2, quarter = warp & 3, key = quarter * 32 + lane, tid = key;      // (thread of the group)
         const int h0 = g * kPer;                               // the group's heads within the CTA's
         const int n_live = max(0, min(kPer, args.h - head0 - h0));
-        const uint32_t live = (1u << n_live) - 1u;             // bit i: the group's head i is one
+        const uint32_t live = ((1u << n_live) - 1u) << (kPer - n_live);      // bit kPer - 1 - i: the group's head i is one
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
         // sixteen heads' scores are 32 columns, first the products with hi, then those with lo; so are their columns of O^T where P has two parts
         const uint32_t sixteen = static_cast<uint32_t>(h0 >> 4), within = static_cast<uint32_t>(h0 & 15);
@@ -449,9 +463,10 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         };
         grid_dependency_wait();
         float factor = query_scale(cur);
+        int keys_left = cur.piece_keys();
         while (!cur.done()) {
             const uint32_t buf = T & 1u, par = (T >> 1) & 1u;
-            const int valid = cur.valid();
+            const int valid = min(kD8Keys, keys_left);
             if (first) {
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) l2[i] = f2(0.f, 0.f);
@@ -479,9 +494,13 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             F2 d[kPairs];
             float s = reinterpret_cast<const float*>(smem + L::kScale)[(T % L::kScales) * kD8Keys + key];
             {
-                uint32_t hi[kPer], lo[kPer];
-                tmem_ld_heads<kPer>(col_s + buf * (2 * kHeads), hi);
-                tmem_ld_heads<kPer>(col_s + buf * (2 * kHeads) + 16, lo);
+                uint32_t raw[2 * kPer];                        // the products with hi, then those with lo
+                if constexpr (kPer == 16) {
+                    tmem_ld_x32(col_s + buf * (2 * kHeads), raw);
+                } else {
+                    tmem_ld_x8(col_s + buf * (2 * kHeads), raw);
+                    tmem_ld_x8(col_s + buf * (2 * kHeads) + 16, raw + kPer);
+                }
                 if (key >= valid || s == 0.f) s = 1.0f;        // (a page as it was made, of zeros: a row of zeros)
                 const float ef = static_cast<float>(static_cast<int>(__float_as_uint(s) >> 23 & 0xffu) - 127);
                 const F2 s2 = f2(s, s), e2 = f2(ef, ef), minus1 = f2(-1.0f, -1.0f);
@@ -493,7 +512,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const int c = 2 * (i + j);
-                        const F2 both = f2_add(f2(__uint_as_float(hi[c]), __uint_as_float(hi[c + 1])), f2(__uint_as_float(lo[c]), __uint_as_float(lo[c + 1])));
+                        const F2 both = f2_add(f2(__uint_as_float(raw[c]), __uint_as_float(raw[c + 1])), f2(__uint_as_float(raw[kPer + c]), __uint_as_float(raw[kPer + c + 1])));
                         // (y rounded before m is taken off: the largest score of a tile is then at its place whatever its size)
                         const F2 y = f2_fma(both, f2_mul(F2{j == 0 ? f4.x : f4.y}, s2), e2);
                         d[i + j] = f2_fma(F2{j == 0 ? m4.x : m4.y}, minus1, y);
@@ -504,20 +523,20 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) d[i] = f2(-INFINITY, -INFINITY);
             }
-            // Does the reference hold?  For every head some key must have d >= 0, and none more than kD8High: a bit a head, and the last.  (A piece's
-            // first tile has no reference yet.)
+            // Does the reference hold?  For every head some key must have d >= 0, and none more than kD8High: the signs of d, a bit a head (the first
+            // head's the highest of them), across the keys, and a bit that is set where nothing is above.  (A piece's first tile has no reference yet.)
             if (!first) {
-                uint32_t held = 0u;
+                uint32_t below = 0u;
                 float most = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) {
                     const float2 v = f2_parts(d[i]);
-                    held |= __any_sync(0xffffffffu, v.x >= 0.f) ? 1u << (2 * i) : 0u;
-                    held |= __any_sync(0xffffffffu, v.y >= 0.f) ? 2u << (2 * i) : 0u;
+                    below = __funnelshift_l(__float_as_uint(v.x), below, 1);
+                    below = __funnelshift_l(__float_as_uint(v.y), below, 1);
                     most = fmax3(most, v.x, v.y);
                 }
-                held |= __any_sync(0xffffffffu, most > kD8High) ? 1u << 16 : 0u;
-                if (lane == 0) vote_s[buf * (4 * L::kGroups) + quarter] = static_cast<int>(held);
+                below = __reduce_and_sync(0xffffffffu, below | (most > kD8High ? 0u : 0x80000000u));
+                if (lane == 0) vote_s[buf * (4 * L::kGroups) + quarter] = static_cast<int>(below);
                 arrive();
             }
             // Probabilities and their parts, while the group's other warps vote
@@ -526,22 +545,17 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             auto weigh = [&]() {
 #pragma unroll
                 for (int i = 0; i < kPer / 4; ++i) {
-                    uint32_t a[2], b[2];
+                    uint32_t p16[2];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const float2 v = f2_parts(L::kSplit ? f2_add(d[2 * i + j], f2(-L::kDrop, -L::kDrop)) : d[2 * i + j]);
                         const float2 w = make_float2(fast_exp2(v.x), fast_exp2(v.y));
                         p[2 * i + j] = f2(w.x, w.y);
                         const __half2 ph = __floats2half2_rn(w.x, w.y);
-                        const uint32_t p16 = *reinterpret_cast<const uint32_t*>(&ph);
-                        a[j] = L::kSplit ? e4m3x2_of_half2(p16) : e5m2x2_of_half2(p16);
-                        const uint32_t held = L::kSplit ? half2_of_e4m3x2(a[j]) : half2_of_e5m2x2(a[j]);
-                        __half2 rest = __hsub2(ph, *reinterpret_cast<const __half2*>(&held));
-                        if constexpr (L::kSplit) rest = __hmul2(rest, __float2half2_rn(kD8LoScale));
-                        b[j] = e4m3x2_of_half2(*reinterpret_cast<const uint32_t*>(&rest));
+                        p16[j] = *reinterpret_cast<const uint32_t*>(&ph);
                     }
-                    hi[i] = __byte_perm(a[0], a[1], 0x5410);
-                    lo[i] = __byte_perm(b[0], b[1], 0x5410);
+                    if constexpr (L::kSplit) parts_e4m3_scaled(p16[0], p16[1], hi[i], lo[i]);
+                    else parts_e5m2_e4m3(p16[0], p16[1], hi[i], lo[i]);
                 }
             };
             if (!first) weigh();
@@ -552,8 +566,8 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             if (!first) {
                 if (!wait_for_group()) break;
                 const int4 votes = *reinterpret_cast<const int4*>(vote_s + buf * (4 * L::kGroups));
-                const uint32_t held = static_cast<uint32_t>(votes.x | votes.y | votes.z | votes.w);
-                holds = (held >> 16) == 0u && (held & live) == live;
+                const uint32_t below = static_cast<uint32_t>(votes.x & votes.y & votes.z & votes.w);
+                holds = (below & (0x80000000u | live)) == 0x80000000u;
             }
             if (!holds) {
                 // The heads' maxima over the tile, then the references they ask for.
@@ -656,10 +670,11 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             __syncwarp();
             if (lane == 0) mbar_arrive(&p_full[buf]);
             first = false;
-            const bool ends = cur.ends_piece();
-            const int b = cur.b;
-            cur.next(args);
-            if (ends) {
+            keys_left -= kD8Keys;
+            if (keys_left <= 0) {
+                const int b = cur.b;
+                cur.next_piece(args);
+                keys_left = cur.piece_keys();
                 factor = query_scale(cur);                     // the next piece's, on its way meanwhile
                 // the sums over the 128 keys, within the warp
                 float sums[kPer];

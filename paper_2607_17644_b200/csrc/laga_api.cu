@@ -860,7 +860,8 @@ template <int kHeads>
 int launch_attn_decode8(const uint8_t* q_rows, const AttnDecode8Args& a, cudaStream_t stream) {
     CUtensorMap tq, tc;
     if (!cached_tmap_codes(&tq, kMapQueries, q_rows, kC8Row, 2ull * a.d.B * a.d.h_pad, kC8Row, 2 * kHeads) ||
-        !cached_tmap_codes(&tc, kMapPages, a.cache.base, 1ull << a.d.page_shift, a.d.n_pages, a.cache.page_bytes(), a.d.page_shift < 6 ? 1u << a.d.page_shift : 64u))
+        !cached_tmap_codes(&tc, kMapPages, a.cache.base, 1ull << a.d.page_shift, a.d.n_pages, a.cache.page_bytes(),
+                           std::min(1u << a.d.page_shift, static_cast<uint32_t>(kD8Unit))))
         return LAGA_ERR_CUDA;
     ScopedKernelEvents ev(LAGA_KERNEL_ATTN_DECODE, stream);
     launch_kernel(attn_decode8_sm100_kernel<kHeads>, dim3(static_cast<unsigned>(a.d.n_groups * a.d.ctas_per_group)), dim3(AttnDecode8Smem<kHeads>::kThreads),
@@ -1635,7 +1636,7 @@ int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int
     if (!geometry_is_v3(d_c, d_nope, d_rope, d_v)) return LAGA_ERR_UNSUPPORTED;
     // rows, keys and units are counted in 32 bits (byte offsets are not), rows of queries too: two for each padded head
     const long long rows = static_cast<long long>(n_pages) << shift, capacity = static_cast<long long>(columns) << shift;
-    if (rows > (1ll << 30) || capacity > (1ll << 30) || ((capacity + kDecKeys - 1) / kDecKeys) * B > (1ll << 30) ||
+    if (rows > (1ll << 30) || capacity > (1ll << 30) || ((capacity + kD8Unit - 1) / kD8Unit) * B > (1ll << 30) ||
         static_cast<long long>(B) * h > (1ll << 26) || h > 65535 || B > 65535 * 8)
         return LAGA_ERR_INVALID_ARG;
     const Decode8Layout w = decode8_layout(B, h);

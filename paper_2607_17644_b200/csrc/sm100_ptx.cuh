@@ -817,11 +817,6 @@ __device__ __forceinline__ void tma_load_turned_chk(unsigned int* status, void* 
             ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(0), "r"(row)
             : "memory");
 }
-// A box of codes to L2 only.
-__device__ __forceinline__ void tma_prefetch_codes(const CUtensorMap* map, int x, int y, int z) {
-    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z)
-                 : "memory");
-}
 // Two values to two codes, `lo` in the low byte; past the largest number they become it, NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     uint16_t r;
@@ -833,20 +828,10 @@ __device__ __forceinline__ uint32_t e4m3x2_of_half2(uint32_t h) {
     asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
     return r;
 }
-__device__ __forceinline__ uint32_t e5m2x2_of_half2(uint32_t h) {
-    uint16_t r;
-    asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
-    return r;
-}
 // ... and back (exact).
 __device__ __forceinline__ uint32_t half2_of_e4m3x2(uint32_t codes) {
     uint32_t r;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(codes)));
-    return r;
-}
-__device__ __forceinline__ uint32_t half2_of_e5m2x2(uint32_t codes) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(codes)));
     return r;
 }
 __device__ __forceinline__ float2 float2_of_half2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
