@@ -55,8 +55,15 @@ struct Cache8AppendArgs {
 };
 
 // Half a warp per row and a ring of rows in shared memory, as latent_norm_rope_fwd_kernel has it (the arithmetic up to the rounding is the
-// same); what it adds is the largest magnitude of the row, the codes and half the bytes to write.
-template <bool kInterleaved>
+// same); what it adds is the largest magnitude of the row, the codes and half the bytes to write.  Instructions bound it: 65535 rows 22.9 us
+// without beta, 5.2 TB/s (magnitudes as masked integers and beta's zeros added: 26.1; rings of three and four rows: 23.4 and 24.6).
+// The largest magnitude of three, NaN if one is.
+__device__ __forceinline__ float largest3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+template <bool kInterleaved, bool kBeta>
 __global__ void __launch_bounds__(kLnWarps * 32, 2)
 cache8_append_kernel(const Cache8AppendArgs a) {
     constexpr int kRowBytes = (kC8Lat + kC8Key) * 2, kPairs = kC8Key / 2;
@@ -81,11 +88,11 @@ cache8_append_kernel(const Cache8AppendArgs a) {
         position = __ldg(a.rot.positions + m + sub);
         slot = __ldg(a.slots + m + sub);
     }
-    uint4 gamma[4], beta[4];
+    uint4 gamma[4], beta[kBeta ? 4 : 1];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         gamma[i] = __ldg(reinterpret_cast<const uint4*>(a.gamma + i * 128 + q * 8));
-        beta[i] = a.beta != nullptr ? __ldg(reinterpret_cast<const uint4*>(a.beta + i * 128 + q * 8)) : make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (kBeta) beta[i] = __ldg(reinterpret_cast<const uint4*>(a.beta + i * 128 + q * 8));
     }
     const unsigned long long step[2] = {rotary_step(__ldg(a.rot.freqs + q)), rotary_step(__ldg(a.rot.freqs + q + 16))};
     int stage = 0;
@@ -129,9 +136,7 @@ cache8_append_kernel(const Cache8AppendArgs a) {
             const float2 in = rotary_load_pair(key, q + 16 * t, kPairs, kInterleaved);
             k2[t] = rotary_apply(rotary_turn(a.rot, here, step[t]), in.x, in.y);
         }
-        // magnitudes compared as the bits of their absolute values, in which NaN is above infinity and infinity above the rest
-        auto mag = [](float x) { return __float_as_uint(x) & 0x7fffffffu; };
-        uint32_t most = max(max(mag(k2[0].x), mag(k2[0].y)), max(mag(k2[1].x), mag(k2[1].y)));
+        float most = largest3(largest3(k2[0].x, k2[0].y, k2[1].x), k2[1].y, 0.f);
         const float2 sqs = f2_parts(sq);
         const float rstd = rsqrtf(half_warp_sum(sqs.x + sqs.y) * (1.0f / kC8Lat) + a.eps);
         const F2 scale = f2(rstd, rstd);
@@ -139,17 +144,19 @@ cache8_append_kernel(const Cache8AppendArgs a) {
         for (int i = 0; i < 4; ++i) {
             F2 gm[4], bt[4];
             f2_unpack(gamma[i], gm);
-            f2_unpack(beta[i], bt);
+            if constexpr (kBeta) f2_unpack(beta[i], bt);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                v[i][k] = f2_fma(f2_mul(v[i][k], scale), gm[k], bt[k]);
+                v[i][k] = f2_mul(v[i][k], scale);
+                if constexpr (kBeta) v[i][k] = f2_fma(v[i][k], gm[k], bt[k]);
+                else v[i][k] = f2_mul(v[i][k], gm[k]);
                 const float2 x = f2_parts(v[i][k]);
-                most = max(most, max(mag(x.x), mag(x.y)));
+                most = largest3(most, x.x, x.y);
             }
         }
 #pragma unroll
-        for (int d = 8; d > 0; d >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
-        const int e = max(scale_exponent(most), -32);
+        for (int d = 8; d > 0; d >>= 1) most = largest3(most, __shfl_xor_sync(0xffffffffu, most, d), 0.f);
+        const int e = max(scale_exponent(__float_as_uint(most) & 0x7fffffffu), -32);
         const float inv = e == 128 ? 0.f : exact_exp2(-e);
         const F2 inv2 = f2(inv, inv);
         uint8_t* codes = a.cache.row(cached ? to : 0);
@@ -190,13 +197,15 @@ cache8_append_kernel(const Cache8AppendArgs a) {
 // Rows slots[m] of the cache as the dense bf16 rows that the attention over a whole prompt takes: latent[m] and k_pe[m]; zeros where the slot
 // is outside the cache.  The latent is exact (four digits times a power of two), the key is rounded once to bf16.
 // A thread turns 16 codes (of a key: 16 and their rests) into 32 bytes: 36 threads a row, kC8ReadRows rows a thread, whose loads go out together.
-constexpr int kC8ReadUnits = kC8Row / 16 - kC8Key / 16, kC8ReadY = 7, kC8ReadRows = 4;
+// HBM bounds it: 131072 rows 38.5 us, 6.1 TB/s (with four rows a thread, of which fewer are resident, 42.0; with two 16-byte stores for one of 32, 43.8).
+constexpr int kC8ReadUnits = kC8Row / 16 - kC8Key / 16, kC8ReadY = 7, kC8ReadRows = 2;
 struct Cache8ReadArgs {
     Cache8 cache;
     const int* slots;
     int M;
     __nv_bfloat16 *latent, *k_pe;
 };
+template <bool kWide>                                        // the results begin on 32-byte boundaries
 __global__ void __launch_bounds__(kC8ReadUnits * kC8ReadY)
 cache8_read_kernel(const Cache8ReadArgs a) {
     const int u = threadIdx.x;
@@ -232,8 +241,12 @@ cache8_read_kernel(const Cache8ReadArgs a) {
             o[j] = pack_bf16x2(x.x * s[k], x.y * s[k]);
         }
         __nv_bfloat16* dst = is_key ? a.k_pe + static_cast<size_t>(m) * kC8Key + (u - kC8Lat / 16) * 16 : a.latent + static_cast<size_t>(m) * kC8Lat + u * 16;
-        *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<uint4*>(dst + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+        if (kWide) {
+            st_global_v8(dst, o);
+        } else {
+            *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(dst + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+        }
     }
 }
 

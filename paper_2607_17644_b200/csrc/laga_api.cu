@@ -1594,8 +1594,10 @@ int laga_cache8_append(const void* kv_a, long long kv_a_pitch, const void* gamma
     const int rows_per_block = kLnWarps * 2, needed = M / rows_per_block + (M % rows_per_block != 0), cap = sm_count() * 2;       // one resident wave
     const dim3 grid(needed < cap ? needed : cap), block(kLnWarps * 32);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (layout == LAGA_ROPE_INTERLEAVED) cache8_append_kernel<true><<<grid, block, 0, st>>>(a);
-    else cache8_append_kernel<false><<<grid, block, 0, st>>>(a);
+    if (layout == LAGA_ROPE_INTERLEAVED)
+        beta ? cache8_append_kernel<true, true><<<grid, block, 0, st>>>(a) : cache8_append_kernel<true, false><<<grid, block, 0, st>>>(a);
+    else
+        beta ? cache8_append_kernel<false, true><<<grid, block, 0, st>>>(a) : cache8_append_kernel<false, false><<<grid, block, 0, st>>>(a);
     return launch_status();
 }
 
@@ -1613,7 +1615,10 @@ int laga_cache8_read(const void* cache, int n_pages, int page_size, const int* s
     const Cache8ReadArgs a{Cache8{static_cast<uint8_t*>(const_cast<void*>(cache)), shift, static_cast<int>(rows)}, slots, M, static_cast<__nv_bfloat16*>(latent),
                            static_cast<__nv_bfloat16*>(k_pe)};
     const int per_block = kC8ReadY * kC8ReadRows;
-    cache8_read_kernel<<<M / per_block + (M % per_block != 0), dim3(kC8ReadUnits, kC8ReadY), 0, static_cast<cudaStream_t>(stream)>>>(a);
+    const bool wide = ((reinterpret_cast<uintptr_t>(latent) | reinterpret_cast<uintptr_t>(k_pe)) & 31u) == 0;
+    const dim3 grid(M / per_block + (M % per_block != 0)), block(kC8ReadUnits, kC8ReadY);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    wide ? cache8_read_kernel<true><<<grid, block, 0, st>>>(a) : cache8_read_kernel<false><<<grid, block, 0, st>>>(a);
     return launch_status();
 }
 
