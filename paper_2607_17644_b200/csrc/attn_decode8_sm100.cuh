@@ -914,22 +914,26 @@ decode_absorb8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
 }
 
 constexpr int kAbsorbRows = 128, kAbsorbRowsThreads = 256;
+// kSlabs of the queries in shared memory: both halves of q_nope's channels, three CTAs an SM; or one after the other in one place, four an SM, for
+// more CTAs than that.  (250 requests, 64 heads, 512 CTAs: 16.6 us with two, 13.8 with one; 200 requests, 32 heads, 256 CTAs: 8.0, 8.7.)
+template <int kSlabs>
 struct DecodeAbsorb8RowsSmem {
     static constexpr int kW = 0;                                 // two slabs of 128 rows x 64 channels; later the parts' boxes
     static constexpr int kQ = kW + 2 * 128 * 128;
-    static constexpr int kMax = kQ + 2 * 128 * 128;              // [2 groups][128], [4 CTAs][128], [128] of the rotated part
+    static constexpr int kMax = kQ + kSlabs * 128 * 128;         // [2 groups][128], [4 CTAs][128], [128] of the rotated part
     static constexpr int kBar = kMax + 7 * 128 * 4;
-    static constexpr int kTotalBytes = kBar + 32;
+    static constexpr int kTotalBytes = kBar + 40;
 };
+template <int kSlabs>
 __global__ void __cluster_dims__(4, 1, 1) __launch_bounds__(kAbsorbRowsThreads)
 decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_out,
                            const __nv_bfloat16* __restrict__ q, int B, int h, int h_pad, uint8_t* __restrict__ rows, float* __restrict__ q_scale,
                            unsigned* status, int status_words) {
-    using L = DecodeAbsorb8RowsSmem;
+    using L = DecodeAbsorb8RowsSmem<kSlabs>;
     extern __shared__ __align__(1024) uint8_t smem[];
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
-    uint64_t* done = full + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 2);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);      // [2] 64 channels of weights and queries
+    uint64_t* done = full + 2;                                   // [2] their product
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + 4);
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
     float *group_max = reinterpret_cast<float*>(smem + L::kMax), *cta_max = group_max + 2 * kAbsorbRows, *turned_max = cta_max + 4 * kAbsorbRows;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -940,13 +944,13 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
         __threadfence();
     }
     if (threadIdx.x == 0) {
-        mbar_init(full, 1); mbar_init(done, 1);
+        for (int i = 0; i < 4; ++i) mbar_init(&full[i], 1);
         abort_flag->value = 0;
         mbar_fence_init();
-        mbar_arrive_expect_tx(full, 4 * 128 * 128);
         for (int k = 0; k < 2; ++k) {
-            tma_load_2d_chk(status, smem + L::kW + k * 128 * 128, &tmap_w, full, head * 256 + k * 64, c0);
-            tma_load_2d_chk(status, smem + L::kQ + k * 128 * 128, &tmap_q, full, head * 192 + k * 64, b0);
+            mbar_arrive_expect_tx(&full[k], 2 * 128 * 128);
+            tma_load_2d_chk(status, smem + L::kW + k * 128 * 128, &tmap_w, &full[k], head * 256 + k * 64, c0);
+            if (k < kSlabs) tma_load_2d_chk(status, smem + L::kQ + k * 128 * 128, &tmap_q, &full[k], head * 192 + k * 64, b0);
         }
     }
     if (warp == 1) { tmem_alloc(tmem_slot, 128); tmem_relinquish(); }
@@ -958,16 +962,26 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
     const uint32_t tmem = *tmem_slot;
     if (warp == 0) {
         if (elect_one()) {
-            if (mbar_wait(full, 0, abort_flag, status, 0x92)) {
+            constexpr uint32_t idesc = make_idesc_bf16(128, 128, 0, 0);
+            const uint64_t da = desc_k_major(smem_u32(smem + L::kQ)), db = desc_k_major(smem_u32(smem + L::kW));
+            bool ok = true;
+#pragma unroll 1
+            for (int k = 0; k < 2 && ok; ++k) {
+                if (k >= kSlabs) {
+                    ok = mbar_wait(done, 0, abort_flag, status, 0x97);
+                    if (!ok) break;
+                    tma_load_2d_chk(status, smem + L::kQ, &tmap_q, full + 1, head * 192 + 64, b0);
+                }
+                ok = mbar_wait(&full[k], 0, abort_flag, status, 0x92);
+                if (!ok) break;
                 tc_fence_after_sync();
-                constexpr uint32_t idesc = make_idesc_bf16(128, 128, 0, 0);
-                const uint64_t da = desc_k_major(smem_u32(smem + L::kQ)), db = desc_k_major(smem_u32(smem + L::kW));
 #pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                    mma_ss(tmem, da + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, db + (kk >> 2) * (128 * 128 / 16) + (kk & 3) * 2, idesc, kk > 0 ? 1u : 0u);
-                mma_commit(done);
-            } else {
+                for (int kk = 0; kk < 4; ++kk) mma_ss(tmem, da + (k < kSlabs ? k : 0) * (128 * 128 / 16) + kk * 2, db + k * (128 * 128 / 16) + kk * 2, idesc, (k > 0 || kk > 0) ? 1u : 0u);
+                mma_commit(&done[k]);
+            }
+            if (!ok) {
                 mbar_wait_quiesce(full, 0);
+                mbar_wait_quiesce(full + 1, 0);                  // (without its queries it costs the limit, which is longer than any load)
             }
         }
         __syncwarp();
@@ -983,7 +997,7 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
         for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
         if ((threadIdx.x & 7) == 0) turned_max[r8] = most;
     }
-    const bool ok = mbar_wait_warp(done, 0, abort_flag, status, 0x93);
+    const bool ok = mbar_wait_warp(done + 1, 0, abort_flag, status, 0x93);
     tc_fence_after_sync();
     const uint32_t column = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64;
     float most = 0.f;
@@ -1041,6 +1055,210 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
     if (__syncthreads_and(ok) && threadIdx.x == 0) {
         for (int part = 0; part < 2; ++part)
             tma_store_2d(&tmap_out, smem + L::kW + part * (128 * 128), (static_cast<int>(row0) + part * 16) * kC8Row + c0, b0);
+        tma_store_commit();
+        tma_store_wait_all();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 128); }
+}
+
+// Many requests: joining the pieces and the value dimension as two kernels (decode_project_kernel, one, keeps a head's weights and goes through its
+// requests sixteen at a time, a chain of loads, sums, stores and MMAs each: 250 requests of 64 heads 30 us, 200 of 32 heads 18).
+//     o[c] = sum_p 2^(m_p - M) o_p[c] / sum_p 2^(m_p - M) l_p      a warp for each request and head, many of them: bf16(o) and bf16(o - bf16(o))
+//     out[v] = sum_c W_uv[c, v] (both parts)[c]                    a plain product for each head, 128 requests a CTA
+// Both have the latents in the pieces' order.  A CTA of the first has eight heads and a run of requests.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads)
+decode8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const int* __restrict__ seq_lens, int columns, int page_shift, int B,
+                    int h, int h_pad, int ctas_per_group, int run, __nv_bfloat16* __restrict__ joined, float* __restrict__ lse) {
+    __shared__ int sums[16];
+    grid_launch_dependents();
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int head = blockIdx.y * (kJoinThreads / 32) + warp, b0 = blockIdx.x * run, b1 = min(B, b0 + run);
+    // Where the requests' units lie on the line, from the lengths (an input of the call: nothing to wait for).
+    auto units_of = [&](int b) { return (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kD8Unit - 1) / kD8Unit; };
+    int sum = 0, before = 0;
+    for (int b = threadIdx.x; b < B; b += kJoinThreads) {
+        const int n = units_of(b);
+        sum += n;
+        before += b < b0 ? n : 0;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        before += __shfl_xor_sync(0xffffffffu, before, d);
+    }
+    if (lane == 0) { sums[warp] = sum; sums[8 + warp] = before; }
+    __syncthreads();
+    sum = sums[lane & 7];
+    before = sums[8 + (lane & 7)];
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        before += __shfl_xor_sync(0xffffffffu, before, d);
+    }
+    const int per = max(1, (sum + ctas_per_group - 1) / ctas_per_group);
+    grid_dependency_wait();
+    if (head >= h) return;
+    int begin = before;
+    for (int b = b0; b < b1; ++b) {
+        const int n = units_of(b), first = begin / per, count = n > 0 ? (begin + n - 1) / per - first + 1 : 0;
+        begin += n;
+        const size_t row = static_cast<size_t>(first + b) * h_pad + head, step = h_pad;      // the request's first piece; the next one's distance
+        const float2* ml = part_ml + row;
+        float M = -INFINITY, l = 0.f;
+        for (int c = lane; c < count; c += 32) M = fmaxf(M, ml[c * step].x);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        for (int c = lane; c < count; c += 32) {
+            const float2 x = ml[c * step];
+            l = fmaf(fast_exp2(x.x - M), x.y, l);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+        const float inv = l == 0.f ? 0.f : 1.0f / l;             // (nothing left: every score was -inf; a NaN stays one)
+        float4 acc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c0 = 0; c0 < count; c0 += 32) {
+            const float mine = c0 + lane < count ? fast_exp2(ml[(c0 + lane) * step].x - M) * inv : 0.f;
+            const int most = min(32, count - c0);
+            const float4* o = reinterpret_cast<const float4*>(part_o + (row + c0 * step) * kDecLat) + lane;
+#pragma unroll 2
+            for (int c = 0; c < most; ++c, o += step * (kDecLat / 4)) {
+                const float w = __shfl_sync(0xffffffffu, mine, c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 x = __ldcs(o + 32 * j);
+                    acc[j] = make_float4(fmaf(x.x, w, acc[j].x), fmaf(x.y, w, acc[j].y), fmaf(x.z, w, acc[j].z), fmaf(x.w, w, acc[j].w));
+                }
+            }
+        }
+        __nv_bfloat16* dst = joined + (static_cast<size_t>(b) * h + head) * (2 * kDecLat) + lane * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t h0 = pack_bf16x2(acc[j].x, acc[j].y), h1 = pack_bf16x2(acc[j].z, acc[j].w);
+            auto rest = [](float a, float b, uint32_t both) { return pack_bf16x2(a - __uint_as_float(both << 16), b - __uint_as_float(both & 0xffff0000u)); };
+            *reinterpret_cast<uint2*>(dst + 128 * j) = make_uint2(h0, h1);
+            *reinterpret_cast<uint2*>(dst + kDecLat + 128 * j) = make_uint2(rest(acc[j].x, acc[j].y, h0), rest(acc[j].z, acc[j].w, h1));
+        }
+        if (lse != nullptr && lane == 0)
+            lse[static_cast<size_t>(b) * h + head] = count > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+// D[128 requests x 128 values] = (hi, lo) (A, K-major) . W_uv (B, MN-major, rows in the pieces' order), a ring of four stages of 64 latents: both parts' slabs
+// and the weights', which serve both.  warp 0 TMA, warp 1 MMAs, warps 4..7 the result.
+constexpr int kValuesThreads = 256, kValuesStages = 4;
+struct Decode8ValuesSmem {
+    static constexpr int kSlab = 128 * 128;                      // 128 requests x 64 latents; or 2 x (64 latents x 64 values)
+    static constexpr int kStage = 3 * kSlab;
+    static constexpr int kBar = kValuesStages * kStage;
+    static constexpr int kTotalBytes = kBar + (2 * kValuesStages + 1) * 8 + 24;
+};
+static_assert(Decode8ValuesSmem::kTotalBytes <= 232448, "shared memory of the values' product");
+__global__ void __launch_bounds__(kValuesThreads, 1)
+decode8_values_kernel(const __grid_constant__ CUtensorMap tmap_o, const __grid_constant__ CUtensorMap tmap_wv, const __grid_constant__ CUtensorMap tmap_out,
+                      unsigned* status) {
+    using L = Decode8ValuesSmem;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
+    uint64_t* empty = full + kValuesStages;
+    uint64_t* done = empty + kValuesStages;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const int head = blockIdx.x, b0 = blockIdx.y * 128;
+    constexpr int kSteps = kDecLat / 64;
+    auto load_weights = [&](int k) {
+        uint8_t* dst = smem + (k % kValuesStages) * L::kStage + 2 * L::kSlab;
+        for (int i = 0; i < 2; ++i)
+            tma_load_turned_chk(status, dst + i * (L::kSlab / 2), &tmap_wv, &full[k % kValuesStages], head * 256 + i * 64, k * 16);
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kValuesStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        mbar_init(done, 1);
+        abort_flag->value = 0;
+        mbar_fence_init();
+        for (int k = 0; k < kValuesStages; ++k) {                // (weights are an input: nothing to wait for)
+            mbar_arrive_expect_tx(&full[k], L::kStage);
+            load_weights(k);
+        }
+    }
+    if (warp == 1) { tmem_alloc(tmem_slot, 128); tmem_relinquish(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    grid_launch_dependents();
+    const uint32_t tmem = *tmem_slot;
+    if (warp == 0) {
+        if (elect_one()) {
+            grid_dependency_wait();
+            bool ok = true;
+            for (int k = 0; k < kSteps; ++k) {
+                const int s = k % kValuesStages;
+                if (k >= kValuesStages) {
+                    ok = mbar_wait(&empty[s], ((k / kValuesStages) & 1) ^ 1, abort_flag, status, 0x94);
+                    if (!ok) break;
+                    mbar_arrive_expect_tx(&full[s], L::kStage);
+                    load_weights(k);
+                }
+                for (int part = 0; part < 2; ++part)
+                    tma_load_2d_chk(status, smem + s * L::kStage + part * L::kSlab, &tmap_o, &full[s], head * (2 * kDecLat) + part * kDecLat + k * 64, b0);
+            }
+            if (!ok)                                             // (stages in flight: each armed in its first turn, or in its second)
+                for (int s = 0; s < kValuesStages; ++s) { mbar_wait_quiesce(&full[s], 0); mbar_wait_quiesce(&full[s], 1); }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (elect_one()) {
+            constexpr uint32_t idesc = make_idesc_bf16(128, 128, 0, 1);
+            bool ok = true;
+            for (int k = 0; k < kSteps; ++k) {
+                const int s = k % kValuesStages;
+                ok = mbar_wait(&full[s], (k / kValuesStages) & 1, abort_flag, status, 0x95);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t base = smem_u32(smem + s * L::kStage);
+                const uint64_t db = desc_mn_major(base + 2 * L::kSlab, L::kSlab / 2);
+                for (int part = 0; part < 2; ++part) {
+                    const uint64_t da = desc_k_major(base + part * L::kSlab);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) mma_ss(tmem, da + kk * 2, db + kk * 128, idesc, (k > 0 || part > 0 || kk > 0) ? 1u : 0u);
+                }
+                mma_commit(&empty[s]);
+            }
+            mma_commit(done);
+            if (!ok) mbar_wait_quiesce(done, 0);
+        }
+        __syncwarp();
+    }
+    bool ok = true;
+    if (warp >= 4) {
+        ok = mbar_wait_warp(done, 0, abort_flag, status, 0x96) && abort_flag->value == 0u;
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after_sync();
+        // two boxes of 128 requests x 64 values, over a stage that has been multiplied
+        const int r = (warp & 3) * 32 + lane;
+        uint8_t* line = smem + r * 128;
+#pragma unroll 1
+        for (int c = 0; c < 128; c += 16) {
+            uint32_t v[16], w[8];
+            tmem_ld_x16(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+            uint8_t* box = line + (c >> 6) * L::kSlab;
+            const int chunk = (c & 63) >> 3;
+            *reinterpret_cast<uint4*>(box + ((chunk ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(box + (((chunk + 1) ^ (r & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+        fence_async_shared();
+    }
+    grid_dependency_wait();
+    if (__syncthreads_and(ok) && threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) tma_store_2d(&tmap_out, smem + i * L::kSlab, head * 128 + i * 64, b0);
         tma_store_commit();
         tma_store_wait_all();
     }

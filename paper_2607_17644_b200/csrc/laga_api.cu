@@ -96,7 +96,7 @@ bool make_tmap_cache(CUtensorMap* map, const void* base, uint64_t rows, uint32_t
 //   kMapPages    the cache: 640 codes x rows of a page x pages (`rows` pages, `stride` bytes apart, of `inner` rows each), 128-byte swizzle
 //   kMapQueries  2-d, 128-byte swizzle: the queries' rows, as the attention reads them and decode_absorb8_rows_kernel writes them
 //   kMapStore    2-d, no swizzle: as decode_absorb8_kernel writes them
-// and one over bf16 weights, kMapTurned: W's rows r as (r % 128, r / 128), boxes of 64 channels x 4 x 64, 128-byte swizzle (`rows`: 512)
+// and one over bf16 weights, kMapTurned: W's rows r as (r % 128, r / 128), boxes of 64 channels x 4 x box_rows, 128-byte swizzle (`rows`: 512)
 enum : uint32_t { kMapPages = 16, kMapQueries = 17, kMapStore = 18, kMapTurned = 19 };
 bool make_tmap_codes(CUtensorMap* map, uint32_t kind, const void* base, uint64_t inner, uint64_t rows, uint64_t stride, uint32_t box_rows) {
     EncodeTiledFn fn = encode_tiled_fn();
@@ -104,7 +104,7 @@ bool make_tmap_codes(CUtensorMap* map, uint32_t kind, const void* base, uint64_t
     if (kind == kMapTurned) {
         cuuint64_t dims[3] = {inner, 4u, rows / 4};
         cuuint64_t strides[2] = {stride * (rows / 4), stride};
-        cuuint32_t box[3] = {64u, 4u, 64u}, estr[3] = {1u, 1u, 1u};
+        cuuint32_t box[3] = {64u, 4u, box_rows}, estr[3] = {1u, 1u, 1u};
         return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
@@ -185,8 +185,10 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_decode8_sm100_kernel<16>, AttnDecode8Smem<16>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<32>, AttnDecode8Smem<32>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<64>, AttnDecode8Smem<64>::kTotalBytes) &&
+              allow_smem(decode8_values_kernel, Decode8ValuesSmem::kTotalBytes) &&
               allow_smem(decode_absorb8_kernel, DecodeAbsorb8Smem::kTotalBytes) &&
-              allow_smem(decode_absorb8_rows_kernel, DecodeAbsorb8RowsSmem::kTotalBytes) &&
+              allow_smem(decode_absorb8_rows_kernel<1>, DecodeAbsorb8RowsSmem<1>::kTotalBytes) &&
+              allow_smem(decode_absorb8_rows_kernel<2>, DecodeAbsorb8RowsSmem<2>::kTotalBytes) &&
               allow_smem(decode_project_kernel<false>, DecodeProjectSmem::kTotalBytes) &&
               allow_smem(decode_project_kernel<true>, DecodeProjectSmem::kTotalBytes) &&
               allow_smem(latent_norm_rope_fwd_kernel<2, false>, latent_fwd_smem(256, kRopeMaxRot)) &&
@@ -827,6 +829,8 @@ int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, flo
 struct Decode8Layout {
     DecodeLayout d;
     size_t q_rows, q_scale;                           // in the place of d's q_abs
+    bool many;                                        // joined and projected by two kernels
+    size_t joined;                                    // what the first leaves to the second: [B][h][2][512] bf16
 };
 Decode8Layout decode8_layout(int B, int h) {
     Decode8Layout w;
@@ -836,7 +840,12 @@ Decode8Layout decode8_layout(int B, int h) {
     w.q_scale = w.q_rows + align_up(heads * 2 * kC8Row, 1024);
     w.d.part_o = w.q_scale + align_up(heads * sizeof(float), 1024);
     w.d.part_ml = w.d.part_o + parts * kDecLat * sizeof(float);
-    w.d.total = w.d.part_ml + align_up(parts * sizeof(float2), 1024);
+    w.joined = w.d.part_ml + align_up(parts * sizeof(float2), 1024);
+    // (decode_project_kernel, tiles of 16 requests, as many CTAs a head as fit: 250 requests of 64 heads are 8 turns, 93.3 us the call, against 88.9 with
+    // the two kernels; 200 of 32 heads 4 turns, 88.5 against 89.0)
+    const int ctas_a_head = kDecMaxCtas / h > 0 ? kDecMaxCtas / h : 1;
+    w.many = (B + 15) / 16 > 4 * ctas_a_head;
+    w.d.total = w.joined + (w.many ? static_cast<size_t>(B) * h * (2 * kDecLat) * 2 : 0);
     return w;
 }
 
@@ -850,8 +859,10 @@ int launch_decode_absorb8(const void* q, const void* w, int B, int h, int h_pad,
         !cached_tmap_codes(&to, few ? kMapStore : kMapQueries, rows, request, B, request, tile))
         return LAGA_ERR_CUDA;
     const dim3 grid = few ? dim3(h, (B + tile - 1) / tile) : dim3(4, h, (B + tile - 1) / tile);
-    launch_kernel(few ? decode_absorb8_kernel : decode_absorb8_rows_kernel, grid, dim3(few ? kAbsorb8Threads : kAbsorbRowsThreads),
-                  few ? DecodeAbsorb8Smem::kTotalBytes : DecodeAbsorb8RowsSmem::kTotalBytes, stream, false, tw, tq, to,
+    const bool two = grid.y * grid.z * 4 <= static_cast<unsigned>(3 * sm_count());
+    launch_kernel(few ? decode_absorb8_kernel : two ? decode_absorb8_rows_kernel<2> : decode_absorb8_rows_kernel<1>, grid,
+                  dim3(few ? kAbsorb8Threads : kAbsorbRowsThreads),
+                  few ? DecodeAbsorb8Smem::kTotalBytes : two ? DecodeAbsorb8RowsSmem<2>::kTotalBytes : DecodeAbsorb8RowsSmem<1>::kTotalBytes, stream, false, tw, tq, to,
                   static_cast<const __nv_bfloat16*>(q), B, h, h_pad, rows, q_scale, status, words);
     return launch_status();
 }
@@ -866,6 +877,23 @@ int launch_attn_decode8(const uint8_t* q_rows, const AttnDecode8Args& a, cudaStr
     ScopedKernelEvents ev(LAGA_KERNEL_ATTN_DECODE, stream);
     launch_kernel(attn_decode8_sm100_kernel<kHeads>, dim3(static_cast<unsigned>(a.d.n_groups * a.d.ctas_per_group)), dim3(AttnDecode8Smem<kHeads>::kThreads),
                   AttnDecode8Smem<kHeads>::kTotalBytes, stream, true, tq, tc, a);
+    return launch_status();
+}
+
+int launch_decode8_join(const void* w, const AttnDecodeArgs& a, void* joined, void* out, float* lse, cudaStream_t stream) {
+    const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv), o_row = static_cast<uint64_t>(a.h) * 2 * kDecLat, out_row = static_cast<uint64_t>(a.h) * kDv;
+    const void* wv = static_cast<const uint8_t*>(w) + kDn * 2;
+    CUtensorMap to, tw, tv;
+    if (!cached_tmap_bf16(&to, joined, o_row, a.B, o_row * 2, 128) || !cached_tmap_codes(&tw, kMapTurned, wv, w_row - kDn, kDc, w_row * 2, 16) ||
+        !cached_tmap_bf16(&tv, out, out_row, a.B, out_row * 2, 128))
+        return LAGA_ERR_CUDA;
+    // eight CTAs an SM; each goes through all lengths once, so not more of them than that
+    const int groups = (a.h + kJoinThreads / 32 - 1) / (kJoinThreads / 32), most = std::max(1, 8 * sm_count() / groups), run = (a.B + most - 1) / most;
+    launch_kernel(decode8_join_kernel, dim3((a.B + run - 1) / run, groups), dim3(kJoinThreads), 0, stream, true, static_cast<const float*>(a.part_o),
+                  static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift, a.B, a.h, a.h_pad, a.ctas_per_group, run,
+                  static_cast<__nv_bfloat16*>(joined), lse);
+    if (const int rc = launch_status(); rc != LAGA_OK) return rc;
+    launch_kernel(decode8_values_kernel, dim3(a.h, (a.B + 127) / 128), dim3(kValuesThreads), Decode8ValuesSmem::kTotalBytes, stream, true, to, tw, tv, a.status);
     return launch_status();
 }
 
@@ -1667,7 +1695,7 @@ int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int
     else if (w.d.heads == 32) rc = launch_attn_decode8<32>(base + w.q_rows, a, st);
     else rc = launch_attn_decode8<64>(base + w.q_rows, a, st);
     if (rc != LAGA_OK) return rc;
-    return launch_decode_project(w_kv_b, a.d, out, lse, st, true);
+    return w.many ? launch_decode8_join(w_kv_b, a.d, base + w.joined, out, lse, st) : launch_decode_project(w_kv_b, a.d, out, lse, st, true);
 }
 
 }  // extern "C"

@@ -61,7 +61,7 @@ def append_and_read(M, page):
 
 if __name__ == "__main__":
     for args in (([1], 1, 16), ([65, 0, 7, 1000], 16, 16), ([130, 511], 40, 64), ([700, 129], 20, 32), ([3000, 1, 64], 130, 32), ([17] * 21, 8, 128),
-                 ([100] * 40, 30, 1024)):
+                 ([100] * 40, 30, 1024), ([3, 90, 0] * 45 + [1200], 70, 16), ([20] * 129, 64, 64)):
         decode(*args)
     for args in ((1, 16), (77, 64), (1025, 1024), (4099, 32)):
         append_and_read(*args)

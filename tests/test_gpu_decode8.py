@@ -82,6 +82,29 @@ def test_several_request_tiles_per_head(laga, B, h):  # noqa: F811
     check(tensors, *run(laga, tensors))
 
 
+@pytest.mark.parametrize("B,h", [(65, 128), (129, 64), (193, 40), (257, 33), (600, 16), (66, 150), (1300, 7)])
+def test_requests_joined_and_projected_apart(laga, B, h):  # noqa: F811
+    g = torch.Generator().manual_seed(B + h)
+    lens = torch.randint(0, 70, (B,), generator=g).tolist()
+    lens[B // 2], lens[-1] = 9000 if h < 64 else 2500, 0     # many pieces; and none
+    tensors = case(lens, h, 32, seed=14)
+    check(tensors, *run(laga, tensors))
+
+
+def test_the_same_requests_with_few_others_and_with_many(laga):  # noqa: F811
+    """Values that are not finite stay with their request, whichever kernels join the pieces."""
+    h = 64
+    q, w, pages, table, lens = case([90, 0, 700, 33] + [5] * 130, h, 16, seed=15)
+    codes, scales = c8.planes(pages)
+    codes[int(table[2, 0]), 3, 7] = 0x7f
+    q[3, 1, 5] = float("nan")
+    many, many_lse = run(laga, (q, w, pages, table, lens))
+    few, few_lse = run(laga, (q[:40], w, pages, table[:40], lens[:40]))
+    assert bool(torch.isnan(many[2].float()).all()) and bool(torch.isnan(many_lse[2]).all()) and bool((many[1] == 0).all())
+    assert bool(torch.isnan(many[3, 1].float()).all()) and not bool(torch.isnan(many[3, 2:].float()).any() | torch.isnan(many[4:].float()).any())
+    assert torch.equal(torch.isnan(many[:40].float()), torch.isnan(few.float())) and torch.equal(torch.isnan(many_lse[:40]), torch.isnan(few_lse))
+
+
 @pytest.mark.parametrize("lens,h,page", [([511], 16, 32), ([9001], 16, 64), ([20011, 3], 4, 16), ([12345, 1, 0, 6000], 32, 64), ([12345, 1, 0, 6000], 64, 64),
                                          ([15000, 777], 128, 256)])
 def test_long_contexts(laga, lens, h, page):  # noqa: F811
