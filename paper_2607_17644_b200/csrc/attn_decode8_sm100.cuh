@@ -72,6 +72,10 @@ struct AttnDecode8Smem {
     static constexpr int kPRow = kSplit ? 2 * kHeads : kHeads; // bytes of a key's row of P
     static constexpr int kPTile = kD8Keys * kPRow;
     static constexpr int kSlabs = kHeads == 16 ? 12 : kHeads == 32 ? 10 : 8;
+    // With 64 heads' queries there are slabs for two tiles but not for their keys' too: the key's slab comes first, into the place of the latent's
+    // first, and is scored while that is still on its way.  (A ring of five slabs a tile let a tile's last slab in only after the values of the
+    // tile before: 8 x 65536, 128 heads 153 -> TODO us.)
+    static constexpr bool kKeyFirst = kHeads == 64;
     static constexpr int kScales = kHeads == 64 ? 2 : 4;       // tiles whose scales are held
     static constexpr int kQSlab = 2 * kHeads * 128;            // 32 rows for every 16 heads, hi then lo, x 128 channels
     static constexpr int kSlab = kD8Keys * 128;
@@ -273,6 +277,16 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         fetch_pages(cur, pages);
         uint32_t slot = kBegin, par = 0, pieces = 0, T = 0;
         bool new_piece = true, ok = true;
+        // a piece's queries behind its first loads: they wait for the last scores of the piece before (the first are the score warp's)
+        auto piece_queries = [&](int b) -> bool {
+            if (!new_piece) return true;
+            if (pieces > 0) {
+                if (!mbar_wait(q_empty, (pieces & 1u) ^ 1u, abort_flag, args.status, 0x81)) return false;
+                fetch_queries(b);
+            }
+            ++pieces;
+            return true;
+        };
         while (!cur.done()) {
             Decode8Cursor next = cur;
             next.next(args);
@@ -290,24 +304,36 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     pages[i] = n_pages;                      // out of the map's range: TMA fills zeros
                     --there;
                     atomicCAS(args.status, kStatusOk, kStatusCheck | 0xF2u);
-                    if (kFirst) {
-                        for (int k = 0; k < kBox; ++k) scales[i * kBox + k] = 1.0f;
-                        fence_async_shared();
-                    }
                 }
             }
 #pragma unroll
-            for (uint32_t s = 0; s < kCount; ++s) {          // the key's slab, then the latent's four
+            for (uint32_t s = 0; s < kCount; ++s) {          // the key's slab, then the latent's four (kKeyFirst: the first of them last)
+                int channel = kBegin + s == 0 ? kC8Lat : static_cast<int>(kBegin + s - 1) * 128;
+                if constexpr (L::kKeyFirst) {
+                    // The tile's four places; the latent's quarter too but for the key's slab.  The first is filled twice a tile, both times by this
+                    // lane, which sees every phase of its barrier one after another (one that did not could take a phase for the one before the last).
+                    const uint32_t which = kFirst ? s & 1u : s + 2u;
+                    slot = (T & 1u) * 4 + which;
+                    par = which > 0 ? (T >> 1) & 1u : s >> 1;
+                    channel = kFirst && s == 0 ? kC8Lat : static_cast<int>(which) * 128;
+                    if (kFirst && s == 2) {                  // (waits for the key's scores, which need the queries)
+                        ok = piece_queries(cur.b);
+                        if (!ok) break;
+                    }
+                }
                 const uint32_t bar = full_a + slot * 8;
                 if (!mbar_test_wait_u32(empty_a + slot * 8, par ^ 1u)) ok = mbar_wait(&empty[slot], par ^ 1u, abort_flag, args.status, 0x80);
                 if (!ok) break;
                 mbar_arrive_expect_tx_u32(bar, boxes * (kBox * 128));
                 const uint32_t dst = slab_a + slot * L::kSlab;
-                const int channel = kBegin + s == 0 ? kC8Lat : static_cast<int>(kBegin + s - 1) * 128;
 #pragma unroll
                 for (int i = 0; i < kSubs; ++i)
                     if (i < boxes) tma_load_codes_chk(args.status, dst + i * (kBox * 128), &tmap_codes, bar, channel, (row0 + i * kBox) & in_page, pages[i], once);
-                if (kFirst && s == 0) {
+                if (kFirst && s == 0) {                      // (the scales that were in this buffer have been read: their tile's values are multiplied)
+                    if (there != static_cast<uint32_t>(boxes)) {
+                        for (int k = 0; k < boxes * kBox; ++k) scales[k] = 1.0f;
+                        fence_async_shared();
+                    }
                     uint64_t* c_bar = &c_full[T % L::kScales];
                     mbar_arrive_expect_tx(c_bar, there * (kBox * 4));
 #pragma unroll
@@ -316,16 +342,15 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                             bulk_load(scales + i * kBox, all.cache.base + pages[i] * all.cache.page_bytes() + (static_cast<size_t>(kC8Row) << shift) +
                                       ((row0 + i * kBox) & in_page) * 4, kBox * 4, c_bar);
                 }
-                slot += s + 1 < kCount ? 1u : 6u - kCount;
-                if (slot >= L::kSlabs) { slot -= L::kSlabs; par ^= 1u; }
+                if constexpr (!L::kKeyFirst) {
+                    slot += s + 1 < kCount ? 1u : 6u - kCount;
+                    if (slot >= L::kSlabs) { slot -= L::kSlabs; par ^= 1u; }
+                }
             }
             if (!ok) break;
-            // a piece's queries after its first tile: they wait for the last scores of the piece before (the first are the score warp's)
-            if (kFirst && new_piece) {
-                if (pieces > 0) ok = mbar_wait(q_empty, (pieces & 1u) ^ 1u, abort_flag, args.status, 0x81);
+            if constexpr (kFirst && !L::kKeyFirst) {
+                ok = piece_queries(cur.b);
                 if (!ok) break;
-                if (pieces > 0) fetch_queries(cur.b);
-                ++pieces;
             }
             new_piece = cur.ends_piece();
             cur = next;
@@ -336,7 +361,14 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         // What a lane has armed is complete when every barrier has left the phase that it was armed for last: slots behind `slot` are a round
         // behind.  (A barrier that was never armed, or is the other lane's, costs the limit at most.)
         if (abort_flag->value != 0u) {
-            for (uint32_t i = 0; i < L::kSlabs; ++i) mbar_wait_quiesce(&full[i], i < slot ? par : par ^ 1u);
+            for (uint32_t i = 0; i < L::kSlabs; ++i) {
+                if constexpr (L::kKeyFirst) {                // (armed for either)
+                    mbar_wait_quiesce(&full[i], 0);
+                    mbar_wait_quiesce(&full[i], 1);
+                } else {
+                    mbar_wait_quiesce(&full[i], i < slot ? par : par ^ 1u);
+                }
+            }
             if (kFirst) {
                 for (uint32_t k = 1; k <= L::kScales && k <= T; ++k) mbar_wait_quiesce(&c_full[(T - k) % L::kScales], ((T - k) / L::kScales) & 1u);
                 if (pieces > 0) mbar_wait_quiesce(q_full, (pieces - 1) & 1u);
@@ -373,16 +405,25 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 new_piece = cur.ends_piece();
                 cur.next(args);
                 // A barrier probe queues behind the lane's MMAs until the tensor pipe has taken them, so the next slab's is made before this one's.
+                // kKeyFirst: the key's slab, the latent's second to fourth, its first.
+                if constexpr (L::kKeyFirst) { slot = buf * 4; par = 0; }
                 bool here = mbar_test_wait(&full[slot], par);
 #pragma unroll 1
                 for (int s = 0; s < 5; ++s) {
                     if (!here) ok = mbar_wait(&full[slot], par, abort_flag, args.status, 0x84);
                     if (!ok) break;
                     const uint32_t at = slot;
-                    if (++slot == L::kSlabs) { slot = 0; par ^= 1u; }
+                    if constexpr (L::kKeyFirst) {
+                        slot = buf * 4 + ((s + 1) & 3);
+                        par = s == 3 ? 1u : (T >> 1) & 1u;
+                    } else if (++slot == L::kSlabs) {
+                        slot = 0;
+                        par ^= 1u;
+                    }
                     if (s < 4) here = mbar_test_wait(&full[slot], par);
                     tc_fence_after_sync();
-                    mma8_ss_chain4<2, 2>(d, k_lo + at * (L::kSlab / 16), hi, q_lo + (s == 0 ? 4 : s - 1) * (L::kQSlab / 16), hi, idesc, s > 0 ? 1u : 0u);
+                    const int quarter = s == 0 ? 4 : L::kKeyFirst ? s & 3 : s - 1;       // of the queries' channels
+                    mma8_ss_chain4<2, 2>(d, k_lo + at * (L::kSlab / 16), hi, q_lo + quarter * (L::kQSlab / 16), hi, idesc, s > 0 ? 1u : 0u);
                     if (s == 0) mma_commit(&empty[at]);
                 }
                 if (!ok) break;
@@ -410,7 +451,8 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint32_t b_lo = p_lo + (L::kSplit ? buf * (L::kPTile / 16) : 0u);
-                if (++slot == L::kSlabs) slot = 0;           // the key's slab
+                if constexpr (L::kKeyFirst) slot = buf * 4;
+                else if (++slot == L::kSlabs) slot = 0;      // the key's slab
 #pragma unroll 1
                 for (uint32_t s = 0; s < 4; ++s) {
                     const uint32_t a_lo = v_lo + slot * (L::kSlab / 16), d = tmem_base + s * L::kCols;
@@ -660,7 +702,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 const int n_zero = 32 - (valid & 31);
                 for (int i = tid; i < 4 * 8 * n_zero; i += 128) {                    // 4 slabs x rows x eight 16-byte chunks
                     const int slab = i / (8 * n_zero), r = valid + (i >> 3) % n_zero;
-                    uint32_t slot = pos + 1 + slab;
+                    uint32_t slot = pos + (L::kKeyFirst ? 0 : 1) + slab;
                     if (slot >= L::kSlabs) slot -= L::kSlabs;
                     *reinterpret_cast<uint4*>(smem + L::kSlab0 + slot * L::kSlab + r * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
@@ -730,7 +772,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 first = true;
             }
             ++T;
-            pos += 5;
+            pos += L::kKeyFirst ? 4 : 5;
             if (pos >= L::kSlabs) pos -= L::kSlabs;
         }
     }
