@@ -67,6 +67,9 @@ struct AttnDecode8Smem {
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 32 * (kSoftWarps + 4);
     static constexpr bool kSplit = kHeads <= 32;               // both parts of P as columns
+    // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (200 requests of 32 heads 88.2 -> 83.2 us;
+    // 64 x 8192 with 16 heads 45.6 -> 46.3, 8 x 65536 with 128 132.3 -> 136.1)
+    static constexpr bool kOneCopy = kHeads == 32;
     static constexpr float kDrop = kSplit ? 3.0f : 0.0f;       // P = 2^(d - kDrop): at most 2^8 in e4m3 (hi and 32 times the rest), 2^11 in e5m2 and its rest
     static constexpr int kCols = kSplit ? 2 * kHeads : kHeads; // TMEM columns of 128 latents of O^T
     static constexpr int kPRow = kSplit ? 2 * kHeads : kHeads; // bytes of a key's row of P
@@ -581,7 +584,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 if (lane == 0) vote_s[buf * (4 * L::kGroups) + quarter] = static_cast<int>(below);
                 arrive();
             }
-            // Probabilities and their parts, while the group's other warps vote
+            // Probabilities and their parts, while the group's other warps vote.
             F2 p[kPairs];
             uint32_t hi[kPer / 4], lo[kPer / 4];
             auto weigh = [&]() {
@@ -600,18 +603,27 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     else parts_e5m2_e4m3(p16[0], p16[1], hi[i], lo[i]);
                 }
             };
-            if (!first) weigh();
-            // (asked now: P's buffer, whose last use must have been multiplied)
+            // Where the references do not hold, once more with those that do (a piece's first tile has none, and does not weigh before).  kOneCopy: in a
+            // second turn of the loop.
             const uint32_t prev = T - (L::kSplit ? 2 : 1);
-            const bool has_prev = T >= (L::kSplit ? 2 : 1), p_free = !has_prev || mbar_test_wait(&pv_done[prev & 1u], (prev >> 1) & 1u);
-            bool holds = false;
-            if (!first) {
-                if (!wait_for_group()) break;
-                const int4 votes = *reinterpret_cast<const int4*>(vote_s + buf * (4 * L::kGroups));
-                const uint32_t below = static_cast<uint32_t>(votes.x & votes.y & votes.z & votes.w);
-                holds = (below & (0x80000000u | live)) == 0x80000000u;
-            }
-            if (!holds) {
+            bool p_free = true, settled = false;
+#pragma unroll 1
+            for (;;) {
+                if (settled || !first) weigh();
+                if (settled) break;
+                settled = true;
+                // (asked now: P's buffer, whose last use must have been multiplied)
+                p_free = T < (L::kSplit ? 2 : 1) || mbar_test_wait(&pv_done[prev & 1u], (prev >> 1) & 1u);
+                if (!first) {
+                    ok = wait_for_group();
+                    if (!ok) break;
+                    const int4 votes = *reinterpret_cast<const int4*>(vote_s + buf * (4 * L::kGroups));
+                    const uint32_t below = static_cast<uint32_t>(votes.x & votes.y & votes.z & votes.w);
+                    if ((below & (0x80000000u | live)) == 0x80000000u) {
+                        seen = true;
+                        break;
+                    }
+                }
                 // The heads' maxima over the tile, then the references they ask for.
                 float tops[kPer];
 #pragma unroll
@@ -623,7 +635,8 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 const float most = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
                 if ((lane & (kShare - 1)) == 0) atomicMax(&top_s[h0 + lane / kShare], ordered(most));
                 arrive();
-                if (!wait_for_group()) break;
+                ok = wait_for_group();
+                if (!ok) break;
                 if (tid < kPer) {
                     const float top = unordered(top_s[h0 + tid]), m = ref_s[h0 + tid];
                     top_s[h0 + tid] = kOrderedLowest;
@@ -636,7 +649,8 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     seen = seen || top > -INFINITY;
                 }
                 arrive();
-                if (!wait_for_group()) break;
+                ok = wait_for_group();
+                if (!ok) break;
                 const ulonglong2 *step = reinterpret_cast<const ulonglong2*>(step_s + h0), *alpha = reinterpret_cast<const ulonglong2*>(alpha_s + h0);
                 const F2 minus1 = f2(-1.0f, -1.0f);
 #pragma unroll
@@ -649,7 +663,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                         l2[i + 1] = f2_mul(l2[i + 1], F2{a4.y});
                     }
                 }
-                weigh();
+                if constexpr (!L::kOneCopy) weigh();
                 if (!first) {
                     // O^T is at rest once the values of the tile before have been multiplied; this tile's wait for p_full below
                     ok = mbar_wait_warp(&pv_done[(T - 1) & 1u], ((T - 1) >> 1) & 1u, abort_flag, args.status, 0x8A);
@@ -674,9 +688,9 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     }
                     tmem_st_wait();
                 }
-            } else {
-                seen = true;
+                if constexpr (!L::kOneCopy) break;
             }
+            if (!ok) break;
             {
                 const float inv = __uint_as_float((254u - min(254u, __float_as_uint(s) >> 23 & 0xffu)) << 23);      // 1 / s
                 const F2 inv2 = f2(inv, inv);
