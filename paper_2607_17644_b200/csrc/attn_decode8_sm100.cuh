@@ -101,9 +101,13 @@ struct AttnDecode8Args {
     const float* q_scale;              // [B][h_pad]
 };
 
+// Where the line's units lie.  A request with tokens begins with a gap as long as what its switch costs -- queries, a tile without references, the accumulator
+// to drain -- and is then its units: stretches of the line are equal work, not equal units, and one that would begin within a gap begins with the request.
+constexpr int decode8_gap(int heads) { return heads == 64 ? 5 : heads == 32 ? 4 : 3; }
+
 // Walks the tiles of one CTA's stretch of the line.
 struct Decode8Cursor {
-    int left, b, t, n, len;            // units left; request; unit within it; its units; its length
+    int left, b, t, n, len, gap;       // of the stretch left; request; unit within it; its units; its length
     __device__ __forceinline__ void open(const AttnDecodeArgs& a) {
         for (; b < a.B; ++b) {
             len = decode_len(a, b);
@@ -113,7 +117,7 @@ struct Decode8Cursor {
         }
         left = 0;                      // the lengths changed under the kernel: stop
     }
-    __device__ __forceinline__ Decode8Cursor(const AttnDecodeArgs& a, int left_, int b_, int t_) : left(left_), b(b_), t(t_), n(0), len(0) {
+    __device__ __forceinline__ Decode8Cursor(const AttnDecodeArgs& a, int gap_, int left_, int b_, int t_) : left(left_), b(b_), t(t_), n(0), len(0), gap(gap_) {
         if (left > 0) open(a);
     }
     __device__ __forceinline__ bool done() const { return left <= 0; }
@@ -127,7 +131,7 @@ struct Decode8Cursor {
     __device__ __forceinline__ void advance(const AttnDecodeArgs& a, int u) {
         left -= u;
         t += u;
-        if (t >= n && left > 0) { t = 0; ++b; open(a); }
+        if (t >= n && left > 0) { t = 0; ++b; open(a); left -= gap; }
     }
 };
 
@@ -217,13 +221,18 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         atomicCAS(args.status, kStatusOk, kStatusCheck | 0xD5u);
     }
 
+    constexpr int kGap = decode8_gap(kHeads);
     // ---- the line of units, and where this CTA's stretch begins ---------------------------------------------
     int my_units = 0;
     {
         const int run = (args.B + L::kThreads - 1) / L::kThreads;
         const int b0 = min(args.B, static_cast<int>(threadIdx.x) * run), b1 = min(args.B, b0 + run);
+        auto line_of = [&](int b) {
+            const int n = (decode_len(args, b) + kD8Unit - 1) / kD8Unit;
+            return n > 0 ? n + kGap : 0;
+        };
         int sum = 0;
-        for (int b = b0; b < b1; ++b) sum += (decode_len(args, b) + kD8Unit - 1) / kD8Unit;
+        for (int b = b0; b < b1; ++b) sum += line_of(b);
         int incl = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -242,13 +251,14 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         const int g0 = cta * per;
         my_units = min(per, total - g0);               // may be negative: nothing to do
         for (int b = b0; b < b1; ++b) {
-            const int n = (decode_len(args, b) + kD8Unit - 1) / kD8Unit;
-            if (g0 >= before && g0 < before + n) { *start_b = b; *start_t = g0 - before; }
+            const int n = line_of(b);
+            if (g0 >= before && g0 < before + n) { *start_b = b; *start_t = g0 - before - kGap; }
             before += n;
         }
         __syncthreads();
     }
-    const int first_b = *start_b, first_t = *start_t;
+    const int first_b = *start_b, first_t = max(0, *start_t);
+    my_units += min(0, *start_t);                      // what is left of a gap; nothing to do where the stretch ends in it
 
     auto fetch_queries = [&](int b) {
         grid_dependency_wait();                              // (returns at once after the first time)
@@ -276,7 +286,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
 #pragma unroll
             for (int i = 0; i < kSubs; ++i) p[i] = k0 + i * kBox < c.len ? __ldg(row + ((k0 + i * kBox) >> shift)) : 0;
         };
-        Decode8Cursor cur(args, my_units, first_b, first_t);
+        Decode8Cursor cur(args, kGap, my_units, first_b, first_t);
         fetch_pages(cur, pages);
         uint32_t slot = kBegin, par = 0, pieces = 0, T = 0;
         bool new_piece = true, ok = true;
@@ -399,7 +409,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             uint32_t slot = 0, par = 0, pieces = 0;
             bool ok = true, new_piece = true;
             fetch_queries(first_b);                          // (a unit of first_b is here, so it is the first request with tokens)
-            Decode8Cursor cur(args, my_units, first_b, first_t);
+            Decode8Cursor cur(args, kGap, my_units, first_b, first_t);
             for (uint32_t T = 0; !cur.done(); ++T) {
                 const uint32_t buf = T & 1u, d = tmem_s + buf * (2 * kHeads);
                 if (T >= 2) ok = mbar_wait(&p_full[buf], ((T >> 1) & 1u) ^ 1u, abort_flag, args.status, 0x82);     // the scores of tile T - 2 have been read
@@ -444,7 +454,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                            p_lo = desc_lo(desc_mn_major_narrow<L::kPRow>(smem_u32(smem + L::kP))), p_hi = desc_hi(desc_mn_major_narrow<L::kPRow>(0));
             uint32_t slot = 0, pieces = 0;
             bool ok = true, new_piece = true;
-            Decode8Cursor cur(args, my_units, first_b, first_t);
+            Decode8Cursor cur(args, kGap, my_units, first_b, first_t);
             for (uint32_t T = 0; !cur.done(); ++T) {
                 const uint32_t buf = T & 1u;
                 const int k_steps = (cur.valid() + 31) >> 5;
@@ -502,7 +512,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             if (lane == 0) mbar_arrive(&group_bar[g]);
         };
         auto wait_for_group = [&]() -> bool { return mbar_wait_warp(&group_bar[g], meetings++ & 1u, abort_flag, args.status, 0x87); };
-        Decode8Cursor cur(args, my_units, first_b, first_t);
+        Decode8Cursor cur(args, kGap, my_units, first_b, first_t);
         auto query_scale = [&](const Decode8Cursor& c) -> float {
             return tid < n_live && !c.done() ? __ldg(all.q_scale + static_cast<size_t>(c.b) * args.h_pad + head0 + h0 + tid) * args.scale_log2 : 0.f;
         };
@@ -1127,7 +1137,7 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
 constexpr int kJoinThreads = 256;
 __global__ void __launch_bounds__(kJoinThreads)
 decode8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const int* __restrict__ seq_lens, int columns, int page_shift, int B,
-                    int h, int h_pad, int ctas_per_group, int run, __nv_bfloat16* __restrict__ joined, float* __restrict__ lse) {
+                    int h, int h_pad, int ctas_per_group, int gap, int run, __nv_bfloat16* __restrict__ joined, float* __restrict__ lse) {
     __shared__ int sums[16];
     grid_launch_dependents();
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -1136,7 +1146,7 @@ decode8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__
     auto units_of = [&](int b) { return (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kD8Unit - 1) / kD8Unit; };
     int sum = 0, before = 0;
     for (int b = threadIdx.x; b < B; b += kJoinThreads) {
-        const int n = units_of(b);
+        const int units = units_of(b), n = units > 0 ? units + gap : 0;
         sum += n;
         before += b < b0 ? n : 0;
     }
@@ -1159,7 +1169,9 @@ decode8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__
     if (head >= h) return;
     int begin = before;
     for (int b = b0; b < b1; ++b) {
-        const int n = units_of(b), first = begin / per, count = n > 0 ? (begin + n - 1) / per - first + 1 : 0;
+        const int n = units_of(b);
+        if (n > 0) begin += gap;
+        const int first = begin / per, count = n > 0 ? (begin + n - 1) / per - first + 1 : 0;
         begin += n;
         const size_t row = static_cast<size_t>(first + b) * h_pad + head, step = h_pad;      // the request's first piece; the next one's distance
         const float2* ml = part_ml + row;

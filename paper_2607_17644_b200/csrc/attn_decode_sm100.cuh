@@ -774,9 +774,10 @@ static_assert(DecodeProjectSmem::kTotalBytes <= 232448 && DecodeProjectSmem::kBa
 template <bool kTurned>
 __global__ void __launch_bounds__(kProjectThreads, 1)
 decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
-                      const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad, int ctas_per_group,
+                      const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad, int ctas_per_group, int line_gap,
                       int tile_requests, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, unsigned* status) {
     using L = DecodeProjectSmem;
+    const int gap = kTurned ? line_gap : 0;                      // what lies on the line before each request that has tokens
     extern __shared__ __align__(1024) uint8_t smem[];
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
     uint64_t* done = full + 1;                                   // [2] the MMAs of the tile in buffer i have completed
@@ -820,7 +821,7 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
         const int s0 = min(B, static_cast<int>(threadIdx.x) * run), s1 = min(B, s0 + run);
         int sum = 0, before = 0;                                 // tiles of this thread's requests, and of those of them before b_first
         for (int b = s0; b < s1; ++b) {
-            const int n = tiles_of(b);
+            const int tiles = tiles_of(b), n = tiles > 0 ? tiles + gap : 0;
             sum += n;
             before += b < b_first ? n : 0;
         }
@@ -847,13 +848,14 @@ decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* 
     auto locate = [&](int i) {
         const int b = (tile0 + i) * tile_requests + lane;
         const int mine = lane < tile_requests && b < B && i < my_tiles ? tiles_of(b) : 0;
-        int incl = mine;
+        const int cost = mine > 0 ? mine + gap : 0;
+        int incl = cost;
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, d);
             if (lane >= d) incl += v;
         }
-        const int begin = position + incl - mine, first = begin / per;
+        const int begin = position + incl - mine, first = begin / per;        // (the tiles lie behind their gap)
         const int count = mine > 0 ? (begin + mine - 1) / per - first + 1 : 0;
         position += __shfl_sync(0xffffffffu, incl, 15);
         int base = count;

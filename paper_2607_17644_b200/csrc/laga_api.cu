@@ -808,7 +808,7 @@ int launch_attn_decode(const void* q, const void* q_abs, const void* cache, long
     return launch_status();
 }
 
-int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, float* lse, cudaStream_t stream, bool turned = false) {
+int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, float* lse, cudaStream_t stream, bool turned = false, int gap = 0) {
     const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv);
     const void* wv = static_cast<const uint8_t*>(w) + kDn * 2;
     CUtensorMap tw;      // starts at W's column d_nope: column 0 of the map is V channel 0 of head 0
@@ -821,7 +821,7 @@ int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, flo
     const int n_tiles = (a.B + tile - 1) / tile, most = sms / a.h > 0 ? sms / a.h : 1;
     launch_kernel(turned ? decode_project_kernel<true> : decode_project_kernel<false>, dim3(a.h, n_tiles < most ? n_tiles : most), dim3(kProjectThreads), DecodeProjectSmem::kTotalBytes, stream,
                   true, tw, static_cast<const float*>(a.part_o), static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift,
-                  a.B, a.h, a.h_pad, a.ctas_per_group, tile, static_cast<__nv_bfloat16*>(out), lse, a.status);
+                  a.B, a.h, a.h_pad, a.ctas_per_group, gap, tile, static_cast<__nv_bfloat16*>(out), lse, a.status);
     return launch_status();
 }
 
@@ -880,7 +880,7 @@ int launch_attn_decode8(const uint8_t* q_rows, const AttnDecode8Args& a, cudaStr
     return launch_status();
 }
 
-int launch_decode8_join(const void* w, const AttnDecodeArgs& a, void* joined, void* out, float* lse, cudaStream_t stream) {
+int launch_decode8_join(const void* w, const AttnDecodeArgs& a, int gap, void* joined, void* out, float* lse, cudaStream_t stream) {
     const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv), o_row = static_cast<uint64_t>(a.h) * 2 * kDecLat, out_row = static_cast<uint64_t>(a.h) * kDv;
     const void* wv = static_cast<const uint8_t*>(w) + kDn * 2;
     CUtensorMap to, tw, tv;
@@ -890,7 +890,7 @@ int launch_decode8_join(const void* w, const AttnDecodeArgs& a, void* joined, vo
     // eight CTAs an SM; each goes through all lengths once, so not more of them than that
     const int groups = (a.h + kJoinThreads / 32 - 1) / (kJoinThreads / 32), most = std::max(1, 8 * sm_count() / groups), run = (a.B + most - 1) / most;
     launch_kernel(decode8_join_kernel, dim3((a.B + run - 1) / run, groups), dim3(kJoinThreads), 0, stream, true, static_cast<const float*>(a.part_o),
-                  static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift, a.B, a.h, a.h_pad, a.ctas_per_group, run,
+                  static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift, a.B, a.h, a.h_pad, a.ctas_per_group, gap, run,
                   static_cast<__nv_bfloat16*>(joined), lse);
     if (const int rc = launch_status(); rc != LAGA_OK) return rc;
     launch_kernel(decode8_values_kernel, dim3(a.h, (a.B + 127) / 128), dim3(kValuesThreads), Decode8ValuesSmem::kTotalBytes, stream, true, to, tw, tv, a.status);
@@ -1695,7 +1695,8 @@ int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int
     else if (w.d.heads == 32) rc = launch_attn_decode8<32>(base + w.q_rows, a, st);
     else rc = launch_attn_decode8<64>(base + w.q_rows, a, st);
     if (rc != LAGA_OK) return rc;
-    return w.many ? launch_decode8_join(w_kv_b, a.d, base + w.joined, out, lse, st) : launch_decode_project(w_kv_b, a.d, out, lse, st, true);
+    return w.many ? launch_decode8_join(w_kv_b, a.d, decode8_gap(w.d.heads), base + w.joined, out, lse, st)
+                  : launch_decode_project(w_kv_b, a.d, out, lse, st, true, decode8_gap(w.d.heads));
 }
 
 }  // extern "C"
