@@ -219,7 +219,8 @@ class LagaBlock(torch.nn.Module):
         Where the plan gave only some requests a token, ``requests`` (int64 [B], on the device, ascending) names them; rows of
         ``hidden`` behind the plan's tokens are padding (any request's number, results to be ignored).
         Appends the tokens' latents and keys to ``pages`` and attends to each request's whole cache, the new token included.  Every call reads lengths and tables on the device, so a step can be captured in a
-        graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``, with cache8 for a cache in 8 bits) and replayed.  A page number outside the cache or a
+        graph (with a workspace of its own, ``laga.paged_decode_workspace_bytes``, with cache8 for a cache in 8 bits) and replayed.
+        A page number outside the cache or a
         length outside the table shows only in the workspace's status: give one, and ``laga.check_status(workspace)`` raises
         (with no workspace given, nothing of it is left to ask)."""
         self._service()

@@ -21,10 +21,18 @@
 // the way of a tile: instead of the maximum the threads vote whether m still holds (one word a warp).
 //   output   O^T[512 latents x heads] (+)= V^T (A, MN-major: the same slabs) . P (B, MN-major: a key's probabilities are 16 bytes of a row)
 //
-// Work split: the line of 64-key units of all requests in equal stretches, as there; a tile is two units, or one where a piece ends in an
-// odd one.  A tile is five slabs of 128 keys x 128 codes around a ring with a barrier per slab: the key's first (only scores read it).
+// Work split: the line of 64-key units of all requests in equal stretches, as there, with a gap before each request (decode8_gap); a tile is two
+// units, or one where a piece ends in an odd one.  A tile is five slabs of 128 keys x 128 codes around a ring with a barrier per slab: the
+// key's first (only scores read it).
 //   warps 0 .. 4g-1  softmax: group w / 4 has 8 heads (16 where the CTA has 64), its thread l of warp w % 4 key 32 (w % 4) + l; and the drain
 //   then four warps: TMA producer of the latent's last two slabs; value MMAs; score MMAs (and the first queries); TMA producer of the rest
+//
+// What bounds it.  Bytes are 644 a token, once for all heads; the MMAs, M = 128 from shared memory, take 41, 49 and 66 clocks for 32, 64 and 128 columns
+// whatever the type's width, 36 of them for a tile up to 32 heads a CTA and 52 with 64.  Measured, the whole call: 64 requests of up to 8192 tokens, 16
+// heads, 44.5 us (this kernel 36; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, 81.5 us (65; 3.35 K clocks a tile, HBM's rate
+// too, and 5 K for each switch of request); 8 of up to 65536, 128 heads, 129 us, in long runs, at the card's power limit, 140 (4.1 K clocks a tile
+// against 2.9 K of MMAs: two tiles are in flight, and a slab's life -- load 1.8 K, scores, softmax 2.4 K, values 1.6 K -- is more than twice that);
+// 250 of up to 600, 64 heads, 79 us (56; two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
 #pragma once
 #include "attn_decode_sm100.cuh"
 #include "cache8_sm100.cuh"
@@ -67,7 +75,7 @@ struct AttnDecode8Smem {
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 32 * (kSoftWarps + 4);
     static constexpr bool kSplit = kHeads <= 32;               // both parts of P as columns
-    // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (200 requests of 32 heads 88.2 -> 83.2 us;
+    // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (200 requests of 32 heads 85.7 -> 81.5 us;
     // 64 x 8192 with 16 heads 45.6 -> 46.3, 8 x 65536 with 128 132.3 -> 136.1)
     static constexpr bool kOneCopy = kHeads == 32;
     static constexpr float kDrop = kSplit ? 3.0f : 0.0f;       // P = 2^(d - kDrop): at most 2^8 in e4m3 (hi and 32 times the rest), 2^11 in e5m2 and its rest
@@ -77,7 +85,8 @@ struct AttnDecode8Smem {
     static constexpr int kSlabs = kHeads == 16 ? 12 : kHeads == 32 ? 10 : 8;
     // With 64 heads' queries there are slabs for two tiles but not for their keys' too: the key's slab comes first, into the place of the latent's
     // first, and is scored while that is still on its way.  (A ring of five slabs a tile let a tile's last slab in only after the values of the
-    // tile before: 8 x 65536, 128 heads 153 -> 133.5 us.)
+    // tile before: 8 x 65536, 128 heads 153 us against 133.5.  A place of 8 KB for the key's codes and then their rests, beside eight for the latent, which one
+    // copy of the queries' rotated part would leave room for: 138.)
     static constexpr bool kKeyFirst = kHeads == 64;
     static constexpr int kScales = kHeads == 64 ? 2 : 4;       // tiles whose scales are held
     static constexpr int kQSlab = 2 * kHeads * 128;            // 32 rows for every 16 heads, hi then lo, x 128 channels
@@ -103,6 +112,8 @@ struct AttnDecode8Args {
 
 // Where the line's units lie.  A request with tokens begins with a gap as long as what its switch costs -- queries, a tile without references, the accumulator
 // to drain -- and is then its units: stretches of the line are equal work, not equal units, and one that would begin within a gap begins with the request.
+// (Against no gap: 250 requests of up to 600 tokens, 64 heads 84.5 -> 78.8 us; 200 of about 2000, 32 heads 83.5 -> 81.5; 64 of up to 8192, 16 heads
+// 45.6 -> 44.5.  Of 8, 6 and 5 units: 79.5, 81.6, 45.3; of 3, 3 and 2: 76.5 but 8 x 65536 129 -> 131.5, 82.0, 44.7.)
 constexpr int decode8_gap(int heads) { return heads == 64 ? 5 : heads == 32 ? 4 : 3; }
 
 // Walks the tiles of one CTA's stretch of the line.
@@ -1130,10 +1141,11 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
 }
 
 // Many requests: joining the pieces and the value dimension as two kernels (decode_project_kernel, one, keeps a head's weights and goes through its
-// requests sixteen at a time, a chain of loads, sums, stores and MMAs each: 250 requests of 64 heads 30 us, 200 of 32 heads 18).
+// requests sixteen at a time, a chain of loads, sums, stores and MMAs each: 250 requests of 64 heads 30 us, against 15 and 9.4).
 //     o[c] = sum_p 2^(m_p - M) o_p[c] / sum_p 2^(m_p - M) l_p      a warp for each request and head, many of them: bf16(o) and bf16(o - bf16(o))
 //     out[v] = sum_c W_uv[c, v] (both parts)[c]                    a plain product for each head, 128 requests a CTA
-// Both have the latents in the pieces' order.  A CTA of the first has eight heads and a run of requests.
+// Both have the latents in the pieces' order.  A CTA of the first has eight heads and a run of requests; L2 bounds it (52 MB of pieces and 33 MB of sums,
+// 5.7 TB/s).  The second reads its 384 KB of operands at 60 bytes a clock, which is what an SM's copies get from L2.
 constexpr int kJoinThreads = 256;
 __global__ void __launch_bounds__(kJoinThreads)
 decode8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const int* __restrict__ seq_lens, int columns, int page_shift, int B,

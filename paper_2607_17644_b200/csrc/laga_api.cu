@@ -841,8 +841,8 @@ Decode8Layout decode8_layout(int B, int h) {
     w.d.part_o = w.q_scale + align_up(heads * sizeof(float), 1024);
     w.d.part_ml = w.d.part_o + parts * kDecLat * sizeof(float);
     w.joined = w.d.part_ml + align_up(parts * sizeof(float2), 1024);
-    // (decode_project_kernel, tiles of 16 requests, as many CTAs a head as fit: 250 requests of 64 heads are 8 turns, 93.3 us the call, against 88.9 with
-    // the two kernels; 200 of 32 heads 4 turns, 88.5 against 89.0)
+    // (decode_project_kernel, tiles of 16 requests, as many CTAs a head as fit: 250 requests of 64 heads are 8 turns, 83 us the call, against 78.8 with
+    // the two kernels; 200 of 32 heads 4 turns, 81.5 with either)
     const int ctas_a_head = kDecMaxCtas / h > 0 ? kDecMaxCtas / h : 1;
     w.many = (B + 15) / 16 > 4 * ctas_a_head;
     w.d.total = w.joined + (w.many ? static_cast<size_t>(B) * h * (2 * kDecLat) * 2 : 0);

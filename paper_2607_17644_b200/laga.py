@@ -542,7 +542,8 @@ def paged_decode_workspace_bytes(B, h, d_c=512, d_nope=128, d_rope=64, d_v=128, 
 def paged_decode(q, w_kv_b, cache, block_table, seq_lens, softmax_scale=None, out=None, lse=None, workspace=None, stream=None):
     """laga_paged_decode: attention of one new token per request (q bf16 [B, h, 192], rope band rotated) over a paged cache
     (bf16 [n_pages, page_size, 576]; block_table int32 [B, columns], seq_lens int32 [B], both on the device), or, as
-    laga_paged_decode8, over one in 8 bits (uint8 [n_pages, page_size * CACHE8_TOKEN]).  lse: fp32 [B, h] to have it written.  Returns (out bf16 [B, h, 128], lse or None, workspace); with B = 0 there is nothing to do."""
+    laga_paged_decode8, over one in 8 bits (uint8 [n_pages, page_size * CACHE8_TOKEN]).  lse: fp32 [B, h] to have it written.  Returns
+    (out bf16 [B, h, 128], lse or None, workspace); with B = 0 there is nothing to do."""
     return _run("paged_decode", stream, q, w_kv_b, cache, block_table, seq_lens, softmax_scale, out, lse, workspace)
 
 

@@ -1,7 +1,8 @@
 """State of a service around ``LagaBlock``: a pool of cache pages shared by a fixed number of request rows.
 
 One token's entry is its normalised latent and its rotated shared key, 576 channels for all heads together: in bf16, 1152 bytes, or as
-e4m3 codes with a scale of their own, 644 (``bits=8``; the format in include/laga.h).  The tables are the same for every layer, so one ``LatentCache`` serves a stack of layers: ``pages[layer]`` is what a layer's
+e4m3 codes with a scale of their own, 644 (``bits=8``; the format in include/laga.h).  The tables are the same for every layer, so one
+``LatentCache`` serves a stack of layers: ``pages[layer]`` is what a layer's
 calls read and write.  Everything lives on the device and is updated there (laga_cache_plan); nothing here waits for the GPU.
 """
 from __future__ import annotations
