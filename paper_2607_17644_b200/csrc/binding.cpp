@@ -139,10 +139,10 @@ struct Plan {
 Tensor fresh(const Tensor& like, at::IntArrayRef shape, ScalarType dtype) { return at::empty(shape, like.options().dtype(dtype)); }
 // Elements offset .. offset + n of `whole`: a tensor on the same storage, made directly (of six results, six allocations or six
 // dispatched views would cost more than the call itself).
-Tensor part(const Tensor& whole, int64_t offset, int64_t n) {
+Tensor part(const Tensor& whole, int64_t offset, at::IntArrayRef shape) {
     auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
     impl->set_storage_offset(offset);
-    impl->set_sizes_contiguous({n});
+    impl->set_sizes_contiguous(shape);
     return Tensor(std::move(impl));
 }
 // 1024-byte aligned (the allocator aligns to 512 at least)
@@ -386,6 +386,11 @@ PyObject* py_cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (latent.defined()) expect(latent, ScalarType::BFloat16, {M, 512}, "latent");
     if (k_pe.defined()) expect(k_pe, ScalarType::BFloat16, {M, 64}, "k_pe");
     const c10::Device device = one_device({&cache, &slots, &latent, &k_pe});
+    if (!latent.defined() && !k_pe.defined()) {              // one allocation for both
+        const Tensor whole = fresh(cache, {M * 576}, ScalarType::BFloat16);
+        latent = part(whole, 0, {M, 512});
+        k_pe = part(whole, M * 512, {M, 64});
+    }
     if (!latent.defined()) latent = fresh(cache, {M, 512}, ScalarType::BFloat16);
     if (!k_pe.defined()) k_pe = fresh(cache, {M, 64}, ScalarType::BFloat16);
     if (M > 0)
