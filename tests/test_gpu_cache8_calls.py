@@ -176,3 +176,38 @@ def test_reads_of_repeated_slots(laga):  # noqa: F811
     for got, rows in zip(laga.cache_read(pages, slots), all_of_them):
         want = rows[slots.long().clamp(0, 95)].masked_fill(((slots < 0) | (slots > 95))[:, None], 0)
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("h", [5, 16, 32, 64])
+def test_a_million_tokens(laga, h):  # noqa: F811
+    """A page named 1024 times weighs its tokens 1024 times: the result of the page alone, and a log-sum-exp larger by ln 1024."""
+    q, w, pages, table, n = (t.cuda() for t in case([1024, 1024], h, 1024, seed=80, fill=0))
+    once, lse = torch.empty(2, h, 128, dtype=BF16, device="cuda"), torch.empty(2, h, device="cuda")
+    laga.paged_decode(q, w, pages, table, n, out=once, lse=lse)
+    far, far_lse = torch.empty_like(once), torch.empty_like(lse)
+    _, _, ws = laga.paged_decode(q, w, pages, table.repeat(1, 1024).contiguous(), n * 1024, out=far, lse=far_lse)
+    laga.check_status(ws)
+    # weights' parts, the joined latent's and the result's roundings, 2^-8 each, on both sides
+    assert float((far.float() - once.float()).norm() / once.float().norm()) <= 8e-3
+    # the sums differ by their weights' roundings, 2^-8 at most and of either sign
+    assert float((far_lse - lse - 6.931471805599453).abs().max()) <= 2.0 ** -7
+
+
+def test_twenty_thousand_requests(laga):  # noqa: F811
+    """Against the same requests in calls of 40, whose lines and kernels are others."""
+    B, h, page = 20_000, 2, 16
+    g = torch.Generator().manual_seed(81)
+    lens = torch.randint(0, 50, (B,), generator=g, dtype=torch.int32)
+    base = case([16] * 400, h, page, seed=82, fill=0)
+    pages, w = base[2].cuda(), base[1].cuda()
+    q = torch.randn(B, h, 192, generator=g).to(BF16).cuda()
+    table = torch.randint(0, 400, (B, 4), generator=g, dtype=torch.int32)
+    table = base[3][:, 0][table.long()].to(torch.int32).contiguous().cuda()      # pages that hold tokens
+    lens = lens.cuda()
+    out, _, ws = laga.paged_decode(q, w, pages, table, lens)
+    laga.check_status(ws)
+    assert bool((out[lens == 0] == 0).all()) and not bool(torch.isnan(out.float()).any())
+    for first in (0, 7_960, 19_960):
+        at = slice(first, first + 40)
+        part = laga.paged_decode(q[at], w, pages, table[at], lens[at])[0].float()
+        assert float((out[at].float() - part).norm() / part.norm()) <= 8e-3
