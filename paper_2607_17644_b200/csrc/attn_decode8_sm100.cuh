@@ -1140,211 +1140,277 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
     if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 128); }
 }
 
-// Many requests: joining the pieces and the value dimension as two kernels (decode_project_kernel, one, keeps a head's weights and goes through its
-// requests sixteen at a time, a chain of loads, sums, stores and MMAs each: 250 requests of 64 heads 30 us, against 15 and 9.4).
-//     o[c] = sum_p 2^(m_p - M) o_p[c] / sum_p 2^(m_p - M) l_p      a warp for each request and head, many of them: bf16(o) and bf16(o - bf16(o))
-//     out[v] = sum_c W_uv[c, v] (both parts)[c]                    a plain product for each head, 128 requests a CTA
-// Both have the latents in the pieces' order.  A CTA of the first has eight heads and a run of requests; L2 bounds it (52 MB of pieces and 33 MB of sums,
-// 5.7 TB/s).  The second reads its 384 KB of operands at 60 bytes a clock, which is what an SM's copies get from L2.
-constexpr int kJoinThreads = 256;
-__global__ void __launch_bounds__(kJoinThreads)
-decode8_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const int* __restrict__ seq_lens, int columns, int page_shift, int B,
-                    int h, int h_pad, int ctas_per_group, int gap, int run, __nv_bfloat16* __restrict__ joined, float* __restrict__ lse) {
-    __shared__ int sums[16];
-    grid_launch_dependents();
-    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int head = blockIdx.y * (kJoinThreads / 32) + warp, b0 = blockIdx.x * run, b1 = min(B, b0 + run);
-    // Where the requests' units lie on the line, from the lengths (an input of the call: nothing to wait for).
-    auto units_of = [&](int b) { return (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kD8Unit - 1) / kD8Unit; };
-    int sum = 0, before = 0;
-    for (int b = threadIdx.x; b < B; b += kJoinThreads) {
-        const int units = units_of(b), n = units > 0 ? units + gap : 0;
-        sum += n;
-        before += b < b0 ? n : 0;
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        before += __shfl_xor_sync(0xffffffffu, before, d);
-    }
-    if (lane == 0) { sums[warp] = sum; sums[8 + warp] = before; }
-    __syncthreads();
-    sum = sums[lane & 7];
-    before = sums[8 + (lane & 7)];
-#pragma unroll
-    for (int d = 4; d > 0; d >>= 1) {
-        sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        before += __shfl_xor_sync(0xffffffffu, before, d);
-    }
-    const int per = max(1, (sum + ctas_per_group - 1) / ctas_per_group);
-    grid_dependency_wait();
-    if (head >= h) return;
-    int begin = before;
-    for (int b = b0; b < b1; ++b) {
-        const int n = units_of(b);
-        if (n > 0) begin += gap;
-        const int first = begin / per, count = n > 0 ? (begin + n - 1) / per - first + 1 : 0;
-        begin += n;
-        const size_t row = static_cast<size_t>(first + b) * h_pad + head, step = h_pad;      // the request's first piece; the next one's distance
-        const float2* ml = part_ml + row;
-        float M = -INFINITY, l = 0.f;
-        for (int c = lane; c < count; c += 32) M = fmaxf(M, ml[c * step].x);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        for (int c = lane; c < count; c += 32) {
-            const float2 x = ml[c * step];
-            l = fmaf(fast_exp2(x.x - M), x.y, l);
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-        const float inv = l == 0.f ? 0.f : 1.0f / l;             // (nothing left: every score was -inf; a NaN stays one)
-        float4 acc[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c0 = 0; c0 < count; c0 += 32) {
-            const float mine = c0 + lane < count ? fast_exp2(ml[(c0 + lane) * step].x - M) * inv : 0.f;
-            const int most = min(32, count - c0);
-            const float4* o = reinterpret_cast<const float4*>(part_o + (row + c0 * step) * kDecLat) + lane;
-#pragma unroll 2
-            for (int c = 0; c < most; ++c, o += step * (kDecLat / 4)) {
-                const float w = __shfl_sync(0xffffffffu, mine, c);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float4 x = __ldcs(o + 32 * j);
-                    acc[j] = make_float4(fmaf(x.x, w, acc[j].x), fmaf(x.y, w, acc[j].y), fmaf(x.z, w, acc[j].z), fmaf(x.w, w, acc[j].w));
-                }
-            }
-        }
-        __nv_bfloat16* dst = joined + (static_cast<size_t>(b) * h + head) * (2 * kDecLat) + lane * 4;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t h0 = pack_bf16x2(acc[j].x, acc[j].y), h1 = pack_bf16x2(acc[j].z, acc[j].w);
-            auto rest = [](float a, float b, uint32_t both) { return pack_bf16x2(a - __uint_as_float(both << 16), b - __uint_as_float(both & 0xffff0000u)); };
-            *reinterpret_cast<uint2*>(dst + 128 * j) = make_uint2(h0, h1);
-            *reinterpret_cast<uint2*>(dst + kDecLat + 128 * j) = make_uint2(rest(acc[j].x, acc[j].y, h0), rest(acc[j].z, acc[j].w, h1));
-        }
-        if (lse != nullptr && lane == 0)
-            lse[static_cast<size_t>(b) * h + head] = count > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
-    }
-}
-
-// D[128 requests x 128 values] = (hi, lo) (A, K-major) . W_uv (B, MN-major, rows in the pieces' order), a ring of four stages of 64 latents: both parts' slabs
-// and the weights', which serve both.  warp 0 TMA, warp 1 MMAs, warps 4..7 the result.
-constexpr int kValuesThreads = 256, kValuesStages = 4;
-struct Decode8ValuesSmem {
+// Joining the pieces and the value dimension for many requests.  (decode_project_kernel keeps a head's weights and goes through its requests sixteen at a
+// time, a chain of loads, sums, stores and MMAs each; two kernels, for the sums and for the product, pass 2 KB a request and head through L2.  250
+// requests of up to 600 tokens, 64 heads, the call replayed: 69.8 us with the first, 66.5 with the two, 62.8 so; L2 bounds it, 52 MB of pieces.)
+// A CTA has a head and up to 128 requests:
+//     w_p = 2^(m_p - M) / sum_p 2^(m_p - M) l_p,   o[c] = sum_p w_p o_p[c] as bf16(o) and bf16(o - bf16(o)),   out[v] = sum_c W_uv[c, v] (both parts)[c]
+// D[128 requests x 128 values] = the parts (A, K-major) . W_uv (B, MN-major, rows in the pieces' order), 64 latents at a time: sixteen warps sum
+// those of all requests, half a warp a request, the next 64 on their way from L2 meanwhile, while the seventeenth multiplies the last.  A
+// request of more than kJoinAlone pieces, of which half a warp would make a long chain, is summed by all of them first, into its first piece's place.
+constexpr int kJoinWarps = 16, kJoinThreads = 32 * (kJoinWarps + 1), kJoinRows = 128, kJoinSteps = kDecLat / 64, kJoinAlone = 8;
+struct Decode8JoinSmem {
     static constexpr int kSlab = 128 * 128;                      // 128 requests x 64 latents; or 2 x (64 latents x 64 values)
-    static constexpr int kStage = 3 * kSlab;
-    static constexpr int kBar = kValuesStages * kStage;
-    static constexpr int kTotalBytes = kBar + (2 * kValuesStages + 1) * 8 + 24;
+    static constexpr int kW = 0;                                 // all of a head's, a slab a step
+    static constexpr int kA = kW + kJoinSteps * kSlab;           // two buffers of both parts; later the results' boxes
+    static constexpr int kMaxPieces = kDecMaxCtas + kJoinRows;
+    static constexpr int kPieces = kA + 4 * kSlab;               // a request's first stretch, how many pieces, where their weights begin
+    static constexpr int kWeights = kPieces + kJoinRows * 16;
+    static constexpr int kScan = kWeights + kMaxPieces * 4;
+    static constexpr int kLong = kScan + 40 * 4;                 // requests of more than kJoinAlone pieces: how many, then which
+    static constexpr int kBar = kLong + (1 + kMaxPieces / (kJoinAlone + 1) + 1) * 4;
+    static constexpr int kTotalBytes = kBar + (kJoinSteps + 5) * 8 + 16;
+    static_assert(kTotalBytes <= 232448 && kBar % 8 == 0 && kPieces % 16 == 0, "shared memory of the join");
 };
-static_assert(Decode8ValuesSmem::kTotalBytes <= 232448, "shared memory of the values' product");
-__global__ void __launch_bounds__(kValuesThreads, 1)
-decode8_values_kernel(const __grid_constant__ CUtensorMap tmap_o, const __grid_constant__ CUtensorMap tmap_wv, const __grid_constant__ CUtensorMap tmap_out,
-                      unsigned* status) {
-    using L = Decode8ValuesSmem;
+__global__ void __launch_bounds__(kJoinThreads, 1)
+decode8_join_kernel(const __grid_constant__ CUtensorMap tmap_wv, const __grid_constant__ CUtensorMap tmap_out, float* part_o,
+                    const float2* __restrict__ part_ml, const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad,
+                    int ctas_per_group, int gap, int n_rows, float* __restrict__ lse, unsigned* status) {
+    using L = Decode8JoinSmem;
     extern __shared__ __align__(1024) uint8_t smem[];
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
-    uint64_t* empty = full + kValuesStages;
-    uint64_t* done = empty + kValuesStages;
+    uint64_t* w_full = reinterpret_cast<uint64_t*>(smem + L::kBar);      // [kJoinSteps]
+    uint64_t* a_full = w_full + kJoinSteps;                              // [2] both parts of 64 latents are in buffer i
+    uint64_t* a_empty = a_full + 2;                                      // [2] ... have been multiplied
+    uint64_t* done = a_empty + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
     AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(tmem_slot + 1);
+    int4* pieces = reinterpret_cast<int4*>(smem + L::kPieces);
+    float* weights = reinterpret_cast<float*>(smem + L::kWeights);
+    int *scan = reinterpret_cast<int*>(smem + L::kScan), *long_ones = reinterpret_cast<int*>(smem + L::kLong);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-    const int head = blockIdx.x, b0 = blockIdx.y * 128;
-    constexpr int kSteps = kDecLat / 64;
-    auto load_weights = [&](int k) {
-        uint8_t* dst = smem + (k % kValuesStages) * L::kStage + 2 * L::kSlab;
-        for (int i = 0; i < 2; ++i)
-            tma_load_turned_chk(status, dst + i * (L::kSlab / 2), &tmap_wv, &full[k % kValuesStages], head * 256 + i * 64, k * 16);
-    };
+    const int head = blockIdx.x, b0 = blockIdx.y * n_rows;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kValuesStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < kJoinSteps; ++i) mbar_init(&w_full[i], 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&a_full[i], kJoinWarps); mbar_init(&a_empty[i], 1); }
         mbar_init(done, 1);
         abort_flag->value = 0;
         mbar_fence_init();
-        for (int k = 0; k < kValuesStages; ++k) {                // (weights are an input: nothing to wait for)
-            mbar_arrive_expect_tx(&full[k], L::kStage);
-            load_weights(k);
+        for (int k = 0; k < kJoinSteps; ++k) {                   // (weights are an input: nothing to wait for)
+            mbar_arrive_expect_tx(&w_full[k], L::kSlab);
+            for (int i = 0; i < 2; ++i)
+                tma_load_turned_chk(status, smem + L::kW + k * L::kSlab + i * (L::kSlab / 2), &tmap_wv, &w_full[k], head * 256 + i * 64, k * 16);
         }
     }
-    if (warp == 1) { tmem_alloc(tmem_slot, 128); tmem_relinquish(); }
+    if (warp == kJoinWarps) { tmem_alloc(tmem_slot, 128); tmem_relinquish(); }
+    // Where the requests lie on the line, from the lengths (an input too).
+    auto units_of = [&](int b) { return (decode_clamp(__ldg(seq_lens + b), columns, page_shift) + kD8Unit - 1) / kD8Unit; };
+    {
+        int sum = 0, before = 0;
+        for (int b = threadIdx.x; b < B; b += kJoinThreads) {
+            const int n = units_of(b), line = n > 0 ? n + gap : 0;
+            sum += line;
+            before += b < b0 ? line : 0;
+        }
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) { scan[warp] = sum; scan[20 + warp] = before; }
+    }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     grid_launch_dependents();
     const uint32_t tmem = *tmem_slot;
-    if (warp == 0) {
-        if (elect_one()) {
-            grid_dependency_wait();
-            bool ok = true;
-            for (int k = 0; k < kSteps; ++k) {
-                const int s = k % kValuesStages;
-                if (k >= kValuesStages) {
-                    ok = mbar_wait(&empty[s], ((k / kValuesStages) & 1) ^ 1, abort_flag, status, 0x94);
-                    if (!ok) break;
-                    mbar_arrive_expect_tx(&full[s], L::kStage);
-                    load_weights(k);
-                }
-                for (int part = 0; part < 2; ++part)
-                    tma_load_2d_chk(status, smem + s * L::kStage + part * L::kSlab, &tmap_o, &full[s], head * (2 * kDecLat) + part * kDecLat + k * 64, b0);
-            }
-            if (!ok)                                             // (stages in flight: each armed in its first turn, or in its second)
-                for (int s = 0; s < kValuesStages; ++s) { mbar_wait_quiesce(&full[s], 0); mbar_wait_quiesce(&full[s], 1); }
+    if (warp == 0) {                                             // four requests a lane, then over the lanes
+        int sum = lane <= kJoinWarps ? scan[lane] : 0, position = lane <= kJoinWarps ? scan[20 + lane] : 0;
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        position = __reduce_add_sync(0xffffffffu, position);
+        const int per = max(1, (sum + ctas_per_group - 1) / ctas_per_group);
+        int n[4], line = 0, count[4], total = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = lane * 4 + i;
+            n[i] = r < n_rows && b0 + r < B ? units_of(b0 + r) : 0;
+            line += n[i] > 0 ? n[i] + gap : 0;
         }
-        __syncwarp();
-    } else if (warp == 1) {
+        auto before_lane = [&](int v) {
+            int incl = v;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += o;
+            }
+            return incl - v;
+        };
+        position += before_lane(line);
+        int first[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (n[i] > 0) position += gap;
+            // (the bounds hold anyway, unless the lengths change under the kernel)
+            first[i] = min(position / per, ctas_per_group - 1);
+            count[i] = n[i] > 0 ? min((position + n[i] - 1) / per, ctas_per_group - 1) - first[i] + 1 : 0;
+            position += n[i];
+            total += count[i];
+        }
+        int base = before_lane(total), n_long = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            count[i] = max(0, min(count[i], L::kMaxPieces - base));
+            pieces[lane * 4 + i] = make_int4(first[i], count[i], base, 0);
+            base += count[i];
+            const uint32_t many = __ballot_sync(0xffffffffu, count[i] > kJoinAlone);
+            if (count[i] > kJoinAlone) long_ones[1 + n_long + __popc(many & ((1u << lane) - 1u))] = lane * 4 + i;
+            n_long += __popc(many);
+        }
+        if (lane == 0) long_ones[0] = n_long;
+    }
+    __syncthreads();
+    grid_dependency_wait();
+    bool ok = true;
+    if (warp == kJoinWarps) {
         if (elect_one()) {
             constexpr uint32_t idesc = make_idesc_bf16(128, 128, 0, 1);
-            bool ok = true;
-            for (int k = 0; k < kSteps; ++k) {
-                const int s = k % kValuesStages;
-                ok = mbar_wait(&full[s], (k / kValuesStages) & 1, abort_flag, status, 0x95);
+            for (int k = 0; k < kJoinSteps; ++k) {
+                const int buf = k & 1;
+                ok = mbar_wait(&w_full[k], 0, abort_flag, status, 0x94);
+                if (ok) ok = mbar_wait(&a_full[buf], (k >> 1) & 1, abort_flag, status, 0x95);
                 if (!ok) break;
                 tc_fence_after_sync();
-                const uint32_t base = smem_u32(smem + s * L::kStage);
-                const uint64_t db = desc_mn_major(base + 2 * L::kSlab, L::kSlab / 2);
+                const uint64_t db = desc_mn_major(smem_u32(smem + L::kW + k * L::kSlab), L::kSlab / 2);
                 for (int part = 0; part < 2; ++part) {
-                    const uint64_t da = desc_k_major(base + part * L::kSlab);
+                    const uint64_t da = desc_k_major(smem_u32(smem + L::kA + (2 * buf + part) * L::kSlab));
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) mma_ss(tmem, da + kk * 2, db + kk * 128, idesc, (k > 0 || part > 0 || kk > 0) ? 1u : 0u);
                 }
-                mma_commit(&empty[s]);
+                mma_commit(&a_empty[buf]);
             }
             mma_commit(done);
-            if (!ok) mbar_wait_quiesce(done, 0);
+            if (!ok) {
+                for (int k = 0; k < kJoinSteps; ++k) mbar_wait_quiesce(&w_full[k], 0);
+                mbar_wait_quiesce(done, 0);
+            }
         }
         __syncwarp();
-    }
-    bool ok = true;
-    if (warp >= 4) {
-        ok = mbar_wait_warp(done, 0, abort_flag, status, 0x96) && abort_flag->value == 0u;
-        ok = __all_sync(0xffffffffu, ok);
-        tc_fence_after_sync();
-        // two boxes of 128 requests x 64 values, over a stage that has been multiplied
-        const int r = (warp & 3) * 32 + lane;
-        uint8_t* line = smem + r * 128;
-#pragma unroll 1
-        for (int c = 0; c < 128; c += 16) {
-            uint32_t v[16], w[8];
-            tmem_ld_x16(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + c, v);
-            tmem_ld_wait();
+    } else {
+        // ---- weights: a warp for a request, the warp's own below ---------------------------------------------
+        for (int i = 0; i < n_rows / kJoinWarps; ++i) {
+            const int r = (i >> 1) * (2 * kJoinWarps) + warp * 2 + (i & 1);
+            if (b0 + r >= B) break;
+            const int4 p = pieces[r];
+            const float2* ml = part_ml + static_cast<size_t>(p.x + b0 + r) * h_pad + head;
+            float M = -INFINITY, l = 0.f;
+            for (int c = lane; c < p.y; c += 32) M = fmaxf(M, ml[static_cast<size_t>(c) * h_pad].x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-            uint8_t* box = line + (c >> 6) * L::kSlab;
-            const int chunk = (c & 63) >> 3;
-            *reinterpret_cast<uint4*>(box + ((chunk ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint4*>(box + (((chunk + 1) ^ (r & 7)) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+            for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+            for (int c = lane; c < p.y; c += 32) {
+                const float2 x = ml[static_cast<size_t>(c) * h_pad];
+                const float w = fast_exp2(x.x - M);
+                weights[p.z + c] = w;
+                l = fmaf(w, x.y, l);
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+            const float inv = l == 0.f ? 0.f : 1.0f / l;         // (nothing left: every score was -inf; a NaN stays one)
+            for (int c = lane; c < p.y; c += 32) weights[p.z + c] *= inv;
+            if (lse != nullptr && lane == 0)
+                lse[static_cast<size_t>(b0 + r) * h + head] = p.y > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        }
+        __syncwarp();
+        const size_t step = static_cast<size_t>(h_pad) * (kDecLat / 4);
+        auto add = [](float4 x, float w, float4 a) { return make_float4(fmaf(x.x, w, a.x), fmaf(x.y, w, a.y), fmaf(x.z, w, a.z), fmaf(x.w, w, a.w)); };
+        const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+        // ---- requests of many pieces: a quarter of the warps every fourth piece, then the four quarters -----------------
+        if (const int n_long = long_ones[0]; n_long > 0) {
+            auto joiners_meet = []() { asm volatile("bar.sync 1, %0;" ::"n"(kJoinWarps * 32) : "memory"); };
+            float4* quarters = reinterpret_cast<float4*>(smem + L::kA);
+            const int col = threadIdx.x & 127, part = threadIdx.x >> 7;
+            joiners_meet();                                      // (all weights are there)
+            for (int i = 0; i < n_long; ++i) {
+                const int r = long_ones[1 + i];
+                const int4 p = pieces[r];
+                float4* o = reinterpret_cast<float4*>(part_o + (static_cast<size_t>(p.x + b0 + r) * h_pad + head) * kDecLat) + col;
+                float4 sum = none;
+#pragma unroll 8
+                for (int c = part; c < p.y; c += 4) sum = add(__ldcs(o + c * step), weights[p.z + c], sum);
+                quarters[part * 128 + col] = sum;
+                joiners_meet();
+                if (part == 0) {
+                    *o = add(quarters[384 + col], 1.f, add(quarters[256 + col], 1.f, add(quarters[128 + col], 1.f, sum)));
+                    if (col == 0) {
+                        pieces[r].y = 1;
+                        weights[p.z] = 1.f;
+                    }
+                }
+                joiners_meet();
+            }
+        }
+        // ---- sums: half a warp a request, four latents a lane; the first two pieces' a step ahead ---------------
+        constexpr int kMost = kJoinRows / (2 * kJoinWarps);
+        const int quad = lane & 15;
+        const float4* src[kMost];
+        int count[kMost], base[kMost];
+        float w0[kMost], w1[kMost];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const int r = i * (2 * kJoinWarps) + warp * 2 + (lane >> 4);
+            const int4 p = r < n_rows && b0 + r < B ? pieces[r] : make_int4(0, 0, 0, 0);
+            src[i] = reinterpret_cast<const float4*>(part_o + (static_cast<size_t>(p.x + b0 + r) * h_pad + head) * kDecLat) + quad;
+            count[i] = p.y;
+            base[i] = p.z;
+            w0[i] = p.y > 0 ? weights[p.z] : 0.f;
+            w1[i] = p.y > 1 ? weights[p.z + 1] : 0.f;
+        }
+        float4 x0[kMost], x1[kMost];
+        auto fetch = [&](int k) {
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                x0[i] = count[i] > 0 ? __ldcs(src[i] + k * 16) : none;
+                x1[i] = count[i] > 1 ? __ldcs(src[i] + step + k * 16) : none;
+            }
+        };
+        fetch(0);
+#pragma unroll 1
+        for (int k = 0; k < kJoinSteps; ++k) {
+            const int buf = k & 1;
+            float4 acc[kMost];
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                acc[i] = add(x1[i], w1[i], add(x0[i], w0[i], none));
+                for (int c = 2; c < count[i]; ++c) acc[i] = add(__ldcs(src[i] + c * step + k * 16), weights[base[i] + c], acc[i]);
+            }
+            if (k + 1 < kJoinSteps) fetch(k + 1);
+            ok = mbar_wait_warp(&a_empty[buf], ((k >> 1) & 1) ^ 1, abort_flag, status, 0x96);
+            if (!ok) break;
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                const int r = i * (2 * kJoinWarps) + warp * 2 + (lane >> 4);
+                if (r >= n_rows) break;                          // (rows that are nobody's: their results are not stored)
+                const uint32_t h0 = pack_bf16x2(acc[i].x, acc[i].y), h1 = pack_bf16x2(acc[i].z, acc[i].w);
+                auto rest = [](float a, float b, uint32_t both) { return pack_bf16x2(a - __uint_as_float(both << 16), b - __uint_as_float(both & 0xffff0000u)); };
+                uint8_t* at = smem + L::kA + 2 * buf * L::kSlab + r * 128 + (((quad >> 1) ^ (r & 7)) << 4) + (quad & 1) * 8;
+                *reinterpret_cast<uint2*>(at) = make_uint2(h0, h1);
+                *reinterpret_cast<uint2*>(at + L::kSlab) = make_uint2(rest(acc[i].x, acc[i].y, h0), rest(acc[i].z, acc[i].w, h1));
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&a_full[buf]);
+        }
+        if (ok) ok = mbar_wait_warp(done, 0, abort_flag, status, 0x98);
+        ok = __all_sync(0xffffffffu, ok && abort_flag->value == 0u);
+        tc_fence_after_sync();
+        // two boxes of requests x 64 values, over the parts, which have been multiplied
+        const int r = (warp & 3) * 32 + lane, c0 = (warp >> 2) * 32;
+        uint32_t v[32];
+        tmem_ld_x32(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + c0, v);
+        tmem_ld_wait();
+        uint8_t* line = smem + L::kA + (c0 >> 6) * L::kSlab + r * 128;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(__uint_as_float(v[8 * i + 2 * j]), __uint_as_float(v[8 * i + 2 * j + 1]));
+            *reinterpret_cast<uint4*>(line + (((((c0 & 63) >> 3) + i) ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
         fence_async_shared();
     }
-    grid_dependency_wait();
     if (__syncthreads_and(ok) && threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) tma_store_2d(&tmap_out, smem + i * L::kSlab, head * 128 + i * 64, b0);
+        for (int i = 0; i < 2; ++i) tma_store_2d(&tmap_out, smem + L::kA + i * L::kSlab, head * 128 + i * 64, b0);
         tma_store_commit();
         tma_store_wait_all();
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 1) { tc_fence_after_sync(); tmem_dealloc(tmem, 128); }
+    if (warp == kJoinWarps) { tc_fence_after_sync(); tmem_dealloc(tmem, 128); }
 }
 
 }  // namespace laga

@@ -185,7 +185,7 @@ void init_device(DeviceInfo* info, int dev) {
               allow_smem(attn_decode8_sm100_kernel<16>, AttnDecode8Smem<16>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<32>, AttnDecode8Smem<32>::kTotalBytes) &&
               allow_smem(attn_decode8_sm100_kernel<64>, AttnDecode8Smem<64>::kTotalBytes) &&
-              allow_smem(decode8_values_kernel, Decode8ValuesSmem::kTotalBytes) &&
+              allow_smem(decode8_join_kernel, Decode8JoinSmem::kTotalBytes) &&
               allow_smem(decode_absorb8_kernel, DecodeAbsorb8Smem::kTotalBytes) &&
               allow_smem(decode_absorb8_rows_kernel<1>, DecodeAbsorb8RowsSmem<1>::kTotalBytes) &&
               allow_smem(decode_absorb8_rows_kernel<2>, DecodeAbsorb8RowsSmem<2>::kTotalBytes) &&
@@ -829,8 +829,6 @@ int launch_decode_project(const void* w, const AttnDecodeArgs& a, void* out, flo
 struct Decode8Layout {
     DecodeLayout d;
     size_t q_rows, q_scale;                           // in the place of d's q_abs
-    bool many;                                        // joined and projected by two kernels
-    size_t joined;                                    // what the first leaves to the second: [B][h][2][512] bf16
 };
 Decode8Layout decode8_layout(int B, int h) {
     Decode8Layout w;
@@ -840,12 +838,7 @@ Decode8Layout decode8_layout(int B, int h) {
     w.q_scale = w.q_rows + align_up(heads * 2 * kC8Row, 1024);
     w.d.part_o = w.q_scale + align_up(heads * sizeof(float), 1024);
     w.d.part_ml = w.d.part_o + parts * kDecLat * sizeof(float);
-    w.joined = w.d.part_ml + align_up(parts * sizeof(float2), 1024);
-    // (decode_project_kernel, tiles of 16 requests, as many CTAs a head as fit: 250 requests of 64 heads are 8 turns, 83 us the call, against 78.8 with
-    // the two kernels; 200 of 32 heads 4 turns, 81.5 with either)
-    const int ctas_a_head = kDecMaxCtas / h > 0 ? kDecMaxCtas / h : 1;
-    w.many = (B + 15) / 16 > 4 * ctas_a_head;
-    w.d.total = w.joined + (w.many ? static_cast<size_t>(B) * h * (2 * kDecLat) * 2 : 0);
+    w.d.total = w.d.part_ml + align_up(parts * sizeof(float2), 1024);
     return w;
 }
 
@@ -880,20 +873,23 @@ int launch_attn_decode8(const uint8_t* q_rows, const AttnDecode8Args& a, cudaStr
     return launch_status();
 }
 
-int launch_decode8_join(const void* w, const AttnDecodeArgs& a, int gap, void* joined, void* out, float* lse, cudaStream_t stream) {
-    const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv), o_row = static_cast<uint64_t>(a.h) * 2 * kDecLat, out_row = static_cast<uint64_t>(a.h) * kDv;
-    const void* wv = static_cast<const uint8_t*>(w) + kDn * 2;
-    CUtensorMap to, tw, tv;
-    if (!cached_tmap_bf16(&to, joined, o_row, a.B, o_row * 2, 128) || !cached_tmap_codes(&tw, kMapTurned, wv, w_row - kDn, kDc, w_row * 2, 16) ||
-        !cached_tmap_bf16(&tv, out, out_row, a.B, out_row * 2, 128))
+// Requests a CTA of decode8_join_kernel; 0 for decode_project_kernel, which has CTAs for fewer requests and all warps for a request's pieces.  By requests over
+// the CTAs that a head can have: 28 of them (256 requests of 400 to 512 tokens, 16 heads) 40.5 us the call with 64 a CTA, 37.6 with the other kernel;
+// 40 (128 heads) 45.3, 43.4; 50 (200 of 1000 to 2048, 32 heads) 67.5, 70.2, with 128 a CTA 72.5; 125 (250 of up to 600, 64 heads) 70.6 and, with 128,
+// 62.8, against 69.8; 228 (2048 of 100 to 128, 16 heads) 127, 109.5, 110.1.
+int decode8_join_rows(int B, int h) {
+    const long long ctas_a_head = std::max(1, kDecMaxCtas / h);
+    return B <= 48 * ctas_a_head ? 0 : B <= 64 * ctas_a_head ? 64 : 128;
+}
+int launch_decode8_join(const void* w, const AttnDecodeArgs& a, int gap, int n_rows, void* out, float* lse, cudaStream_t stream) {
+    const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv), out_row = static_cast<uint64_t>(a.h) * kDv;
+    CUtensorMap tw, to;
+    if (!cached_tmap_codes(&tw, kMapTurned, static_cast<const uint8_t*>(w) + kDn * 2, w_row - kDn, kDc, w_row * 2, 16) ||
+        !cached_tmap_bf16(&to, out, out_row, a.B, out_row * 2, n_rows))
         return LAGA_ERR_CUDA;
-    // eight CTAs an SM; each goes through all lengths once, so not more of them than that
-    const int groups = (a.h + kJoinThreads / 32 - 1) / (kJoinThreads / 32), most = std::max(1, 8 * sm_count() / groups), run = (a.B + most - 1) / most;
-    launch_kernel(decode8_join_kernel, dim3((a.B + run - 1) / run, groups), dim3(kJoinThreads), 0, stream, true, static_cast<const float*>(a.part_o),
-                  static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift, a.B, a.h, a.h_pad, a.ctas_per_group, gap, run,
-                  static_cast<__nv_bfloat16*>(joined), lse);
-    if (const int rc = launch_status(); rc != LAGA_OK) return rc;
-    launch_kernel(decode8_values_kernel, dim3(a.h, (a.B + 127) / 128), dim3(kValuesThreads), Decode8ValuesSmem::kTotalBytes, stream, true, to, tw, tv, a.status);
+    launch_kernel(decode8_join_kernel, dim3(a.h, (a.B + n_rows - 1) / n_rows), dim3(kJoinThreads), Decode8JoinSmem::kTotalBytes, stream, true, tw, to,
+                  a.part_o, static_cast<const float2*>(a.part_ml), a.seq_lens, a.columns, a.page_shift, a.B, a.h, a.h_pad,
+                  a.ctas_per_group, gap, n_rows, lse, a.status);
     return launch_status();
 }
 
@@ -1695,8 +1691,8 @@ int laga_paged_decode8(const void* q, const void* w_kv_b, const void* cache, int
     else if (w.d.heads == 32) rc = launch_attn_decode8<32>(base + w.q_rows, a, st);
     else rc = launch_attn_decode8<64>(base + w.q_rows, a, st);
     if (rc != LAGA_OK) return rc;
-    return w.many ? launch_decode8_join(w_kv_b, a.d, decode8_gap(w.d.heads), base + w.joined, out, lse, st)
-                  : launch_decode_project(w_kv_b, a.d, out, lse, st, true, decode8_gap(w.d.heads));
+    const int gap = decode8_gap(w.d.heads), join_rows = decode8_join_rows(B, h);
+    return join_rows > 0 ? launch_decode8_join(w_kv_b, a.d, gap, join_rows, out, lse, st) : launch_decode_project(w_kv_b, a.d, out, lse, st, true, gap);
 }
 
 }  // extern "C"

@@ -92,7 +92,7 @@ def test_requests_joined_and_projected_apart(laga, B, h):  # noqa: F811
 
 
 def test_the_same_requests_with_few_others_and_with_many(laga):  # noqa: F811
-    """Values that are not finite stay with their request, whichever kernels join the pieces."""
+    """Values that are not finite stay with their request, whichever kernel joins the pieces."""
     h = 64
     q, w, pages, table, lens = case([90, 0, 700, 33] + [5] * 130, h, 16, seed=15)
     codes, scales = c8.planes(pages)
