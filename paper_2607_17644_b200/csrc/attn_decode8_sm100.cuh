@@ -29,10 +29,10 @@
 //
 // What bounds it.  Bytes are 644 a token, once for all heads; the MMAs, M = 128 from shared memory, take 41, 49 and 66 clocks for 32, 64 and 128 columns
 // whatever the type's width, 36 of them for a tile up to 32 heads a CTA and 52 with 64.  Measured, the whole call: 64 requests of up to 8192 tokens, 16
-// heads, 44.5 us (this kernel 35; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, 81.5 us (63; 3.35 K clocks a tile, HBM's rate
+// heads, 44.5 us (this kernel 35; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, 78.7 us (63; 3.35 K clocks a tile, HBM's rate
 // too, and 5 K for each switch of request); 8 of up to 65536, 128 heads, 129 us, in long runs, at the card's power limit, 149 (125; 4.1 K clocks a tile
 // against 2.9 K of MMAs: two tiles are in flight, and a slab's life -- load 1.8 K, scores, softmax 2.4 K, values 1.6 K -- is more than twice that);
-// 250 of up to 600, 64 heads, 78 us (50; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
+// 250 of up to 600, 64 heads, 74.5 us (50; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
 #pragma once
 #include "attn_decode_sm100.cuh"
 #include "cache8_sm100.cuh"
@@ -75,8 +75,8 @@ struct AttnDecode8Smem {
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 32 * (kSoftWarps + 4);
     static constexpr bool kSplit = kHeads <= 32;               // both parts of P as columns
-    // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (200 requests of 32 heads 85.7 -> 81.5 us;
-    // 64 x 8192 with 16 heads 45.6 -> 46.3, 8 x 65536 with 128 132.3 -> 136.1)
+    // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (saves 4.2 us for 200 requests
+    // of about 2000 tokens, 32 heads; would cost 0.7 at 64 x 8192 with 16 heads and 3.8 at 8 x 65536 with 128)
     static constexpr bool kOneCopy = kHeads == 32;
     static constexpr float kDrop = kSplit ? 3.0f : 0.0f;       // P = 2^(d - kDrop): at most 2^8 in e4m3 (hi and 32 times the rest), 2^11 in e5m2 and its rest
     static constexpr int kCols = kSplit ? 2 * kHeads : kHeads; // TMEM columns of 128 latents of O^T
@@ -112,8 +112,8 @@ struct AttnDecode8Args {
 
 // Where the line's units lie.  A request with tokens begins with a gap as long as what its switch costs -- queries, a tile without references, the accumulator
 // to drain -- and is then its units: stretches of the line are equal work, not equal units, and one that would begin within a gap begins with the request.
-// (Against no gap: 250 requests of up to 600 tokens, 64 heads 84.5 -> 78.8 us; 200 of about 2000, 32 heads 83.5 -> 81.5; 64 of up to 8192, 16 heads
-// 45.6 -> 44.5.  Of 8, 6 and 5 units: 79.5, 81.6, 45.3; of 3, 3 and 2: 76.5 but 8 x 65536 129 -> 131.5, 82.0, 44.7.)
+// (Saves 5.7 us for 250 requests of up to 600 tokens, 64 heads, 2.0 for 200 of about 2000, 32 heads, 1.1 for 64 of up to 8192, 16 heads.  Of 8, 6 and 5
+// units: 1.3, 0.1 and 0.8 less; of 3, 3 and 2: 2.3 more, but 2.4 lost at 8 x 65536 with 128 heads, 0.5 and 0.2 less.)
 constexpr int decode8_gap(int heads) { return heads == 64 ? 5 : heads == 32 ? 4 : 3; }
 
 // Walks the tiles of one CTA's stretch of the line.
