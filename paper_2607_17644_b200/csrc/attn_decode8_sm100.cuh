@@ -1282,27 +1282,29 @@ decode8_join_kernel(const __grid_constant__ CUtensorMap tmap_wv, const __grid_co
         }
         __syncwarp();
     } else {
-        // ---- weights: a warp for a request, the warp's own below ---------------------------------------------
-        for (int i = 0; i < n_rows / kJoinWarps; ++i) {
-            const int r = (i >> 1) * (2 * kJoinWarps) + warp * 2 + (i & 1);
-            if (b0 + r >= B) break;
-            const int4 p = pieces[r];
+        // ---- weights: four lanes a request, of the eight that this warp sums below ------------------------------
+        {
+            const int r = (lane >> 3) * (2 * kJoinWarps) + warp * 2 + ((lane >> 2) & 1), q = lane & 3;
+            const bool mine = r < n_rows && b0 + r < B;
+            const int4 p = mine ? pieces[r] : make_int4(0, 0, 0, 0);
             const float2* ml = part_ml + static_cast<size_t>(p.x + b0 + r) * h_pad + head;
             float M = -INFINITY, l = 0.f;
-            for (int c = lane; c < p.y; c += 32) M = fmaxf(M, ml[static_cast<size_t>(c) * h_pad].x);
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-            for (int c = lane; c < p.y; c += 32) {
+#pragma unroll 4
+            for (int c = q; c < p.y; c += 4) M = fmaxf(M, ml[static_cast<size_t>(c) * h_pad].x);
+            M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 1));
+            M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, 2));
+#pragma unroll 4
+            for (int c = q; c < p.y; c += 4) {
                 const float2 x = ml[static_cast<size_t>(c) * h_pad];
                 const float w = fast_exp2(x.x - M);
                 weights[p.z + c] = w;
                 l = fmaf(w, x.y, l);
             }
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
             const float inv = l == 0.f ? 0.f : 1.0f / l;         // (nothing left: every score was -inf; a NaN stays one)
-            for (int c = lane; c < p.y; c += 32) weights[p.z + c] *= inv;
-            if (lse != nullptr && lane == 0)
+            for (int c = q; c < p.y; c += 4) weights[p.z + c] *= inv;
+            if (mine && q == 0 && lse != nullptr)
                 lse[static_cast<size_t>(b0 + r) * h + head] = p.y > 0 ? (M + log2f(l)) * 0.6931471805599453f : -INFINITY;
         }
         __syncwarp();
