@@ -29,10 +29,10 @@
 //
 // What bounds it.  Bytes are 644 a token, once for all heads; the MMAs, M = 128 from shared memory, take 41, 49 and 66 clocks for 32, 64 and 128 columns
 // whatever the type's width, 36 of them for a tile up to 32 heads a CTA and 52 with 64.  Measured, the whole call: 64 requests of up to 8192 tokens, 16
-// heads, 44.5 us (this kernel 35; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, 78.7 us (63; 3.35 K clocks a tile, HBM's rate
+// heads, 44.5 us (this kernel 35; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, 75.9 us (62; 3.35 K clocks a tile, HBM's rate
 // too, and 5 K for each switch of request); 8 of up to 65536, 128 heads, 129 us, in long runs, at the card's power limit, 149 (125; 4.1 K clocks a tile
 // against 2.9 K of MMAs: two tiles are in flight, and a slab's life -- load 1.8 K, scores, softmax 2.4 K, values 1.6 K -- is more than twice that);
-// 250 of up to 600, 64 heads, 74.5 us (50; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
+// 250 of up to 600, 64 heads, 69.5 us (49; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
 #pragma once
 #include "attn_decode_sm100.cuh"
 #include "cache8_sm100.cuh"
@@ -1142,7 +1142,8 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
 
 // Joining the pieces and the value dimension for many requests.  (decode_project_kernel keeps a head's weights and goes through its requests sixteen at a
 // time, a chain of loads, sums, stores and MMAs each; two kernels, for the sums and for the product, pass 2 KB a request and head through L2.  250
-// requests of up to 600 tokens, 64 heads, the call replayed: 69.8 us with the first, 66.5 with the two, 62.8 so; L2 bounds it, 52 MB of pieces.)
+// requests of up to 600 tokens, 64 heads, the call replayed: 69.8 us with the first, 66.5 with the two, 55.6 so.  Itself 15.4 us, of which L2 needs some 8 for
+// 52 MB of pieces; the rest are a launch, the weights of the sum and eight steps' latencies.)
 // A CTA has a head and up to 128 requests:
 //     w_p = 2^(m_p - M) / sum_p 2^(m_p - M) l_p,   o[c] = sum_p w_p o_p[c] as bf16(o) and bf16(o - bf16(o)),   out[v] = sum_c W_uv[c, v] (both parts)[c]
 // D[128 requests x 128 values] = the parts (A, K-major) . W_uv (B, MN-major, rows in the pieces' order), 64 latents at a time: sixteen warps sum

@@ -874,12 +874,12 @@ int launch_attn_decode8(const uint8_t* q_rows, const AttnDecode8Args& a, cudaStr
 }
 
 // Requests a CTA of decode8_join_kernel; 0 for decode_project_kernel, which has CTAs for fewer requests and all warps for a request's pieces.  By requests over
-// the CTAs that a head can have: 28 of them (256 requests of 400 to 512 tokens, 16 heads) 40.5 us the call with 64 a CTA, 37.6 with the other kernel;
-// 40 (128 heads) 45.3, 43.4; 50 (200 of 1000 to 2048, 32 heads) 67.5, 70.2, with 128 a CTA 72.5; 125 (250 of up to 600, 64 heads) 70.6 and, with 128,
-// 62.8, against 69.8; 228 (2048 of 100 to 128, 16 heads) 127, 109.5, 110.1.
+// the CTAs that a head can have: 28 of them (256 requests of 400 to 512 tokens, 16 heads) 37.7 us the call with 64 a CTA, 37.5 with the other kernel;
+// 37 (150 of 100 to 2000, 32 heads) 51.3, 51.1; 44 (400 of 400 to 512, 16 heads) 46.5, 49.0; 50 (200 of 1000 to 2048, 32 heads) 64.6, 69.7, and
+// with 128 a CTA five more; 125 (250 of up to 600, 64 heads) 55.6 with 128, 69.8.
 int decode8_join_rows(int B, int h) {
     const long long ctas_a_head = std::max(1, kDecMaxCtas / h);
-    return B <= 48 * ctas_a_head ? 0 : B <= 64 * ctas_a_head ? 64 : 128;
+    return B <= 40 * ctas_a_head ? 0 : B <= 64 * ctas_a_head ? 64 : 128;
 }
 int launch_decode8_join(const void* w, const AttnDecodeArgs& a, int gap, int n_rows, void* out, float* lse, cudaStream_t stream) {
     const uint64_t w_row = static_cast<uint64_t>(a.h) * (kDn + kDv), out_row = static_cast<uint64_t>(a.h) * kDv;
