@@ -32,7 +32,7 @@
 // heads, 44.5 us (this kernel 35; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, 75.9 us (62; 3.35 K clocks a tile, HBM's rate
 // too, and 5 K for each switch of request); 8 of up to 65536, 128 heads, 129 us, in long runs, at the card's power limit, 149 (125; 4.1 K clocks a tile
 // against 2.9 K of MMAs: two tiles are in flight, and a slab's life -- load 1.8 K, scores, softmax 2.4 K, values 1.6 K -- is more than twice that);
-// 250 of up to 600, 64 heads, 69.5 us (49; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
+// 250 of up to 600, 64 heads, 67.4 us (48; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
 #pragma once
 #include "attn_decode_sm100.cuh"
 #include "cache8_sm100.cuh"
