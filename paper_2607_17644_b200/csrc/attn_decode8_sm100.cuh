@@ -34,6 +34,7 @@
 // against 2.9 K of MMAs: two tiles are in flight, and a slab's life -- load 1.8 K, scores, softmax 2.4 K, values 1.6 K -- is more than twice that);
 // 250 of up to 600, 64 heads, 67.4 us (48; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
 #pragma once
+#include "armed_ring.cuh"
 #include "attn_decode_sm100.cuh"
 #include "cache8_sm100.cuh"
 
@@ -300,6 +301,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         Decode8Cursor cur(args, kGap, my_units, first_b, first_t);
         fetch_pages(cur, pages);
         uint32_t slot = kBegin, par = 0, pieces = 0, T = 0;
+        ArmedRing<L::kScales> armed_scales;                  // (tile T's, in the lane that has them)
         bool new_piece = true, ok = true;
         // a piece's queries behind its first loads: they wait for the last scores of the piece before (the first are the score warp's)
         auto piece_queries = [&](int b) -> bool {
@@ -316,7 +318,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             next.next(args);
             fetch_pages(next, pages_next);
             const int boxes = (cur.valid() + kBox - 1) / kBox, row0 = (cur.t * kD8Unit) & in_page;       // boxes of this tile that hold a key
-            float* scales = reinterpret_cast<float*>(smem + L::kScale) + (T % L::kScales) * kD8Keys;
+            float* scales = reinterpret_cast<float*>(smem + L::kScale) + armed_scales.at() * kD8Keys;
             bool all_there = true;
 #pragma unroll
             for (int i = 0; i < kSubs; ++i) all_there = all_there && static_cast<uint32_t>(pages[i]) < static_cast<uint32_t>(n_pages);
@@ -358,8 +360,9 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                         for (int k = 0; k < boxes * kBox; ++k) scales[k] = 1.0f;
                         fence_async_shared();
                     }
-                    uint64_t* c_bar = &c_full[T % L::kScales];
+                    uint64_t* c_bar = &c_full[armed_scales.at()];
                     mbar_arrive_expect_tx(c_bar, there * (kBox * 4));
+                    armed_scales.arm();
 #pragma unroll
                     for (int i = 0; i < kSubs; ++i)
                         if (i < boxes && pages[i] < n_pages)
@@ -394,7 +397,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 }
             }
             if (kFirst) {
-                for (uint32_t k = 1; k <= L::kScales && k <= T; ++k) mbar_wait_quiesce(&c_full[(T - k) % L::kScales], ((T - k) / L::kScales) & 1u);
+                armed_scales.last_phases([&](uint32_t i, uint32_t parity) { mbar_wait_quiesce(&c_full[i], parity); });
                 if (pieces > 0) mbar_wait_quiesce(q_full, (pieces - 1) & 1u);
             }
         }
