@@ -109,7 +109,7 @@ bwd_delta_kernel(const __nv_bfloat16* __restrict__ out, const __nv_bfloat16* __r
 // shared by every head, so its gradient is the sum over the head shard).  The dK/dV kernel adds each
 // head's columns into an fp32 accumulator with atomics; this kernel rounds the sums to bf16.
 __global__ void __launch_bounds__(256)
-bwd_dkpe_convert_kernel(const float* __restrict__ dkpe_acc, int S, __nv_bfloat16* __restrict__ dk_pe) {
+bwd_dkpe_convert_kernel(const float* dkpe_acc, int S, __nv_bfloat16* __restrict__ dk_pe) {
     // Launched behind the dQ kernel, whose output it does not touch: what it reads is complete once the dQ
     // kernel's CTAs have passed THEIR dependency wait (they signal their dependents only after it), so it starts
     // beside them and, like the delta kernel, waits at its end.  The sums were written by another grid's atomics:
@@ -128,7 +128,7 @@ bwd_dkpe_convert_kernel(const float* __restrict__ dkpe_acc, int S, __nv_bfloat16
 
 // Deterministic alternative to the atomics: sum the per-head buffers in head order.
 __global__ void __launch_bounds__(256)
-bwd_dkpe_reduce_kernel(const float* __restrict__ dk_rope, int S, int h, __nv_bfloat16* __restrict__ dk_pe) {
+bwd_dkpe_reduce_kernel(const float* dk_rope, int S, int h, __nv_bfloat16* __restrict__ dk_pe) {
     grid_launch_dependents();
     grid_dependency_wait();
     const size_t idx = static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;

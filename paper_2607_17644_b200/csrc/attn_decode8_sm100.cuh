@@ -108,7 +108,7 @@ struct AttnDecode8Smem {
 struct AttnDecode8Args {
     AttnDecodeArgs d;
     Cache8 cache;
-    const float* q_scale;              // [B][h_pad]
+    const float* q_scale;              // [B][h_pad]; written by the kernel before, which may still run when this one starts: no load of constants (here and in the joins)
 };
 
 // Where the line's units lie.  A request with tokens begins with a gap as long as what its switch costs -- queries, a tile without references, the accumulator
@@ -528,7 +528,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
         auto wait_for_group = [&]() -> bool { return mbar_wait_warp(&group_bar[g], meetings++ & 1u, abort_flag, args.status, 0x87); };
         Decode8Cursor cur(args, kGap, my_units, first_b, first_t);
         auto query_scale = [&](const Decode8Cursor& c) -> float {
-            return tid < n_live && !c.done() ? __ldg(all.q_scale + static_cast<size_t>(c.b) * args.h_pad + head0 + h0 + tid) * args.scale_log2 : 0.f;
+            return tid < n_live && !c.done() ? all.q_scale[static_cast<size_t>(c.b) * args.h_pad + head0 + h0 + tid] * args.scale_log2 : 0.f;
         };
         grid_dependency_wait();
         float factor = query_scale(cur);
@@ -1168,7 +1168,7 @@ struct Decode8JoinSmem {
 };
 __global__ void __launch_bounds__(kJoinThreads, 1)
 decode8_join_kernel(const __grid_constant__ CUtensorMap tmap_wv, const __grid_constant__ CUtensorMap tmap_out, float* part_o,
-                    const float2* __restrict__ part_ml, const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad,
+                    const float2* part_ml, const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad,
                     int ctas_per_group, int gap, int n_rows, float* __restrict__ lse, unsigned* status) {
     using L = Decode8JoinSmem;
     extern __shared__ __align__(1024) uint8_t smem[];

@@ -770,10 +770,12 @@ struct DecodeProjectSmem {
     static constexpr int kTotalBytes = kBar + 48;
 };
 static_assert(DecodeProjectSmem::kTotalBytes <= 232448 && DecodeProjectSmem::kBar % 8 == 0, "projection kernel's shared memory");
+// (part_o and part_ml are not __restrict__: what the kernel before writes while this one starts must not be loaded as constants, which CUDA allows only of
+// memory that nobody writes as long as the kernel lives.)
 // kTurned: the pieces hold latent 128 c + l at 4 l + c.  The order of a product's terms is free: the weights' rows are loaded in it.
 template <bool kTurned>
 __global__ void __launch_bounds__(kProjectThreads, 1)
-decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
+decode_project_kernel(const __grid_constant__ CUtensorMap tmap_wv, const float* part_o, const float2* part_ml,
                       const int* __restrict__ seq_lens, int columns, int page_shift, int B, int h, int h_pad, int ctas_per_group, int line_gap,
                       int tile_requests, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, unsigned* status) {
     using L = DecodeProjectSmem;

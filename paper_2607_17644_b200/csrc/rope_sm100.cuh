@@ -501,7 +501,7 @@ latent_norm_rope_bwd_kernel(const LatentNormRopeBwdArgs a) {
 // flight at once: the kernel is one round trip to L2), added in a fixed order.  Columns [0, D) are dgamma, [D, 2D) dbeta
 // (dropped when dbeta is null).
 __global__ void __launch_bounds__(1024)
-latent_norm_sums_kernel(const float* __restrict__ partial, int n_blocks, int D, float* dgamma, float* dbeta) {
+latent_norm_sums_kernel(const float* partial, int n_blocks, int D, float* dgamma, float* dbeta) {
     __shared__ float part[32][33];
     grid_dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
