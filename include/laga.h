@@ -308,7 +308,9 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
  *   the rotated queries are carried in two e4m3 parts each, over a power of two for each request and head (together 2^-8 of a channel, half a
  *   step of bf16).  So are the weights, each the probability times the token's scale (2^-8, over 32 heads 2^-7 of it), at a reference that each
  *   tile of 128 keys is held to: besides, a weight may be off by 2^-12 of its tile's largest (over 32 heads 2^-10), so that smaller ones may be
- *   lost.  Sums, references and the accumulator are fp32.
+ *   lost.  Not beside a few that stand far above all others, by 2^11 (over 32 heads 2^10) or more: up to two tokens of 32 neighbours, where the tile (the
+ *   first of a request has its first tokens) has 32 others without such a one, are computed apart, in fp32, and the rest is held relative to its
+ *   own largest (2^40 below them at most).  Sums, references and the accumulator are fp32.
  */
 int laga_cache8_append(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps, const int* positions,
                        const double* freqs, int M, int layout, float mscale, void* cache, int n_pages, int page_size, const int* slots,

@@ -13,8 +13,9 @@
 //     y_t = score_t log2(e) + log2 s_t,   P_t = 2^(y_t - m),   O = sum P_t code_t,   l = sum P_t / s_t,   out = O / l
 // What e4m3 can hold of P is 2^17, so the reference m is kept near the tile's maximum of y, both ways: where a tile's lies outside [m, m + 11]
 // it becomes that maximum less 7 (never more than 2^40 below its highest: what came before is then all that counts, and the
-// accumulator must not overflow), and O and l are rescaled.  Weights of 2^-12 of a tile's largest are kept, and typically
-// of 2^-19.
+// accumulator must not overflow), and O and l are rescaled.  Up to 32 heads a CTA weights are held to 2^-12 of a tile's largest, and typically to
+// 2^-19; with 64, to 2^-10 and 2^-17 (and, as e5m2 reaches further, to 2^-3 of themselves down to 2^-14 and 2^-21).  A few that stand far above all others
+// are no part of P (kD8Places).
 //
 // Scores are computed the other way round from the bf16 kernel, S^T[128 keys x (hi, lo columns of the heads)] = K (A) . Q^T (B): the long
 // operand is read from shared memory once for both parts, a thread has all 16 heads' scores of one key, so no reduction is on
@@ -45,6 +46,19 @@ constexpr int kD8Unit = kDecKeys;            // keys of a unit of the line: a ti
 constexpr float kD8Lift = 7.0f;              // where a tile's maximum is put ...
 constexpr float kD8High = 11.0f;             // ... and the most it may become; the least is 0
 constexpr float kD8Fall = 40.0f;
+// Weights that stand apart.  What P can hold is relative to its tile's largest weight, so that a token with a large key (and with it a large scale), a high score and
+// a small value, as they are found where a context begins, would drown its neighbours: with 13 nats between them and 2^7 between the scales, all 127 of them.
+// So a key that is more than 2^kApart above the rest of its tile is no part of P: the reference is put where the rest needs it, the key's d are kept in the
+// piece's place of the workspace, which is written only when the piece ends, and before the accumulator is drained the token's codes are fetched from the cache
+// once more and multiplied in fp32.  The reference goes down no further than 2^kD8Fall below what is left out.
+// Which: in a piece's first tile, keys of one warp (32 neighbours) where no other warp has anything near; in a later one, keys that far above the window.  Of each
+// warp kD8Places in a piece at most; where there are more, the tile's largest weight sets the reference as it does otherwise.
+// A tile with some costs about 2 us, meetings and latencies (one request of 511 tokens 16.3 -> 16.8 us, 200 of about 2000, 32 heads, a key each 75.3 -> 80, 250 of up to
+// 600, 64 heads 59 -> 68.5, 64 of up to 8192, 16 heads 42.6 -> 43.3); looking for them 0.4 us a call and 2 % where scores are flat.  (Kept per head instead of for the
+// group's heads together, at the accumulator's end by a walk over their places: 3 to 5 us a tile.  As called functions: 5 % lost where nothing stands apart.)
+constexpr int kD8Places = 2;
+constexpr int kD8Looks = 2;                  // tiles of a piece from which keys may be left out
+constexpr int kD8Place = 36;                 // words of a kept key: d of up to 16 heads, its place in the request, 1 / its scale, and m of then
 constexpr float kD8LoScale = 32.0f;
 
 // Two pairs of fp16 numbers as four codes and the codes of what is left: e4m3, and 32 times the rest; or e5m2, and the rest in e4m3.  (One block of
@@ -79,6 +93,7 @@ struct AttnDecode8Smem {
     // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (saves 4.2 us for 200 requests
     // of about 2000 tokens, 32 heads; would cost 0.7 at 64 x 8192 with 16 heads and 3.8 at 8 x 65536 with 128)
     static constexpr bool kOneCopy = kHeads == 32;
+    static constexpr float kApart = kSplit ? 11.0f : 10.0f;    // how far above the rest of its tile a weight stands that is left out of P
     static constexpr float kDrop = kSplit ? 3.0f : 0.0f;       // P = 2^(d - kDrop): at most 2^8 in e4m3 (hi and 32 times the rest), 2^11 in e5m2 and its rest
     static constexpr int kCols = kSplit ? 2 * kHeads : kHeads; // TMEM columns of 128 latents of O^T
     static constexpr int kPRow = kSplit ? 2 * kHeads : kHeads; // bytes of a key's row of P
@@ -96,8 +111,8 @@ struct AttnDecode8Smem {
     static constexpr int kP = kQ + 5 * kQSlab;                 // two buffers, or the two parts
     static constexpr int kSlab0 = kP + 2 * kPTile;
     static constexpr int kScale = kSlab0 + kSlabs * kSlab;
-    static constexpr int kRef = kScale + kScales * kD8Keys * 4;    // per head: m; query factor, step of m and its power, tile maximum (the last four: a piece's sums, a row a warp)
-    static constexpr int kVote = kRef + 5 * kHeads * 4;            // [2][groups][4 warps]
+    static constexpr int kRef = kScale + kScales * kD8Keys * 4;    // per head: m; query factor, step of m and its power, tile maximum (these four: a piece's sums, a row a warp); maximum of the rest
+    static constexpr int kVote = kRef + 6 * kHeads * 4;            // [2][groups][4 warps]
     static constexpr int kBar = kVote + 2 * kGroups * 16;
     static constexpr int kBars = 2 * kSlabs + 12 + kScales + kGroups;
     static constexpr int kMisc = kBar + kBars * 8;             // TMEM slot, abort flag, start, scan
@@ -200,7 +215,11 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
     int* scan = start_b + 2;                          // per-warp sums of the unit counts
     float* ref_s = reinterpret_cast<float*>(smem + L::kRef);
     float *factor_s = ref_s + kHeads, *step_s = factor_s + kHeads, *alpha_s = step_s + kHeads;
-    int* top_s = reinterpret_cast<int*>(alpha_s + kHeads);
+    int *top_s = reinterpret_cast<int*>(alpha_s + kHeads), *rest_s = top_s + kHeads;
+    float* most_s = step_s;                           // [4 warps][kHeads], in a piece's first tile before the four have their values
+    // once the stretch is found: keys that each softmax warp has left out of P in this piece; for each group, how many of its tiles something stands apart in
+    // (upper half), and for which heads of this one
+    int *took_s = scan, *apart_s = scan + L::kSoftWarps;
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int group = static_cast<int>(blockIdx.x) % args.n_groups;
@@ -542,8 +561,10 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 if (tid < kPer) {
                     factor_s[h0 + tid] = factor;
                     ref_s[h0 + tid] = tid < n_live ? 0.f : 1e30f;        // (a head that is none: every weight zero, and no rescaling for it)
-                    top_s[h0 + tid] = kOrderedLowest;
+                    rest_s[h0 + tid] = kOrderedLowest;
                 }
+                if (lane == 0) took_s[warp] = 0;
+                if (tid == 0) apart_s[g] = 0;
                 seen = false;
                 peak = kDecLowest;
                 arrive();
@@ -657,24 +678,109 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     tops[2 * i + 1] = v.y;
                 }
                 const float most = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
-                if ((lane & (kShare - 1)) == 0) atomicMax(&top_s[h0 + lane / kShare], ordered(most));
-                arrive();
-                ok = wait_for_group();
-                if (!ok) break;
-                if (tid < kPer) {
-                    const float top = unordered(top_s[h0 + tid]), m = ref_s[h0 + tid];
-                    top_s[h0 + tid] = kOrderedLowest;
-                    if (seen) peak = fmaxf(peak, m);
-                    float to = m;
-                    if (tid < n_live && top > -INFINITY && !(top >= 0.f && top <= kD8High)) to = fmaxf(m + (top - kD8Lift), peak - kD8Fall);
-                    ref_s[h0 + tid] = to;
-                    step_s[h0 + tid] = to - m;                 // (the step that was taken, with the sum's rounding)
-                    alpha_s[h0 + tid] = fast_exp2(m - to);
-                    seen = seen || top > -INFINITY;
+                if (!first) {
+                    if ((lane & (kShare - 1)) == 0) atomicMax(&top_s[h0 + lane / kShare], ordered(most));
+                } else if (valid > 32 || valid == 1 || quarter > 1) {
+                    if ((lane & (kShare - 1)) == 0) most_s[quarter * kHeads + h0 + lane / kShare] = most;
+                } else if (quarter == 0) {                     // all keys are one warp's: as if the odd ones were another's
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) {
+                            const float2 v = f2_parts(d[i]);
+                            tops[2 * i] = (lane & 1) == half ? v.x : -INFINITY;
+                            tops[2 * i + 1] = (lane & 1) == half ? v.y : -INFINITY;
+                        }
+                        const float most_half = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
+                        if ((lane & (kShare - 1)) == 0) most_s[half * kHeads + h0 + lane / kShare] = most_half;
+                    }
                 }
                 arrive();
                 ok = wait_for_group();
                 if (!ok) break;
+                bool apart = false;
+                if (tid < kPer) {
+                    const float m = ref_s[h0 + tid];
+                    float top;
+                    // Does something stand apart?  Then it is far above what the reference was for; in the first tile, one warp has it, and no other anything near it.
+                    if (first) {
+                        const float* of = most_s + h0 + tid;
+                        const float a = fmaxf(of[0], of[kHeads]), b = fmaxf(of[2 * kHeads], of[3 * kHeads]);
+                        top = fmaxf(a, b);
+                        rest_s[h0 + tid] = kOrderedLowest;
+                        apart = valid > 1 && top - fmaxf(fminf(a, b), a >= b ? fminf(of[0], of[kHeads]) : fminf(of[2 * kHeads], of[3 * kHeads])) > L::kApart;
+                    } else {
+                        top = unordered(top_s[h0 + tid]);
+                        apart = top > kD8High + L::kApart && apart_s[g] < kD8Looks << 16;
+                    }
+                    top_s[h0 + tid] = kOrderedLowest;
+                    if (seen) peak = fmaxf(peak, m);
+                    const bool given = tid < n_live && top > -INFINITY;
+                    apart = apart && given;
+                    float to = m;
+                    if (given && !apart && (first || !(top >= 0.f && top <= kD8High))) to = fmaxf(m + (top - kD8Lift), peak - kD8Fall);
+                    ref_s[h0 + tid] = to;
+                    step_s[h0 + tid] = to - m;                 // (the step that was taken, with the sum's rounding)
+                    alpha_s[h0 + tid] = apart ? top : fast_exp2(m - to);
+                    seen = seen || top > -INFINITY;
+                }
+                if (quarter == 0) {
+                    const uint32_t heads = __ballot_sync(0xffffffffu, apart);
+                    if (heads != 0u && lane == 0) apart_s[g] += 0x10000 + static_cast<int>(heads);
+                }
+                arrive();
+                ok = wait_for_group();
+                if (!ok) break;
+                const uint32_t apart_heads = static_cast<uint32_t>(apart_s[g]) & 0xffffu;        // (the same for the whole group)
+                bool may_leave = false;                        // this key is one of few that are far above all others of their warp
+                if (__builtin_expect(apart_heads != 0u, 0)) {
+                    // The largest of the rest, and the references that it asks for.
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        const float2 v = f2_parts(d[i >> 1]);
+                        tops[i] = (i & 1) ? v.y : v.x;
+                        const float limit = __shfl_sync(0xffffffffu, most, i * kShare) - L::kApart;
+                        may_leave = may_leave || ((apart_heads >> i & 1u) != 0u && tops[i] > limit);
+                    }
+                    const int held = took_s[warp];             // a bit a place
+                    const uint32_t few = __ballot_sync(0xffffffffu, may_leave);
+                    may_leave = may_leave && __popc(few) <= kD8Places - __popc(held);
+                    if (may_leave) {                           // kept for the end of the piece, if it is left out: d and m of all the group's heads, its place in the request, 1 / s
+                        const uint32_t slot = static_cast<uint32_t>(cta + cur.b);
+                        float* place = args.part_o + static_cast<size_t>(slot * args.h_pad + head0 + h0 + kPer - 1) * kDecLat +
+                                       (quarter * kD8Places + (held == 0 ? __popc(few & ((1u << lane) - 1u)) : 2 - held)) * kD8Place;
+                        if (device_check(slot < static_cast<uint32_t>(args.ctas_per_group + args.B), args.status, 0xEB0000u | cta)) {
+#pragma unroll
+                            for (int i = 0; i < kPairs; i += 2) reinterpret_cast<ulonglong2*>(place)[i >> 1] = make_ulonglong2(d[i].v, d[i + 1].v);
+                            place[16] = __int_as_float(cur.t * kD8Unit + cur.piece_keys() - keys_left + key);
+                            place[17] = __uint_as_float((254u - min(254u, __float_as_uint(s) >> 23 & 0xffu)) << 23);
+#pragma unroll 1
+                            for (int i = 0; i < kPer; ++i) place[20 + i] = ref_s[h0 + i] - step_s[h0 + i];      // (heads that do not look have taken theirs)
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) tops[i] = may_leave ? -INFINITY : tops[i];
+                    const float rest = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
+                    if ((lane & (kShare - 1)) == 0) atomicMax(&rest_s[h0 + lane / kShare], ordered(rest));
+                    arrive();
+                    ok = wait_for_group();
+                    if (!ok) break;
+                    if (apart) {
+                        const float top = alpha_s[h0 + tid], others = unordered(rest_s[h0 + tid]), m = ref_s[h0 + tid];
+                        const float aim = others > -INFINITY && top - others > L::kApart ? others : top;
+                        float to = aim >= 0.f && aim <= kD8High ? m : fmaxf(m + (aim - kD8Lift), peak - kD8Fall);
+                        to = fmaxf(to, m + (top - kD8Lift) - kD8Fall);
+                        if (top - (to - m) > kD8High) peak = fmaxf(peak, m + (top - kD8Lift));
+                        ref_s[h0 + tid] = to;
+                        step_s[h0 + tid] = to - m;
+                        alpha_s[h0 + tid] = fast_exp2(m - to);
+                    }
+                    if (tid < kPer) rest_s[h0 + tid] = kOrderedLowest;
+                    if (tid == 0) apart_s[g] &= ~0xffff;
+                    arrive();
+                    ok = wait_for_group();
+                    if (!ok) break;
+                }
                 const ulonglong2 *step = reinterpret_cast<const ulonglong2*>(step_s + h0), *alpha = reinterpret_cast<const ulonglong2*>(alpha_s + h0);
                 const F2 minus1 = f2(-1.0f, -1.0f);
 #pragma unroll
@@ -686,6 +792,21 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                         l2[i] = f2_mul(l2[i], F2{a4.x});
                         l2[i + 1] = f2_mul(l2[i + 1], F2{a4.y});
                     }
+                }
+                if (const uint32_t few = __ballot_sync(0xffffffffu, may_leave); __builtin_expect(few != 0u, 0)) {
+                    // A key that is above the window now is left out, for all of the group's heads.
+                    float largest = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        const float2 v = f2_parts(d[i]);
+                        largest = fmax3(largest, v.x, v.y);
+                    }
+                    const bool out = may_leave && largest > kD8High;
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) d[i] = out ? f2(-INFINITY, -INFINITY) : d[i];
+                    const int held = took_s[warp];
+                    const uint32_t more = __reduce_or_sync(0xffffffffu, out ? 1u << (held == 0 ? __popc(few & ((1u << lane) - 1u)) : 2 - held) : 0u);
+                    if (lane == 0) took_s[warp] = held | static_cast<int>(more);
                 }
                 if constexpr (!L::kOneCopy) weigh();
                 if (!first) {
@@ -774,6 +895,44 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 const size_t slot = static_cast<size_t>(cta) + b;
                 // (a slot past the workspace would mean that the roles disagree about the pieces)
                 const bool store = device_check(slot < static_cast<size_t>(args.ctas_per_group) + args.B, args.status, 0xEB0000u | cta);
+                const bool any_taken = store && apart_s[g] != 0;       // (or looked at, at least)
+                const float* places = args.part_o + (slot * args.h_pad + head0 + h0 + kPer - 1) * kDecLat;
+                if (__builtin_expect(any_taken, 0)) {
+                    ok = wait_for_group();
+                    if (!ok) break;
+                    // What was left out, in a fixed order: the token's codes from the cache once more, into the accumulator of each head.
+#pragma unroll 1
+                    for (int k = 0; k < 4 * kD8Places; ++k) {
+                        if ((took_s[g * 4 + k / kD8Places] >> k % kD8Places & 1) == 0) continue;
+                        const float* place = places + k * kD8Place;
+                        auto weight = [&](int i) { return fast_exp2(place[i] + place[20 + i] - (ref_s[h0 + i] + L::kDrop)); };
+                        if (tid < n_live) lsum_s[h0 + tid] += weight(tid) * place[17];
+                        __syncwarp();
+                        const int at = __float_as_int(place[16]);
+                        if (static_cast<uint32_t>(at) >= static_cast<uint32_t>(args.columns) << args.page_shift) continue;       // (checked, not trusted)
+                        const int page = __ldg(args.block_table + static_cast<size_t>(b) * args.columns + (at >> args.page_shift));
+                        if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(args.n_pages)) continue;        // (zeros)
+                        const int token = (page << args.page_shift) | (at & ((1 << args.page_shift) - 1));
+                        const uint8_t* row = all.cache.row(token) + key;
+                        float codes[4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) codes[c] = float2_of_half2(half2_of_e4m3x2(row[c * 128])).x;
+#pragma unroll 1
+                        for (int i = 0; i < kPer; ++i) {
+                            const float w = weight(i);
+                            uint32_t o[4];
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) tmem_ld_x1(col_o + c * L::kCols + i, &o[c]);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) tmem_st_x1(col_o + c * L::kCols + i, __float_as_uint(fmaf(w, codes[c], __uint_as_float(o[c]))));
+                        }
+                        tmem_st_wait();                        // (the next key reads them)
+                    }
+                    arrive();                                  // (the places are read by all before they are written over)
+                    ok = wait_for_group();
+                    if (!ok) break;
+                }
                 // A head's 512 latents in the order that a thread has them in, latent 128 c + l at 4 l + c: 16 bytes a store, 512 of a warp side by side.
                 float4* dst = reinterpret_cast<float4*>(args.part_o + (slot * args.h_pad + head0 + h0) * kDecLat) + key;
 #pragma unroll 1
@@ -800,7 +959,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     for (int v = 0; v < 8; ++v)
                         if (store && v0 + v < n_live) dst[(v0 + v) * (kDecLat / 4)] = make_float4(x[v][0], x[v][1], x[v][2], x[v][3]);
                 }
-                if (!wait_for_group()) break;
+                if (!any_taken && !wait_for_group()) break;
                 if (store && tid < n_live) {
                     const float l = ((lsum_s[h0 + tid] + lsum_s[kHeads + h0 + tid]) + lsum_s[2 * kHeads + h0 + tid]) + lsum_s[3 * kHeads + h0 + tid];
                     // (no weight at all: nothing that another piece's reference should be compared with)
