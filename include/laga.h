@@ -295,7 +295,7 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
  * Format.  A page of n tokens is n * 644 bytes: n rows of 640 e4m3 codes (512 of the normalised latent, 64 of the rotated key, 64 of what
  * the key's first codes left), then the n rows' scales in fp32.  latent = scale * code, key = scale * (code + second code).  The scale is
  * the smallest power of two, 2^-32 at least, with which no channel exceeds 448 scale, and each code the nearest (ties to even): a latent
- * channel is off by at most 2^-4 of itself, a key channel by 2^-8, and by 2^-10 of the scale where they are smaller than 2^-6 of it.
+ * channel is off by at most 2^-4 of itself or 2^-10 of the scale, a key channel by 2^-8 of itself or 2^-10 of the scale, whichever is more.
  * A token with a channel that is not finite is NaN in all of them.  Pages, slots, tables and lengths are those of the bf16 cache
  * (laga_cache_plan makes them); the cache is 16-byte aligned, page_size a power of two from 16 to 1024, n_pages * page_size at most 2^30.
  *
@@ -305,8 +305,8 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
  *   k_pe; zeros where a slot is outside the cache.  Slots may repeat.
  * laga_paged_decode8: laga_paged_decode over such a cache, with its arguments, limits, errors and results, and a workspace of its own size.  A
  *   scale must be a power of two from 2^-32 on, or zero in a row whose codes are zeros (a page that was cleared: a row of zeros).  q W_uk and
- *   the rotated queries are carried in two e4m3 parts each, over a power of two for each request and head (together 2^-8 of a channel, half a
- *   step of bf16).  So are the weights, each the probability times the token's scale (2^-8, over 32 heads 2^-7 of it), at a reference that each
+ *   the rotated queries are carried in two e4m3 parts each, over a power of two for each request and head that brings the largest within 448 (together
+ *   2^-8 of a channel, half a step of bf16, or 2^-10 of that power, whichever is more).  So are the weights, each the probability times the token's scale (2^-8, over 32 heads 2^-7 of it), at a reference that each
  *   tile of 128 keys is held to: besides, a weight may be off by 2^-12 of its tile's largest (over 32 heads 2^-10), so that smaller ones may be
  *   lost.  Not beside a few that stand far above all others, by 2^11 (over 32 heads 2^10) or more: up to two tokens of 32 neighbours, where the tile (the
  *   first of a request has its first tokens) has 32 others without such a one, are computed apart, in fp32, and the rest is held relative to its

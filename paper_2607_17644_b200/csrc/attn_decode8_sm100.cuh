@@ -4,7 +4,7 @@
 // The codes are never widened: they go from the cache to shared memory by TMA and from there to the tensor cores (kind::f8f6f4) as
 // they are.  What multiplies them is brought to 8 bits instead, in two parts each, which together hold as much as a bf16 number:
 //   queries        q_lat / r = hi + lo, both e4m3, with a power of two r per (request, head): off by at most 2^-4 * 2^-4 = 2^-8 of a
-//                  channel, half a step of bf16.  The key's 64 channels multiply both the key's codes and their rests.
+//                  channel, half a step of bf16, or 2^-10 r (the largest channel is 224 r or more).  The key's 64 channels multiply both the key's codes and their rests.
 //   probabilities  p / 2^m = hi + lo likewise.  Up to 32 heads a CTA the parts are columns of one MMA (hi e4m3, lo 32 times the rest
 //                  in e4m3); with 64 heads TMEM has no room for those columns, so that lo is a second MMA into the same accumulator,
 //                  cannot be scaled, and hi is e5m2, whose range is wide enough for the weights of which lo keeps nothing (2^-7).

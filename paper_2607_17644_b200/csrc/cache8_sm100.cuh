@@ -4,8 +4,8 @@
 //     s = the smallest power of two, 2^-32 at least, such that no channel exceeds 448 s     (448: the largest e4m3 number)
 // it is held as codes, latent e4m3(x / s), key e4m3(k / s), and what the key's rounding left, e4m3(k / s - first code): read back as
 // x = s code, k = s (code + second code).  e4m3 has four binary digits: a latent channel is off by at most 2^-4 of itself, a key
-// channel by at most 2^-8, half a step of bf16: scores lie on the key's positions, and 64 of 576 channels cost little.  Channels below
-// 2^-6 s are held to 2^-10 s.  s is a power of two because nothing is gained by another (the codes are floating) and everything that
+// channel by at most 2^-8, half a step of bf16: scores lie on the key's positions, and 64 of 576 channels cost little.  Where that is less than 2^-10 s -- a
+// latent channel below 2^-6 s, a key channel below 2^-2 s -- they are held to 2^-10 s.  s is a power of two because nothing is gained by another (the codes are floating) and everything that
 // multiplies by it stays exact; one s for latent and key, so that a score is one product of codes.  One s a token, because a token
 // that joins a page must not change those that are there.  A token with a channel that is not finite has s = NaN: all of it reads as NaN.
 //
@@ -138,6 +138,8 @@ cache8_append_kernel(const Cache8AppendArgs a) {
         }
         float most = largest3(largest3(k2[0].x, k2[0].y, k2[1].x), k2[1].y, 0.f);
         const float2 sqs = f2_parts(sq);
+        // (rsqrtf is off by 2^-22 at most and each product by 2^-24, as the sums are: some 2^-18 of the codes, whose steps are 2^-4 to 2^-3 of them, fall to the
+        // neighbour of the one that exact arithmetic gives)
         const float rstd = rsqrtf(half_warp_sum(sqs.x + sqs.y) * (1.0f / kC8Lat) + a.eps);
         const F2 scale = f2(rstd, rstd);
 #pragma unroll

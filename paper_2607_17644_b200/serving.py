@@ -32,7 +32,7 @@ class LatentCache:
     """n_pages pages of page_size tokens (a power of two from 16 to 1024) in each of n_layers layers; n_requests rows, each with
     room for max_tokens tokens (in whole pages: a plan takes up to ceil(max_tokens / page_size) * page_size).
     bits: 16, ``pages[layer]`` bf16 [n_pages, page_size, 576], or 8, uint8 [n_pages, page_size * 644]: 1.8 times the tokens in the same
-    memory; a latent channel is held to 2^-4 of itself, a key channel to 2^-8.  ``LagaBlock`` takes either."""
+    memory; a latent channel is held to 2^-4 of itself, a key channel to 2^-8, and either to 2^-10 of the token's scale.  ``LagaBlock`` takes either."""
 
     ROW = 576
 
