@@ -138,8 +138,8 @@ cache8_append_kernel(const Cache8AppendArgs a) {
         }
         float most = largest3(largest3(k2[0].x, k2[0].y, k2[1].x), k2[1].y, 0.f);
         const float2 sqs = f2_parts(sq);
-        // (rsqrtf is off by 2^-22 at most and each product by 2^-24, as the sums are: some 2^-18 of the codes, whose steps are 2^-4 to 2^-3 of them, fall to the
-        // neighbour of the one that exact arithmetic gives)
+        // (rsqrtf and the products after it: of 33.5 million codes 37 to 43 are the neighbours of those that exact arithmetic gives; with a root and a division
+        // in fp32, 36 to 45)
         const float rstd = rsqrtf(half_warp_sum(sqs.x + sqs.y) * (1.0f / kC8Lat) + a.eps);
         const F2 scale = f2(rstd, rstd);
 #pragma unroll
