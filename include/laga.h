@@ -305,12 +305,13 @@ int laga_paged_decode(const void* q, const void* w_kv_b, const void* cache, int 
  *   k_pe; zeros where a slot is outside the cache.  Slots may repeat.
  * laga_paged_decode8: laga_paged_decode over such a cache, with its arguments, limits, errors and results, and a workspace of its own size.  A
  *   scale must be a power of two from 2^-32 on, or zero in a row whose codes are zeros (a page that was cleared: a row of zeros).  q W_uk and
- *   the rotated queries are carried in two e4m3 parts each, over a power of two for each request and head that brings the largest within 448 (together
- *   2^-8 of a channel, half a step of bf16, or 2^-10 of that power, whichever is more).  So are the weights, each the probability times the token's scale (2^-8, over 32 heads 2^-7 of it), at a reference that each
- *   tile of 128 keys is held to: besides, a weight may be off by 2^-12 of its tile's largest (over 32 heads 2^-10), so that smaller ones may be
- *   lost.  Not beside a few that stand far above all others, by 2^11 (over 32 heads 2^10) or more: up to two tokens of 32 neighbours, where the tile (the
- *   first of a request has its first tokens) has 32 others without such a one, are computed apart, in fp32, and the rest is held relative to its
- *   own largest (2^40 below them at most).  Sums, references and the accumulator are fp32.
+ *   the rotated queries are carried in two e4m3 parts each, over a power of two for each request and head that brings the largest within 448
+ *   (together 2^-8 of a channel, half a step of bf16, or 2^-10 of that power, whichever is more).  So are the weights, each the probability
+ *   times the token's scale (2^-8, over 32 heads 2^-7 of it), at a reference that each tile of 128 keys is held to: besides, a weight may be
+ *   off by 2^-12 of its tile's largest (over 32 heads 2^-10), so that smaller ones may be lost.  Not beside a few that stand far above all
+ *   others, by 2^11 (over 32 heads 2^10) or more: up to four tokens of 32 neighbours, where half of the tile's runs of 32 have none, are
+ *   computed apart, in fp32, and the rest is held relative to its own largest (2^40 below them at most; a request's first tile has its first
+ *   tokens). Sums, references and the accumulator are fp32.
  */
 int laga_cache8_append(const void* kv_a, long long kv_a_pitch, const void* gamma, const void* beta, float eps, const int* positions,
                        const double* freqs, int M, int layout, float mscale, void* cache, int n_pages, int page_size, const int* slots,

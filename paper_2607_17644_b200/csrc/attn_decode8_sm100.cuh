@@ -51,12 +51,13 @@ constexpr float kD8Fall = 40.0f;
 // So a key that is more than 2^kApart above the rest of its tile is no part of P: the reference is put where the rest needs it, the key's d are kept in the
 // piece's place of the workspace, which is written only when the piece ends, and before the accumulator is drained the token's codes are fetched from the cache
 // once more and multiplied in fp32.  The reference goes down no further than 2^kD8Fall below what is left out.
-// Which: in a piece's first tile, keys of one warp (32 neighbours) where no other warp has anything near; in a later one, keys that far above the window.  Of each
-// warp kD8Places in a piece at most; where there are more, the tile's largest weight sets the reference as it does otherwise.
+// Which: in a piece's first tile, keys of some warps (32 neighbours each) where as many others have nothing near (of a tile with three warps' keys, or two,
+// one other; with one's, every fourth key counts as another's); in a later one, keys that far above the window.  Of each warp kD8Places in a piece at
+// most; where there are more, the tile's largest weight sets the reference as it does otherwise.
 // A tile with some costs about 2 us, meetings and latencies (one request of 511 tokens 16.3 -> 16.8 us, 200 of about 2000, 32 heads, a key each 75.3 -> 80, 250 of up to
 // 600, 64 heads 59 -> 68.5, 64 of up to 8192, 16 heads 42.6 -> 43.3); looking for them 0.4 us a call and 2 % where scores are flat.  (Kept per head instead of for the
 // group's heads together, at the accumulator's end by a walk over their places: 3 to 5 us a tile.  As called functions: 5 % lost where nothing stands apart.)
-constexpr int kD8Places = 2;
+constexpr int kD8Places = 4;
 constexpr int kD8Looks = 2;                  // tiles of a piece from which keys may be left out
 constexpr int kD8Place = 36;                 // words of a kept key: d of up to 16 heads, its place in the request, 1 / its scale, and m of then
 constexpr float kD8LoScale = 32.0f;
@@ -117,6 +118,7 @@ struct AttnDecode8Smem {
     static constexpr int kBars = 2 * kSlabs + 12 + kScales + kGroups;
     static constexpr int kMisc = kBar + kBars * 8;             // TMEM slot, abort flag, start, scan
     static constexpr int kTotalBytes = kMisc + 16 + 4 * (kThreads / 32);
+    static_assert(4 * kD8Places * kD8Place <= 2 * 512, "what is left out does not fit two heads of a piece");
     static_assert(kTotalBytes <= 232448 && kSlab0 % 1024 == 0 && kP % 1024 == 0 && kVote % 16 == 0 && kBar % 8 == 0, "decode kernel's shared memory");
 };
 
@@ -545,6 +547,11 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
             if (lane == 0) mbar_arrive(&group_bar[g]);
         };
         auto wait_for_group = [&]() -> bool { return mbar_wait_warp(&group_bar[g], meetings++ & 1u, abort_flag, args.status, 0x87); };
+        auto place_of = [&](int held, uint32_t few) -> int {   // of the warp's places that are not held, this lane's
+            uint32_t left = ~static_cast<uint32_t>(held);
+            for (uint32_t before = few & ((1u << lane) - 1u); before != 0u; before &= before - 1u) left &= left - 1u;
+            return __ffs(static_cast<int>(left)) - 1;
+        };
         Decode8Cursor cur(args, kGap, my_units, first_b, first_t);
         auto query_scale = [&](const Decode8Cursor& c) -> float {
             return tid < n_live && !c.done() ? all.q_scale[static_cast<size_t>(c.b) * args.h_pad + head0 + h0 + tid] * args.scale_log2 : 0.f;
@@ -680,19 +687,19 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 const float most = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
                 if (!first) {
                     if ((lane & (kShare - 1)) == 0) atomicMax(&top_s[h0 + lane / kShare], ordered(most));
-                } else if (valid > 32 || valid == 1 || quarter > 1) {
+                } else if (valid > 32 || valid == 1) {
                     if ((lane & (kShare - 1)) == 0) most_s[quarter * kHeads + h0 + lane / kShare] = most;
-                } else if (quarter == 0) {                     // all keys are one warp's: as if the odd ones were another's
+                } else if (quarter == 0) {                     // all keys are one warp's: as if every fourth were another's
 #pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {
+                    for (int c = 0; c < 4; ++c) {
 #pragma unroll
                         for (int i = 0; i < kPairs; ++i) {
                             const float2 v = f2_parts(d[i]);
-                            tops[2 * i] = (lane & 1) == half ? v.x : -INFINITY;
-                            tops[2 * i + 1] = (lane & 1) == half ? v.y : -INFINITY;
+                            tops[2 * i] = (lane & 3) == c ? v.x : -INFINITY;
+                            tops[2 * i + 1] = (lane & 3) == c ? v.y : -INFINITY;
                         }
-                        const float most_half = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
-                        if ((lane & (kShare - 1)) == 0) most_s[half * kHeads + h0 + lane / kShare] = most_half;
+                        const float most_c = warp_reduce_each(tops, lane, [](float x, float y) { return fmaxf(x, y); });
+                        if ((lane & (kShare - 1)) == 0) most_s[c * kHeads + h0 + lane / kShare] = most_c;
                     }
                 }
                 arrive();
@@ -705,10 +712,11 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     // Does something stand apart?  Then it is far above what the reference was for; in the first tile, one warp has it, and no other anything near it.
                     if (first) {
                         const float* of = most_s + h0 + tid;
-                        const float a = fmaxf(of[0], of[kHeads]), b = fmaxf(of[2 * kHeads], of[3 * kHeads]);
-                        top = fmaxf(a, b);
+                        const float a = fmaxf(of[0], of[kHeads]), b = fmaxf(of[2 * kHeads], of[3 * kHeads]), u = fminf(a, b),
+                                    v = fmaxf(fminf(of[0], of[kHeads]), fminf(of[2 * kHeads], of[3 * kHeads]));
+                        top = fmaxf(a, b);                     // of the warps' maxima; behind it the larger of u and v, then the smaller
                         rest_s[h0 + tid] = kOrderedLowest;
-                        apart = valid > 1 && top - fmaxf(fminf(a, b), a >= b ? fminf(of[0], of[kHeads]) : fminf(of[2 * kHeads], of[3 * kHeads])) > L::kApart;
+                        apart = valid > 1 && top - (valid > 64 || (valid >= 4 && valid <= 32) ? fminf(u, v) : fmaxf(u, v)) > L::kApart;
                     } else {
                         top = unordered(top_s[h0 + tid]);
                         apart = top > kD8High + L::kApart && apart_s[g] < kD8Looks << 16;
@@ -747,8 +755,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                     may_leave = may_leave && __popc(few) <= kD8Places - __popc(held);
                     if (may_leave) {                           // kept for the end of the piece, if it is left out: d and m of all the group's heads, its place in the request, 1 / s
                         const uint32_t slot = static_cast<uint32_t>(cta + cur.b);
-                        float* place = args.part_o + static_cast<size_t>(slot * args.h_pad + head0 + h0 + kPer - 1) * kDecLat +
-                                       (quarter * kD8Places + (held == 0 ? __popc(few & ((1u << lane) - 1u)) : 2 - held)) * kD8Place;
+                        float* place = args.part_o + static_cast<size_t>(slot * args.h_pad + head0 + h0 + kPer - 2) * kDecLat + (quarter * kD8Places + place_of(held, few)) * kD8Place;
                         if (device_check(slot < static_cast<uint32_t>(args.ctas_per_group + args.B), args.status, 0xEB0000u | cta)) {
 #pragma unroll
                             for (int i = 0; i < kPairs; i += 2) reinterpret_cast<ulonglong2*>(place)[i >> 1] = make_ulonglong2(d[i].v, d[i + 1].v);
@@ -805,7 +812,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) d[i] = out ? f2(-INFINITY, -INFINITY) : d[i];
                     const int held = took_s[warp];
-                    const uint32_t more = __reduce_or_sync(0xffffffffu, out ? 1u << (held == 0 ? __popc(few & ((1u << lane) - 1u)) : 2 - held) : 0u);
+                    const uint32_t more = __reduce_or_sync(0xffffffffu, out ? 1u << place_of(held, few) : 0u);
                     if (lane == 0) took_s[warp] = held | static_cast<int>(more);
                 }
                 if constexpr (!L::kOneCopy) weigh();
@@ -896,7 +903,7 @@ attn_decode8_sm100_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gr
                 // (a slot past the workspace would mean that the roles disagree about the pieces)
                 const bool store = device_check(slot < static_cast<size_t>(args.ctas_per_group) + args.B, args.status, 0xEB0000u | cta);
                 const bool any_taken = store && apart_s[g] != 0;       // (or looked at, at least)
-                const float* places = args.part_o + (slot * args.h_pad + head0 + h0 + kPer - 1) * kDecLat;
+                const float* places = args.part_o + (slot * args.h_pad + head0 + h0 + kPer - 2) * kDecLat;
                 if (__builtin_expect(any_taken, 0)) {
                     ok = wait_for_group();
                     if (!ok) break;
