@@ -29,11 +29,15 @@
 //   then four warps: TMA producer of the latent's last two slabs; value MMAs; score MMAs (and the first queries); TMA producer of the rest
 //
 // What bounds it.  Bytes are 644 a token, once for all heads; the MMAs, M = 128 from shared memory, take 41, 49 and 66 clocks for 32, 64 and 128 columns
-// whatever the type's width, 36 of them for a tile up to 32 heads a CTA and 52 with 64.  Measured, the whole call: 64 requests of up to 8192 tokens, 16
-// heads, 44.5 us (this kernel 35; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, 75.9 us (62; 3.35 K clocks a tile, HBM's rate
-// too, and 5 K for each switch of request); 8 of up to 65536, 128 heads, 129 us, in long runs, at the card's power limit, 149 (125; 4.1 K clocks a tile
-// against 2.9 K of MMAs: two tiles are in flight, and a slab's life -- load 1.8 K, scores, softmax 2.4 K, values 1.6 K -- is more than twice that);
-// 250 of up to 600, 64 heads, 67.4 us (48; one or two switches a CTA, 10 K clocks each: 128 KB of accumulator to L2 and a tile without references).
+// whatever the type's width, 36 of them for a tile up to 32 heads a CTA and 52 with 64.  Measured, the whole call replayed (and this kernel under a profiler), scores of
+// deviation about 1: 64 requests of up to 8192 tokens, 16 heads, pages of 64, 42.5 us (35; a tile in 3.5 K clocks, HBM's rate); 200 of about 2000, 32 heads, pages
+// of 128, 76 us (64; HBM's rate too, and 5 K clocks for each switch of request); 8 of up to 65536, 128 heads, pages of 64, 131 us, in long runs, at the
+// card's power limit, 153 (128; 4.2 K clocks a tile against 2.9 K of MMAs: two tiles are in flight, and a slab's life -- load 1.8 K, scores, softmax 2.4 K,
+// values 1.6 K -- is more than twice that); 250 of up to 600, 64 heads, 60 us with pages of 64 and 67 with pages of 16 (48 with pages of 16; one or two switches a CTA,
+// 10 K clocks each: 128 KB of accumulator to L2 and a tile without references; the three kernels' starts overlap).  Pages of 16 tokens are 40 copies a tile for two
+// lanes where pages of 64 are 10: 64 x 8192 64 us, 200 x 2000 106.
+// Scores of deviation 2 and 3, the same four (250 x 600 with pages of 64): 46, 90, 176, 65 and 51, 98, 191, 74: of a softmax group's ten tiles 4 and 7 to
+// 9 find a reference that does not hold, against one (and a piece's first, which has none): two meetings more, the weights a second time, the values of the tile before waited for.
 #pragma once
 #include "armed_ring.cuh"
 #include "attn_decode_sm100.cuh"
@@ -54,9 +58,10 @@ constexpr float kD8Fall = 40.0f;
 // Which: in a piece's first tile, keys of some warps (32 neighbours each) where as many others have nothing near (of a tile with three warps' keys, or two,
 // one other; with one's, every fourth key counts as another's); in a later one, keys that far above the window.  Of each warp kD8Places in a piece at
 // most; where there are more, the tile's largest weight sets the reference as it does otherwise.
-// A tile with some costs about 2 us, meetings and latencies (one request of 511 tokens 16.3 -> 16.8 us, 200 of about 2000, 32 heads, a key each 75.3 -> 80, 250 of up to
-// 600, 64 heads 59 -> 68.5, 64 of up to 8192, 16 heads 42.6 -> 43.3); looking for them 0.4 us a call and 2 % where scores are flat.  (Kept per head instead of for the
-// group's heads together, at the accumulator's end by a walk over their places: 3 to 5 us a tile.  As called functions: 5 % lost where nothing stands apart.)
+// A tile with some costs 2 to 4 us, meetings and latencies (with one in each request: 511 tokens 16.5 -> 17.3 us, 64 of up to 8192, 16 heads 42.2 -> 44.8, 200 of about
+// 2000, 32 heads 75.8 -> 82.5, 250 of up to 600, 64 heads 60 -> 71.5); that they may come costs 0.6 us a call and 2 % where scores are flat, and some 5 to 15 % of scores of
+// deviation 2 and more, whose references move often.  (Kept per head instead of for the group's heads together, at the end by a walk over their places: 3 to 5 us a
+// tile.  As called functions: 5 % lost where nothing stands apart.)
 constexpr int kD8Places = 4;
 constexpr int kD8Looks = 2;                  // tiles of a piece from which keys may be left out
 constexpr int kD8Place = 36;                 // words of a kept key: d of up to 16 heads, its place in the request, 1 / its scale, and m of then
@@ -91,8 +96,8 @@ struct AttnDecode8Smem {
     static constexpr int kSoftWarps = 4 * kGroups;
     static constexpr int kThreads = 32 * (kSoftWarps + 4);
     static constexpr bool kSplit = kHeads <= 32;               // both parts of P as columns
-    // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (saves 4.2 us for 200 requests
-    // of about 2000 tokens, 32 heads; would cost 0.7 at 64 x 8192 with 16 heads and 3.8 at 8 x 65536 with 128)
+    // One copy of the instructions that make P of scores, not two: fewer registers, of which 20 warps have 96 each (saves 1.4 us for 200 requests
+    // of about 2000 tokens, 32 heads, costs 4 for 1024 of up to 300; would cost 0.4 at 64 x 8192 with 16 heads and 1 to 2 at 8 x 65536 with 128)
     static constexpr bool kOneCopy = kHeads == 32;
     static constexpr float kApart = kSplit ? 11.0f : 10.0f;    // how far above the rest of its tile a weight stands that is left out of P
     static constexpr float kDrop = kSplit ? 3.0f : 0.0f;       // P = 2^(d - kDrop): at most 2^8 in e4m3 (hi and 32 times the rest), 2^11 in e5m2 and its rest
@@ -130,8 +135,8 @@ struct AttnDecode8Args {
 
 // Where the line's units lie.  A request with tokens begins with a gap as long as what its switch costs -- queries, a tile without references, the accumulator
 // to drain -- and is then its units: stretches of the line are equal work, not equal units, and one that would begin within a gap begins with the request.
-// (Saves 5.7 us for 250 requests of up to 600 tokens, 64 heads, 2.0 for 200 of about 2000, 32 heads, 1.1 for 64 of up to 8192, 16 heads.  Of 8, 6 and 5
-// units: 1.3, 0.1 and 0.8 less; of 3, 3 and 2: 2.3 more, but 2.4 lost at 8 x 65536 with 128 heads, 0.5 and 0.2 less.)
+// (Saves 13.6 us for 250 requests of up to 600 tokens, 64 heads, 11 for 1024 of up to 300, 32 heads, 7.7 for 130 of up to 900, 128 heads, 1.7 each for 200 of about 2000, 32
+// heads, and 64 of up to 8192, 16 heads, with pages of 64, and costs 0.8 for one of 511.  Gaps of 8, 6 and 5 units, or of 3, 3 and 2, were 0.1 to 2.4 us worse in one or other of these.)
 constexpr int decode8_gap(int heads) { return heads == 64 ? 5 : heads == 32 ? 4 : 3; }
 
 // Walks the tiles of one CTA's stretch of the line.
@@ -1311,8 +1316,8 @@ decode_absorb8_rows_kernel(const __grid_constant__ CUtensorMap tmap_w, const __g
 
 // Joining the pieces and the value dimension for many requests.  (decode_project_kernel keeps a head's weights and goes through its requests sixteen at a
 // time, a chain of loads, sums, stores and MMAs each; two kernels, for the sums and for the product, pass 2 KB a request and head through L2.  250
-// requests of up to 600 tokens, 64 heads, the call replayed: 69.8 us with the first, 66.5 with the two, 55.6 so.  Itself 15.4 us, of which L2 needs some 8 for
-// 52 MB of pieces; the rest are a launch, the weights of the sum and eight steps' latencies.)
+// requests of 1 to 600 tokens, 64 heads, pages of 64, the call replayed: 68.6 us with the first, 55.5 so; the two were 3.3 better than the first.  Itself, alone, 15.4 us, of which L2
+// needs some 8 for 52 MB of pieces; the rest are the weights of the sum, eight steps' latencies, and a launch and W_uv's load, which the call hides.)
 // A CTA has a head and up to 128 requests:
 //     w_p = 2^(m_p - M) / sum_p 2^(m_p - M) l_p,   o[c] = sum_p w_p o_p[c] as bf16(o) and bf16(o - bf16(o)),   out[v] = sum_c W_uv[c, v] (both parts)[c]
 // D[128 requests x 128 values] = the parts (A, K-major) . W_uv (B, MN-major, rows in the pieces' order), 64 latents at a time: sixteen warps sum

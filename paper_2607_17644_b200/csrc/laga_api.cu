@@ -874,9 +874,10 @@ int launch_attn_decode8(const uint8_t* q_rows, const AttnDecode8Args& a, cudaStr
 }
 
 // Requests a CTA of decode8_join_kernel; 0 for decode_project_kernel, which has CTAs for fewer requests and all warps for a request's pieces.  By requests over
-// the CTAs that a head can have: 28 of them (256 requests of 400 to 512 tokens, 16 heads) 37.7 us the call with 64 a CTA, 37.5 with the other kernel;
-// 37 (150 of 100 to 2000, 32 heads) 51.3, 51.1; 44 (400 of 400 to 512, 16 heads) 46.5, 49.0; 50 (200 of 1000 to 2048, 32 heads) 64.6, 69.7, and
-// with 128 a CTA five more; 125 (250 of up to 600, 64 heads) 55.6 with 128, 69.8.
+// the CTAs that a head can have, the call replayed, pages of 64: 28 of them (256 requests of 400 to 512 tokens, 16 heads) 38.3 us with 64 a CTA, 37.8 with the other kernel;
+// 37 (150 of 100 to 2000, 32 heads) 52.8, 53.0; 44 (400 of 400 to 512, 16 heads) 47.2, 49.6; 50 (200 of 1000 to 2048, 32 heads) 67.1, 72.5, and
+// with 128 a CTA 69.6; 125 (250 of 1 to 600, 64 heads) 55.5 with 128, 64.3 with 64, 68.6.  (In one order of the lengths; another
+// moves the last by 4.  Pages of 16 add 12 to each of its three.)
 int decode8_join_rows(int B, int h) {
     const long long ctas_a_head = std::max(1, kDecMaxCtas / h);
     return B <= 40 * ctas_a_head ? 0 : B <= 64 * ctas_a_head ? 64 : 128;
